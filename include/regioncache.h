@@ -489,6 +489,152 @@ rc_status rc_linear(rc_ctx* ctx, const void* x, const void* W, const float* b, f
 rc_status rc_attention(rc_ctx* ctx, const void* Q, int ldq, const void* K, const void* V,
                        int ldkv, int Nq, int Nk, void* O, int ldo, rc_stream stream);
 
+/* ------------------------------------------------------ eight-bit serving */
+
+/* Weights, activations and cached keys / values in eight bits (no counterpart
+ * in the paper; serving plumbing).  A value is an e4m3 code (4 exponent, 3
+ * mantissa bits, no infinity, largest 448) times its block's scale, a power
+ * of two held as one byte: byte b stands for 2^(b - 127), 255 for NaN.  The
+ * scale of a block whose largest magnitude is a is the least 2^e, e >= -127,
+ * with a <= 448 * 2^e; codes are rounded to nearest, ties to even.  A block
+ * that holds a non-finite value has scale 255 and NaN codes (0x7f) throughout,
+ * so everything computed from it is NaN.  (A power of two costs e4m3 no
+ * relative precision within its 2^15 of normal range, a scale can be raised
+ * later without rounding the codes again, and the tensor core applies it.)
+ *
+ * Entry points below take a context for its error word only (rc_sync), keep
+ * no state and no scratch in it, and allocate nothing: calls on different
+ * streams may overlap as long as their buffers do not.  The context's device
+ * must be current (RC_ERR_INVALID_ARG otherwise).  All of them may be
+ * captured into a graph, which keeps the pointers and sizes. */
+#define RC_BF16 0
+#define RC_F32 1
+
+/* A quantised matrix of `rows` x `cols` values, blocks of `group` rows (1 or
+ * 128) by 128 columns.
+ *   codes   u8 [rows][ld], 16-B aligned, ld >= cols a multiple of 16; columns
+ *           cols .. ld - 1 are neither read nor written.
+ *   scales  u8 [ceil(cols / 128)][lds], lds >= ceil(rows / group): the scale
+ *           of (r, c) is scales[c / 128][r / group].
+ * cols is at most RC_FP8_MAX_COLS. */
+#define RC_FP8_MAX_COLS 4194304
+typedef struct rc_fp8 {
+  void* codes;
+  void* scales;
+  int rows, cols, ld, lds, group;
+} rc_fp8;
+
+/* out = x quantised.  x: rows x cols values of `type` (RC_BF16, RC_F32) with
+ * row stride ldx >= cols, aligned to its element size (16-B aligned rows are
+ * read faster).  out->rows = 0 is legal and does nothing.  Errors:
+ * RC_ERR_INVALID_ARG (null, alignment, type, group), RC_ERR_SHAPE. */
+rc_status rc_fp8_quantize(rc_ctx* ctx, const void* x, int ldx, int type, const rc_fp8* out,
+                          rc_stream stream);
+
+/* rc_linear on quantised operands: y = x W^T + b with f32 accumulation.
+ *   x  [rows][k], W [n][k] (x->cols == W->cols), each with either group.
+ *   b  f32 [n] or null.
+ *   y  `type` (RC_BF16, RC_F32) [rows][ldy], ldy >= n, aligned to its element
+ *      size (16-B aligned rows are written faster); columns n .. ldy - 1 are
+ *      not written.
+ * Any rows >= 0, n >= 1, k >= 1.  Results are bit-identical from call to
+ * call.  Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+rc_status rc_fp8_linear(rc_ctx* ctx, const rc_fp8* x, const rc_fp8* W, const float* b, void* y,
+                        int ldy, int type, rc_stream stream);
+
+/* A paged key / value cache in eight bits: blocks of RC_KV8_BLOCK tokens, one
+ * scale for each (block, head) of the keys and of the values.
+ *   k, v              u8 codes [blocks][kv_heads][RC_KV8_BLOCK][head_dim],
+ *                     16-B aligned; head_dim 64, 72 or 128.
+ *   k_scale, v_scale  u8 [blocks][kv_heads].
+ * A new pool is filled with zeros by its owner.  A token's slot is
+ * block * RC_KV8_BLOCK + its place in the block; blocks * RC_KV8_BLOCK must
+ * stay below 2^31. */
+#define RC_KV8_BLOCK 64
+typedef struct rc_kv8 {
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+  int blocks, kv_heads, head_dim;
+} rc_kv8;
+
+/* Block table and slot map of a step, built on the device from the requests'
+ * lengths.  For each of n_requests (1 .. RC_KV8_MAX_REQUESTS) requests r:
+ *   lengths      i32: its tokens once this step's rows are stored.
+ *   counts       i32: its rows of this step (null: lengths, a first fill),
+ *                0 <= counts[r] <= lengths[r].
+ *   table        i32 [n_requests][ld_table], in/out: the blocks of its
+ *                tokens; ceil(lengths[r] / RC_KV8_BLOCK) <= ld_table.
+ *   row_offsets  out, i32 [n_requests + 1]: the rows of all requests one after
+ *                another; request r owns rows row_offsets[r] ..
+ *   slots        out, i32 [n_slots]: the slot of each row; entries behind the
+ *                last row are -1.  n_slots >= the sum of counts.
+ * Without positions (null) the rows are the request's last counts[r] tokens.
+ * Blocks that no earlier token lies in are taken from free_blocks (i32
+ * [n_free], null: 0 .. n_free - 1) in order, request by request, and written
+ * to the table; *used (out, i32) is how many were taken.  With positions (i32
+ * [n_slots], the token of each row, 0 .. lengths[r] - 1: an edit's dirty
+ * tokens) the table is only read and *used is 0.
+ * Device checks (RC_ERR_DEVICE_ASSERT at rc_sync): a request with bad counts
+ * or too long for its table has no rows; a row whose block is missing (the
+ * free blocks have run out, a negative table entry) or whose position is out
+ * of range has slot -1; rows beyond n_slots are dropped.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_KV8_MAX_REQUESTS 4096
+rc_status rc_kv8_tables(rc_ctx* ctx, const int32_t* lengths, const int32_t* counts,
+                        const int32_t* positions, int n_requests, const int32_t* free_blocks,
+                        int n_free, int32_t* table, int ld_table, int32_t* row_offsets,
+                        int32_t* slots, int n_slots, int32_t* used, rc_stream stream);
+
+/* Stores key and value rows into their slots.
+ *   k, v    `type` (RC_BF16, RC_F32) [n][ldkv], head h in columns
+ *           h * head_dim ..; ldkv >= kv_heads * head_dim; aligned to the
+ *           element size (16-B aligned rows are read faster).
+ *   slots   i32 [n]; a negative slot skips its row.  Slots are distinct, and
+ *           the rows of one block stand next to one another (as
+ *           rc_kv8_tables gives them for ascending tokens).
+ *   count   i32 on the device, the rows to store (null: n), 0 .. n.
+ *   mode    RC_KV8_UPDATE: a block's scale is raised when the new rows need
+ *           it (the codes of its other tokens move with it) and never
+ *           lowered.  RC_KV8_APPEND: a block whose first token is among the
+ *           rows starts anew, its scale set by these rows alone and its other
+ *           tokens void; other blocks as in RC_KV8_UPDATE.
+ * Device checks: a slot beyond the pool or a slot twice in a block's rows is
+ * skipped and reported.  Rows of one block in two places of the list are not
+ * detected: their scale may be wrong.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_KV8_UPDATE 0
+#define RC_KV8_APPEND 1
+rc_status rc_kv8_store(rc_ctx* ctx, const rc_kv8* pool, const void* k, const void* v, int ldkv,
+                       int type, const int32_t* slots, int n, const int32_t* count, int mode,
+                       rc_stream stream);
+
+/* rc_attention over the paged eight-bit cache for several requests at once:
+ * for each row i of request r and each of `heads` query heads h,
+ *   O = softmax(q K^T / sqrt(head_dim)) V
+ * over the cached tokens 0 .. lengths[r] - 1 of r's blocks, with key head
+ * h / (heads / kv_heads).  With causal != 0 the rows are the request's last
+ * tokens and row i of n sees tokens 0 .. lengths[r] - n + i only.  A row that
+ * sees no token gives zeros.
+ *   Q            bf16 [q_rows][ldq], O bf16 [q_rows][ldo], 16-B aligned; ldq,
+ *                ldo >= heads * head_dim, multiples of 8.
+ *   row_offsets  i32 [n_requests + 1], as from rc_kv8_tables: request r owns
+ *                rows row_offsets[r] .. row_offsets[r + 1] - 1, at most max_q
+ *                of them.  Rows of no request are left as they were.
+ *   lengths      i32 [n_requests], 0 .. ld_table * RC_KV8_BLOCK.
+ *   table        i32 [n_requests][ld_table].
+ * Keys are exact in the products; softmax weights and the result are rounded
+ * to bf16, sums are f32.  Results are bit-identical from call to call.
+ * Device checks: a request with bad offsets, more than max_q rows or a bad
+ * length is left out; a table entry outside the pool hides its tokens.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE (heads not a multiple of kv_heads,
+ * heads / kv_heads > 16). */
+rc_status rc_kv8_attention(rc_ctx* ctx, const rc_kv8* pool, const void* Q, int ldq, int q_rows,
+                           const int32_t* row_offsets, const int32_t* lengths, int n_requests,
+                           int max_q, const int32_t* table, int ld_table, int heads, int causal,
+                           void* O, int ldo, rc_stream stream);
+
 /* Waits for `stream`, then reports (and clears) the context's device error
  * word: RC_ERR_DEVICE_ASSERT if a kernel met a bad index or count,
  * RC_ERR_TIMEOUT if a bounded wait gave up, RC_ERR_CUDA on a CUDA error. */

@@ -1,0 +1,106 @@
+// Eight-bit values: e4m3 codes with a power-of-two scale byte (see
+// rc_fp8 / rc_kv8 in include/regioncache.h).
+#pragma once
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace rc {
+
+// The scale byte of a block whose largest magnitude has the f32 bits `a`
+// (sign cleared): the least e >= -127 with a <= 448 2^e = 1.75 2^(e + 8), plus
+// 127.  Magnitudes compare like their bits, NaN above infinity, so an integer
+// maximum over a block keeps non-finite values.
+__device__ __forceinline__ int scale_byte(uint32_t a) {
+  if (a >= 0x7f800000u) return 255;
+  const int e = int(a >> 23) - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e < 0 ? 0 : e;
+}
+// 2^(127 - b) in f32, NaN for 255 (b <= 247 otherwise: scale_byte of FLT_MAX).
+__device__ __forceinline__ float scale_inverse(int b) {
+  return __uint_as_float(b == 255 ? 0x7fffffffu : uint32_t(254 - b) << 23);
+}
+// 2^(b - 127) in f32, NaN for 255.
+__device__ __forceinline__ float scale_value(int b) {
+  return __uint_as_float(b == 255 ? 0x7fffffffu : b == 0 ? 0x400000u : uint32_t(b) << 23);
+}
+// Two values as e4m3 codes (nearest, ties to even; `lo` in the low byte).
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Two codes as f16 (exact).
+__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(uint16_t(codes)));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3x2_f32(uint32_t codes) {
+  const uint32_t h = e4m3x2_f16x2(codes);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Eight consecutive source values as f32 bits' magnitudes' maximum and as
+// eight codes: of bf16 (one 16-byte load) or f32 (two).
+template <class T>
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+  uint4 u;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    u = *reinterpret_cast<const uint4*>(p);
+  }
+  // values [0, n) of an unaligned or ragged run; the rest are zero
+  __device__ __forceinline__ void load_some(const __nv_bfloat16* p, int n) {
+    const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (2 * i < n ? uint32_t(s[2 * i]) : 0u) |
+             (2 * i + 1 < n ? uint32_t(s[2 * i + 1]) << 16 : 0u);
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ void zero() { u = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ uint32_t top() const {  // f32 bits of the largest magnitude
+    const uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu),
+                                __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+    const uint32_t a = m << 16, b = m & 0xffff0000u;
+    return a > b ? a : b;
+  }
+  __device__ __forceinline__ uint32_t four(uint32_t a, uint32_t b, float inv) const {
+    return e4m3x2(__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv) |
+           e4m3x2(__uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv) << 16;
+  }
+  __device__ __forceinline__ uint2 codes(float inv) const {
+    return make_uint2(four(u.x, u.y, inv), four(u.z, u.w, inv));
+  }
+};
+template <>
+struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + 4);
+  }
+  __device__ __forceinline__ void load_some(const float* p, int n) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+    a = make_float4(v[0], v[1], v[2], v[3]);
+    b = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  static __device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+  __device__ __forceinline__ uint32_t top() const {
+    return max(max(max(mag(a.x), mag(a.y)), max(mag(a.z), mag(a.w))),
+               max(max(mag(b.x), mag(b.y)), max(mag(b.z), mag(b.w))));
+  }
+  __device__ __forceinline__ uint2 codes(float inv) const {
+    return make_uint2(e4m3x2(a.x * inv, a.y * inv) | e4m3x2(a.z * inv, a.w * inv) << 16,
+                      e4m3x2(b.x * inv, b.y * inv) | e4m3x2(b.z * inv, b.w * inv) << 16);
+  }
+};
+
+}  // namespace rc

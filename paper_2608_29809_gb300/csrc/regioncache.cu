@@ -155,6 +155,8 @@ int ctx_timesteps(const ::rc_ctx* c) { return c->T; }
 const ::rc_ctx* cache_context(const ::rc_cache* k) { return k->ctx; }
 int cache_sessions(const ::rc_cache* k) { return k->sessions; }
 bool cache_host_tier(const ::rc_cache* k) { return k->host_tier; }
+unsigned* ctx_error_word(const ::rc_ctx* c) { return c->err; }
+int ctx_device(const ::rc_ctx* c) { return c->device; }
 }  // namespace rc
 
 namespace {

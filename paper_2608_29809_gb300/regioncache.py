@@ -59,6 +59,23 @@ class rc_batch_item(C.Structure):
                 ("dirty_idx", C.c_void_p), ("D", C.c_int), ("dirty_count", C.c_void_p)]
 
 
+class rc_fp8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)] + [
+        (n, C.c_int) for n in ("rows", "cols", "ld", "lds", "group")]
+
+
+class rc_kv8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, C.c_int) for n in ("blocks", "kv_heads", "head_dim")]
+
+
+RC_BF16, RC_F32 = header_define("RC_BF16"), header_define("RC_F32")
+DTYPES = {torch.bfloat16: RC_BF16, torch.float32: RC_F32}
+RC_KV8_BLOCK = header_define("RC_KV8_BLOCK")
+RC_KV8_MAX_REQUESTS = header_define("RC_KV8_MAX_REQUESTS")
+RC_KV8_UPDATE, RC_KV8_APPEND = header_define("RC_KV8_UPDATE"), header_define("RC_KV8_APPEND")
+
+
 LAYER_FIELDS = ("W_qkv", "b_qkv", "W_o", "b_o", "W_xq", "b_xq", "W_xkv", "b_xkv", "W_xo",
                 "b_xo", "W_1", "b_1", "W_2", "b_2", "table")
 GLOBAL_FIELDS = ("W_e", "b_e", "pos", "W_t1", "b_t1", "W_t2", "b_t2", "W_tb", "b_tb", "table_f",
@@ -117,6 +134,12 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "rc_step_dense": (I, [P, P, I, P, I, P]),
         "rc_linear": (I, [P, P, P, P, P, I, I, I, P]),
         "rc_attention": (I, [P, P, I, P, P, I, I, I, P, I, P]),
+        "rc_fp8_quantize": (I, [P, P, I, I, C.POINTER(rc_fp8), P]),
+        "rc_fp8_linear": (I, [P, C.POINTER(rc_fp8), C.POINTER(rc_fp8), P, P, I, I, P]),
+        "rc_kv8_tables": (I, [P, P, P, P, I, P, I, P, I, P, P, I, P, P]),
+        "rc_kv8_store": (I, [P, C.POINTER(rc_kv8), P, P, I, I, P, I, P, I, P]),
+        "rc_kv8_attention": (I, [P, C.POINTER(rc_kv8), P, I, I, P, P, I, I, P, I, I, I, P, I,
+                                 P]),
         "rc_sync": (I, [P, P]),
         "rc_probe_enable": (I, [P, I, I]),
         "rc_probe_read": (I, [P, C.POINTER(C.c_double), C.POINTER(I)]),
@@ -369,6 +392,38 @@ def rc_attention(ctx, Q, ldq, K, V, ldkv, Nq, Nk, O, ldo, stream=None):
                              _stream(stream)))
 
 
+def rc_fp8_quantize(ctx, x, ldx, type, out, stream=None):
+    """out: an Fp8Matrix (or rc_fp8)."""
+    _check(_lib.rc_fp8_quantize(ctx, _ptr(x), ldx, type, out, _stream(stream)))
+
+
+def rc_fp8_linear(ctx, x, W, b, y, ldy, type, stream=None):
+    """x, W: Fp8Matrix (or rc_fp8)."""
+    _check(_lib.rc_fp8_linear(ctx, x, W, _ptr(b), _ptr(y), ldy, type, _stream(stream)))
+
+
+def rc_kv8_tables(ctx, lengths, counts, positions, n_requests, free_blocks, n_free, table,
+                  ld_table, row_offsets, slots, n_slots, used, stream=None):
+    _check(_lib.rc_kv8_tables(ctx, _ptr(lengths), _ptr(counts), _ptr(positions), n_requests,
+                              _ptr(free_blocks), n_free, _ptr(table), ld_table,
+                              _ptr(row_offsets), _ptr(slots), n_slots, _ptr(used),
+                              _stream(stream)))
+
+
+def rc_kv8_store(ctx, pool, k, v, ldkv, type, slots, n, count, mode, stream=None):
+    """pool: a Kv8Pool (or rc_kv8)."""
+    _check(_lib.rc_kv8_store(ctx, pool, _ptr(k), _ptr(v), ldkv, type, _ptr(slots), n,
+                             _ptr(count), mode, _stream(stream)))
+
+
+def rc_kv8_attention(ctx, pool, Q, ldq, q_rows, row_offsets, lengths, n_requests, max_q, table,
+                     ld_table, heads, causal, O, ldo, stream=None):
+    """pool: a Kv8Pool (or rc_kv8)."""
+    _check(_lib.rc_kv8_attention(ctx, pool, _ptr(Q), ldq, q_rows, _ptr(row_offsets),
+                                 _ptr(lengths), n_requests, max_q, _ptr(table), ld_table, heads,
+                                 1 if causal else 0, _ptr(O), ldo, _stream(stream)))
+
+
 def rc_selftest_wait(ctx, timeout_us, set_flag, stream=None):
     _check(_lib.rc_selftest_wait(ctx, timeout_us, 1 if set_flag else 0, _stream(stream)))
 
@@ -414,6 +469,74 @@ def rc_last_error() -> str:
 def dims_struct(d, max_batch: int = 1) -> rc_dims:
     return rc_dims(d.hidden, d.heads, d.mlp, d.layers, d.grid_h, d.grid_w, d.patch, d.in_ch,
                    d.out_ch, d.text_len, d.timesteps, d.freq_dim, max_batch)
+
+
+class Fp8Matrix:
+    """The device buffers of an rc_fp8 and the structure that names them (made
+    once: it is what the entry points take).  codes u8 [rows][ld], scales u8
+    [ceil(cols / 128)][ceil(rows / group)]."""
+
+    def __init__(self, rows, cols, group=1, device="cuda"):
+        self._hold(torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.uint8, device=device),
+                   torch.zeros(-(-cols // 128), -(-rows // group), dtype=torch.uint8,
+                               device=device), cols, group)
+
+    def _hold(self, codes, scales, cols, group):
+        for t, n in ((codes, codes.shape[0]), (scales, scales.shape[0])):
+            if t.dtype != torch.uint8 or t.dim() != 2 or (n and t.stride(1) != 1):
+                raise ValueError("codes and scales are uint8 matrices with rows in one piece")
+        self.codes, self.scales = codes, scales
+        # (a single row's stride says nothing about the next one)
+        ld = codes.stride(0) if codes.shape[0] > 1 else max(codes.stride(0), codes.shape[1])
+        lds = scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), scales.shape[1])
+        self.c = rc_fp8(_ptr(codes), _ptr(scales), codes.shape[0], cols, ld, lds, group)
+        self._as_parameter_ = C.pointer(self.c)
+
+    @classmethod
+    def of(cls, codes, scales, cols, group):
+        """The matrix of `cols` columns that these tensors hold."""
+        m = cls.__new__(cls)
+        m._hold(codes, scales, cols, group)
+        return m
+
+    def values(self):
+        """What the codes stand for, f32 [rows][cols]."""
+        b = self.scales.int()
+        s = torch.where(b > 0, b << 23, 0x400000).view(torch.float32)
+        s = torch.where(b == 255, float("nan"), s).t()
+        s = s.repeat_interleave(self.c.group, 0)[:self.c.rows].repeat_interleave(128, 1)
+        return self.codes[:, :self.c.cols].view(torch.float8_e4m3fn).float() * \
+            s[:, :self.c.cols]
+
+
+class Kv8Pool:
+    """The device buffers of an rc_kv8 and the structure that names them.  k, v
+    u8 [blocks][kv_heads][RC_KV8_BLOCK][head_dim], k_scale, v_scale u8
+    [blocks][kv_heads], all zero at first."""
+
+    def __init__(self, blocks, kv_heads, head_dim, device="cuda"):
+        shape = (blocks, kv_heads, RC_KV8_BLOCK, head_dim)
+        self._hold(*[torch.zeros(s, dtype=torch.uint8, device=device)
+                     for s in (shape, shape, shape[:2], shape[:2])])
+
+    def _hold(self, k, v, k_scale, v_scale):
+        for t in (k, v, k_scale, v_scale):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or \
+                    t.shape != (k.shape if t is k or t is v else k.shape[:2]):
+                raise ValueError("codes and scales are contiguous uint8 tensors of one pool")
+        if k.dim() != 4 or k.shape[2] != RC_KV8_BLOCK:
+            raise ValueError(f"codes are [blocks][kv_heads][{RC_KV8_BLOCK}][head_dim]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = rc_kv8(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), k.shape[0], k.shape[1],
+                        k.shape[3])
+        self._as_parameter_ = C.pointer(self.c)
+
+    @classmethod
+    def of(cls, k, v, k_scale, v_scale):
+        """The pool that these tensors hold."""
+        p = cls.__new__(cls)
+        p._hold(k, v, k_scale, v_scale)
+        return p
 
 
 class Model:
