@@ -126,7 +126,7 @@ rc_status rc_fp8_linear(rc_ctx* c, const rc_fp8* x, const rc_fp8* W, const float
     return fail(RC_ERR_INVALID_ARG, "%s: y or b is not aligned to its type", fn);
   RC_CHECK(check_device(c, fn));
   return launched(rc::launch_fp8_linear(mx, mw, b, y, ldy, type == RC_F32,
-                                        static_cast<cudaStream_t>(stream)), fn);
+                                        rc::ctx_error_word(c), static_cast<cudaStream_t>(stream)), fn);
 }
 
 rc_status rc_kv8_tables(rc_ctx* c, const int32_t* lengths, const int32_t* counts,

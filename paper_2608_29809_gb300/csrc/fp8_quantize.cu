@@ -1,4 +1,4 @@
-// Quantised matrices (rc_fp8): the quantiser and the product y = x W^T + b.
+// Quantised matrices (rc_fp8): the quantiser.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "kernels.h"
@@ -108,51 +108,6 @@ cudaError_t quantize(const T* x, int ldx, const Fp8Mat& out, cudaStream_t st) {
                   ldx, out.rows, out.cols, out.codes, out.ld, out.scales, out.lds);
 }
 
-// ---------------------------------------------------------------- product
-// 64 x 64 outputs a CTA, 4 x 4 a thread, both operands scaled to f32 in
-// shared memory 32 columns at a time.
-template <class T>
-__global__ void __launch_bounds__(256)
-linear_kernel(const __grid_constant__ Fp8Mat x, const __grid_constant__ Fp8Mat w,
-              const float* __restrict__ bias, T* __restrict__ y, int ldy) {
-  pdl_wait();
-  pdl_trigger();
-  __shared__ float sx[32][65], sw[32][65];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int r0 = blockIdx.x * 64, n0 = blockIdx.y * 64;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < x.cols; k0 += 32) {
-    for (int i = threadIdx.x; i < 64 * 32; i += 256) {
-      const int row = i >> 5, c = k0 + (i & 31);
-      float a = 0.f, b = 0.f;
-      if (c < x.cols && r0 + row < x.rows)
-        a = e4m3x2_f32(x.codes[(long long)(r0 + row) * x.ld + c]).x *
-            scale_value(x.scales[(long long)(c / GROUP) * x.lds + (r0 + row) / x.group]);
-      if (c < x.cols && n0 + row < w.rows)
-        b = e4m3x2_f32(w.codes[(long long)(n0 + row) * w.ld + c]).x *
-            scale_value(w.scales[(long long)(c / GROUP) * w.lds + (n0 + row) / w.group]);
-      sx[i & 31][row] = a;
-      sw[i & 31][row] = b;
-    }
-    __syncthreads();
-#pragma unroll 8
-    for (int c = 0; c < 32; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += sx[c][ty + 16 * i] * sw[c][tx + 16 * j];
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = r0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (r < x.rows && n < w.rows)
-        y[(long long)r * ldy + n] = T(acc[i][j] + (bias ? bias[n] : 0.f));
-    }
-}
-
 }  // namespace
 
 cudaError_t launch_fp8_quantize(const void* x, int ldx, bool f32, const Fp8Mat& out,
@@ -165,16 +120,6 @@ cudaError_t launch_fp8_quantize(const void* x, int ldx, bool f32, const Fp8Mat& 
   }
   const bf16* p = static_cast<const bf16*>(x);
   return wide ? quantize<bf16, true>(p, ldx, out, st) : quantize<bf16, false>(p, ldx, out, st);
-}
-
-cudaError_t launch_fp8_linear(const Fp8Mat& x, const Fp8Mat& w, const float* b, void* y, int ldy,
-                              bool f32, cudaStream_t st) {
-  const dim3 grid(unsigned((x.rows + 63) / 64), unsigned((w.rows + 63) / 64));
-  count_launches(1);
-  if (f32)
-    return launch_k(linear_kernel<float>, grid, dim3(256), 0, st, x, w, b, static_cast<float*>(y),
-                    ldy);
-  return launch_k(linear_kernel<bf16>, grid, dim3(256), 0, st, x, w, b, static_cast<bf16*>(y), ldy);
 }
 
 }  // namespace rc

@@ -248,7 +248,7 @@ cudaError_t launch_fp8_quantize(const void* x, int ldx, bool f32, const Fp8Mat& 
                                 cudaStream_t st);
 // y = x w^T + b, y f32 or bf16 [x.rows][ldy].
 cudaError_t launch_fp8_linear(const Fp8Mat& x, const Fp8Mat& w, const float* b, void* y, int ldy,
-                              bool f32, cudaStream_t st);
+                              bool f32, unsigned* err, cudaStream_t st);
 
 // Paged eight-bit cache (rc_kv8): side 0 the keys, 1 the values.
 constexpr int KV8_BLOCK = 64;

@@ -43,4 +43,20 @@ inline cudaError_t tma_map(const __nv_bfloat16* p, int rank, const cuuint64_t* d
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// Bytes [rows][cols], rows ld bytes apart (a multiple of 16); boxes of 128
+// bytes x box_rows with the 128-byte swizzle; reads outside give zero.
+inline cudaError_t tma_map_bytes(const uint8_t* p, int rows, int cols, int ld, int box_rows,
+                                 CUtensorMap* out) {
+  auto fn = tma_encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {cuuint64_t(ld)};
+  const cuuint32_t box[2] = {128, cuuint32_t(box_rows)}, es[2] = {1, 1};
+  const CUresult r =
+      fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, box, es,
+         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 }  // namespace rc
