@@ -6,11 +6,13 @@
 //
 // Persistent CTAs of 16 warps: warp 0 loads x by TMA, warp 2 W (128 columns =
 // 128 bytes a row, 128-byte swizzle; what lies outside the matrix reads as
-// zero), warp 1 issues the MMAs, warps 4..7 put the scale bytes of every
-// 128-column block into tensor memory (one word of four equal bytes a row,
-// in each of the four lane partitions), warps 8..15 drain the accumulator.
-// Two accumulators of up to 192 columns and a ring of scale words beside
-// them fill the 512 columns of tensor memory.
+// zero), warp 1 issues the MMAs, warps 4..7 put the scale bytes into tensor
+// memory, warps 8..15 drain the accumulator.  A row's word there holds the
+// bytes of four consecutive blocks, of which an MMA names one, so a word is
+// written (in each of the four lane partitions) once for 512 columns; with a
+// word and a handshake for every block the scale warps held up the MMAs
+// (16384 x 1152 x 4608: 301 us).  Two accumulators of up to 224 columns and
+// a ring of scale words fill the 512 columns of tensor memory.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "kernels.h"
@@ -27,20 +29,29 @@ constexpr int BM = 128, BK = 128;
 constexpr int THREADS = 512;
 constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 8;
 constexpr int STAGE_A = BM * BK;
-constexpr int RING_BYTES = 168 * 1024, MAX_STAGES = 7;
+constexpr int RING_BYTES = 188 * 1024, MAX_STAGES = 7;
 constexpr int STAGING_WARP = 32 * 128;  // 32 rows of 32 f32 per epilogue warp
-constexpr size_t SMEM_BYTES = size_t(RING_BYTES) + EPI_WARPS * STAGING_WARP + 1024 + 256;
-// tensor memory: accumulators at 0 and MAX_BN, then the scale words of the
-// ring's stages (4 columns for x, up to 8 for W)
-constexpr int MAX_BN = 192, SCALE_COL = 2 * MAX_BN, SCALE_STEP = 12, TMEM_COLS = 512;
-static_assert(SCALE_COL + MAX_STAGES * SCALE_STEP <= TMEM_COLS, "tensor memory");
+// tensor memory: accumulators at 0 and MAX_BN, then a ring of scale words
+// (4 columns for x, up to 7 for W), each for WORD_KB blocks
+constexpr int MAX_BN = 224, SCALE_COL = 2 * MAX_BN, SCALE_STEP = 12, TMEM_COLS = 512;
+constexpr int SCALES = 5, WORD_KB = 4;
+// the scale words of a batch of blocks in shared memory: 128 rows of x, then
+// up to 224 of W
+constexpr int SCALE_BATCH = 16, SCALE_ROWS = 128 + MAX_BN;
+constexpr int SCALE_BYTES = SCALE_BATCH / WORD_KB * SCALE_ROWS * 4;
+constexpr size_t SMEM_BYTES =
+    size_t(RING_BYTES) + EPI_WARPS * STAGING_WARP + SCALE_BYTES + 1024 + 256;
+static_assert(SCALE_COL + SCALES * SCALE_STEP <= TMEM_COLS, "tensor memory");
 // Instruction descriptor of kind::mxf8f6f4: e4m3 x e4m3 into f32, both
-// K-major, power-of-two scale bytes, byte 0 of each word; N >> 3 at bit 17,
-// M >> 7 at bit 27.
+// K-major, power-of-two scale bytes; N >> 3 at bit 17, M >> 7 at bit 27, the
+// byte of each scale word that the MMA takes at bits 4 (W) and 29 (x).
 constexpr uint32_t IDESC = 1u << 23;
 
 struct Plan {
   int bn, stages, mt, nt, tiles, kb;
+  int n_first;  // neighbouring tiles share rows of x (otherwise of W)
+  __device__ __forceinline__ int m(int t) const { return n_first ? t / nt : t % mt; }
+  __device__ __forceinline__ int n(int t) const { return n_first ? t % nt : t / mt; }
 };
 template <bool PAIR>
 __host__ __device__ constexpr int stage_bytes(int bn) {
@@ -112,6 +123,9 @@ __device__ __forceinline__ void write_chunk(const Out<T>& o, uint8_t* stg, int l
   __syncwarp();  // the staging area is rewritten by the next chunk
 }
 
+// Named barrier of the four scale warps.
+__device__ __forceinline__ void scale_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
 // PAIR: clusters of two CTAs share each MMA (M = 256): a CTA loads its own 128
 // rows of x and half of the W tile.
 template <class T, bool PAIR>
@@ -123,12 +137,13 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   uint8_t* stg = smem + RING_BYTES;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(stg + EPI_WARPS * STAGING_WARP);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * MAX_STAGES + 4);
+  uint32_t* sw_words = reinterpret_cast<uint32_t*>(stg + EPI_WARPS * STAGING_WARP);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(stg + EPI_WARPS * STAGING_WARP + SCALE_BYTES);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 2 * SCALES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const uint32_t full0 = saddr(bars), empty0 = full0 + 8 * MAX_STAGES;
-  const uint32_t sfull0 = empty0 + 8 * MAX_STAGES, tfull0 = sfull0 + 8 * MAX_STAGES;
-  const uint32_t tempty0 = tfull0 + 16;
+  const uint32_t sfull0 = empty0 + 8 * MAX_STAGES, sempty0 = sfull0 + 8 * SCALES;
+  const uint32_t tfull0 = sempty0 + 8 * SCALES, tempty0 = tfull0 + 16;
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0;
@@ -137,7 +152,10 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
     for (int s = 0; s < MAX_STAGES; ++s) {
       mbar_init(full0 + 8 * s, PAIR ? 1 : 2);  // (x's and W's loads)
       mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int s = 0; s < SCALES; ++s) {
       mbar_init(sfull0 + 8 * s, 4 * CTAS);
+      mbar_init(sempty0 + 8 * s, 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(tfull0 + 8 * a, 1);
@@ -169,7 +187,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       int stage = 0;
       uint32_t phase = 0;
       for (int t = pos; ok && t < pl.tiles; t += G) {
-        const int m = (t % pl.mt) * CTAS + int(rank), nn = t / pl.mt;
+        const int m = pl.m(t) * CTAS + int(rank), nn = pl.n(t);
         for (int kb = 0; kb < KB; ++kb) {
           if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
           const uint32_t st = saddr(smem + stage * STAGE), fb = full0 + 8 * stage;
@@ -195,29 +213,40 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       const uint32_t idesc =
           IDESC | (uint32_t(BN >> 3) << 17) | (uint32_t(PAIR ? 2 : 1) << 27);
       const uint64_t da = sw128_desc(saddr(smem)), db = sw128_desc(saddr(smem + STAGE_A));
-      int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
+      int stage = 0, acc = 0, sc = 0;
+      uint32_t phase = 0, acc_phase = 0, sc_phase = 0;
+      bool ready = false;  // the current stage was seen full already
       for (int t = pos; ok && t < pl.tiles; t += G) {
         if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
         const uint32_t d = tmem + uint32_t(acc * MAX_BN);
         for (int kb = 0; kb < KB; ++kb) {
-          if (!mbar_wait(full0 + 8 * stage, phase, abort_flag) ||
-              !mbar_wait(sfull0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
-          tc_fence_after();
+          const int byte = kb % WORD_KB;
+          if (byte == 0 && !mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
+          if (!ready && !mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
           const uint64_t so = uint64_t((stage * STAGE) >> 4);
-          const uint32_t sa = tmem + uint32_t(SCALE_COL + stage * SCALE_STEP), sb = sa + 4;
+          const uint32_t eb = empty0 + 8 * stage;
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          // (the next stage's test runs beside this one's MMAs)
+          ready = mbar_test(full0 + 8 * stage, phase);
+          tc_fence_after();
+          const uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_STEP), sb = sa + 4;
+          const uint32_t id = idesc | uint32_t(byte) << 4 | uint32_t(byte) << 29;
 #pragma unroll
           for (int kk = 0; kk < BK / 32; ++kk) {
             if (PAIR)
-              umma_e4m3_scaled_pair(d, da + so + 2 * kk, db + so + 2 * kk, idesc, sa, sb,
+              umma_e4m3_scaled_pair(d, da + so + 2 * kk, db + so + 2 * kk, id, sa, sb,
                                     (kb | kk) ? 1u : 0u);
             else
-              umma_e4m3_scaled(d, da + so + 2 * kk, db + so + 2 * kk, idesc, sa, sb,
+              umma_e4m3_scaled(d, da + so + 2 * kk, db + so + 2 * kk, id, sa, sb,
                                (kb | kk) ? 1u : 0u);
           }
-          if (PAIR) umma_commit_pair(empty0 + 8 * stage);
-          else umma_commit(empty0 + 8 * stage);
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          if (PAIR) umma_commit_pair(eb);
+          else umma_commit(eb);
+          if (byte == WORD_KB - 1 || kb == KB - 1) {
+            if (PAIR) umma_commit_pair(sempty0 + 8 * sc);
+            else umma_commit(sempty0 + 8 * sc);
+            if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
+          }
         }
         if (!ok) break;
         if (PAIR) umma_commit_pair(tfull0 + 8 * acc);
@@ -227,54 +256,74 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
     }
   } else if (warp >= SCALE_WARP && warp < EPI_WARP) {
     // -------------------------------------------------------- scale words
-    // Four blocks' bytes are loaded at a time (a load takes longer than the
-    // MMAs of a block).
-    constexpr int AHEAD = 4;
     pdl_wait();
-    const int sx = x.group == 1 ? 0 : 7, sw = w.group == 1 ? 0 : 7, words = BN / 32;
+    const int sx = x.group == 1 ? 0 : 7, sw = w.group == 1 ? 0 : 7;
     const uint32_t part = uint32_t((warp & 3) * 32) << 16;
-    int stage = 0;
-    uint32_t phase = 0;
-    for (int t = pos; ok && t < pl.tiles; t += G) {
-      const int m = (t % pl.mt) * CTAS + int(rank), nn = t / pl.mt;
-      for (int kb0 = 0; ok && kb0 < KB; kb0 += AHEAD) {
-        uint32_t a[AHEAD][4], b[AHEAD][6];
+    // A batch is the bytes of SCALE_BATCH blocks: each of the 128 threads loads
+    // those of one row of x and of two of W, without a branch and from clamped
+    // places, so that the loads are under way together (beside the operand
+    // stream one round trip takes longer than the MMAs of four blocks), packs
+    // them into words and leaves the words in shared memory, where every warp
+    // takes what it stores.  The next batch's loads run meanwhile.  Rows and
+    // blocks that there are none of multiply zeros and take the scale 1.
+    const int tid = int(threadIdx.x) - SCALE_WARP * 32;
+    uint32_t next[3][SCALE_BATCH / WORD_KB];
+    const auto load = [&](int t, int kb) {
+      const int m = pl.m(t) * CTAS + int(rank), nn = pl.n(t);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const bool in = kb0 + u < KB;
-          const uint8_t* px = x.scales + (long long)(kb0 + u) * x.lds;
-          const uint8_t* pw = w.scales + (long long)(kb0 + u) * w.lds;
+      for (int i = 0; i < 3; ++i) {
+        const int r = i == 0 ? m * BM + tid : nn * BN + (i - 1) * 128 + tid;
+        const int rows = i == 0 ? x.rows : w.rows;
+        const uint8_t* p = i == 0 ? x.scales + (min(r, rows - 1) >> sx)
+                                  : w.scales + (min(r, rows - 1) >> sw);
+        const long long step = i == 0 ? x.lds : w.lds;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = m * BM + 32 * i + lane;
-            a[u][i] = in && r < x.rows ? px[r >> sx] : 127;
-          }
+        for (int g = 0; g < SCALE_BATCH / WORD_KB; ++g) {
+          uint32_t b[WORD_KB];
 #pragma unroll
-          for (int i = 0; i < 6; ++i) {
-            const int r = nn * BN + 32 * i + lane;
-            b[u][i] = in && i < words && r < w.rows ? pw[r >> sw] : 127;
-          }
+          for (int u = 0; u < WORD_KB; ++u) b[u] = p[min(kb + g * WORD_KB + u, KB - 1) * step];
+          const uint32_t word = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+          next[i][g] = r < rows ? word : 0x7f7f7f7fu;
         }
+      }
+    };
+    int sc = 0, t = pos, kb = 0;
+    uint32_t sc_phase = 0;
+    if (t < pl.tiles) load(t, kb);
+    while (t < pl.tiles) {
+      scale_sync();  // (the batch before has been taken)
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          if (kb0 + u >= KB) break;
-          if (!mbar_sleep_warp(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int g = 0; g < SCALE_BATCH / WORD_KB; ++g)
+          if (i < 2 || tid < SCALE_ROWS - 256) sw_words[g * SCALE_ROWS + i * 128 + tid] = next[i][g];
+      scale_sync();
+      const int groups = (min(KB - kb, SCALE_BATCH) + WORD_KB - 1) / WORD_KB;
+      kb += SCALE_BATCH;
+      if (kb >= KB) { kb = 0; t += G; }
+      if (t < pl.tiles) load(t, kb);
+      for (int g = 0; g < groups; ++g) {
+        uint32_t v[12];
+#pragma unroll
+        for (int i = 0; i < 11; ++i) v[i] = sw_words[g * SCALE_ROWS + 32 * i + lane];
+        v[11] = 0x7f7f7f7fu;
+        if (ok) ok = mbar_wait(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
+        // (after a failed wait the warp goes on to the barriers, without work)
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok) {
           tc_fence_after();
-          const uint32_t ta = tmem + uint32_t(SCALE_COL + stage * SCALE_STEP) + part;
-          constexpr uint32_t R = 0x01010101u;
-          tmem_st4(ta, a[u][0] * R, a[u][1] * R, a[u][2] * R, a[u][3] * R);
-          tmem_st2(ta + 4, b[u][0] * R, b[u][1] * R);
-          if (words > 2) tmem_st2(ta + 6, b[u][2] * R, b[u][3] * R);
-          if (words > 4) tmem_st2(ta + 8, b[u][4] * R, b[u][5] * R);
+          const uint32_t ta = tmem + uint32_t(SCALE_COL + sc * SCALE_STEP) + part;
+          tmem_st4(ta, v[0], v[1], v[2], v[3]);
+          tmem_st8(ta + 4, v + 4);
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
-            if (PAIR) mbar_arrive_cluster(mapa_shared(sfull0 + 8 * stage, 0));
-            else mbar_arrive(sfull0 + 8 * stage);
+            if (PAIR) mbar_arrive_cluster(mapa_shared(sfull0 + 8 * sc, 0));
+            else mbar_arrive(sfull0 + 8 * sc);
           }
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
+        if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
       }
     }
   } else if (warp >= EPI_WARP) {
@@ -285,7 +334,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = pos; t < pl.tiles; t += G) {
-      const int m = (t % pl.mt) * CTAS + int(rank), nn = t / pl.mt;
+      const int m = pl.m(t) * CTAS + int(rank), nn = pl.n(t);
       if (!mbar_sleep_warp(tfull0 + 8 * acc, acc_phase, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const uint32_t tb = tmem + uint32_t(acc * MAX_BN) + (uint32_t(sp * 32) << 16);
@@ -337,6 +386,7 @@ cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, cudaSt
   pl.mt = int((x.rows + (long long)rows - 1) / rows);
   pl.nt = int((w.rows + (long long)bn - 1) / bn);
   pl.kb = (x.cols + BK - 1) / BK;
+  pl.n_first = w.rows < x.rows;
   const long long tiles = (long long)pl.mt * pl.nt;
   if (tiles > 0x7fffffff - SMS) return cudaErrorInvalidValue;
   pl.tiles = int(tiles);

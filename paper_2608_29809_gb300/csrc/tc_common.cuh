@@ -206,8 +206,9 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
       : "memory");
 }
 // D (+)= A B of e4m3 tiles (K-major, 32 columns), each row's products times
-// 2^(scale byte - 127) of A's and of B's row: scale bytes in tensor memory,
-// row i in lane i % 32 (of every 32-lane partition), column i / 32, low byte.
+// 2^(scale byte - 127) of A's and of B's row: scale words in tensor memory,
+// row i in lane i % 32 (of every 32-lane partition), column i / 32; the
+// instruction descriptor names the byte.
 __device__ __forceinline__ void umma_e4m3_scaled(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc,
                                                  uint32_t idesc, uint32_t tmem_sa,
                                                  uint32_t tmem_sb, uint32_t accumulate) {
@@ -339,10 +340,6 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b,
                                          uint32_t d) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(a),
                "r"(b), "r"(c), "r"(d)
-               : "memory");
-}
-__device__ __forceinline__ void tmem_st2(uint32_t taddr, uint32_t a, uint32_t b) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1,%2};" ::"r"(taddr), "r"(a), "r"(b)
                : "memory");
 }
 // One f32 column of this thread's TMEM lane (no wait).
