@@ -8,11 +8,12 @@
 // 128 bytes a row, 128-byte swizzle; what lies outside the matrix reads as
 // zero), warp 1 issues the MMAs, warps 4..7 put the scale bytes into tensor
 // memory, warps 8..15 drain the accumulator.  A row's word there holds the
-// bytes of four consecutive blocks, of which an MMA names one, so a word is
-// written (in each of the four lane partitions) once for 512 columns; with a
-// word and a handshake for every block the scale warps held up the MMAs
-// (16384 x 1152 x 4608: 301 us).  Two accumulators of up to 224 columns and
-// a ring of scale words fill the 512 columns of tensor memory.
+// bytes of four consecutive blocks, of which an MMA names one; the words of
+// sixteen blocks (2048 columns) are stored and handed over together.  The
+// hand-over is what must be rare: with one for every block, and bytes loaded
+// where they were needed, 16384 x 1152 x 4608 took 301 us; with one for every
+// four, and loads a batch ahead, 82.  Two accumulators of up to 192 columns
+// and a ring of scale words fill the 512 columns of tensor memory.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "kernels.h"
@@ -30,18 +31,17 @@ constexpr int THREADS = 512;
 constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 8;
 constexpr int STAGE_A = BM * BK;
 constexpr int RING_BYTES = 188 * 1024, MAX_STAGES = 7;
-constexpr int STAGING_WARP = 32 * 128;  // 32 rows of 32 f32 per epilogue warp
-// tensor memory: accumulators at 0 and MAX_BN, then a ring of scale words
-// (4 columns for x, up to 7 for W), each for WORD_KB blocks
-constexpr int MAX_BN = 224, SCALE_COL = 2 * MAX_BN, SCALE_STEP = 12, TMEM_COLS = 512;
-constexpr int SCALES = 5, WORD_KB = 4;
-// the scale words of a batch of blocks in shared memory: 128 rows of x, then
-// up to 224 of W
-constexpr int SCALE_BATCH = 16, SCALE_ROWS = 128 + MAX_BN;
-constexpr int SCALE_BYTES = SCALE_BATCH / WORD_KB * SCALE_ROWS * 4;
+constexpr int STAGING_WARP = 32 * 128;  // 32 rows of 32 columns per epilogue warp
+// tensor memory: accumulators at 0 and MAX_BN, then a ring of scale words: a
+// batch holds, for each WORD_KB blocks, 4 columns for x and 6 for W
+constexpr int MAX_BN = 192, SCALE_COL = 2 * MAX_BN, TMEM_COLS = 512;
+constexpr int WORD_KB = 4, SCALE_BATCH = 16, SCALE_GROUPS = SCALE_BATCH / WORD_KB;
+constexpr int SCALE_STEP = 10, SCALE_SLOT = SCALE_GROUPS * SCALE_STEP, SCALES = 3;
+static_assert(SCALE_COL + SCALES * SCALE_SLOT <= TMEM_COLS, "tensor memory");
+// the batch's words in shared memory: up to 128 rows of x, up to 192 of W
+constexpr int SCALE_ROWS = 128 + MAX_BN, SCALE_BYTES = SCALE_GROUPS * SCALE_ROWS * 4;
 constexpr size_t SMEM_BYTES =
     size_t(RING_BYTES) + EPI_WARPS * STAGING_WARP + SCALE_BYTES + 1024 + 256;
-static_assert(SCALE_COL + SCALES * SCALE_STEP <= TMEM_COLS, "tensor memory");
 // Instruction descriptor of kind::mxf8f6f4: e4m3 x e4m3 into f32, both
 // K-major, power-of-two scale bytes; N >> 3 at bit 17, M >> 7 at bit 27, the
 // byte of each scale word that the MMA takes at bits 4 (W) and 29 (x).
@@ -63,62 +63,54 @@ struct Out {
   T* y;
   const float* bias;
   int ldy, rows, n;
-  bool wide;  // rows are 16-byte aligned
+  bool tma;  // y's rows are 16-byte aligned: chunks leave by TMA
   unsigned* err;
 };
 
 // One warp's 32 x 32 chunk of the accumulator (lane = row r0 + lane, v = its
-// columns c0 ..): through shared memory, XOR-swizzled in 16-byte units, so
-// that neighbouring lanes write neighbouring columns.
+// columns c0 .., `bias` that of column c0 + lane), by way of the warp's own
+// shared memory.
+// TMA: in the layout of a box of 32 columns with a swizzle as wide as its rows
+// (which also keeps the row-per-lane writes free of bank conflicts); what lies
+// outside y is not written.
+template <class T>
+__device__ __forceinline__ void store_chunk(const CUtensorMap* map, uint8_t* stg, int lane,
+                                            const float* v, int r0, int c0) {
+  const uint32_t s0 = saddr(stg);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       s0 + lane * 128 + 16 * (j ^ (lane & 7))),
+                   "f"(v[4 * j]), "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       s0 + lane * 64 + 16 * (j ^ ((lane >> 1) & 3))),
+                   "r"(pack_bf16x2(v[8 * j], v[8 * j + 1])),
+                   "r"(pack_bf16x2(v[8 * j + 2], v[8 * j + 3])),
+                   "r"(pack_bf16x2(v[8 * j + 4], v[8 * j + 5])),
+                   "r"(pack_bf16x2(v[8 * j + 6], v[8 * j + 7]))
+                   : "memory");
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) tma_store_2d(map, s0, c0, r0);
+}
+// Any alignment: neighbouring lanes write neighbouring columns.
 template <class T>
 __device__ __forceinline__ void write_chunk(const Out<T>& o, uint8_t* stg, int lane,
                                             const float* v, int r0, int c0) {
-  const uint32_t s0 = saddr(stg);
+  float* s = reinterpret_cast<float*>(stg);
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
-                     s0 + lane * 128 + 16 * (j ^ (lane & 7))),
-                 "f"(v[4 * j]), "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
-                 : "memory");
+  for (int j = 0; j < 32; ++j) s[lane * 32 + (j ^ lane)] = v[j];
   __syncwarp();
-  const int rows = min(32, o.rows - r0), cols = min(32, o.n - c0);
-  if (o.wide && cols == 32) {
-    constexpr int PER = 16 / sizeof(T), GROUPS = 32 / PER, STEP = 32 / GROUPS;
-    const int g = lane % GROUPS;
-    float b[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) b[i] = o.bias ? __ldg(o.bias + c0 + g * PER + i) : 0.f;
-#pragma unroll
-    for (int p = 0; p < 32 / STEP; ++p) {
-      const int row = p * STEP + lane / GROUPS;
-      float x[PER];
-#pragma unroll
-      for (int i = 0; i < PER / 4; ++i) {
-        const float4 q = *reinterpret_cast<const float4*>(
-            stg + row * 128 + 16 * ((g * (PER / 4) + i) ^ (row & 7)));
-        x[4 * i] = q.x + b[4 * i];
-        x[4 * i + 1] = q.y + b[4 * i + 1];
-        x[4 * i + 2] = q.z + b[4 * i + 2];
-        x[4 * i + 3] = q.w + b[4 * i + 3];
-      }
-      if (row < rows) {
-        T* dst = o.y + (long long)(r0 + row) * o.ldy + c0 + g * PER;
-        if constexpr (sizeof(T) == 4)
-          *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-        else
-          *reinterpret_cast<uint4*>(dst) =
-              make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
-                         pack_bf16x2(x[PER - 4], x[PER - 3]), pack_bf16x2(x[PER - 2], x[PER - 1]));
-      }
-    }
-  } else if (lane < cols) {
-    const float b = o.bias ? __ldg(o.bias + c0 + lane) : 0.f;
-    for (int row = 0; row < rows; ++row) {
-      const float x = *reinterpret_cast<const float*>(stg + row * 128 +
-                                                      16 * ((lane >> 2) ^ (row & 7)) +
-                                                      4 * (lane & 3)) + b;
-      o.y[(long long)(r0 + row) * o.ldy + c0 + lane] = T(x);
-    }
+  const int rows = min(32, o.rows - r0);
+  if (lane < o.n - c0) {
+    T* y = o.y + (long long)r0 * o.ldy + c0 + lane;
+    for (int row = 0; row < rows; ++row, y += o.ldy) *y = T(s[row * 32 + (lane ^ row)]);
   }
   __syncwarp();  // the staging area is rewritten by the next chunk
 }
@@ -131,13 +123,14 @@ __device__ __forceinline__ void scale_sync() { asm volatile("bar.sync 1, 128;" :
 template <class T, bool PAIR>
 __global__ void __launch_bounds__(THREADS, 1)
 fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
+                  const __grid_constant__ CUtensorMap tmY,
                   const __grid_constant__ Fp8Mat x, const __grid_constant__ Fp8Mat w,
                   const __grid_constant__ Out<T> out, const __grid_constant__ Plan pl) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   uint8_t* stg = smem + RING_BYTES;
-  uint32_t* sw_words = reinterpret_cast<uint32_t*>(stg + EPI_WARPS * STAGING_WARP);
+  uint32_t* words = reinterpret_cast<uint32_t*>(stg + EPI_WARPS * STAGING_WARP);
   uint64_t* bars = reinterpret_cast<uint64_t*>(stg + EPI_WARPS * STAGING_WARP + SCALE_BYTES);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 2 * SCALES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -220,8 +213,8 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
         if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
         const uint32_t d = tmem + uint32_t(acc * MAX_BN);
         for (int kb = 0; kb < KB; ++kb) {
-          const int byte = kb % WORD_KB;
-          if (byte == 0 && !mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
+          const int in_batch = kb % SCALE_BATCH, byte = kb % WORD_KB;
+          if (in_batch == 0 && !mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
           if (!ready && !mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
           const uint64_t so = uint64_t((stage * STAGE) >> 4);
           const uint32_t eb = empty0 + 8 * stage;
@@ -229,7 +222,8 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
           // (the next stage's test runs beside this one's MMAs)
           ready = mbar_test(full0 + 8 * stage, phase);
           tc_fence_after();
-          const uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_STEP), sb = sa + 4;
+          const uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT +
+                                              in_batch / WORD_KB * SCALE_STEP), sb = sa + 4;
           const uint32_t id = idesc | uint32_t(byte) << 4 | uint32_t(byte) << 29;
 #pragma unroll
           for (int kk = 0; kk < BK / 32; ++kk) {
@@ -242,7 +236,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
           }
           if (PAIR) umma_commit_pair(eb);
           else umma_commit(eb);
-          if (byte == WORD_KB - 1 || kb == KB - 1) {
+          if (in_batch == SCALE_BATCH - 1 || kb == KB - 1) {
             if (PAIR) umma_commit_pair(sempty0 + 8 * sc);
             else umma_commit(sempty0 + 8 * sc);
             if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
@@ -257,94 +251,132 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   } else if (warp >= SCALE_WARP && warp < EPI_WARP) {
     // -------------------------------------------------------- scale words
     pdl_wait();
-    const int sx = x.group == 1 ? 0 : 7, sw = w.group == 1 ? 0 : 7;
-    const uint32_t part = uint32_t((warp & 3) * 32) << 16;
-    // A batch is the bytes of SCALE_BATCH blocks: each of the 128 threads loads
-    // those of one row of x and of two of W, without a branch and from clamped
-    // places, so that the loads are under way together (beside the operand
-    // stream one round trip takes longer than the MMAs of four blocks), packs
-    // them into words and leaves the words in shared memory, where every warp
-    // takes what it stores.  The next batch's loads run meanwhile.  Rows and
-    // blocks that there are none of multiply zeros and take the scale 1.
+    // The bytes of the next batch are under way (without a branch, from
+    // clamped places) while this one's words go by way of shared memory into
+    // tensor memory.  A thread loads sixteen blocks' bytes of one row of x and
+    // of two of W; where 128 rows share a scale, one byte of the three shared
+    // rows that a tile can meet.  Rows and blocks that there are none of
+    // multiply zeros and take the scale 1.
     const int tid = int(threadIdx.x) - SCALE_WARP * 32;
-    uint32_t next[3][SCALE_BATCH / WORD_KB];
-    const auto load = [&](int t, int kb) {
-      const int m = pl.m(t) * CTAS + int(rank), nn = pl.n(t);
+    const uint32_t part = uint32_t((warp & 3) * 32) << 16;
+    uint8_t bx[SCALE_BATCH], bw[2][SCALE_BATCH];
+    const auto load = [&](const Fp8Mat& o, int row0, int r, int kb, uint8_t* b) {
+      if (o.group == 1) {
+        const uint8_t* p = o.scales + min(row0 + r, o.rows - 1);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const int r = i == 0 ? m * BM + tid : nn * BN + (i - 1) * 128 + tid;
-        const int rows = i == 0 ? x.rows : w.rows;
-        const uint8_t* p = i == 0 ? x.scales + (min(r, rows - 1) >> sx)
-                                  : w.scales + (min(r, rows - 1) >> sw);
-        const long long step = i == 0 ? x.lds : w.lds;
-#pragma unroll
-        for (int g = 0; g < SCALE_BATCH / WORD_KB; ++g) {
-          uint32_t b[WORD_KB];
-#pragma unroll
-          for (int u = 0; u < WORD_KB; ++u) b[u] = p[min(kb + g * WORD_KB + u, KB - 1) * step];
-          const uint32_t word = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
-          next[i][g] = r < rows ? word : 0x7f7f7f7fu;
-        }
+        for (int u = 0; u < SCALE_BATCH; ++u)
+          b[u] = p[(long long)min(kb + u, KB - 1) * o.lds];
+      } else {
+        const int e = min(row0 / 128 + r / SCALE_BATCH, (o.rows - 1) / 128);
+        b[0] = o.scales[(long long)min(kb + r % SCALE_BATCH, KB - 1) * o.lds + e];
       }
+    };
+    // the words of up to `most` rows, or of three shared ones, at `to`
+    const auto keep = [&](const Fp8Mat& o, int row0, int r, int most, const uint8_t* b,
+                          uint32_t* to) {
+      if (o.group == 1) {
+        if (r >= most) return;
+        const bool in = row0 + r < o.rows;
+#pragma unroll
+        for (int g = 0; g < SCALE_GROUPS; ++g)
+          to[g * SCALE_ROWS + r] =
+              in ? uint32_t(b[4 * g]) | uint32_t(b[4 * g + 1]) << 8 |
+                       uint32_t(b[4 * g + 2]) << 16 | uint32_t(b[4 * g + 3]) << 24
+                 : 0x7f7f7f7fu;
+      } else if (r < 3 * SCALE_BATCH) {
+        const int u = r % SCALE_BATCH;
+        reinterpret_cast<uint8_t*>(to + u / WORD_KB * SCALE_ROWS + r / SCALE_BATCH)[u % WORD_KB] =
+            b[0];
+      }
+    };
+    const int m_rows = x.group == 1 ? 1 : 0, w_rows = w.group == 1 ? 1 : 0;
+    const auto fetch = [&](int t, int kb) {
+      load(x, (pl.m(t) * CTAS + int(rank)) * BM, tid, kb, bx);
+      load(w, pl.n(t) * BN, tid, kb, bw[0]);
+      if (w_rows) load(w, pl.n(t) * BN, tid + 128, kb, bw[1]);
     };
     int sc = 0, t = pos, kb = 0;
     uint32_t sc_phase = 0;
-    if (t < pl.tiles) load(t, kb);
+    if (t < pl.tiles) fetch(t, kb);
     while (t < pl.tiles) {
+      const int x0 = (pl.m(t) * CTAS + int(rank)) * BM, w0 = pl.n(t) * BN;
       scale_sync();  // (the batch before has been taken)
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-#pragma unroll
-        for (int g = 0; g < SCALE_BATCH / WORD_KB; ++g)
-          if (i < 2 || tid < SCALE_ROWS - 256) sw_words[g * SCALE_ROWS + i * 128 + tid] = next[i][g];
+      keep(x, x0, tid, 128, bx, words);
+      keep(w, w0, tid, MAX_BN, bw[0], words + 128);
+      if (w_rows) keep(w, w0, tid + 128, MAX_BN, bw[1], words + 128);
       scale_sync();
-      const int groups = (min(KB - kb, SCALE_BATCH) + WORD_KB - 1) / WORD_KB;
       kb += SCALE_BATCH;
       if (kb >= KB) { kb = 0; t += G; }
-      if (t < pl.tiles) load(t, kb);
-      for (int g = 0; g < groups; ++g) {
-        uint32_t v[12];
+      if (t < pl.tiles) fetch(t, kb);
+      if (ok) ok = mbar_wait(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
+      // (after a failed wait the warp goes on to the barriers, without work)
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) {
+        tc_fence_after();
+        uint32_t v[SCALE_SLOT];
 #pragma unroll
-        for (int i = 0; i < 11; ++i) v[i] = sw_words[g * SCALE_ROWS + 32 * i + lane];
-        v[11] = 0x7f7f7f7fu;
-        if (ok) ok = mbar_wait(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
-        // (after a failed wait the warp goes on to the barriers, without work)
-        ok = __all_sync(0xffffffffu, ok);
-        if (ok) {
-          tc_fence_after();
-          const uint32_t ta = tmem + uint32_t(SCALE_COL + sc * SCALE_STEP) + part;
-          tmem_st4(ta, v[0], v[1], v[2], v[3]);
-          tmem_st8(ta + 4, v + 4);
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (PAIR) mbar_arrive_cluster(mapa_shared(sfull0 + 8 * sc, 0));
-            else mbar_arrive(sfull0 + 8 * sc);
-          }
+        for (int g = 0; g < SCALE_GROUPS; ++g) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[g * SCALE_STEP + i] = words[g * SCALE_ROWS + (m_rows ? 32 * i + lane : 0)];
+#pragma unroll
+          for (int i = 0; i < 6; ++i)
+            v[g * SCALE_STEP + 4 + i] =
+                words[g * SCALE_ROWS + 128 +
+                      (w_rows ? 32 * i + lane : (w0 + 32 * i + lane) / 128 - w0 / 128)];
         }
-        if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
+        const uint32_t ta = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT) + part;
+        tmem_st16(ta, v);
+        tmem_st16(ta + 16, v + 16);
+        tmem_st8(ta + 32, v + 32);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_cluster(mapa_shared(sfull0 + 8 * sc, 0));
+          else mbar_arrive(sfull0 + 8 * sc);
+        }
       }
+      if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
     }
   } else if (warp >= EPI_WARP) {
     // ------------------------------------------------------------ epilogue
     pdl_wait();
     const int sp = warp & 3, half = (warp - EPI_WARP) >> 2;
     const uint32_t tempty_r0 = PAIR ? mapa_shared(tempty0, 0) : tempty0;
-    int acc = 0;
+    uint8_t* own = stg + (warp - EPI_WARP) * STAGING_WARP;
+    constexpr int BUFS = sizeof(T) == 4 ? 1 : 2;  // staging of this many chunks
+    int acc = 0, buf = 0;
     uint32_t acc_phase = 0;
     for (int t = pos; t < pl.tiles; t += G) {
       const int m = pl.m(t) * CTAS + int(rank), nn = pl.n(t);
+      // (the bias before the accumulator is ready)
+      float bias[MAX_BN / 64];
+#pragma unroll
+      for (int i = 0; i < MAX_BN / 64; ++i) {
+        const int c = nn * BN + (half + 2 * i) * 32 + lane;
+        bias[i] = out.bias && c < out.n ? __ldg(out.bias + c) : 0.f;
+      }
       if (!mbar_sleep_warp(tfull0 + 8 * acc, acc_phase, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const uint32_t tb = tmem + uint32_t(acc * MAX_BN) + (uint32_t(sp * 32) << 16);
-#pragma unroll 1
-      for (int ch = half; ch < BN / 32; ch += 2) {
+#pragma unroll
+      for (int i = 0; i < MAX_BN / 64; ++i) {
+        const int ch = half + 2 * i, r0 = m * BM + sp * 32, c0 = nn * BN + ch * 32;
+        if (ch >= BN / 32 || r0 >= out.rows || c0 >= out.n) break;
         float v[32];
         tmem_ld32(tb + uint32_t(ch * 32), v);
-        const int r0 = m * BM + sp * 32, c0 = nn * BN + ch * 32;
-        if (r0 < out.rows && c0 < out.n)
-          write_chunk(out, stg + (warp - EPI_WARP) * STAGING_WARP, lane, v, r0, c0);
+        if (out.bias)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bias[i], j);
+        if (out.tma) {
+          if (lane == 0) tma_store_wait_read<BUFS - 1>();  // this buffer's chunk has been read
+          __syncwarp();
+          store_chunk<T>(&tmY, own + buf * (STAGING_WARP / 2), lane, v, r0, c0);
+          if (BUFS == 2) buf ^= 1;
+        } else {
+          write_chunk(out, own, lane, v, r0, c0);
+        }
       }
       tc_fence_before();
       __syncwarp();
@@ -354,6 +386,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
+    if (lane == 0) tma_store_wait_read<0>();
   }
   if (!ok) {
     *abort_flag = 1;
@@ -373,6 +406,23 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
 
 constexpr int SMS = 152;
 
+// y [rows][n] in boxes of 32 x 32 whose rows are swizzled over their own width.
+template <class T>
+cudaError_t tma_map_chunks(T* y, int rows, int n, int ld, CUtensorMap* out) {
+  auto fn = tma_encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  constexpr bool F32 = sizeof(T) == 4;
+  const cuuint64_t dims[2] = {cuuint64_t(n), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {cuuint64_t(ld) * sizeof(T)};
+  const cuuint32_t box[2] = {32, 32}, es[2] = {1, 1};
+  const CUresult r =
+      fn(out, F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, y, dims,
+         strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+         F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+         CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <class T, bool PAIR>
 cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, cudaStream_t st) {
   // (an attribute of the current device, so set for each call)
@@ -390,22 +440,24 @@ cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, cudaSt
   const long long tiles = (long long)pl.mt * pl.nt;
   if (tiles > 0x7fffffff - SMS) return cudaErrorInvalidValue;
   pl.tiles = int(tiles);
-  CUtensorMap mx, mw;
+  CUtensorMap mx, mw, my;
   RC_TRY(tma_map_bytes(x.codes, x.rows, x.cols, x.ld, BM, &mx));
   RC_TRY(tma_map_bytes(w.codes, w.rows, w.cols, w.ld, PAIR ? bn / 2 : bn, &mw));
+  my = mx;  // (not used without out.tma)
+  if (o.tma) RC_TRY(tma_map_chunks(o.y, o.rows, o.n, o.ldy, &my));
   count_launches(1);
   const int slots = PAIR ? SMS / 2 : SMS, used = pl.tiles < slots ? pl.tiles : slots;
   if (PAIR)
     return launch_k_cluster(fp8_linear_kernel<T, true>, dim3(unsigned(2 * used)), dim3(THREADS),
-                            SMEM_BYTES, 2, st, mx, mw, x, w, o, pl);
+                            SMEM_BYTES, 2, st, mx, mw, my, x, w, o, pl);
   return launch_k(fp8_linear_kernel<T, false>, dim3(unsigned(used)), dim3(THREADS), SMEM_BYTES, st,
-                  mx, mw, x, w, o, pl);
+                  mx, mw, my, x, w, o, pl);
 }
 
 template <class T>
 cudaError_t linear(const Fp8Mat& x, const Fp8Mat& w, const float* b, T* y, int ldy, unsigned* err,
                    cudaStream_t st) {
-  const uintptr_t row = x.rows > 1 ? uintptr_t(ldy) * sizeof(T) : 0;
+  const uintptr_t row = uintptr_t(ldy) * sizeof(T);
   const Out<T> o{y, b, ldy, x.rows, w.rows,
                  ((reinterpret_cast<uintptr_t>(y) | row) & 15u) == 0, err};
   const long long mt = (x.rows + BM - 1LL) / BM;
