@@ -48,7 +48,7 @@ constexpr size_t SMEM_BYTES =
 constexpr uint32_t IDESC = 1u << 23;
 
 struct Plan {
-  int bn, stages, mt, nt, tiles, kb;
+  int bn, stages, mt, nt, tiles, kb, parts;
   int n_first;  // neighbouring tiles share rows of x (otherwise of W)
   __device__ __forceinline__ int m(int t) const { return n_first ? t / nt : t % mt; }
   __device__ __forceinline__ int n(int t) const { return n_first ? t % nt : t / mt; }
@@ -118,14 +118,19 @@ __device__ __forceinline__ void write_chunk(const Out<T>& o, uint8_t* stg, int l
 // Named barrier of the four scale warps.
 __device__ __forceinline__ void scale_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-// PAIR: clusters of two CTAs share each MMA (M = 256): a CTA loads its own 128
-// rows of x and half of the W tile.
-template <class T, bool PAIR>
+// How CTAs work together.  PAIR: clusters of two share each MMA (M = 256): a
+// CTA loads its own 128 rows of x and half of the W tile.  SPLIT: a cluster
+// shares a tile's blocks of columns; each CTA leaves its part in shared
+// memory, and the parts are added there in the order of the ranks.
+enum Mode { ALONE, PAIRS, SPLIT };
+
+template <class T, Mode MODE>
 __global__ void __launch_bounds__(THREADS, 1)
 fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
                   const __grid_constant__ CUtensorMap tmY,
                   const __grid_constant__ Fp8Mat x, const __grid_constant__ Fp8Mat w,
                   const __grid_constant__ Out<T> out, const __grid_constant__ Plan pl) {
+  constexpr bool PAIR = MODE == PAIRS;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -139,7 +144,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   const uint32_t tfull0 = sempty0 + 8 * SCALES, tempty0 = tfull0 + 16;
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const uint32_t rank = PAIR ? cluster_ctarank() : 0;
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0;  // in a pair
   constexpr int CTAS = PAIR ? 2 : 1;
   if (threadIdx.x == 0) {
     for (int s = 0; s < MAX_STAGES; ++s) {
@@ -167,13 +172,18 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   const uint32_t tmem = *tmem_slot;
   if (PAIR) cluster_sync();  // (the peer's barriers are ready)
 
-  const int BN = pl.bn, STAGES = pl.stages, KB = pl.kb;
+  const int BN = pl.bn, STAGES = pl.stages;
   const int STAGE = stage_bytes<PAIR>(BN);
-  const int G = int(gridDim.x) / CTAS, pos = int(blockIdx.x) / CTAS;
+  // this CTA's (or pair's) tiles pos, pos + G .. and, of each, its blocks
+  // k0 .. k0 + KB - 1
+  const int parts = MODE == SPLIT ? pl.parts : 1;
+  const int part_of = MODE == SPLIT ? int(cluster_ctarank()) : 0;
+  const int k0 = part_of * pl.kb / parts, KB = (part_of + 1) * pl.kb / parts - k0;
+  const int G = int(gridDim.x) / (CTAS * parts), pos = int(blockIdx.x) / (CTAS * parts);
   bool ok = true;
 
-  if (warp == 0 || (warp == 2 && !PAIR)) {
-    // ------------------------------------------------- TMA: x (and W for pairs), W
+  if (warp == 0 || warp == 2) {
+    // ------------------------------------------------------------ TMA: x, W
     if (elect_one()) {
       pdl_wait();
       if (warp == 0) pdl_trigger();
@@ -184,17 +194,23 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
         for (int kb = 0; kb < KB; ++kb) {
           if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
           const uint32_t st = saddr(smem + stage * STAGE), fb = full0 + 8 * stage;
-          if (PAIR) {  // (both CTAs' bytes land on rank 0's barrier)
-            if (rank == 0) mbar_expect_tx(fb, 2 * STAGE);
+          // (a barrier may see bytes before it is told of them: its phase still
+          // needs that arrival)
+          if (PAIR) {  // both CTAs' bytes land on rank 0's barrier
             const uint32_t f0 = mapa_shared(fb, 0);
-            tma_load_2d_pair(st, &tmX, f0, kb * BK, m * BM);
-            tma_load_2d_pair(st + STAGE_A, &tmW, f0, kb * BK, nn * BN + int(rank) * (BN / 2));
+            if (warp == 0) {
+              if (rank == 0) mbar_expect_tx(fb, 2 * STAGE);
+              tma_load_2d_pair(st, &tmX, f0, (k0 + kb) * BK, m * BM);
+            } else {
+              tma_load_2d_pair(st + STAGE_A, &tmW, f0, (k0 + kb) * BK,
+                               nn * BN + int(rank) * (BN / 2));
+            }
           } else if (warp == 0) {
             mbar_expect_tx(fb, STAGE_A);
-            tma_load_2d(st, &tmX, fb, kb * BK, m * BM);
+            tma_load_2d(st, &tmX, fb, (k0 + kb) * BK, m * BM);
           } else {
             mbar_expect_tx(fb, STAGE - STAGE_A);
-            tma_load_2d(st + STAGE_A, &tmW, fb, kb * BK, nn * BN);
+            tma_load_2d(st + STAGE_A, &tmW, fb, (k0 + kb) * BK, nn * BN);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
@@ -208,39 +224,49 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       const uint64_t da = sw128_desc(saddr(smem)), db = sw128_desc(saddr(smem + STAGE_A));
       int stage = 0, acc = 0, sc = 0;
       uint32_t phase = 0, acc_phase = 0, sc_phase = 0;
+      uint64_t so = 0;     // the stage's offset in the descriptors' address field
       bool ready = false;  // the current stage was seen full already
       for (int t = pos; ok && t < pl.tiles; t += G) {
         if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
         const uint32_t d = tmem + uint32_t(acc * MAX_BN);
-        for (int kb = 0; kb < KB; ++kb) {
-          const int in_batch = kb % SCALE_BATCH, byte = kb % WORD_KB;
-          if (in_batch == 0 && !mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
-          if (!ready && !mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
-          const uint64_t so = uint64_t((stage * STAGE) >> 4);
-          const uint32_t eb = empty0 + 8 * stage;
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
-          // (the next stage's test runs beside this one's MMAs)
-          ready = mbar_test(full0 + 8 * stage, phase);
-          tc_fence_after();
-          const uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT +
-                                              in_batch / WORD_KB * SCALE_STEP), sb = sa + 4;
-          const uint32_t id = idesc | uint32_t(byte) << 4 | uint32_t(byte) << 29;
+        uint32_t accumulate = 0;
+        // (what a block's issue needs beyond its stage is constant or one
+        // addition a group away: the issuing thread is what bounds small tiles)
+        for (int kb = 0; ok && kb < KB;) {
+          if (!mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
+          uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT);
+          const int end = min(kb + SCALE_BATCH, KB);
+          while (ok && kb < end) {
 #pragma unroll
-          for (int kk = 0; kk < BK / 32; ++kk) {
-            if (PAIR)
-              umma_e4m3_scaled_pair(d, da + so + 2 * kk, db + so + 2 * kk, id, sa, sb,
-                                    (kb | kk) ? 1u : 0u);
-            else
-              umma_e4m3_scaled(d, da + so + 2 * kk, db + so + 2 * kk, id, sa, sb,
-                               (kb | kk) ? 1u : 0u);
+            for (int byte = 0; byte < WORD_KB; ++byte) {
+              if (kb >= end) break;
+              if (!ready && !mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
+              const uint64_t a = da + so, b = db + so;
+              const uint32_t eb = empty0 + 8 * stage;
+              ++kb;
+              so += uint64_t(STAGE >> 4);
+              if (++stage == STAGES) { stage = 0; phase ^= 1; so = 0; }
+              // (the next stage's test runs beside this one's MMAs)
+              ready = mbar_test(full0 + 8 * stage, phase);
+              tc_fence_after();
+              const uint32_t id = idesc | uint32_t(byte) << 4 | uint32_t(byte) << 29;
+#pragma unroll
+              for (int kk = 0; kk < BK / 32; ++kk) {
+                if (PAIR)
+                  umma_e4m3_scaled_pair(d, a + 2 * kk, b + 2 * kk, id, sa, sa + 4, accumulate);
+                else
+                  umma_e4m3_scaled(d, a + 2 * kk, b + 2 * kk, id, sa, sa + 4, accumulate);
+                accumulate = 1;
+              }
+              if (PAIR) umma_commit_pair(eb);
+              else umma_commit(eb);
+            }
+            sa += SCALE_STEP;
           }
-          if (PAIR) umma_commit_pair(eb);
-          else umma_commit(eb);
-          if (in_batch == SCALE_BATCH - 1 || kb == KB - 1) {
-            if (PAIR) umma_commit_pair(sempty0 + 8 * sc);
-            else umma_commit(sempty0 + 8 * sc);
-            if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
-          }
+          if (!ok) break;
+          if (PAIR) umma_commit_pair(sempty0 + 8 * sc);
+          else umma_commit(sempty0 + 8 * sc);
+          if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
         }
         if (!ok) break;
         if (PAIR) umma_commit_pair(tfull0 + 8 * acc);
@@ -265,10 +291,10 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
         const uint8_t* p = o.scales + min(row0 + r, o.rows - 1);
 #pragma unroll
         for (int u = 0; u < SCALE_BATCH; ++u)
-          b[u] = p[(long long)min(kb + u, KB - 1) * o.lds];
+          b[u] = p[(long long)min(k0 + kb + u, pl.kb - 1) * o.lds];
       } else {
         const int e = min(row0 / 128 + r / SCALE_BATCH, (o.rows - 1) / 128);
-        b[0] = o.scales[(long long)min(kb + r % SCALE_BATCH, KB - 1) * o.lds + e];
+        b[0] = o.scales[(long long)min(k0 + kb + r % SCALE_BATCH, pl.kb - 1) * o.lds + e];
       }
     };
     // the words of up to `most` rows, or of three shared ones, at `to`
@@ -308,7 +334,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       kb += SCALE_BATCH;
       if (kb >= KB) { kb = 0; t += G; }
       if (t < pl.tiles) fetch(t, kb);
-      if (ok) ok = mbar_wait(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
+      if (ok) ok = mbar_sleep(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
       // (after a failed wait the warp goes on to the barriers, without work)
       ok = __all_sync(0xffffffffu, ok);
       if (ok) {
@@ -366,6 +392,12 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
         if (ch >= BN / 32 || r0 >= out.rows || c0 >= out.n) break;
         float v[32];
         tmem_ld32(tb + uint32_t(ch * 32), v);
+        if (MODE == SPLIT) {  // (every MMA is done: the operand ring is free)
+          float* to = reinterpret_cast<float*>(smem + (ch * 4 + sp) * 4096);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) to[32 * j + lane] = v[j];
+          continue;
+        }
         if (out.bias)
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bias[i], j);
@@ -386,7 +418,41 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
-    if (lane == 0) tma_store_wait_read<0>();
+    if (MODE != SPLIT && lane == 0) tma_store_wait_read<0>();
+  }
+  if (MODE == SPLIT) {
+    // chunk u of the tile (32 rows x 32 columns) is finished by CTA u mod
+    // parts of the cluster, by one of its epilogue warps
+    cluster_sync();
+    if (warp >= EPI_WARP) {
+      const int m = pl.m(pos), nn = pl.n(pos);
+      uint8_t* own = stg + (warp - EPI_WARP) * STAGING_WARP;
+      for (int u = part_of + (warp - EPI_WARP) * parts; u < BN / 8; u += EPI_WARPS * parts) {
+        const int r0 = m * BM + (u & 3) * 32, c0 = nn * BN + (u >> 2) * 32;
+        if (r0 >= out.rows || c0 >= out.n) continue;
+        const float b = out.bias && c0 + lane < out.n ? __ldg(out.bias + c0 + lane) : 0.f;
+        float v[32] = {};
+        for (int p = 0; p < parts; ++p) {
+          const uint32_t from = mapa_shared(saddr(smem + u * 4096), uint32_t(p)) + 4 * lane;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            float a;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(a) : "r"(from + 128 * j));
+            v[j] += a;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, b, j);
+        if (out.tma) {
+          if (lane == 0) tma_store_wait_read<0>();
+          __syncwarp();
+          store_chunk<T>(&tmY, own, lane, v, r0, c0);
+        } else {
+          write_chunk(out, own, lane, v, r0, c0);
+        }
+      }
+      if (lane == 0) tma_store_wait_read<0>();
+    }
   }
   if (!ok) {
     *abort_flag = 1;
@@ -394,8 +460,8 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
   }
   tc_fence_before();
   __syncthreads();
-  // no CTA leaves while its peer may still load, commit or arrive into it
-  if (PAIR) cluster_sync();
+  // no CTA leaves while a peer may still load, commit, arrive or read there
+  if (MODE != ALONE) cluster_sync();
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
@@ -423,10 +489,12 @@ cudaError_t tma_map_chunks(T* y, int rows, int n, int ld, CUtensorMap* out) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <class T, bool PAIR>
-cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, cudaStream_t st) {
+template <class T, Mode MODE>
+cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, int parts,
+               cudaStream_t st) {
+  constexpr bool PAIR = MODE == PAIRS;
   // (an attribute of the current device, so set for each call)
-  RC_TRY(cudaFuncSetAttribute(fp8_linear_kernel<T, PAIR>,
+  RC_TRY(cudaFuncSetAttribute(fp8_linear_kernel<T, MODE>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize, int(SMEM_BYTES)));
   Plan pl;
   pl.bn = bn;
@@ -436,6 +504,7 @@ cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, cudaSt
   pl.mt = int((x.rows + (long long)rows - 1) / rows);
   pl.nt = int((w.rows + (long long)bn - 1) / bn);
   pl.kb = (x.cols + BK - 1) / BK;
+  pl.parts = parts;
   pl.n_first = w.rows < x.rows;
   const long long tiles = (long long)pl.mt * pl.nt;
   if (tiles > 0x7fffffff - SMS) return cudaErrorInvalidValue;
@@ -446,12 +515,57 @@ cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, cudaSt
   my = mx;  // (not used without out.tma)
   if (o.tma) RC_TRY(tma_map_chunks(o.y, o.rows, o.n, o.ldy, &my));
   count_launches(1);
-  const int slots = PAIR ? SMS / 2 : SMS, used = pl.tiles < slots ? pl.tiles : slots;
-  if (PAIR)
-    return launch_k_cluster(fp8_linear_kernel<T, true>, dim3(unsigned(2 * used)), dim3(THREADS),
-                            SMEM_BYTES, 2, st, mx, mw, my, x, w, o, pl);
-  return launch_k(fp8_linear_kernel<T, false>, dim3(unsigned(used)), dim3(THREADS), SMEM_BYTES, st,
-                  mx, mw, my, x, w, o, pl);
+  const int cluster = PAIR ? 2 : parts, slots = SMS / cluster;
+  const unsigned ctas =
+      unsigned(cluster * (MODE == SPLIT || pl.tiles < slots ? pl.tiles : slots));
+  if (MODE != ALONE)
+    return launch_k_cluster(fp8_linear_kernel<T, MODE>, dim3(ctas), dim3(THREADS), SMEM_BYTES,
+                            cluster, st, mx, mw, my, x, w, o, pl);
+  return launch_k(fp8_linear_kernel<T, MODE>, dim3(ctas), dim3(THREADS), SMEM_BYTES, st, mx, mw,
+                  my, x, w, o, pl);
+}
+
+// The tile width, and how CTAs share a tile, of least estimated duration (SM
+// cycles).  Rates measured on products of 1152 and 4608 columns at 39 to 16384
+// rows: a CTA's block of columns takes 220 + 1.83 BN (its loads: TMA brings
+// about 70 B/clk to an SM), a pair's 405 + 0.42 BN, and a tile's change 7 to
+// 9.5 BN more; a launch of pairs takes 3000 longer (16384 x
+// 1152 x 4608: pairs of 192 60.0 us, alone 68.2; 831 x 3456 x 1152: 8.9 and
+// 7.3; 4096 x 1152 x 4608: alone at 128 21.2 us, pairs 24.1).  Adding
+// the parts of a split tile takes 600 + 800 a part (39 x 1152 x 4608: one CTA
+// a tile 9.4 us, four 7; 39 x 1152 x 1152: one 4.9, two 5.9).  Clusters above
+// four CTAs do not all find a place at once and take twice as long.
+struct Choice {
+  Mode mode;
+  int bn, parts;
+};
+Choice choose(long long rows, long long n, int kb) {
+  Choice best{ALONE, 64, 1};
+  double least = 1e30;
+  const auto look = [&](Mode mode, int bn, int parts) {
+    const long long high = mode == PAIRS ? 2 * BM : BM;
+    const long long tiles = ((rows + high - 1) / high) * ((n + bn - 1) / bn);
+    double cost;
+    if (mode == SPLIT) {
+      if (tiles * parts > SMS - 8) return;
+      cost = (kb + parts - 1) / parts * (220 + 1.83 * bn) + 7.0 * bn + 600 + 800 * parts;
+    } else {
+      const long long slots = mode == PAIRS ? SMS / 2 : SMS, waves = (tiles + slots - 1) / slots;
+      cost = double(waves) * (mode == PAIRS ? kb * (405 + 0.42 * bn) + 9.5 * bn
+                                            : kb * (220 + 1.83 * bn) + 7.0 * bn);
+      if (mode == PAIRS) cost += 3000;
+    }
+    if (cost < least) {
+      least = cost;
+      best = Choice{mode, bn, parts};
+    }
+  };
+  for (int bn = MAX_BN; bn >= 64; bn -= 32) {
+    look(ALONE, bn, 1);
+    if (rows > BM && bn >= 128) look(PAIRS, bn, 1);
+  }
+  for (int parts = 2; parts <= 4 && parts <= kb; ++parts) look(SPLIT, 64, parts);
+  return best;
 }
 
 template <class T>
@@ -460,11 +574,10 @@ cudaError_t linear(const Fp8Mat& x, const Fp8Mat& w, const float* b, T* y, int l
   const uintptr_t row = uintptr_t(ldy) * sizeof(T);
   const Out<T> o{y, b, ldy, x.rows, w.rows,
                  ((reinterpret_cast<uintptr_t>(y) | row) & 15u) == 0, err};
-  const long long mt = (x.rows + BM - 1LL) / BM;
-  const auto tiles = [&](int bn) { return mt * ((w.rows + bn - 1LL) / bn); };
-  if (x.rows > BM && tiles(192) >= SMS) return go<T, true>(x, w, o, 192, st);
-  if (tiles(128) >= SMS) return go<T, false>(x, w, o, 128, st);
-  return go<T, false>(x, w, o, 64, st);
+  const Choice c = choose(x.rows, w.rows, (x.cols + BK - 1) / BK);
+  if (c.mode == PAIRS) return go<T, PAIRS>(x, w, o, c.bn, 1, st);
+  if (c.mode == SPLIT) return go<T, SPLIT>(x, w, o, c.bn, c.parts, st);
+  return go<T, ALONE>(x, w, o, c.bn, 1, st);
 }
 
 }  // namespace
