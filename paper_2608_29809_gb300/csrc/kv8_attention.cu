@@ -80,6 +80,7 @@ cudaError_t attention(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st
 }  // namespace
 
 cudaError_t launch_kv8_attention(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
+  if ((long long)a.max_q * (a.heads / pool.heads) <= 64) return launch_kv8_few(pool, a, st);
   switch (pool.dh) {
     case 64: return attention<64>(pool, a, st);
     case 72: return attention<72>(pool, a, st);
