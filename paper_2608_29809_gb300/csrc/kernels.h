@@ -279,5 +279,7 @@ struct Kv8AttnArgs {
 cudaError_t launch_kv8_attention(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st);
 // The same for requests of a few rows each (every sixteen read the cache).
 cudaError_t launch_kv8_few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st);
+// And for requests of many rows (the tensor memory path).
+cudaError_t launch_kv8_many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st);
 
 }  // namespace rc

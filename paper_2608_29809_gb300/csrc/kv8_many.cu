@@ -1,0 +1,633 @@
+// Attention of many query rows over the paged eight-bit cache (rc_kv8), on the
+// tensor cores (tcgen05, scores and results in tensor memory).
+//
+// A unit is up to 256 rows (query, head of the key head's group) of one
+// request and key head: two tiles of 128 rows that share every key block of
+// 128 tokens (two cache blocks), or one tile whose key blocks two streams take
+// in turn.  A cluster of CTAs may share the unit's keys.
+//   warps 0-3, 4-7   softmax of a stream, one thread a row: S from tensor
+//                    memory, weights back over it as bf16
+//   warps 8-11       codes from global memory to registers, to operands in
+//                    shared memory: keys as f16 (exact, K-major), values as
+//                    bf16 (exact, MN-major), both with the 128-byte swizzle
+//   warp 12          issues S = Q K^T (kind f16) and O += P V (kind bf16)
+// Each code is converted once for 256 rows, so its four instructions or so
+// stay beside the softmax; a pass that wrote bf16 copies for the kernel of
+// rc_attention would move five bytes for each one.  Q is f16 over the power of
+// two of its row's largest magnitude.  A block's key scale joins the factor of
+// its scores, its value scale the exponent of its weights (relative to a
+// reference kept per stream), so that both cost nothing per element; bf16
+// weights have f32's range, so neither can underflow f32's neighbours.
+// The maximum is taken in a row's first block only: later blocks use the same
+// reference unless their weights' sum passes 2^64 (or a value scale passes
+// 2^40 of its reference); then it is raised, O rescaled, the block done again.
+#include <math.h>
+
+#include "common.cuh"
+#include "fp8.cuh"
+#include "kernels.h"
+#include "tc_common.cuh"
+
+namespace rc {
+
+namespace {
+
+using namespace rc::tc;
+
+constexpr int BQ = 128, BKV = 128, THREADS = 416;
+constexpr int CONV_WARP = 8, MMA_WARP = 12;
+constexpr int PAGES = BKV / KV8_BLOCK;
+constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;  // S (P over it) of each stream, then O
+constexpr float RAISE_SUM = 18446744073709551616.f;  // 2^64
+constexpr int RAISE_VALUE = 40;
+
+template <int DH>
+struct MCfg {
+  static constexpr bool TAIL = DH == 72;
+  static constexpr int ATOMS = (DH + 63) / 64;       // 64-channel parts of a V row
+  static constexpr int FULL = DH / 64;               // 64-channel parts of a K row
+  static constexpr int ODIM = TAIL ? 80 : DH;        // columns of O
+  static constexpr int Q_BYTES = FULL * BQ * 128 + (TAIL ? BQ * 32 : 0);
+  static constexpr int K_BYTES = FULL * BKV * 128 + (TAIL ? BKV * 32 : 0);
+  static constexpr int V_BYTES = ATOMS * BKV * 128;
+  static constexpr int KST = DH == 128 ? 2 : 3, VST = DH == 128 ? 2 : 3;
+  static constexpr int RING = 2 * Q_BYTES + KST * K_BYTES + VST * V_BYTES;
+  static constexpr size_t SMEM = size_t(RING) + 1024 + 256;
+  static constexpr int UNITS = BKV * DH / 8 / 128;   // 8-code pieces of K (or V) a thread
+  static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(BKV >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
+  static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) |
+                                       (uint32_t(ODIM >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
+  static constexpr int PSTRIDE = DH + 2;             // floats of a partial row
+  static_assert(2 * BQ * PSTRIDE * 4 <= RING, "the parts fit the operands' memory");
+  static_assert(TM_O + 2 * ODIM <= TMEM_COLS, "tensor memory");
+};
+
+__device__ __forceinline__ uint64_t pair64(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float2 split64(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c,
+                                       uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c),
+               "r"(d)
+               : "memory");
+}
+// Four codes as bf16: the pairs (0, 2) and (1, 3).  A code's bits below its
+// sign, seven places down a bf16, are its value times 2^-120 (subnormals
+// included); the product is exact.  (A NaN code becomes a number: blocks
+// without value have a NaN scale.)
+__device__ __forceinline__ uint32_t times_2_120(uint32_t x) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x7b807b80u));
+  return r;
+}
+__device__ __forceinline__ uint32_t codes_02(uint32_t u) {
+  return times_2_120(((u << 8) & 0x80008000u) | ((u << 4) & 0x07f007f0u));
+}
+__device__ __forceinline__ uint32_t codes_13(uint32_t u) {
+  return times_2_120((u & 0x80008000u) | ((u >> 4) & 0x07f007f0u));
+}
+// Place of channel c among O's columns (the pairs above).
+__device__ __forceinline__ constexpr int o_column(int c) {
+  return (c & ~3) | ((c & 1) << 1) | ((c >> 1) & 1);
+}
+
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
+// Blocks and scale bytes of the two cache blocks of a key block.
+struct Info {
+  int page[PAGES], k[PAGES], v[PAGES];
+};
+
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1)
+many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
+                 int parts, int unit_rows) {
+  using C = MCfg<DH>;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING);
+  const uint32_t sq = saddr(smem), sk = sq + 2 * C::Q_BYTES, sv = sk + C::KST * C::K_BYTES;
+  const uint32_t bar = saddr(bars);
+  const uint32_t k_full = bar, k_empty = k_full + 8 * C::KST, v_full = k_empty + 8 * C::KST;
+  const uint32_t v_empty = v_full + 8 * C::VST, s_full = v_empty + 8 * C::VST;
+  const uint32_t p_full = s_full + 16, o_full = p_full + 16, q_full = o_full + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::KST + 2 * C::VST + 7);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+
+  pdl_wait();
+  pdl_trigger();
+  const int part = parts > 1 ? int(cluster_ctarank()) : 0;
+  const int group = a.heads / pool.heads;
+  const int head = blockIdx.y % pool.heads, chunk = blockIdx.y / pool.heads, req = blockIdx.z;
+  const int q0 = a.offsets[req], nq = a.offsets[req + 1] - q0, len = a.lengths[req];
+  // (the same for every CTA of a cluster)
+  if (q0 < 0 || nq < 0 || nq > a.max_q || q0 > a.q_rows - nq || len < 0 ||
+      len > (long long)a.ld_table * KV8_BLOCK) {
+    if (threadIdx.x == 0) atomicOr(a.err, DEVERR_COUNT);
+    return;
+  }
+  const long long all = (long long)nq * group;
+  const long long row0 = (long long)chunk * unit_rows;
+  if (row0 >= all) return;
+  const int rows = int(all - row0 < unit_rows ? all - row0 : unit_rows);
+  const bool two = rows > BQ;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::KST; ++i) {
+      mbar_init(k_full + 8 * i, 4);
+      mbar_init(k_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < C::VST; ++i) {
+      mbar_init(v_full + 8 * i, 4);
+      mbar_init(v_empty + 8 * i, 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(s_full + 8 * x, 1);
+      mbar_init(p_full + 8 * x, 4);
+      mbar_init(o_full + 8 * x, 1);
+    }
+    mbar_init(q_full, 8);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (C::TAIL) {  // channels 72 .. 79 of the products are zeros
+    for (int i = threadIdx.x; i < 2 * BQ * 2; i += THREADS)
+      sts128(sq + (i / (2 * BQ)) * C::Q_BYTES + BQ * 128 + (i % (2 * BQ)) * 16, 0, 0, 0, 0);
+    for (int i = threadIdx.x; i < C::KST * BKV * 2; i += THREADS)
+      sts128(sk + (i / (2 * BKV)) * C::K_BYTES + BKV * 128 + (i % (2 * BKV)) * 16, 0, 0, 0, 0);
+  }
+  if (warp == MMA_WARP) tmem_alloc(saddr(tmem_slot), TMEM_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  // the tokens that the unit's last row sees, in key blocks b0 .. b0 + nb - 1
+  // of this CTA
+  const int last_query = int((row0 + rows - 1) / group);
+  const int reach = a.causal ? max(0, len - nq + last_query + 1) : len;
+  const int blocks = (reach + BKV - 1) / BKV;
+  const int b0 = int((long long)part * blocks / parts);
+  const int nb = int((long long)(part + 1) * blocks / parts) - b0;
+  const int pages = (len + KV8_BLOCK - 1) / KV8_BLOCK;
+  const int* table = a.table + (long long)req * a.ld_table;
+  const auto page_of = [&](int p, bool report) {
+    if (p >= pages) return -1;
+    const int page = table[p];
+    if (page >= 0 && page < pool.blocks) return page;
+    if (report) atomicOr(a.err, DEVERR_INDEX);
+    return -1;
+  };
+  bool ok = true;
+
+  if (warp == MMA_WARP) {
+    // ----------------------------------------------------------------- MMA
+    if (nb > 0 && elect_one()) {
+      const int events = two ? 2 * nb : nb;
+      const auto scores = [&](int e) {
+        const int x = e & 1, b = two ? e >> 1 : e, st = b % C::KST;
+        if ((!two || x == 0) &&
+            !mbar_wait(k_full + 8 * st, (b / C::KST) & 1, abort_flag)) return false;
+        tc_fence_after();
+        const uint32_t q = sq + (two ? x : 0) * C::Q_BYTES, k = sk + st * C::K_BYTES;
+        const uint32_t d = tmem + uint32_t(x * BKV);
+#pragma unroll
+        for (int f = 0; f < C::FULL; ++f)
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            umma_bf16(d, sw128_desc(q + f * BQ * 128) + 2 * kk,
+                      sw128_desc(k + f * BKV * 128) + 2 * kk, C::IDESC_S, (f | kk) ? 1u : 0u);
+        if (C::TAIL)
+          umma_bf16(d, sw32_kmajor_desc(q + BQ * 128), sw32_kmajor_desc(k + BKV * 128), C::IDESC_S,
+                    1u);
+        umma_commit(s_full + 8 * x);
+        if (!two || x == 1) umma_commit(k_empty + 8 * st);
+        return true;
+      };
+      ok = mbar_wait(q_full, 0, abort_flag) && scores(0) && (events < 2 || scores(1));
+      for (int e = 0; ok && e < events; ++e) {
+        const int x = e & 1, b = two ? e >> 1 : e, i = e >> 1, st = b % C::VST;
+        if (((!two || x == 0) && !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
+            !mbar_wait(p_full + 8 * x, i & 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d = tmem + uint32_t(TM_O + x * C::ODIM), p = tmem + uint32_t(x * BKV);
+        const uint64_t v = sw128_mnmajor_desc_lbo(sv + st * C::V_BYTES, BKV * 128);
+#pragma unroll
+        for (int kk = 0; kk < BKV / 16; ++kk)
+          umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | kk) ? 1u : 0u);
+        if (!two || x == 1) umma_commit(v_empty + 8 * st);
+        if (e + 2 >= events) umma_commit(o_full + 8 * x);
+        else if (!scores(e + 2)) ok = false;
+      }
+    }
+  } else if (warp >= CONV_WARP) {
+    // ---------------------------------------------------------- conversion
+    // Thread `tid` takes the 8-code pieces tid + 128 j of the block's 128
+    // rows (piece c of row r: 8 channels); a cache block's rows are one run.
+    const int tid = int(threadIdx.x) - CONV_WARP * 32;
+    constexpr int PER_ROW = DH / 8;
+    uint2 kr[C::UNITS], vr[C::UNITS];
+    int page[PAGES], ahead[PAGES];
+    const auto fetch = [&](int side, uint2* to) {
+#pragma unroll
+      for (int j = 0; j < C::UNITS; ++j) {
+        const int u = tid + 128 * j, pg = u >= KV8_BLOCK * PER_ROW ? 1 : 0;
+        const int p = pg ? page[1] : page[0];
+        to[j] = make_uint2(0, 0);
+        if (p >= 0)
+          to[j] = *reinterpret_cast<const uint2*>(
+              pool.code[side] + ((long long)p * pool.heads + head) * (KV8_BLOCK * DH) +
+              (u - pg * KV8_BLOCK * PER_ROW) * 8);
+      }
+    };
+    if (nb > 0) {
+#pragma unroll
+      for (int i = 0; i < PAGES; ++i) {
+        page[i] = page_of(PAGES * b0 + i, tid == 0);
+        ahead[i] = nb > 1 ? page_of(PAGES * (b0 + 1) + i, tid == 0) : -1;
+      }
+      fetch(0, kr);
+      fetch(1, vr);
+    }
+    for (int b = 0; b < nb; ++b) {
+      const int ks = b % C::KST, vs = b % C::VST;
+#pragma unroll
+      for (int i = 0; i < PAGES; ++i) {
+        page[i] = ahead[i];
+        ahead[i] = b + 2 < nb ? page_of(PAGES * (b0 + b + 2) + i, tid == 0) : -1;
+      }
+      if (ok) ok = mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+#pragma unroll
+      for (int j = 0; j < C::UNITS; ++j) {
+        const int u = tid + 128 * j, r = u / PER_ROW, c = u - r * PER_ROW;
+        const uint32_t tile = sk + ks * C::K_BYTES;
+        const uint32_t at = C::TAIL && c == 8
+                                ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
+                                : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4);
+        sts128(at, e4m3x2_f16x2(kr[j].x & 0xffffu), e4m3x2_f16x2(kr[j].x >> 16),
+               e4m3x2_f16x2(kr[j].y & 0xffffu), e4m3x2_f16x2(kr[j].y >> 16));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(k_full + 8 * ks);
+      if (b + 1 < nb) fetch(0, kr);
+      if (ok) ok = mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+#pragma unroll
+      for (int j = 0; j < C::UNITS; ++j) {
+        const int u = tid + 128 * j, r = u / PER_ROW, c = u - r * PER_ROW;
+        const uint32_t at = sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 +
+                            (((c ^ r) & 7) << 4);
+        sts128(at, codes_02(vr[j].x), codes_13(vr[j].x), codes_02(vr[j].y), codes_13(vr[j].y));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(v_full + 8 * vs);
+      if (b + 1 < nb) fetch(1, vr);
+    }
+  } else {
+    // -------------------------------------------------------------- softmax
+    const int x = warp >> 2, tr = threadIdx.x & 127;  // stream, row of its tile
+    const int ur = (two ? x * BQ : 0) + tr;           // row of the unit
+    const bool in = ur < rows;
+    const int query = int((row0 + (in ? ur : 0)) / group);
+    const int gh = int(row0 + (in ? ur : 0) - (long long)query * group);
+    // (rows past the unit's last see what it sees: their warp need not mask)
+    const int seen = !in ? reach : a.causal ? max(0, len - nq + query + 1) : len;
+    // ---- the row's queries, f16 over the power of two of their largest
+    int qe;
+    {
+      const bf16* q = a.q + (long long)(q0 + query) * a.ldq + (head * group + gh) * DH;
+      uint32_t top = 0;
+#pragma unroll
+      for (int c = 0; c < DH / 8; ++c) {
+        const uint4 v = in ? *reinterpret_cast<const uint4*>(q + 8 * c) : make_uint4(0, 0, 0, 0);
+        const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu),
+                                    __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+        top = max(top, max(m << 16, m & 0xffff0000u));
+      }
+      qe = min(int(top >> 23), 240);
+      const float f = __uint_as_float(uint32_t(254 - qe) << 23);
+      if (two || x == 0) {
+        const uint32_t tile = sq + (two ? x : 0) * C::Q_BYTES;
+#pragma unroll
+        for (int c = 0; c < DH / 8; ++c) {
+          const uint4 v = in ? *reinterpret_cast<const uint4*>(q + 8 * c) : make_uint4(0, 0, 0, 0);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          uint32_t h[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 y = unpack_bf16x2(w[j]);
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[j]) : "f"(y.y * f), "f"(y.x * f));
+          }
+          const uint32_t at = C::TAIL && c == 8
+                                  ? tile + BQ * 128 + tr * 32 + (((tr >> 2) & 1) << 4)
+                                  : tile + (c >> 3) * (BQ * 128) + tr * 128 + (((c ^ tr) & 7) << 4);
+          sts128(at, h[0], h[1], h[2], h[3]);
+        }
+        fence_proxy_async_smem();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+    }
+    const float unit = 1.4426950408889634f * rsqrtf(float(DH));  // scores in base 2
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + uint32_t(x * BKV) + lanes;
+    const uint32_t to = tmem + uint32_t(TM_O + x * C::ODIM) + lanes;
+    const int mine = two ? nb : (nb + 1 - x) / 2;  // this stream's key blocks
+    const auto block_of = [&](int i) { return b0 + (two ? i : 2 * i + x); };
+    const auto look_up = [&](int i, int* page) {
+#pragma unroll
+      for (int p = 0; p < PAGES; ++p)
+        page[p] = i < mine ? page_of(PAGES * block_of(i) + p, false) : -1;
+    };
+    const auto scales = [&](Info& d) {
+#pragma unroll
+      for (int p = 0; p < PAGES; ++p) {
+        d.k[p] = d.v[p] = 0;
+        if (d.page[p] >= 0) {
+          const long long at = (long long)d.page[p] * pool.heads + head;
+          d.k[p] = pool.scale[0][at];
+          d.v[p] = pool.scale[1][at];
+        }
+      }
+    };
+    Info now, next;
+    look_up(0, now.page);
+    scales(now);
+    look_up(1, next.page);
+    // (a row that sees nothing here needs no maximum)
+    const bool blind = seen <= block_of(0) * BKV;
+    float m = blind ? 0.f : -INFINITY, l = 0.f;
+    int ref = -1;  // value scale byte that O is in units of (-1: none yet)
+
+    for (int i = 0; i < mine; ++i) {
+      scales(next);
+      int ahead[PAGES];
+      look_up(i + 2, ahead);
+      if (ok) ok = mbar_sleep(s_full + 8 * x, i & 1, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      tc_fence_after();
+      const int key0 = block_of(i) * BKV;
+      // ---- per cache block: factor of the scores, exponent of the weights
+      float f[PAGES];
+      int vmax = -1;
+#pragma unroll
+      for (int p = 0; p < PAGES; ++p) {
+        const int e = qe + now.k[p] - 127;
+        f[p] = now.k[p] == 255 ? __uint_as_float(0x7fffffffu)
+               : e < 1         ? 0.f
+                               : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
+        if (now.page[p] >= 0 && now.v[p] < 255) vmax = max(vmax, now.v[p]);
+      }
+      // columns that the row sees: all of a block's, or those below `limit`
+      // (a missing block's none)
+      const int limit = seen - key0;
+      const bool here = now.page[0] >= 0 && now.page[PAGES - 1] >= 0;
+      const auto hidden = [&](int c) {
+        return c >= limit || (c < KV8_BLOCK ? now.page[0] : now.page[1]) < 0;
+      };
+      int raise_to = ref;
+      if (ref < 0 || vmax > ref + RAISE_VALUE) raise_to = vmax;  // (uniform in the stream)
+      // (no column hidden, no value scale far below the reference)
+      const bool whole = __all_sync(0xffffffffu, limit >= BKV && here) &&
+                         min(now.v[0], now.v[1]) - raise_to >= -60;
+      bool raise_max = m == -INFINITY;
+      uint32_t w[BKV / 2];
+      float sum;
+      for (bool again = false;; again = true) {
+        const bool shift = raise_to != ref;
+        if (__any_sync(0xffffffffu, raise_max) || shift) {
+          // ---- a new reference: the row's largest score (where asked for)
+          float top = m;
+#pragma unroll 1
+          for (int c0 = 0; c0 < BKV; c0 += 32) {
+            float s[32];
+            tmem_ld32(ts + c0, s);
+            const float fc = c0 < KV8_BLOCK ? f[0] : f[1];
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              const float y = s[c] * fc;
+              top = fmaxf(top, hidden(c0 + c) ? -INFINITY : y);
+            }
+          }
+          const float to_max = raise_max ? top : m;
+          float corr = to_max == -INFINITY ? 1.f : ex2_ftz(m - to_max);
+          l *= corr;
+          if (shift && ref >= 0) corr *= scale_value(max(127 + ref - raise_to, 0));
+          m = to_max;
+          ref = raise_to;
+          if (i > 0) {  // (S of this block is there, so O has every block before)
+#pragma unroll 1
+            for (int c0 = 0; c0 < C::ODIM; c0 += 16) {
+              uint32_t o[16];
+              tmem_ld16_nowait(to + c0, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
+              tmem_st16(to + c0, o);
+            }
+            tmem_wait_st();
+          }
+        }
+        // ---- weights 2^(score - m + value scale's exponent over ref's)
+        const float mm = m == -INFINITY ? 0.f : m;
+        sum = 0.f;
+        const auto weights = [&](auto fast) {
+#pragma unroll
+          for (int p = 0; p < PAGES; ++p) {
+            // (2^-126 is the least that bf16 weights can carry; the sum is
+            // taken from 2^-60 up, so that it keeps small weights)
+            const int d = max(now.v[p] - ref, -126);
+            const float dv = now.v[p] == 255 ? __uint_as_float(0x7fffffffu) : float(max(d, -60));
+            const float less = d < -60 ? scale_value(127 + d + 60) : 1.f;
+            const uint64_t ff = pair64(f[p], f[p]), sh = pair64(dv - mm, dv - mm);
+            uint64_t total = 0;
+#pragma unroll
+            for (int c0 = p * KV8_BLOCK; c0 < (p + 1) * KV8_BLOCK; c0 += 32) {
+              float s[32];
+              tmem_ld32(ts + c0, s);
+#pragma unroll
+              for (int c = 0; c < 32; c += 2) {
+                float2 y = split64(fma2(pair64(s[c], s[c + 1]), ff, sh));
+                if (!decltype(fast)::value) {
+                  if (hidden(c0 + c)) y.x = -INFINITY;
+                  if (hidden(c0 + c + 1)) y.y = -INFINITY;
+                }
+                y.x = ex2_ftz(y.x);
+                y.y = ex2_ftz(y.y);
+                total = add2(total, pair64(y.x, y.y));
+                if (!decltype(fast)::value) {
+                  y.x *= less;
+                  y.y *= less;
+                }
+                w[(c0 + c) / 2] = pack_bf16x2(y.x, y.y);
+              }
+            }
+            const float2 t = split64(total);
+            // (a block that the row sees nothing of adds nothing, whatever its scale)
+            if (limit > p * KV8_BLOCK && now.page[p] >= 0) sum += (t.x + t.y) * ex2_ftz(-dv);
+          }
+        };
+        if (whole) weights(Yes{});
+        else weights(No{});
+        raise_max = sum > RAISE_SUM;
+        if (again || !__any_sync(0xffffffffu, raise_max)) break;
+      }
+      l += sum;
+#pragma unroll
+      for (int c = 0; c < BKV / 2; c += 16) tmem_st16(ts + c, w + c);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + 8 * x);
+      now = next;
+#pragma unroll
+      for (int p = 0; p < PAGES; ++p) next.page[p] = ahead[p];
+    }
+
+    // ---- result: O of a row in f32, or its part to be joined
+    if (ok && mine > 0) ok = mbar_sleep_warp(o_full + 8 * x, 0, abort_flag);
+    ok = __all_sync(0xffffffffu, ok);
+    tc_fence_after();
+    const float back = ref < 0 ? 0.f : scale_value(ref);
+    const auto row_out = [&](int r) {
+      const int qi = int((row0 + r) / group), g = int(row0 + r - (long long)qi * group);
+      return a.o + (long long)(q0 + qi) * a.ldo + (head * group + g) * DH;
+    };
+    // eight channels from 8 c of O, in their order
+    const auto eight = [&](int c, float* v) {
+      uint32_t o[8];
+      tmem_ld8_nowait(to + 8 * c, o);
+      tmem_wait_ld();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[o_column(j)]) * back;
+    };
+    const auto put = [&](bf16* p, const float* v, float inv) {
+      *reinterpret_cast<uint4*>(p) =
+          make_uint4(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv),
+                     pack_bf16x2(v[4] * inv, v[5] * inv), pack_bf16x2(v[6] * inv, v[7] * inv));
+    };
+    if (two && parts == 1) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      bf16* p = row_out(in ? ur : 0);
+#pragma unroll
+      for (int c = 0; c < DH / 8; ++c) {
+        float v[8];
+        if (mine > 0) eight(c, v);
+        else
+          for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        if (in && ok) put(p + 8 * c, v, l == 0.f ? 0.f : inv);
+      }
+    } else {
+      // parts over the operands' memory, once every MMA has read it: per row
+      // its channels, its maximum, its sum.  One tile: both streams' parts of
+      // a row; two: each stream's own rows
+      soft_sync();
+      float* part_at = reinterpret_cast<float*>(smem) + (x * BQ + tr) * C::PSTRIDE;
+      for (int c = 0; c < DH / 8; ++c) {
+        float v[8];
+        if (mine > 0) eight(c, v);
+        else
+          for (int j = 0; j < 8; ++j) v[j] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part_at[8 * c + j] = v[j];
+      }
+      part_at[DH] = blind ? -INFINITY : m;
+      part_at[DH + 1] = l;
+      soft_sync();
+      if (parts > 1) cluster_sync();
+      // the row's parts: streams (one tile) of each CTA of the cluster
+      const int streams = two ? 1 : 2, n = streams * parts;
+      const uint32_t base = sq;
+      const auto at = [&](int k, int r, int c) {
+        const uint32_t p = base + 4 * (((two ? 0 : k % streams) * BQ + r) * C::PSTRIDE + c);
+        float v;
+        if (parts == 1)
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(p));
+        else
+          asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                       : "=f"(v)
+                       : "r"(mapa_shared(p, uint32_t(k / streams))));
+        return v;
+      };
+      for (int e = part * 256 + int(threadIdx.x); e < rows * (DH / 8); e += parts * 256) {
+        const int r = e / (DH / 8), c = (e - r * (DH / 8)) * 8;
+        float top = -INFINITY, total = 0.f, v[8] = {};
+        for (int k = 0; k < n; ++k) top = fmaxf(top, at(k, r, DH));
+        const float rf = top == -INFINITY ? 0.f : top;
+        for (int k = 0; k < n; ++k) {
+          const float y = ex2_ftz(at(k, r, DH) - rf);
+          total += y * at(k, r, DH + 1);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += y * at(k, r, c + j);
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (ok) put(row_out(r) + c, v, inv);
+      }
+    }
+  }
+  if (parts > 1 && warp >= CONV_WARP) cluster_sync();  // (as the softmax warps did)
+  if (!ok) {
+    *abort_flag = 1;
+    atomicOr(a.err, DEVERR_TIMEOUT);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (parts > 1) cluster_sync();  // (no CTA leaves while its parts may be read)
+  if (warp == MMA_WARP) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+template <int DH>
+cudaError_t many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
+  using C = MCfg<DH>;
+  RC_TRY(cudaFuncSetAttribute(many_rows_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              int(C::SMEM)));
+  const int unit_rows = 256, parts = 1;
+  const long long rows = (long long)a.max_q * (a.heads / pool.heads);
+  const long long chunks = (rows + unit_rows - 1) / unit_rows;
+  if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
+  const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
+  count_launches(1);
+  return launch_k_cluster(many_rows_kernel<DH>, grid, dim3(THREADS), C::SMEM, parts, st, pool, a,
+                          parts, unit_rows);
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
+  switch (pool.dh) {
+    case 64: return many<64>(pool, a, st);
+    case 72: return many<72>(pool, a, st);
+    default: return many<128>(pool, a, st);
+  }
+}
+
+}  // namespace rc
