@@ -6,20 +6,24 @@
 // 128 tokens (two cache blocks), or one tile whose key blocks two streams take
 // in turn.  A cluster of CTAs may share the unit's keys.
 //   warps 0-3, 4-7   softmax of a stream, one thread a row: S from tensor
-//                    memory, weights back over it as bf16
-//   warps 8-11       codes from global memory to registers, to operands in
-//                    shared memory: keys as f16 (exact, K-major), values as
-//                    bf16 (exact, MN-major), both with the 128-byte swizzle
+//                    memory, weights back over it as bf16, a cache block (64
+//                    tokens) at a time, so that P V of the first half runs
+//                    beside the second half's exponentials
+//   warps 8-11       codes to operands in shared memory: keys as f16 (exact,
+//                    K-major), values as bf16 (exact, MN-major), both with the
+//                    128-byte swizzle
 //   warp 12          issues S = Q K^T (kind f16) and O += P V (kind bf16)
+//   warp 13          bulk copies of the codes into a ring ahead of warps 8-11
 // Each code is converted once for 256 rows, so its four instructions or so
 // stay beside the softmax; a pass that wrote bf16 copies for the kernel of
 // rc_attention would move five bytes for each one.  Q is f16 over the power of
-// two of its row's largest magnitude.  A block's key scale joins the factor of
-// its scores, its value scale the exponent of its weights (relative to a
-// reference kept per stream), so that both cost nothing per element; bf16
-// weights have f32's range, so neither can underflow f32's neighbours.
-// The maximum is taken in a row's first block only: later blocks use the same
-// reference unless their weights' sum passes 2^64 (or a value scale passes
+// two of its row's largest magnitude, and stays in tensor memory where that
+// has room (head_dim 64 and 72: then an MMA reads only the keys from shared
+// memory).  A block's key scale joins the factor of its scores, its value
+// scale the exponent of its weights (relative to a reference kept per stream),
+// so that both cost nothing per element; bf16 weights have f32's range.
+// The maximum is taken in a row's first cache block only: later ones use the
+// same reference unless their weights' sum passes 2^64 (or a value scale passes
 // 2^40 of its reference); then it is raised, O rescaled, the block done again.
 #include <math.h>
 
@@ -34,10 +38,11 @@ namespace {
 
 using namespace rc::tc;
 
-constexpr int BQ = 128, BKV = 128, THREADS = 416;
-constexpr int CONV_WARP = 8, MMA_WARP = 12;
+constexpr int BQ = 128, BKV = 128, THREADS = 448;
+constexpr int CONV_WARP = 8, MMA_WARP = 12, LOAD_WARP = 13;
 constexpr int PAGES = BKV / KV8_BLOCK;
-constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;  // S (P over it) of each stream, then O
+// S (P over it) of each stream, then O, then Q where it fits
+constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;
 constexpr float RAISE_SUM = 18446744073709551616.f;  // 2^64
 constexpr int RAISE_VALUE = 40;
 
@@ -47,17 +52,24 @@ struct MCfg {
   static constexpr int ATOMS = (DH + 63) / 64;       // 64-channel parts of a V row
   static constexpr int FULL = DH / 64;               // 64-channel parts of a K row
   static constexpr int ODIM = TAIL ? 80 : DH;        // columns of O
-  static constexpr int Q_BYTES = FULL * BQ * 128 + (TAIL ? BQ * 32 : 0);
+  static constexpr int KSTEPS = (DH + 15) / 16;
+  static constexpr int TM_Q = TM_O + 2 * ODIM, Q_COLS = 8 * KSTEPS;
+  static constexpr bool Q_TMEM = TM_Q + 2 * Q_COLS <= TMEM_COLS;
+  static constexpr int Q_BYTES = Q_TMEM ? 0 : FULL * BQ * 128;
   static constexpr int K_BYTES = FULL * BKV * 128 + (TAIL ? BKV * 32 : 0);
   static constexpr int V_BYTES = ATOMS * BKV * 128;
   static constexpr int KST = DH == 128 ? 2 : 3, VST = DH == 128 ? 2 : 3;
-  static constexpr int RING = 2 * Q_BYTES + KST * K_BYTES + VST * V_BYTES;
+  // codes of a key block's keys, then its values, .. in a ring
+  static constexpr int RAW_BYTES = BKV * DH, RAWS = DH == 128 ? 2 : 4;
+  static constexpr int OPERANDS = 2 * Q_BYTES + KST * K_BYTES + VST * V_BYTES;
+  static constexpr int RING = OPERANDS + RAWS * RAW_BYTES;
   static constexpr size_t SMEM = size_t(RING) + 1024 + 256;
   static constexpr int UNITS = BKV * DH / 8 / 128;   // 8-code pieces of K (or V) a thread
   static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(BKV >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) |
                                        (uint32_t(ODIM >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr int PSTRIDE = DH + 2;             // floats of a partial row
+  static_assert(Q_TMEM || !TAIL, "queries in shared memory have no tail");
   static_assert(2 * BQ * PSTRIDE * 4 <= RING, "the parts fit the operands' memory");
   static_assert(TM_O + 2 * ODIM <= TMEM_COLS, "tensor memory");
 };
@@ -110,6 +122,19 @@ __device__ __forceinline__ constexpr int o_column(int c) {
 
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
+                                          uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+          "r"(dst), "l"(src), "r"(bytes), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
@@ -131,8 +156,13 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   const uint32_t bar = saddr(bars);
   const uint32_t k_full = bar, k_empty = k_full + 8 * C::KST, v_full = k_empty + 8 * C::KST;
   const uint32_t v_empty = v_full + 8 * C::VST, s_full = v_empty + 8 * C::VST;
-  const uint32_t p_full = s_full + 16, o_full = p_full + 16, q_full = o_full + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::KST + 2 * C::VST + 7);
+  // (a stream's softmax may hand over both halves of its weights before either
+  // is waited for, so each half has a barrier)
+  const uint32_t p_full = s_full + 16, o_done = p_full + 16 * PAGES, o_full = o_done + 16;
+  const uint32_t q_full = o_full + 16, raw_full = q_full + 8, raw_empty = raw_full + 8 * C::RAWS;
+  const uint32_t raw = sq + C::OPERANDS;
+  uint32_t* tmem_slot =
+      reinterpret_cast<uint32_t*>(bars + 2 * C::KST + 2 * C::VST + 7 + 2 * PAGES + 2 * C::RAWS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = warp_index(), lane = threadIdx.x & 31;
 
@@ -140,7 +170,8 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   pdl_trigger();
   const int part = parts > 1 ? int(cluster_ctarank()) : 0;
   const int group = a.heads / pool.heads;
-  const int head = blockIdx.y % pool.heads, chunk = blockIdx.y / pool.heads, req = blockIdx.z;
+  // (a request's last chunk, which may be short, among the last to start)
+  const int head = blockIdx.z % pool.heads, chunk = blockIdx.z / pool.heads, req = blockIdx.y;
   const int q0 = a.offsets[req], nq = a.offsets[req + 1] - q0, len = a.lengths[req];
   // (the same for every CTA of a cluster)
   if (q0 < 0 || nq < 0 || nq > a.max_q || q0 > a.q_rows - nq || len < 0 ||
@@ -165,18 +196,22 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(s_full + 8 * x, 1);
-      mbar_init(p_full + 8 * x, 4);
+      for (int h = 0; h < PAGES; ++h) mbar_init(p_full + 16 * h + 8 * x, 4);
+      mbar_init(o_done + 8 * x, 1);
       mbar_init(o_full + 8 * x, 1);
+    }
+    for (int i = 0; i < C::RAWS; ++i) {
+      mbar_init(raw_full + 8 * i, 1);
+      mbar_init(raw_empty + 8 * i, 4);
     }
     mbar_init(q_full, 8);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (C::TAIL) {  // channels 72 .. 79 of the products are zeros
-    for (int i = threadIdx.x; i < 2 * BQ * 2; i += THREADS)
-      sts128(sq + (i / (2 * BQ)) * C::Q_BYTES + BQ * 128 + (i % (2 * BQ)) * 16, 0, 0, 0, 0);
     for (int i = threadIdx.x; i < C::KST * BKV * 2; i += THREADS)
       sts128(sk + (i / (2 * BKV)) * C::K_BYTES + BKV * 128 + (i % (2 * BKV)) * 16, 0, 0, 0, 0);
+    fence_proxy_async_smem();
   }
   if (warp == MMA_WARP) tmem_alloc(saddr(tmem_slot), TMEM_COLS);
   tc_fence_before();
@@ -211,17 +246,23 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
         if ((!two || x == 0) &&
             !mbar_wait(k_full + 8 * st, (b / C::KST) & 1, abort_flag)) return false;
         tc_fence_after();
-        const uint32_t q = sq + (two ? x : 0) * C::Q_BYTES, k = sk + st * C::K_BYTES;
-        const uint32_t d = tmem + uint32_t(x * BKV);
-#pragma unroll
-        for (int f = 0; f < C::FULL; ++f)
+        const uint32_t k = sk + st * C::K_BYTES, d = tmem + uint32_t(x * BKV);
+        const int tile = two ? x : 0;
+        if constexpr (C::Q_TMEM) {
+          const uint32_t q = tmem + uint32_t(C::TM_Q + tile * C::Q_COLS);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            umma_bf16(d, sw128_desc(q + f * BQ * 128) + 2 * kk,
-                      sw128_desc(k + f * BKV * 128) + 2 * kk, C::IDESC_S, (f | kk) ? 1u : 0u);
-        if (C::TAIL)
-          umma_bf16(d, sw32_kmajor_desc(q + BQ * 128), sw32_kmajor_desc(k + BKV * 128), C::IDESC_S,
-                    1u);
+            umma_bf16_ta(d, q + 8 * kk, sw128_desc(k) + 2 * kk, C::IDESC_S, kk ? 1u : 0u);
+          if (C::TAIL) umma_bf16_ta(d, q + 32, sw32_kmajor_desc(k + BKV * 128), C::IDESC_S, 1u);
+        } else {
+          const uint32_t q = sq + tile * C::Q_BYTES;
+#pragma unroll
+          for (int f = 0; f < C::FULL; ++f)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              umma_bf16(d, sw128_desc(q + f * BQ * 128) + 2 * kk,
+                        sw128_desc(k + f * BKV * 128) + 2 * kk, C::IDESC_S, (f | kk) ? 1u : 0u);
+        }
         umma_commit(s_full + 8 * x);
         if (!two || x == 1) umma_commit(k_empty + 8 * st);
         return true;
@@ -229,84 +270,90 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       ok = mbar_wait(q_full, 0, abort_flag) && scores(0) && (events < 2 || scores(1));
       for (int e = 0; ok && e < events; ++e) {
         const int x = e & 1, b = two ? e >> 1 : e, i = e >> 1, st = b % C::VST;
-        if (((!two || x == 0) && !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
-            !mbar_wait(p_full + 8 * x, i & 1, abort_flag)) { ok = false; break; }
-        tc_fence_after();
         const uint32_t d = tmem + uint32_t(TM_O + x * C::ODIM), p = tmem + uint32_t(x * BKV);
         const uint64_t v = sw128_mnmajor_desc_lbo(sv + st * C::V_BYTES, BKV * 128);
 #pragma unroll
-        for (int kk = 0; kk < BKV / 16; ++kk)
-          umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | kk) ? 1u : 0u);
+        for (int h = 0; h < PAGES; ++h) {
+          if ((h == 0 && (!two || x == 0) &&
+               !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
+              !mbar_wait(p_full + 16 * h + 8 * x, i & 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int kk = 4 * h; kk < 4 * h + 4; ++kk)
+            umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | kk) ? 1u : 0u);
+          umma_commit(o_done + 8 * x);
+        }
+        if (!ok) break;
         if (!two || x == 1) umma_commit(v_empty + 8 * st);
         if (e + 2 >= events) umma_commit(o_full + 8 * x);
         else if (!scores(e + 2)) ok = false;
       }
     }
+  } else if (warp == LOAD_WARP) {
+    // ------------------------------------------------------------- loading
+    // (the copies are whole cache blocks; one that is missing is left out:
+    // what it leaves in the ring is hidden by the softmax)
+    if (elect_one()) {
+      int page[PAGES];
+      for (int j = 0; ok && j < 2 * nb; ++j) {
+        const int st = j % C::RAWS, side = j & 1;
+        if (side == 0)
+#pragma unroll
+          for (int i = 0; i < PAGES; ++i) page[i] = page_of(PAGES * (b0 + (j >> 1)) + i, true);
+        if (!mbar_wait(raw_empty + 8 * st, ((j / C::RAWS) & 1) ^ 1, abort_flag)) { ok = false; break; }
+        constexpr uint32_t BYTES = KV8_BLOCK * DH;
+        mbar_expect_tx(raw_full + 8 * st,
+                       BYTES * ((page[0] >= 0 ? 1u : 0u) + (page[1] >= 0 ? 1u : 0u)));
+#pragma unroll
+        for (int i = 0; i < PAGES; ++i)
+          if (page[i] >= 0)
+            bulk_load(raw + st * C::RAW_BYTES + i * BYTES,
+                      pool.code[side] + ((long long)page[i] * pool.heads + head) * BYTES, BYTES,
+                      raw_full + 8 * st);
+      }
+    }
   } else if (warp >= CONV_WARP) {
     // ---------------------------------------------------------- conversion
     // Thread `tid` takes the 8-code pieces tid + 128 j of the block's 128
-    // rows (piece c of row r: 8 channels); a cache block's rows are one run.
+    // rows (piece c of row r: 8 channels).
     const int tid = int(threadIdx.x) - CONV_WARP * 32;
     constexpr int PER_ROW = DH / 8;
-    uint2 kr[C::UNITS], vr[C::UNITS];
-    int page[PAGES], ahead[PAGES];
-    const auto fetch = [&](int side, uint2* to) {
-#pragma unroll
-      for (int j = 0; j < C::UNITS; ++j) {
-        const int u = tid + 128 * j, pg = u >= KV8_BLOCK * PER_ROW ? 1 : 0;
-        const int p = pg ? page[1] : page[0];
-        to[j] = make_uint2(0, 0);
-        if (p >= 0)
-          to[j] = *reinterpret_cast<const uint2*>(
-              pool.code[side] + ((long long)p * pool.heads + head) * (KV8_BLOCK * DH) +
-              (u - pg * KV8_BLOCK * PER_ROW) * 8);
-      }
-    };
-    if (nb > 0) {
-#pragma unroll
-      for (int i = 0; i < PAGES; ++i) {
-        page[i] = page_of(PAGES * b0 + i, tid == 0);
-        ahead[i] = nb > 1 ? page_of(PAGES * (b0 + 1) + i, tid == 0) : -1;
-      }
-      fetch(0, kr);
-      fetch(1, vr);
-    }
-    for (int b = 0; b < nb; ++b) {
-      const int ks = b % C::KST, vs = b % C::VST;
-#pragma unroll
-      for (int i = 0; i < PAGES; ++i) {
-        page[i] = ahead[i];
-        ahead[i] = b + 2 < nb ? page_of(PAGES * (b0 + b + 2) + i, tid == 0) : -1;
-      }
-      if (ok) ok = mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag);
+    for (int j = 0; j < 2 * nb; ++j) {
+      const int b = j >> 1, st = j % C::RAWS, ks = b % C::KST, vs = b % C::VST;
+      if (ok)
+        ok = mbar_sleep(raw_full + 8 * st, (j / C::RAWS) & 1, abort_flag) &&
+             (j & 1 ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
+                    : mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag));
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      const uint32_t from = raw + st * C::RAW_BYTES + 8 * tid;
+      if ((j & 1) == 0) {
 #pragma unroll
-      for (int j = 0; j < C::UNITS; ++j) {
-        const int u = tid + 128 * j, r = u / PER_ROW, c = u - r * PER_ROW;
-        const uint32_t tile = sk + ks * C::K_BYTES;
-        const uint32_t at = C::TAIL && c == 8
-                                ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
-                                : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4);
-        sts128(at, e4m3x2_f16x2(kr[j].x & 0xffffu), e4m3x2_f16x2(kr[j].x >> 16),
-               e4m3x2_f16x2(kr[j].y & 0xffffu), e4m3x2_f16x2(kr[j].y >> 16));
+        for (int i = 0; i < C::UNITS; ++i) {
+          const int u = tid + 128 * i, r = u / PER_ROW, c = u - r * PER_ROW;
+          const uint2 q = lds64(from + 1024 * i);
+          const uint32_t tile = sk + ks * C::K_BYTES;
+          const uint32_t at = C::TAIL && c == 8
+                                  ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
+                                  : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4);
+          sts128(at, e4m3x2_f16x2(q.x & 0xffffu), e4m3x2_f16x2(q.x >> 16),
+                 e4m3x2_f16x2(q.y & 0xffffu), e4m3x2_f16x2(q.y >> 16));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < C::UNITS; ++i) {
+          const int u = tid + 128 * i, r = u / PER_ROW, c = u - r * PER_ROW;
+          const uint2 q = lds64(from + 1024 * i);
+          const uint32_t at = sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 +
+                              (((c ^ r) & 7) << 4);
+          sts128(at, codes_02(q.x), codes_13(q.x), codes_02(q.y), codes_13(q.y));
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(k_full + 8 * ks);
-      if (b + 1 < nb) fetch(0, kr);
-      if (ok) ok = mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-#pragma unroll
-      for (int j = 0; j < C::UNITS; ++j) {
-        const int u = tid + 128 * j, r = u / PER_ROW, c = u - r * PER_ROW;
-        const uint32_t at = sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 +
-                            (((c ^ r) & 7) << 4);
-        sts128(at, codes_02(vr[j].x), codes_13(vr[j].x), codes_02(vr[j].y), codes_13(vr[j].y));
+      if (lane == 0) {
+        mbar_arrive(raw_empty + 8 * st);
+        mbar_arrive(j & 1 ? v_full + 8 * vs : k_full + 8 * ks);
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(v_full + 8 * vs);
-      if (b + 1 < nb) fetch(1, vr);
     }
   } else {
     // -------------------------------------------------------------- softmax
@@ -332,23 +379,36 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       qe = min(int(top >> 23), 240);
       const float f = __uint_as_float(uint32_t(254 - qe) << 23);
       if (two || x == 0) {
-        const uint32_t tile = sq + (two ? x : 0) * C::Q_BYTES;
 #pragma unroll
-        for (int c = 0; c < DH / 8; ++c) {
-          const uint4 v = in ? *reinterpret_cast<const uint4*>(q + 8 * c) : make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-          uint32_t h[4];
+        for (int c = 0; c < C::KSTEPS; ++c) {  // sixteen channels
+          uint32_t h[8] = {};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 y = unpack_bf16x2(w[j]);
-            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[j]) : "f"(y.y * f), "f"(y.x * f));
+          for (int k = 0; k < 2; ++k) {
+            if (16 * c + 8 * k >= DH) continue;
+            const uint4 v = in ? *reinterpret_cast<const uint4*>(q + 16 * c + 8 * k)
+                               : make_uint4(0, 0, 0, 0);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 y = unpack_bf16x2(w[j]);
+              asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h[4 * k + j]) : "f"(y.y * f), "f"(y.x * f));
+            }
           }
-          const uint32_t at = C::TAIL && c == 8
-                                  ? tile + BQ * 128 + tr * 32 + (((tr >> 2) & 1) << 4)
-                                  : tile + (c >> 3) * (BQ * 128) + tr * 128 + (((c ^ tr) & 7) << 4);
-          sts128(at, h[0], h[1], h[2], h[3]);
+          if constexpr (C::Q_TMEM) {
+            tmem_st8(tmem + uint32_t(C::TM_Q + (two ? x : 0) * C::Q_COLS + 8 * c) +
+                         (uint32_t((warp & 3) * 32) << 16), h);
+          } else {
+            const uint32_t row = sq + (two ? x : 0) * C::Q_BYTES + (c >> 2) * (BQ * 128) + tr * 128;
+            sts128(row + (((2 * c) ^ tr) & 7) * 16, h[0], h[1], h[2], h[3]);
+            sts128(row + (((2 * c + 1) ^ tr) & 7) * 16, h[4], h[5], h[6], h[7]);
+          }
         }
-        fence_proxy_async_smem();
+        if (C::Q_TMEM) {
+          tmem_wait_st();
+          tc_fence_before();
+        } else {
+          fence_proxy_async_smem();
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
@@ -391,91 +451,84 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       if (ok) ok = mbar_sleep(s_full + 8 * x, i & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-      const int key0 = block_of(i) * BKV;
-      // ---- per cache block: factor of the scores, exponent of the weights
-      float f[PAGES];
-      int vmax = -1;
-#pragma unroll
-      for (int p = 0; p < PAGES; ++p) {
-        const int e = qe + now.k[p] - 127;
-        f[p] = now.k[p] == 255 ? __uint_as_float(0x7fffffffu)
-               : e < 1         ? 0.f
-                               : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
-        if (now.page[p] >= 0 && now.v[p] < 255) vmax = max(vmax, now.v[p]);
-      }
-      // columns that the row sees: all of a block's, or those below `limit`
-      // (a missing block's none)
-      const int limit = seen - key0;
-      const bool here = now.page[0] >= 0 && now.page[PAGES - 1] >= 0;
-      const auto hidden = [&](int c) {
-        return c >= limit || (c < KV8_BLOCK ? now.page[0] : now.page[1]) < 0;
-      };
-      int raise_to = ref;
-      if (ref < 0 || vmax > ref + RAISE_VALUE) raise_to = vmax;  // (uniform in the stream)
-      // (no column hidden, no value scale far below the reference)
-      const bool whole = __all_sync(0xffffffffu, limit >= BKV && here) &&
-                         min(now.v[0], now.v[1]) - raise_to >= -60;
-      bool raise_max = m == -INFINITY;
-      uint32_t w[BKV / 2];
-      float sum;
-      for (bool again = false;; again = true) {
-        const bool shift = raise_to != ref;
-        if (__any_sync(0xffffffffu, raise_max) || shift) {
-          // ---- a new reference: the row's largest score (where asked for)
-          float top = m;
 #pragma unroll 1
-          for (int c0 = 0; c0 < BKV; c0 += 32) {
-            float s[32];
-            tmem_ld32(ts + c0, s);
-            const float fc = c0 < KV8_BLOCK ? f[0] : f[1];
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              const float y = s[c] * fc;
-              top = fmaxf(top, hidden(c0 + c) ? -INFINITY : y);
-            }
-          }
-          const float to_max = raise_max ? top : m;
-          float corr = to_max == -INFINITY ? 1.f : ex2_ftz(m - to_max);
-          l *= corr;
-          if (shift && ref >= 0) corr *= scale_value(max(127 + ref - raise_to, 0));
-          m = to_max;
-          ref = raise_to;
-          if (i > 0) {  // (S of this block is there, so O has every block before)
+      for (int h = 0; h < PAGES; ++h) {
+        // ---- a cache block: factor of its scores, exponent of its weights
+        const int page = h ? now.page[1] : now.page[0];
+        const int bk = h ? now.k[1] : now.k[0], bv = h ? now.v[1] : now.v[0];
+        const int e = qe + bk - 127;
+        const float f = bk == 255 ? __uint_as_float(0x7fffffffu)
+                        : e < 1   ? 0.f
+                                  : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
+        const uint32_t s_at = ts + uint32_t(h * KV8_BLOCK);
+        // columns that the row sees: those below `limit`
+        const int limit = page < 0 ? 0 : seen - block_of(i) * BKV - h * KV8_BLOCK;
+        // (the reference of value scales, like all of this but seen, is the
+        // same for every row of the stream)
+        int raise_to = ref;
+        if (page >= 0 && bv < 255 && (ref < 0 || bv > ref + RAISE_VALUE)) raise_to = bv;
+        bool raise_max = m == -INFINITY;
+        // no column hidden, no value scale far below the reference
+        const bool whole =
+            __all_sync(0xffffffffu, limit >= KV8_BLOCK) && (bv == 255 || bv - raise_to >= -60);
+        uint32_t w[KV8_BLOCK / 2];
+        float sum;
+        for (bool again = false;; again = true) {
+          if (__any_sync(0xffffffffu, raise_max) || raise_to != ref) {
+            // ---- a new reference: the row's largest score (where asked for)
+            float top = m;
 #pragma unroll 1
-            for (int c0 = 0; c0 < C::ODIM; c0 += 16) {
-              uint32_t o[16];
-              tmem_ld16_nowait(to + c0, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
-              tmem_st16(to + c0, o);
-            }
-            tmem_wait_st();
-          }
-        }
-        // ---- weights 2^(score - m + value scale's exponent over ref's)
-        const float mm = m == -INFINITY ? 0.f : m;
-        sum = 0.f;
-        const auto weights = [&](auto fast) {
-#pragma unroll
-          for (int p = 0; p < PAGES; ++p) {
-            // (2^-126 is the least that bf16 weights can carry; the sum is
-            // taken from 2^-60 up, so that it keeps small weights)
-            const int d = max(now.v[p] - ref, -126);
-            const float dv = now.v[p] == 255 ? __uint_as_float(0x7fffffffu) : float(max(d, -60));
-            const float less = d < -60 ? scale_value(127 + d + 60) : 1.f;
-            const uint64_t ff = pair64(f[p], f[p]), sh = pair64(dv - mm, dv - mm);
-            uint64_t total = 0;
-#pragma unroll
-            for (int c0 = p * KV8_BLOCK; c0 < (p + 1) * KV8_BLOCK; c0 += 32) {
+            for (int c0 = 0; c0 < KV8_BLOCK; c0 += 32) {
               float s[32];
-              tmem_ld32(ts + c0, s);
+              tmem_ld32(s_at + c0, s);
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                top = fmaxf(top, c0 + c < limit ? s[c] * f : -INFINITY);
+            }
+            const float to_max = raise_max ? top : m;
+            float corr = to_max == -INFINITY ? 1.f : ex2_ftz(m - to_max);
+            l *= corr;
+            if (raise_to != ref && ref >= 0) corr *= scale_value(max(127 + ref - raise_to, 0));
+            m = to_max;
+            ref = raise_to;
+            // once the P V before has ended (its phase is 2 i + h - 1, and the next
+            // one's weights are not there yet)
+            if (i + h > 0) {
+              if (ok) ok = mbar_wait(o_done + 8 * x, h ^ 1, abort_flag);
+              ok = __all_sync(0xffffffffu, ok);
+              tc_fence_after();
+#pragma unroll 1
+              for (int c0 = 0; c0 < C::ODIM; c0 += 16) {
+                uint32_t o[16];
+                tmem_ld16_nowait(to + c0, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
+                tmem_st16(to + c0, o);
+              }
+              tmem_wait_st();
+            }
+          }
+          // ---- weights 2^(score - m + value scale's exponent over ref's);
+          // 2^-126 is the least that bf16 weights can carry, and the sum is
+          // taken from 2^-60 up, so that it keeps small weights
+          const float mm = m == -INFINITY ? 0.f : m;
+          const int d = max(bv - ref, -126);
+          const float dv = bv == 255 ? __uint_as_float(0x7fffffffu) : float(max(d, -60));
+          const uint64_t ff = pair64(f, f), sh = pair64(dv - mm, dv - mm);
+          uint64_t total = 0;
+          const auto weights = [&](auto fast) {
+            const float less = d < -60 ? scale_value(127 + d + 60) : 1.f;
+#pragma unroll
+            for (int c0 = 0; c0 < KV8_BLOCK; c0 += 32) {
+              float s[32];
+              tmem_ld32(s_at + c0, s);
 #pragma unroll
               for (int c = 0; c < 32; c += 2) {
                 float2 y = split64(fma2(pair64(s[c], s[c + 1]), ff, sh));
                 if (!decltype(fast)::value) {
-                  if (hidden(c0 + c)) y.x = -INFINITY;
-                  if (hidden(c0 + c + 1)) y.y = -INFINITY;
+                  if (c0 + c >= limit) y.x = -INFINITY;
+                  if (c0 + c + 1 >= limit) y.y = -INFINITY;
                 }
                 y.x = ex2_ftz(y.x);
                 y.y = ex2_ftz(y.y);
@@ -487,23 +540,23 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
                 w[(c0 + c) / 2] = pack_bf16x2(y.x, y.y);
               }
             }
-            const float2 t = split64(total);
-            // (a block that the row sees nothing of adds nothing, whatever its scale)
-            if (limit > p * KV8_BLOCK && now.page[p] >= 0) sum += (t.x + t.y) * ex2_ftz(-dv);
-          }
-        };
-        if (whole) weights(Yes{});
-        else weights(No{});
-        raise_max = sum > RAISE_SUM;
-        if (again || !__any_sync(0xffffffffu, raise_max)) break;
+          };
+          if (whole) weights(Yes{});
+          else weights(No{});
+          const float2 t = split64(total);
+          // (a block that the row sees nothing of adds nothing, whatever its scale)
+          sum = limit > 0 ? (t.x + t.y) * ex2_ftz(-dv) : 0.f;
+          raise_max = sum > RAISE_SUM;
+          if (again || !__any_sync(0xffffffffu, raise_max)) break;
+        }
+        l += sum;
+        tmem_st16(ts + uint32_t(h * (KV8_BLOCK / 2)), w);
+        tmem_st16(ts + uint32_t(h * (KV8_BLOCK / 2) + 16), w + 16);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 16 * h + 8 * x);
       }
-      l += sum;
-#pragma unroll
-      for (int c = 0; c < BKV / 2; c += 16) tmem_st16(ts + c, w + c);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_full + 8 * x);
       now = next;
 #pragma unroll
       for (int p = 0; p < PAGES; ++p) next.page[p] = ahead[p];
@@ -614,7 +667,7 @@ cudaError_t many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   const long long rows = (long long)a.max_q * (a.heads / pool.heads);
   const long long chunks = (rows + unit_rows - 1) / unit_rows;
   if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
-  const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
+  const dim3 grid(unsigned(parts), unsigned(a.n), unsigned(chunks * pool.heads));
   count_launches(1);
   return launch_k_cluster(many_rows_kernel<DH>, grid, dim3(THREADS), C::SMEM, parts, st, pool, a,
                           parts, unit_rows);
