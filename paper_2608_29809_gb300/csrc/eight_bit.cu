@@ -190,6 +190,8 @@ rc_status rc_kv8_attention(rc_ctx* c, const rc_kv8* pool, const void* Q, int ldq
                 "%s: %d rows, max_q %d, %d requests (at most %d), ld_table %d, ldq %d, ldo %d "
                 "(multiples of 8, >= %d)", fn, q_rows, max_q, n, RC_KV8_MAX_REQUESTS, ld_table,
                 ldq, ldo, heads * p.dh);
+  if ((long long)q_rows * (heads / p.heads) > 0x7fffffffLL)
+    return fail(RC_ERR_SHAPE, "%s: %d rows of %d heads a key head", fn, q_rows, heads / p.heads);
   if (q_rows == 0 || max_q == 0 || n == 0) return RC_OK;
   if (!Q || !O || !row_offsets || !lengths || !table)
     return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);

@@ -9,11 +9,11 @@
 //                    memory, weights back over it as bf16, a cache block (64
 //                    tokens) at a time, so that P V of the first half runs
 //                    beside the second half's exponentials
-//   warps 8-11       codes to operands in shared memory: keys as f16 (exact,
-//                    K-major), values as bf16 (exact, MN-major), both with the
-//                    128-byte swizzle
-//   warp 12          issues S = Q K^T (kind f16) and O += P V (kind bf16)
-//   warp 13          bulk copies of the codes into a ring ahead of warps 8-11
+//   warps 8-10       key codes to operands in shared memory: f16 (exact),
+//                    K-major, 128-byte swizzle
+//   warps 12-14      value codes: bf16 (exact), MN-major, 128-byte swizzle
+//   warp 11          issues S = Q K^T (kind f16) and O += P V (kind bf16)
+//   warp 15          bulk copies of the codes into a ring ahead of the converters
 // Each code is converted once for 256 rows, so its four instructions or so
 // stay beside the softmax; a pass that wrote bf16 copies for the kernel of
 // rc_attention would move five bytes for each one.  Q is f16 over the power of
@@ -38,8 +38,13 @@ namespace {
 
 using namespace rc::tc;
 
-constexpr int BQ = 128, BKV = 128, THREADS = 448;
-constexpr int CONV_WARP = 8, MMA_WARP = 12, LOAD_WARP = 13;
+constexpr int BQ = 128, BKV = 128, THREADS = 512;
+// (warpgroups 2 and 3: three converting warps each, of keys and of values, and
+// one of these)
+constexpr int CONV_WARP = 8, MMA_WARP = 11, LOAD_WARP = 15, CONV_THREADS = 96;
+// Registers: 512 threads are launched with 128 each; the softmax's two
+// warpgroups take 160, the other two keep 96.
+constexpr int SOFT_REGS = 160, OTHER_REGS = 96;
 constexpr int PAGES = BKV / KV8_BLOCK;
 // S (P over it) of each stream, then O, then Q where it fits
 constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;
@@ -64,7 +69,8 @@ struct MCfg {
   static constexpr int OPERANDS = 2 * Q_BYTES + KST * K_BYTES + VST * V_BYTES;
   static constexpr int RING = OPERANDS + RAWS * RAW_BYTES;
   static constexpr size_t SMEM = size_t(RING) + 1024 + 256;
-  static constexpr int UNITS = BKV * DH / 8 / 128;   // 8-code pieces of K (or V) a thread
+  static constexpr int PER_ROW = DH / 8;             // 8-code pieces of a row
+  static constexpr int PASS = CONV_THREADS / PER_ROW;  // rows converted at a time
   static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(BKV >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) |
                                        (uint32_t(ODIM >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
@@ -135,8 +141,33 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
   return v;
 }
 
-struct Yes { static constexpr bool value = true; };
-struct No { static constexpr bool value = false; };
+// A row's 64 scores s to weights 2^(s f + shift), two a word as bf16 in the
+// first half of r (times `less`, where FAST is false: then columns from `limit`
+// on are hidden).  Returns their sum before that, in two parts.  In place: the
+// registers are what a row's scores leave.
+template <bool FAST>
+__device__ __forceinline__ float2 weights(uint32_t* r, float f, float shift, int limit,
+                                          float less) {
+  const uint64_t ff = pair64(f, f), sh = pair64(shift, shift);
+  uint64_t total[2] = {0, 0};
+#pragma unroll
+  for (int c = 0; c < KV8_BLOCK; c += 2) {
+    float2 y = split64(fma2(pair64(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), ff, sh));
+    if (!FAST) {
+      if (c >= limit) y.x = -INFINITY;
+      if (c + 1 >= limit) y.y = -INFINITY;
+    }
+    y.x = ex2_ftz(y.x);
+    y.y = ex2_ftz(y.y);
+    total[(c >> 1) & 1] = add2(total[(c >> 1) & 1], pair64(y.x, y.y));
+    if (!FAST) {
+      y.x *= less;
+      y.y *= less;
+    }
+    r[c >> 1] = pack_bf16x2(y.x, y.y);
+  }
+  return split64(add2(total[0], total[1]));
+}
 
 // Blocks and scale bytes of the two cache blocks of a key block.
 struct Info {
@@ -179,19 +210,18 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     if (threadIdx.x == 0) atomicOr(a.err, DEVERR_COUNT);
     return;
   }
-  const long long all = (long long)nq * group;
-  const long long row0 = (long long)chunk * unit_rows;
+  const int all = nq * group, row0 = chunk * unit_rows;  // (below 2^31: the entry point's check)
   if (row0 >= all) return;
-  const int rows = int(all - row0 < unit_rows ? all - row0 : unit_rows);
+  const int rows = min(all - row0, unit_rows);
   const bool two = rows > BQ;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::KST; ++i) {
-      mbar_init(k_full + 8 * i, 4);
+      mbar_init(k_full + 8 * i, 3);
       mbar_init(k_empty + 8 * i, 1);
     }
     for (int i = 0; i < C::VST; ++i) {
-      mbar_init(v_full + 8 * i, 4);
+      mbar_init(v_full + 8 * i, 3);
       mbar_init(v_empty + 8 * i, 1);
     }
     for (int x = 0; x < 2; ++x) {
@@ -202,7 +232,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     }
     for (int i = 0; i < C::RAWS; ++i) {
       mbar_init(raw_full + 8 * i, 1);
-      mbar_init(raw_empty + 8 * i, 4);
+      mbar_init(raw_empty + 8 * i, 3);
     }
     mbar_init(q_full, 8);
     *abort_flag = 0;
@@ -221,21 +251,22 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
 
   // the tokens that the unit's last row sees, in key blocks b0 .. b0 + nb - 1
   // of this CTA
-  const int last_query = int((row0 + rows - 1) / group);
+  const int last_query = (row0 + rows - 1) / group;
   const int reach = a.causal ? max(0, len - nq + last_query + 1) : len;
   const int blocks = (reach + BKV - 1) / BKV;
-  const int b0 = int((long long)part * blocks / parts);
-  const int nb = int((long long)(part + 1) * blocks / parts) - b0;
+  const int b0 = part * blocks / parts, nb = (part + 1) * blocks / parts - b0;
   const int pages = (len + KV8_BLOCK - 1) / KV8_BLOCK;
   const int* table = a.table + (long long)req * a.ld_table;
-  const auto page_of = [&](int p, bool report) {
-    if (p >= pages) return -1;
-    const int page = table[p];
-    if (page >= 0 && page < pool.blocks) return page;
-    if (report) atomicOr(a.err, DEVERR_INDEX);
-    return -1;
-  };
+  // the table's entry of cache block p, and later, where its value is there, its
+  // place in the pool (-1: none)
+  const auto entry = [&](int p) { return p < pages ? table[p] : -1; };
+  const auto checked = [&](int e) { return e < pool.blocks ? max(e, -1) : -1; };
   bool ok = true;
+
+  if (warp < CONV_WARP)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
+  else
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
 
   if (warp == MMA_WARP) {
     // ----------------------------------------------------------------- MMA
@@ -294,12 +325,22 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     // (the copies are whole cache blocks; one that is missing is left out:
     // what it leaves in the ring is hidden by the softmax)
     if (elect_one()) {
-      int page[PAGES];
+      int page[PAGES], ahead[2][PAGES];
+#pragma unroll
+      for (int i = 0; i < PAGES; ++i) {
+        ahead[0][i] = nb > 0 ? entry(PAGES * b0 + i) : -1;
+        ahead[1][i] = nb > 1 ? entry(PAGES * (b0 + 1) + i) : -1;
+      }
       for (int j = 0; ok && j < 2 * nb; ++j) {
-        const int st = j % C::RAWS, side = j & 1;
+        const int st = j % C::RAWS, side = j & 1, b = j >> 1;
         if (side == 0)
 #pragma unroll
-          for (int i = 0; i < PAGES; ++i) page[i] = page_of(PAGES * (b0 + (j >> 1)) + i, true);
+          for (int i = 0; i < PAGES; ++i) {
+            page[i] = checked(ahead[0][i]);
+            if (page[i] < 0 && PAGES * (b0 + b) + i < pages) atomicOr(a.err, DEVERR_INDEX);
+            ahead[0][i] = ahead[1][i];
+            ahead[1][i] = b + 2 < nb ? entry(PAGES * (b0 + b + 2) + i) : -1;
+          }
         if (!mbar_wait(raw_empty + 8 * st, ((j / C::RAWS) & 1) ^ 1, abort_flag)) { ok = false; break; }
         constexpr uint32_t BYTES = KV8_BLOCK * DH;
         mbar_expect_tx(raw_full + 8 * st,
@@ -314,45 +355,48 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     }
   } else if (warp >= CONV_WARP) {
     // ---------------------------------------------------------- conversion
-    // Thread `tid` takes the 8-code pieces tid + 128 j of the block's 128
-    // rows (piece c of row r: 8 channels).
-    const int tid = int(threadIdx.x) - CONV_WARP * 32;
-    constexpr int PER_ROW = DH / 8;
-    for (int j = 0; j < 2 * nb; ++j) {
-      const int b = j >> 1, st = j % C::RAWS, ks = b % C::KST, vs = b % C::VST;
+    // A thread takes one 8-code piece (8 channels) of every PASS-th row.
+    const bool values = warp >= CONV_WARP + 4;
+    const int tid = int(threadIdx.x) - (values ? CONV_WARP + 4 : CONV_WARP) * 32;
+    const int r0 = tid / C::PER_ROW, c = tid - r0 * C::PER_ROW;
+    const bool tail = C::TAIL && c == 8;
+    for (int b = 0; b < nb; ++b) {
+      const int j = 2 * b + (values ? 1 : 0), st = j % C::RAWS, ks = b % C::KST, vs = b % C::VST;
       if (ok)
-        ok = mbar_sleep(raw_full + 8 * st, (j / C::RAWS) & 1, abort_flag) &&
-             (j & 1 ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
-                    : mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag));
+        ok = (values ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
+                     : mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag)) &&
+             mbar_sleep(raw_full + 8 * st, (j / C::RAWS) & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      const uint32_t from = raw + st * C::RAW_BYTES + 8 * tid;
-      if ((j & 1) == 0) {
+      const uint32_t from = raw + st * C::RAW_BYTES + (r0 * C::PER_ROW + c) * 8;
+      constexpr int PASSES = (BKV + C::PASS - 1) / C::PASS, BATCH = 5;
 #pragma unroll
-        for (int i = 0; i < C::UNITS; ++i) {
-          const int u = tid + 128 * i, r = u / PER_ROW, c = u - r * PER_ROW;
-          const uint2 q = lds64(from + 1024 * i);
-          const uint32_t tile = sk + ks * C::K_BYTES;
-          const uint32_t at = C::TAIL && c == 8
-                                  ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
-                                  : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4);
-          sts128(at, e4m3x2_f16x2(q.x & 0xffffu), e4m3x2_f16x2(q.x >> 16),
-                 e4m3x2_f16x2(q.y & 0xffffu), e4m3x2_f16x2(q.y >> 16));
-        }
-      } else {
+      for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
+        uint2 q[BATCH];
 #pragma unroll
-        for (int i = 0; i < C::UNITS; ++i) {
-          const int u = tid + 128 * i, r = u / PER_ROW, c = u - r * PER_ROW;
-          const uint2 q = lds64(from + 1024 * i);
-          const uint32_t at = sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 +
-                              (((c ^ r) & 7) << 4);
-          sts128(at, codes_02(q.x), codes_13(q.x), codes_02(q.y), codes_13(q.y));
+        for (int p = p0; p < p0 + BATCH && p < PASSES; ++p)
+          if (r0 < C::PASS && r0 + p * C::PASS < BKV) q[p - p0] = lds64(from + p * C::PASS * DH);
+#pragma unroll
+        for (int p = p0; p < p0 + BATCH && p < PASSES; ++p) {
+          const int r = r0 + p * C::PASS;
+          if (r0 >= C::PASS || r >= BKV) continue;
+          const uint2 u = q[p - p0];
+          if (values) {
+            sts128(sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
+                   codes_02(u.x), codes_13(u.x), codes_02(u.y), codes_13(u.y));
+          } else {
+            const uint32_t tile = sk + ks * C::K_BYTES;
+            sts128(tail ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
+                        : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
+                   e4m3x2_f16x2(u.x & 0xffffu), e4m3x2_f16x2(u.x >> 16),
+                   e4m3x2_f16x2(u.y & 0xffffu), e4m3x2_f16x2(u.y >> 16));
+          }
         }
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(raw_empty + 8 * st);
-        mbar_arrive(j & 1 ? v_full + 8 * vs : k_full + 8 * ks);
+        mbar_arrive(values ? v_full + 8 * vs : k_full + 8 * ks);
       }
     }
   } else {
@@ -360,8 +404,8 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     const int x = warp >> 2, tr = threadIdx.x & 127;  // stream, row of its tile
     const int ur = (two ? x * BQ : 0) + tr;           // row of the unit
     const bool in = ur < rows;
-    const int query = int((row0 + (in ? ur : 0)) / group);
-    const int gh = int(row0 + (in ? ur : 0) - (long long)query * group);
+    const int query = (row0 + (in ? ur : 0)) / group;
+    const int gh = row0 + (in ? ur : 0) - query * group;
     // (rows past the unit's last see what it sees: their warp need not mask)
     const int seen = !in ? reach : a.causal ? max(0, len - nq + query + 1) : len;
     // ---- the row's queries, f16 over the power of two of their largest
@@ -422,12 +466,13 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     const auto look_up = [&](int i, int* page) {
 #pragma unroll
       for (int p = 0; p < PAGES; ++p)
-        page[p] = i < mine ? page_of(PAGES * block_of(i) + p, false) : -1;
+        page[p] = i < mine ? entry(PAGES * block_of(i) + p) : -1;
     };
     const auto scales = [&](Info& d) {
 #pragma unroll
       for (int p = 0; p < PAGES; ++p) {
         d.k[p] = d.v[p] = 0;
+        d.page[p] = checked(d.page[p]);
         if (d.page[p] >= 0) {
           const long long at = (long long)d.page[p] * pool.heads + head;
           d.k[p] = pool.scale[0][at];
@@ -448,30 +493,36 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       scales(next);
       int ahead[PAGES];
       look_up(i + 2, ahead);
+      // ---- of each cache block: factor of its scores, exponent of its weights
+      // (the same for every row but for the row's own power of two)
+      const int key0 = block_of(i) * BKV;
+      float factor[PAGES];
+      int limits[PAGES];
+      bool full[PAGES];
+#pragma unroll
+      for (int h = 0; h < PAGES; ++h) {
+        const int e = qe + now.k[h] - 127;
+        factor[h] = now.k[h] == 255 ? __uint_as_float(0x7fffffffu)
+                    : e < 1         ? 0.f
+                                    : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
+        // columns that the row sees: those below the limit
+        limits[h] = now.page[h] < 0 ? 0 : seen - key0 - h * KV8_BLOCK;
+        full[h] = __all_sync(0xffffffffu, limits[h] >= KV8_BLOCK);
+      }
       if (ok) ok = mbar_sleep(s_full + 8 * x, i & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-#pragma unroll 1
+#pragma unroll
       for (int h = 0; h < PAGES; ++h) {
-        // ---- a cache block: factor of its scores, exponent of its weights
-        const int page = h ? now.page[1] : now.page[0];
-        const int bk = h ? now.k[1] : now.k[0], bv = h ? now.v[1] : now.v[0];
-        const int e = qe + bk - 127;
-        const float f = bk == 255 ? __uint_as_float(0x7fffffffu)
-                        : e < 1   ? 0.f
-                                  : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
+        const int bv = now.v[h], limit = limits[h];
+        const float f = factor[h];
         const uint32_t s_at = ts + uint32_t(h * KV8_BLOCK);
-        // columns that the row sees: those below `limit`
-        const int limit = page < 0 ? 0 : seen - block_of(i) * BKV - h * KV8_BLOCK;
-        // (the reference of value scales, like all of this but seen, is the
-        // same for every row of the stream)
         int raise_to = ref;
-        if (page >= 0 && bv < 255 && (ref < 0 || bv > ref + RAISE_VALUE)) raise_to = bv;
+        if (now.page[h] >= 0 && bv < 255 && (ref < 0 || bv > ref + RAISE_VALUE)) raise_to = bv;
         bool raise_max = m == -INFINITY;
         // no column hidden, no value scale far below the reference
-        const bool whole =
-            __all_sync(0xffffffffu, limit >= KV8_BLOCK) && (bv == 255 || bv - raise_to >= -60);
-        uint32_t w[KV8_BLOCK / 2];
+        const bool whole = full[h] && (bv == 255 || bv - raise_to >= -60);
+        uint32_t w[KV8_BLOCK];
         float sum;
         for (bool again = false;; again = true) {
           if (__any_sync(0xffffffffu, raise_max) || raise_to != ref) {
@@ -515,43 +566,17 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
           const float mm = m == -INFINITY ? 0.f : m;
           const int d = max(bv - ref, -126);
           const float dv = bv == 255 ? __uint_as_float(0x7fffffffu) : float(max(d, -60));
-          const uint64_t ff = pair64(f, f), sh = pair64(dv - mm, dv - mm);
-          uint64_t total = 0;
-          const auto weights = [&](auto fast) {
-            const float less = d < -60 ? scale_value(127 + d + 60) : 1.f;
-#pragma unroll
-            for (int c0 = 0; c0 < KV8_BLOCK; c0 += 32) {
-              float s[32];
-              tmem_ld32(s_at + c0, s);
-#pragma unroll
-              for (int c = 0; c < 32; c += 2) {
-                float2 y = split64(fma2(pair64(s[c], s[c + 1]), ff, sh));
-                if (!decltype(fast)::value) {
-                  if (c0 + c >= limit) y.x = -INFINITY;
-                  if (c0 + c + 1 >= limit) y.y = -INFINITY;
-                }
-                y.x = ex2_ftz(y.x);
-                y.y = ex2_ftz(y.y);
-                total = add2(total, pair64(y.x, y.y));
-                if (!decltype(fast)::value) {
-                  y.x *= less;
-                  y.y *= less;
-                }
-                w[(c0 + c) / 2] = pack_bf16x2(y.x, y.y);
-              }
-            }
-          };
-          if (whole) weights(Yes{});
-          else weights(No{});
-          const float2 t = split64(total);
+          tmem_ld64(s_at, w);
+          float2 t;
+          if (whole) t = weights<true>(w, f, dv - mm, KV8_BLOCK, 1.f);
+          else t = weights<false>(w, f, dv - mm, limit, d < -60 ? scale_value(127 + d + 60) : 1.f);
           // (a block that the row sees nothing of adds nothing, whatever its scale)
           sum = limit > 0 ? (t.x + t.y) * ex2_ftz(-dv) : 0.f;
           raise_max = sum > RAISE_SUM;
           if (again || !__any_sync(0xffffffffu, raise_max)) break;
         }
         l += sum;
-        tmem_st16(ts + uint32_t(h * (KV8_BLOCK / 2)), w);
-        tmem_st16(ts + uint32_t(h * (KV8_BLOCK / 2) + 16), w + 16);
+        tmem_st32(ts + uint32_t(h * (KV8_BLOCK / 2)), w);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -568,7 +593,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     tc_fence_after();
     const float back = ref < 0 ? 0.f : scale_value(ref);
     const auto row_out = [&](int r) {
-      const int qi = int((row0 + r) / group), g = int(row0 + r - (long long)qi * group);
+      const int qi = (row0 + r) / group, g = row0 + r - qi * group;
       return a.o + (long long)(q0 + qi) * a.ldo + (head * group + g) * DH;
     };
     // eight channels from 8 c of O, in their order
