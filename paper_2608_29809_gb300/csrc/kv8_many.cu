@@ -7,8 +7,8 @@
 // in turn.  A cluster of CTAs may share the unit's keys.
 //   warps 0-3, 4-7   softmax of a stream, one thread a row: S from tensor
 //                    memory, weights back over it as bf16, a cache block (64
-//                    tokens) at a time, so that P V of the first half runs
-//                    beside the second half's exponentials
+//                    tokens) at a time; the other half of S meanwhile takes
+//                    the next one's scores
 //   warps 8-10       key codes to operands in shared memory: f16 (exact),
 //                    K-major, 128-byte swizzle
 //   warps 12-14      value codes: bf16 (exact), MN-major, 128-byte swizzle
@@ -46,6 +46,9 @@ constexpr int CONV_WARP = 8, MMA_WARP = 11, LOAD_WARP = 15, CONV_THREADS = 96;
 // warpgroups take 160, the other two keep 96.
 constexpr int SOFT_REGS = 160, OTHER_REGS = 96;
 constexpr int PAGES = BKV / KV8_BLOCK;
+// scale bytes of a CTA's first cache blocks kept in shared memory (those of
+// later ones, past 16384 tokens, are read where they are needed)
+constexpr int FACTS = 256;
 // S (P over it) of each stream, then O, then Q where it fits
 constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;
 constexpr float RAISE_SUM = 18446744073709551616.f;  // 2^64
@@ -68,10 +71,10 @@ struct MCfg {
   static constexpr int RAW_BYTES = BKV * DH, RAWS = DH == 128 ? 2 : 4;
   static constexpr int OPERANDS = 2 * Q_BYTES + KST * K_BYTES + VST * V_BYTES;
   static constexpr int RING = OPERANDS + RAWS * RAW_BYTES;
-  static constexpr size_t SMEM = size_t(RING) + 1024 + 256;
+  static constexpr size_t SMEM = size_t(RING) + FACTS * 4 + 1024 + 256;
   static constexpr int PER_ROW = DH / 8;             // 8-code pieces of a row
   static constexpr int PASS = CONV_THREADS / PER_ROW;  // rows converted at a time
-  static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(BKV >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
+  static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(KV8_BLOCK >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) |
                                        (uint32_t(ODIM >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr int PSTRIDE = DH + 2;             // floats of a partial row
@@ -169,11 +172,6 @@ __device__ __forceinline__ float2 weights(uint32_t* r, float f, float shift, int
   return split64(add2(total[0], total[1]));
 }
 
-// Blocks and scale bytes of the two cache blocks of a key block.
-struct Info {
-  int page[PAGES], k[PAGES], v[PAGES];
-};
-
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1)
 many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
@@ -182,18 +180,18 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING);
+  uint32_t* facts = reinterpret_cast<uint32_t*>(smem + C::RING);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + FACTS * 4);
   const uint32_t sq = saddr(smem), sk = sq + 2 * C::Q_BYTES, sv = sk + C::KST * C::K_BYTES;
   const uint32_t bar = saddr(bars);
   const uint32_t k_full = bar, k_empty = k_full + 8 * C::KST, v_full = k_empty + 8 * C::KST;
   const uint32_t v_empty = v_full + 8 * C::VST, s_full = v_empty + 8 * C::VST;
-  // (a stream's softmax may hand over both halves of its weights before either
-  // is waited for, so each half has a barrier)
-  const uint32_t p_full = s_full + 16, o_done = p_full + 16 * PAGES, o_full = o_done + 16;
+  // (per cache block of the two that S holds, and stream)
+  const uint32_t p_full = s_full + 16 * PAGES, o_done = p_full + 16 * PAGES, o_full = o_done + 16;
   const uint32_t q_full = o_full + 16, raw_full = q_full + 8, raw_empty = raw_full + 8 * C::RAWS;
   const uint32_t raw = sq + C::OPERANDS;
   uint32_t* tmem_slot =
-      reinterpret_cast<uint32_t*>(bars + 2 * C::KST + 2 * C::VST + 7 + 2 * PAGES + 2 * C::RAWS);
+      reinterpret_cast<uint32_t*>(bars + 2 * C::KST + 2 * C::VST + 5 + 4 * PAGES + 2 * C::RAWS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = warp_index(), lane = threadIdx.x & 31;
 
@@ -225,8 +223,10 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       mbar_init(v_empty + 8 * i, 1);
     }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(s_full + 8 * x, 1);
-      for (int h = 0; h < PAGES; ++h) mbar_init(p_full + 16 * h + 8 * x, 4);
+      for (int h = 0; h < PAGES; ++h) {
+        mbar_init(s_full + 16 * h + 8 * x, 1);
+        mbar_init(p_full + 16 * h + 8 * x, 4);
+      }
       mbar_init(o_done + 8 * x, 1);
       mbar_init(o_full + 8 * x, 1);
     }
@@ -270,21 +270,32 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
 
   if (warp == MMA_WARP) {
     // ----------------------------------------------------------------- MMA
+    // Each stream's S holds two cache blocks; the scores of the second next one
+    // follow the products that used their place, so that a stream's softmax
+    // finds its next scores ready.
     if (nb > 0 && elect_one()) {
-      const int events = two ? 2 * nb : nb;
-      const auto scores = [&](int e) {
-        const int x = e & 1, b = two ? e >> 1 : e, st = b % C::KST;
-        if ((!two || x == 0) &&
+      const int rounds = two ? nb : (nb + 1) / 2;  // key blocks of stream 0
+      // key block of a stream's i-th, and whether a stream is the first or the
+      // last to use it
+      const auto block = [&](int i, int x) { return two ? i : 2 * i + x; };
+      const auto scores = [&](int i, int h, int x) {
+        const int b = block(i, x), st = b % C::KST;
+        if (b >= nb) return true;
+        if (h == 0 && (!two || x == 0) &&
             !mbar_wait(k_full + 8 * st, (b / C::KST) & 1, abort_flag)) return false;
         tc_fence_after();
-        const uint32_t k = sk + st * C::K_BYTES, d = tmem + uint32_t(x * BKV);
+        const uint32_t k = sk + st * C::K_BYTES + h * (KV8_BLOCK * 128);
+        const uint32_t d = tmem + uint32_t(x * BKV + h * KV8_BLOCK);
         const int tile = two ? x : 0;
         if constexpr (C::Q_TMEM) {
           const uint32_t q = tmem + uint32_t(C::TM_Q + tile * C::Q_COLS);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
             umma_bf16_ta(d, q + 8 * kk, sw128_desc(k) + 2 * kk, C::IDESC_S, kk ? 1u : 0u);
-          if (C::TAIL) umma_bf16_ta(d, q + 32, sw32_kmajor_desc(k + BKV * 128), C::IDESC_S, 1u);
+          if (C::TAIL)
+            umma_bf16_ta(d, q + 32,
+                         sw32_kmajor_desc(sk + st * C::K_BYTES + BKV * 128 + h * (KV8_BLOCK * 32)),
+                         C::IDESC_S, 1u);
         } else {
           const uint32_t q = sq + tile * C::Q_BYTES;
 #pragma unroll
@@ -294,30 +305,39 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
               umma_bf16(d, sw128_desc(q + f * BQ * 128) + 2 * kk,
                         sw128_desc(k + f * BKV * 128) + 2 * kk, C::IDESC_S, (f | kk) ? 1u : 0u);
         }
-        umma_commit(s_full + 8 * x);
-        if (!two || x == 1) umma_commit(k_empty + 8 * st);
+        umma_commit(s_full + 16 * h + 8 * x);
+        if (h == PAGES - 1 && (!two || x == 1)) umma_commit(k_empty + 8 * st);
         return true;
       };
-      ok = mbar_wait(q_full, 0, abort_flag) && scores(0) && (events < 2 || scores(1));
-      for (int e = 0; ok && e < events; ++e) {
-        const int x = e & 1, b = two ? e >> 1 : e, i = e >> 1, st = b % C::VST;
-        const uint32_t d = tmem + uint32_t(TM_O + x * C::ODIM), p = tmem + uint32_t(x * BKV);
-        const uint64_t v = sw128_mnmajor_desc_lbo(sv + st * C::V_BYTES, BKV * 128);
+      ok = mbar_wait(q_full, 0, abort_flag);
+      for (int h = 0; h < PAGES; ++h)
+        for (int x = 0; x < 2; ++x) ok = ok && scores(0, h, x);
+      for (int i = 0; ok && i < rounds; ++i) {
 #pragma unroll
         for (int h = 0; h < PAGES; ++h) {
-          if ((h == 0 && (!two || x == 0) &&
-               !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
-              !mbar_wait(p_full + 16 * h + 8 * x, i & 1, abort_flag)) { ok = false; break; }
-          tc_fence_after();
+          for (int x = 0; x < 2; ++x) {
+            const int b = block(i, x), st = b % C::VST;
+            if (b >= nb) continue;
+            if ((h == 0 && (!two || x == 0) &&
+                 !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
+                !mbar_wait(p_full + 16 * h + 8 * x, i & 1, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t d = tmem + uint32_t(TM_O + x * C::ODIM);
+            const uint32_t p = tmem + uint32_t(x * BKV + h * KV8_BLOCK);
+            const uint64_t v = sw128_mnmajor_desc_lbo(
+                sv + st * C::V_BYTES + h * (KV8_BLOCK * 128), BKV * 128);
 #pragma unroll
-          for (int kk = 4 * h; kk < 4 * h + 4; ++kk)
-            umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | kk) ? 1u : 0u);
-          umma_commit(o_done + 8 * x);
+            for (int kk = 0; kk < KV8_BLOCK / 16; ++kk)
+              umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | h | kk) ? 1u : 0u);
+            umma_commit(o_done + 8 * x);
+            if (h == PAGES - 1) {
+              if (!two || x == 1) umma_commit(v_empty + 8 * st);
+              if (block(i + 1, x) >= nb) umma_commit(o_full + 8 * x);
+            }
+            if (!scores(i + 1, h, x)) { ok = false; break; }
+          }
+          if (!ok) break;
         }
-        if (!ok) break;
-        if (!two || x == 1) umma_commit(v_empty + 8 * st);
-        if (e + 2 >= events) umma_commit(o_full + 8 * x);
-        else if (!scores(e + 2)) ok = false;
       }
     }
   } else if (warp == LOAD_WARP) {
@@ -463,69 +483,50 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     const uint32_t to = tmem + uint32_t(TM_O + x * C::ODIM) + lanes;
     const int mine = two ? nb : (nb + 1 - x) / 2;  // this stream's key blocks
     const auto block_of = [&](int i) { return b0 + (two ? i : 2 * i + x); };
-    const auto look_up = [&](int i, int* page) {
-#pragma unroll
-      for (int p = 0; p < PAGES; ++p)
-        page[p] = i < mine ? entry(PAGES * block_of(i) + p) : -1;
+    // a cache block's scale bytes (key, value), bit 16 set; 0 for a missing one
+    const auto fact = [&](int p) {
+      const int page = checked(entry(p));
+      if (page < 0) return 0u;
+      const long long at = (long long)page * pool.heads + head;
+      return 1u << 16 | uint32_t(pool.scale[1][at]) << 8 | pool.scale[0][at];
     };
-    const auto scales = [&](Info& d) {
-#pragma unroll
-      for (int p = 0; p < PAGES; ++p) {
-        d.k[p] = d.v[p] = 0;
-        d.page[p] = checked(d.page[p]);
-        if (d.page[p] >= 0) {
-          const long long at = (long long)d.page[p] * pool.heads + head;
-          d.k[p] = pool.scale[0][at];
-          d.v[p] = pool.scale[1][at];
-        }
-      }
-    };
-    Info now, next;
-    look_up(0, now.page);
-    scales(now);
-    look_up(1, next.page);
+    for (int p = int(threadIdx.x); p < min(FACTS, PAGES * nb); p += 256)
+      facts[p] = fact(PAGES * b0 + p);
+    soft_sync();
     // (a row that sees nothing here needs no maximum)
     const bool blind = seen <= block_of(0) * BKV;
     float m = blind ? 0.f : -INFINITY, l = 0.f;
     int ref = -1;  // value scale byte that O is in units of (-1: none yet)
+    const int least = __reduce_min_sync(0xffffffffu, seen);  // what every row of the warp sees
+    bool searching = __any_sync(0xffffffffu, m == -INFINITY);
 
-    for (int i = 0; i < mine; ++i) {
-      scales(next);
-      int ahead[PAGES];
-      look_up(i + 2, ahead);
-      // ---- of each cache block: factor of its scores, exponent of its weights
-      // (the same for every row but for the row's own power of two)
-      const int key0 = block_of(i) * BKV;
-      float factor[PAGES];
-      int limits[PAGES];
-      bool full[PAGES];
-#pragma unroll
-      for (int h = 0; h < PAGES; ++h) {
-        const int e = qe + now.k[h] - 127;
-        factor[h] = now.k[h] == 255 ? __uint_as_float(0x7fffffffu)
-                    : e < 1         ? 0.f
-                                    : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
-        // columns that the row sees: those below the limit
-        limits[h] = now.page[h] < 0 ? 0 : seen - key0 - h * KV8_BLOCK;
-        full[h] = __all_sync(0xffffffffu, limits[h] >= KV8_BLOCK);
-      }
-      if (ok) ok = mbar_sleep(s_full + 8 * x, i & 1, abort_flag);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+    for (int g = 0; g < PAGES * mine; ++g) {
+      const int h = g % PAGES, i = g / PAGES;
+      const int own_page = PAGES * (block_of(i) - b0) + h, key0 = (PAGES * b0 + own_page) * KV8_BLOCK;
+      const uint32_t now = own_page < FACTS ? facts[own_page] : fact(PAGES * b0 + own_page);
+      const int bk = int(now & 255), bv = int(now >> 8 & 255);
+      const uint32_t s_at = ts + uint32_t(h * KV8_BLOCK);
+      // factor of the scores: 2^(the row's exponent + the block's), in base 2
+      const int e = qe + bk - 127;
+      const float f = bk == 255 ? __uint_as_float(0x7fffffffu)
+                      : e < 1   ? 0.f
+                                : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
+      // columns that the row sees: those below `limit`
+      const int limit = now ? seen - key0 : 0;
+      int raise_to = ref;
+      if (now && bv < 255 && (ref < 0 || bv > ref + RAISE_VALUE)) raise_to = bv;
+      // no column hidden, no value scale far below the reference
+      const bool whole = now && least - key0 >= KV8_BLOCK && (bv == 255 || bv - raise_to >= -60);
+      bool raise_max = searching && m == -INFINITY;
+      // (after a failed wait the rows go on, without waiting)
+      if (ok) ok = mbar_sleep(s_full + 16 * h + 8 * x, i & 1, abort_flag);
+      __syncwarp();
       tc_fence_after();
-#pragma unroll
-      for (int h = 0; h < PAGES; ++h) {
-        const int bv = now.v[h], limit = limits[h];
-        const float f = factor[h];
-        const uint32_t s_at = ts + uint32_t(h * KV8_BLOCK);
-        int raise_to = ref;
-        if (now.page[h] >= 0 && bv < 255 && (ref < 0 || bv > ref + RAISE_VALUE)) raise_to = bv;
-        bool raise_max = m == -INFINITY;
-        // no column hidden, no value scale far below the reference
-        const bool whole = full[h] && (bv == 255 || bv - raise_to >= -60);
+      {
         uint32_t w[KV8_BLOCK];
         float sum;
         for (bool again = false;; again = true) {
-          if (__any_sync(0xffffffffu, raise_max) || raise_to != ref) {
+          if (again || searching || raise_to != ref) {
             // ---- a new reference: the row's largest score (where asked for)
             float top = m;
 #pragma unroll 1
@@ -542,11 +543,11 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
             if (raise_to != ref && ref >= 0) corr *= scale_value(max(127 + ref - raise_to, 0));
             m = to_max;
             ref = raise_to;
-            // once the P V before has ended (its phase is 2 i + h - 1, and the next
-            // one's weights are not there yet)
-            if (i + h > 0) {
+            // once the P V before has ended (phase g - 1; the one before that
+            // had when these scores were there)
+            if (g > 0) {
               if (ok) ok = mbar_wait(o_done + 8 * x, h ^ 1, abort_flag);
-              ok = __all_sync(0xffffffffu, ok);
+              __syncwarp();
               tc_fence_after();
 #pragma unroll 1
               for (int c0 = 0; c0 < C::ODIM; c0 += 16) {
@@ -576,15 +577,13 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
           if (again || !__any_sync(0xffffffffu, raise_max)) break;
         }
         l += sum;
-        tmem_st32(ts + uint32_t(h * (KV8_BLOCK / 2)), w);
+        tmem_st32(s_at, w);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full + 16 * h + 8 * x);
+        if (searching) searching = __any_sync(0xffffffffu, m == -INFINITY);
       }
-      now = next;
-#pragma unroll
-      for (int p = 0; p < PAGES; ++p) next.page[p] = ahead[p];
     }
 
     // ---- result: O of a row in f32, or its part to be joined
