@@ -43,16 +43,17 @@ constexpr int BQ = 128, BKV = 128, THREADS = 512;
 // one of these)
 constexpr int CONV_WARP = 8, MMA_WARP = 11, LOAD_WARP = 15, CONV_THREADS = 96;
 // Registers: 512 threads are launched with 128 each; the softmax's two
-// warpgroups take 160, the other two keep 96.
-constexpr int SOFT_REGS = 160, OTHER_REGS = 96;
+// warpgroups take 176, the other two keep 80 (asked for by each warpgroup in one
+// place, ahead of its warps' roles).
+constexpr int SOFT_REGS = 176, OTHER_REGS = 80;
 constexpr int PAGES = BKV / KV8_BLOCK;
-// scale bytes of a CTA's first cache blocks kept in shared memory (those of
-// later ones, past 16384 tokens, are read where they are needed)
-constexpr int FACTS = 256;
+// what the rows share of a cache block: the key scale (NaN where a block has no
+// value) and the value scale's exponent (ABSENT: the block is missing)
+constexpr float ABSENT = -2e30f, NO_REF = -1e30f;
 // S (P over it) of each stream, then O, then Q where it fits
 constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;
-constexpr float RAISE_SUM = 18446744073709551616.f;  // 2^64
-constexpr int RAISE_VALUE = 40;
+constexpr float RAISE_SUM = 18446744073709551616.f, RAISE_VALUE = 40.f;  // 2^64, 2^40
+
 
 template <int DH>
 struct MCfg {
@@ -71,15 +72,18 @@ struct MCfg {
   static constexpr int RAW_BYTES = BKV * DH, RAWS = DH == 128 ? 2 : 4;
   static constexpr int OPERANDS = 2 * Q_BYTES + KST * K_BYTES + VST * V_BYTES;
   static constexpr int RING = OPERANDS + RAWS * RAW_BYTES;
-  static constexpr size_t SMEM = size_t(RING) + FACTS * 4 + 1024 + 256;
+  // facts of a CTA's first cache blocks, kept in shared memory (those of later
+  // ones are read where they are needed)
+  static constexpr int FACTS = DH == 128 ? 128 : 256;
+  static constexpr size_t SMEM = size_t(RING) + FACTS * 8 + 1024 + 256;
   static constexpr int PER_ROW = DH / 8;             // 8-code pieces of a row
   static constexpr int PASS = CONV_THREADS / PER_ROW;  // rows converted at a time
   static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(KV8_BLOCK >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) |
                                        (uint32_t(ODIM >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
-  static constexpr int PSTRIDE = DH + 2;             // floats of a partial row
+  static constexpr int PSTRIDE = DH + 4;             // floats of a partial row
   static_assert(Q_TMEM || !TAIL, "queries in shared memory have no tail");
-  static_assert(2 * BQ * PSTRIDE * 4 <= RING, "the parts fit the operands' memory");
+  static_assert((2 * BQ + 16) * PSTRIDE * 4 <= RING, "the parts fit the operands' memory");
   static_assert(TM_O + 2 * ODIM <= TMEM_COLS, "tensor memory");
 };
 
@@ -144,15 +148,14 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
   return v;
 }
 
-// A row's 64 scores s to weights 2^(s f + shift), two a word as bf16 in the
-// first half of r (times `less`, where FAST is false: then columns from `limit`
-// on are hidden).  Returns their sum before that, in two parts.  In place: the
-// registers are what a row's scores leave.
+// A row's 64 scores of a cache block, r, to weights 2^(s f + shift), two a word
+// as bf16 in w (times `less`, where FAST is false: then columns from `limit` on
+// are hidden).  `total` gets their sums before that.  w may be r: a word is
+// written behind the scores it is made of.
 template <bool FAST>
-__device__ __forceinline__ float2 weights(uint32_t* r, float f, float shift, int limit,
-                                          float less) {
+__device__ __forceinline__ void weights(const uint32_t* r, uint32_t* w, float f, float shift,
+                                        int limit, float less, uint64_t* total) {
   const uint64_t ff = pair64(f, f), sh = pair64(shift, shift);
-  uint64_t total[2] = {0, 0};
 #pragma unroll
   for (int c = 0; c < KV8_BLOCK; c += 2) {
     float2 y = split64(fma2(pair64(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), ff, sh));
@@ -167,9 +170,18 @@ __device__ __forceinline__ float2 weights(uint32_t* r, float f, float shift, int
       y.x *= less;
       y.y *= less;
     }
-    r[c >> 1] = pack_bf16x2(y.x, y.y);
+    w[c >> 1] = pack_bf16x2(y.x, y.y);
   }
-  return split64(add2(total[0], total[1]));
+}
+
+// Into this or another CTA's shared memory.
+__device__ __forceinline__ void store_four(uint32_t at, const float* v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v[0]), "f"(v[1]),
+               "f"(v[2]), "f"(v[3])
+               : "memory");
+}
+__device__ __forceinline__ void store_two(uint32_t at, float a, float b) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(a), "f"(b) : "memory");
 }
 
 template <int DH>
@@ -180,8 +192,8 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  uint32_t* facts = reinterpret_cast<uint32_t*>(smem + C::RING);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + FACTS * 4);
+  float2* facts = reinterpret_cast<float2*>(smem + C::RING);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::FACTS * 8);
   const uint32_t sq = saddr(smem), sk = sq + 2 * C::Q_BYTES, sv = sk + C::KST * C::K_BYTES;
   const uint32_t bar = saddr(bars);
   const uint32_t k_full = bar, k_empty = k_full + 8 * C::KST, v_full = k_empty + 8 * C::KST;
@@ -263,164 +275,9 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   const auto checked = [&](int e) { return e < pool.blocks ? max(e, -1) : -1; };
   bool ok = true;
 
-  if (warp < CONV_WARP)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
-  else
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-
-  if (warp == MMA_WARP) {
-    // ----------------------------------------------------------------- MMA
-    // Each stream's S holds two cache blocks; the scores of the second next one
-    // follow the products that used their place, so that a stream's softmax
-    // finds its next scores ready.
-    if (nb > 0 && elect_one()) {
-      const int rounds = two ? nb : (nb + 1) / 2;  // key blocks of stream 0
-      // key block of a stream's i-th, and whether a stream is the first or the
-      // last to use it
-      const auto block = [&](int i, int x) { return two ? i : 2 * i + x; };
-      const auto scores = [&](int i, int h, int x) {
-        const int b = block(i, x), st = b % C::KST;
-        if (b >= nb) return true;
-        if (h == 0 && (!two || x == 0) &&
-            !mbar_wait(k_full + 8 * st, (b / C::KST) & 1, abort_flag)) return false;
-        tc_fence_after();
-        const uint32_t k = sk + st * C::K_BYTES + h * (KV8_BLOCK * 128);
-        const uint32_t d = tmem + uint32_t(x * BKV + h * KV8_BLOCK);
-        const int tile = two ? x : 0;
-        if constexpr (C::Q_TMEM) {
-          const uint32_t q = tmem + uint32_t(C::TM_Q + tile * C::Q_COLS);
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            umma_bf16_ta(d, q + 8 * kk, sw128_desc(k) + 2 * kk, C::IDESC_S, kk ? 1u : 0u);
-          if (C::TAIL)
-            umma_bf16_ta(d, q + 32,
-                         sw32_kmajor_desc(sk + st * C::K_BYTES + BKV * 128 + h * (KV8_BLOCK * 32)),
-                         C::IDESC_S, 1u);
-        } else {
-          const uint32_t q = sq + tile * C::Q_BYTES;
-#pragma unroll
-          for (int f = 0; f < C::FULL; ++f)
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              umma_bf16(d, sw128_desc(q + f * BQ * 128) + 2 * kk,
-                        sw128_desc(k + f * BKV * 128) + 2 * kk, C::IDESC_S, (f | kk) ? 1u : 0u);
-        }
-        umma_commit(s_full + 16 * h + 8 * x);
-        if (h == PAGES - 1 && (!two || x == 1)) umma_commit(k_empty + 8 * st);
-        return true;
-      };
-      ok = mbar_wait(q_full, 0, abort_flag);
-      for (int h = 0; h < PAGES; ++h)
-        for (int x = 0; x < 2; ++x) ok = ok && scores(0, h, x);
-      for (int i = 0; ok && i < rounds; ++i) {
-#pragma unroll
-        for (int h = 0; h < PAGES; ++h) {
-          for (int x = 0; x < 2; ++x) {
-            const int b = block(i, x), st = b % C::VST;
-            if (b >= nb) continue;
-            if ((h == 0 && (!two || x == 0) &&
-                 !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
-                !mbar_wait(p_full + 16 * h + 8 * x, i & 1, abort_flag)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t d = tmem + uint32_t(TM_O + x * C::ODIM);
-            const uint32_t p = tmem + uint32_t(x * BKV + h * KV8_BLOCK);
-            const uint64_t v = sw128_mnmajor_desc_lbo(
-                sv + st * C::V_BYTES + h * (KV8_BLOCK * 128), BKV * 128);
-#pragma unroll
-            for (int kk = 0; kk < KV8_BLOCK / 16; ++kk)
-              umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | h | kk) ? 1u : 0u);
-            umma_commit(o_done + 8 * x);
-            if (h == PAGES - 1) {
-              if (!two || x == 1) umma_commit(v_empty + 8 * st);
-              if (block(i + 1, x) >= nb) umma_commit(o_full + 8 * x);
-            }
-            if (!scores(i + 1, h, x)) { ok = false; break; }
-          }
-          if (!ok) break;
-        }
-      }
-    }
-  } else if (warp == LOAD_WARP) {
-    // ------------------------------------------------------------- loading
-    // (the copies are whole cache blocks; one that is missing is left out:
-    // what it leaves in the ring is hidden by the softmax)
-    if (elect_one()) {
-      int page[PAGES], ahead[2][PAGES];
-#pragma unroll
-      for (int i = 0; i < PAGES; ++i) {
-        ahead[0][i] = nb > 0 ? entry(PAGES * b0 + i) : -1;
-        ahead[1][i] = nb > 1 ? entry(PAGES * (b0 + 1) + i) : -1;
-      }
-      for (int j = 0; ok && j < 2 * nb; ++j) {
-        const int st = j % C::RAWS, side = j & 1, b = j >> 1;
-        if (side == 0)
-#pragma unroll
-          for (int i = 0; i < PAGES; ++i) {
-            page[i] = checked(ahead[0][i]);
-            if (page[i] < 0 && PAGES * (b0 + b) + i < pages) atomicOr(a.err, DEVERR_INDEX);
-            ahead[0][i] = ahead[1][i];
-            ahead[1][i] = b + 2 < nb ? entry(PAGES * (b0 + b + 2) + i) : -1;
-          }
-        if (!mbar_wait(raw_empty + 8 * st, ((j / C::RAWS) & 1) ^ 1, abort_flag)) { ok = false; break; }
-        constexpr uint32_t BYTES = KV8_BLOCK * DH;
-        mbar_expect_tx(raw_full + 8 * st,
-                       BYTES * ((page[0] >= 0 ? 1u : 0u) + (page[1] >= 0 ? 1u : 0u)));
-#pragma unroll
-        for (int i = 0; i < PAGES; ++i)
-          if (page[i] >= 0)
-            bulk_load(raw + st * C::RAW_BYTES + i * BYTES,
-                      pool.code[side] + ((long long)page[i] * pool.heads + head) * BYTES, BYTES,
-                      raw_full + 8 * st);
-      }
-    }
-  } else if (warp >= CONV_WARP) {
-    // ---------------------------------------------------------- conversion
-    // A thread takes one 8-code piece (8 channels) of every PASS-th row.
-    const bool values = warp >= CONV_WARP + 4;
-    const int tid = int(threadIdx.x) - (values ? CONV_WARP + 4 : CONV_WARP) * 32;
-    const int r0 = tid / C::PER_ROW, c = tid - r0 * C::PER_ROW;
-    const bool tail = C::TAIL && c == 8;
-    for (int b = 0; b < nb; ++b) {
-      const int j = 2 * b + (values ? 1 : 0), st = j % C::RAWS, ks = b % C::KST, vs = b % C::VST;
-      if (ok)
-        ok = (values ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
-                     : mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag)) &&
-             mbar_sleep(raw_full + 8 * st, (j / C::RAWS) & 1, abort_flag);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      const uint32_t from = raw + st * C::RAW_BYTES + (r0 * C::PER_ROW + c) * 8;
-      constexpr int PASSES = (BKV + C::PASS - 1) / C::PASS, BATCH = 5;
-#pragma unroll
-      for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
-        uint2 q[BATCH];
-#pragma unroll
-        for (int p = p0; p < p0 + BATCH && p < PASSES; ++p)
-          if (r0 < C::PASS && r0 + p * C::PASS < BKV) q[p - p0] = lds64(from + p * C::PASS * DH);
-#pragma unroll
-        for (int p = p0; p < p0 + BATCH && p < PASSES; ++p) {
-          const int r = r0 + p * C::PASS;
-          if (r0 >= C::PASS || r >= BKV) continue;
-          const uint2 u = q[p - p0];
-          if (values) {
-            sts128(sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
-                   codes_02(u.x), codes_13(u.x), codes_02(u.y), codes_13(u.y));
-          } else {
-            const uint32_t tile = sk + ks * C::K_BYTES;
-            sts128(tail ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
-                        : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
-                   e4m3x2_f16x2(u.x & 0xffffu), e4m3x2_f16x2(u.x >> 16),
-                   e4m3x2_f16x2(u.y & 0xffffu), e4m3x2_f16x2(u.y >> 16));
-          }
-        }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(raw_empty + 8 * st);
-        mbar_arrive(values ? v_full + 8 * vs : k_full + 8 * ks);
-      }
-    }
-  } else {
+  if (warp < CONV_WARP) {
     // -------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
     const int x = warp >> 2, tr = threadIdx.x & 127;  // stream, row of its tile
     const int ur = (two ? x * BQ : 0) + tr;           // row of the unit
     const bool in = ur < rows;
@@ -477,120 +334,123 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
     }
-    const float unit = 1.4426950408889634f * rsqrtf(float(DH));  // scores in base 2
+    // factor of the row's scores, in base 2
+    const float own = 1.4426950408889634f * rsqrtf(float(DH)) * scale_value(qe);
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + uint32_t(x * BKV) + lanes;
     const uint32_t to = tmem + uint32_t(TM_O + x * C::ODIM) + lanes;
     const int mine = two ? nb : (nb + 1 - x) / 2;  // this stream's key blocks
     const auto block_of = [&](int i) { return b0 + (two ? i : 2 * i + x); };
-    // a cache block's scale bytes (key, value), bit 16 set; 0 for a missing one
     const auto fact = [&](int p) {
       const int page = checked(entry(p));
-      if (page < 0) return 0u;
+      if (page < 0) return make_float2(0.f, ABSENT);
       const long long at = (long long)page * pool.heads + head;
-      return 1u << 16 | uint32_t(pool.scale[1][at]) << 8 | pool.scale[0][at];
+      const int k = pool.scale[0][at], v = pool.scale[1][at];
+      return make_float2(scale_value(max(k, v) == 255 ? 255 : k), float(v));
     };
-    for (int p = int(threadIdx.x); p < min(FACTS, PAGES * nb); p += 256)
+    for (int p = int(threadIdx.x); p < min(C::FACTS, PAGES * nb); p += 256)
       facts[p] = fact(PAGES * b0 + p);
     soft_sync();
     // (a row that sees nothing here needs no maximum)
     const bool blind = seen <= block_of(0) * BKV;
     float m = blind ? 0.f : -INFINITY, l = 0.f;
-    int ref = -1;  // value scale byte that O is in units of (-1: none yet)
+    float ref = NO_REF;  // exponent of the value scale that O is in units of
     const int least = __reduce_min_sync(0xffffffffu, seen);  // what every row of the warp sees
     bool searching = __any_sync(0xffffffffu, m == -INFINITY);
 
-    for (int g = 0; g < PAGES * mine; ++g) {
-      const int h = g % PAGES, i = g / PAGES;
-      const int own_page = PAGES * (block_of(i) - b0) + h, key0 = (PAGES * b0 + own_page) * KV8_BLOCK;
-      const uint32_t now = own_page < FACTS ? facts[own_page] : fact(PAGES * b0 + own_page);
-      const int bk = int(now & 255), bv = int(now >> 8 & 255);
-      const uint32_t s_at = ts + uint32_t(h * KV8_BLOCK);
-      // factor of the scores: 2^(the row's exponent + the block's), in base 2
-      const int e = qe + bk - 127;
-      const float f = bk == 255 ? __uint_as_float(0x7fffffffu)
-                      : e < 1   ? 0.f
-                                : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
-      // columns that the row sees: those below `limit`
-      const int limit = now ? seen - key0 : 0;
-      int raise_to = ref;
-      if (now && bv < 255 && (ref < 0 || bv > ref + RAISE_VALUE)) raise_to = bv;
+    const int count = PAGES * mine;
+    const int skip = (two ? 1 : 2) * PAGES - 1;  // from a key block's second cache block to the next
+    int page = PAGES * (block_of(0) - b0);       // of the CTA's
+    const auto facts_of = [&](int p) { return p < C::FACTS ? facts[p] : fact(PAGES * b0 + p); };
+    const auto s_bar = [&](int g) { return s_full + 16 * (g & 1) + 8 * x; };
+    const auto hand_over = [&](int g) {  // block g's weights
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + 16 * (g & 1) + 8 * x);
+    };
+    uint32_t w[KV8_BLOCK];  // a cache block's scores, then its weights
+    float2 now = count > 0 ? facts_of(page) : make_float2(0.f, ABSENT);
+#pragma unroll 1
+    for (int g = 0; g < count; ++g) {
+      const uint32_t s_at = ts + uint32_t((g & 1) * KV8_BLOCK);
+      float f = own * now.x;
+      f = f > 3e38f ? 3e38f : f;  // (an infinite factor would make NaN of a score of 0)
+      const int key0 = (PAGES * b0 + page) * KV8_BLOCK;
+      const int limit = now.y < NO_REF ? 0 : seen - key0;  // columns that the row sees
+      const float raise_to = now.y > ref + RAISE_VALUE ? now.y : ref;
       // no column hidden, no value scale far below the reference
-      const bool whole = now && least - key0 >= KV8_BLOCK && (bv == 255 || bv - raise_to >= -60);
+      const bool whole = least - key0 >= KV8_BLOCK && now.y - raise_to >= -60.f;
+      const int next = page + (g & 1 ? skip : 1);
       bool raise_max = searching && m == -INFINITY;
       // (after a failed wait the rows go on, without waiting)
-      if (ok) ok = mbar_sleep(s_full + 16 * h + 8 * x, i & 1, abort_flag);
+      if (ok) ok = mbar_sleep(s_bar(g), (g >> 1) & 1, abort_flag);
       __syncwarp();
       tc_fence_after();
-      {
-        uint32_t w[KV8_BLOCK];
-        float sum;
-        for (bool again = false;; again = true) {
-          if (again || searching || raise_to != ref) {
-            // ---- a new reference: the row's largest score (where asked for)
-            float top = m;
-#pragma unroll 1
-            for (int c0 = 0; c0 < KV8_BLOCK; c0 += 32) {
-              float s[32];
-              tmem_ld32(s_at + c0, s);
+      float sum;
+      for (bool again = false;; again = true) {
+        if (again || searching || raise_to != ref) {
+          // ---- a new reference: the row's largest score (where asked for)
+          tmem_ld64(s_at, w);
+          float top = m;
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                top = fmaxf(top, c0 + c < limit ? s[c] * f : -INFINITY);
-            }
-            const float to_max = raise_max ? top : m;
-            float corr = to_max == -INFINITY ? 1.f : ex2_ftz(m - to_max);
-            l *= corr;
-            if (raise_to != ref && ref >= 0) corr *= scale_value(max(127 + ref - raise_to, 0));
-            m = to_max;
-            ref = raise_to;
+          for (int c = 0; c < KV8_BLOCK; ++c)
+            top = fmaxf(top, c < limit ? __uint_as_float(w[c]) * f : -INFINITY);
+          const float to_max = raise_max ? top : m;
+          float corr = to_max == -INFINITY ? 1.f : ex2_ftz(m - to_max);
+          l *= corr;
+          if (raise_to != ref && ref > NO_REF) corr *= ex2_ftz(ref - raise_to);
+          m = to_max;
+          ref = raise_to;
+          if (g > 0) {
             // once the P V before has ended (phase g - 1; the one before that
             // had when these scores were there)
-            if (g > 0) {
-              if (ok) ok = mbar_wait(o_done + 8 * x, h ^ 1, abort_flag);
-              __syncwarp();
-              tc_fence_after();
+            if (ok) ok = mbar_wait(o_done + 8 * x, (g - 1) & 1, abort_flag);
+            __syncwarp();
+            tc_fence_after();
 #pragma unroll 1
-              for (int c0 = 0; c0 < C::ODIM; c0 += 16) {
-                uint32_t o[16];
-                tmem_ld16_nowait(to + c0, o);
-                tmem_wait_ld();
+            for (int c0 = 0; c0 < C::ODIM; c0 += 16) {
+              uint32_t o[16];
+              tmem_ld16_nowait(to + c0, o);
+              tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
-                tmem_st16(to + c0, o);
-              }
-              tmem_wait_st();
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * corr);
+              tmem_st16(to + c0, o);
             }
+            tmem_wait_st();
           }
-          // ---- weights 2^(score - m + value scale's exponent over ref's);
-          // 2^-126 is the least that bf16 weights can carry, and the sum is
-          // taken from 2^-60 up, so that it keeps small weights
-          const float mm = m == -INFINITY ? 0.f : m;
-          const int d = max(bv - ref, -126);
-          const float dv = bv == 255 ? __uint_as_float(0x7fffffffu) : float(max(d, -60));
-          tmem_ld64(s_at, w);
-          float2 t;
-          if (whole) t = weights<true>(w, f, dv - mm, KV8_BLOCK, 1.f);
-          else t = weights<false>(w, f, dv - mm, limit, d < -60 ? scale_value(127 + d + 60) : 1.f);
-          // (a block that the row sees nothing of adds nothing, whatever its scale)
-          sum = limit > 0 ? (t.x + t.y) * ex2_ftz(-dv) : 0.f;
-          raise_max = sum > RAISE_SUM;
-          if (again || !__any_sync(0xffffffffu, raise_max)) break;
         }
-        l += sum;
-        tmem_st32(s_at, w);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 16 * h + 8 * x);
-        if (searching) searching = __any_sync(0xffffffffu, m == -INFINITY);
+        // ---- weights 2^(score - m + value scale's exponent over ref's);
+        // 2^-126 is the least that bf16 weights can carry, and the sum is
+        // taken from 2^-60 up, so that it keeps small weights
+        const float mm = m == -INFINITY ? 0.f : m;
+        const float d = now.y - ref, dv = fmaxf(d, -60.f), shift = dv - mm;
+        uint64_t total[2] = {0, 0};
+        tmem_ld64(s_at, w);
+        if (whole)
+          weights<true>(w, w, f, shift, KV8_BLOCK, 1.f, total);
+        else
+          weights<false>(w, w, f, shift, limit, ex2_ftz(fmaxf(d, -126.f) - dv), total);
+        const float2 t = split64(add2(total[0], total[1]));
+        // (a block that the row sees nothing of adds nothing, whatever its scale)
+        sum = limit > 0 ? (t.x + t.y) * ex2_ftz(-dv) : 0.f;
+        raise_max = sum > RAISE_SUM;
+        if (again || !__any_sync(0xffffffffu, raise_max)) break;
       }
+      l += sum;
+      tmem_st32(s_at, w);
+      hand_over(g);
+      page = next;
+      if (g + 1 < count) now = facts_of(page);
+      if (searching) searching = __any_sync(0xffffffffu, m == -INFINITY);
     }
+    ok = __all_sync(0xffffffffu, ok);
 
     // ---- result: O of a row in f32, or its part to be joined
     if (ok && mine > 0) ok = mbar_sleep_warp(o_full + 8 * x, 0, abort_flag);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
-    const float back = ref < 0 ? 0.f : scale_value(ref);
+    const float back = ref > NO_REF ? scale_value(int(ref)) : 0.f;
     const auto row_out = [&](int r) {
       const int qi = (row0 + r) / group, g = row0 + r - qi * group;
       return a.o + (long long)(q0 + qi) * a.ldo + (head * group + g) * DH;
@@ -620,61 +480,213 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
         if (in && ok) put(p + 8 * c, v, l == 0.f ? 0.f : inv);
       }
     } else {
-      // parts over the operands' memory, once every MMA has read it: per row
-      // its channels, its maximum, its sum.  One tile: both streams' parts of
-      // a row; two: each stream's own rows
-      soft_sync();
-      float* part_at = reinterpret_cast<float*>(smem) + (x * BQ + tr) * C::PSTRIDE;
-      for (int c = 0; c < DH / 8; ++c) {
-        float v[8];
-        if (mine > 0) eight(c, v);
-        else
-          for (int j = 0; j < 8; ++j) v[j] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) part_at[8 * c + j] = v[j];
-      }
-      part_at[DH] = blind ? -INFINITY : m;
-      part_at[DH + 1] = l;
+      // The row's parts (of both streams where they share a tile, of every CTA
+      // of the cluster) meet in the shared memory of the CTA that owns the row,
+      // over its operands once every MMA has read them: channels, maximum, sum.
+      const int streams = two ? 1 : 2, n = streams * parts;
+      const int each = ((two ? 2 : 1) * BQ + parts - 1) / parts;  // rows of a CTA
+      const auto slot = [&](int k, int r) { return sq + 4 * uint32_t((k * each + r) * C::PSTRIDE); };
       soft_sync();
       if (parts > 1) cluster_sync();
-      // the row's parts: streams (one tile) of each CTA of the cluster
-      const int streams = two ? 1 : 2, n = streams * parts;
-      const uint32_t base = sq;
-      const auto at = [&](int k, int r, int c) {
-        const uint32_t p = base + 4 * (((two ? 0 : k % streams) * BQ + r) * C::PSTRIDE + c);
-        float v;
-        if (parts == 1)
-          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(p));
-        else
-          asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                       : "=f"(v)
-                       : "r"(mapa_shared(p, uint32_t(k / streams))));
-        return v;
-      };
-      for (int e = part * 256 + int(threadIdx.x); e < rows * (DH / 8); e += parts * 256) {
-        const int r = e / (DH / 8), c = (e - r * (DH / 8)) * 8;
+      const uint32_t mine_at = slot(part * streams + (two ? 0 : x), ur % each);
+      const uint32_t put_at = parts > 1 ? mapa_shared(mine_at, uint32_t(ur / each)) : mine_at;
+#pragma unroll 1
+      for (int c = 0; c < DH / 8; ++c) {
+        float v[8] = {};
+        if (mine > 0) eight(c, v);  // (every row of a warp takes part in the load)
+        if (in) {
+          store_four(put_at + 32 * c, v);
+          store_four(put_at + 32 * c + 16, v + 4);
+        }
+      }
+      if (in) store_two(put_at + 4 * DH, blind ? -INFINITY : m, l);
+      if (parts > 1) cluster_sync();
+      else soft_sync();
+      const int first = part * each, live = min(each, rows - first);
+      for (int e = int(threadIdx.x); e < live * (DH / 8); e += 256) {
+        const int r = e / (DH / 8), c = e - r * (DH / 8);
+        const float* at = reinterpret_cast<const float*>(smem) + r * C::PSTRIDE;
+        const int far = each * C::PSTRIDE;  // from a row's part to its next
         float top = -INFINITY, total = 0.f, v[8] = {};
-        for (int k = 0; k < n; ++k) top = fmaxf(top, at(k, r, DH));
+        for (int k = 0; k < n; ++k) top = fmaxf(top, at[k * far + DH]);
         const float rf = top == -INFINITY ? 0.f : top;
         for (int k = 0; k < n; ++k) {
-          const float y = ex2_ftz(at(k, r, DH) - rf);
-          total += y * at(k, r, DH + 1);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] += y * at(k, r, c + j);
+          const float y = ex2_ftz(at[k * far + DH] - rf);
+          total += y * at[k * far + DH + 1];
+          const float4 p0 = *reinterpret_cast<const float4*>(at + k * far + 8 * c);
+          const float4 p1 = *reinterpret_cast<const float4*>(at + k * far + 8 * c + 4);
+          v[0] += y * p0.x; v[1] += y * p0.y; v[2] += y * p0.z; v[3] += y * p0.w;
+          v[4] += y * p1.x; v[5] += y * p1.y; v[6] += y * p1.z; v[7] += y * p1.w;
         }
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        if (ok) put(row_out(r) + c, v, inv);
+        if (ok) put(row_out(first + r) + 8 * c, v, total == 0.f ? 0.f : 1.f / total);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+    if (warp == MMA_WARP) {
+      // ----------------------------------------------------------------- MMA
+      // Each stream's S holds two cache blocks; the scores of the second next one
+      // follow the products that used their place, so that a stream's softmax
+      // finds its next scores ready.
+      if (nb > 0 && elect_one()) {
+        const int rounds = two ? nb : (nb + 1) / 2;  // key blocks of stream 0
+        // key block of a stream's i-th, and whether a stream is the first or the
+        // last to use it
+        const auto block = [&](int i, int x) { return two ? i : 2 * i + x; };
+        const auto scores = [&](int i, int h, int x) {
+          const int b = block(i, x), st = b % C::KST;
+          if (b >= nb) return true;
+          if (h == 0 && (!two || x == 0) &&
+              !mbar_wait(k_full + 8 * st, (b / C::KST) & 1, abort_flag)) return false;
+          tc_fence_after();
+          const uint32_t k = sk + st * C::K_BYTES + h * (KV8_BLOCK * 128);
+          const uint32_t d = tmem + uint32_t(x * BKV + h * KV8_BLOCK);
+          const int tile = two ? x : 0;
+          if constexpr (C::Q_TMEM) {
+            const uint32_t q = tmem + uint32_t(C::TM_Q + tile * C::Q_COLS);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              umma_bf16_ta(d, q + 8 * kk, sw128_desc(k) + 2 * kk, C::IDESC_S, kk ? 1u : 0u);
+            if (C::TAIL)
+              umma_bf16_ta(d, q + 32,
+                           sw32_kmajor_desc(sk + st * C::K_BYTES + BKV * 128 + h * (KV8_BLOCK * 32)),
+                           C::IDESC_S, 1u);
+          } else {
+            const uint32_t q = sq + tile * C::Q_BYTES;
+#pragma unroll
+            for (int f = 0; f < C::FULL; ++f)
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)
+                umma_bf16(d, sw128_desc(q + f * BQ * 128) + 2 * kk,
+                          sw128_desc(k + f * BKV * 128) + 2 * kk, C::IDESC_S, (f | kk) ? 1u : 0u);
+          }
+          umma_commit(s_full + 16 * h + 8 * x);
+          if (h == PAGES - 1 && (!two || x == 1)) umma_commit(k_empty + 8 * st);
+          return true;
+        };
+        ok = mbar_wait(q_full, 0, abort_flag);
+        for (int h = 0; h < PAGES; ++h)
+          for (int x = 0; x < 2; ++x) ok = ok && scores(0, h, x);
+        for (int i = 0; ok && i < rounds; ++i) {
+#pragma unroll
+          for (int h = 0; h < PAGES; ++h) {
+            for (int x = 0; x < 2; ++x) {
+              const int b = block(i, x), st = b % C::VST;
+              if (b >= nb) continue;
+            if ((h == 0 && (!two || x == 0) &&
+                   !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
+                  !mbar_wait(p_full + 16 * h + 8 * x, i & 1, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              const uint32_t d = tmem + uint32_t(TM_O + x * C::ODIM);
+              const uint32_t p = tmem + uint32_t(x * BKV + h * KV8_BLOCK);
+              const uint64_t v = sw128_mnmajor_desc_lbo(
+                  sv + st * C::V_BYTES + h * (KV8_BLOCK * 128), BKV * 128);
+#pragma unroll
+              for (int kk = 0; kk < KV8_BLOCK / 16; ++kk)
+                umma_bf16_ta(d, p + 8 * kk, v + 128 * kk, C::IDESC_PV, (i | h | kk) ? 1u : 0u);
+              umma_commit(o_done + 8 * x);
+              if (h == PAGES - 1) {
+                if (!two || x == 1) umma_commit(v_empty + 8 * st);
+                if (block(i + 1, x) >= nb) umma_commit(o_full + 8 * x);
+              }
+              if (!scores(i + 1, h, x)) { ok = false; break; }
+            }
+            if (!ok) break;
+          }
+        }
+      }
+    } else if (warp == LOAD_WARP) {
+      // ------------------------------------------------------------- loading
+      // (the copies are whole cache blocks; one that is missing is left out:
+      // what it leaves in the ring is hidden by the softmax)
+      if (elect_one()) {
+        int page[PAGES], ahead[2][PAGES];
+#pragma unroll
+        for (int i = 0; i < PAGES; ++i) {
+          ahead[0][i] = nb > 0 ? entry(PAGES * b0 + i) : -1;
+          ahead[1][i] = nb > 1 ? entry(PAGES * (b0 + 1) + i) : -1;
+        }
+        for (int j = 0; ok && j < 2 * nb; ++j) {
+          const int st = j % C::RAWS, side = j & 1, b = j >> 1;
+          if (side == 0)
+#pragma unroll
+            for (int i = 0; i < PAGES; ++i) {
+              page[i] = checked(ahead[0][i]);
+              if (page[i] < 0 && PAGES * (b0 + b) + i < pages) atomicOr(a.err, DEVERR_INDEX);
+              ahead[0][i] = ahead[1][i];
+              ahead[1][i] = b + 2 < nb ? entry(PAGES * (b0 + b + 2) + i) : -1;
+            }
+          if (!mbar_wait(raw_empty + 8 * st, ((j / C::RAWS) & 1) ^ 1, abort_flag)) { ok = false; break; }
+          constexpr uint32_t BYTES = KV8_BLOCK * DH;
+          mbar_expect_tx(raw_full + 8 * st,
+                         BYTES * ((page[0] >= 0 ? 1u : 0u) + (page[1] >= 0 ? 1u : 0u)));
+#pragma unroll
+          for (int i = 0; i < PAGES; ++i)
+            if (page[i] >= 0)
+              bulk_load(raw + st * C::RAW_BYTES + i * BYTES,
+                        pool.code[side] + ((long long)page[i] * pool.heads + head) * BYTES, BYTES,
+                        raw_full + 8 * st);
+        }
+      }
+    } else if (warp >= CONV_WARP) {
+      // ---------------------------------------------------------- conversion
+      // A thread takes one 8-code piece (8 channels) of every PASS-th row.
+      const bool values = warp >= CONV_WARP + 4;
+      const int tid = int(threadIdx.x) - (values ? CONV_WARP + 4 : CONV_WARP) * 32;
+      const int r0 = tid / C::PER_ROW, c = tid - r0 * C::PER_ROW;
+      const bool tail = C::TAIL && c == 8;
+      for (int b = 0; b < nb; ++b) {
+        const int j = 2 * b + (values ? 1 : 0), st = j % C::RAWS, ks = b % C::KST, vs = b % C::VST;
+      if (ok)
+        ok = (values ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
+                       : mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag)) &&
+               mbar_sleep(raw_full + 8 * st, (j / C::RAWS) & 1, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      const uint32_t from = raw + st * C::RAW_BYTES + (r0 * C::PER_ROW + c) * 8;
+        constexpr int PASSES = (BKV + C::PASS - 1) / C::PASS, BATCH = 5;
+#pragma unroll
+        for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
+          uint2 q[BATCH];
+#pragma unroll
+          for (int p = p0; p < p0 + BATCH && p < PASSES; ++p)
+            if (r0 < C::PASS && r0 + p * C::PASS < BKV) q[p - p0] = lds64(from + p * C::PASS * DH);
+#pragma unroll
+          for (int p = p0; p < p0 + BATCH && p < PASSES; ++p) {
+            const int r = r0 + p * C::PASS;
+            if (r0 >= C::PASS || r >= BKV) continue;
+            const uint2 u = q[p - p0];
+            if (values) {
+              sts128(sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
+                     codes_02(u.x), codes_13(u.x), codes_02(u.y), codes_13(u.y));
+            } else {
+              const uint32_t tile = sk + ks * C::K_BYTES;
+              sts128(tail ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
+                          : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
+                     e4m3x2_f16x2(u.x & 0xffffu), e4m3x2_f16x2(u.x >> 16),
+                     e4m3x2_f16x2(u.y & 0xffffu), e4m3x2_f16x2(u.y >> 16));
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(raw_empty + 8 * st);
+          mbar_arrive(values ? v_full + 8 * vs : k_full + 8 * ks);
+        }
       }
     }
   }
-  if (parts > 1 && warp >= CONV_WARP) cluster_sync();  // (as the softmax warps did)
+  if (parts > 1 && warp >= CONV_WARP) {  // (as the softmax warps did)
+    __syncwarp();
+    cluster_sync();
+    cluster_sync();
+  }
   if (!ok) {
     *abort_flag = 1;
     atomicOr(a.err, DEVERR_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();
-  if (parts > 1) cluster_sync();  // (no CTA leaves while its parts may be read)
   if (warp == MMA_WARP) {
     __syncwarp();
     tc_fence_after();
@@ -682,13 +694,49 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   }
 }
 
+constexpr int SMS = 152;
+
+// Rows of a unit and CTAs that share its keys, of least estimated time (us) for
+// requests of the mean number of rows and the longest possible length.  Rates
+// measured at 4096 keys, head_dim 72, 16 heads: a key block takes a unit of 256
+// rows 1.45 us and one of 128 1.1, a unit 4.5 beyond that, and joining parts 5
+// (2.5) and 0.65 for each (256 rows: one part 52.8 us, six 22.2; 831: two 35.3,
+// one 54.0; 4096: one 106, two 132).  Clusters above six CTAs do not all find a
+// place at once.
+struct Shape {
+  int unit_rows, parts;
+};
+Shape choose(const Kv8AttnArgs& a, int kv_heads, int group) {
+  const long long most = (long long)a.n * a.max_q, rows = most < a.q_rows ? most : a.q_rows;
+  const double mean = double(rows) * group / a.n;
+  const double blocks = double(a.ld_table) * KV8_BLOCK / BKV;
+  Shape best{256, 1};
+  double least = 1e30;
+  for (int ur = 256; ur >= 128; ur -= 128)
+    for (int parts = 1; parts <= 6; ++parts) {
+      if (parts > 1 && blocks < 2 * parts) break;
+      const double units = ceil(mean / ur) * kv_heads * a.n * parts;
+      const double waves = units <= SMS ? 1.0 : units / SMS + 0.5;
+      const bool wide = ur == 256 && mean > 128;
+      const double one = ceil(blocks / parts) * (wide ? 1.45 : 1.1) + 4.5 +
+                         (parts > 1 ? (wide ? 5.0 : 2.5) + 0.65 * parts : 0.0);
+      if (waves * one < least * 0.98) {
+        least = waves * one;
+        best = Shape{ur, parts};
+      }
+    }
+  return best;
+}
+
 template <int DH>
 cudaError_t many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   using C = MCfg<DH>;
   RC_TRY(cudaFuncSetAttribute(many_rows_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               int(C::SMEM)));
-  const int unit_rows = 256, parts = 1;
-  const long long rows = (long long)a.max_q * (a.heads / pool.heads);
+  const int group = a.heads / pool.heads;
+  const Shape sh = choose(a, pool.heads, group);
+  const int unit_rows = sh.unit_rows, parts = sh.parts;
+  const long long rows = (long long)a.max_q * group;
   const long long chunks = (rows + unit_rows - 1) / unit_rows;
   if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
   const dim3 grid(unsigned(parts), unsigned(a.n), unsigned(chunks * pool.heads));
