@@ -1,18 +1,23 @@
 // Attention of few query rows over the paged eight-bit cache (rc_kv8): what
-// bounds it is the cache's bytes, read once for each sixteen rows of a key head.
+// bounds it is the cache's bytes, read once for each eight or sixteen rows of a
+// key head.
 //
-// A unit is sixteen rows (query, head of the key head's group) of one request
-// and key head.  A cluster of up to eight CTAs shares the unit's keys, four
-// warps a CTA; a warp takes every fourth half block of its CTA's (32 tokens: a
+// A unit is up to 8 NR rows (query, head of the key head's group) of one
+// request and key head.  A cluster of CTAs shares the unit's keys, four warps a
+// CTA; a warp takes every fourth half block of its CTA's (32 tokens: a
 // contiguous run of keys and one of values), which bulk copies bring ahead of
-// it into a ring of its own.  Codes become f16 exactly in registers and go
-// through mma.sync with the rows as M = 16 (the tensor memory path has no use
-// for a sixteenth of its rows).  Keys and channels are taken in an order that
-// makes each lane's fragment a contiguous piece of a row: a sum's order is
-// free.  Running maximum and sum per row in f32; a block's key scale joins the
-// row's power of two in the exponent of one factor, its value scale multiplies
-// the block's products as they are added in f32.  Warps' and CTAs' parts are
-// added in their order, through shared memory and the cluster's.
+// it into a ring of its own.  Codes become f16 exactly in registers and are the
+// A operand of mma.sync (16 keys, then 16 channels), the rows N = 8: with rows
+// as M = 16 the same work took twice the MMAs and half as many more
+// instructions.  Keys and channels are taken in an order that makes each
+// lane's fragment a contiguous piece of a row: a sum's order is free.
+//   S^T = K Q^T    maximum and sum of a row over the eight lanes that hold it
+//   O^T += V^T P^T  P as B by transposing 8 x 8 tiles in registers
+// As in the kernel for many rows, a block's key scale joins the factor of its
+// scores and its value scale the exponent of its weights, both relative to
+// references that are raised (and O rescaled) only when the weights would
+// leave 2^12; weights are f16, so a block whose value scale lies more than
+// 2^10 below the reference is multiplied apart and added in f32.
 #include <math.h>
 
 #include "common.cuh"
@@ -26,20 +31,26 @@ namespace {
 
 using namespace rc::tc;
 
-constexpr int WARPS = 4, ROWS = 16, HALF = 32;  // HALF: tokens of a ring stage
+constexpr int WARPS = 4, HALF = 32;  // HALF: tokens of a ring stage
+constexpr int MAX_PARTS = 8;
+constexpr float ABSENT = -2e30f, NO_REF = -1e30f;
+// how far scores and value scales may pass their references, and fall below
+constexpr float RAISE = 8.f, RAISE_VALUE = 4.f, APART = -10.f;
 
-template <int DH>
+template <int DH, int NR>
 struct FCfg {
+  static constexpr int ROWS = 8 * NR;
   static constexpr int PART = HALF * DH;       // bytes of a stage's keys
   static constexpr int STAGE = 2 * PART;
   static constexpr int STAGES = DH == 128 ? 3 : 5;
   static constexpr int RING = WARPS * STAGES * STAGE;
   static constexpr int KS = (DH + 15) / 16;    // MMA steps of 16 channels
-  static constexpr int NB = DH / 8;            // blocks of 8 channels of the result
+  static constexpr int MB = (DH + 15) / 16;    // blocks of 16 channels of the result
   static constexpr int PSTRIDE = DH + 4;       // floats of a partial row: channels, max, sum
-  static constexpr int PARTS = WARPS * ROWS * PSTRIDE * 4;  // goes over the ring
-  static_assert(PARTS <= RING, "the parts fit the ring");
-  static constexpr size_t SMEM = size_t(RING) + WARPS * STAGES * 8 + 16;
+  static_assert(WARPS * ROWS * PSTRIDE * 4 <= RING, "the warps' parts fit the ring");
+  // a row's parts of the cluster's CTAs, in its owner
+  static constexpr int JOIN = (ROWS + MAX_PARTS) * PSTRIDE * 4;
+  static constexpr size_t SMEM = size_t(RING) + JOIN + WARPS * STAGES * 8 + 16;
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
@@ -49,17 +60,30 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
           "r"(dst), "l"(src), "r"(bytes), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
       "{%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {  // of an 8 x 8 tile of f16
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+  return r;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+// Four codes as f16: the lower and the upper two.
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
@@ -76,19 +100,70 @@ __device__ __forceinline__ uint32_t lds8(uint32_t a) {
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ float lds_cluster(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a));
-  return v;
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
-template <int DH>
+// O^T += V^T P^T of a half block: acc[mb][r] are 16 channels x 8 rows, pf the
+// weights of its two 16-key steps; `left` tokens of it are the request's (those
+// behind may hold NaN codes).
+template <int DH, int NR>
+__device__ __forceinline__ void add_values(float (*acc)[NR][4], const uint32_t (*pf)[NR][2],
+                                           uint32_t vs, int g, int t, int left) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t row = vs + (16 * u + t) * DH;
+#pragma unroll
+    for (int b = 0; b < DH / 64; ++b) {
+      uint2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = lds64(row + 4 * k * DH + 64 * b + 8 * g);
+        if (left < HALF && 16 * u + t + 4 * k >= left) v[k] = make_uint2(0, 0);
+      }
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t k0 = w ? v[0].y : v[0].x, k1 = w ? v[1].y : v[1].x;
+        const uint32_t k2 = w ? v[2].y : v[2].x, k3 = w ? v[3].y : v[3].x;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          // the channels 4 w + 2 p and the next of this lane's eight
+          const uint32_t sel = p ? 0x7362 : 0x5140;
+          uint32_t a0, a1, a2, a3;
+          codes_f16(__byte_perm(k0, k1, sel), a0, a1);
+          codes_f16(__byte_perm(k2, k3, sel), a2, a3);
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            mma_f16(acc[4 * b + 2 * w + p][r], a0, a1, a2, a3, pf[u][r][0], pf[u][r][1]);
+        }
+      }
+    }
+    if (DH == 72) {
+      uint32_t v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = lds8(row + 4 * k * DH + 64 + g);
+        if (left < HALF && 16 * u + t + 4 * k >= left) v[k] = 0;
+      }
+      uint32_t a0, a2;
+      codes_f16(v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24, a0, a2);
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+        mma_f16(acc[4][r], a0, 0u, a2, 0u, pf[u][r][0], pf[u][r][1]);
+    }
+  }
+}
+
+template <int DH, int NR>
 __global__ void __launch_bounds__(WARPS * 32, 2)
 few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
                 int parts) {
-  using C = FCfg<DH>;
+  using C = FCfg<DH, NR>;
   extern __shared__ __align__(128) uint8_t smem[];
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::JOIN);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + WARPS * C::STAGES);
   const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t ring = saddr(smem) + warp * (C::STAGES * C::STAGE);
@@ -111,44 +186,9 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     if (threadIdx.x == 0) atomicOr(a.err, DEVERR_COUNT);
     return;
   }
-  const int rows = nq * group, row0 = chunk * ROWS;
+  const int rows = nq * group, row0 = chunk * C::ROWS;  // (below 2^31: the entry point's check)
   if (row0 >= rows) return;
-
-  // ---- queries: two rows a lane, in the channel order of the key fragments
-  // (step s < 4 of a 64-channel part: channels 16 t + 4 s ..; the last 8 of 72:
-  // 4 t .. for t < 2), each row divided by the power of two of its largest
-  // magnitude so that it fits f16 (what falls below f16's range there is below
-  // 2^-24 of it)
-  uint32_t qf[C::KS][4];
-  int qe[2], seen[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = row0 + g + 8 * h;
-    const bool in = row < rows;
-    const int i = in ? row / group : 0;
-    seen[h] = !in ? 0 : a.causal ? max(0, len - nq + i + 1) : len;
-    const bf16* q = a.q + (long long)(q0 + i) * a.ldq + (head * group + row - i * group) * DH;
-    uint2 raw[C::KS];
-    uint32_t top = 0;
-#pragma unroll
-    for (int s = 0; s < C::KS; ++s) {
-      const int c = DH == 72 && s == 4 ? 64 + 4 * t : (s >> 2) * 64 + 16 * t + 4 * (s & 3);
-      raw[s] = make_uint2(0, 0);
-      if (in && c < DH) raw[s] = *reinterpret_cast<const uint2*>(q + c);
-      const uint32_t m = __vmaxu2(raw[s].x & 0x7fff7fffu, raw[s].y & 0x7fff7fffu);
-      top = max(top, max(m << 16, m & 0xffff0000u));
-    }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    qe[h] = min(int(top >> 23), 240);
-    const float f = __uint_as_float(uint32_t(254 - qe[h]) << 23);
-#pragma unroll
-    for (int s = 0; s < C::KS; ++s) {
-      const float2 lo = unpack_bf16x2(raw[s].x), hi = unpack_bf16x2(raw[s].y);
-      qf[s][h] = pack_f16(lo.x * f, lo.y * f);
-      qf[s][2 + h] = pack_f16(hi.x * f, hi.y * f);
-    }
-  }
+  if (parts > 1) cluster_arrive();  // (waited for before anything is put into a peer)
 
   // ---- this warp's half blocks: first + 4 i for i < mine
   const int halves = (len + HALF - 1) / HALF;
@@ -156,25 +196,28 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
   const int h1 = int((long long)(part + 1) * halves / parts);
   const int first = h0 + warp, mine = first < h1 ? (h1 - first + WARPS - 1) / WARPS : 0;
   const int* table = a.table + (long long)req * a.ld_table;
-  // lane l holds block and scale bytes of half blocks l of the current 32 and
-  // of the next 32
-  int page[2], sk[2], sv[2];
+  // lane l holds place, key scale (NaN: no value) and value exponent of half
+  // blocks l of the current 32 and of the next 32
+  int page[2];
+  float sk[2], sv[2];
   const auto look_up = [&](int from, int b) {
     page[b] = -1;
-    sk[b] = sv[b] = 0;
+    sk[b] = 0.f;
+    sv[b] = ABSENT;
     if (from + lane < mine) {
       const int p = table[(first + (from + lane) * WARPS) / (KV8_BLOCK / HALF)];
       if (p < 0 || p >= pool.blocks) {
         atomicOr(a.err, DEVERR_INDEX);
       } else {
         page[b] = p;
-        sk[b] = pool.scale[0][(long long)p * pool.heads + head];
-        sv[b] = pool.scale[1][(long long)p * pool.heads + head];
+        const int k = pool.scale[0][(long long)p * pool.heads + head];
+        const int v = pool.scale[1][(long long)p * pool.heads + head];
+        sk[b] = scale_value(max(k, v) == 255 ? 255 : k);
+        sv[b] = float(v);
       }
     }
   };
   look_up(0, 0);
-  look_up(32, 1);
   // (i is at most one batch of 32 ahead of the current one)
   const auto issue = [&](int i, int base) {
     if (i >= mine) return;
@@ -188,17 +231,72 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     bulk_load(ring + st * C::STAGE, pool.code[0] + at, C::PART, bar0 + 8 * st);
     bulk_load(ring + st * C::STAGE + C::PART, pool.code[1] + at, C::PART, bar0 + 8 * st);
   };
+  page[1] = -1;
   for (int i = 0; i < C::STAGES; ++i) issue(i, 0);
+  look_up(32, 1);
 
-  float o[C::NB][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  // ---- queries as B fragments, row 8 r + g, in the channel order of the keys
+  // (step s < 4 of a 64-channel part: channels 16 t + 4 s ..; the last 8 of 72:
+  // 4 t .. for t < 2), each row divided by the power of two of its largest
+  // magnitude so that it fits f16 (what falls below f16's range there is below
+  // 2^-24 of it).  Softmax works on rows 8 r + 2 t + c: their factors come from
+  // the lanes that hold them.
+  uint32_t qf[C::KS][NR][2];
+  float own[NR][2];
+  int seen[NR][2], least = len;
 #pragma unroll
-  for (int n = 0; n < C::NB; ++n)
+  for (int r = 0; r < NR; ++r) {
+    const int row = row0 + 8 * r + g;
+    const bool in = row < rows;
+    const int i = in ? row / group : 0;
+    const bf16* q = a.q + (long long)(q0 + i) * a.ldq + (head * group + row - i * group) * DH;
+    uint2 raw[C::KS];
+    uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[n][j] = 0.f;
-  const float unit = 1.4426950408889634f * rsqrtf(float(DH));  // scores in base 2
+    for (int s = 0; s < C::KS; ++s) {
+      const int c = DH == 72 && s == 4 ? 64 + 4 * t : (s >> 2) * 64 + 16 * t + 4 * (s & 3);
+      raw[s] = make_uint2(0, 0);
+      if (in && c < DH) raw[s] = *reinterpret_cast<const uint2*>(q + c);
+      const uint32_t m = __vmaxu2(raw[s].x & 0x7fff7fffu, raw[s].y & 0x7fff7fffu);
+      top = max(top, max(m << 16, m & 0xffff0000u));
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = min(int(top >> 23), 240);
+    const float f = __uint_as_float(uint32_t(254 - e) << 23);
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) {
+      const float2 lo = unpack_bf16x2(raw[s].x), hi = unpack_bf16x2(raw[s].y);
+      qf[s][r][0] = pack_f16(lo.x * f, lo.y * f);
+      qf[s][r][1] = pack_f16(hi.x * f, hi.y * f);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int er = __shfl_sync(0xffffffffu, e, 4 * (2 * t + c));
+      own[r][c] = 1.4426950408889634f * rsqrtf(float(DH)) * scale_value(er);  // in base 2
+      const int mr = row0 + 8 * r + 2 * t + c;
+      // (rows past the unit's last see what it sees)
+      seen[r][c] = a.causal ? max(0, len - nq + min(mr, rows - 1) / group + 1) : len;
+      least = min(least, seen[r][c]);
+    }
+  }
+  least = __reduce_min_sync(0xffffffffu, least);
+
+  float o[C::MB][NR][4], m[NR][2], l[NR][2], ref = NO_REF;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+#pragma unroll
+    for (int b = 0; b < C::MB; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[b][r][j] = 0.f;
+    m[r][0] = m[r][1] = -INFINITY;
+    l[r][0] = l[r][1] = 0.f;
+  }
   uint32_t phases = 0;  // a bit for each stage
   bool ok = true;
 
+  int st = 0;
+#pragma unroll 1
   for (int i = 0, base = 0; i < mine; ++i) {
     if (i - base == 32) {
       base += 32;
@@ -207,139 +305,145 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
       sv[0] = sv[1];
       look_up(base + 32, 1);
     }
-    const int src = i - base, st = i % C::STAGES;
-    const int p = __shfl_sync(0xffffffffu, page[0], src);
-    const int bk = __shfl_sync(0xffffffffu, sk[0], src);
-    const int bv = __shfl_sync(0xffffffffu, sv[0], src);
-    const int key0 = (first + i * WARPS) * HALF;
-    if (p >= 0) {
+    const float kf = __shfl_sync(0xffffffffu, sk[0], i - base);
+    const float bv = __shfl_sync(0xffffffffu, sv[0], i - base);
+    if (bv > NO_REF) {
+      const int key0 = (first + i * WARPS) * HALF;
       if (!mbar_sleep_warp(bar0 + 8 * st, (phases >> st) & 1, abort_flag)) { ok = false; break; }
       phases ^= 1u << st;
-      const uint32_t ks = ring + st * C::STAGE, vs = ks + C::PART;
-      // ---- scores of 32 keys: place n of 8-key block j is key
-      // 16 (j / 2) + 8 (j % 2) + n / 2 + 4 (n % 2), so that a lane's weights
-      // belong to keys t, t + 4, t + 8, t + 12 of each sixteen
-      float s[4][4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-        const uint32_t row = ks + (8 * j + (g >> 1) + 4 * (g & 1)) * DH;
-        uint32_t w[(C::KS + 3) & ~3];
-#pragma unroll
-        for (int b = 0; b < DH / 64; ++b) {
-          const uint2 x = lds64(row + 64 * b + 16 * t), y = lds64(row + 64 * b + 16 * t + 8);
-          w[4 * b] = x.x;
-          w[4 * b + 1] = x.y;
-          w[4 * b + 2] = y.x;
-          w[4 * b + 3] = y.y;
-        }
-        if (DH == 72) w[4] = t < 2 ? lds32(row + 64 + 4 * t) : 0u;
-#pragma unroll
-        for (int k = 0; k < C::KS; ++k)
-          mma_f16(s[j], qf[k], e4m3x2_f16x2(w[k] & 0xffffu), e4m3x2_f16x2(w[k] >> 16));
-      }
-      // ---- softmax of the two rows
-      float corr[2];
-      bool any[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // 2^(row's exponent + block's) log2(e) / sqrt(DH)
-        const int e = qe[h] + bk - 127;
-        const float f = bk == 255 ? __uint_as_float(0x7fffffffu)
-                        : e < 1   ? 0.f
-                                  : unit * __uint_as_float(uint32_t(min(e, 254)) << 23);
-        any[h] = seen[h] > key0;
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float& x = s[j][2 * h + c];
-            x = key0 + 8 * j + t + 4 * c < seen[h] ? x * f : -INFINITY;
-            top = fmaxf(top, x);
-          }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const float next = fmaxf(m[h], top), ref = next == -INFINITY ? 0.f : next;
-        corr[h] = ex2_ftz(m[h] - ref);
-        m[h] = next;
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float& x = s[j][2 * h + c];
-            x = ex2_ftz(x - ref);
-            sum += x;
-          }
-        l[h] = l[h] * corr[h] + sum;  // (this lane's keys; the lanes' sums meet at the end)
-      }
-      // ---- values: weights of sixteen keys as A fragments (f16: half a step
-      // is 2^-11 of a weight), eight channels at a time as B
-      uint32_t pf[2][4];
+      const uint32_t ks = ring + st * C::STAGE;
+      // ---- scores of 32 keys, 16 an MMA: its row n is key n / 2 + 4 (n % 2)
+      // (+ 8 for n >= 8), so that a lane's weights, transposed, belong to keys
+      // t, t + 4, t + 8, t + 12 of each sixteen
+      float s[2][NR][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        pf[u][0] = pack_f16(s[2 * u][0], s[2 * u][1]);
-        pf[u][1] = pack_f16(s[2 * u][2], s[2 * u][3]);
-        pf[u][2] = pack_f16(s[2 * u + 1][0], s[2 * u + 1][1]);
-        pf[u][3] = pack_f16(s[2 * u + 1][2], s[2 * u + 1][3]);
-      }
-      const float value = scale_value(bv);
-      const int left = len - key0;  // (tokens behind the last may hold NaN codes)
-      const auto add = [&](int n, const float* x) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int r = 0; r < NR; ++r) s[u][r][0] = s[u][r][1] = s[u][r][2] = s[u][r][3] = 0.f;
+        const uint32_t row = ks + (16 * u + (g >> 1) + 4 * (g & 1)) * DH;
+        uint32_t w[2][(C::KS + 3) & ~3];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {  // keys of rows g and g + 8
+#pragma unroll
+          for (int b = 0; b < DH / 64; ++b) {
+            const uint2 x = lds64(row + 8 * k * DH + 64 * b + 16 * t);
+            const uint2 y = lds64(row + 8 * k * DH + 64 * b + 16 * t + 8);
+            w[k][4 * b] = x.x;
+            w[k][4 * b + 1] = x.y;
+            w[k][4 * b + 2] = y.x;
+            w[k][4 * b + 3] = y.y;
+          }
+          if (DH == 72) w[k][4] = t < 2 ? lds32(row + 8 * k * DH + 64 + 4 * t) : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < C::KS; ++k) {
+          uint32_t a0, a1, a2, a3;
+          codes_f16(w[0][k], a0, a2);
+          codes_f16(w[1][k], a1, a3);
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+            mma_f16(s[u][r], a0, a1, a2, a3, qf[k][r][0], qf[k][r][1]);
+        }
+      }
+      // ---- in base 2, hidden ones -infinity; this lane's largest of each row.
+      // Place [u][r][2 j + c] is key 16 u + 8 j + g / 2 + 4 (g % 2), row 2 t + c
+      const bool whole = least - key0 >= HALF;
+      float top[NR][2];
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float f = own[r][c] * kf;
+          f = f > 3e38f ? 3e38f : f;  // (an infinite factor would make NaN of a score of 0)
+          top[r][c] = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float& x = s[u][r][2 * j + c];
+              x *= f;
+              if (!whole &&
+                  key0 + 16 * u + 8 * j + (g >> 1) + 4 * (g & 1) >= seen[r][c]) x = -INFINITY;
+              top[r][c] = fmaxf(top[r][c], x);
+            }
+        }
+      // ---- references: raised where a row's scores, or the values, pass them
+      bool raise = bv > ref + RAISE_VALUE;
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) raise |= top[r][c] > m[r][c] + RAISE;
+      if (__any_sync(0xffffffffu, raise)) {
+        const float to = bv > ref + RAISE_VALUE ? bv : ref;
+        const float values = ref > NO_REF ? ex2_ftz(ref - to) : 1.f;
+        ref = to;
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float& y = o[n][2 * h + c];
-            y = y * corr[h] + (any[h] ? value * x[2 * h + c] : 0.f);
-          }
-      };
+            float x = top[r][c];  // of the eight lanes that hold the row
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            x = fmaxf(x, m[r][c]);
+            const float corr = x == -INFINITY ? 1.f : ex2_ftz(m[r][c] - x);
+            m[r][c] = x;
+            l[r][c] *= corr;
 #pragma unroll
-      for (int b = 0; b < DH / 64; ++b) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          float x[4][4];
-#pragma unroll
-          for (int n = 0; n < 4; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            uint32_t v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int key = 16 * u + t + 4 * k;
-              v[k] = lds32(vs + key * DH + 64 * b + 8 * g + 4 * w);
-              if (key >= left) v[k] = 0;
+            for (int b = 0; b < C::MB; ++b) {
+              o[b][r][c] *= corr * values;
+              o[b][r][2 + c] *= corr * values;
             }
-            const uint32_t a01 = __byte_perm(v[0], v[1], 0x5140), b01 = __byte_perm(v[0], v[1], 0x7362);
-            const uint32_t a23 = __byte_perm(v[2], v[3], 0x5140), b23 = __byte_perm(v[2], v[3], 0x7362);
-            mma_f16(x[0], pf[u], e4m3x2_f16x2(a01 & 0xffffu), e4m3x2_f16x2(a23 & 0xffffu));
-            mma_f16(x[1], pf[u], e4m3x2_f16x2(a01 >> 16), e4m3x2_f16x2(a23 >> 16));
-            mma_f16(x[2], pf[u], e4m3x2_f16x2(b01 & 0xffffu), e4m3x2_f16x2(b23 & 0xffffu));
-            mma_f16(x[3], pf[u], e4m3x2_f16x2(b01 >> 16), e4m3x2_f16x2(b23 >> 16));
           }
-#pragma unroll
-          for (int n = 0; n < 4; ++n) add(8 * b + 4 * w + n, x[n]);
-        }
       }
-      if (DH == 72) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
+      // ---- weights: f16 (half a step is 2^-11 of a weight), transposed to B
+      const float d = bv - ref;
+      const bool apart = d < APART;
+      const float dv = apart ? 0.f : d, back = ex2_ftz(-dv);
+      uint32_t pf[2][NR][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          uint32_t v[4];
+      for (int r = 0; r < NR; ++r) {
+        float sum[2] = {0.f, 0.f};
+        const float m0 = m[r][0] == -INFINITY ? 0.f : m[r][0] - dv;
+        const float m1 = m[r][1] == -INFINITY ? 0.f : m[r][1] - dv;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int key = 16 * u + t + 4 * k;
-            v[k] = lds8(vs + key * DH + 64 + g);
-            if (key >= left) v[k] = 0;
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float x = ex2_ftz(s[u][r][2 * j] - m0), y = ex2_ftz(s[u][r][2 * j + 1] - m1);
+            sum[0] += x;
+            sum[1] += y;
+            pf[u][r][j] = transposed(pack_f16(x, y));
           }
-          mma_f16(x, pf[u], e4m3x2_f16x2(v[0] | v[1] << 8), e4m3x2_f16x2(v[2] | v[3] << 8));
-        }
-        add(C::NB - 1, x);
+        // (this lane's keys; the lanes' sums meet at the end)
+        l[r][0] += sum[0] * back;
+        l[r][1] += sum[1] * back;
+      }
+      // ---- values
+      const int left = len - key0;
+      if (!apart) {
+        add_values<DH, NR>(o, pf, ks + C::PART, g, t, left);
+      } else {
+        float x[C::MB][NR][4];
+        const float f = ex2_ftz(fmaxf(d, -126.f));
+#pragma unroll
+        for (int b = 0; b < C::MB; ++b)
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[b][r][j] = 0.f;
+        add_values<DH, NR>(x, pf, ks + C::PART, g, t, left);
+#pragma unroll
+        for (int b = 0; b < C::MB; ++b)
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[b][r][j] += f * x[b][r][j];
       }
       __syncwarp();  // the stage has been read
     }
     issue(i + C::STAGES, base);
+    if (++st == C::STAGES) st = 0;
   }
   if (!ok) {
     *abort_flag = 1;
@@ -348,117 +452,126 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
 
   // ---- the warps' parts, over the ring: per row its channels, maximum, sum
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-  }
+  for (int r = 0; r < NR; ++r)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int x = 4; x < 32; x *= 2) l[r][c] += __shfl_xor_sync(0xffffffffu, l[r][c], x);
   __syncthreads();
-  float* mine_at = reinterpret_cast<float*>(smem) + warp * ROWS * C::PSTRIDE;
+  const float unit = ref > NO_REF ? scale_value(int(ref)) : 0.f;
+  float* mine_at = reinterpret_cast<float*>(smem) + warp * C::ROWS * C::PSTRIDE;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float* r = mine_at + (g + 8 * h) * C::PSTRIDE;
+  for (int r = 0; r < NR; ++r)
 #pragma unroll
-    for (int n = 0; n < C::NB; ++n)
+    for (int c = 0; c < 2; ++c) {
+      float* row = mine_at + (8 * r + 2 * t + c) * C::PSTRIDE;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int place = 2 * t + c;  // the result's column of its 8-channel block
-        const int ch = DH == 72 && n == 8 ? 64 + place : (n >> 3) * 64 + 8 * place + (n & 7);
-        r[ch] = o[n][2 * h + c];
+      for (int b = 0; b < C::MB; ++b) {
+        if (DH == 72 && b == 4) {
+          row[64 + g] = o[b][r][c] * unit;
+        } else {  // channels 8 g + 2 (b % 4) and the next of a 64-channel part
+          const int ch = 64 * (b >> 2) + 8 * g + 2 * (b & 3);
+          row[ch] = o[b][r][c] * unit;
+          row[ch + 1] = o[b][r][2 + c] * unit;
+        }
       }
-    if (t == 0) {
-      r[DH] = m[h];
-      r[DH + 1] = l[h];
+      if (g == 0) {
+        row[DH] = m[r][c];
+        row[DH + 1] = l[r][c];
+      }
     }
-  }
   __syncthreads();
-  const auto join = [&](int row, int ch, int n, auto at, float& top, float& sum) {
-    // n parts of a row's channel: their common maximum, sum and products
+  // n parts of a row's channel, `far` floats apart: their common maximum, sum
+  // and products
+  const auto join = [&](const float* at, int n, int far, int ch, float& top, float& sum) {
     top = -INFINITY;
-    for (int p = 0; p < n; ++p) top = fmaxf(top, at(p, row, DH));
-    const float ref = top == -INFINITY ? 0.f : top;
+    for (int p = 0; p < n; ++p) top = fmaxf(top, at[p * far + DH]);
+    const float base = top == -INFINITY ? 0.f : top;
     float x = 0.f;
     sum = 0.f;
     for (int p = 0; p < n; ++p) {
-      const float f = ex2_ftz(at(p, row, DH) - ref);
-      x += f * at(p, row, ch);
-      sum += f * at(p, row, DH + 1);
+      const float f = ex2_ftz(at[p * far + DH] - base);
+      x += f * at[p * far + ch];
+      sum += f * at[p * far + DH + 1];
     }
     return x;
   };
-  const int live = min(ROWS, rows - row0);
+  const int live = min(C::ROWS, rows - row0);
   const auto write = [&](int row, int ch, float x, float sum) {
     const int i = (row0 + row) / group, h = head * group + row0 + row - i * group;
     a.o[(long long)(q0 + i) * a.ldo + h * DH + ch] = f2bf(sum == 0.f ? 0.f : x / sum);
   };
   const float* warps = reinterpret_cast<const float*>(smem);
-  const auto of_warp = [&](int p, int row, int c) {
-    return warps[(p * ROWS + row) * C::PSTRIDE + c];
-  };
-  if (parts == 1) {
-    for (int e = threadIdx.x; e < live * DH; e += WARPS * 32) {
-      float top, sum;
-      const float x = join(e / DH, e % DH, WARPS, of_warp, top, sum);
-      write(e / DH, e % DH, x, sum);
-    }
-    return;
-  }
-  // the CTA's part, behind the warps'
-  float* cta = reinterpret_cast<float*>(smem) + WARPS * ROWS * C::PSTRIDE;
-  static_assert(C::PARTS + ROWS * C::PSTRIDE * 4 <= C::RING, "the CTA's part fits the ring");
+  // row r's owner in the cluster is CTA r mod parts, which keeps its parts at
+  // [r / parts][part]
+  const uint32_t joined = saddr(smem) + C::RING;
+  if (parts > 1) cluster_wait();  // (every CTA of the cluster has begun)
   for (int e = threadIdx.x; e < live * DH; e += WARPS * 32) {
     float top, sum;
-    const int row = e / DH, ch = e % DH;
-    cta[row * C::PSTRIDE + ch] = join(row, ch, WARPS, of_warp, top, sum);
-    if (ch == 0) {
-      cta[row * C::PSTRIDE + DH] = top;
-      cta[row * C::PSTRIDE + DH + 1] = sum;
+    const int row = e / DH, ch = e - row * DH;
+    const float x = join(warps + row * C::PSTRIDE, WARPS, C::ROWS * C::PSTRIDE, ch, top, sum);
+    if (parts == 1) {
+      write(row, ch, x, sum);
+      continue;
     }
+    const uint32_t at = mapa_shared(
+        joined + 4 * ((row / parts * parts + part) * C::PSTRIDE), uint32_t(row % parts));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4 * ch), "f"(x) : "memory");
+    if (ch == 0)
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at + 4 * DH), "f"(top),
+                   "f"(sum)
+                   : "memory");
   }
+  if (parts == 1) return;
   cluster_sync();
-  const uint32_t base = saddr(cta);
-  const auto of_cta = [&](int p, int row, int c) {
-    return lds_cluster(mapa_shared(base + 4 * (row * C::PSTRIDE + c), uint32_t(p)));
-  };
-  for (int e = part * WARPS * 32 + threadIdx.x; e < live * DH; e += parts * WARPS * 32) {
+  const float* parts_at = reinterpret_cast<const float*>(smem + C::RING);
+  const int rows_here = live > part ? (live - part + parts - 1) / parts : 0;
+  for (int e = threadIdx.x; e < rows_here * DH; e += WARPS * 32) {
     float top, sum;
-    const float x = join(e / DH, e % DH, parts, of_cta, top, sum);
-    write(e / DH, e % DH, x, sum);
+    const int k = e / DH, ch = e - k * DH;
+    const float x = join(parts_at + k * parts * C::PSTRIDE, parts, C::PSTRIDE, ch, top, sum);
+    write(k * parts + part, ch, x, sum);
   }
-  cluster_sync();  // (no CTA leaves while its part may be read)
 }
 
 constexpr int SMS = 152;
 
-template <int DH>
+template <int DH, int NR>
 cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
-  using C = FCfg<DH>;
-  RC_TRY(cudaFuncSetAttribute(few_rows_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              int(C::SMEM)));
+  using C = FCfg<DH, NR>;
+  RC_TRY(cudaFuncSetAttribute(few_rows_kernel<DH, NR>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM)));
   const int group = a.heads / pool.heads;
-  const long long chunks = ((long long)a.max_q * group + ROWS - 1) / ROWS;
+  const long long chunks = ((long long)a.max_q * group + C::ROWS - 1) / C::ROWS;
   const long long units = chunks * pool.heads * a.n;
   // Enough CTAs for two an SM, several times over where lengths may differ,
   // and no fewer than four half blocks a warp
   long long parts = (2 * SMS * (a.n > 1 ? 4 : 1)) / units;
   const long long most = (long long)a.ld_table * (KV8_BLOCK / HALF) / (4 * WARPS);
   if (parts > most) parts = most;
-  if (parts > 8) parts = 8;
+  if (parts > MAX_PARTS) parts = MAX_PARTS;
   if (parts < 1) parts = 1;
   if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
   const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
   count_launches(1);
-  return launch_k_cluster(few_rows_kernel<DH>, grid, dim3(WARPS * 32), C::SMEM, int(parts), st,
+  return launch_k_cluster(few_rows_kernel<DH, NR>, grid, dim3(WARPS * 32), C::SMEM, int(parts), st,
                           pool, a, int(parts));
+}
+
+template <int NR>
+cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
+  switch (pool.dh) {
+    case 64: return few<64, NR>(pool, a, st);
+    case 72: return few<72, NR>(pool, a, st);
+    default: return few<128, NR>(pool, a, st);
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_kv8_few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
-  switch (pool.dh) {
-    case 64: return few<64>(pool, a, st);
-    case 72: return few<72>(pool, a, st);
-    default: return few<128>(pool, a, st);
-  }
+  if ((long long)a.max_q * (a.heads / pool.heads) <= 8) return few<1>(pool, a, st);
+  return few<2>(pool, a, st);
 }
 
 }  // namespace rc
