@@ -3,10 +3,10 @@
 // key head.
 //
 // A unit is up to 8 NR rows (query, head of the key head's group) of one
-// request and key head.  A cluster of CTAs shares the unit's keys, four warps a
-// CTA; a warp takes every fourth half block of its CTA's (32 tokens: a
-// contiguous run of keys and one of values), which bulk copies bring ahead of
-// it into a ring of its own.  Codes become f16 exactly in registers and are the
+// request and key head.  A cluster of CTAs shares the unit's keys, six warps a CTA
+// and two CTAs an SM; a warp takes every sixth half block of its CTA's (32
+// tokens: a contiguous run of keys and one of values), which bulk copies bring
+// ahead of it into a ring of its own.  Codes become f16 exactly in registers and are the
 // A operand of mma.sync (16 keys, then 16 channels), the rows N = 8: with rows
 // as M = 16 the same work took twice the MMAs and half as many more
 // instructions.  Keys and channels are taken in an order that makes each
@@ -31,7 +31,7 @@ namespace {
 
 using namespace rc::tc;
 
-constexpr int WARPS = 4, HALF = 32;  // HALF: tokens of a ring stage
+constexpr int HALF = 32;  // tokens of a ring stage
 constexpr int MAX_PARTS = 8;
 constexpr float ABSENT = -2e30f, NO_REF = -1e30f;
 // how far scores and value scales may pass their references, and fall below
@@ -40,9 +40,10 @@ constexpr float RAISE = 8.f, RAISE_VALUE = 4.f, APART = -10.f;
 template <int DH, int NR>
 struct FCfg {
   static constexpr int ROWS = 8 * NR;
+  static constexpr int WARPS = 6;
   static constexpr int PART = HALF * DH;       // bytes of a stage's keys
   static constexpr int STAGE = 2 * PART;
-  static constexpr int STAGES = DH == 128 ? 3 : 5;
+  static constexpr int STAGES = DH == 128 ? 2 : DH == 72 ? 3 : 4;
   static constexpr int RING = WARPS * STAGES * STAGE;
   static constexpr int KS = (DH + 15) / 16;    // MMA steps of 16 channels
   static constexpr int MB = (DH + 15) / 16;    // blocks of 16 channels of the result
@@ -158,10 +159,11 @@ __device__ __forceinline__ void add_values(float (*acc)[NR][4], const uint32_t (
 }
 
 template <int DH, int NR>
-__global__ void __launch_bounds__(WARPS * 32, 2)
+__global__ void __launch_bounds__(FCfg<DH, NR>::WARPS * 32, 2)
 few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
                 int parts) {
   using C = FCfg<DH, NR>;
+  constexpr int WARPS = C::WARPS;
   extern __shared__ __align__(128) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::JOIN);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + WARPS * C::STAGES);
@@ -190,7 +192,7 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
   if (row0 >= rows) return;
   if (parts > 1) cluster_arrive();  // (waited for before anything is put into a peer)
 
-  // ---- this warp's half blocks: first + 4 i for i < mine
+  // ---- this warp's half blocks: first + WARPS i for i < mine
   const int halves = (len + HALF - 1) / HALF;
   const int h0 = int((long long)part * halves / parts);
   const int h1 = int((long long)(part + 1) * halves / parts);
@@ -539,16 +541,23 @@ constexpr int SMS = 152;
 template <int DH, int NR>
 cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   using C = FCfg<DH, NR>;
+  constexpr int WARPS = C::WARPS;
   RC_TRY(cudaFuncSetAttribute(few_rows_kernel<DH, NR>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM)));
   const int group = a.heads / pool.heads;
   const long long chunks = ((long long)a.max_q * group + C::ROWS - 1) / C::ROWS;
   const long long units = chunks * pool.heads * a.n;
-  // Enough CTAs for two an SM, several times over where lengths may differ,
-  // and no fewer than four half blocks a warp
-  long long parts = (2 * SMS * (a.n > 1 ? 4 : 1)) / units;
-  const long long most = (long long)a.ld_table * (KV8_BLOCK / HALF) / (4 * WARPS);
-  if (parts > most) parts = most;
+  // CTAs for two an SM at once; more of them where requests may differ much,
+  // as long as a warp keeps 24 half blocks, beside which a CTA's 6 us of start
+  // and end count little (16 heads of 72: 8 requests of 4096 tokens, one part
+  // 25.9 us, two 20.6, eight 32.6; 16: one 32.1, two 38.1.  48 requests of 500 to
+  // 12000 tokens, 8 key heads of 128: one 131.5, four 117.7, eight 142.4)
+  const long long halves = (long long)a.ld_table * (KV8_BLOCK / HALF);
+  long long parts = 2 * SMS / units, more = halves / (24 * WARPS);
+  if (more > 4) more = 4;
+  if (parts > 4 && units * parts > 240) parts = 240 / units;  // (larger clusters need room)
+  if (a.n > 1 && parts < more) parts = more;
+  if (parts > halves / WARPS) parts = halves / WARPS;
   if (parts > MAX_PARTS) parts = MAX_PARTS;
   if (parts < 1) parts = 1;
   if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
