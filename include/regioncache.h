@@ -569,7 +569,7 @@ typedef struct rc_kv8 {
  *   row_offsets  out, i32 [n_requests + 1]: the rows of all requests one after
  *                another; request r owns rows row_offsets[r] ..
  *   slots        out, i32 [n_slots]: the slot of each row; entries behind the
- *                last row are -1.  n_slots >= the sum of counts.
+ *                last row are -1.  The sum of counts <= n_slots <= 2^30.
  * Without positions (null) the rows are the request's last counts[r] tokens.
  * Blocks that no earlier token lies in are taken from free_blocks (i32
  * [n_free], null: 0 .. n_free - 1) in order, request by request, and written

@@ -137,7 +137,7 @@ rc_status rc_kv8_tables(rc_ctx* c, const int32_t* lengths, const int32_t* counts
   if (!c || !lengths || !table || !row_offsets || !used || (n_slots > 0 && !slots))
     return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
   if (n < 1 || n > RC_KV8_MAX_REQUESTS || n_free < 0 || n_free > 0x7fffffff / RC_KV8_BLOCK ||
-      ld_table < 1 || ld_table > 0x7fffffff / RC_KV8_BLOCK || n_slots < 0)
+      ld_table < 1 || ld_table > 0x7fffffff / RC_KV8_BLOCK || n_slots < 0 || n_slots > 1 << 30)
     return fail(RC_ERR_SHAPE, "%s: %d requests (at most %d), %d free blocks, ld_table %d, %d slots",
                 fn, n, RC_KV8_MAX_REQUESTS, n_free, ld_table, n_slots);
   const void* ints[] = {lengths, counts, positions, free_blocks, table, row_offsets, slots, used};

@@ -10,41 +10,52 @@ namespace {
 constexpr int GROUP = 128;  // columns of a scale
 
 // ------------------------------------------------------------- quantiser
-// One scale per row and 128 columns: half a warp takes the 128 values of a
-// group (16 lanes of eight values), finds their largest magnitude by four
-// shuffles and writes its 128 codes; one pass over x.
+// One scale per row and 128 columns.  A warp takes eight groups of its row, two
+// at a time: the 16 lanes of a group hold eight values each, find the largest
+// magnitude by four shuffles and write the codes; one pass over x with four
+// loads a lane under way.  The scales of a CTA's eight rows leave together.
+// (With the groups of all rows dealt one by one, and their scales written byte
+// by byte: 4096 x 4608 bf16 15.5 us.)
+constexpr int ROWS = 8, GROUPS = 8;  // of a CTA
 template <class T, bool WIDE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(32 * ROWS)
 quant_rows_kernel(const T* __restrict__ x, int ldx, int rows, int cols, int groups,
                   uint8_t* __restrict__ codes, int ld, uint8_t* __restrict__ scales, int lds) {
   pdl_wait();
   pdl_trigger();
-  const int half = (blockIdx.x * 256 + threadIdx.x) >> 4, halves = gridDim.x * 16;
-  const int sub = threadIdx.x & 15;
-  const long long units = (long long)rows * groups;
-  const long long rounds = (units + halves - 1) / halves;
-  for (long long it = 0; it < rounds; ++it) {  // (every lane takes part in the shuffles)
-    const long long u = it * halves + half;
-    const int r = int(u / groups), g = int(u - (long long)r * groups);
-    const int c = g * GROUP + sub * 8;
-    const int n = u < units ? cols - c : 0;
-    Eight<T> v;
-    if (WIDE && n >= 8) v.load(x + (long long)r * ldx + c);
-    else if (n > 0) v.load_some(x + (long long)r * ldx + c, n);
-    else v.zero();
-    uint32_t top = v.top();
+  __shared__ uint8_t s_scale[GROUPS][ROWS];
+  const int warp = threadIdx.x >> 5, half = (threadIdx.x >> 4) & 1, sub = threadIdx.x & 15;
+  const long long r0 = (long long)blockIdx.x * ROWS, r = r0 + warp;
+  const int g0 = blockIdx.y * GROUPS;
+  Eight<T> v[GROUPS / 2];
+  int n[GROUPS / 2];
+#pragma unroll
+  for (int i = 0; i < GROUPS / 2; ++i) {
+    const int c = (g0 + 2 * i + half) * GROUP + sub * 8;
+    n[i] = r < rows ? cols - c : 0;
+    if (WIDE && n[i] >= 8) v[i].load(x + r * ldx + c);
+    else if (n[i] > 0) v[i].load_some(x + r * ldx + c, n[i]);
+    else v[i].zero();
+  }
+#pragma unroll
+  for (int i = 0; i < GROUPS / 2; ++i) {
+    uint32_t top = v[i].top();
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const int b = scale_byte(top);
-    const uint2 q = v.codes(scale_inverse(b));
-    uint8_t* dst = codes + (long long)r * ld + c;
-    if (n >= 8) {
+    const uint2 q = v[i].codes(scale_inverse(b));
+    uint8_t* dst = codes + r * ld + (g0 + 2 * i + half) * GROUP + sub * 8;
+    if (n[i] >= 8) {
       *reinterpret_cast<uint2*>(dst) = q;
     } else {
-      for (int i = 0; i < n; ++i) dst[i] = uint8_t((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+      for (int k = 0; k < n[i]; ++k) dst[k] = uint8_t((k < 4 ? q.x : q.y) >> (8 * (k & 3)));
     }
-    if (sub == 0 && u < units) scales[(long long)g * lds + r] = uint8_t(b);
+    if (sub == 0) s_scale[2 * i + half][warp] = uint8_t(b);
   }
+  __syncthreads();
+  const int k = threadIdx.x % ROWS, g = threadIdx.x / ROWS;
+  if (g < GROUPS && g0 + g < groups && r0 + k < rows)
+    scales[(long long)(g0 + g) * lds + r0 + k] = s_scale[g][k];
 }
 
 // One scale per 128 x 128 values: a CTA holds the block in registers (16
@@ -96,13 +107,12 @@ template <class T, bool WIDE>
 cudaError_t quantize(const T* x, int ldx, const Fp8Mat& out, cudaStream_t st) {
   const int groups = (out.cols + GROUP - 1) / GROUP;
   count_launches(1);
-  if (out.group == 1) {
-    const long long units = (long long)out.rows * groups;
-    const long long ctas = (units + 15) / 16;
-    return launch_k(quant_rows_kernel<T, WIDE>, dim3(unsigned(ctas < 152 * 8 ? ctas : 152 * 8)),
-                    dim3(256), 0, st, x, ldx, out.rows, out.cols, groups, out.codes, out.ld,
+  if (out.group == 1)
+    return launch_k(quant_rows_kernel<T, WIDE>,
+                    dim3(unsigned((out.rows + (long long)ROWS - 1) / ROWS),
+                         unsigned((groups + GROUPS - 1) / GROUPS)),
+                    dim3(32 * ROWS), 0, st, x, ldx, out.rows, out.cols, groups, out.codes, out.ld,
                     out.scales, out.lds);
-  }
   return launch_k(quant_blocks_kernel<T, WIDE>,
                   dim3(unsigned((out.rows + 127LL) / 128), unsigned(groups)), dim3(256), 0, st, x,
                   ldx, out.rows, out.cols, out.codes, out.ld, out.scales, out.lds);

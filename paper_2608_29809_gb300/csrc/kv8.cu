@@ -7,18 +7,24 @@ namespace rc {
 
 namespace {
 
+constexpr int SMS = 152;
+
 // ------------------------------------------------------- tables and slots
 // One launch: every CTA sums the requests' rows and new blocks itself (at most
 // KV8_MAX_REQUESTS of them, four a thread) and then writes its own part of the
-// slot map.  The rows of a new block include the block's first token, so the
-// thread that maps that row also writes the block's table entry, and no CTA
-// reads what another one writes.
+// slot map, four slots a thread.  The rows of a new block include the block's
+// first token, so the thread that maps that row also writes the block's table
+// entry, and no CTA reads what another one writes.
 constexpr int TAB_THREADS = 1024;
 constexpr int TAB_PER = KV8_MAX_REQUESTS / TAB_THREADS;  // requests of a thread
+constexpr int TAB_SLOTS = 4;                             // slots of a thread at a time
 
 struct Request {
   int len, cnt, held, fresh;  // tokens, rows, blocks before, new blocks
 };
+__device__ __forceinline__ int blocks_of(int tokens) {
+  return (int)((unsigned(tokens) + KV8_BLOCK - 1) / KV8_BLOCK);
+}
 __device__ __forceinline__ Request request(const Kv8TablesArgs& a, int r, bool report) {
   Request q{0, 0, 0, 0};
   if (r >= a.n) return q;
@@ -27,11 +33,10 @@ __device__ __forceinline__ Request request(const Kv8TablesArgs& a, int r, bool r
     if (report) atomicOr(a.err, DEVERR_COUNT);
     return q;
   }
-  const int blocks = (len + KV8_BLOCK - 1) / KV8_BLOCK;
   q.len = len;
   q.cnt = cnt;
-  q.held = a.positions ? blocks : (len - cnt + KV8_BLOCK - 1) / KV8_BLOCK;
-  q.fresh = blocks - q.held;
+  q.held = blocks_of(a.positions ? len : len - cnt);
+  q.fresh = blocks_of(len) - q.held;
   return q;
 }
 
@@ -39,18 +44,23 @@ __global__ void __launch_bounds__(TAB_THREADS)
 tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
   pdl_wait();
   pdl_trigger();
-  // first row and first free block of each request (and behind the last)
-  __shared__ int s_row[KV8_MAX_REQUESTS + 1], s_free[KV8_MAX_REQUESTS];
+  // a request's first row (and behind the last one's), first free block, tokens
+  extern __shared__ int s_tab[];
+  const int n = a.n;
+  int *s_row = s_tab, *s_free = s_row + n + 1, *s_len = s_free + n;
   __shared__ unsigned long long s_warp[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool first = blockIdx.x == 0;
   // rows in the high and blocks in the low half of one 64-bit sum
   unsigned long long mine[TAB_PER], sum = 0;
+  const int per = (n + TAB_THREADS - 1) / TAB_THREADS;
 #pragma unroll
   for (int i = 0; i < TAB_PER; ++i) {
-    const Request q = request(a, tid * TAB_PER + i, first);
+    const int r = tid * per + i;
+    const Request q = i < per ? request(a, r, first) : Request{0, 0, 0, 0};
     mine[i] = (unsigned long long)(unsigned)q.cnt << 32 | unsigned(q.fresh);
     sum += mine[i];
+    if (i < per && r < n) s_len[r] = q.len;
   }
   unsigned long long incl = sum;
 #pragma unroll
@@ -60,165 +70,229 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
   }
   if (lane == 31) s_warp[warp] = incl;
   __syncthreads();
-  unsigned long long at = incl - sum;
-  for (int i = 0; i < warp; ++i) at += s_warp[i];
+  unsigned long long before = lane < warp ? s_warp[lane] : 0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+  unsigned long long at = before + incl - sum;
 #pragma unroll
   for (int i = 0; i < TAB_PER; ++i) {
-    const int r = tid * TAB_PER + i;
-    s_row[r] = int(min(at >> 32, 0x7fffffffull));
-    s_free[r] = int(at & 0xffffffffull);
-    if (first && r < a.n) a.offsets[r] = s_row[r];
+    const int r = tid * per + i;
+    if (i < per && r < n) {
+      s_row[r] = int(min(at >> 32, 0x7fffffffull));
+      s_free[r] = int(at & 0xffffffffull);
+      if (first) a.offsets[r] = s_row[r];
+    }
     at += mine[i];
   }
   if (tid == TAB_THREADS - 1) {
     const int total = int(min(at >> 32, 0x7fffffffull)), taken = int(at & 0xffffffffull);
-    s_row[KV8_MAX_REQUESTS] = total;
+    s_row[n] = total;
     if (first) {
-      a.offsets[a.n] = total;
+      a.offsets[n] = total;
       *a.used = taken;
       if (total > a.n_slots || taken > a.n_free) atomicOr(a.err, DEVERR_COUNT);
     }
   }
   __syncthreads();
-  const int total = min(s_row[KV8_MAX_REQUESTS], a.n_slots);
-  const int i0 = blockIdx.x * rows_per_cta, i1 = min(i0 + rows_per_cta, a.n_slots);
-  for (int i = i0 + tid; i < i1; i += TAB_THREADS) {
-    int slot = -1;
-    if (i < total) {
-      int lo = 0, hi = a.n;  // the request with s_row[r] <= i < s_row[r + 1]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s_row[mid] <= i) lo = mid;
+  const int total = min(s_row[n], a.n_slots);
+  const long long i0 = (long long)blockIdx.x * rows_per_cta;
+  const int i1 = int(min(i0 + rows_per_cta, (long long)a.n_slots));
+  for (long long b = i0 + tid * TAB_SLOTS; b < i1; b += TAB_THREADS * TAB_SLOTS) {
+    const int base = int(b);
+    int slot[TAB_SLOTS], r = 0;
+    if (base < total) {
+      int hi = n;  // the last request with s_row[r] <= base
+      while (hi - r > 1) {
+        const int mid = (r + hi) >> 1;
+        if (s_row[mid] <= base) r = mid;
         else hi = mid;
       }
-      const Request q = request(a, lo, false);
-      const int p = a.positions ? a.positions[i] : q.len - q.cnt + (i - s_row[lo]);
-      if (p < 0 || p >= q.len) {
+    }
+    int blk = -1, page = -1, in = -1;  // of the row before
+#pragma unroll
+    for (int k = 0; k < TAB_SLOTS; ++k) {
+      const int i = base + k;
+      slot[k] = -1;
+      if (i >= total || i >= i1) continue;
+      while (s_row[r + 1] <= i) ++r;  // (requests without rows are passed over)
+      const int len = s_len[r], cnt = s_row[r + 1] - s_row[r];
+      const int p = a.positions ? a.positions[i] : len - cnt + (i - s_row[r]);
+      if (p < 0 || p >= len) {
         atomicOr(a.err, DEVERR_INDEX);
-      } else {
-        const int blk = p / KV8_BLOCK;
-        int* entry = a.table + (long long)lo * a.ld_table + blk;
-        int page;
-        if (blk < q.held) {
+        continue;
+      }
+      if (p / KV8_BLOCK != blk || r != in) {
+        blk = p / KV8_BLOCK;
+        in = r;
+        int* entry = a.table + (long long)r * a.ld_table + blk;
+        const int held = blocks_of(a.positions ? len : len - cnt);
+        if (blk < held) {
           page = *entry;
         } else {
-          const int f = s_free[lo] + blk - q.held;
+          const int f = s_free[r] + blk - held;
           page = f >= a.n_free ? -1 : a.free_blocks ? a.free_blocks[f] : f;
           if (p % KV8_BLOCK == 0) *entry = page;
         }
-        if (page < 0) atomicOr(a.err, DEVERR_INDEX);
-        else slot = page * KV8_BLOCK + p % KV8_BLOCK;
       }
+      if (page < 0) atomicOr(a.err, DEVERR_INDEX);
+      else slot[k] = page * KV8_BLOCK + p % KV8_BLOCK;
     }
-    a.slots[i] = slot;
+    if (base + TAB_SLOTS <= i1 && (reinterpret_cast<uintptr_t>(a.slots + base) & 15) == 0) {
+      *reinterpret_cast<int4*>(a.slots + base) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < TAB_SLOTS; ++k)
+        if (base + k < i1) a.slots[base + k] = slot[k];
+    }
   }
 }
 
 // ------------------------------------------------------------------ store
-// A run is the rows of one block, next to one another in the list.  A CTA
-// takes the runs that start among its `chunk` rows, four heads of the keys or
-// of the values; the threads stand as row lanes x (heads x pieces of eight
-// channels), so that a block's rows are read once, stay in registers while
-// their largest magnitude is found, and leave as codes.
-constexpr int ST_THREADS = 256, ST_HEADS = 4, ST_CHUNK = 16;
+// A run is the rows of one block, next to one another in the list.  A warp
+// takes, for one head of the keys or of the values, the runs that start among
+// its `chunk` rows: a row is PIECES lanes of eight channels, so the warp reads a
+// run once, keeps it in registers while the largest magnitude is found, and
+// writes it as codes; nothing is shared between warps.  (A run that does not
+// fit the registers is read again, from L2.)  With CTAs of four
+// heads that met at barriers, 4 x 831 rows took 23.9 us.
+constexpr int ST_WARPS = 4, ST_CHUNK = 16;
 
 template <class T, int DH, bool WIDE>
-__global__ void __launch_bounds__(ST_THREADS)
+__global__ void __launch_bounds__(32 * ST_WARPS)
 store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
              const T* __restrict__ vx, int ldx, const int* __restrict__ slots, int n_bound,
              const int* __restrict__ count, int append, int chunk, unsigned* __restrict__ err) {
-  constexpr int PIECES = DH / 8, COLS = ST_HEADS * PIECES;
-  constexpr int LANES = ST_THREADS / COLS;               // row lanes
-  constexpr int PER = (KV8_BLOCK + LANES - 1) / LANES;   // rows of a lane
-  __shared__ int s_slot[ST_CHUNK + KV8_BLOCK + 2];       // from the row before the chunk
-  __shared__ unsigned s_top[ST_HEADS];
-  __shared__ int s_own[KV8_BLOCK];                       // the row of each place of the block
+  constexpr int PIECES = DH / 8, AT_ONCE = 32 / PIECES;  // lanes of a row, rows of the warp
+  constexpr int KEEP = sizeof(T) == 2 ? 8 : 4;           // passes held in registers
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, c0 = blockIdx.x * chunk;
-  const int n = live_count(count, n_bound, tid == 0 ? err : nullptr);
+  const int lane = threadIdx.x & 31, unit = blockIdx.y * ST_WARPS + (threadIdx.x >> 5);
+  const int head = unit >> 1, side = unit & 1;
+  if (head >= pool.heads) return;
+  const bool speaks = unit == 0;  // reports what every unit sees
+  const int n = live_count(count, n_bound, speaks && lane == 0 ? err : nullptr);
+  const int c0 = blockIdx.x * chunk;
   if (c0 >= n) return;
-  const long long top_slot = (long long)pool.blocks * KV8_BLOCK;
-  for (int i = tid; i < chunk + KV8_BLOCK + 2; i += ST_THREADS) {
-    const int r = c0 - 1 + i;
+  // slots of the rows from the one before the chunk, 32 apart; -1 for none
+  const long long beyond = (long long)pool.blocks * KV8_BLOCK;
+  int slot[3];
+  unsigned begins[3];  // rows whose block is not the row before's
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const long long r = (long long)c0 - 1 + 32 * i + lane;
     int s = r >= 0 && r < n ? slots[r] : -1;
-    if (s >= top_slot) {
-      if (i > 0 && i <= chunk) atomicOr(err, DEVERR_INDEX);
+    if (s >= beyond) {
+      if (speaks && r >= c0 && r < c0 + chunk) atomicOr(err, DEVERR_INDEX);
       s = -1;
     }
-    s_slot[i] = s < 0 ? -1 : s;
+    slot[i] = s < 0 ? -1 : s;
   }
-  const int side = blockIdx.z;
-  const int lane = tid / COLS, col = tid - lane * COLS;
-  const int hl = col / PIECES, piece = col - hl * PIECES, head = blockIdx.y * ST_HEADS + hl;
-  const bool on = lane < LANES && head < pool.heads;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    int prev = __shfl_up_sync(0xffffffffu, slot[i], 1);
+    const int last = __shfl_sync(0xffffffffu, slot[i > 0 ? i - 1 : 0], 31);
+    if (lane == 0) prev = i > 0 ? last : -1;
+    begins[i] = __ballot_sync(0xffffffffu, slot[i] < 0 || prev < 0 ||
+                                               slot[i] / KV8_BLOCK != prev / KV8_BLOCK);
+  }
+  const int sub = lane / PIECES, piece = lane - sub * PIECES;
+  const bool on = sub < AT_ONCE;
+  const auto slot_of = [&](int i) {  // (i < 96, the same or not in each lane)
+    const int a = __shfl_sync(0xffffffffu, slot[0], i & 31);
+    const int b = __shfl_sync(0xffffffffu, slot[1], i & 31);
+    const int c = __shfl_sync(0xffffffffu, slot[2], i & 31);
+    return i < 32 ? a : i < 64 ? b : c;
+  };
   const T* src = (side ? vx : kx) + head * DH + piece * 8;
-  __syncthreads();
-  for (int start = 1; start <= chunk; ++start) {  // (uniform: every thread sees the same runs)
-    const int slot0 = s_slot[start];
+
+  for (int start = 1; start <= chunk && c0 + start - 1 < n; ++start) {
+    if (!(begins[0] >> start & 1)) continue;  // (chunk < 32)
+    const int slot0 = slot_of(start);
     if (slot0 < 0) continue;
     const int block = slot0 / KV8_BLOCK;
-    if (s_slot[start - 1] >= 0 && s_slot[start - 1] / KV8_BLOCK == block) continue;
-    int len = 1;
-    while (len <= KV8_BLOCK && s_slot[start + len] >= 0 &&
-           s_slot[start + len] / KV8_BLOCK == block)
-      ++len;
-    // (more rows than the block has tokens: some slot came twice)
+    // rows up to the next beginning (row 96 counts as one)
+    const int after = start + 1;
+    int end = 96;
+    if (begins[0] >> 1 >> start) end = after + __ffs(begins[0] >> 1 >> start) - 1;
+    else if (begins[1]) end = 31 + __ffs(begins[1]);
+    else if (begins[2]) end = 63 + __ffs(begins[2]);
+    int len = end - start;
+    // the places that the rows fill; more rows than places, or a place twice:
+    // the first row of a place counts
     if (len > KV8_BLOCK) {
       len = KV8_BLOCK;
-      if (tid == 0) atomicOr(err, DEVERR_INDEX);
+      if (speaks && lane == 0) atomicOr(err, DEVERR_INDEX);
     }
-    __syncthreads();  // the run before has been read
-    if (tid < KV8_BLOCK) s_own[tid] = KV8_BLOCK;
-    if (tid < ST_HEADS) s_top[tid] = 0;
-    __syncthreads();
-    // the first row of a place fills it
-    bool begins = false;
-    if (tid < len) {
-      const int off = s_slot[start + tid] % KV8_BLOCK;
-      begins = off == 0;
-      if (atomicMin(&s_own[off], tid) != KV8_BLOCK) atomicOr(err, DEVERR_INDEX);
-    }
-    const bool fresh = __syncthreads_or(begins) && append;
-    Eight<T> v[PER];
-    unsigned top = 0;
-    bool live[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int k = lane + i * LANES;
-      live[i] = on && k < len && s_own[s_slot[start + k] % KV8_BLOCK] == k;
-      if (live[i]) {
-        const T* p = src + (long long)(c0 + start - 1 + k) * ldx;
-        if (WIDE) v[i].load(p);
-        else v[i].load_some(p, 8);
-      } else {
-        v[i].zero();
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) top = max(top, v[i].top());
-    if (on) atomicMax(&s_top[hl], top);
+    const int off0 = slot_of(start + lane) % KV8_BLOCK;
+    const int off1 = slot_of(min(start + 32 + lane, 95)) % KV8_BLOCK;
+    const bool in0 = lane < len, in1 = lane + 32 < len;
+    unsigned fill[2];  // places filled
+    fill[0] = __reduce_or_sync(0xffffffffu, (in0 && off0 < 32 ? 1u << off0 : 0u) |
+                                                (in1 && off1 < 32 ? 1u << off1 : 0u));
+    fill[1] = __reduce_or_sync(0xffffffffu, (in0 && off0 >= 32 ? 1u << (off0 - 32) : 0u) |
+                                                (in1 && off1 >= 32 ? 1u << (off1 - 32) : 0u));
+    const bool twice = __popc(fill[0]) + __popc(fill[1]) != len;
+    if (twice && speaks && lane == 0) atomicOr(err, DEVERR_INDEX);
+    const bool fresh = append && (fill[0] & 1);
+    const auto is_first = [&](int k) {  // of its place (every lane takes part)
+      const int s = slot_of(start + k);
+      bool first = true;
+      for (int j = 0; j < len; ++j) first &= !(slot_of(start + j) == s && j < k);
+      return first;
+    };
     uint8_t* sc = pool.scale[side] + (long long)block * pool.heads + head;
-    const int old = on && !fresh ? *sc : 0;
-    __syncthreads();
-    if (!on) continue;
-    const int b = max(old, scale_byte(s_top[hl]));
+    const int old = fresh ? 0 : *sc;
+
+    Eight<T> v[KEEP];
+    unsigned top = 0;
+    const auto row_in = [&](int k) {  // (every lane takes part)
+      const bool ok = !twice || is_first(min(k, len - 1));
+      return on && k < len && ok;
+    };
+    const auto fetch = [&](Eight<T>& e, int k, bool in) {
+      if (in) {
+        const T* p = src + (long long)(c0 + start - 1 + k) * ldx;
+        if (WIDE) e.load(p);
+        else e.load_some(p, 8);
+      } else {
+        e.zero();
+      }
+    };
+    const int passes = (len + AT_ONCE - 1) / AT_ONCE;
+    const auto fetch_from = [&](int p0) {
+#pragma unroll
+      for (int p = 0; p < KEEP; ++p) {
+        const int k = (p0 + p) * AT_ONCE + sub;
+        if (p0 + p < passes) fetch(v[p], k, row_in(k));
+        else v[p].zero();
+      }
+    };
+    for (int p0 = 0; p0 < passes; p0 += KEEP) {
+      fetch_from(p0);
+#pragma unroll
+      for (int p = 0; p < KEEP; ++p) top = max(top, v[p].top());
+    }
+    const int b = max(old, scale_byte(__reduce_max_sync(0xffffffffu, top)));
+    const float inv = scale_inverse(b);
     uint8_t* base =
         pool.code[side] + ((long long)block * pool.heads + head) * (KV8_BLOCK * DH) + piece * 8;
-    const float inv = scale_inverse(b);
+    for (int p0 = 0; p0 < passes; p0 += KEEP) {
+      if (passes > KEEP) fetch_from(p0);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      if (!live[i]) continue;
-      const int off = s_slot[start + lane + i * LANES] % KV8_BLOCK;
-      *reinterpret_cast<uint2*>(base + off * DH) = v[i].codes(inv);
+      for (int p = 0; p < KEEP; ++p) {
+        if (p0 + p >= passes) break;
+        const int k = (p0 + p) * AT_ONCE + sub;
+        const int off = slot_of(start + min(k, len - 1)) % KV8_BLOCK;
+        if (row_in(k)) *reinterpret_cast<uint2*>(base + off * DH) = v[p].codes(inv);
+      }
     }
-    if (b > old && !fresh) {
+    if (b > old && !fresh && on) {
       // the other tokens' codes move to the raised scale (2^(old - b); below
       // 2^-126 every code becomes zero)
       const float f =
           b == 255 ? scale_value(255) : __uint_as_float(uint32_t(max(127 + old - b, 1)) << 23);
-      for (int off = lane; off < KV8_BLOCK; off += LANES) {
-        if (s_own[off] != KV8_BLOCK) continue;
+      for (int off = sub; off < KV8_BLOCK; off += AT_ONCE) {
+        if (fill[off >> 5] >> (off & 31) & 1) continue;
         uint2* p = reinterpret_cast<uint2*>(base + off * DH);
         uint2 q = *p;
         uint32_t* w = reinterpret_cast<uint32_t*>(&q);
@@ -230,35 +304,42 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
         *p = q;
       }
     }
-    if (lane == 0 && piece == 0 && (b != old || fresh)) *sc = uint8_t(b);
+    if (lane == 0 && (b != old || fresh)) *sc = uint8_t(b);
   }
 }
 
 template <class T, int DH>
 cudaError_t store(const Kv8Pool& pool, const T* k, const T* v, int ld, bool wide, const int* slots,
                   int n, const int* count, bool append, unsigned* err, cudaStream_t st) {
-  // rows of a CTA: a decode step's rows are a run each, and want a CTA each;
-  // past eight CTAs an SM a run's rows share one
-  const int parts = 2 * ((pool.heads + ST_HEADS - 1) / ST_HEADS);
-  const long long c = (long long)n * parts / (152 * 8);
+  // rows of a warp: a decode step's rows are a run each, and want a warp each;
+  // past 32 warps an SM a run's rows share one
+  const long long units = 2LL * pool.heads, c = (long long)n * units / (SMS * 32);
   const int chunk = c < 1 ? 1 : c > ST_CHUNK ? ST_CHUNK : int(c);
-  const dim3 grid(unsigned((n + chunk - 1) / chunk), unsigned(parts / 2), 2);
+  const dim3 grid(unsigned((n + (long long)chunk - 1) / chunk),
+                  unsigned((units + ST_WARPS - 1) / ST_WARPS));
   count_launches(1);
   if (wide)
-    return launch_k(store_kernel<T, DH, true>, grid, dim3(ST_THREADS), 0, st, pool, k, v, ld,
+    return launch_k(store_kernel<T, DH, true>, grid, dim3(32 * ST_WARPS), 0, st, pool, k, v, ld,
                     slots, n, count, append ? 1 : 0, chunk, err);
-  return launch_k(store_kernel<T, DH, false>, grid, dim3(ST_THREADS), 0, st, pool, k, v, ld, slots,
-                  n, count, append ? 1 : 0, chunk, err);
+  return launch_k(store_kernel<T, DH, false>, grid, dim3(32 * ST_WARPS), 0, st, pool, k, v, ld,
+                  slots, n, count, append ? 1 : 0, chunk, err);
 }
 
 }  // namespace
 
 cudaError_t launch_kv8_tables(const Kv8TablesArgs& a, cudaStream_t st) {
-  int per = 4 * TAB_THREADS;
+  // at most two CTAs an SM: each sums the requests itself
+  constexpr int LEAST = TAB_THREADS * TAB_SLOTS;
+  long long per = ((long long)a.n_slots + 2 * SMS - 1) / (2 * SMS);
+  per = per < LEAST ? LEAST : (per + TAB_SLOTS - 1) / TAB_SLOTS * TAB_SLOTS;
   const long long ctas = ((long long)a.n_slots + per - 1) / per;
+  const size_t smem = size_t(3 * a.n + 1) * sizeof(int);
+  if (smem > 48 * 1024)
+    RC_TRY(cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                int(smem)));
   count_launches(1);
-  return launch_k(tables_kernel, dim3(unsigned(ctas < 1 ? 1 : ctas)), dim3(TAB_THREADS), 0, st, a,
-                  per);
+  return launch_k(tables_kernel, dim3(unsigned(ctas < 1 ? 1 : ctas)), dim3(TAB_THREADS), smem, st,
+                  a, int(per));
 }
 
 cudaError_t launch_kv8_store(const Kv8Pool& pool, const void* k, const void* v, int ld, bool f32,
