@@ -31,6 +31,21 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// Two values times inv as codes (one packed product).
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi, uint64_t inv) {
+  uint64_t v;
+  asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tmul.rn.f32x2 %0, t, %3;\n\t}"
+      : "=l"(v)
+      : "f"(lo), "f"(hi), "l"(inv));
+  float a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+  return e4m3x2(a, b);
+}
+__device__ __forceinline__ uint64_t both(float v) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(v));
+  return r;
+}
 // Two codes as f16 (exact).
 __device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t codes) {
   uint32_t r;
@@ -69,12 +84,13 @@ struct Eight<__nv_bfloat16> {
     const uint32_t a = m << 16, b = m & 0xffff0000u;
     return a > b ? a : b;
   }
-  __device__ __forceinline__ uint32_t four(uint32_t a, uint32_t b, float inv) const {
-    return e4m3x2(__uint_as_float(a << 16) * inv, __uint_as_float(a & 0xffff0000u) * inv) |
-           e4m3x2(__uint_as_float(b << 16) * inv, __uint_as_float(b & 0xffff0000u) * inv) << 16;
+  static __device__ __forceinline__ uint32_t four(uint32_t a, uint32_t b, uint64_t inv) {
+    return __byte_perm(
+        e4m3x2(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), inv),
+        e4m3x2(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u), inv), 0x5410);
   }
   __device__ __forceinline__ uint2 codes(float inv) const {
-    return make_uint2(four(u.x, u.y, inv), four(u.z, u.w, inv));
+    return make_uint2(four(u.x, u.y, both(inv)), four(u.z, u.w, both(inv)));
   }
 };
 template <>
@@ -98,8 +114,9 @@ struct Eight<float> {
                max(max(mag(b.x), mag(b.y)), max(mag(b.z), mag(b.w))));
   }
   __device__ __forceinline__ uint2 codes(float inv) const {
-    return make_uint2(e4m3x2(a.x * inv, a.y * inv) | e4m3x2(a.z * inv, a.w * inv) << 16,
-                      e4m3x2(b.x * inv, b.y * inv) | e4m3x2(b.z * inv, b.w * inv) << 16);
+    const uint64_t i = both(inv);
+    return make_uint2(__byte_perm(e4m3x2(a.x, a.y, i), e4m3x2(a.z, a.w, i), 0x5410),
+                      __byte_perm(e4m3x2(b.x, b.y, i), e4m3x2(b.z, b.w, i), 0x5410));
   }
 };
 

@@ -155,7 +155,7 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
 // writes it as codes; nothing is shared between warps.  (A run that does not
 // fit the registers is read again, from L2.)  With CTAs of four
 // heads that met at barriers, 4 x 831 rows took 23.9 us.
-constexpr int ST_WARPS = 4, ST_CHUNK = 16;
+constexpr int ST_WARPS = 4, ST_CHUNK = 31;
 
 template <class T, int DH, bool WIDE>
 __global__ void __launch_bounds__(32 * ST_WARPS)
@@ -205,15 +205,18 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
   };
   const T* src = (side ? vx : kx) + head * DH + piece * 8;
 
-  for (int start = 1; start <= chunk && c0 + start - 1 < n; ++start) {
-    if (!(begins[0] >> start & 1)) continue;  // (chunk < 32)
-    const int slot0 = slot_of(start);
+  // the runs that begin in the chunk (below 32 rows; what begins behind the
+  // last row has no slot)
+  unsigned todo = begins[0] & ((2u << chunk) - 2u);
+  while (todo) {
+    const int start = __ffs(todo) - 1;
+    todo &= todo - 1;
+    const int slot0 = __shfl_sync(0xffffffffu, slot[0], start);
     if (slot0 < 0) continue;
     const int block = slot0 / KV8_BLOCK;
     // rows up to the next beginning (row 96 counts as one)
-    const int after = start + 1;
     int end = 96;
-    if (begins[0] >> 1 >> start) end = after + __ffs(begins[0] >> 1 >> start) - 1;
+    if (begins[0] >> 1 >> start) end = start + __ffs(begins[0] >> 1 >> start);
     else if (begins[1]) end = 31 + __ffs(begins[1]);
     else if (begins[2]) end = 63 + __ffs(begins[2]);
     int len = end - start;
@@ -234,10 +237,15 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
     const bool twice = __popc(fill[0]) + __popc(fill[1]) != len;
     if (twice && speaks && lane == 0) atomicOr(err, DEVERR_INDEX);
     const bool fresh = append && (fill[0] & 1);
-    const auto is_first = [&](int k) {  // of its place (every lane takes part)
-      const int s = slot_of(start + k);
+    const auto place = [&](int k) {  // of row k of the run (every lane takes part)
+      const int a = __shfl_sync(0xffffffffu, off0, k & 31);
+      const int b = __shfl_sync(0xffffffffu, off1, k & 31);
+      return k < 32 ? a : b;
+    };
+    const auto is_first = [&](int k) {  // of its place
+      const int s = place(k);
       bool first = true;
-      for (int j = 0; j < len; ++j) first &= !(slot_of(start + j) == s && j < k);
+      for (int j = 0; j < len; ++j) first &= !(place(j) == s && j < k);
       return first;
     };
     uint8_t* sc = pool.scale[side] + (long long)block * pool.heads + head;
@@ -245,26 +253,20 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
 
     Eight<T> v[KEEP];
     unsigned top = 0;
-    const auto row_in = [&](int k) {  // (every lane takes part)
-      const bool ok = !twice || is_first(min(k, len - 1));
-      return on && k < len && ok;
-    };
-    const auto fetch = [&](Eight<T>& e, int k, bool in) {
-      if (in) {
-        const T* p = src + (long long)(c0 + start - 1 + k) * ldx;
-        if (WIDE) e.load(p);
-        else e.load_some(p, 8);
-      } else {
-        e.zero();
-      }
-    };
     const int passes = (len + AT_ONCE - 1) / AT_ONCE;
+    const T* rows = src + (long long)(c0 + start - 1 + sub) * ldx;
     const auto fetch_from = [&](int p0) {
+      const T* p = rows + (long long)p0 * AT_ONCE * ldx;
 #pragma unroll
-      for (int p = 0; p < KEEP; ++p) {
-        const int k = (p0 + p) * AT_ONCE + sub;
-        if (p0 + p < passes) fetch(v[p], k, row_in(k));
-        else v[p].zero();
+      for (int i = 0; i < KEEP; ++i, p += (long long)AT_ONCE * ldx) {
+        const int k = (p0 + i) * AT_ONCE + sub;
+        if (on && k < len) {
+          if (WIDE) v[i].load(p);
+          else v[i].load_some(p, 8);
+        } else {
+          v[i].zero();
+        }
+        if (twice && !is_first(min(k, len - 1))) v[i].zero();
       }
     };
     for (int p0 = 0; p0 < passes; p0 += KEEP) {
@@ -282,8 +284,9 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
       for (int p = 0; p < KEEP; ++p) {
         if (p0 + p >= passes) break;
         const int k = (p0 + p) * AT_ONCE + sub;
-        const int off = slot_of(start + min(k, len - 1)) % KV8_BLOCK;
-        if (row_in(k)) *reinterpret_cast<uint2*>(base + off * DH) = v[p].codes(inv);
+        const int off = place(k & 63);
+        const bool counts = !twice || is_first(min(k, len - 1));
+        if (on && k < len && counts) *reinterpret_cast<uint2*>(base + off * DH) = v[p].codes(inv);
       }
     }
     if (b > old && !fresh && on) {
@@ -292,7 +295,7 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
       const float f =
           b == 255 ? scale_value(255) : __uint_as_float(uint32_t(max(127 + old - b, 1)) << 23);
       for (int off = sub; off < KV8_BLOCK; off += AT_ONCE) {
-        if (fill[off >> 5] >> (off & 31) & 1) continue;
+        if ((off < 32 ? fill[0] : fill[1]) >> (off & 31) & 1) continue;
         uint2* p = reinterpret_cast<uint2*>(base + off * DH);
         uint2 q = *p;
         uint32_t* w = reinterpret_cast<uint32_t*>(&q);
@@ -312,8 +315,8 @@ template <class T, int DH>
 cudaError_t store(const Kv8Pool& pool, const T* k, const T* v, int ld, bool wide, const int* slots,
                   int n, const int* count, bool append, unsigned* err, cudaStream_t st) {
   // rows of a warp: a decode step's rows are a run each, and want a warp each;
-  // past 32 warps an SM a run's rows share one
-  const long long units = 2LL * pool.heads, c = (long long)n * units / (SMS * 32);
+  // past 20 warps an SM a run's rows share one
+  const long long units = 2LL * pool.heads, c = (long long)n * units / (SMS * 20);
   const int chunk = c < 1 ? 1 : c > ST_CHUNK ? ST_CHUNK : int(c);
   const dim3 grid(unsigned((n + (long long)chunk - 1) / chunk),
                   unsigned((units + ST_WARPS - 1) / ST_WARPS));
