@@ -52,6 +52,13 @@ __device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t codes) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(uint16_t(codes)));
   return r;
 }
+// Four codes as f16: the lower and the upper two.
+__device__ __forceinline__ void e4m3x4_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
 __device__ __forceinline__ float2 e4m3x2_f32(uint32_t codes) {
   const uint32_t h = e4m3x2_f16x2(codes);
   return __half22float2(*reinterpret_cast<const __half2*>(&h));

@@ -79,13 +79,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Four codes as f16: the lower and the upper two.
-__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
-      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
-      : "=r"(lo), "=r"(hi)
-      : "r"(w));
-}
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
@@ -134,8 +127,8 @@ __device__ __forceinline__ void add_values(float (*acc)[NR][4], const uint32_t (
           // the channels 4 w + 2 p and the next of this lane's eight
           const uint32_t sel = p ? 0x7362 : 0x5140;
           uint32_t a0, a1, a2, a3;
-          codes_f16(__byte_perm(k0, k1, sel), a0, a1);
-          codes_f16(__byte_perm(k2, k3, sel), a2, a3);
+          e4m3x4_f16(__byte_perm(k0, k1, sel), a0, a1);
+          e4m3x4_f16(__byte_perm(k2, k3, sel), a2, a3);
 #pragma unroll
           for (int r = 0; r < NR; ++r)
             mma_f16(acc[4 * b + 2 * w + p][r], a0, a1, a2, a3, pf[u][r][0], pf[u][r][1]);
@@ -150,7 +143,7 @@ __device__ __forceinline__ void add_values(float (*acc)[NR][4], const uint32_t (
         if (left < HALF && 16 * u + t + 4 * k >= left) v[k] = 0;
       }
       uint32_t a0, a2;
-      codes_f16(v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24, a0, a2);
+      e4m3x4_f16(v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24, a0, a2);
 #pragma unroll
       for (int r = 0; r < NR; ++r)
         mma_f16(acc[4][r], a0, 0u, a2, 0u, pf[u][r][0], pf[u][r][1]);
@@ -340,8 +333,8 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
 #pragma unroll
         for (int k = 0; k < C::KS; ++k) {
           uint32_t a0, a1, a2, a3;
-          codes_f16(w[0][k], a0, a2);
-          codes_f16(w[1][k], a1, a3);
+          e4m3x4_f16(w[0][k], a0, a2);
+          e4m3x4_f16(w[1][k], a1, a3);
 #pragma unroll
           for (int r = 0; r < NR; ++r)
             mma_f16(s[u][r], a0, a1, a2, a3, qf[k][r][0], qf[k][r][1]);

@@ -23,8 +23,8 @@
 // scale the exponent of its weights (relative to a reference kept per stream),
 // so that both cost nothing per element; bf16 weights have f32's range.
 // The maximum is taken in a row's first cache block only: later ones use the
-// same reference unless their weights' sum passes 2^64 (or a value scale passes
-// 2^40 of its reference); then it is raised, O rescaled, the block done again.
+// same reference unless their weights' sum passes 2^20 (or a value scale passes
+// 2^5 of its reference); then it is raised, O rescaled, the block done again.
 #include <math.h>
 
 #include "common.cuh"
@@ -43,16 +43,20 @@ constexpr int BQ = 128, BKV = 128, THREADS = 512;
 // one of these)
 constexpr int CONV_WARP = 8, MMA_WARP = 11, LOAD_WARP = 15, CONV_THREADS = 96;
 // Registers: 512 threads are launched with 128 each; the softmax's two
-// warpgroups take 176, the other two keep 80 (asked for by each warpgroup in one
+// warpgroups take 160, the other two keep 96 (asked for by each warpgroup in one
 // place, ahead of its warps' roles).
-constexpr int SOFT_REGS = 176, OTHER_REGS = 80;
+constexpr int SOFT_REGS = 160, OTHER_REGS = 96;
 constexpr int PAGES = BKV / KV8_BLOCK;
 // what the rows share of a cache block: the key scale (NaN where a block has no
 // value) and the value scale's exponent (ABSENT: the block is missing)
 constexpr float ABSENT = -2e30f, NO_REF = -1e30f;
 // S (P over it) of each stream, then O, then Q where it fits
 constexpr int TMEM_COLS = 512, TM_O = 2 * BKV;
-constexpr float RAISE_SUM = 18446744073709551616.f, RAISE_VALUE = 40.f;  // 2^64, 2^40
+// The values' operand is 2^-120 of the values, so weights are taken 2^100 up,
+// which leaves them 2^27: to raised sums of 2^20 and value scales 2^5 above
+// their reference.
+constexpr float WEIGHT_UP = 100.f, VALUE_DOWN = 1048576.f;  // 2^100, 2^(120 - 100)
+constexpr float RAISE_SUM = 1048576.f, RAISE_VALUE = 5.f;
 
 
 template <int DH>
@@ -76,8 +80,11 @@ struct MCfg {
   // ones are read where they are needed)
   static constexpr int FACTS = DH == 128 ? 128 : 256;
   static constexpr size_t SMEM = size_t(RING) + FACTS * 8 + 1024 + 256;
-  static constexpr int PER_ROW = DH / 8;             // 8-code pieces of a row
-  static constexpr int PASS = CONV_THREADS / PER_ROW;  // rows converted at a time
+  // conversion: threads of a row, 8-code pieces of a thread, rows at a time (a
+  // multiple of 8, so that a piece keeps its place in the swizzle)
+  static constexpr int ROW_THREADS = DH == 72 ? 3 : 4;
+  static constexpr int PIECES = DH / 8 / ROW_THREADS, PASS = CONV_THREADS / ROW_THREADS;
+  static_assert(PASS % 8 == 0 && PIECES * ROW_THREADS * 8 == DH, "conversion");
   static constexpr uint32_t IDESC_S = (1u << 4) | (uint32_t(KV8_BLOCK >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
   static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) |
                                        (uint32_t(ODIM >> 3) << 17) | (uint32_t(BQ >> 4) << 24);
@@ -113,20 +120,15 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
                "r"(d)
                : "memory");
 }
-// Four codes as bf16: the pairs (0, 2) and (1, 3).  A code's bits below its
-// sign, seven places down a bf16, are its value times 2^-120 (subnormals
-// included); the product is exact.  (A NaN code becomes a number: blocks
-// without value have a NaN scale.)
-__device__ __forceinline__ uint32_t times_2_120(uint32_t x) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x7b807b80u));
-  return r;
-}
+// Four codes as bf16, times 2^-120: the pairs (0, 2) and (1, 3).  A code's bits
+// below its sign, seven places down a bf16, are its value so far down
+// (subnormals included).  (A NaN code becomes a number: blocks without value
+// have a NaN scale.)
 __device__ __forceinline__ uint32_t codes_02(uint32_t u) {
-  return times_2_120(((u << 8) & 0x80008000u) | ((u << 4) & 0x07f007f0u));
+  return ((u << 8) & 0x80008000u) | ((u << 4) & 0x07f007f0u);
 }
 __device__ __forceinline__ uint32_t codes_13(uint32_t u) {
-  return times_2_120((u & 0x80008000u) | ((u >> 4) & 0x07f007f0u));
+  return (u & 0x80008000u) | ((u >> 4) & 0x07f007f0u);
 }
 // Place of channel c among O's columns (the pairs above).
 __device__ __forceinline__ constexpr int o_column(int c) {
@@ -420,17 +422,17 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
             tmem_wait_st();
           }
         }
-        // ---- weights 2^(score - m + value scale's exponent over ref's);
-        // 2^-126 is the least that bf16 weights can carry, and the sum is
-        // taken from 2^-60 up, so that it keeps small weights
+        // ---- weights 2^(score - m + value scale's exponent over ref's + 100);
+        // the sum is taken from value scales of 2^-60 of the reference's up, so
+        // that it keeps small weights
         const float mm = m == -INFINITY ? 0.f : m;
-        const float d = now.y - ref, dv = fmaxf(d, -60.f), shift = dv - mm;
+        const float d = now.y - ref, dv = fmaxf(d, -60.f) + WEIGHT_UP, shift = dv - mm;
         uint64_t total[2] = {0, 0};
         tmem_ld64(s_at, w);
         if (whole)
           weights<true>(w, w, f, shift, KV8_BLOCK, 1.f, total);
         else
-          weights<false>(w, w, f, shift, limit, ex2_ftz(fmaxf(d, -126.f) - dv), total);
+          weights<false>(w, w, f, shift, limit, ex2_ftz(fmaxf(d, -126.f) + WEIGHT_UP - dv), total);
         const float2 t = split64(add2(total[0], total[1]));
         // (a block that the row sees nothing of adds nothing, whatever its scale)
         sum = limit > 0 ? (t.x + t.y) * ex2_ftz(-dv) : 0.f;
@@ -461,7 +463,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       tmem_ld8_nowait(to + 8 * c, o);
       tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[o_column(j)]) * back;
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[o_column(j)]) * VALUE_DOWN * back;
     };
     const auto put = [&](bf16* p, const float* v, float inv) {
       *reinterpret_cast<uint4*>(p) =
@@ -630,40 +632,48 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
       }
     } else if (warp >= CONV_WARP) {
       // ---------------------------------------------------------- conversion
-      // A thread takes one 8-code piece (8 channels) of every PASS-th row.
+      // A thread takes the same pieces (8 channels each) of every PASS-th row.
       const bool values = warp >= CONV_WARP + 4;
       const int tid = int(threadIdx.x) - (values ? CONV_WARP + 4 : CONV_WARP) * 32;
-      const int r0 = tid / C::PER_ROW, c = tid - r0 * C::PER_ROW;
-      const bool tail = C::TAIL && c == 8;
+      const int r0 = tid / C::ROW_THREADS, c0 = (tid - r0 * C::ROW_THREADS) * C::PIECES;
+      uint32_t to[C::PIECES];  // a piece's place in row r0 of a tile of keys or values
+#pragma unroll
+      for (int k = 0; k < C::PIECES; ++k) {
+        const int c = c0 + k;
+        to[k] = !values && C::TAIL && c == 8
+                    ? BKV * 128 + r0 * 32 + (((r0 >> 2) & 1) << 4)
+                    : (c >> 3) * (BKV * 128) + r0 * 128 + (((c ^ r0) & 7) << 4);
+      }
+      const bool tail = !values && C::TAIL && c0 + C::PIECES == 9;  // (its last piece)
       for (int b = 0; b < nb; ++b) {
         const int j = 2 * b + (values ? 1 : 0), st = j % C::RAWS, ks = b % C::KST, vs = b % C::VST;
-      if (ok)
-        ok = (values ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
+        if (ok)
+          ok = (values ? mbar_sleep(v_empty + 8 * vs, ((b / C::VST) & 1) ^ 1, abort_flag)
                        : mbar_sleep(k_empty + 8 * ks, ((b / C::KST) & 1) ^ 1, abort_flag)) &&
                mbar_sleep(raw_full + 8 * st, (j / C::RAWS) & 1, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      const uint32_t from = raw + st * C::RAW_BYTES + (r0 * C::PER_ROW + c) * 8;
-        constexpr int PASSES = (BKV + C::PASS - 1) / C::PASS, BATCH = 5;
+        const uint32_t from = raw + st * C::RAW_BYTES + r0 * DH + c0 * 8;
+        const uint32_t tile = values ? sv + vs * C::V_BYTES : sk + ks * C::K_BYTES;
+        constexpr int PASSES = (BKV + C::PASS - 1) / C::PASS;
 #pragma unroll
-        for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
-          uint2 q[BATCH];
+        for (int p = 0; p < PASSES; ++p) {
+          if (r0 + p * C::PASS >= BKV) break;
+          uint2 q[C::PIECES];
 #pragma unroll
-          for (int p = p0; p < p0 + BATCH && p < PASSES; ++p)
-            if (r0 < C::PASS && r0 + p * C::PASS < BKV) q[p - p0] = lds64(from + p * C::PASS * DH);
+          for (int k = 0; k < C::PIECES; ++k) q[k] = lds64(from + p * C::PASS * DH + 8 * k);
+          if (values) {
 #pragma unroll
-          for (int p = p0; p < p0 + BATCH && p < PASSES; ++p) {
-            const int r = r0 + p * C::PASS;
-            if (r0 >= C::PASS || r >= BKV) continue;
-            const uint2 u = q[p - p0];
-            if (values) {
-              sts128(sv + vs * C::V_BYTES + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
-                     codes_02(u.x), codes_13(u.x), codes_02(u.y), codes_13(u.y));
-            } else {
-              const uint32_t tile = sk + ks * C::K_BYTES;
-              sts128(tail ? tile + BKV * 128 + r * 32 + (((r >> 2) & 1) << 4)
-                          : tile + (c >> 3) * (BKV * 128) + r * 128 + (((c ^ r) & 7) << 4),
-                     e4m3x2_f16x2(u.x & 0xffffu), e4m3x2_f16x2(u.x >> 16),
-                     e4m3x2_f16x2(u.y & 0xffffu), e4m3x2_f16x2(u.y >> 16));
+            for (int k = 0; k < C::PIECES; ++k)
+              sts128(tile + to[k] + p * C::PASS * 128, codes_02(q[k].x), codes_13(q[k].x),
+                     codes_02(q[k].y), codes_13(q[k].y));
+          } else {
+#pragma unroll
+            for (int k = 0; k < C::PIECES; ++k) {
+              uint32_t h[4];
+              e4m3x4_f16(q[k].x, h[0], h[1]);
+              e4m3x4_f16(q[k].y, h[2], h[3]);
+              sts128(tile + to[k] + p * C::PASS * (k == C::PIECES - 1 && tail ? 32 : 128), h[0],
+                     h[1], h[2], h[3]);
             }
           }
         }
