@@ -12,8 +12,9 @@
 // sixteen blocks (2048 columns) are stored and handed over together.  The
 // hand-over is what must be rare: with one for every block, and bytes loaded
 // where they were needed, 16384 x 1152 x 4608 took 301 us; with one for every
-// four, and loads a batch ahead, 82.  Two accumulators of up to 192 columns
-// and a ring of scale words fill the 512 columns of tensor memory.
+// four, and loads a batch ahead, 82.  Two accumulators of up to 192 columns (or
+// one of up to 256, where a CTA has one tile) and two batches of scale words fill
+// the 512 columns of tensor memory.
 #include "common.cuh"
 #include "fp8.cuh"
 #include "kernels.h"
@@ -30,15 +31,15 @@ constexpr int BM = 128, BK = 128;
 constexpr int THREADS = 512;
 constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 8;
 constexpr int STAGE_A = BM * BK;
-constexpr int RING_BYTES = 188 * 1024, MAX_STAGES = 7;
+constexpr int RING_BYTES = 187 * 1024, MAX_STAGES = 7;
 constexpr int STAGING_WARP = 32 * 128;  // 32 rows of 32 columns per epilogue warp
-// tensor memory: accumulators at 0 and MAX_BN, then a ring of scale words: a
-// batch holds, for each WORD_KB blocks, 4 columns for x and 6 for W
-constexpr int MAX_BN = 192, SCALE_COL = 2 * MAX_BN, TMEM_COLS = 512;
+// tensor memory: accumulators at 0 and PAIR_BN, then a ring of scale words: a
+// batch holds, for each WORD_KB blocks, 4 columns for x and 8 for W
+constexpr int PAIR_BN = 192, MAX_BN = 256, SCALE_COL = 2 * PAIR_BN, TMEM_COLS = 512;
 constexpr int WORD_KB = 4, SCALE_BATCH = 16, SCALE_GROUPS = SCALE_BATCH / WORD_KB;
-constexpr int SCALE_STEP = 10, SCALE_SLOT = SCALE_GROUPS * SCALE_STEP, SCALES = 3;
+constexpr int SCALE_STEP = 12, SCALE_SLOT = SCALE_GROUPS * SCALE_STEP, SCALES = 2;
 static_assert(SCALE_COL + SCALES * SCALE_SLOT <= TMEM_COLS, "tensor memory");
-// the batch's words in shared memory: up to 128 rows of x, up to 192 of W
+// the batch's words in shared memory: up to 128 rows of x, up to 256 of W
 constexpr int SCALE_ROWS = 128 + MAX_BN, SCALE_BYTES = SCALE_GROUPS * SCALE_ROWS * 4;
 constexpr size_t SMEM_BYTES =
     size_t(RING_BYTES) + EPI_WARPS * STAGING_WARP + SCALE_BYTES + 1024 + 256;
@@ -228,7 +229,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       bool ready = false;  // the current stage was seen full already
       for (int t = pos; ok && t < pl.tiles; t += G) {
         if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
-        const uint32_t d = tmem + uint32_t(acc * MAX_BN);
+        const uint32_t d = tmem + uint32_t(acc * PAIR_BN);
         uint32_t accumulate = 0;
         // (what a block's issue needs beyond its stage is constant or one
         // addition a group away: the issuing thread is what bounds small tiles)
@@ -346,15 +347,14 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
           for (int i = 0; i < 4; ++i)
             v[g * SCALE_STEP + i] = words[g * SCALE_ROWS + (m_rows ? 32 * i + lane : 0)];
 #pragma unroll
-          for (int i = 0; i < 6; ++i)
+          for (int i = 0; i < 8; ++i)
             v[g * SCALE_STEP + 4 + i] =
                 words[g * SCALE_ROWS + 128 +
                       (w_rows ? 32 * i + lane : (w0 + 32 * i + lane) / 128 - w0 / 128)];
         }
         const uint32_t ta = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT) + part;
         tmem_st16(ta, v);
-        tmem_st16(ta + 16, v + 16);
-        tmem_st8(ta + 32, v + 32);
+        tmem_st32(ta + 16, v + 16);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -385,7 +385,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
       }
       if (!mbar_sleep_warp(tfull0 + 8 * acc, acc_phase, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      const uint32_t tb = tmem + uint32_t(acc * MAX_BN) + (uint32_t(sp * 32) << 16);
+      const uint32_t tb = tmem + uint32_t(acc * PAIR_BN) + (uint32_t(sp * 32) << 16);
 #pragma unroll
       for (int i = 0; i < MAX_BN / 64; ++i) {
         const int ch = half + 2 * i, r0 = m * BM + sp * 32, c0 = nn * BN + ch * 32;
@@ -561,8 +561,10 @@ Choice choose(long long rows, long long n, int kb) {
     }
   };
   for (int bn = MAX_BN; bn >= 64; bn -= 32) {
+    // (the wider tiles have one accumulator: no second tile)
+    if (bn > PAIR_BN && ((rows + BM - 1) / BM) * ((n + bn - 1) / bn) > SMS) continue;
     look(ALONE, bn, 1);
-    if (rows > BM && bn >= 128) look(PAIRS, bn, 1);
+    if (rows > BM && bn >= 128 && bn <= PAIR_BN) look(PAIRS, bn, 1);
   }
   for (int parts = 2; parts <= 4 && parts <= kb; ++parts) look(SPLIT, 64, parts);
   return best;

@@ -114,7 +114,8 @@ def _linear_reference(xm, wm, b, dtype):
 @pytest.mark.parametrize("rows,n,k", [
     (1, 1, 1), (1, 128, 128), (1, 1152, 4608), (5, 33, 70), (31, 384, 129), (64, 200, 1000),
     (128, 256, 256), (129, 193, 1152), (39, 3456, 1152), (257, 1152, 384), (300, 97, 16),
-    (831, 640, 1152), (1500, 1152, 130), (2049, 320, 260)])
+    (831, 640, 1152), (1500, 1152, 130), (2049, 320, 260), (831, 3500, 260), (700, 4608, 2100),
+    (16384, 1160, 300), (9000, 2304, 1152)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("bias", [True, False])
 def test_linear(lib, rows, n, k, dtype, bias):
