@@ -516,7 +516,8 @@ rc_status rc_attention(rc_ctx* ctx, const void* Q, int ldq, const void* K, const
  *           cols .. ld - 1 are neither read nor written.
  *   scales  u8 [ceil(cols / 128)][lds], lds >= ceil(rows / group): the scale
  *           of (r, c) is scales[c / 128][r / group].
- * cols is at most RC_FP8_MAX_COLS. */
+ * rows is at most RC_FP8_MAX_ROWS, cols RC_FP8_MAX_COLS. */
+#define RC_FP8_MAX_ROWS 1073741824
 #define RC_FP8_MAX_COLS 4194304
 typedef struct rc_fp8 {
   void* codes;
@@ -629,7 +630,7 @@ rc_status rc_kv8_store(rc_ctx* ctx, const rc_kv8* pool, const void* k, const voi
  * Device checks: a request with bad offsets, more than max_q rows or a bad
  * length is left out; a table entry outside the pool hides its tokens.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE (heads not a multiple of kv_heads,
- * heads / kv_heads > 16). */
+ * heads / kv_heads > 16 or q_rows * heads / kv_heads >= 2^31). */
 rc_status rc_kv8_attention(rc_ctx* ctx, const rc_kv8* pool, const void* Q, int ldq, int q_rows,
                            const int32_t* row_offsets, const int32_t* lengths, int n_requests,
                            int max_q, const int32_t* table, int ld_table, int heads, int causal,

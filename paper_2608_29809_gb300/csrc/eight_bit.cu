@@ -4,7 +4,7 @@
 #include <stdio.h>
 
 #include "../../include/regioncache.h"
-#include "kernels.h"
+#include "eight_bit.h"
 
 static_assert(RC_KV8_BLOCK == rc::KV8_BLOCK && RC_KV8_MAX_REQUESTS == rc::KV8_MAX_REQUESTS,
               "the header's limits are the kernels'");
@@ -44,9 +44,9 @@ rc_status check_device(const rc_ctx* c, const char* fn) {
 
 // A quantised matrix as a kernel argument.
 rc_status check_matrix(const rc_fp8* m, const char* fn, const char* name, rc::Fp8Mat* out) {
-  if (m->rows < 0 || m->cols < 1 || m->cols > RC_FP8_MAX_COLS)
-    return fail(RC_ERR_SHAPE, "%s: %s is %d x %d (at most %d columns)", fn, name, m->rows, m->cols,
-                RC_FP8_MAX_COLS);
+  if (m->rows < 0 || m->rows > RC_FP8_MAX_ROWS || m->cols < 1 || m->cols > RC_FP8_MAX_COLS)
+    return fail(RC_ERR_SHAPE, "%s: %s is %d x %d (at most %d x %d)", fn, name, m->rows, m->cols,
+                RC_FP8_MAX_ROWS, RC_FP8_MAX_COLS);
   if (m->group != 1 && m->group != 128)
     return fail(RC_ERR_INVALID_ARG, "%s: %s.group %d is not 1 or 128", fn, name, m->group);
   const long long scales = (m->rows + (long long)m->group - 1) / m->group;
@@ -201,7 +201,8 @@ rc_status rc_kv8_attention(rc_ctx* c, const rc_kv8* pool, const void* Q, int ldq
   RC_CHECK(check_device(c, fn));
   const rc::Kv8AttnArgs a{static_cast<const rc::bf16*>(Q), static_cast<rc::bf16*>(O), ldq, ldo,
                           q_rows, n, max_q < q_rows ? max_q : q_rows, ld_table, heads,
-                          causal ? 1 : 0, row_offsets, lengths, table, rc::ctx_error_word(c)};
+                          causal ? 1 : 0, row_offsets, lengths, table, rc::ctx_error_word(c), 1,
+                          0x7fffffff};
   return launched(rc::launch_kv8_attention(p, a, static_cast<cudaStream_t>(stream)), fn);
 }
 

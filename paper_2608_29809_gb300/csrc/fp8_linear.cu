@@ -16,9 +16,9 @@
 // one of up to 256, where a CTA has one tile) and two batches of scale words fill
 // the 512 columns of tensor memory.
 #include "common.cuh"
+#include "eight_bit.h"
 #include "fp8.cuh"
-#include "kernels.h"
-#include "tc_common.cuh"
+#include "tc_eight_bit.cuh"
 #include "tma_host.h"
 
 namespace rc {

@@ -1,7 +1,7 @@
 // Quantised matrices (rc_fp8): the quantiser.
 #include "common.cuh"
+#include "eight_bit.h"
 #include "fp8.cuh"
-#include "kernels.h"
 
 namespace rc {
 

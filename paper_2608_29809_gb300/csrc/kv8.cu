@@ -1,7 +1,7 @@
 // Paged eight-bit cache (rc_kv8): block tables and slot maps, and the store.
 #include "common.cuh"
+#include "eight_bit.h"
 #include "fp8.cuh"
-#include "kernels.h"
 
 namespace rc {
 
@@ -155,7 +155,7 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
 // writes it as codes; nothing is shared between warps.  (A run that does not
 // fit the registers is read again, from L2.)  With CTAs of four
 // heads that met at barriers, 4 x 831 rows took 23.9 us.
-constexpr int ST_WARPS = 4, ST_CHUNK = 31;
+constexpr int ST_WARPS = 4, ST_CHUNK = 24;
 
 template <class T, int DH, bool WIDE>
 __global__ void __launch_bounds__(32 * ST_WARPS)

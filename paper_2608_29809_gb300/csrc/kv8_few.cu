@@ -21,9 +21,9 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "eight_bit.h"
 #include "fp8.cuh"
-#include "kernels.h"
-#include "tc_common.cuh"
+#include "tc_eight_bit.cuh"
 
 namespace rc {
 
@@ -54,13 +54,6 @@ struct FCfg {
   static constexpr size_t SMEM = size_t(RING) + JOIN + WARPS * STAGES * 8 + 16;
 };
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
-                                          uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
-          "r"(dst), "l"(src), "r"(bytes), "r"(bar)
-      : "memory");
-}
 __device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -78,11 +71,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   uint32_t v;
@@ -182,7 +170,7 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     return;
   }
   const int rows = nq * group, row0 = chunk * C::ROWS;  // (below 2^31: the entry point's check)
-  if (row0 >= rows) return;
+  if (row0 >= rows || rows > a.most_rows) return;
   if (parts > 1) cluster_arrive();  // (waited for before anything is put into a peer)
 
   // ---- this warp's half blocks: first + WARPS i for i < mine
@@ -538,7 +526,9 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   RC_TRY(cudaFuncSetAttribute(few_rows_kernel<DH, NR>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM)));
   const int group = a.heads / pool.heads;
-  const long long chunks = ((long long)a.max_q * group + C::ROWS - 1) / C::ROWS;
+  const long long most_rows = (long long)a.max_q * group;
+  const long long chunks =
+      ((most_rows < a.most_rows ? most_rows : a.most_rows) + C::ROWS - 1) / C::ROWS;
   const long long units = chunks * pool.heads * a.n;
   // CTAs for two an SM at once; more of them where requests may differ much,
   // as long as a warp keeps 24 half blocks, beside which a CTA's 6 us of start
@@ -553,7 +543,6 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   if (parts > halves / WARPS) parts = halves / WARPS;
   if (parts > MAX_PARTS) parts = MAX_PARTS;
   if (parts < 1) parts = 1;
-  if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
   const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
   count_launches(1);
   return launch_k_cluster(few_rows_kernel<DH, NR>, grid, dim3(WARPS * 32), C::SMEM, int(parts), st,

@@ -28,9 +28,9 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "eight_bit.h"
 #include "fp8.cuh"
-#include "kernels.h"
-#include "tc_common.cuh"
+#include "tc_eight_bit.cuh"
 
 namespace rc {
 
@@ -79,7 +79,7 @@ struct MCfg {
   // facts of a CTA's first cache blocks, kept in shared memory (those of later
   // ones are read where they are needed)
   static constexpr int FACTS = DH == 128 ? 128 : 256;
-  static constexpr size_t SMEM = size_t(RING) + FACTS * 8 + 1024 + 256;
+  static constexpr size_t SMEM = size_t(RING) + FACTS * 8 + 1024 + 256 + 128;
   // conversion: threads of a row, 8-code pieces of a thread, rows at a time (a
   // multiple of 8, so that a piece keeps its place in the swizzle)
   static constexpr int ROW_THREADS = DH == 72 ? 3 : 4;
@@ -137,18 +137,6 @@ __device__ __forceinline__ constexpr int o_column(int c) {
 
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
-                                          uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
-          "r"(dst), "l"(src), "r"(bytes), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
-}
 
 // A row's 64 scores of a cache block, r, to weights 2^(s f + shift), two a word
 // as bf16 in w (times `less`, where FAST is false: then columns from `limit` on
@@ -189,7 +177,7 @@ __device__ __forceinline__ void store_two(uint32_t at, float a, float b) {
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1)
 many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
-                 int parts, int unit_rows) {
+                 int parts, int unit_rows, int compact) {
   using C = MCfg<DH>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -207,23 +195,78 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
   uint32_t* tmem_slot =
       reinterpret_cast<uint32_t*>(bars + 2 * C::KST + 2 * C::VST + 5 + 4 * PAGES + 2 * C::RAWS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int *sums = reinterpret_cast<int*>(tmem_slot + 2), *found = sums + THREADS / 32;
   const int warp = warp_index(), lane = threadIdx.x & 31;
 
   pdl_wait();
   pdl_trigger();
   const int part = parts > 1 ? int(cluster_ctarank()) : 0;
-  const int group = a.heads / pool.heads;
-  // (a request's last chunk, which may be short, among the last to start)
-  const int head = blockIdx.z % pool.heads, chunk = blockIdx.z / pool.heads, req = blockIdx.y;
-  const int q0 = a.offsets[req], nq = a.offsets[req + 1] - q0, len = a.lengths[req];
-  // (the same for every CTA of a cluster)
-  if (q0 < 0 || nq < 0 || nq > a.max_q || q0 > a.q_rows - nq || len < 0 ||
-      len > (long long)a.ld_table * KV8_BLOCK) {
-    if (threadIdx.x == 0) atomicOr(a.err, DEVERR_COUNT);
-    return;
+  const int group = a.heads / pool.heads, place = int(blockIdx.x) / parts;
+  const auto rows_of = [&](int r, bool report) {
+    const int first = a.offsets[r], count = a.offsets[r + 1] - first, tokens = a.lengths[r];
+    if (first < 0 || count < 0 || count > a.max_q || first > a.q_rows - count || tokens < 0 ||
+        tokens > (long long)a.ld_table * KV8_BLOCK) {
+      if (report) atomicOr(a.err, DEVERR_COUNT);
+      return 0;
+    }
+    return count * group >= a.least_rows ? count * group : 0;
+  };
+  int head, req, chunk;  // (the same for every CTA of a cluster)
+  if (!compact) {
+    // a place for each chunk that a request may have, key head and request
+    req = place % a.n;
+    head = place / a.n % pool.heads;
+    chunk = place / a.n / pool.heads;
+    if (chunk * unit_rows >= rows_of(req, threadIdx.x == 0)) return;
+  } else {
+    // Places for as many units as the rows can make: whole ones first, then the
+    // requests' short last ones, the key heads of each together.  This one's
+    // request is found by counting (as many requests at a time as the CTA has
+    // threads).  A bad request has none, and is reported.
+    head = place % pool.heads;
+    const int unit = place / pool.heads;
+    int whole = 0;  // units, of all requests
+    for (int r = int(threadIdx.x); r < a.n; r += THREADS)
+      whole += rows_of(r, blockIdx.x == 0) / unit_rows;
+    whole = __reduce_add_sync(0xffffffffu, whole);
+    if (lane == 0) sums[warp] = whole;
+    if (threadIdx.x == 0) found[0] = -1;
+    __syncthreads();
+    whole = 0;
+    for (int i = 0; i < THREADS / 32; ++i) whole += sums[i];
+    const bool last = unit >= whole;
+    const int wanted = last ? unit - whole : unit;
+    int before = 0;  // such units of the requests counted so far
+    for (int r0 = 0; r0 < a.n; r0 += THREADS) {
+      const int r = r0 + int(threadIdx.x), rows = r < a.n ? rows_of(r, false) : 0;
+      const int units = last ? (rows % unit_rows ? 1 : 0) : rows / unit_rows;
+      int incl = units;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      __syncthreads();  // (what `sums` had before has been read)
+      if (lane == 31) sums[warp] = incl;
+      __syncthreads();
+      int at = before + incl - units;
+      for (int i = 0; i < THREADS / 32; ++i) {
+        if (i < warp) at += sums[i];
+        before += sums[i];
+      }
+      if (wanted >= at && wanted < at + units) {
+        found[0] = r;
+        found[1] = last ? rows / unit_rows : wanted - at;
+      }
+      if (wanted < before) break;
+    }
+    __syncthreads();
+    req = __shfl_sync(0xffffffffu, found[0], 0);
+    chunk = __shfl_sync(0xffffffffu, found[1], 0);
+    if (req < 0) return;
   }
+  const int q0 = a.offsets[req], nq = a.offsets[req + 1] - q0, len = a.lengths[req];
   const int all = nq * group, row0 = chunk * unit_rows;  // (below 2^31: the entry point's check)
-  if (row0 >= all) return;
   const int rows = min(all - row0, unit_rows);
   const bool two = rows > BQ;
 
@@ -746,13 +789,20 @@ cudaError_t many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   const int group = a.heads / pool.heads;
   const Shape sh = choose(a, pool.heads, group);
   const int unit_rows = sh.unit_rows, parts = sh.parts;
-  const long long rows = (long long)a.max_q * group;
-  const long long chunks = (rows + unit_rows - 1) / unit_rows;
-  if (chunks * pool.heads > 65535) return cudaErrorInvalidConfiguration;
-  const dim3 grid(unsigned(parts), unsigned(a.n), unsigned(chunks * pool.heads));
+  // Units at most: whole ones and a last one for each request.  Where places for
+  // every chunk of every request would be more than twice that, the kernel counts
+  // out the units that there are (a place without one costs a CTA's launch, the
+  // counting every CTA 1.2 us)
+  const long long most = (long long)a.n * a.max_q, rows = most < a.q_rows ? most : a.q_rows;
+  const long long all = ((long long)a.max_q * group + unit_rows - 1) / unit_rows * a.n;
+  const long long units = rows * group / unit_rows + a.n;
+  const int compact = all > 2 * units ? 1 : 0;
+  const long long ctas = (compact ? units : all) * pool.heads * parts;
+  if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const dim3 grid{unsigned(ctas), 1u, 1u};
   count_launches(1);
   return launch_k_cluster(many_rows_kernel<DH>, grid, dim3(THREADS), C::SMEM, parts, st, pool, a,
-                          parts, unit_rows);
+                          parts, unit_rows, compact);
 }
 
 }  // namespace

@@ -14,6 +14,7 @@
 
 #include "../../include/regioncache.h"
 #include "common.cuh"
+#include "eight_bit.h"
 #include "kernels.h"
 
 using rc::bf16;

@@ -75,7 +75,8 @@ def _mat(R, **kw):
     return C.byref(R.rc_fp8(*[a[f] for f, _ in R.rc_fp8._fields_]))
 
 
-BAD_MATRIX = [(dict(rows=-1), 2), (dict(cols=0), 2), (dict(cols=4194305, ld=4194320), 2),
+BAD_MATRIX = [(dict(rows=-1), 2), (dict(rows=2 ** 30 + 1, lds=2 ** 31 - 1), 2), (dict(cols=0), 2),
+              (dict(cols=4194305, ld=4194320), 2),
               (dict(group=64), 1), (dict(ld=248), 2), (dict(ld=260), 2), (dict(lds=7), 2),
               (dict(codes=None), 1), (dict(scales=None), 1), (dict(codes=A + 8), 1)]
 
@@ -129,7 +130,7 @@ def test_tables_refusals(R):
         assert call(**{name: A + 2}) == 1
     assert call(positions=A + 1) == 1 and call(free=A + 2) == 1 and call(counts=A + 3) == 1
     for kw in (dict(n=0), dict(n=4097), dict(n_free=-1), dict(n_free=2 ** 26), dict(ld=0),
-               dict(ld=2 ** 26), dict(n_slots=-1)):
+               dict(ld=2 ** 26), dict(n_slots=-1), dict(n_slots=2 ** 30 + 1)):
         assert call(**kw) == 2, kw
 
 
@@ -175,7 +176,8 @@ def test_attention_refusals(R):
     assert R._lib.rc_kv8_attention(CTX, None, A, 288, 5, A, A, 2, 3, A, 4, 4, 0, A, 288, None) == 1
     for kw in (dict(heads=3), dict(heads=0), dict(heads=34, ldq=9999 // 8 * 8, ldo=9992),
                dict(ldq=280), dict(ldo=280), dict(ldq=290), dict(ldo=292), dict(rows=-1),
-               dict(max_q=-1), dict(n=-1), dict(n=4097), dict(ldt=0), dict(ldt=2 ** 26)):
+               dict(max_q=-1), dict(n=-1), dict(n=4097), dict(ldt=0), dict(ldt=2 ** 26),
+               dict(rows=2 ** 30 + 1)):
         assert call(**kw) == 2, kw
     for name in ("q", "off", "lens", "table", "o"):
         assert call(**{name: None}) == 1

@@ -313,7 +313,8 @@ class Case:
         assert bool((out[rows:] == 7).all()) and bool((out[:, wide:] == 7).all())
         return out[:rows, :wide].double().cpu()
 
-    def check(self, got, causal):
+    def check(self, got, causal, only=None):
+        """only: (request, query head) pairs to look at (all of them where None)."""
         k = E.cache_values(self.pool.k, self.pool.k_scale)
         v = E.cache_values(self.pool.v, self.pool.v_scale)
         dh, q = self.dh, self.q.double().cpu()
@@ -321,6 +322,8 @@ class Case:
             pages = self.table[r, :_blocks(l)].long()
             rows = slice(self.offsets[r], self.offsets[r + 1])
             for h in range(self.heads):
+                if only is not None and (r, h) not in only:
+                    continue
                 g = h // (self.heads // self.kvh)
                 o, pv, reach = E.attention(
                     q[rows, h * dh:(h + 1) * dh], k[pages, g].reshape(-1, dh)[:l],
@@ -356,6 +359,31 @@ def test_attention_many_rows(lib, lens, counts, heads, kvh, dh, causal):
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("lens,counts", [
+    ([500] * 30, [1] * 10 + [300] + [2] * 10 + [17] + [16] * 7 + [0]),
+    ([64, 3000] + [200] * 600, [1, 700] + [1] * 600), ([900, 300, 100], [40, 0, 200])])
+@pytest.mark.parametrize("heads,kvh,dh", [(2, 2, 72), (4, 1, 64)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_few_and_many_rows_together(lib, lens, counts, heads, kvh, dh, causal):
+    R, ctx = lib
+    c = Case(R, lens, counts, heads, kvh, dh, 28)
+    got = c.run(R, ctx, causal)
+    c.check(got, causal, None if len(lens) < 40 else
+            {(r, h) for r in (0, 1, 2, 300, 511, 512, 601) for h in (0, heads - 1)})
+    R.rc_sync(ctx)
+
+
+@pytest.mark.parametrize("lens,counts,heads,kvh,dh", [
+    ([9000] * 4, [260, 300, 270, 290], 16, 16, 128), ([20000, 17000], [70, 500], 2, 2, 64),
+    ([40000], [3], 2, 2, 72)])
+def test_attention_over_long_caches(lib, lens, counts, heads, kvh, dh):
+    R, ctx = lib
+    c = Case(R, lens, counts, heads, kvh, dh, 29)
+    got = c.run(R, ctx, True)
+    c.check(got, True, {(0, 0), (len(lens) - 1, heads - 1)})
+    R.rc_sync(ctx)
+
+
 @pytest.mark.parametrize("counts", [[1, 2], [150, 90]])
 @pytest.mark.parametrize("scale", [8.0, 60.0])
 def test_attention_scores_far_apart(lib, counts, scale):
@@ -381,6 +409,38 @@ def test_attention_extreme_queries_and_scales(lib, counts):
         c.pool.k_scale.fill_(b)
         c.pool.v_scale.fill_(245 - b)
         c.check(c.run(R, ctx, False), False)
+    R.rc_sync(ctx)
+
+
+@pytest.mark.parametrize("counts", [[2, 1], [150, 40]])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_attention_of_a_query_without_value(lib, counts, bad):
+    """Its row is NaN and no other."""
+    R, ctx = lib
+    c = Case(R, [300, 100], counts, 2, 2, 72, 30)
+    want = c.run(R, ctx, False)
+    c.q[1, 72 + 5] = bad
+    got = c.run(R, ctx, False)
+    assert bool(got[1, 72:].isnan().all())
+    got[1, 72:] = want[1, 72:]
+    assert torch.equal(got, want)
+    R.rc_sync(ctx)
+
+
+@pytest.mark.parametrize("counts", [[3], [200]])
+def test_attention_value_scales_at_both_ends(lib, counts):
+    """Rows that see one block with values of 2^100 times the others', before or behind them:
+    what the others give is lost beside it where it counts, and whole where it does not."""
+    R, ctx = lib
+    for at in (0, 1, 4):
+        c = Case(R, [300], counts, 2, 2, 64, 31)
+        c.pool.v_scale.fill_(60)
+        c.pool.v_scale[c.table[0, at].item()] = 160
+        c.check(c.run(R, ctx, False), False)
+        c.pool.v_scale.fill_(130)
+        c.pool.v_scale[c.table[0, at].item()] = 0
+        c.pool.v[c.table[0, at].item()] = 0
+        c.check(c.run(R, ctx, True), True)
     R.rc_sync(ctx)
 
 
