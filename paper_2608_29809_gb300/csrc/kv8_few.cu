@@ -48,6 +48,7 @@ struct FCfg {
   static constexpr int KS = (DH + 15) / 16;    // MMA steps of 16 channels
   static constexpr int MB = (DH + 15) / 16;    // blocks of 16 channels of the result
   static constexpr int PSTRIDE = DH + 4;       // floats of a partial row: channels, max, sum
+  static_assert((WARPS * 32 + 1) * 4 <= ROWS * PSTRIDE * 4, "the lengths fit a row's parts");
   static_assert(WARPS * ROWS * PSTRIDE * 4 <= RING, "the warps' parts fit the ring");
   // a row's parts of the cluster's CTAs, in its owner
   static constexpr int JOIN = (ROWS + MAX_PARTS) * PSTRIDE * 4;
@@ -81,6 +82,16 @@ __device__ __forceinline__ uint32_t lds8(uint32_t a) {
   uint32_t v;
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
 __device__ __forceinline__ void cluster_arrive() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -142,7 +153,7 @@ __device__ __forceinline__ void add_values(float (*acc)[NR][4], const uint32_t (
 template <int DH, int NR>
 __global__ void __launch_bounds__(FCfg<DH, NR>::WARPS * 32, 2)
 few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
-                int parts) {
+                int parts, int longest_first) {
   using C = FCfg<DH, NR>;
   constexpr int WARPS = C::WARPS;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -161,7 +172,28 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
   pdl_trigger();
   const int part = parts > 1 ? int(cluster_ctarank()) : 0;
   const int group = a.heads / pool.heads;
-  const int head = blockIdx.y % pool.heads, chunk = blockIdx.y / pool.heads, req = blockIdx.z;
+  const int head = blockIdx.y % pool.heads, chunk = blockIdx.y / pool.heads;
+  int req = blockIdx.z;
+  if (longest_first) {
+    // The request of this rank among the lengths (in steps of a half block; the
+    // lower number first): a thread ranks each.  No two keys are the same, and
+    // places behind the last request hold zeros.
+    const uint32_t keys = saddr(smem) + C::RING;
+    volatile int* found = reinterpret_cast<volatile int*>(smem + C::RING + WARPS * 32 * 4);
+    const int halves = int(threadIdx.x) < a.n ? max(a.lengths[threadIdx.x], 0) / HALF : 0;
+    const uint32_t key = uint32_t(min(halves, (1 << 24) - 1)) << 8 | (255 - threadIdx.x);
+    sts32(keys + 4 * threadIdx.x, int(threadIdx.x) < a.n ? key : 0u);
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 4
+    for (int r = 0; r < a.n; r += 4) {
+      const uint4 k = lds128(keys + 4 * r);
+      rank += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+    }
+    if (int(threadIdx.x) < a.n && rank == int(blockIdx.z)) *found = int(threadIdx.x);
+    __syncthreads();
+    req = __shfl_sync(0xffffffffu, *found, 0);
+  }
   const int q0 = a.offsets[req], nq = a.offsets[req + 1] - q0, len = a.lengths[req];
   // (the same for every CTA of a cluster)
   if (q0 < 0 || nq < 0 || nq > a.max_q || q0 > a.q_rows - nq || len < 0 ||
@@ -530,23 +562,29 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   const long long chunks =
       ((most_rows < a.most_rows ? most_rows : a.most_rows) + C::ROWS - 1) / C::ROWS;
   const long long units = chunks * pool.heads * a.n;
-  // CTAs for two an SM at once; more of them where requests may differ much,
-  // as long as a warp keeps 24 half blocks, beside which a CTA's 6 us of start
-  // and end count little (16 heads of 72: 8 requests of 4096 tokens, one part
-  // 25.9 us, two 20.6, eight 32.6; 16: one 32.1, two 38.1.  48 requests of 500 to
-  // 12000 tokens, 8 key heads of 128: one 131.5, four 117.7, eight 142.4)
+  // CTAs for two an SM at once.  Of requests that may differ, half as long as the
+  // longest on average, the longest is done within the others' time when there
+  // are about 600 CTAs, as long as a warp keeps 16 half blocks, beside which a
+  // CTA's 5 us of start and end count little (16 heads of 72: 8 requests of 4096
+  // tokens, one part 24.6 us, two 19.8, three 27.8; 16: one 30.8, two 38.1, but of
+  // 500 to 9000 tokens one 57.6, two 37.6, three 44.1; 64 of 100 to 8000: one 101,
+  // two 122.  48 of 500 to 12000, 8 key heads of 128: one 117, two 102.9, three 116)
   const long long halves = (long long)a.ld_table * (KV8_BLOCK / HALF);
-  long long parts = 2 * SMS / units, more = halves / (24 * WARPS);
-  if (more > 4) more = 4;
+  long long parts = 2 * SMS / units, more = halves / (16 * WARPS);
+  if (more > (600 + units / 2) / units) more = (600 + units / 2) / units;
   if (parts > 4 && units * parts > 240) parts = 240 / units;  // (larger clusters need room)
   if (a.n > 1 && parts < more) parts = more;
   if (parts > halves / WARPS) parts = halves / WARPS;
   if (parts > MAX_PARTS) parts = MAX_PARTS;
   if (parts < 1) parts = 1;
   const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
+  // Where CTAs wait for others' places, the longest requests go first, so that
+  // none is left alone at the end (the 48 requests above: 102.9 us, in their own
+  // order 114.6; 64 of 2000 tokens each: 61.9 and 59.3)
+  const int longest_first = a.n > 1 && a.n <= WARPS * 32 && units * parts > 2 * SMS ? 1 : 0;
   count_launches(1);
   return launch_k_cluster(few_rows_kernel<DH, NR>, grid, dim3(WARPS * 32), C::SMEM, int(parts), st,
-                          pool, a, int(parts));
+                          pool, a, int(parts), longest_first);
 }
 
 template <int NR>

@@ -373,6 +373,18 @@ def test_attention_few_and_many_rows_together(lib, lens, counts, heads, kvh, dh,
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("n", [37, 40, 191, 192, 193])
+def test_attention_of_many_single_rows(lib, n):
+    """Requests of every length, some the same, some without a token or a row."""
+    R, ctx = lib
+    lens = [(i * 89) % 301 // 3 * 3 if i % 7 else 128 for i in range(n)]
+    lens[3] = 0
+    c = Case(R, lens, [0 if i % 11 == 5 else 1 for i in range(n)], 18, 9, 64, 32)
+    got = c.run(R, ctx, True)
+    c.check(got, True, {(r, h) for r in list(range(0, n, 5)) + [n - 1] for h in (0, 9, 17)})
+    R.rc_sync(ctx)
+
+
 @pytest.mark.parametrize("lens,counts,heads,kvh,dh", [
     ([9000] * 4, [260, 300, 270, 290], 16, 16, 128), ([20000, 17000], [70, 500], 2, 2, 64),
     ([40000], [3], 2, 2, 72)])
