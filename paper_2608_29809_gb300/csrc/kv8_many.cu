@@ -174,10 +174,14 @@ __device__ __forceinline__ void store_two(uint32_t at, float a, float b) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(a), "f"(b) : "memory");
 }
 
+// how a CTA finds its unit
+constexpr int IN_PLACE = 0, BY_WORK = 1, COUNTED = 2;
+constexpr int MAX_RANKED = 64;  // requests BY_WORK
+
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1)
 many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
-                 int parts, int unit_rows, int compact) {
+                 int parts, int unit_rows, int order) {
   using C = MCfg<DH>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -212,17 +216,54 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     return count * group >= a.least_rows ? count * group : 0;
   };
   int head, req, chunk;  // (the same for every CTA of a cluster)
-  if (!compact) {
+  if (order == IN_PLACE) {
     // a place for each chunk that a request may have, key head and request
     req = place % a.n;
     head = place / a.n % pool.heads;
     chunk = place / a.n / pool.heads;
     if (chunk * unit_rows >= rows_of(req, threadIdx.x == 0)) return;
+  } else if (order == BY_WORK) {
+    // Units in the order of their work, the key heads of each together: a
+    // request has whole ones and perhaps a shorter last one, a thread counts the
+    // units before each of the two (no two keys are the same).
+    head = place % pool.heads;
+    const int unit = place / pool.heads, e = int(threadIdx.x), r = e >> 1;
+    const bool last = e & 1;
+    uint2* works = reinterpret_cast<uint2*>(smem);
+    int rows = 0, count = 0;
+    uint32_t key = 0;
+    if (e < 2 * a.n) {
+      rows = rows_of(r, blockIdx.x == 0);
+      count = last ? (rows % unit_rows ? 1 : 0) : rows / unit_rows;
+      // blocks, one stream's at three quarters of two's, and what a unit starts with
+      const int blocks = min(max(a.lengths[r], 0), 1 << 28) / BKV;
+      const int per = (last ? rows % unit_rows : unit_rows) > BQ ? 4 : 3;
+      key = uint32_t(blocks * per + 12) << 7 | uint32_t(127 - e);
+      works[e] = make_uint2(key, count);
+    }
+    if (e == 0) found[0] = -1;
+    __syncthreads();
+    if (e < 2 * a.n) {
+      int before = 0;
+#pragma unroll 4
+      for (int i = 0; i < 2 * a.n; ++i) {
+        const uint2 w = works[i];
+        before += w.x > key ? int(w.y) : 0;
+      }
+      if (unit >= before && unit < before + count) {
+        found[0] = r;
+        found[1] = last ? rows / unit_rows : count - 1 - (unit - before);
+      }
+    }
+    fence_proxy_async_smem();  // (copies come where the keys were)
+    __syncthreads();
+    req = __shfl_sync(0xffffffffu, found[0], 0);
+    chunk = __shfl_sync(0xffffffffu, found[1], 0);
+    if (req < 0) return;
   } else {
-    // Places for as many units as the rows can make: whole ones first, then the
-    // requests' short last ones, the key heads of each together.  This one's
-    // request is found by counting (as many requests at a time as the CTA has
-    // threads).  A bad request has none, and is reported.
+    // Whole units first, then the requests' short last ones, the key heads of each
+    // together.  This place's is found by counting (as many requests at a time as
+    // the CTA has threads).  A bad request has none, and is reported.
     head = place % pool.heads;
     const int unit = place / pool.heads;
     int whole = 0;  // units, of all requests
@@ -789,20 +830,26 @@ cudaError_t many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   const int group = a.heads / pool.heads;
   const Shape sh = choose(a, pool.heads, group);
   const int unit_rows = sh.unit_rows, parts = sh.parts;
-  // Units at most: whole ones and a last one for each request.  Where places for
-  // every chunk of every request would be more than twice that, the kernel counts
-  // out the units that there are (a place without one costs a CTA's launch, the
-  // counting every CTA 1.2 us)
+  // Units at most: whole ones and a last one for each request.  Where CTAs wait
+  // for others' places the longest go first, of up to 64 requests; of more, the
+  // kernel counts out the units that there are where places for every chunk of
+  // every request would be more than twice as many (a place without one costs a
+  // CTA's launch, the counting every CTA 1.2 us).  16 requests of 500 to 9000
+  // tokens and 100 to 400 rows: 147 us, in place 180; 32 of 500 to 8000, 40 to 200
+  // rows, 4 heads a key head of 128: 317 and 390; 8 of 4096, 201 to 831 rows: 123
+  // and 125; 4 of 4096, 512 rows each, 4 heads of 128: 141 and 136.
   const long long most = (long long)a.n * a.max_q, rows = most < a.q_rows ? most : a.q_rows;
   const long long all = ((long long)a.max_q * group + unit_rows - 1) / unit_rows * a.n;
-  const long long units = rows * group / unit_rows + a.n;
-  const int compact = all > 2 * units ? 1 : 0;
-  const long long ctas = (compact ? units : all) * pool.heads * parts;
+  long long units = rows * group / unit_rows + a.n;
+  const int order = a.n > 1 && a.n <= MAX_RANKED && all * pool.heads * parts > SMS ? BY_WORK
+                    : all > 2 * units ? COUNTED : IN_PLACE;
+  if (order == IN_PLACE || units > all) units = all;
+  const long long ctas = units * pool.heads * parts;
   if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
   const dim3 grid{unsigned(ctas), 1u, 1u};
   count_launches(1);
   return launch_k_cluster(many_rows_kernel<DH>, grid, dim3(THREADS), C::SMEM, parts, st, pool, a,
-                          parts, unit_rows, compact);
+                          parts, unit_rows, order);
 }
 
 }  // namespace

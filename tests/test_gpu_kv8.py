@@ -385,6 +385,18 @@ def test_attention_of_many_single_rows(lib, n):
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("n", [63, 64, 65])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_of_requests_of_every_size(lib, n, causal):
+    """More units than SMs: whole and last ones of many lengths, some requests without any."""
+    R, ctx = lib
+    c = Case(R, [(i * 37) % 211 * (1 + i % 3) for i in range(n)],
+             [0 if i % 9 == 4 else 1 + (i * 53) % 390 for i in range(n)], 6, 3, 64, 33)
+    got = c.run(R, ctx, causal)
+    c.check(got, causal, {(r, h) for r in list(range(0, n, 4)) + [n - 1] for h in (0, 3, 5)})
+    R.rc_sync(ctx)
+
+
 @pytest.mark.parametrize("lens,counts,heads,kvh,dh", [
     ([9000] * 4, [260, 300, 270, 290], 16, 16, 128), ([20000, 17000], [70, 500], 2, 2, 64),
     ([40000], [3], 2, 2, 72)])
