@@ -530,6 +530,26 @@ def test_attention_leaves_out_and_reports_bad_requests(lib, counts):
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("counts", [[1] * 60, [40] * 60, [3] * 99 + [900] + [30] * 20])
+def test_attention_leaves_bad_requests_out_of_the_order(lib, counts):
+    """Batches of more CTAs than places: the other requests' rows keep their bits."""
+    R, ctx = lib
+    n = len(counts)
+    lens = [(i * 31) % 160 + 1 for i in range(n)]
+    c = Case(R, lens, counts, 6, 6, 64, 34)
+    want = c.run(R, ctx, False)
+    for r in (0, 7, n - 1):
+        for bad in (-1, c.width * 64 + 1):
+            c.lens = lens[:r] + [bad] + lens[r + 1:]
+            got = c.run(R, ctx, False)
+            _reported(R, ctx)
+            rows = slice(c.offsets[r], c.offsets[r + 1])
+            assert bool((got[rows] == 7).all())
+            got[rows] = want[rows]
+            assert torch.equal(got, want)
+    R.rc_sync(ctx)
+
+
 def test_attention_gives_the_same_bits_again(lib):
     R, ctx = lib
     for lens, counts in (([5000, 300], [1, 1]), ([3000, 700], [130, 200])):
