@@ -579,7 +579,7 @@ typedef struct rc_kv8 {
  * tokens) the table is only read and *used is 0.
  * Device checks (RC_ERR_DEVICE_ASSERT at rc_sync): a request with bad counts
  * or too long for its table has no rows; a row whose block is missing (the
- * free blocks have run out, a negative table entry) or whose position is out
+ * free blocks have run out, an entry below 0 or of 2^25 on) or whose position is out
  * of range has slot -1; rows beyond n_slots are dropped.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
 #define RC_KV8_MAX_REQUESTS 4096

@@ -17,9 +17,10 @@ __device__ __forceinline__ int scale_byte(uint32_t a) {
   const int e = int(a >> 23) - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);
   return e < 0 ? 0 : e;
 }
-// 2^(127 - b) in f32, NaN for 255 (b <= 247 otherwise: scale_byte of FLT_MAX).
+// 2^(127 - b) in f32, NaN for 255.  (scale_byte gives at most 247, but a pool may
+// come with a scale of 254, whose inverse is a subnormal.)
 __device__ __forceinline__ float scale_inverse(int b) {
-  return __uint_as_float(b == 255 ? 0x7fffffffu : uint32_t(254 - b) << 23);
+  return __uint_as_float(b == 255 ? 0x7fffffffu : b == 254 ? 0x400000u : uint32_t(254 - b) << 23);
 }
 // 2^(b - 127) in f32, NaN for 255.
 __device__ __forceinline__ float scale_value(int b) {

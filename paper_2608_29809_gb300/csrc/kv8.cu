@@ -51,7 +51,13 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
   __shared__ unsigned long long s_warp[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool first = blockIdx.x == 0;
-  // rows in the high and blocks in the low half of one 64-bit sum
+  // rows in the high and blocks in the low half of one 64-bit sum, neither past
+  // 2^31 - 1 (more than any call may have, so that a sum behind it is reported)
+  const auto plus = [](unsigned long long u, unsigned long long v) {
+    const unsigned lo = min(unsigned(u) + unsigned(v), 0x7fffffffu);
+    const unsigned hi = min(unsigned(u >> 32) + unsigned(v >> 32), 0x7fffffffu);
+    return (unsigned long long)hi << 32 | lo;
+  };
   unsigned long long mine[TAB_PER], sum = 0;
   const int per = (n + TAB_THREADS - 1) / TAB_THREADS;
 #pragma unroll
@@ -59,33 +65,34 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
     const int r = tid * per + i;
     const Request q = i < per ? request(a, r, first) : Request{0, 0, 0, 0};
     mine[i] = (unsigned long long)(unsigned)q.cnt << 32 | unsigned(q.fresh);
-    sum += mine[i];
+    sum = plus(sum, mine[i]);
     if (i < per && r < n) s_len[r] = q.len;
   }
   unsigned long long incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const unsigned long long v = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += v;
+    if (lane >= o) incl = plus(incl, v);
   }
   if (lane == 31) s_warp[warp] = incl;
   __syncthreads();
   unsigned long long before = lane < warp ? s_warp[lane] : 0;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-  unsigned long long at = before + incl - sum;
+  for (int o = 16; o > 0; o >>= 1) before = plus(before, __shfl_xor_sync(0xffffffffu, before, o));
+  const unsigned long long others = __shfl_up_sync(0xffffffffu, incl, 1);
+  unsigned long long at = lane > 0 ? plus(before, others) : before;
 #pragma unroll
   for (int i = 0; i < TAB_PER; ++i) {
     const int r = tid * per + i;
     if (i < per && r < n) {
-      s_row[r] = int(min(at >> 32, 0x7fffffffull));
+      s_row[r] = int(at >> 32);
       s_free[r] = int(at & 0xffffffffull);
       if (first) a.offsets[r] = s_row[r];
     }
-    at += mine[i];
+    at = plus(at, mine[i]);
   }
   if (tid == TAB_THREADS - 1) {
-    const int total = int(min(at >> 32, 0x7fffffffull)), taken = int(at & 0xffffffffull);
+    const int total = int(at >> 32), taken = int(at & 0xffffffffull);
     s_row[n] = total;
     if (first) {
       a.offsets[n] = total;
@@ -129,12 +136,13 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
         if (blk < held) {
           page = *entry;
         } else {
-          const int f = s_free[r] + blk - held;
-          page = f >= a.n_free ? -1 : a.free_blocks ? a.free_blocks[f] : f;
+          const unsigned f = unsigned(s_free[r]) + unsigned(blk - held);  // (below 2^32)
+          page = f >= unsigned(a.n_free) ? -1 : a.free_blocks ? a.free_blocks[f] : int(f);
           if (p % KV8_BLOCK == 0) *entry = page;
         }
       }
-      if (page < 0) atomicOr(a.err, DEVERR_INDEX);
+      // (a block that no pool has would give another one's slot)
+      if (page < 0 || page > 0x7fffffff / KV8_BLOCK) atomicOr(a.err, DEVERR_INDEX);
       else slot[k] = page * KV8_BLOCK + p % KV8_BLOCK;
     }
     if (base + TAB_SLOTS <= i1 && (reinterpret_cast<uintptr_t>(a.slots + base) & 15) == 0) {
@@ -337,7 +345,7 @@ cudaError_t launch_kv8_tables(const Kv8TablesArgs& a, cudaStream_t st) {
   per = per < LEAST ? LEAST : (per + TAB_SLOTS - 1) / TAB_SLOTS * TAB_SLOTS;
   const long long ctas = ((long long)a.n_slots + per - 1) / per;
   const size_t smem = size_t(3 * a.n + 1) * sizeof(int);
-  if (smem > 48 * 1024)
+  if (smem > 40 * 1024)  // (beside the static part)
     RC_TRY(cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 int(smem)));
   count_launches(1);

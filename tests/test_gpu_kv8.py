@@ -89,6 +89,46 @@ def test_tables(lib, lengths, counts, free_list):
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("n", [1023, 1024, 4074, 4075, 4095])
+def test_tables_of_any_number_of_requests(lib, n):
+    R, ctx = lib
+    lengths = [(i * 5) % 66 for i in range(n)]
+    need = sum(map(_blocks, lengths))
+    table = torch.full((n, 2), -1, dtype=torch.int32, device="cuda")
+    offsets, slots, used = _tables(R, ctx, lengths, None, None, range(need), table, sum(lengths),
+                                   free_list=False)
+    at, want = 0, []
+    for l in lengths:
+        want += [at * BLOCK + p for p in range(l)]
+        at += _blocks(l)
+    assert slots == want and used == need and offsets[-1] == len(want)
+    R.rc_sync(ctx)
+
+
+def test_tables_report_sums_that_pass_the_integers(lib):
+    """Rows and new blocks of all requests together beyond 2^32: the first rows as ever."""
+    R, ctx = lib
+    table = torch.full((4096, 16384), -1, dtype=torch.int32, device="cuda")
+    offsets, slots, used = _tables(R, ctx, [2 ** 20] * 4096, None, None, [7, 3], table, 100)
+    _reported(R, ctx)
+    assert offsets[:3] == [0, 2 ** 20, 2 ** 21] and offsets[-1] == 2 ** 31 - 1
+    assert offsets == sorted(offsets) and used == 4096 * 16384
+    assert slots == [7 * 64 + i for i in range(64)] + [3 * 64 + i for i in range(36)]
+
+
+@pytest.mark.parametrize("entry", [2 ** 25, 2 ** 26, 2 ** 31 - 1])
+def test_tables_give_no_slot_in_a_block_that_no_pool_has(lib, entry):
+    R, ctx = lib
+    table = torch.full((1, 2), entry, dtype=torch.int32, device="cuda")
+    assert _tables(R, ctx, [70], [2], None, [], table, 2)[1] == [-1, -1]
+    _reported(R, ctx)
+    assert _tables(R, ctx, [3], None, None, [entry], table, 3)[1] == [-1] * 3
+    _reported(R, ctx)
+    table.fill_(2 ** 25 - 1)
+    assert _tables(R, ctx, [70], [2], None, [], table, 2)[1] == [2 ** 31 - 60, 2 ** 31 - 59]
+    R.rc_sync(ctx)
+
+
 def test_tables_of_dirty_tokens(lib):
     R, ctx = lib
     lengths, counts = [300, 64, 0, 1000], [3, 2, 0, 5]
@@ -227,6 +267,17 @@ def test_store_scales_far_apart(lib):
     for i, top in enumerate((0.0, 1e-42, 1e-30, 1e-3, 1.0, 500.0, 3e38)):
         x = _rand(10, 256, seed=8 + i).clamp(-4, 4) / 4 * top
         _store_and_check(R, ctx, p, x, x[:, 128:], [s + i for s in slots], False)
+    R.rc_sync(ctx)
+
+
+@pytest.mark.parametrize("byte", [248, 253, 254])
+def test_store_under_scales_that_it_never_gives_itself(lib, byte):
+    R, ctx = lib
+    p = _pool(R, 2, 2, 64, seed=17)
+    p.k_scale.fill_(byte)
+    p.v_scale.fill_(byte)
+    x = _rand(9, 256, seed=18).clamp(-4, 4) / 4 * 3e38
+    _store_and_check(R, ctx, p, x, x[:, 128:], list(range(70, 79)), False)
     R.rc_sync(ctx)
 
 
