@@ -611,6 +611,48 @@ def test_attention_gives_the_same_bits_again(lib):
     R.rc_sync(ctx)
 
 
+def test_attention_captured_on_streams_at_once(lib):
+    """Graphs of batches for either kernel and for both, replayed at once on streams of their own
+    with other lengths than at capture."""
+    R, ctx = lib
+    cases = [Case(R, lens, counts, 8, 4, 64, 35 + len(lens)) for lens, counts in (
+        ([900] * 3, [1] * 3), ([700] * 5, [90, 200, 3, 40, 150]),
+        ([300] * 90, [1] * 80 + [100] * 10), ([5000], [300]))]
+    runs = []
+    for c in cases:
+        wide, rows = 8 * 64, sum(c.counts)
+        full, short = _ints(c.lens), _ints([l - 70 * (i % 3) for i, l in enumerate(c.lens)])
+        lens, offsets, table = full.clone(), _ints(c.offsets), c.table.cuda()
+        out = torch.zeros(rows, wide, dtype=torch.bfloat16, device="cuda")
+
+        def go(c=c, lens=lens, offsets=offsets, table=table, out=out, rows=rows, wide=wide):
+            R.rc_kv8_attention(ctx, c.pool, c.q, wide + 8, rows, offsets, lens, len(c.lens),
+                               max(c.counts), table, c.width, c.heads, True, out, wide)
+
+        want = []
+        for l in (short, full):
+            lens.copy_(l)
+            go()
+            want.append(out.clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            go()
+        runs.append((graph, torch.cuda.Stream(), go, lens, (short, full), out, want))
+    for i in (0, 1, 0):
+        for *_, lens, choice, out, want in runs:
+            lens.copy_(choice[i])
+            out.zero_()
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for graph, stream, *_ in runs:
+                with torch.cuda.stream(stream):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for *_, out, want in runs:
+            assert torch.equal(out, want[i])
+    R.rc_sync(ctx)
+
+
 # ---------------------------------------------------------------- together
 def test_a_region_sublayer_in_eight_bits(lib):
     """Quantised q | k | v product, slot map of the dirty tokens, store, attention and quantised
