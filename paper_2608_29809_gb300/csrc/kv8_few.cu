@@ -33,7 +33,7 @@ using namespace rc::tc;
 
 constexpr int HALF = 32;  // tokens of a ring stage
 constexpr int MAX_PARTS = 8;
-constexpr float ABSENT = -2e30f, NO_REF = -1e30f;
+constexpr float NO_REF = -1e30f;
 // how far scores and value scales may pass their references, and fall below
 constexpr float RAISE = 8.f, RAISE_VALUE = 4.f, APART = -10.f;
 
@@ -194,6 +194,13 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     __syncthreads();
     req = __shfl_sync(0xffffffffu, *found, 0);
   }
+  // This warp's half blocks are first + stride i: the table's first entries are
+  // asked for beside the request's sizes (an entry that it has no use for is not
+  // looked at).
+  const int first = part * WARPS + warp, stride = parts * WARPS;
+  const int* table = a.table + (long long)req * a.ld_table;
+  const auto place = [&](int i) { return (first + i * stride) / (KV8_BLOCK / HALF); };
+  const int entry = place(lane) < a.ld_table ? table[place(lane)] : -1;
   const int q0 = a.offsets[req], nq = a.offsets[req + 1] - q0, len = a.lengths[req];
   // (the same for every CTA of a cluster)
   if (q0 < 0 || nq < 0 || nq > a.max_q || q0 > a.q_rows - nq || len < 0 ||
@@ -205,34 +212,24 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
   if (row0 >= rows || rows > a.most_rows) return;
   if (parts > 1) cluster_arrive();  // (waited for before anything is put into a peer)
 
-  // ---- this warp's half blocks: first + WARPS i for i < mine
+  // ---- lane l holds place and scales (-1: none) of half blocks l of the current
+  // 32 and of the next 32; the next ones' scales are still on their way
   const int halves = (len + HALF - 1) / HALF;
-  const int h0 = int((long long)part * halves / parts);
-  const int h1 = int((long long)(part + 1) * halves / parts);
-  const int first = h0 + warp, mine = first < h1 ? (h1 - first + WARPS - 1) / WARPS : 0;
-  const int* table = a.table + (long long)req * a.ld_table;
-  // lane l holds place, key scale (NaN: no value) and value exponent of half
-  // blocks l of the current 32 and of the next 32
-  int page[2];
-  float sk[2], sv[2];
-  const auto look_up = [&](int from, int b) {
+  const int mine = first < halves ? (halves - first + stride - 1) / stride : 0;
+  int page[2], scales, scale_k, scale_v;
+  const auto look_up = [&](int b, bool in, int p) {
     page[b] = -1;
-    sk[b] = 0.f;
-    sv[b] = ABSENT;
-    if (from + lane < mine) {
-      const int p = table[(first + (from + lane) * WARPS) / (KV8_BLOCK / HALF)];
-      if (p < 0 || p >= pool.blocks) {
-        atomicOr(a.err, DEVERR_INDEX);
-      } else {
-        page[b] = p;
-        const int k = pool.scale[0][(long long)p * pool.heads + head];
-        const int v = pool.scale[1][(long long)p * pool.heads + head];
-        sk[b] = scale_value(max(k, v) == 255 ? 255 : k);
-        sv[b] = float(v);
-      }
+    if (!in) return;
+    if (p < 0 || p >= pool.blocks) {
+      atomicOr(a.err, DEVERR_INDEX);
+    } else {
+      page[b] = p;
+      scale_k = pool.scale[0][(long long)p * pool.heads + head];
+      scale_v = pool.scale[1][(long long)p * pool.heads + head];
     }
   };
-  look_up(0, 0);
+  const auto looked_up = [&](int b) { return page[b] < 0 ? -1 : scale_v << 8 | scale_k; };
+  look_up(0, lane < mine, entry);
   // (i is at most one batch of 32 ahead of the current one)
   const auto issue = [&](int i, int base) {
     if (i >= mine) return;
@@ -240,7 +237,7 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     const int p1 = __shfl_sync(0xffffffffu, page[1], i & 31);
     const int p = i - base < 32 ? p0 : p1;
     if (p < 0 || lane != 0) return;
-    const int h = (first + i * WARPS) % (KV8_BLOCK / HALF), st = i % C::STAGES;
+    const int h = (first + i * stride) % (KV8_BLOCK / HALF), st = i % C::STAGES;
     const long long at = (((long long)p * pool.heads + head) * KV8_BLOCK + h * HALF) * DH;
     mbar_expect_tx(bar0 + 8 * st, C::STAGE);
     bulk_load(ring + st * C::STAGE, pool.code[0] + at, C::PART, bar0 + 8 * st);
@@ -248,7 +245,8 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
   };
   page[1] = -1;
   for (int i = 0; i < C::STAGES; ++i) issue(i, 0);
-  look_up(32, 1);
+  scales = looked_up(0);
+  look_up(1, 32 + lane < mine, 32 + lane < mine ? table[place(32 + lane)] : -1);
 
   // ---- queries as B fragments, row 8 r + g, in the channel order of the keys
   // (step s < 4 of a 64-channel part: channels 16 t + 4 s ..; the last 8 of 72:
@@ -316,14 +314,15 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     if (i - base == 32) {
       base += 32;
       page[0] = page[1];
-      sk[0] = sk[1];
-      sv[0] = sv[1];
-      look_up(base + 32, 1);
+      scales = looked_up(1);
+      const int next = base + 32 + lane;
+      look_up(1, next < mine, next < mine ? table[place(next)] : -1);
     }
-    const float kf = __shfl_sync(0xffffffffu, sk[0], i - base);
-    const float bv = __shfl_sync(0xffffffffu, sv[0], i - base);
-    if (bv > NO_REF) {
-      const int key0 = (first + i * WARPS) * HALF;
+    const int both = __shfl_sync(0xffffffffu, scales, i - base);
+    if (both >= 0) {
+      const int kb = both & 255, vb = both >> 8;
+      const float kf = scale_value(max(kb, vb) == 255 ? 255 : kb), bv = float(vb);
+      const int key0 = (first + i * stride) * HALF;
       if (!mbar_sleep_warp(bar0 + 8 * st, (phases >> st) & 1, abort_flag)) { ok = false; break; }
       phases ^= 1u << st;
       const uint32_t ks = ring + st * C::STAGE;
