@@ -4,9 +4,9 @@
 //
 // A unit is up to 8 NR rows (query, head of the key head's group) of one
 // request and key head.  A cluster of CTAs shares the unit's keys, six warps a CTA
-// and two CTAs an SM; a warp takes every sixth half block of its CTA's (32
-// tokens: a contiguous run of keys and one of values), which bulk copies bring
-// ahead of it into a ring of its own.  Codes become f16 exactly in registers and are the
+// and two CTAs an SM (or twelve and one, where units are few); a warp takes its
+// turn of the half blocks (32 tokens: a contiguous run of keys and one of
+// values), which bulk copies bring ahead of it into a ring of its own.  Codes become f16 exactly in registers and are the
 // A operand of mma.sync (16 keys, then 16 channels), the rows N = 8: with rows
 // as M = 16 the same work took twice the MMAs and half as many more
 // instructions.  Keys and channels are taken in an order that makes each
@@ -19,6 +19,8 @@
 // leave 2^12; weights are f16, so a block whose value scale lies more than
 // 2^10 below the reference is multiplied apart and added in f32.
 #include <math.h>
+
+#include <atomic>
 
 #include "common.cuh"
 #include "eight_bit.h"
@@ -33,14 +35,15 @@ using namespace rc::tc;
 
 constexpr int HALF = 32;  // tokens of a ring stage
 constexpr int MAX_PARTS = 8;
+constexpr int WARPS_OF_TWO = 6;  // of a CTA, two an SM (twice as many of one alone)
 constexpr float NO_REF = -1e30f;
 // how far scores and value scales may pass their references, and fall below
 constexpr float RAISE = 8.f, RAISE_VALUE = 4.f, APART = -10.f;
 
-template <int DH, int NR>
+template <int DH, int NR, int W>
 struct FCfg {
   static constexpr int ROWS = 8 * NR;
-  static constexpr int WARPS = 6;
+  static constexpr int WARPS = W;
   static constexpr int PART = HALF * DH;       // bytes of a stage's keys
   static constexpr int STAGE = 2 * PART;
   static constexpr int STAGES = DH == 128 ? 2 : DH == 72 ? 3 : 4;
@@ -150,11 +153,11 @@ __device__ __forceinline__ void add_values(float (*acc)[NR][4], const uint32_t (
   }
 }
 
-template <int DH, int NR>
-__global__ void __launch_bounds__(FCfg<DH, NR>::WARPS * 32, 2)
+template <int DH, int NR, int W>
+__global__ void __launch_bounds__(W * 32, 2 * WARPS_OF_TWO / W)
 few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv8AttnArgs a,
                 int parts, int longest_first) {
-  using C = FCfg<DH, NR>;
+  using C = FCfg<DH, NR, W>;
   constexpr int WARPS = C::WARPS;
   extern __shared__ __align__(128) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::JOIN);
@@ -550,16 +553,53 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
 
 constexpr int SMS = 152;
 
+template <int DH, int NR, int W>
+cudaError_t launch(const Kv8Pool& pool, const Kv8AttnArgs& a, long long chunks, long long parts,
+                   bool longest_first, cudaStream_t st) {
+  using C = FCfg<DH, NR, W>;
+  RC_TRY(cudaFuncSetAttribute(few_rows_kernel<DH, NR, W>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM)));
+  const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
+  count_launches(1);
+  return launch_k_cluster(few_rows_kernel<DH, NR, W>, grid, dim3(W * 32), C::SMEM, int(parts), st,
+                          pool, a, int(parts), longest_first ? 1 : 0);
+}
+
+// How many clusters of `parts` CTAs of W warps the GPU holds at once (found out
+// at the first call; 0 where that fails).
+template <int DH, int NR, int W>
+int clusters_at_once(int parts) {
+  static std::atomic<int> known[MAX_PARTS + 1];
+  int n = known[parts].load(std::memory_order_relaxed) - 1;
+  if (n >= 0) return n;
+  using C = FCfg<DH, NR, W>;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = unsigned(parts);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(parts));
+  cfg.blockDim = dim3(W * 32);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(few_rows_kernel<DH, NR, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           int(C::SMEM)) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, few_rows_kernel<DH, NR, W>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    n = 0;
+  }
+  known[parts].store(n + 1, std::memory_order_relaxed);
+  return n;
+}
+
 template <int DH, int NR>
 cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
-  using C = FCfg<DH, NR>;
-  constexpr int WARPS = C::WARPS;
-  RC_TRY(cudaFuncSetAttribute(few_rows_kernel<DH, NR>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::SMEM)));
+  constexpr int WARPS = WARPS_OF_TWO, ROWS = FCfg<DH, NR, WARPS>::ROWS;
   const int group = a.heads / pool.heads;
   const long long most_rows = (long long)a.max_q * group;
   const long long chunks =
-      ((most_rows < a.most_rows ? most_rows : a.most_rows) + C::ROWS - 1) / C::ROWS;
+      ((most_rows < a.most_rows ? most_rows : a.most_rows) + ROWS - 1) / ROWS;
   const long long units = chunks * pool.heads * a.n;
   // CTAs for two an SM at once.  Of requests that may differ, half as long as the
   // longest on average, the longest is done within the others' time when there
@@ -576,14 +616,19 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   if (parts > halves / WARPS) parts = halves / WARPS;
   if (parts > MAX_PARTS) parts = MAX_PARTS;
   if (parts < 1) parts = 1;
-  const dim3 grid(unsigned(parts), unsigned(chunks * pool.heads), unsigned(a.n));
+  // Where there are few units and much to read, CTAs of twice the warps, one an SM,
+  // as many of them a unit as still find a place all at once (16 heads of 72,
+  // one row: 4096 tokens 7.1 us with six warps, 6.5 with twelve; 40000: 32.7 and
+  // 25.0; clusters that wait for others take twice as long)
+  if (units <= 30 && halves > MAX_PARTS * WARPS)
+    for (int p = MAX_PARTS; p >= 5; --p)
+      if (units <= clusters_at_once<DH, NR, 2 * WARPS>(p))
+        return launch<DH, NR, 2 * WARPS>(pool, a, chunks, p, false, st);
   // Where CTAs wait for others' places, the longest requests go first, so that
   // none is left alone at the end (the 48 requests above: 102.9 us, in their own
   // order 114.6; 64 of 2000 tokens each: 61.9 and 59.3)
-  const int longest_first = a.n > 1 && a.n <= WARPS * 32 && units * parts > 2 * SMS ? 1 : 0;
-  count_launches(1);
-  return launch_k_cluster(few_rows_kernel<DH, NR>, grid, dim3(WARPS * 32), C::SMEM, int(parts), st,
-                          pool, a, int(parts), longest_first);
+  const bool longest_first = a.n > 1 && a.n <= WARPS * 32 && units * parts > 2 * SMS;
+  return launch<DH, NR, WARPS>(pool, a, chunks, parts, longest_first, st);
 }
 
 template <int NR>

@@ -450,7 +450,8 @@ def test_attention_of_requests_of_every_size(lib, n, causal):
 
 @pytest.mark.parametrize("lens,counts,heads,kvh,dh", [
     ([9000] * 4, [260, 300, 270, 290], 16, 16, 128), ([20000, 17000], [70, 500], 2, 2, 64),
-    ([40000], [3], 2, 2, 72)])
+    ([40000], [3], 2, 2, 72), ([3100], [1], 16, 16, 72), ([2900], [2], 22, 22, 64),
+    ([2000, 3300], [4, 1], 12, 6, 128), ([2500], [1], 30, 30, 72)])
 def test_attention_over_long_caches(lib, lens, counts, heads, kvh, dh):
     R, ctx = lib
     c = Case(R, lens, counts, heads, kvh, dh, 29)
