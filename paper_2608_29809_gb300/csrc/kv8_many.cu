@@ -659,7 +659,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
             for (int x = 0; x < 2; ++x) {
               const int b = block(i, x), st = b % C::VST;
               if (b >= nb) continue;
-            if ((h == 0 && (!two || x == 0) &&
+              if ((h == 0 && (!two || x == 0) &&
                    !mbar_wait(v_full + 8 * st, (b / C::VST) & 1, abort_flag)) ||
                   !mbar_wait(p_full + 16 * h + 8 * x, i & 1, abort_flag)) { ok = false; break; }
               tc_fence_after();
