@@ -15,7 +15,7 @@ constexpr int GROUP = 128;  // columns of a scale
 // magnitude by four shuffles and write the codes; one pass over x with four
 // loads a lane under way.  The scales of a CTA's eight rows leave together.
 // (With the groups of all rows dealt one by one, and their scales written byte
-// by byte: 4096 x 4608 bf16 15.5 us.)
+// by byte: 4096 x 4608 bf16 15.5 us; now 10.9, 5.2 TB/s.)
 constexpr int ROWS = 8, GROUPS = 8;  // of a CTA
 template <class T, bool WIDE>
 __global__ void __launch_bounds__(32 * ROWS)

@@ -18,6 +18,8 @@
 // references that are raised (and O rescaled) only when the weights would
 // leave 2^12; weights are f16, so a block whose value scale lies more than
 // 2^10 below the reference is multiplied apart and added in f32.
+// 48 requests of 500 to 12000 tokens, a row each, 32 heads over 8 of 128: 615 MB
+// in 100 us, 6.1 TB/s (a copy runs at 6.8).
 #include <math.h>
 
 #include <atomic>
@@ -605,9 +607,9 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   // longest on average, the longest is done within the others' time when there
   // are about 600 CTAs, as long as a warp keeps 16 half blocks, beside which a
   // CTA's 5 us of start and end count little (16 heads of 72: 8 requests of 4096
-  // tokens, one part 24.6 us, two 19.8, three 27.8; 16: one 30.8, two 38.1, but of
-  // 500 to 9000 tokens one 57.6, two 37.6, three 44.1; 64 of 100 to 8000: one 101,
-  // two 122.  48 of 500 to 12000, 8 key heads of 128: one 117, two 102.9, three 116)
+  // tokens, one part 23.5 us, two 19.2, three 26.1; 16: one 29.3, two 36.3, but of
+  // 500 to 9000 tokens one 54.7, two 35.9, three 41.6; 64 of 100 to 8000: one 96,
+  // two 116.  48 of 500 to 12000, 8 key heads of 128: one 117, two 100.9, three 113)
   const long long halves = (long long)a.ld_table * (KV8_BLOCK / HALF);
   long long parts = 2 * SMS / units, more = halves / (16 * WARPS);
   if (more > (600 + units / 2) / units) more = (600 + units / 2) / units;
@@ -625,8 +627,8 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
       if (units <= clusters_at_once<DH, NR, 2 * WARPS>(p))
         return launch<DH, NR, 2 * WARPS>(pool, a, chunks, p, false, st);
   // Where CTAs wait for others' places, the longest requests go first, so that
-  // none is left alone at the end (the 48 requests above: 102.9 us, in their own
-  // order 114.6; 64 of 2000 tokens each: 61.9 and 59.3)
+  // none is left alone at the end (the 48 requests above: 100.9 us, in their own
+  // order 114.0; 64 of 2000 tokens each: 58.5 and 55.9)
   const bool longest_first = a.n > 1 && a.n <= WARPS * 32 && units * parts > 2 * SMS;
   return launch<DH, NR, WARPS>(pool, a, chunks, parts, longest_first, st);
 }
