@@ -6,10 +6,10 @@
 // request and key head.  A cluster of CTAs shares the unit's keys, six warps a CTA
 // and two CTAs an SM (or twelve and one, where units are few); a warp takes its
 // turn of the half blocks (32 tokens: a contiguous run of keys and one of
-// values), which bulk copies bring ahead of it into a ring of its own.  Codes become f16 exactly in registers and are the
-// A operand of mma.sync (16 keys, then 16 channels), the rows N = 8: with rows
-// as M = 16 the same work took twice the MMAs and half as many more
-// instructions.  Keys and channels are taken in an order that makes each
+// values), which bulk copies bring ahead of it into a ring of its own.  Codes
+// become f16 exactly in registers and are the A operand of mma.sync (16 keys,
+// then 16 channels), the rows N = 8: with rows as M = 16 the same work took
+// twice the MMAs and half as many more instructions.  Keys and channels are taken in an order that makes each
 // lane's fragment a contiguous piece of a row: a sum's order is free.
 //   S^T = K Q^T    maximum and sum of a row over the eight lanes that hold it
 //   O^T += V^T P^T  P as B by transposing 8 x 8 tiles in registers
