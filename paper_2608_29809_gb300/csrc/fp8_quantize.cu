@@ -10,13 +10,14 @@ namespace {
 constexpr int GROUP = 128;  // columns of a scale
 
 // ------------------------------------------------------------- quantiser
-// One scale per row and 128 columns.  A warp takes eight groups of its row, two
+// One scale per row and 128 columns.  A warp takes four groups of its row, two
 // at a time: the 16 lanes of a group hold eight values each, find the largest
-// magnitude by four shuffles and write the codes; one pass over x with four
-// loads a lane under way.  The scales of a CTA's eight rows leave together.
+// magnitude by four shuffles and write the codes; one pass over x, all its loads
+// under way at once.  The scales of a CTA's eight rows leave together.
 // (With the groups of all rows dealt one by one, and their scales written byte
-// by byte: 4096 x 4608 bf16 15.5 us; now 10.9, 5.2 TB/s.)
-constexpr int ROWS = 8, GROUPS = 8;  // of a CTA
+// by byte: 4096 x 4608 bf16 15.5 us; now 10.4, 5.5 TB/s.  Eight groups a warp: 10.9,
+// and 14.8 against 12.8 at 16384 x 1152, where more of its lanes have nothing.)
+constexpr int ROWS = 8, GROUPS = 4;  // of a CTA
 template <class T, bool WIDE>
 __global__ void __launch_bounds__(32 * ROWS)
 quant_rows_kernel(const T* __restrict__ x, int ldx, int rows, int cols, int groups,
