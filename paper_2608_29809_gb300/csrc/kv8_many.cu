@@ -795,8 +795,10 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
 constexpr int SMS = 152;
 
 // Rows of a unit and CTAs that share its keys, of least estimated time (us) for
-// requests of the mean number of rows and the longest possible length.  Rates
-// measured at 4096 keys, head_dim 72, 16 heads: a key block takes a unit of 256
+// requests of the mean number of rows and the longest possible length; where there
+// are several, the mean of that and of the time for lengths spread evenly, the
+// longest units first (8 requests of 256 rows, 16 heads of 72: of 500 to 12000
+// tokens one part 138 us, two 88; of 12000 each 142 and 154).  Rates measured at 4096 keys, head_dim 72, 16 heads: a key block takes a unit of 256
 // rows 1.45 us and one of 128 1.1, a unit 4.5 beyond that, and joining parts 5
 // (2.5) and 0.65 for each (256 rows: one part 52.8 us, six 22.2; 831: two 35.3,
 // one 54.0; 4096: one 106, two 132).  Clusters above six CTAs do not all find a
@@ -816,10 +818,16 @@ Shape choose(const Kv8AttnArgs& a, int kv_heads, int group) {
       const double units = ceil(mean / ur) * kv_heads * a.n * parts;
       const double waves = units <= SMS ? 1.0 : units / SMS + 0.5;
       const bool wide = ur == 256 && mean > 128;
-      const double one = ceil(blocks / parts) * (wide ? 1.45 : 1.1) + 4.5 +
-                         (parts > 1 ? (wide ? 5.0 : 2.5) + 0.65 * parts : 0.0);
-      if (waves * one < least * 0.98) {
-        least = waves * one;
+      const double block = wide ? 1.45 : 1.1;
+      const double start = 4.5 + (parts > 1 ? (wide ? 5.0 : 2.5) + 0.65 * parts : 0.0);
+      const double one = ceil(blocks / parts) * block + start;
+      double cost = waves * one;
+      if (a.n > 1) {
+        const double some = units * (0.55 * blocks / parts * block + start) / SMS;
+        cost = 0.5 * (cost + (some > one ? some : one));
+      }
+      if (cost < least * (a.n > 1 ? 0.95 : 0.98)) {
+        least = cost;
         best = Shape{ur, parts};
       }
     }
