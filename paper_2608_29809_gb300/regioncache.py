@@ -482,9 +482,19 @@ class Fp8Matrix:
                                device=device), cols, group)
 
     def _hold(self, codes, scales, cols, group):
-        for t, n in ((codes, codes.shape[0]), (scales, scales.shape[0])):
-            if t.dtype != torch.uint8 or t.dim() != 2 or (n and t.stride(1) != 1):
+        for t in (codes, scales):
+            if t.dtype != torch.uint8 or t.dim() != 2 or (t.shape[0] and t.stride(1) != 1):
                 raise ValueError("codes and scales are uint8 matrices with rows in one piece")
+        # (the entry points see strides only; what these tensors hold bounds the kernels)
+        if group not in (1, 128):
+            raise ValueError("a scale's group is 1 or 128 rows")
+        least = (-(-cols // 128), -(-codes.shape[0] // group))
+        if not 1 <= cols <= codes.shape[1] or scales.shape[0] < least[0] or \
+                scales.shape[1] < least[1]:
+            raise ValueError(f"{cols} columns in codes {tuple(codes.shape)}, scales "
+                             f"{tuple(scales.shape)} of at least {least}")
+        if codes.device != scales.device:
+            raise ValueError("codes and scales lie on one device")
         self.codes, self.scales = codes, scales
         # (a single row's stride says nothing about the next one)
         ld = codes.stride(0) if codes.shape[0] > 1 else max(codes.stride(0), codes.shape[1])
@@ -521,7 +531,7 @@ class Kv8Pool:
 
     def _hold(self, k, v, k_scale, v_scale):
         for t in (k, v, k_scale, v_scale):
-            if t.dtype != torch.uint8 or not t.is_contiguous() or \
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.device != k.device or \
                     t.shape != (k.shape if t is k or t is v else k.shape[:2]):
                 raise ValueError("codes and scales are contiguous uint8 tensors of one pool")
         if k.dim() != 4 or k.shape[2] != RC_KV8_BLOCK:

@@ -185,3 +185,36 @@ def test_attention_refusals(R):
     assert call(q=A + 8) == 1 and call(o=A + 8) == 1
     for kw in (dict(rows=0), dict(max_q=0), dict(n=0)):
         assert call(q=None, o=None, **kw) == 0
+
+
+def test_a_matrix_names_no_more_than_its_tensors_hold(R):
+    """What the structure says is read and written by the kernels: tensors that hold less (or lie
+    elsewhere) are refused where they are named."""
+    def u8(*shape):
+        return torch.zeros(*shape, dtype=torch.uint8)
+
+    for group, wide in ((1, 130), (128, 2)):
+        assert R.Fp8Matrix.of(u8(130, 304), u8(3, wide), 300, group).c.lds == wide
+        assert R.Fp8Matrix.of(u8(130, 320)[:, :304], u8(4, wide + 6)[:, :wide], 300, group).c.lds \
+            == wide + 6
+        for codes, scales, cols in (
+                (u8(130, 304), u8(2, wide), 300),                   # a block of columns short
+                (u8(130, 304), u8(0, wide), 300),
+                (u8(130, 304), u8(3, wide - 1), 300),               # a block of rows short
+                (u8(130, 304), u8(3, wide + 6)[:, :wide - 1], 300),  # .. as the last row's are
+                (u8(130, 288), u8(3, wide), 300),                   # columns short
+                (u8(130, 320)[:, :288], u8(3, wide), 300),
+                (u8(1, 288), u8(3, 1), 300),
+                (u8(130, 304), u8(3, wide), 0),
+                (u8(130, 304), u8(3, wide).to("meta"), 300)):
+            with pytest.raises(ValueError):
+                R.Fp8Matrix.of(codes, scales, cols, group)
+    for group in (0, 2, -128):
+        with pytest.raises(ValueError):
+            R.Fp8Matrix.of(u8(130, 304), u8(3, 130), 300, group)
+    assert R.Fp8Matrix.of(u8(0, 304), u8(3, 0), 300, 1).c.rows == 0
+    p = R.Kv8Pool(3, 2, 72, device="cpu")
+    with pytest.raises(ValueError):
+        R.Kv8Pool.of(p.k, p.v.to("meta"), p.k_scale, p.v_scale)
+    with pytest.raises(ValueError):
+        R.Kv8Pool.of(p.k, p.v, p.k_scale, p.k_scale[:, :1].contiguous())
