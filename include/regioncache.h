@@ -594,7 +594,8 @@ rc_status rc_kv8_tables(rc_ctx* ctx, const int32_t* lengths, const int32_t* coun
  *           element size (16-B aligned rows are read faster).
  *   slots   i32 [n]; a negative slot skips its row.  Slots are distinct, and
  *           the rows of one block stand next to one another (as
- *           rc_kv8_tables gives them for ascending tokens).
+ *           rc_kv8_tables gives them for ascending tokens), with nothing but
+ *           skipped rows between them, within RC_KV8_BLOCK rows of the list.
  *   count   i32 on the device, the rows to store (null: n), 0 .. n.
  *   mode    RC_KV8_UPDATE: a block's scale is raised when the new rows need
  *           it (the codes of its other tokens move with it) and never
@@ -602,8 +603,8 @@ rc_status rc_kv8_tables(rc_ctx* ctx, const int32_t* lengths, const int32_t* coun
  *           rows starts anew, its scale set by these rows alone and its other
  *           tokens void; other blocks as in RC_KV8_UPDATE.
  * Device checks: a slot beyond the pool or a slot twice in a block's rows is
- * skipped and reported.  Rows of one block in two places of the list are not
- * detected: their scale may be wrong.
+ * skipped and reported.  Rows of one block in two places of the list, or
+ * farther apart, are not detected: the block's codes and scale may be wrong.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
 #define RC_KV8_UPDATE 0
 #define RC_KV8_APPEND 1

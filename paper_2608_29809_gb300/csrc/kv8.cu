@@ -157,12 +157,13 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
 }
 
 // ------------------------------------------------------------------ store
-// A run is the rows of one block, next to one another in the list.  A warp
-// takes, for one head of the keys or of the values, the runs that start among
-// its `chunk` rows: a row is PIECES lanes of eight channels, so the warp reads a
-// run once, keeps it in registers while the largest magnitude is found, and
-// writes it as codes; nothing is shared between warps.  (A run that does not
-// fit the registers is read again, from L2.)  With CTAs of four
+// A run is the rows of one block, next to one another in the list but for
+// skipped rows, within 64 rows of it.  A warp takes, for one head of the keys or
+// of the values, the runs that start among its `chunk` rows: a row is PIECES lanes
+// of eight channels, so the warp reads a run once, keeps it in registers while the
+// largest magnitude is found, and writes it as codes; nothing is shared between
+// warps, so no two of them may have rows of one block.  (A run that does not fit
+// the registers is read again, from L2.)  With CTAs of four
 // heads that met at barriers, 4 x 831 rows of 16 heads of 72 took 23.9 us, now
 // 10.1 (latency: a run's rows, their largest magnitude, its codes); eight fills of
 // 4096 tokens, 226 MB, 37 (6.1 TB/s).
@@ -186,77 +187,101 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
   if (c0 >= n) return;
   // slots of the rows from the one before the chunk, 32 apart; -1 for none
   const long long beyond = (long long)pool.blocks * KV8_BLOCK;
+  const auto slot_at = [&](long long r) {
+    const int s = r >= 0 && r < n ? slots[r] : -1;
+    return s >= beyond ? -2 : max(s, -1);
+  };
   int slot[3];
-  unsigned begins[3];  // rows whose block is not the row before's
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     const long long r = (long long)c0 - 1 + 32 * i + lane;
-    int s = r >= 0 && r < n ? slots[r] : -1;
-    if (s >= beyond) {
-      if (speaks && r >= c0 && r < c0 + chunk) atomicOr(err, DEVERR_INDEX);
-      s = -1;
+    slot[i] = slot_at(r);
+    if (slot[i] == -2 && speaks && r >= c0 && r < c0 + chunk) atomicOr(err, DEVERR_INDEX);
+  }
+  // A run begins at a row (below 32 here) whose block is not that of the last row
+  // with a slot, or that has none among the 63 before it.
+  unsigned todo = __ballot_sync(0xffffffffu, slot[0] >= 0);
+  {
+    const unsigned below = todo & ((1u << lane) - 1);
+    int prev = __shfl_sync(0xffffffffu, slot[0], below ? 31 - __clz(below) : 0);
+    if (!(todo & 1) && c0 > 1 && (todo & ((2u << chunk) - 2u))) {
+      // (the row before the chunk is skipped: those before it)
+      const long long r = (long long)c0 - 2 - lane;  // lane + 1 rows before the one of lane 0
+      const int s0 = slot_at(r), s1 = slot_at(r - 32);
+      const unsigned some0 = __ballot_sync(0xffffffffu, s0 >= 0);
+      const unsigned some1 = __ballot_sync(0xffffffffu, s1 >= 0);
+      const int at = some0 ? __ffs(some0) - 1 : some1 ? __ffs(some1) - 1 : 0;
+      const int far = __shfl_sync(0xffffffffu, some0 ? s0 : s1, at);
+      const int rows = at + 1 + (some0 ? 0 : 32) + lane;  // from there to this one
+      if (!below) prev = rows < KV8_BLOCK ? far : -1;
+    } else if (!below) {
+      prev = -1;
     }
-    slot[i] = s < 0 ? -1 : s;
+    todo = __ballot_sync(0xffffffffu,
+                         slot[0] >= 0 && (prev < 0 || slot[0] / KV8_BLOCK != prev / KV8_BLOCK)) &
+           ((2u << chunk) - 2u);
   }
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    int prev = __shfl_up_sync(0xffffffffu, slot[i], 1);
-    const int last = __shfl_sync(0xffffffffu, slot[i > 0 ? i - 1 : 0], 31);
-    if (lane == 0) prev = i > 0 ? last : -1;
-    begins[i] = __ballot_sync(0xffffffffu, slot[i] < 0 || prev < 0 ||
-                                               slot[i] / KV8_BLOCK != prev / KV8_BLOCK);
-  }
-  const int sub = lane / PIECES, piece = lane - sub * PIECES;
-  const bool on = sub < AT_ONCE;
   const auto slot_of = [&](int i) {  // (i < 96, the same or not in each lane)
     const int a = __shfl_sync(0xffffffffu, slot[0], i & 31);
     const int b = __shfl_sync(0xffffffffu, slot[1], i & 31);
     const int c = __shfl_sync(0xffffffffu, slot[2], i & 31);
     return i < 32 ? a : i < 64 ? b : c;
   };
+  const int sub = lane / PIECES, piece = lane - sub * PIECES;
+  const bool on = sub < AT_ONCE;
   const T* src = (side ? vx : kx) + head * DH + piece * 8;
 
-  // the runs that begin in the chunk (below 32 rows; what begins behind the
-  // last row has no slot)
-  unsigned todo = begins[0] & ((2u << chunk) - 2u);
   while (todo) {
     const int start = __ffs(todo) - 1;
     todo &= todo - 1;
-    const int slot0 = __shfl_sync(0xffffffffu, slot[0], start);
-    if (slot0 < 0) continue;
-    const int block = slot0 / KV8_BLOCK;
-    // rows up to the next beginning (row 96 counts as one)
-    int end = 96;
-    if (begins[0] >> 1 >> start) end = start + __ffs(begins[0] >> 1 >> start);
-    else if (begins[1]) end = 31 + __ffs(begins[1]);
-    else if (begins[2]) end = 63 + __ffs(begins[2]);
-    int len = end - start;
-    // the places that the rows fill; more rows than places, or a place twice:
-    // the first row of a place counts
-    if (len > KV8_BLOCK) {
-      len = KV8_BLOCK;
-      if (speaks && lane == 0) atomicOr(err, DEVERR_INDEX);
+    const int block = __shfl_sync(0xffffffffu, slot[0], start) / KV8_BLOCK;
+    // the run's rows among the 64 from here on: those with a slot, ahead of another
+    // block's first
+    const int s0 = slot_of(start + lane), s1 = slot_of(start + 32 + lane);
+    unsigned rows_in[2];
+    {
+      const unsigned stop0 = __ballot_sync(0xffffffffu, s0 >= 0 && s0 / KV8_BLOCK != block);
+      const unsigned stop1 = __ballot_sync(0xffffffffu, s1 >= 0 && s1 / KV8_BLOCK != block);
+      rows_in[0] = __ballot_sync(0xffffffffu, s0 >= 0) & (stop0 ? (stop0 & -stop0) - 1 : ~0u);
+      rows_in[1] = __ballot_sync(0xffffffffu, s1 >= 0) &
+                   (stop0 ? 0u : stop1 ? (stop1 & -stop1) - 1 : ~0u);
+      // more rows than places, or a place twice: the first row of a place counts
+      if (!stop0 && !stop1) {
+        const int next = slot_of(start + KV8_BLOCK);
+        if (speaks && lane == 0 && next >= 0 && next / KV8_BLOCK == block)
+          atomicOr(err, DEVERR_INDEX);
+      }
     }
-    const int off0 = slot_of(start + lane) % KV8_BLOCK;
-    const int off1 = slot_of(min(start + 32 + lane, 95)) % KV8_BLOCK;
-    const bool in0 = lane < len, in1 = lane + 32 < len;
+    const int len = rows_in[1] ? 64 - __clz(rows_in[1]) : 32 - __clz(rows_in[0]);
+    const auto takes = [&](int k) {  // row k of the run's 64 (k < 64)
+      return ((k < 32 ? rows_in[0] : rows_in[1]) >> (k & 31) & 1) != 0;
+    };
+    const int off0 = s0 & (KV8_BLOCK - 1), off1 = s1 & (KV8_BLOCK - 1);
+    const bool in0 = takes(lane), in1 = takes(lane + 32);
     unsigned fill[2];  // places filled
     fill[0] = __reduce_or_sync(0xffffffffu, (in0 && off0 < 32 ? 1u << off0 : 0u) |
                                                 (in1 && off1 < 32 ? 1u << off1 : 0u));
     fill[1] = __reduce_or_sync(0xffffffffu, (in0 && off0 >= 32 ? 1u << (off0 - 32) : 0u) |
                                                 (in1 && off1 >= 32 ? 1u << (off1 - 32) : 0u));
-    const bool twice = __popc(fill[0]) + __popc(fill[1]) != len;
+    const bool twice =
+        __popc(fill[0]) + __popc(fill[1]) != __popc(rows_in[0]) + __popc(rows_in[1]);
     if (twice && speaks && lane == 0) atomicOr(err, DEVERR_INDEX);
+    const bool odd = twice || __popc(rows_in[0]) + __popc(rows_in[1]) != len;
     const bool fresh = append && (fill[0] & 1);
-    const auto place = [&](int k) {  // of row k of the run (every lane takes part)
+    const auto place = [&](int k) {  // of such a row (every lane takes part)
       const int a = __shfl_sync(0xffffffffu, off0, k & 31);
       const int b = __shfl_sync(0xffffffffu, off1, k & 31);
       return k < 32 ? a : b;
     };
-    const auto is_first = [&](int k) {  // of its place
-      const int s = place(k);
-      bool first = true;
-      for (int j = 0; j < len; ++j) first &= !(place(j) == s && j < k);
+    const auto counts = [&](int k) {  // (k < len) it has a slot, and is the first of its place
+      bool first = takes(k);
+      if (twice) {
+        const int s = place(k);
+        for (int j = 0; j < len; ++j) {
+          const bool same = place(j) == s;
+          first &= !(same && takes(j) && j < k);
+        }
+      }
       return first;
     };
     uint8_t* sc = pool.scale[side] + (long long)block * pool.heads + head;
@@ -265,7 +290,7 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
     Eight<T> v[KEEP];
     unsigned top = 0;
     const int passes = (len + AT_ONCE - 1) / AT_ONCE;
-    const T* rows = src + (long long)(c0 + start - 1 + sub) * ldx;
+    const T* rows = src + ((long long)c0 + start - 1 + sub) * ldx;
     const auto fetch_from = [&](int p0) {
       const T* p = rows + (long long)p0 * AT_ONCE * ldx;
 #pragma unroll
@@ -277,7 +302,7 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
         } else {
           v[i].zero();
         }
-        if (twice && !is_first(min(k, len - 1))) v[i].zero();
+        if (odd && !counts(min(k, len - 1))) v[i].zero();
       }
     };
     for (int p0 = 0; p0 < passes; p0 += KEEP) {
@@ -296,8 +321,8 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
         if (p0 + p >= passes) break;
         const int k = (p0 + p) * AT_ONCE + sub;
         const int off = place(k & 63);
-        const bool counts = !twice || is_first(min(k, len - 1));
-        if (on && k < len && counts) *reinterpret_cast<uint2*>(base + off * DH) = v[p].codes(inv);
+        const bool stays = !odd || counts(min(k, len - 1));
+        if (on && k < len && stays) *reinterpret_cast<uint2*>(base + off * DH) = v[p].codes(inv);
       }
     }
     if (b > old && !fresh && on) {
@@ -319,6 +344,7 @@ store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
       }
     }
     if (lane == 0 && (b != old || fresh)) *sc = uint8_t(b);
+    __syncwarp();
   }
 }
 

@@ -259,6 +259,52 @@ def test_store_of_many_rows(lib):
     R.rc_sync(ctx)
 
 
+def _holes(name):
+    """Slots whose skipped rows (negative) lie among the rows of a block."""
+    if name == "one":
+        return [64, 65, -1, 67, 68]
+    if name == "few":  # the run's first row skipped, its last, and all between
+        return [-1, 129, -3, -1, 132, -1] + [5 * 64] + [-1] * 62 + [5 * 64 + 63] + [-2, 200, -1, 193]
+    if name == "far":  # a block's rows 64 rows from end to end, in every place of a warp's rows
+        return sum(([64 * b + 3] + [-1] * 62 + [64 * b + 60] + [-1] * (b % 5) for b in range(40)), [])
+    keep = _perm(2560, 21)  # a scattered fill of which many rows are skipped
+    pages = _perm(40, 22)
+    return [pages[t // 64] * 64 + t % 64 if keep[t] % 7 < 4 else -1 - t for t in range(2560)]
+
+
+@pytest.mark.parametrize("name", ["one", "few", "far", "fill"])
+@pytest.mark.parametrize("heads,dh", [(1, 64), (16, 72), (5, 128)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("append", [False, True])
+def test_store_skips_rows_inside_a_block(lib, name, heads, dh, dtype, append):
+    """One scale for all of a block's rows, whatever lies between them: each larger than those
+    before it in turn, so that a second run of the block would raise the scale again."""
+    R, ctx = lib
+    slots, wide = _holes(name), heads * dh
+    p = _pool(R, 41, heads, dh, seed=19)
+    for seed, up in ((20, 1.0), (21, -1.0)):
+        steps = torch.arange(len(slots), device="cuda") % 64 * 0.25
+        kv = _rand(len(slots), 2 * wide, seed=seed) * torch.exp2(up * steps)[:, None]
+        kv = kv.to(dtype)
+        _store_and_check(R, ctx, p, kv, kv[:, wide:], slots, append)
+    R.rc_sync(ctx)
+
+
+def test_store_reports_a_slot_beyond_the_pool_inside_a_block(lib):
+    """It is skipped as a negative one is: the block's other rows share their scale."""
+    R, ctx = lib
+    p = _pool(R, 4, 2, 72, seed=23)
+    kv = _rand(5, 288, seed=24) * torch.exp2(4.0 * torch.arange(5, device="cuda"))[:, None]
+    want = _state(p)
+    for (codes, scales), x in zip(want, (kv, kv[:, 144:])):
+        E.store(codes, scales, x[:, :144].double().cpu().view(5, 2, 72), [64, 65, -1, 67, 68], True)
+    R.rc_kv8_store(ctx, p, kv, kv[:, 144:], 288, R.RC_F32, _ints([64, 65, 4 * 64, 67, 68]), 5, None,
+                   R.RC_KV8_APPEND)
+    _reported(R, ctx)
+    for (codes, scales), (gc, gs) in zip(want, _state(p)):
+        assert torch.equal(scales, gs) and torch.equal(codes, gc)
+
+
 def test_store_scales_far_apart(lib):
     """Scales raised by up to the whole range, zero rows, and the greatest values."""
     R, ctx = lib
