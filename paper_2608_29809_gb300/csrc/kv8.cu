@@ -374,9 +374,11 @@ cudaError_t launch_kv8_tables(const Kv8TablesArgs& a, cudaStream_t st) {
   per = per < LEAST ? LEAST : (per + TAB_SLOTS - 1) / TAB_SLOTS * TAB_SLOTS;
   const long long ctas = ((long long)a.n_slots + per - 1) / per;
   const size_t smem = size_t(3 * a.n + 1) * sizeof(int);
-  if (smem > 40 * 1024)  // (beside the static part)
-    RC_TRY(cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                int(smem)));
+  // (beside the static part.  The attribute is the device's, not the call's: always
+  // the most that any call takes, so that none lowers it under another thread's launch)
+  constexpr int MOST = (3 * KV8_MAX_REQUESTS + 1) * int(sizeof(int));
+  if (smem > 40 * 1024)
+    RC_TRY(cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST));
   count_launches(1);
   return launch_k(tables_kernel, dim3(unsigned(ctas < 1 ? 1 : ctas)), dim3(TAB_THREADS), smem, st,
                   a, int(per));

@@ -1,6 +1,7 @@
 """The paged eight-bit cache: block tables and slot maps and the store bit for
 bit, the attention against float64, and all of them together."""
 import math
+import threading
 
 import pytest
 import torch
@@ -102,6 +103,36 @@ def test_tables_of_any_number_of_requests(lib, n):
         want += [at * BLOCK + p for p in range(l)]
         at += _blocks(l)
     assert slots == want and used == need and offsets[-1] == len(want)
+    R.rc_sync(ctx)
+
+
+def test_tables_from_threads_at_once(lib):
+    """Calls of different numbers of requests, whose shared memory differs, on streams and buffers
+    of their own: none is refused because of another's."""
+    R, ctx = lib
+    errors = []
+
+    def calls(n):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                table = torch.full((n, 1), -1, dtype=torch.int32, device="cuda")
+                lengths, offsets, slots, used = (_ints([1] * n), _ints([0] * (n + 1)),
+                                                 _ints([0] * n), _ints([0]))
+                for _ in range(4000):
+                    R.rc_kv8_tables(ctx, lengths, None, None, n, None, n, table, 1, offsets, slots,
+                                    n, used, stream)
+                stream.synchronize()
+                assert slots.tolist() == [64 * i for i in range(n)]
+        except Exception as e:  # noqa: BLE001  (told to the main thread)
+            errors.append((n, e))
+
+    threads = [threading.Thread(target=calls, args=(n,)) for n in (4096, 3500, 4000, 3600)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
     R.rc_sync(ctx)
 
 
