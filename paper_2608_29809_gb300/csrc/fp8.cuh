@@ -26,6 +26,14 @@ __device__ __forceinline__ float scale_inverse(int b) {
 __device__ __forceinline__ float scale_value(int b) {
   return __uint_as_float(b == 255 ? 0x7fffffffu : b == 0 ? 0x400000u : uint32_t(b) << 23);
 }
+// A part of a softmax row (sum l of weights 2^(s - m), products with the values)
+// is kept as l 2^-e, m + e and products 2^-e: with this e the sum lies in [2^-8,
+// 2^-7), so that up to 96 parts' products add up without passing the largest
+// value.  Products take their value scale after 2^-e: only a result that f32
+// cannot hold overflows.
+__device__ __forceinline__ int part_exponent(float l) {
+  return l > 0.f ? min(int(__float_as_uint(l) >> 23) - 127 + 8, 126) : 0;
+}
 // Two values as e4m3 codes (nearest, ties to even; `lo` in the low byte).
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   uint16_t r;

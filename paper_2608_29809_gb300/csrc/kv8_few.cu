@@ -56,6 +56,7 @@ struct FCfg {
   static_assert((WARPS * 32 + 1) * 4 <= ROWS * PSTRIDE * 4, "the lengths fit a row's parts");
   static_assert(WARPS * ROWS * PSTRIDE * 4 <= RING, "the warps' parts fit the ring");
   // a row's parts of the cluster's CTAs, in its owner
+  static_assert(WARPS * MAX_PARTS <= 96, "part_exponent");
   static constexpr int JOIN = (ROWS + MAX_PARTS) * PSTRIDE * 4;
   static constexpr size_t SMEM = size_t(RING) + JOIN + WARPS * STAGES * 8 + 16;
 };
@@ -469,7 +470,8 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     atomicOr(a.err, DEVERR_TIMEOUT);
   }
 
-  // ---- the warps' parts, over the ring: per row its channels, maximum, sum
+  // ---- the warps' parts (part_exponent), over the ring: per row its channels,
+  // maximum, sum
 #pragma unroll
   for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -484,19 +486,21 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       float* row = mine_at + (8 * r + 2 * t + c) * C::PSTRIDE;
+      const int e = part_exponent(l[r][c]);
+      const float down = __uint_as_float(uint32_t(127 - e) << 23);
 #pragma unroll
       for (int b = 0; b < C::MB; ++b) {
         if (DH == 72 && b == 4) {
-          row[64 + g] = o[b][r][c] * unit;
+          row[64 + g] = o[b][r][c] * down * unit;
         } else {  // channels 8 g + 2 (b % 4) and the next of a 64-channel part
           const int ch = 64 * (b >> 2) + 8 * g + 2 * (b & 3);
-          row[ch] = o[b][r][c] * unit;
-          row[ch + 1] = o[b][r][2 + c] * unit;
+          row[ch] = o[b][r][c] * down * unit;
+          row[ch + 1] = o[b][r][2 + c] * down * unit;
         }
       }
       if (g == 0) {
-        row[DH] = m[r][c];
-        row[DH + 1] = l[r][c];
+        row[DH] = m[r][c] + float(e);
+        row[DH + 1] = l[r][c] * down;
       }
     }
   __syncthreads();

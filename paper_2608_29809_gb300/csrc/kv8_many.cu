@@ -540,26 +540,30 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     if (ok && mine > 0) ok = mbar_sleep_warp(o_full + 8 * x, 0, abort_flag);
     ok = __all_sync(0xffffffffu, ok);
     tc_fence_after();
+    // (before the value scale the products are divided by their sum, or by its
+    // power of two where parts will be joined)
+    const bool alone = two && parts == 1;
+    const int e = part_exponent(l);
+    const float down = alone ? (l == 0.f ? 0.f : 1.f / l) : __uint_as_float(uint32_t(127 - e) << 23);
     const float back = ref > NO_REF ? scale_value(int(ref)) : 0.f;
     const auto row_out = [&](int r) {
       const int qi = (row0 + r) / group, g = row0 + r - qi * group;
       return a.o + (long long)(q0 + qi) * a.ldo + (head * group + g) * DH;
     };
-    // eight channels from 8 c of O, in their order
+    // eight channels from 8 c of the row's result, in their order
     const auto eight = [&](int c, float* v) {
       uint32_t o[8];
       tmem_ld8_nowait(to + 8 * c, o);
       tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[o_column(j)]) * VALUE_DOWN * back;
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(o[o_column(j)]) * (VALUE_DOWN * down) * back;
     };
     const auto put = [&](bf16* p, const float* v, float inv) {
       *reinterpret_cast<uint4*>(p) =
           make_uint4(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv),
                      pack_bf16x2(v[4] * inv, v[5] * inv), pack_bf16x2(v[6] * inv, v[7] * inv));
     };
-    if (two && parts == 1) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (alone) {
       bf16* p = row_out(in ? ur : 0);
 #pragma unroll
       for (int c = 0; c < DH / 8; ++c) {
@@ -567,7 +571,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
         if (mine > 0) eight(c, v);
         else
           for (int j = 0; j < 8; ++j) v[j] = 0.f;
-        if (in && ok) put(p + 8 * c, v, l == 0.f ? 0.f : inv);
+        if (in && ok) put(p + 8 * c, v, 1.f);
       }
     } else {
       // The row's parts (of both streams where they share a tile, of every CTA
@@ -589,7 +593,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
           store_four(put_at + 32 * c + 16, v + 4);
         }
       }
-      if (in) store_two(put_at + 4 * DH, blind ? -INFINITY : m, l);
+      if (in) store_two(put_at + 4 * DH, blind ? -INFINITY : m + float(e), l * down);
       if (parts > 1) cluster_sync();
       else soft_sync();
       const int first = part * each, live = min(each, rows - first);

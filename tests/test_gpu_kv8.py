@@ -597,6 +597,26 @@ def test_attention_value_scales_at_both_ends(lib, counts):
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("lens,counts,heads,kvh,dh", [
+    ([300], [3], 2, 2, 72), ([700, 64], [16, 2], 4, 2, 128), ([5000], [1], 2, 2, 64),
+    ([300], [200], 2, 2, 64), ([260], [100], 1, 1, 128), ([3000], [150], 2, 2, 72),
+    ([200] * 40, [45] * 40, 6, 6, 72)])
+@pytest.mark.parametrize("byte", [3, 20, 240, 244])
+def test_attention_of_the_smallest_and_largest_values(lib, lens, counts, heads, kvh, dh, byte):
+    """A mean of values near f32's ends lies there too, whatever the sum of its weights (scores of
+    up to some tens: the first blocks' may lie far below a row's largest)."""
+    R, ctx = lib
+    c = Case(R, lens, counts, heads, kvh, dh, 43, scale=0.5)
+    c.pool.v_scale.fill_(byte)
+    got = c.run(R, ctx, False)
+    up = 2.0 ** (127 - byte)  # (the tolerance's floor is for values near 1)
+    kept, c.pool.v_scale = c.pool.v_scale, torch.full_like(c.pool.v_scale, 127)
+    assert bool(got.isfinite().all())
+    c.check(got * up, False)
+    c.pool.v_scale = kept
+    R.rc_sync(ctx)
+
+
 @pytest.mark.parametrize("counts", [[1, 1], [3, 150]])
 def test_attention_block_without_value(lib, counts):
     """NaN blocks reach the rows that see them and no others; behind the last token and in
