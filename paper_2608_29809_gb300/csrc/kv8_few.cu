@@ -17,7 +17,10 @@
 // scores and its value scale the exponent of its weights, both relative to
 // references that are raised (and O rescaled) only when the weights would
 // leave 2^12; weights are f16, so a block whose value scale lies more than
-// 2^10 below the reference is multiplied apart and added in f32.
+// 2^10 below the reference is multiplied apart and added in f32.  Causal rows keep
+// the value reference of the last block that they see: later ones may have far
+// larger values, or none (scale 255: NaN weights for the rows that see the block,
+// and its value codes are left out).
 // 48 requests of 500 to 12000 tokens, a row each, 32 heads over 8 of 128: 615 MB
 // in 100 us, 6.1 TB/s (a copy runs at 6.8).
 #include <math.h>
@@ -301,7 +304,8 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
   }
   least = __reduce_min_sync(0xffffffffu, least);
 
-  float o[C::MB][NR][4], m[NR][2], l[NR][2], ref = NO_REF;
+  // (the rows that see a block have seen all before it, so they share `ref`)
+  float o[C::MB][NR][4], m[NR][2], l[NR][2], ref = NO_REF, own_ref[NR][2];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
 #pragma unroll
@@ -310,6 +314,7 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
       for (int j = 0; j < 4; ++j) o[b][r][j] = 0.f;
     m[r][0] = m[r][1] = -INFINITY;
     l[r][0] = l[r][1] = 0.f;
+    own_ref[r][0] = own_ref[r][1] = NO_REF;
   }
   uint32_t phases = 0;  // a bit for each stage
   bool ok = true;
@@ -327,7 +332,8 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
     const int both = __shfl_sync(0xffffffffu, scales, i - base);
     if (both >= 0) {
       const int kb = both & 255, vb = both >> 8;
-      const float kf = scale_value(max(kb, vb) == 255 ? 255 : kb), bv = float(vb);
+      const float kf = scale_value(max(kb, vb) == 255 ? 255 : kb);
+      const float bv = vb == 255 ? ref : float(vb);
       const int key0 = (first + i * stride) * HALF;
       if (!mbar_sleep_warp(bar0 + 8 * st, (phases >> st) & 1, abort_flag)) { ok = false; break; }
       phases ^= 1u << st;
@@ -406,13 +412,17 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
             x = fmaxf(x, m[r][c]);
-            const float corr = x == -INFINITY ? 1.f : ex2_ftz(m[r][c] - x);
+            float corr = x == -INFINITY ? 1.f : ex2_ftz(m[r][c] - x);
             m[r][c] = x;
             l[r][c] *= corr;
+            if (seen[r][c] > key0) {
+              corr *= values;
+              own_ref[r][c] = ref;
+            }
 #pragma unroll
             for (int b = 0; b < C::MB; ++b) {
-              o[b][r][c] *= corr * values;
-              o[b][r][2 + c] *= corr * values;
+              o[b][r][c] *= corr;
+              o[b][r][2 + c] *= corr;
             }
           }
       }
@@ -441,7 +451,9 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
       }
       // ---- values
       const int left = len - key0;
-      if (!apart) {
+      if (vb == 255) {
+        // (0 times a NaN code would reach the rows that do not see it)
+      } else if (!apart) {
         add_values<DH, NR>(o, pf, ks + C::PART, g, t, left);
       } else {
         float x[C::MB][NR][4];
@@ -479,13 +491,13 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
 #pragma unroll
       for (int x = 4; x < 32; x *= 2) l[r][c] += __shfl_xor_sync(0xffffffffu, l[r][c], x);
   __syncthreads();
-  const float unit = ref > NO_REF ? scale_value(int(ref)) : 0.f;
   float* mine_at = reinterpret_cast<float*>(smem) + warp * C::ROWS * C::PSTRIDE;
 #pragma unroll
   for (int r = 0; r < NR; ++r)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       float* row = mine_at + (8 * r + 2 * t + c) * C::PSTRIDE;
+      const float unit = own_ref[r][c] > NO_REF ? scale_value(int(own_ref[r][c])) : 0.f;
       const int e = part_exponent(l[r][c]);
       const float down = __uint_as_float(uint32_t(127 - e) << 23);
 #pragma unroll

@@ -444,7 +444,10 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     // (a row that sees nothing here needs no maximum)
     const bool blind = seen <= block_of(0) * BKV;
     float m = blind ? 0.f : -INFINITY, l = 0.f;
-    float ref = NO_REF;  // exponent of the value scale that O is in units of
+    // Exponent of the value scale that O is in units of.  A row keeps that of the
+    // last block that it sees (`own_ref`): later ones may have far larger values, or
+    // none.  (Rows that see a block have seen all before it, so they share `ref`.)
+    float ref = NO_REF, own_ref = NO_REF;
     const int least = __reduce_min_sync(0xffffffffu, seen);  // what every row of the warp sees
     bool searching = __any_sync(0xffffffffu, m == -INFINITY);
 
@@ -489,7 +492,10 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
           const float to_max = raise_max ? top : m;
           float corr = to_max == -INFINITY ? 1.f : ex2_ftz(m - to_max);
           l *= corr;
-          if (raise_to != ref && ref > NO_REF) corr *= ex2_ftz(ref - raise_to);
+          if (seen > key0) {
+            if (raise_to != ref && ref > NO_REF) corr *= ex2_ftz(ref - raise_to);
+            own_ref = raise_to;
+          }
           m = to_max;
           ref = raise_to;
           if (g > 0) {
@@ -545,7 +551,7 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
     const bool alone = two && parts == 1;
     const int e = part_exponent(l);
     const float down = alone ? (l == 0.f ? 0.f : 1.f / l) : __uint_as_float(uint32_t(127 - e) << 23);
-    const float back = ref > NO_REF ? scale_value(int(ref)) : 0.f;
+    const float back = own_ref > NO_REF ? scale_value(int(own_ref)) : 0.f;
     const auto row_out = [&](int r) {
       const int qi = (row0 + r) / group, g = row0 + r - qi * group;
       return a.o + (long long)(q0 + qi) * a.ldo + (head * group + g) * DH;

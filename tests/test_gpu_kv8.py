@@ -640,6 +640,74 @@ def test_attention_block_without_value(lib, counts):
     R.rc_sync(ctx)
 
 
+def _causal_rows(c, got):
+    """Causal rows against what each one sees, and nothing else: (its first and last visible block
+    or None, result, definition, tolerance) of every row and query head."""
+    k = E.cache_values(c.pool.k, c.pool.k_scale)
+    v = E.cache_values(c.pool.v, c.pool.v_scale)
+    q, dh = c.q.double().cpu(), c.dh
+    for r, (l, n) in enumerate(zip(c.lens, c.counts)):
+        pages = c.table[r, :_blocks(l)].long()
+        for h in range(c.heads):
+            g = h // (c.heads // c.kvh)
+            kh, vh = k[pages, g].reshape(-1, dh), v[pages, g].reshape(-1, dh)
+            for i in range(n):
+                sees = max(0, l - n + i + 1)
+                row, cols = c.offsets[r] + i, slice(h * dh, (h + 1) * dh)
+                o, pv, reach = E.attention(q[row:row + 1, cols], kh[:sees], vh[:sees], False)
+                yield (r, sees, got[row:row + 1, cols], o,
+                       E.attention_tolerance(o, pv, reach, dh) if sees else None)
+
+
+# few rows of one CTA and of clusters, many rows of one CTA (one tile and two) and of clusters,
+# grouped heads, and requests whose first rows see nothing
+LATER = [([66], [4], 2, 2, 72), ([66], [70], 1, 1, 64), ([130], [16], 2, 1, 128),
+         ([20], [60], 1, 1, 72), ([5000], [13], 2, 2, 72), ([70, 200], [90, 160], 2, 2, 72),
+         ([200], [230], 1, 1, 128), ([1500], [200], 4, 2, 64), ([700], [150], 1, 1, 64),
+         ([100] * 40, [17, 45] * 20, 6, 6, 64)]
+
+
+@pytest.mark.parametrize("lens,counts,heads,kvh,dh", LATER)
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_attention_block_without_value_behind_causal_rows(lib, lens, counts, heads, kvh, dh, side):
+    """A block that is not finite reaches the rows that see one of its tokens, and no others: with
+    the codes that the store leaves there, and with any."""
+    R, ctx = lib
+    for codes in (False, True):
+        c = Case(R, lens, counts, heads, kvh, dh, 41)
+        scale, code = (c.pool.k_scale, c.pool.k) if side == "k" else (c.pool.v_scale, c.pool.v)
+        first = [_blocks(l) - 1 for l in lens]
+        for r, b in enumerate(first):
+            scale[c.table[r, b].item()] = 255
+            if codes:
+                code[c.table[r, b].item()] = 0x7f
+        rows = [0, 0]
+        for r, sees, got, o, tol in _causal_rows(c, c.run(R, ctx, True)):
+            if sees > first[r] * BLOCK:
+                assert bool(got.isnan().all())
+            elif sees == 0:
+                assert bool((got == 0).all())
+            else:
+                assert bool(((got - o).abs() <= tol).all()), (r, sees)
+            rows[sees > first[r] * BLOCK] += 1
+        assert min(rows) > 0
+    R.rc_sync(ctx)
+
+
+@pytest.mark.parametrize("lens,counts,heads,kvh,dh", LATER)
+def test_attention_value_scales_far_apart_behind_causal_rows(lib, lens, counts, heads, kvh, dh):
+    """Values of 2^128 times the earlier blocks' in a later one: lost beside them for the rows that
+    see both, and nothing to those that do not."""
+    R, ctx = lib
+    c = Case(R, lens, counts, heads, kvh, dh, 42)
+    c.pool.v_scale -= 20  # (95 .. 102)
+    for r, l in enumerate(lens):
+        c.pool.v_scale[c.table[r, _blocks(l) - 1].item()] = 230
+    for r, sees, got, o, tol in _causal_rows(c, c.run(R, ctx, True)):
+        assert bool((got == 0).all() if sees == 0 else ((got - o).abs() <= tol).all()), (r, sees)
+    R.rc_sync(ctx)
+
+
 @pytest.mark.parametrize("counts", [[2, 3, 1], [200, 130, 5]])
 def test_attention_leaves_out_and_reports_bad_requests(lib, counts):
     R, ctx = lib
