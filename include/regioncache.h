@@ -626,8 +626,10 @@ rc_status rc_kv8_store(rc_ctx* ctx, const rc_kv8* pool, const void* k, const voi
  *                of them.  Rows of no request are left as they were.
  *   lengths      i32 [n_requests], 0 .. ld_table * RC_KV8_BLOCK.
  *   table        i32 [n_requests][ld_table].
- * Keys are exact in the products; softmax weights and the result are rounded
- * to bf16, sums are f32.  Results are bit-identical from call to call.
+ * Keys are exact in the products; sums are f32, the result is rounded to bf16.
+ * Softmax weights are bf16 or finer: off by at most 2^-8 of themselves, or 2^-25
+ * of their row's largest.  Values more than 2^80 below the largest that a row sees
+ * may count as zero.  Results are bit-identical from call to call.
  * Device checks: a request with bad offsets, more than max_q rows or a bad
  * length is left out; a table entry outside the pool hides its tokens.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE (heads not a multiple of kv_heads,

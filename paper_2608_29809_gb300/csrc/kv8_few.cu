@@ -16,8 +16,11 @@
 // As in the kernel for many rows, a block's key scale joins the factor of its
 // scores and its value scale the exponent of its weights, both relative to
 // references that are raised (and O rescaled) only when the weights would
-// leave 2^12; weights are f16, so a block whose value scale lies more than
-// 2^10 below the reference is multiplied apart and added in f32.  Causal rows keep
+// leave 2^11.  Weights are f16, taken 2^4 up: to 2^15, and exact to 2^-9 of
+// themselves down to 2^-20 of that reference.  So that they stay there, a block
+// whose value scale lies more than 2^4 below its reference is multiplied apart and
+// added in f32: a weight is off by at most 2^-9 of itself or 2^-25 of its row's
+// largest.  Causal rows keep
 // the value reference of the last block that they see: later ones may have far
 // larger values, or none (scale 255: NaN weights for the rows that see the block,
 // and its value codes are left out).
@@ -43,7 +46,10 @@ constexpr int MAX_PARTS = 8;
 constexpr int WARPS_OF_TWO = 6;  // of a CTA, two an SM (twice as many of one alone)
 constexpr float NO_REF = -1e30f;
 // how far scores and value scales may pass their references, and fall below
-constexpr float RAISE = 8.f, RAISE_VALUE = 4.f, APART = -10.f;
+constexpr float RAISE = 8.f, RAISE_VALUE = 3.f, APART = -4.f;
+// weights' exponent beside that
+constexpr float WEIGHT_UP = 4.f, PRODUCT_DOWN = 1.f / 16.f;
+static_assert(RAISE + RAISE_VALUE + WEIGHT_UP <= 15.f, "f16");
 
 template <int DH, int NR, int W>
 struct FCfg {
@@ -429,7 +435,7 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
       // ---- weights: f16 (half a step is 2^-11 of a weight), transposed to B
       const float d = bv - ref;
       const bool apart = d < APART;
-      const float dv = apart ? 0.f : d, back = ex2_ftz(-dv);
+      const float dv = (apart ? 0.f : d) + WEIGHT_UP, back = ex2_ftz(-dv);
       uint32_t pf[2][NR][2];
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -500,14 +506,15 @@ few_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ Kv
       const float unit = own_ref[r][c] > NO_REF ? scale_value(int(own_ref[r][c])) : 0.f;
       const int e = part_exponent(l[r][c]);
       const float down = __uint_as_float(uint32_t(127 - e) << 23);
+      const float o_down = down * PRODUCT_DOWN;
 #pragma unroll
       for (int b = 0; b < C::MB; ++b) {
         if (DH == 72 && b == 4) {
-          row[64 + g] = o[b][r][c] * down * unit;
+          row[64 + g] = o[b][r][c] * o_down * unit;
         } else {  // channels 8 g + 2 (b % 4) and the next of a 64-channel part
           const int ch = 64 * (b >> 2) + 8 * g + 2 * (b & 3);
-          row[ch] = o[b][r][c] * down * unit;
-          row[ch + 1] = o[b][r][2 + c] * down * unit;
+          row[ch] = o[b][r][c] * o_down * unit;
+          row[ch + 1] = o[b][r][2 + c] * o_down * unit;
         }
       }
       if (g == 0) {

@@ -617,6 +617,45 @@ def test_attention_of_the_smallest_and_largest_values(lib, lens, counts, heads, 
     R.rc_sync(ctx)
 
 
+@pytest.mark.parametrize("tail", [15.5, 18.0, 21.0])
+@pytest.mark.parametrize("up", [0, 3, 4, 5, 10, 13])
+@pytest.mark.parametrize("count", [1, 5, 100])
+def test_attention_long_tail_of_small_weights(lib, tail, up, count):
+    """One key in 32 of the first 3200 outweighs all others but has no values; the next 3200 have
+    values of 2^up times the last ones', but no weight; the last 8192, all about 2^-tail of the first
+    ones, give the result.  No weight is off by more than 2^-8 of itself or 2^-25 of the largest."""
+    R, ctx = lib
+    head, length, dh = 3200, 2 * 3200 + 8192, 64
+    c = Case(R, [length], [count], 1, 1, dh, 44)
+    unit = tail * 8 / math.log2(math.e)  # a key of -1 has the score -tail, in base 2
+    c.q.zero_()
+    c.q[:, 0] = unit
+    key = torch.full((length,), -16.0)
+    key[:head:32] = 0.0
+    key[2 * head:] = -1.0
+    value = (_rand(length, dh, seed=45).abs().clamp(max=3.0).cpu() + 1.0) * 100
+    value[:head:32] = 0.0
+    codes = torch.zeros(length, dh)
+    codes[:, 0] = key
+    pages = c.table[0].long().cuda()
+    c.pool.k[pages, 0] = codes.view(-1, 64, dh).to(E.F8).view(torch.uint8).cuda()
+    c.pool.v[pages, 0] = value.view(-1, 64, dh).to(E.F8).view(torch.uint8).cuda()
+    c.pool.k_scale.fill_(127)
+    c.pool.v_scale.fill_(120)
+    c.pool.v_scale[pages[head // 64:2 * head // 64]] = 120 + up
+    got = c.run(R, ctx, False)
+    k = E.cache_values(c.pool.k, c.pool.k_scale)[pages.cpu(), 0].reshape(-1, dh)
+    v = E.cache_values(c.pool.v, c.pool.v_scale)[pages.cpu(), 0].reshape(-1, dh)
+    o, pv, reach = E.attention(c.q[:count, :dh].double().cpu(), k, v, False)
+    largest = 1 / (head // 32)  # (a little more than the largest weight)
+    # weights of zero are exact; the block of no weight has no part in the bound
+    small = 2.0 ** -25 * largest * v[2 * head:].abs().sum(0)
+    tol = E.attention_tolerance(o, pv, reach, dh) + small
+    err = (got - o).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+    R.rc_sync(ctx)
+
+
 @pytest.mark.parametrize("counts", [[1, 1], [3, 150]])
 def test_attention_block_without_value(lib, counts):
     """NaN blocks reach the rows that see them and no others; behind the last token and in
