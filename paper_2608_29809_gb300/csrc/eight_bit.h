@@ -1,5 +1,6 @@
 // Internal launchers of eight-bit serving (rc_fp8_*, rc_kv8_*).  Every launcher
-// queues one kernel on `st` and returns the cudaError_t of the launch.
+// queues one kernel on `st` (the attention two, for batches of many short and a few
+// long requests) and returns the cudaError_t of the launch.
 #pragma once
 #include "kernels.h"
 

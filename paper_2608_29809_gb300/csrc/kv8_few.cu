@@ -28,11 +28,10 @@
 // in 100 us, 6.1 TB/s (a copy runs at 6.8).
 #include <math.h>
 
-#include <atomic>
-
 #include "common.cuh"
 #include "eight_bit.h"
 #include "fp8.cuh"
+#include "per_device.h"
 #include "tc_eight_bit.cuh"
 
 namespace rc {
@@ -590,32 +589,38 @@ cudaError_t launch(const Kv8Pool& pool, const Kv8AttnArgs& a, long long chunks, 
                           pool, a, int(parts), longest_first ? 1 : 0);
 }
 
-// How many clusters of `parts` CTAs of W warps the GPU holds at once (found out
-// at the first call; 0 where that fails).
+// How many clusters of `parts` CTAs of W warps the current device holds at once
+// (found out at the first call; -1 where that fails).
 template <int DH, int NR, int W>
 int clusters_at_once(int parts) {
-  static std::atomic<int> known[MAX_PARTS + 1];
-  int n = known[parts].load(std::memory_order_relaxed) - 1;
-  if (n >= 0) return n;
-  using C = FCfg<DH, NR, W>;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = unsigned(parts);
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(parts));
-  cfg.blockDim = dim3(W * 32);
-  cfg.dynamicSmemBytes = C::SMEM;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaFuncSetAttribute(few_rows_kernel<DH, NR, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           int(C::SMEM)) != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, few_rows_kernel<DH, NR, W>, &cfg) != cudaSuccess) {
+  static PerDevice<MAX_PARTS + 1> known;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
     cudaGetLastError();
-    n = 0;
+    return -1;
   }
-  known[parts].store(n + 1, std::memory_order_relaxed);
-  return n;
+  return known.get(dev, parts, [&] {
+    using C = FCfg<DH, NR, W>;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(parts);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(parts));
+    cfg.blockDim = dim3(W * 32);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = -1;
+    if (cudaFuncSetAttribute(few_rows_kernel<DH, NR, W>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             int(C::SMEM)) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, few_rows_kernel<DH, NR, W>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return -1;
+    }
+    return n;
+  });
 }
 
 template <int DH, int NR>

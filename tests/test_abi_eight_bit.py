@@ -41,6 +41,43 @@ def test_structures_match_the_header(R):
     assert (R.RC_BF16, R.RC_F32, R.RC_KV8_BLOCK) == (0, 1, 64)
 
 
+def test_answers_of_devices_are_kept_apart():
+    """What one device answered is no other's answer, and a failure is not kept."""
+    source = r"""
+#include <stdio.h>
+#include "per_device.h"
+static rc::PerDevice<9> known;
+static int asked = 0;
+static void show(int device, int kind, int answer) {
+  printf("%d ", known.get(device, kind, [&] { ++asked; return answer; }));
+}
+int main() {
+  show(0, 8, -1);  // fails: asked again
+  show(0, 8, 19);
+  show(0, 8, 5);   // kept
+  show(1, 8, 12);  // another device's
+  show(1, 8, 7);
+  show(0, 7, 0);   // another question's (0 is an answer)
+  show(0, 7, 3);
+  show(-1, 8, 4);  // devices beyond those kept
+  show(64, 8, 6);
+  show(0, 8, 1);
+  show(63, 0, 2);
+  printf("%d\n", asked);
+  return 0;
+}
+"""
+    with tempfile.TemporaryDirectory(dir=os.path.join(ROOT, "tests")) as tmp:
+        src, exe = os.path.join(tmp, "d.cpp"), os.path.join(tmp, "d")
+        with open(src, "w") as f:
+            f.write(source)
+        subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I",
+                        os.path.join(ROOT, "paper_2608_29809_gb300", "csrc"), src, "-o", exe],
+                       check=True)
+        out = subprocess.run([exe], check=True, capture_output=True, text=True).stdout.split()
+    assert [int(v) for v in out] == [-1, 19, 19, 12, 12, 0, 0, 4, 6, 19, 2, 7]
+
+
 def test_wrappers(R):
     m = R.Fp8Matrix(130, 300, 128, device="cpu")
     assert m.codes.shape == (130, 304) and m.scales.shape == (3, 2)
