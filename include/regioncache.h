@@ -626,6 +626,8 @@ rc_status rc_kv8_store(rc_ctx* ctx, const rc_kv8* pool, const void* k, const voi
  *                of them.  Rows of no request are left as they were.
  *   lengths      i32 [n_requests], 0 .. ld_table * RC_KV8_BLOCK.
  *   table        i32 [n_requests][ld_table].
+ * The work is shared out on the host, for requests as long as the table holds
+ * and max_q rows at most: values far above the requests' cost time, not results.
  * Keys are exact in the products; sums are f32, the result is rounded to bf16.
  * Softmax weights are bf16 or finer: off by at most 2^-8 of themselves, or 2^-25
  * of their row's largest.  Values more than 2^80 below the largest that a row sees

@@ -13,8 +13,9 @@
 // hand-over is what must be rare: with one for every block, and bytes loaded
 // where they were needed, 16384 x 1152 x 4608 took 301 us; with one for every
 // four, and loads a batch ahead, 82; now 66 with f32 results (2.6 PFLOP/s, 2.9 at
-// 60 with bf16; TMA brings about 70 bytes a clock to an SM and bounds it).  Two
-// accumulators of up to 192 columns (or one of up to 256, where a CTA has one
+// 60 with bf16).  What is left there: 384 tiles of 256 x 192 on 76 pairs are 5.05
+// rounds and take six, and a pair's block of columns takes 486 cycles, of which
+// its MMAs fill 384.  Two accumulators of up to 192 columns (or one of up to 256, where a CTA has one
 // tile) and two batches of scale words fill the 512 columns of tensor memory.
 #include "common.cuh"
 #include "eight_bit.h"

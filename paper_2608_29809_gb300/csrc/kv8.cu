@@ -165,8 +165,9 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
 // warps, so no two of them may have rows of one block.  (A run that does not fit
 // the registers is read again, from L2.)  With CTAs of four
 // heads that met at barriers, 4 x 831 rows of 16 heads of 72 took 23.9 us, now
-// 10.1 (latency: a run's rows, their largest magnitude, its codes); eight fills of
-// 4096 tokens, 226 MB, 37 (6.1 TB/s).
+// 10.0 (latency: a run's rows, their largest magnitude, its codes); eight fills of
+// 4096 tokens, 226 MB, 36 (6.2 TB/s).  (Heads of 72 spill up to 24 bytes at 72
+// registers, the least that the compiler chooses.)
 constexpr int ST_WARPS = 4, ST_CHUNK = 24;
 
 template <class T, int DH, bool WIDE>

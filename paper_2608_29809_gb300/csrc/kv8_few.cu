@@ -25,7 +25,8 @@
 // larger values, or none (scale 255: NaN weights for the rows that see the block,
 // and its value codes are left out).
 // 48 requests of 500 to 12000 tokens, a row each, 32 heads over 8 of 128: 615 MB
-// in 100 us, 6.1 TB/s (a copy runs at 6.8).
+// in 101 us, 6.1 TB/s (a copy runs at 6.8).  Sixteen rows of 128 channels want more
+// than the 168 registers that two CTAs an SM leave a thread (72 bytes spilled).
 #include <math.h>
 
 #include "common.cuh"
@@ -637,7 +638,9 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   // CTA's 5 us of start and end count little (16 heads of 72: 8 requests of 4096
   // tokens, one part 23.5 us, two 19.2, three 26.1; 16: one 29.3, two 36.3, but of
   // 500 to 9000 tokens one 54.7, two 35.9, three 41.6; 64 of 100 to 8000: one 96,
-  // two 116.  48 of 500 to 12000, 8 key heads of 128: one 117, two 100.9, three 113)
+  // two 116.  48 of 500 to 12000, 8 key heads of 128: one 117, two 101, three 113).
+  // The longest length is what the table holds: 8 requests of 500 tokens take 6.6
+  // us with a table of that width and 14.7 with one of 16384 tokens.
   const long long halves = (long long)a.ld_table * (KV8_BLOCK / HALF);
   long long parts = 2 * SMS / units, more = halves / (16 * WARPS);
   if (more > (600 + units / 2) / units) more = (600 + units / 2) / units;
@@ -648,8 +651,8 @@ cudaError_t few(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   if (parts < 1) parts = 1;
   // Where there are few units and much to read, CTAs of twice the warps, one an SM,
   // as many of them a unit as still find a place all at once (16 heads of 72,
-  // one row: 4096 tokens 7.1 us with six warps, 6.5 with twelve; 40000: 32.7 and
-  // 25.0; clusters that wait for others take twice as long)
+  // one row: 4096 tokens 7.1 us with six warps, 6.7 with twelve; 40000: 32.7 and
+  // 25.4; clusters that wait for others take twice as long)
   if (units <= 30 && halves > MAX_PARTS * WARPS)
     for (int p = MAX_PARTS; p >= 5; --p)
       if (units <= clusters_at_once<DH, NR, 2 * WARPS>(p))

@@ -26,8 +26,8 @@
 // same reference unless their weights' sum passes 2^20 (or a value scale passes
 // 2^5 of its reference); then it is raised, O rescaled, the block done again.
 // 8 requests of 4096 tokens, 201 to 831 rows, 16 heads of 72: 123 us, 627 TFLOP/s,
-// the tensor pipe busy 38 % of the time; 4 of 512 rows, 32 heads over 8 of 128: 141
-// us, 913 TFLOP/s.  Softmax and conversion fill half the issue slots: it is
+// the tensor pipe busy 38 % of the time; 4 of 512 rows, 32 heads over 8 of 128: 142
+// us, 905 TFLOP/s.  Softmax and conversion fill half the issue slots: it is
 // their chain with the products, page by page, that bounds it.
 #include <math.h>
 
@@ -805,14 +805,16 @@ many_rows_kernel(const __grid_constant__ Kv8Pool pool, const __grid_constant__ K
 constexpr int SMS = 152;
 
 // Rows of a unit and CTAs that share its keys, of least estimated time (us) for
-// requests of the mean number of rows and the longest possible length; where there
-// are several, the mean of that and of the time for lengths spread evenly, the
-// longest units first (8 requests of 256 rows, 16 heads of 72: of 500 to 12000
-// tokens one part 138 us, two 88; of 12000 each 142 and 154).  Rates measured at 4096 keys, head_dim 72, 16 heads: a key block takes a unit of 256
-// rows 1.45 us and one of 128 1.1, a unit 4.5 beyond that, and joining parts 5
-// (2.5) and 0.65 for each (256 rows: one part 52.8 us, six 22.2; 831: two 35.3,
-// one 54.0; 4096: one 106, two 132).  Clusters above six CTAs do not all find a
-// place at once.
+// requests of the mean number of rows and the longest length that the table holds
+// (8 requests of 500 tokens, 256 rows: 17 us with a table of that width, 33 with one
+// of 16384 tokens).  Where there are several requests, the mean of that and of the
+// time for lengths spread evenly, the longest units first (8 requests of 256 rows,
+// 16 heads of 72: of 500 to 12000 tokens one part 140 us, two 89; of 12000 each 141
+// and 157).  Rates measured at 4096 keys, head_dim 72, 16 heads: a key block takes a
+// unit of 256 rows 1.45 us and one of 128 1.1, a unit 4.5 beyond that, and joining
+// parts 5 (2.5) and 0.65 for each (256 rows: one part 52.8 us, six 22.2; 831: two
+// 35.3, one 54.0; 4096: one 106, two 132).  Clusters above six CTAs do not all find
+// a place at once.
 struct Shape {
   int unit_rows, parts;
 };
@@ -857,9 +859,9 @@ cudaError_t many(const Kv8Pool& pool, const Kv8AttnArgs& a, cudaStream_t st) {
   // kernel counts out the units that there are where places for every chunk of
   // every request would be more than twice as many (a place without one costs a
   // CTA's launch, the counting every CTA 1.2 us).  16 requests of 500 to 9000
-  // tokens and 100 to 400 rows: 147 us, in place 180; 32 of 500 to 8000, 40 to 200
-  // rows, 4 heads a key head of 128: 317 and 390; 8 of 4096, 201 to 831 rows: 123
-  // and 125; 4 of 4096, 512 rows each, 4 heads of 128: 141 and 136.
+  // tokens and 100 to 400 rows: 146 us, in place 180; 32 of 500 to 8000, 40 to 200
+  // rows, 4 heads a key head of 128: 320 and 390; 8 of 4096, 201 to 831 rows: 123
+  // and 125; 4 of 4096, 512 rows each, 4 heads of 128: 142 and 136.
   const long long most = (long long)a.n * a.max_q, rows = most < a.q_rows ? most : a.q_rows;
   const long long all = ((long long)a.max_q * group + unit_rows - 1) / unit_rows * a.n;
   long long units = rows * group / unit_rows + a.n;
