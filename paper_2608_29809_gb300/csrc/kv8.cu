@@ -165,13 +165,14 @@ tables_kernel(const __grid_constant__ Kv8TablesArgs a, int rows_per_cta) {
 // warps, so no two of them may have rows of one block.  (A run that does not fit
 // the registers is read again, from L2.)  With CTAs of four
 // heads that met at barriers, 4 x 831 rows of 16 heads of 72 took 23.9 us, now
-// 10.0 (latency: a run's rows, their largest magnitude, its codes); eight fills of
-// 4096 tokens, 226 MB, 36 (6.2 TB/s).  (Heads of 72 spill up to 24 bytes at 72
-// registers, the least that the compiler chooses.)
-constexpr int ST_WARPS = 4, ST_CHUNK = 24;
+// 9.5 (latency: a run's rows, their largest magnitude, its codes); eight fills of
+// 4096 tokens, 226 MB, 36.8 (6.1 TB/s).  Six CTAs an SM leave a thread 80 registers
+// and nothing is spilled (the compiler's own choice of 64 to 80 spilled up to 24
+// bytes: heads of 64 8.4 us, with 80 7.7; five CTAs: the fills 41.1).
+constexpr int ST_WARPS = 4, ST_CHUNK = 24, ST_CTAS = 6;
 
 template <class T, int DH, bool WIDE>
-__global__ void __launch_bounds__(32 * ST_WARPS)
+__global__ void __launch_bounds__(32 * ST_WARPS, ST_CTAS)
 store_kernel(const __grid_constant__ Kv8Pool pool, const T* __restrict__ kx,
              const T* __restrict__ vx, int ldx, const int* __restrict__ slots, int n_bound,
              const int* __restrict__ count, int append, int chunk, unsigned* __restrict__ err) {
