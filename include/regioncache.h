@@ -641,6 +641,147 @@ rc_status rc_kv8_attention(rc_ctx* ctx, const rc_kv8* pool, const void* Q, int l
                            int max_q, const int32_t* table, int ld_table, int heads, int causal,
                            void* O, int ldo, rc_stream stream);
 
+/* --------------------------------------------------- the rest of a block */
+
+/* What a transformer block needs between its quantised products and the
+ * eight-bit cache (no counterpart in the paper; serving plumbing): norms with
+ * gate and residual, and rotary positions.  As above:
+ * the context serves for its error word and device only, nothing is allocated
+ * or kept, calls on different streams may overlap as long as their buffers do
+ * not, and all calls but rc_rotary_plan (host code) may be captured.  Results
+ * are bit-identical from call to call. */
+
+/* A norm over the columns of a row: RC_NORM_LAYER (v - mean) / sqrt(var + eps),
+ * RC_NORM_RMS v / sqrt(mean of v^2 + eps), RC_NORM_NONE v itself; then times
+ * weight and plus bias (f32 [cols], each null for none; not with RC_NORM_NONE).
+ * Sums are f32, the variance is that of the differences from the mean.
+ * eps >= 0. */
+#define RC_NORM_NONE 0
+#define RC_NORM_LAYER 1
+#define RC_NORM_RMS 2
+typedef struct rc_norm {
+  int kind;
+  float eps;
+  const float* weight;
+  const float* bias;
+} rc_norm;
+
+/* The row work between two products, in one pass: for each row
+ *   r  = post(b)            b: the row of h, or with top_k > 0 the sum over j of
+ *                           weights[row][j] * h[places[row][j]]
+ *   x' = residual_scale * x + gate * r
+ *   y  = pre(x') * (1 + scale) + shift
+ * all in f32, rounded once where x' and y are written (y is made of x' before
+ * its rounding).
+ *   rows, cols   cols 1 .. RC_NORM_MAX_COLS.
+ *   x            x_type (RC_BF16, RC_F32) [rows][ldx], or null for zeros.
+ *   x_out        x_type [rows][ldx_out], may be x itself, or null: not written.
+ *   h            h_type [rows][ldh] ([h_rows][ldh] with top_k > 0), or null: no
+ *                branch, x' = residual_scale * x.
+ *   places, weights  i32, f32 [rows][top_k], top_k 0 .. RC_EXPERTS_MAX_TOP_K; an
+ *                entry below 0 is passed over, and so is its weight.
+ *   gate, scale, shift  f32 [n_items][ld_mod], each null for 1, 0 and 0.
+ *   row_offsets  i32 [n_items + 1] on the device: item i owns rows
+ *                row_offsets[i] .. row_offsets[i + 1] - 1.  Rows of no item are
+ *                left as they were.  Null with n_items = 1: all rows.
+ *   y            y_type [rows][ldy], or null.
+ *   y8           y as codes instead (then y is null): rows x cols or more rows,
+ *                group 1; codes and scales as rc_fp8_quantize gives them for the
+ *                f32 values.  null: none.
+ * One of x_out, y and y8 at least.  Buffers overlap only where x_out is x with
+ * the same stride.  Pointers are aligned to their types (rows of 16-B aligned
+ * pieces are read and written faster).
+ * Device checks: row_offsets that descend or leave 0 .. rows (rows near them may
+ * be left out) and a place of h_rows and more (passed over) are reported.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_NORM_MAX_COLS 16384
+#define RC_EXPERTS_MAX_TOP_K 16
+typedef struct rc_residual {
+  int rows, cols, n_items, top_k;
+  const int32_t* row_offsets;
+  const void* x;
+  void* x_out;
+  const void* h;
+  const int32_t* places;
+  const float* weights;
+  const float* gate;
+  const float* scale;
+  const float* shift;
+  void* y;
+  const rc_fp8* y8;
+  int x_type, ldx, ldx_out, h_type, ldh, h_rows, ld_mod, y_type, ldy;
+  float residual_scale;
+  rc_norm post, pre;
+} rc_residual;
+rc_status rc_norm_residual(rc_ctx* ctx, const rc_residual* op, rc_stream stream);
+
+/* Rotary positions.  A head's channels first .. first + rot - 1 form rot / 2
+ * pairs, each turned by its row's position times the pair's frequency:
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin).
+ * RC_ROTARY_HALF pairs channel i with i + rot / 2, RC_ROTARY_PAIRS 2 i with
+ * 2 i + 1.  Up to three axes (a token's place in text, or in an image's rows
+ * and columns) take pairs[a] pairs each, one after another; axis a's position
+ * is positions[row][a].
+ *
+ * rc_rotary_plan (host code, no context) fills a plan from its description:
+ *   rot        2 .. 256, even; pairs[0 .. axes - 1] positive, summing to rot / 2.
+ *   theta      > 0.  Pair i of an axis with p pairs turns f = theta^(-i / p)
+ *              radians a position, changed by `scaling` for contexts `factor`
+ *              (>= 1) times as long as the native_length the model was made for:
+ *     RC_ROTARY_PLAIN   f;
+ *     RC_ROTARY_LINEAR  f / factor;
+ *     RC_ROTARY_BASE    theta taken times factor^(p / (p - 1)) (p > 1);
+ *     RC_ROTARY_BANDS   k f + (1 - k) f / factor with k = (native_length f / 2 pi -
+ *                       slow) / (fast - slow), cut to 0 .. 1: pairs that turn often
+ *                       stay, slow ones are stretched;
+ *     RC_ROTARY_RAMP    the same with k = 1 - (i - lo) / (hi - lo), cut to 0 .. 1,
+ *                       where lo (rounded down, at least 0) and hi (up, at most
+ *                       p - 1) are the indexes of pairs that turn fast and slow times, and hi - lo
+ *                       counts as 0.001 at least; theta > 1.
+ *              fast > slow > 0 (in turns over native_length > 0) for the last two.
+ *   amplitude  finite.
+ * A plan holds a pair's turns a position as a fraction of 2^64: a position
+ * times it, modulo 2^64, is the exact place within the turn, so far positions
+ * lose nothing to range reduction.  A caller may fill turns itself.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_ROTARY_HALF 0
+#define RC_ROTARY_PAIRS 1
+#define RC_ROTARY_PLAIN 0
+#define RC_ROTARY_LINEAR 1
+#define RC_ROTARY_BASE 2
+#define RC_ROTARY_BANDS 3
+#define RC_ROTARY_RAMP 4
+#define RC_ROTARY_MAX 256
+typedef struct rc_rotary_spec {
+  int rot, first, layout, axes, pairs[3], scaling;
+  double theta, factor, native_length, fast, slow, amplitude;
+} rc_rotary_spec;
+typedef struct rc_rotary {
+  int rot, first, layout, axes, pairs[3];
+  float amplitude;
+  uint64_t turns[RC_ROTARY_MAX / 2];
+} rc_rotary;
+rc_status rc_rotary_plan(const rc_rotary_spec* spec, rc_rotary* out);
+
+/* y = x with its heads' pairs turned.
+ *   x, y       `type` (RC_BF16, RC_F32) [rows][ldx], [rows][ldy], head h in
+ *              columns h * head_dim ..; y may be x itself with the same stride
+ *              (no other overlap): the channels outside first .. first + rot - 1
+ *              are then left alone, otherwise copied.  Query and key heads that
+ *              lie side by side are turned in one call.  rows and heads >= 0;
+ *              head_dim up to RC_ROTARY_MAX_HEAD; pointers aligned to the type
+ *              (more makes wider accesses).
+ *   positions  i32 [rows][axes], any value; null: the row's index, on all axes.
+ *   count      i32 on the device: the rows to turn (null: rows), 0 .. rows; the
+ *              rest are left as they were.
+ *   inverse    != 0: turned back (the transposed map: also the gradient).
+ * Device checks: a count out of range is reported and taken as 0.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_ROTARY_MAX_HEAD 1024
+rc_status rc_rotary_apply(rc_ctx* ctx, const rc_rotary* plan, const void* x, int ldx, int type,
+                          int rows, int heads, int head_dim, const int32_t* positions,
+                          const int32_t* count, int inverse, void* y, int ldy, rc_stream stream);
+
 /* Waits for `stream`, then reports (and clears) the context's device error
  * word: RC_ERR_DEVICE_ASSERT if a kernel met a bad index or count,
  * RC_ERR_TIMEOUT if a bounded wait gave up, RC_ERR_CUDA on a CUDA error. */

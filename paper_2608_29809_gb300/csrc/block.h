@@ -1,0 +1,46 @@
+// Internal launchers of a block's row work and rotary positions
+// (rc_norm_residual, rc_rotary_*).  Every launcher queues one
+// kernel on `st` and returns the cudaError_t of the launch.
+#pragma once
+#include "../../include/regioncache.h"
+#include "eight_bit.h"
+
+namespace rc {
+
+struct NormOf {
+  int kind;  // RC_NORM_*
+  float eps;
+  const float *weight, *bias;
+};
+// As rc_residual; y8.codes null for none.
+struct ResidualArgs {
+  int rows, cols, n_items, top_k;
+  const int* row_offsets;
+  const void* x;
+  void* x_out;
+  const void* h;
+  const int* places;
+  const float *weights, *gate, *scale, *shift;
+  void* y;
+  Fp8Mat y8;
+  bool x_f32, h_f32, y_f32;
+  int ldx, ldx_out, ldh, h_rows, ld_mod, ldy;
+  float residual_scale;
+  NormOf post, pre;
+  unsigned* err;
+};
+cudaError_t launch_norm_residual(const ResidualArgs& a, cudaStream_t st);
+
+struct RotaryArgs {
+  ::rc_rotary plan;
+  const void* x;
+  void* y;
+  int ldx, ldy, rows, heads, head_dim;
+  bool f32;
+  const int *positions, *count;
+  int inverse, per;  // per: rows of a CTA, set by the launcher
+  unsigned* err;
+};
+cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st);
+
+}  // namespace rc

@@ -1,0 +1,154 @@
+// Rotary positions (rc_rotary_plan, rc_rotary_apply).
+#include <math.h>
+
+#include "../../include/regioncache.h"
+#include "block.h"
+#include "common.cuh"
+
+namespace rc {
+
+namespace {
+
+// cos and sin of a place within the turn (a fraction of 2^64).  The nearest
+// quarter turn comes off in integers, so nothing is lost; on what is left, at
+// most an eighth of a turn, the Taylor series up to the 10th (cos) and 9th
+// degree (sin): the next terms are below 2^-33 and 2^-29 of the result.
+__device__ __forceinline__ float2 cos_sin(uint64_t place) {
+  const uint32_t quarter = uint32_t((place + (uint64_t(1) << 61)) >> 62) & 3u;
+  const long long rest = (long long)(place - (uint64_t(quarter) << 62));
+  const float t = float(rest) * (6.283185307179586f * 5.421010862427522e-20f);  // 2 pi 2^-64
+  const float s = t * t;
+  float c = fmaf(s, -1.f / 3628800.f, 1.f / 40320.f);
+  c = fmaf(c, s, -1.f / 720.f);
+  c = fmaf(c, s, 1.f / 24.f);
+  c = fmaf(c, s, -0.5f);
+  c = fmaf(c, s, 1.f);
+  float n = fmaf(s, 1.f / 362880.f, -1.f / 5040.f);
+  n = fmaf(n, s, 1.f / 120.f);
+  n = fmaf(n, s, -1.f / 6.f);
+  n = fmaf(n * s, t, t);
+  const float a = quarter & 1 ? n : c, b = quarter & 1 ? c : n;
+  return make_float2(quarter == 1 || quarter == 2 ? -a : a, quarter >= 2 ? -b : b);
+}
+
+template <class T, int W>
+struct alignas(sizeof(T) * W) Some {
+  T v[W];
+};
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(bf16 v) { return bf2f(v); }
+__device__ __forceinline__ void put(float& to, float v) { to = v; }
+__device__ __forceinline__ void put(bf16& to, float v) { to = f2bf(v); }
+
+// A CTA turns `per` rows: the cosines and sines of their pairs (the same for all
+// heads) go to shared memory, then the threads take the rows' units.  In a head,
+// units 0 .. pair_units - 1 are W pairs each (HALF: W channels and the W that are
+// rot / 2 further; PAIRS: 2 W neighbours), the others W channels that are only
+// copied.
+template <class T, int W, bool HALF>
+__global__ void __launch_bounds__(256)
+rotary_kernel(const __grid_constant__ RotaryArgs a) {
+  extern __shared__ float2 turns[];
+  pdl_wait();
+  pdl_trigger();
+  const int half = a.plan.rot / 2;
+  const int rows = a.count ? live_count(a.count, a.rows, blockIdx.x == 0 && threadIdx.x == 0
+                                                             ? a.err : nullptr) : a.rows;
+  const long long row0 = (long long)blockIdx.x * a.per;
+  const int here = int(min((long long)a.per, rows - row0));
+  if (here <= 0) return;
+  for (int i = threadIdx.x; i < here * half; i += blockDim.x) {
+    const int r = i / half, p = i - r * half;
+    const int axis = (p >= a.plan.pairs[0]) + (p >= a.plan.pairs[0] + a.plan.pairs[1]);
+    const long long at = a.positions
+                             ? (long long)a.positions[(row0 + r) * a.plan.axes + axis]
+                             : row0 + r;
+    const float2 cs = cos_sin(uint64_t(at) * a.plan.turns[p]);
+    turns[i] = make_float2(a.plan.amplitude * cs.x,
+                           a.inverse ? -a.plan.amplitude * cs.y : a.plan.amplitude * cs.y);
+  }
+  __syncthreads();
+
+  const int pair_units = half / W, rest = a.y == a.x ? 0 : (a.head_dim - a.plan.rot) / W;
+  const int units = pair_units + rest, first = a.plan.first;
+  const T* x = static_cast<const T*>(a.x);
+  T* y = static_cast<T*>(a.y);
+  for (int i = threadIdx.x; i < here * a.heads * units; i += blockDim.x) {
+    const int r = i / (a.heads * units), j = i - r * a.heads * units;
+    const int head = j / units, u = j - head * units;
+    const T* from = x + (row0 + r) * a.ldx + (long long)head * a.head_dim;
+    T* to = y + (row0 + r) * a.ldy + (long long)head * a.head_dim;
+    if (u >= pair_units) {
+      int c = (u - pair_units) * W;
+      if (c >= first) c += a.plan.rot;
+      *reinterpret_cast<Some<T, W>*>(to + c) = *reinterpret_cast<const Some<T, W>*>(from + c);
+      continue;
+    }
+    const float2* cs = turns + r * half + u * W;
+    if (HALF) {
+      const int c = first + u * W;
+      Some<T, W> p = *reinterpret_cast<const Some<T, W>*>(from + c);
+      Some<T, W> q = *reinterpret_cast<const Some<T, W>*>(from + c + half);
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const float va = value(p.v[k]), vb = value(q.v[k]);
+        put(p.v[k], va * cs[k].x - vb * cs[k].y);
+        put(q.v[k], vb * cs[k].x + va * cs[k].y);
+      }
+      *reinterpret_cast<Some<T, W>*>(to + c) = p;
+      *reinterpret_cast<Some<T, W>*>(to + c + half) = q;
+    } else {
+      const int c = first + 2 * u * W;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {  // (W channels at a time)
+        Some<T, W> p = *reinterpret_cast<const Some<T, W>*>(from + c + k * W);
+        if (W > 1) {
+#pragma unroll
+          for (int m = 0; m + 1 < W; m += 2) {
+            const float2 t = cs[(k * W + m) / 2];
+            const float va = value(p.v[m]), vb = value(p.v[m + 1]);
+            put(p.v[m], va * t.x - vb * t.y);
+            put(p.v[m + 1], vb * t.x + va * t.y);
+          }
+          *reinterpret_cast<Some<T, W>*>(to + c + k * W) = p;
+        } else if (k == 0) {
+          const float va = value(p.v[0]), vb = value(from[c + 1]);
+          put(to[c], va * cs[0].x - vb * cs[0].y);
+          put(to[c + 1], vb * cs[0].x + va * cs[0].y);
+        }
+      }
+    }
+  }
+}
+
+template <class T, int W>
+cudaError_t go(const RotaryArgs& a, cudaStream_t st) {
+  const int half = a.plan.rot / 2;
+  const size_t smem = size_t(a.per) * half * sizeof(float2);
+  const dim3 grid(unsigned((a.rows + (long long)a.per - 1) / a.per));
+  count_launches(1);
+  if (a.plan.layout == RC_ROTARY_HALF)
+    return launch_k(rotary_kernel<T, W, true>, grid, dim3(256), smem, st, a);
+  return launch_k(rotary_kernel<T, W, false>, grid, dim3(256), smem, st, a);
+}
+
+template <class T>
+cudaError_t widest(RotaryArgs a, cudaStream_t st) {
+  // channels a thread moves at once: what divides every offset in a row, up to 16 B
+  uintptr_t all = (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y)) / sizeof(T);
+  all |= uintptr_t(a.ldx) | uintptr_t(a.ldy) | uintptr_t(a.head_dim) | uintptr_t(a.plan.first) |
+         uintptr_t(a.plan.rot / 2);
+  const int units = a.heads * a.head_dim * int(sizeof(T)) / 32;
+  a.per = units >= 1024 ? 1 : units < 64 ? 16 : (1024 + units - 1) / units;
+  if (sizeof(T) == 2 && all % 8 == 0) return go<T, 8>(a, st);
+  if (all % 4 == 0) return go<T, 4>(a, st);
+  return go<T, 1>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st) {
+  return a.f32 ? widest<float>(a, st) : widest<bf16>(a, st);
+}
+
+}  // namespace rc

@@ -76,6 +76,44 @@ RC_KV8_MAX_REQUESTS = header_define("RC_KV8_MAX_REQUESTS")
 RC_KV8_UPDATE, RC_KV8_APPEND = header_define("RC_KV8_UPDATE"), header_define("RC_KV8_APPEND")
 
 
+class rc_norm(C.Structure):
+    _fields_ = [("kind", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p),
+                ("bias", C.c_void_p)]
+
+
+class rc_residual(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rows", "cols", "n_items", "top_k")] + [
+        (n, C.c_void_p) for n in ("row_offsets", "x", "x_out", "h", "places", "weights", "gate",
+                                  "scale", "shift", "y")] + [("y8", C.POINTER(rc_fp8))] + [
+        (n, C.c_int) for n in ("x_type", "ldx", "ldx_out", "h_type", "ldh", "h_rows", "ld_mod",
+                               "y_type", "ldy")] + [
+        ("residual_scale", C.c_float), ("post", rc_norm), ("pre", rc_norm)]
+
+
+RC_NORM_NONE, RC_NORM_LAYER, RC_NORM_RMS = (
+    header_define("RC_NORM_" + n) for n in ("NONE", "LAYER", "RMS"))
+RC_NORM_MAX_COLS = header_define("RC_NORM_MAX_COLS")
+RC_EXPERTS_MAX_TOP_K = header_define("RC_EXPERTS_MAX_TOP_K")
+RC_ROTARY_HALF, RC_ROTARY_PAIRS = header_define("RC_ROTARY_HALF"), header_define("RC_ROTARY_PAIRS")
+RC_ROTARY_PLAIN, RC_ROTARY_LINEAR, RC_ROTARY_BASE, RC_ROTARY_BANDS, RC_ROTARY_RAMP = (
+    header_define("RC_ROTARY_" + n) for n in ("PLAIN", "LINEAR", "BASE", "BANDS", "RAMP"))
+RC_ROTARY_MAX, RC_ROTARY_MAX_HEAD = (
+    header_define("RC_ROTARY_MAX"), header_define("RC_ROTARY_MAX_HEAD"))
+
+
+class rc_rotary_spec(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rot", "first", "layout", "axes")] + [
+        ("pairs", C.c_int * 3), ("scaling", C.c_int)] + [
+        (n, C.c_double) for n in ("theta", "factor", "native_length", "fast", "slow",
+                                  "amplitude")]
+
+
+class rc_rotary(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rot", "first", "layout", "axes")] + [
+        ("pairs", C.c_int * 3), ("amplitude", C.c_float),
+        ("turns", C.c_uint64 * (RC_ROTARY_MAX // 2))]
+
+
 LAYER_FIELDS = ("W_qkv", "b_qkv", "W_o", "b_o", "W_xq", "b_xq", "W_xkv", "b_xkv", "W_xo",
                 "b_xo", "W_1", "b_1", "W_2", "b_2", "table")
 GLOBAL_FIELDS = ("W_e", "b_e", "pos", "W_t1", "b_t1", "W_t2", "b_t2", "W_tb", "b_tb", "table_f",
@@ -140,6 +178,9 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "rc_kv8_store": (I, [P, C.POINTER(rc_kv8), P, P, I, I, P, I, P, I, P]),
         "rc_kv8_attention": (I, [P, C.POINTER(rc_kv8), P, I, I, P, P, I, I, P, I, I, I, P, I,
                                  P]),
+        "rc_norm_residual": (I, [P, C.POINTER(rc_residual), P]),
+        "rc_rotary_plan": (I, [C.POINTER(rc_rotary_spec), C.POINTER(rc_rotary)]),
+        "rc_rotary_apply": (I, [P, C.POINTER(rc_rotary), P, I, I, I, I, I, P, P, I, P, I, P]),
         "rc_sync": (I, [P, P]),
         "rc_probe_enable": (I, [P, I, I]),
         "rc_probe_read": (I, [P, C.POINTER(C.c_double), C.POINTER(I)]),
@@ -424,6 +465,23 @@ def rc_kv8_attention(ctx, pool, Q, ldq, q_rows, row_offsets, lengths, n_requests
                                  1 if causal else 0, _ptr(O), ldo, _stream(stream)))
 
 
+def rc_norm_residual(ctx, op, stream=None):
+    """op: a ResidualNorm (or rc_residual)."""
+    _check(_lib.rc_norm_residual(ctx, op, _stream(stream)))
+
+
+def rc_rotary_plan(spec, out):
+    _check(_lib.rc_rotary_plan(C.byref(spec), C.byref(out)))
+
+
+def rc_rotary_apply(ctx, plan, x, ldx, type, rows, heads, head_dim, positions, count, inverse, y,
+                    ldy, stream=None):
+    """plan: a Rotary (or rc_rotary)."""
+    _check(_lib.rc_rotary_apply(ctx, plan, _ptr(x), ldx, type, rows, heads, head_dim,
+                                _ptr(positions), _ptr(count), 1 if inverse else 0, _ptr(y), ldy,
+                                _stream(stream)))
+
+
 def rc_selftest_wait(ctx, timeout_us, set_flag, stream=None):
     _check(_lib.rc_selftest_wait(ctx, timeout_us, 1 if set_flag else 0, _stream(stream)))
 
@@ -547,6 +605,112 @@ class Kv8Pool:
         p = cls.__new__(cls)
         p._hold(k, v, k_scale, v_scale)
         return p
+
+
+def _parameter(t, n, what):
+    """f32 [.., n] in one piece, or None."""
+    if t is not None and (t.dtype != torch.float32 or t.shape[-1] != n or t.stride(-1) != 1):
+        raise ValueError(f"{what} is float32 of {n} in one piece")
+    return t
+
+
+class Norm:
+    """A norm over rows (rc_norm): kind RC_NORM_*, weight and bias f32 [cols] or None."""
+
+    def __init__(self, kind, eps, weight=None, bias=None):
+        self.kind, self.eps, self.weight, self.bias = kind, eps, weight, bias
+
+    def struct(self, cols):
+        for t in (self.weight, self.bias):
+            if t is not None and t.dim() != 1:
+                raise ValueError("a norm's weight and bias have one dimension")
+        return rc_norm(self.kind, self.eps, _ptr(_parameter(self.weight, cols, "weight")),
+                       _ptr(_parameter(self.bias, cols, "bias")))
+
+
+class ResidualNorm:
+    """The tensors of an rc_residual (kept alive here) and the structure that names them, made
+    once: what rc_norm_residual takes.  x, x_out, h, y: bf16 or f32 matrices of `cols` columns
+    with rows in one piece; y may be an Fp8Matrix.  gate, scale, shift: f32 [items][cols], rows
+    equally far apart."""
+
+    def __init__(self, cols, x=None, h=None, x_out=None, y=None, post=None, pre=None, gate=None,
+                 scale=None, shift=None, residual_scale=1.0, row_offsets=None, places=None,
+                 weights=None):
+        y8 = y if isinstance(y, Fp8Matrix) else None
+        mats = {"x": x, "h": h, "x_out": x_out, "y": None if y8 else y}
+        for n, t in mats.items():
+            if t is not None and (t.dim() != 2 or t.shape[1] != cols or t.dtype not in DTYPES or
+                                  (t.shape[0] and t.stride(1) != 1)):
+                raise ValueError(f"{n} is a bfloat16 or float32 matrix of {cols} columns with "
+                                 "rows in one piece")
+        if x is not None and x_out is not None and x.dtype != x_out.dtype:
+            raise ValueError("x and x_out have one type")
+        if (places is None) != (weights is None) or (places is not None and h is None):
+            raise ValueError("places and weights come together, with h")
+        if places is not None and (
+                places.dtype != torch.int32 or weights.dtype != torch.float32 or
+                places.dim() != 2 or places.shape != weights.shape or
+                not places.is_contiguous() or not weights.is_contiguous()):
+            raise ValueError("places int32, weights float32: contiguous, [rows][top_k]")
+        if row_offsets is not None and (row_offsets.dtype != torch.int32 or
+                                        row_offsets.dim() != 1 or len(row_offsets) < 2 or
+                                        not row_offsets.is_contiguous()):
+            raise ValueError("row_offsets is int32 [items + 1]")
+        of_rows = [t for t in (x, x_out, mats["y"], places, h if places is None else None)
+                   if t is not None]
+        rows = len(of_rows[0]) if of_rows else y8.c.rows if y8 else 0
+        if any(len(t) != rows for t in of_rows) or (y8 and y8.c.rows < rows):
+            raise ValueError("x, h, x_out and y have one number of rows")
+        if y8 and (y8.c.cols != cols or y8.c.group != 1):
+            raise ValueError(f"y's codes are of {cols} columns, a scale for each row")
+        items = 1 if row_offsets is None else len(row_offsets) - 1
+        mods = {"gate": gate, "scale": scale, "shift": shift}
+        for n, t in mods.items():
+            if t is not None and (t.dim() != 2 or len(t) != items):
+                raise ValueError(f"{n} has a row for each of {items} items")
+            _parameter(t, cols, n)
+        ld_mod = {t.stride(0) for t in mods.values() if t is not None and items > 1} or {cols}
+        if len(ld_mod) > 1:
+            raise ValueError("gate, scale and shift have one row stride")
+        keep = [x, x_out, h, mats["y"], places, weights, gate, scale, shift, row_offsets,
+                y8 and y8.codes] + [t for n in (post, pre) if n for t in (n.weight, n.bias)]
+        if len({t.device for t in keep if t is not None}) > 1:
+            raise ValueError("all tensors lie on one device")
+        self._keep = keep + [y8]
+        none = rc_norm(RC_NORM_NONE, 0.0, None, None)
+
+        def ld(t):
+            return cols if t is None else t.stride(0) if len(t) > 1 else max(t.stride(0), cols)
+
+        def of(t):
+            return RC_BF16 if t is None else DTYPES[t.dtype]
+
+        self.c = rc_residual(
+            rows, cols, items, 0 if places is None else places.shape[1], _ptr(row_offsets),
+            _ptr(x), _ptr(x_out), _ptr(h), _ptr(places), _ptr(weights), _ptr(gate), _ptr(scale),
+            _ptr(shift), _ptr(mats["y"]), C.pointer(y8.c) if y8 else None,
+            of(x if x is not None else x_out), ld(x), ld(x_out), of(h), ld(h),
+            0 if h is None else len(h), ld_mod.pop(), of(mats["y"]), ld(mats["y"]),
+            residual_scale, post.struct(cols) if post else none,
+            pre.struct(cols) if pre else none)
+        self._as_parameter_ = C.pointer(self.c)
+
+
+class Rotary:
+    """A plan of rotary positions (rc_rotary_plan).  pairs: of each axis, None for one axis."""
+
+    def __init__(self, rot, theta=10000.0, pairs=None, first=0, layout=RC_ROTARY_HALF,
+                 scaling=RC_ROTARY_PLAIN, factor=1.0, native_length=0.0, fast=32.0, slow=1.0,
+                 amplitude=1.0):
+        pairs = [rot // 2] if pairs is None else list(pairs)
+        if not 1 <= len(pairs) <= 3:
+            raise ValueError("one to three axes")
+        spec = rc_rotary_spec(rot, first, layout, len(pairs), (C.c_int * 3)(*pairs), scaling,
+                              theta, factor, native_length, fast, slow, amplitude)
+        self.c = rc_rotary()
+        rc_rotary_plan(spec, self.c)
+        self._as_parameter_ = C.pointer(self.c)
 
 
 class Model:

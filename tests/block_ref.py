@@ -1,0 +1,101 @@
+"""The rest of a block in 64 bits, from the definitions of the header, on the
+CPU: norms with gate and residual, rotary positions (test helper)."""
+import math
+
+import torch
+
+F32_HALF = 2.0 ** -24  # half a step of f32, relative
+
+
+def rounding(dtype):
+    """Largest relative error of a rounding to the type."""
+    return torch.finfo(dtype).eps / 2
+
+
+def norm(kind, eps, w, b, v, dv):
+    """A norm of the rows of v (f64), and how far f32 may be off where v is off by dv: sums of n
+    terms in at most n / 32 + 16 steps (each 2^-24 of the magnitudes added), the difference and
+    root of the statistics, three more roundings."""
+    if kind == "none":
+        return v, dv
+    n = v.shape[1]
+    steps = (n / 32 + 16) * F32_HALF
+    mean = v.mean(1, keepdim=True) if kind == "layer" else torch.zeros(len(v), 1).double()
+    dmean = steps * v.abs().mean(1, keepdim=True) + dv.mean(1, keepdim=True)
+    d = v - mean
+    dd = dv + (dmean if kind == "layer" else 0) + F32_HALF * d.abs()
+    var = (d * d).mean(1, keepdim=True)
+    r = 1 / torch.sqrt(var + eps)
+    # of the variance, relative; a row whose differences are all error has none to speak of
+    dvar = steps + ((2 * d.abs() * dd + dd * dd).mean(1, keepdim=True) / (var + eps))
+    w = torch.ones(n).double() if w is None else w.cpu().double()
+    b = torch.zeros(n).double() if b is None else b.cpu().double()
+    y = d * r * w + b
+    return y, (dd + d.abs() * (dvar + 8 * F32_HALF)) * r * w.abs() + 2 * F32_HALF * y.abs()
+
+
+def residual(x, branch, dbranch, gate, a, post, pre, scale, shift):
+    """x', y of rows (f64) and their tolerances before they are rounded.  branch None: none."""
+    dx = torch.zeros_like(x)
+    x1 = a * x
+    if branch is not None:
+        r, dr = norm(*post, branch, dbranch)
+        g = torch.ones(x.shape[1]).double() if gate is None else gate
+        x1 = x1 + g * r
+        dx = 3 * F32_HALF * ((a * x).abs() + (g * r).abs()) + g.abs() * dr
+    else:
+        dx = F32_HALF * x1.abs()
+    y, dy = norm(*pre, x1, dx)
+    s = 0 if scale is None else scale
+    t = torch.zeros(x.shape[1]).double() if shift is None else shift
+    out = y * (1 + s) + t
+    factor = (1 + s) if scale is not None else torch.ones(x.shape[1]).double()
+    return x1, dx, out, dy * factor.abs() + 3 * F32_HALF * (y.abs() * (1 + abs(s)) + t.abs())
+
+
+def close(got, want, tol, dtype, what=""):
+    """Within tol before the rounding to dtype and half a step (and the least subnormal) after."""
+    got = got.cpu().double()
+    limit = tol + rounding(dtype) * (want.abs() + tol) + 1e-37
+    bad = ~((got - want).abs() <= limit)
+    assert not bool(bad.any()), \
+        f"{what}: {int(bad.sum())} of {bad.numel()} off, at most {float(((got - want).abs() / limit).max()):.2f} of the limit"
+
+
+def frequencies(pairs, theta, scaling="plain", factor=1.0, native=0.0, fast=0.0, slow=0.0):
+    """Radians a position of every pair, and its axis."""
+    f, axis = [], []
+    for a, n in enumerate(pairs):
+        base = theta * factor ** (n / (n - 1)) if scaling == "base" and n > 1 else theta
+        if scaling == "ramp":
+            at = [n * math.log(native / (2 * math.pi * t)) / math.log(base) for t in (fast, slow)]
+            lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), n - 1)
+        for i in range(n):
+            v = base ** (-i / n)
+            keep = 1.0
+            if scaling == "linear":
+                keep = 0.0
+            if scaling == "bands":
+                keep = (native * v / (2 * math.pi) - slow) / (fast - slow)
+            if scaling == "ramp":
+                keep = 1 - (i - lo) / max(hi - lo, 0.001)
+            keep = min(max(keep, 0.0), 1.0)
+            f.append(keep * v + (1 - keep) * v / factor)
+            axis.append(a)
+    return f, axis
+
+
+def rotate(x, positions, f, axis, first, half_layout, amplitude=1.0, inverse=False):
+    """x [rows][heads][head_dim] turned (f64), each pair as a complex number."""
+    rot = 2 * len(f)
+    at = positions.cpu().double()[:, axis] * torch.tensor(f, dtype=torch.float64)
+    turn = amplitude * torch.exp(1j * (-at if inverse else at))[:, None]
+    y = x.clone()
+    part = x[..., first:first + rot]
+    a, b = (part.chunk(2, -1)) if half_layout else (part[..., 0::2], part[..., 1::2])
+    z = torch.complex(a.contiguous(), b.contiguous()) * turn
+    if half_layout:
+        y[..., first:first + rot] = torch.cat([z.real, z.imag], -1)
+    else:
+        y[..., first:first + rot] = torch.view_as_real(z).flatten(-2)
+    return y
