@@ -645,7 +645,7 @@ rc_status rc_kv8_attention(rc_ctx* ctx, const rc_kv8* pool, const void* Q, int l
 
 /* What a transformer block needs between its quantised products and the
  * eight-bit cache (no counterpart in the paper; serving plumbing): norms with
- * gate and residual, and rotary positions.  As above:
+ * gate and residual, rotary positions, and the routing of rows to experts.  As above:
  * the context serves for its error word and device only, nothing is allocated
  * or kept, calls on different streams may overlap as long as their buffers do
  * not, and all calls but rc_rotary_plan (host code) may be captured.  Results
@@ -781,6 +781,60 @@ rc_status rc_rotary_plan(const rc_rotary_spec* spec, rc_rotary* out);
 rc_status rc_rotary_apply(rc_ctx* ctx, const rc_rotary* plan, const void* x, int ldx, int type,
                           int rows, int heads, int head_dim, const int32_t* positions,
                           const int32_t* count, int inverse, void* y, int ldy, rc_stream stream);
+
+/* The experts of each row.  With a row's logits z, its scores are
+ * RC_SCORE_SOFTMAX exp(z) / sum of exp(z), or RC_SCORE_SIGMOID 1 / (1 + exp(-z)).
+ * An expert counts by score + bias (bias f32 [experts], null for zeros: balances
+ * the load and does not enter the weights).  Of `groups` groups of neighbouring
+ * experts only the top_groups with the largest value take part, the value being
+ * the sum of a group's group_best best experts.  The top_k best experts are
+ * chosen, best first; ties go to the lower index, of groups too.  weights are
+ * the chosen scores, with `renormalise` divided by their sum (all 0 where that
+ * is 0), times `scale`.
+ * Which expert is larger is decided as if scores were computed in f64: f32
+ * scores closer than they are exact are computed again.  Without bias, and with
+ * groups valued by one expert, it is decided by the logits themselves.
+ * An expert whose logit or bias is NaN or -inf (a mask) is never chosen and
+ * adds nothing to a softmax; a logit or bias of +inf counts as the largest f32.  Where fewer than
+ * top_k are left, the rest of ids is -1 with weight 0.
+ *   experts 1 .. RC_EXPERTS_MAX, a multiple of groups; top_k 1 ..
+ *   RC_EXPERTS_MAX_TOP_K; groups 1 .. 32, top_groups 1 .. groups, group_best 1
+ *   or 2; scale finite.
+ *   logits       `type` (RC_BF16, RC_F32) [rows][ld], ld >= experts.
+ *   count        i32 on the device, rows to route (null: rows); the others' ids are
+ *                set to -1 and their weights to 0.
+ *   ids, weights out, i32 and f32 [rows][top_k].
+ * Device checks: a count out of range is reported and taken as 0.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_SCORE_SOFTMAX 0
+#define RC_SCORE_SIGMOID 1
+#define RC_EXPERTS_MAX 1024
+typedef struct rc_routing {
+  int experts, top_k, score, groups, top_groups, group_best, renormalise;
+  float scale;
+  const float* bias;
+} rc_routing;
+rc_status rc_experts_route(rc_ctx* ctx, const rc_routing* routing, const void* logits, int ld,
+                           int type, int rows, const int32_t* count, int32_t* ids, float* weights,
+                           rc_stream stream);
+
+/* The rows of each expert, one expert after another and in ascending order.
+ *   ids      i32 [rows][top_k], as from rc_experts_route (below 0: no expert).
+ *            rows * top_k <= RC_EXPERTS_MAX_PAIRS, experts 1 .. RC_EXPERTS_MAX.
+ *   count    i32 on the device, rows to sort (null: rows); the others have no
+ *            expert.
+ *   offsets  out, i32 [experts + 1]: expert e owns places offsets[e] ..
+ *            offsets[e + 1] - 1.
+ *   source   out, i32 [rows * top_k]: the row of each place; entries from
+ *            offsets[experts] on are left as they were.
+ *   places   out, i32 [rows][top_k]: the place of each pair, -1 without one.
+ * Device checks: an id of `experts` or more is reported and taken as none, a
+ * count out of range is reported and taken as 0.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_EXPERTS_MAX_PAIRS 1073741824
+rc_status rc_experts_sort(rc_ctx* ctx, const int32_t* ids, int rows, int top_k, int experts,
+                          const int32_t* count, int32_t* offsets, int32_t* source,
+                          int32_t* places, rc_stream stream);
 
 /* Waits for `stream`, then reports (and clears) the context's device error
  * word: RC_ERR_DEVICE_ASSERT if a kernel met a bad index or count,

@@ -199,4 +199,55 @@ rc_status rc_rotary_apply(rc_ctx* c, const rc_rotary* plan, const void* x, int l
   return launched(rc::launch_rotary(a, static_cast<cudaStream_t>(stream)), fn);
 }
 
+rc_status rc_experts_route(rc_ctx* c, const rc_routing* r, const void* logits, int ld, int type,
+                           int rows, const int32_t* count, int32_t* ids, float* weights,
+                           rc_stream stream) {
+  const char* fn = "rc_experts_route";
+  if (!c || !r) return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
+  RC_CHECK(check_type(type, fn));
+  if (rows < 0 || r->experts < 1 || r->experts > RC_EXPERTS_MAX || r->top_k < 1 ||
+      r->top_k > RC_EXPERTS_MAX_TOP_K || ld < r->experts)
+    return fail(RC_ERR_SHAPE, "%s: %d rows, %d experts (at most %d), top_k %d (at most %d), ld %d",
+                fn, rows, r->experts, RC_EXPERTS_MAX, r->top_k, RC_EXPERTS_MAX_TOP_K, ld);
+  if (r->groups < 1 || r->groups > 32 || r->experts % r->groups || r->top_groups < 1 ||
+      r->top_groups > r->groups)
+    return fail(RC_ERR_SHAPE, "%s: %d of %d groups (at most 32) of %d experts", fn, r->top_groups,
+                r->groups, r->experts);
+  if (r->group_best != 1 && r->group_best != 2)
+    return fail(RC_ERR_INVALID_ARG, "%s: group_best %d is not 1 or 2", fn, r->group_best);
+  if (r->score != RC_SCORE_SOFTMAX && r->score != RC_SCORE_SIGMOID)
+    return fail(RC_ERR_INVALID_ARG, "%s: score %d", fn, r->score);
+  if (!is_finite(r->scale)) return fail(RC_ERR_INVALID_ARG, "%s: scale is not finite", fn);
+  if (!aligned(logits, type == RC_F32 ? 4 : 2) || !aligned(r->bias, 4) || !aligned(count, 4) ||
+      !aligned(ids, 4) || !aligned(weights, 4))
+    return fail(RC_ERR_INVALID_ARG, "%s: a pointer is not aligned to its type", fn);
+  if (rows == 0) return RC_OK;
+  if (!logits || !ids || !weights) return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
+  RC_CHECK(check_device(c, fn));
+  const rc::RoutingArgs a{logits, type == RC_F32, ld, rows, r->experts, r->top_k, r->score,
+                          r->groups, r->top_groups, r->group_best, r->renormalise != 0, r->scale,
+                          r->bias, count, ids, weights, rc::ctx_error_word(c)};
+  return launched(rc::launch_experts_route(a, static_cast<cudaStream_t>(stream)), fn);
+}
+
+rc_status rc_experts_sort(rc_ctx* c, const int32_t* ids, int rows, int top_k, int experts,
+                          const int32_t* count, int32_t* offsets, int32_t* source, int32_t* places,
+                          rc_stream stream) {
+  const char* fn = "rc_experts_sort";
+  if (!c || !offsets) return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
+  if (rows < 0 || top_k < 1 || top_k > RC_EXPERTS_MAX_TOP_K || experts < 1 ||
+      experts > RC_EXPERTS_MAX || (long long)rows * top_k > RC_EXPERTS_MAX_PAIRS)
+    return fail(RC_ERR_SHAPE, "%s: %d rows of %d (at most %d) of %d experts (at most %d)", fn, rows,
+                top_k, RC_EXPERTS_MAX_TOP_K, experts, RC_EXPERTS_MAX);
+  if (rows > 0 && (!ids || !source || !places))
+    return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
+  const void* ints[] = {ids, count, offsets, source, places};
+  for (const void* p : ints)
+    if (!aligned(p, 4)) return fail(RC_ERR_INVALID_ARG, "%s: a pointer is not 4-B aligned", fn);
+  RC_CHECK(check_device(c, fn));
+  const rc::SortArgs a{ids, rows, top_k, experts, count, offsets, source, places,
+                       rc::ctx_error_word(c)};
+  return launched(rc::launch_experts_sort(a, static_cast<cudaStream_t>(stream)), fn);
+}
+
 }  // extern "C"

@@ -1,5 +1,5 @@
-// Internal launchers of a block's row work and rotary positions
-// (rc_norm_residual, rc_rotary_*).  Every launcher queues one
+// Internal launchers of a block's row work, rotary positions and experts
+// (rc_norm_residual, rc_rotary_*, rc_experts_*).  Every launcher queues one
 // kernel on `st` and returns the cudaError_t of the launch.
 #pragma once
 #include "../../include/regioncache.h"
@@ -42,5 +42,26 @@ struct RotaryArgs {
   unsigned* err;
 };
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st);
+
+struct RoutingArgs {
+  const void* logits;
+  bool f32;
+  int ld, rows, experts, top_k, score, groups, top_groups, group_best, renormalise;
+  float scale;
+  const float* bias;
+  const int* count;
+  int* ids;
+  float* weights;
+  unsigned* err;
+};
+cudaError_t launch_experts_route(const RoutingArgs& a, cudaStream_t st);
+struct SortArgs {
+  const int* ids;
+  int rows, top_k, experts;
+  const int* count;
+  int *offsets, *source, *places;
+  unsigned* err;
+};
+cudaError_t launch_experts_sort(const SortArgs& a, cudaStream_t st);
 
 }  // namespace rc

@@ -114,6 +114,18 @@ class rc_rotary(C.Structure):
         ("turns", C.c_uint64 * (RC_ROTARY_MAX // 2))]
 
 
+RC_SCORE_SOFTMAX, RC_SCORE_SIGMOID = (
+    header_define("RC_SCORE_SOFTMAX"), header_define("RC_SCORE_SIGMOID"))
+RC_EXPERTS_MAX, RC_EXPERTS_MAX_PAIRS = (
+    header_define("RC_EXPERTS_MAX"), header_define("RC_EXPERTS_MAX_PAIRS"))
+
+
+class rc_routing(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("experts", "top_k", "score", "groups", "top_groups",
+                                       "group_best", "renormalise")] + [
+        ("scale", C.c_float), ("bias", C.c_void_p)]
+
+
 LAYER_FIELDS = ("W_qkv", "b_qkv", "W_o", "b_o", "W_xq", "b_xq", "W_xkv", "b_xkv", "W_xo",
                 "b_xo", "W_1", "b_1", "W_2", "b_2", "table")
 GLOBAL_FIELDS = ("W_e", "b_e", "pos", "W_t1", "b_t1", "W_t2", "b_t2", "W_tb", "b_tb", "table_f",
@@ -181,6 +193,8 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "rc_norm_residual": (I, [P, C.POINTER(rc_residual), P]),
         "rc_rotary_plan": (I, [C.POINTER(rc_rotary_spec), C.POINTER(rc_rotary)]),
         "rc_rotary_apply": (I, [P, C.POINTER(rc_rotary), P, I, I, I, I, I, P, P, I, P, I, P]),
+        "rc_experts_route": (I, [P, C.POINTER(rc_routing), P, I, I, I, P, P, P, P]),
+        "rc_experts_sort": (I, [P, P, I, I, I, P, P, P, P, P]),
         "rc_sync": (I, [P, P]),
         "rc_probe_enable": (I, [P, I, I]),
         "rc_probe_read": (I, [P, C.POINTER(C.c_double), C.POINTER(I)]),
@@ -482,6 +496,17 @@ def rc_rotary_apply(ctx, plan, x, ldx, type, rows, heads, head_dim, positions, c
                                 _stream(stream)))
 
 
+def rc_experts_route(ctx, routing, logits, ld, type, rows, count, ids, weights, stream=None):
+    """routing: a Routing (or rc_routing)."""
+    _check(_lib.rc_experts_route(ctx, routing, _ptr(logits), ld, type, rows, _ptr(count),
+                                 _ptr(ids), _ptr(weights), _stream(stream)))
+
+
+def rc_experts_sort(ctx, ids, rows, top_k, experts, count, offsets, source, places, stream=None):
+    _check(_lib.rc_experts_sort(ctx, _ptr(ids), rows, top_k, experts, _ptr(count), _ptr(offsets),
+                                _ptr(source), _ptr(places), _stream(stream)))
+
+
 def rc_selftest_wait(ctx, timeout_us, set_flag, stream=None):
     _check(_lib.rc_selftest_wait(ctx, timeout_us, 1 if set_flag else 0, _stream(stream)))
 
@@ -710,6 +735,21 @@ class Rotary:
                               theta, factor, native_length, fast, slow, amplitude)
         self.c = rc_rotary()
         rc_rotary_plan(spec, self.c)
+        self._as_parameter_ = C.pointer(self.c)
+
+
+class Routing:
+    """How rows choose their experts (rc_routing).  bias: f32 [experts] or None (kept alive
+    here); top_groups: all of them unless given."""
+
+    def __init__(self, experts, top_k, score=RC_SCORE_SOFTMAX, bias=None, groups=1,
+                 top_groups=None, group_best=1, renormalise=True, scale=1.0):
+        if bias is not None and bias.dim() != 1:
+            raise ValueError("a routing's bias has one dimension")
+        self.bias = _parameter(bias, experts, "bias")
+        self.c = rc_routing(experts, top_k, score, groups,
+                            groups if top_groups is None else top_groups, group_best,
+                            1 if renormalise else 0, scale, _ptr(bias))
         self._as_parameter_ = C.pointer(self.c)
 
 

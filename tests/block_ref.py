@@ -99,3 +99,59 @@ def rotate(x, positions, f, axis, first, half_layout, amplitude=1.0, inverse=Fal
     else:
         y[..., first:first + rot] = torch.view_as_real(z).flatten(-2)
     return y
+
+
+BIG = torch.finfo(torch.float32).max
+
+
+def route(z, score, k, bias=None, groups=1, top_groups=1, group_best=1, renormalise=True,
+          scale=1.0):
+    """ids and weights (f64) of the rows' experts."""
+    z = z.cpu().double().clamp(max=BIG)
+    rows, e = z.shape
+    b = torch.zeros(e).double() if bias is None else bias.cpu().double().clamp(max=BIG)
+    there = (z > -math.inf) & (b > -math.inf)
+    z = torch.where(there, z, -math.inf)
+    if score == "softmax":
+        s = torch.exp(z - z.amax(1, keepdim=True).clamp(min=-BIG))
+        s = s / s.sum(1, keepdim=True)
+    else:
+        s = 1 / (1 + torch.exp(-z))
+    ids, w = torch.full((rows, k), -1), torch.zeros(rows, k).double()
+    # (without a bias larger logits have larger scores, also where f64 has them equal)
+    plain = bias is None and (top_groups == groups or group_best == 1)
+    value = z if plain else s + b
+    size = e // groups
+    for r in range(rows):
+        left = [i for i in range(e) if there[r, i]]
+        if top_groups < groups:
+            of = {}
+            for i in left:
+                of.setdefault(i // size, []).append(float(value[r, i]))
+            worth = {g: sum(sorted(v, reverse=True)[:group_best]) for g, v in of.items()}
+            best = sorted(worth, key=lambda g: (-worth[g], g))[:top_groups]
+            left = [i for i in left if i // size in best]
+        chosen = sorted(left, key=lambda i: (-float(value[r, i]), i))[:k]
+        for j, i in enumerate(chosen):
+            ids[r, j], w[r, j] = i, s[r, i]
+    if renormalise:
+        total = w.sum(1, keepdim=True)
+        w = torch.where(total > 0, w / total, 0.0)
+    return ids.int(), w * scale
+
+
+def sort(ids, experts):
+    """Offsets, rows in order of the experts, places of the pairs."""
+    rows, k = ids.shape
+    pairs = [(e, i) for i, e in enumerate(ids.flatten().tolist()) if 0 <= e < experts]
+    pairs.sort()
+    offsets = [0] * (experts + 1)
+    for e, _ in pairs:
+        offsets[e + 1] += 1
+    for e in range(experts):
+        offsets[e + 1] += offsets[e]
+    places = torch.full((rows * k,), -1, dtype=torch.int32)
+    source = torch.zeros(len(pairs), dtype=torch.int32)
+    for p, (_, i) in enumerate(pairs):
+        places[i], source[p] = p, i // k
+    return torch.tensor(offsets, dtype=torch.int32), source, places.view(rows, k)

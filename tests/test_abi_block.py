@@ -25,7 +25,7 @@ def R():
 
 
 def test_structures_match_the_header(R):
-    structs = (R.rc_norm, R.rc_residual, R.rc_rotary_spec, R.rc_rotary)
+    structs = (R.rc_norm, R.rc_residual, R.rc_rotary_spec, R.rc_rotary, R.rc_routing)
     lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "regioncache.h"',
              "int main(void) {"]
     for s in structs:
@@ -158,6 +158,45 @@ def test_rotary_apply_refusals(R):
     bad.c.rot, bad.c.layout = 64, 7
     assert call(p=bad) == 1
     assert call(rows=0, x=None, y=None) == 0 and call(heads=0, x=None, y=None) == 0
+
+
+def test_route_refusals(R):
+    def call(ctx=CTX, z=A, ld=64, type=0, rows=4, count=None, ids=A, w=A, **kw):
+        a = dict(experts=64, top_k=2, score=0, groups=4, top_groups=2, group_best=1,
+                 renormalise=1, scale=1.0, bias=None)
+        a.update(kw)
+        r = R.rc_routing(*[a[f] for f, _ in R.rc_routing._fields_])
+        return R._lib.rc_experts_route(ctx, C.byref(r), z, ld, type, rows, count, ids, w, None)
+
+    assert call(ctx=None) == 1
+    assert R._lib.rc_experts_route(CTX, None, A, 64, 0, 4, None, A, A, None) == 1
+    for kw in (dict(rows=-1), dict(experts=0), dict(experts=1025, ld=1025), dict(top_k=0),
+               dict(top_k=17), dict(ld=63), dict(groups=0), dict(groups=3), dict(groups=64),
+               dict(top_groups=0), dict(top_groups=5)):
+        assert call(**kw) == 2, kw
+    for kw in (dict(group_best=0), dict(group_best=3), dict(score=2), dict(score=-1),
+               dict(scale=math.nan), dict(type=2), dict(z=ODD), dict(z=A + 2, type=1),
+               dict(bias=A + 2), dict(count=A + 2), dict(ids=A + 2), dict(w=ODD), dict(z=None),
+               dict(ids=None), dict(w=None)):
+        assert call(**kw) == 1, kw
+    assert call(rows=0, z=None, ids=None, w=None) == 0
+    with pytest.raises(ValueError):
+        R.Routing(8, 2, bias=torch.zeros(7))
+    with pytest.raises(ValueError):
+        R.Routing(8, 2, bias=torch.zeros(8, dtype=torch.double))
+
+
+def test_sort_refusals(R):
+    def call(ctx=CTX, ids=A, rows=4, k=2, e=8, count=None, off=A, src=A, at=A):
+        return R._lib.rc_experts_sort(ctx, ids, rows, k, e, count, off, src, at, None)
+
+    assert call(ctx=None) == 1
+    for kw in (dict(rows=-1), dict(k=0), dict(k=17), dict(e=0), dict(e=1025),
+               dict(rows=2 ** 30, k=2)):
+        assert call(**kw) == 2, kw
+    for kw in (dict(ids=None), dict(off=None), dict(src=None), dict(at=None), dict(ids=A + 2),
+               dict(count=A + 1), dict(off=A + 2), dict(src=ODD), dict(at=A + 3)):
+        assert call(**kw) == 1, kw
 
 
 def test_wrappers_refuse_tensors_that_do_not_fit(R):
