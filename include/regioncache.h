@@ -645,7 +645,7 @@ rc_status rc_kv8_attention(rc_ctx* ctx, const rc_kv8* pool, const void* Q, int l
 
 /* What a transformer block needs between its quantised products and the
  * eight-bit cache (no counterpart in the paper; serving plumbing): norms with
- * gate and residual, rotary positions, and the routing of rows to experts.  As above:
+ * gate and residual, rotary positions, and feed-forward experts.  As above:
  * the context serves for its error word and device only, nothing is allocated
  * or kept, calls on different streams may overlap as long as their buffers do
  * not, and all calls but rc_rotary_plan (host code) may be captured.  Results
@@ -835,6 +835,38 @@ rc_status rc_experts_route(rc_ctx* ctx, const rc_routing* routing, const void* l
 rc_status rc_experts_sort(rc_ctx* ctx, const int32_t* ids, int rows, int top_k, int experts,
                           const int32_t* count, int32_t* offsets, int32_t* source,
                           int32_t* places, rc_stream stream);
+
+/* rc_fp8_linear for each expert's rows, with its activation: for the places p
+ * of expert e,  y[p] = act(x[row] W_e^T + b_e),  row = source[p], or p without
+ * source.
+ *   x        group 1; without source of `pairs` rows at least.
+ *   W        group 128, W->rows a multiple of experts * 128: expert e's matrix
+ *            is rows e * W->rows / experts .., of which the first N count:
+ *            N = n, or 2 n with a gated activation.  x->cols == W->cols.
+ *   b        f32 [experts][N] or null.
+ *   offsets  i32 [experts + 1] as from rc_experts_sort, 0 .. pairs.
+ *   source   i32, the row of x of each place, or null.
+ *   act      of the f32 sums: RC_ACT_NONE; RC_ACT_GELU v (1 + tanh(sqrt(2 / pi)
+ *            (v + 0.044715 v^3))) / 2; RC_ACT_SILU v / (1 + exp(-v));
+ *            RC_ACT_GATED_SILU silu(column j) * column n + j.
+ *   y        `type` (RC_BF16, RC_F32) [pairs][ldy], ldy >= n, or null with
+ *   y8       codes instead: pairs rows at least, n columns, group 1, as
+ *            rc_fp8_quantize gives them for the f32 values.
+ * Places outside offsets are left as they were.  experts 1 .. RC_EXPERTS_MAX,
+ * pairs 0 .. RC_EXPERTS_MAX_PAIRS, (pairs / 128 + experts) * (n / 32 + 1) < 2^31 - 152.
+ * Results are bit-identical from call to call.  One expert without source is a plain quantised
+ * layer with its activation: offsets {0, rows}.
+ * Device checks: offsets that descend or leave 0 .. pairs (the expert is left
+ * out) and a source outside x (taken as row 0) are reported.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */
+#define RC_ACT_NONE 0
+#define RC_ACT_GELU 1
+#define RC_ACT_SILU 2
+#define RC_ACT_GATED_SILU 3
+rc_status rc_experts_linear(rc_ctx* ctx, const rc_fp8* x, const rc_fp8* W, const float* b,
+                            int experts, int n, const int32_t* offsets, const int32_t* source,
+                            int pairs, int act, void* y, int ldy, int type, const rc_fp8* y8,
+                            rc_stream stream);
 
 /* Waits for `stream`, then reports (and clears) the context's device error
  * word: RC_ERR_DEVICE_ASSERT if a kernel met a bad index or count,

@@ -250,4 +250,52 @@ rc_status rc_experts_sort(rc_ctx* c, const int32_t* ids, int rows, int top_k, in
   return launched(rc::launch_experts_sort(a, static_cast<cudaStream_t>(stream)), fn);
 }
 
+rc_status rc_experts_linear(rc_ctx* c, const rc_fp8* x, const rc_fp8* W, const float* b,
+                            int experts, int n, const int32_t* offsets, const int32_t* source,
+                            int pairs, int act, void* y, int ldy, int type, const rc_fp8* y8,
+                            rc_stream stream) {
+  const char* fn = "rc_experts_linear";
+  if (!c || !x || !W) return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
+  rc::ExpertsArgs a = {};
+  RC_CHECK(check_matrix(x, fn, "x", &a.x));
+  RC_CHECK(check_matrix(W, fn, "W", &a.w));
+  if (x->group != 1 || W->group != 128)
+    return fail(RC_ERR_INVALID_ARG, "%s: groups of x and W are %d and %d (1 and 128)", fn, x->group,
+                W->group);
+  if (act < RC_ACT_NONE || act > RC_ACT_GATED_SILU)
+    return fail(RC_ERR_INVALID_ARG, "%s: act %d", fn, act);
+  if (experts < 1 || experts > RC_EXPERTS_MAX || n < 1 || pairs < 0 ||
+      pairs > RC_EXPERTS_MAX_PAIRS ||
+      (pairs / 128LL + experts) * (n / 32LL + 1) >= 0x7fffffffLL - 152)
+    return fail(RC_ERR_SHAPE, "%s: %d experts (at most %d) of %d outputs, %d pairs", fn, experts,
+                RC_EXPERTS_MAX, n, pairs);
+  const long long wide = act == RC_ACT_GATED_SILU ? 2LL * n : n;
+  if (x->cols != W->cols || W->rows < 1 || W->rows % (experts * 128) || W->rows / experts < wide)
+    return fail(RC_ERR_SHAPE,
+                "%s: x has %d columns, W is %d x %d for %d experts of %lld rows (in 128s each)", fn,
+                x->cols, W->rows, W->cols, experts, wide);
+  if (pairs > 0 && x->rows < (source ? 1 : pairs))
+    return fail(RC_ERR_SHAPE, "%s: x has %d rows for %d pairs", fn, x->rows, pairs);
+  if (y && y8) return fail(RC_ERR_INVALID_ARG, "%s: both y and y8", fn);
+  if (y8) {
+    RC_CHECK(check_matrix(y8, fn, "y8", &a.y8));
+    if (y8->group != 1 || y8->cols != n || y8->rows < pairs)
+      return fail(RC_ERR_SHAPE, "%s: y8 is %d x %d in groups of %d for %d x %d", fn, y8->rows,
+                  y8->cols, y8->group, pairs, n);
+  } else {
+    RC_CHECK(check_rows(y, type, ldy, n, fn, "y"));
+  }
+  if (pairs == 0) return RC_OK;
+  if (!offsets || (!y && !y8)) return fail(RC_ERR_INVALID_ARG, "%s: null argument", fn);
+  if (!aligned(b, 4) || !aligned(offsets, 4) || !aligned(source, 4))
+    return fail(RC_ERR_INVALID_ARG, "%s: a pointer is not 4-B aligned", fn);
+  RC_CHECK(check_device(c, fn));
+  a.bias = b;
+  a.experts = experts, a.n = n, a.offsets = offsets, a.source = source, a.pairs = pairs;
+  a.act = act;
+  a.y = y, a.ldy = ldy, a.f32 = type == RC_F32;
+  a.err = rc::ctx_error_word(c);
+  return launched(rc::launch_experts_linear(a, static_cast<cudaStream_t>(stream)), fn);
+}
+
 }  // extern "C"

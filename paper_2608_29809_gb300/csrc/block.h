@@ -63,5 +63,19 @@ struct SortArgs {
   unsigned* err;
 };
 cudaError_t launch_experts_sort(const SortArgs& a, cudaStream_t st);
+// w: the experts' matrices one below the other; y8.codes null for none.
+struct ExpertsArgs {
+  Fp8Mat x, w;
+  const float* bias;
+  int experts, n;
+  const int *offsets, *source;
+  int pairs, act;
+  void* y;
+  int ldy;
+  bool f32, tma;  // tma: y's rows are 16-byte aligned, set by the launcher
+  Fp8Mat y8;
+  unsigned* err;
+};
+cudaError_t launch_experts_linear(const ExpertsArgs& a, cudaStream_t st);
 
 }  // namespace rc

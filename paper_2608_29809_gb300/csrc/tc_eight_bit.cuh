@@ -15,6 +15,26 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
       : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// Four rows of a matrix (a map whose box is one row high), one below the other in
+// this CTA's shared memory; their bytes are counted by `bar`, of PAIR either CTA's.
+template <bool PAIR>
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, uint32_t bar,
+                                            int x, const int* rows) {
+  if (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
+        ".mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(rows[0]), "r"(rows[1]),
+        "r"(rows[2]), "r"(rows[3])
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4"
+        ".mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(rows[0]), "r"(rows[1]),
+        "r"(rows[2]), "r"(rows[3])
+        : "memory");
+}
 // All but the thread's last N bulk groups have read their shared memory.
 template <int N>
 __device__ __forceinline__ void tma_store_wait_read() {

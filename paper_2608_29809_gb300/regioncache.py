@@ -119,6 +119,9 @@ RC_SCORE_SOFTMAX, RC_SCORE_SIGMOID = (
 RC_EXPERTS_MAX, RC_EXPERTS_MAX_PAIRS = (
     header_define("RC_EXPERTS_MAX"), header_define("RC_EXPERTS_MAX_PAIRS"))
 
+RC_ACT_NONE, RC_ACT_GELU, RC_ACT_SILU, RC_ACT_GATED_SILU = (
+    header_define("RC_ACT_" + n) for n in ("NONE", "GELU", "SILU", "GATED_SILU"))
+
 
 class rc_routing(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("experts", "top_k", "score", "groups", "top_groups",
@@ -195,6 +198,8 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "rc_rotary_apply": (I, [P, C.POINTER(rc_rotary), P, I, I, I, I, I, P, P, I, P, I, P]),
         "rc_experts_route": (I, [P, C.POINTER(rc_routing), P, I, I, I, P, P, P, P]),
         "rc_experts_sort": (I, [P, P, I, I, I, P, P, P, P, P]),
+        "rc_experts_linear": (I, [P, C.POINTER(rc_fp8), C.POINTER(rc_fp8), P, I, I, P, P, I, I, P,
+                                  I, I, C.POINTER(rc_fp8), P]),
         "rc_sync": (I, [P, P]),
         "rc_probe_enable": (I, [P, I, I]),
         "rc_probe_read": (I, [P, C.POINTER(C.c_double), C.POINTER(I)]),
@@ -505,6 +510,13 @@ def rc_experts_route(ctx, routing, logits, ld, type, rows, count, ids, weights, 
 def rc_experts_sort(ctx, ids, rows, top_k, experts, count, offsets, source, places, stream=None):
     _check(_lib.rc_experts_sort(ctx, _ptr(ids), rows, top_k, experts, _ptr(count), _ptr(offsets),
                                 _ptr(source), _ptr(places), _stream(stream)))
+
+
+def rc_experts_linear(ctx, x, W, b, experts, n, offsets, source, pairs, act, y, ldy, type,
+                      y8=None, stream=None):
+    """x, W, y8: Fp8Matrix (or rc_fp8)."""
+    _check(_lib.rc_experts_linear(ctx, x, W, _ptr(b), experts, n, _ptr(offsets), _ptr(source),
+                                  pairs, act, _ptr(y), ldy, type, y8, _stream(stream)))
 
 
 def rc_selftest_wait(ctx, timeout_us, set_flag, stream=None):

@@ -199,6 +199,41 @@ def test_sort_refusals(R):
         assert call(**kw) == 1, kw
 
 
+def _matrix(R, **kw):
+    a = dict(codes=A, scales=A, rows=8, cols=256, ld=256, lds=2 ** 20, group=1)
+    a.update(kw)
+    return C.pointer(R.rc_fp8(*[a[f] for f, _ in R.rc_fp8._fields_]))
+
+
+def test_experts_linear_refusals(R):
+    def call(ctx=CTX, x=0, W=0, b=None, experts=3, n=200, off=A, src=None, pairs=8, act=0, y=A,
+             ldy=200, type=0, y8=None):
+        x = _matrix(R) if x == 0 else x
+        W = _matrix(R, rows=768, group=128) if W == 0 else W
+        return R._lib.rc_experts_linear(ctx, x, W, b, experts, n, off, src, pairs, act, y, ldy,
+                                        type, y8, None)
+
+    assert call(ctx=None) == 1 and call(x=None) == 1 and call(W=None) == 1
+    for kw in (dict(x=_matrix(R, ld=248)), dict(W=_matrix(R, rows=768, group=128, lds=5)),
+               dict(experts=0), dict(experts=1025), dict(n=0), dict(pairs=-1),
+               dict(pairs=2 ** 30 + 1), dict(n=257, ldy=257), dict(act=3), dict(experts=4),
+               dict(x=_matrix(R, cols=255)), dict(W=_matrix(R, rows=0, group=128)),
+               dict(x=_matrix(R, rows=7)), dict(x=_matrix(R, rows=0, codes=None), src=A),
+               dict(ldy=199), dict(y=None, y8=_matrix(R, rows=7, cols=200)),
+               dict(y=None, y8=_matrix(R, cols=199)),
+               dict(y=None, y8=_matrix(R, cols=200, group=128)),
+               dict(x=_matrix(R, rows=2 ** 30, lds=2 ** 30), pairs=2 ** 30, experts=1, n=8192,
+                    ldy=8192, W=_matrix(R, rows=8192, group=128))):
+        assert call(**kw) == 2, kw
+    for kw in (dict(x=_matrix(R, group=128)), dict(W=_matrix(R, rows=768)), dict(act=4),
+               dict(act=-1), dict(y8=_matrix(R, cols=200)), dict(y=None), dict(off=None),
+               dict(type=2), dict(y=ODD), dict(y=A + 2, type=1), dict(b=A + 2), dict(off=A + 2),
+               dict(src=A + 1), dict(x=_matrix(R, codes=A + 8)), dict(x=_matrix(R, scales=None)),
+               dict(W=_matrix(R, rows=768, group=128, codes=None))):
+        assert call(**kw) == 1, kw
+    assert call(pairs=0, off=None, y=None) == 0
+
+
 def test_wrappers_refuse_tensors_that_do_not_fit(R):
     x = torch.zeros(6, 40)
     h = torch.zeros(6, 40, dtype=torch.bfloat16)
