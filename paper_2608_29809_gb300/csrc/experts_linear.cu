@@ -3,14 +3,18 @@
 // tensor core, with the work shared out on the device (only it knows how many rows
 // each expert has).
 //
-// Persistent CTAs of 16 warps, as in rc_fp8_linear: warp 0 brings the rows of x
-// (gathered by TMA, four rows an instruction and lane), warp 2 W, warp 1 issues
-// the MMAs, warps 4..7 put the scale bytes into tensor memory, warps 8..15 drain
-// the accumulator.  Each CTA first lists the experts that have rows, with the
-// tiles of BM rows before each; a tile's number names its rows by a search there,
-// and its columns.  Rows of an accumulator do not mix, so what a tile holds beyond
-// its expert's rows (stale shared memory, the next expert's rows) is only never
-// written.
+// Persistent CTAs of 28 warps, as in rc_fp8_linear: warps 0, 3 and 24..27 bring the
+// rows of x, warp 2 W, warp 1 issues the MMAs, warps 4..7 put the scale bytes into
+// tensor memory, warps 8..23 drain the accumulator.  Rows are gathered by TMA, four an
+// instruction, of which a warp issues one in 60 to 130 cycles: 16384 x 2 rows, 1152 x
+// 4608, took 508 us with one warp, 290 with two; now 214 (neighbouring rows, in one
+// box: 155).  Two things bound the rest more than the tensor core (90 us): the roles'
+// code has to stay in the SM's instruction cache (at 96 KB it did not: 180 us for
+// neighbouring rows), and nothing may be spilled (registers for 28 warps: 72).
+// Each CTA first lists the experts that have rows, with the tiles of BM rows before
+// each; a tile's number names its rows by a search there, and its columns.  Rows of
+// an accumulator do not mix, so what a tile holds beyond its expert's rows (stale
+// shared memory, the next expert's rows) is only never written.
 #include <float.h>
 
 #include "../../include/regioncache.h"
@@ -26,10 +30,10 @@ namespace {
 using namespace rc::tc;
 
 constexpr int BM = 128, BK = 128;
-constexpr int THREADS = 512;
-constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 8;
+constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 16, MORE_X_WARP = 24;
+constexpr int X_WARPS = 6, THREADS = 32 * (MORE_X_WARP + X_WARPS - 2);
 constexpr int STAGE_A = BM * BK;
-constexpr int RING_BYTES = 172 * 1024, MAX_STAGES = 7;
+constexpr int RING_BYTES = 168 * 1024, MAX_STAGES = 7;
 // tensor memory: accumulators at 0 and ACC_BN (one, where a tile is wider), then a
 // ring of scale words: a batch holds, for each WORD_KB blocks, 4 columns for x and
 // 8 for W
@@ -47,8 +51,13 @@ struct Tables {
   unsigned long long parts[THREADS / 32];
 };
 constexpr int TOPS_BYTES = 2 * EPI_WARPS * 32 * 4;
-constexpr size_t SMEM_BYTES = size_t(RING_BYTES) + EPI_WARPS * CHUNK_STAGING + SCALE_BYTES +
-                              TOPS_BYTES + sizeof(Tables) + 1024 + 256;
+constexpr int CHUNKS = MAX_BN / 128;  // of an epilogue warp, at most
+constexpr int BIAS_BYTES = EPI_WARPS * CHUNKS * 32 * 4;
+constexpr int FOURS = X_WARPS * ((BM / 4 + X_WARPS - 1) / X_WARPS);  // of rows of x
+constexpr int STAGING = 32 * 64;  // of an epilogue warp: 32 rows of 64 bytes
+constexpr size_t SMEM_BYTES = size_t(RING_BYTES) + EPI_WARPS * STAGING + SCALE_BYTES +
+                              TOPS_BYTES + BIAS_BYTES + FOURS * 16 +
+                              sizeof(Tables) + 1024 + 256;
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 static_assert(MAX_BN * 129 * 4 <= RING_BYTES, "a split tile's part");
 
@@ -68,27 +77,100 @@ struct TypeOf<F32> { typedef float T; };
 template <>
 struct TypeOf<CODES> { typedef uint8_t T; };
 
-// v / (1 + 2^e).  Quotient and power on the special-function unit are good to a
-// few steps of f32.
-__device__ __forceinline__ float over_one_plus(float v, float e) {
-  return __fdividef(v, 1.f + ex2_ftz(e));
+// v / (1 + 2^e) of four values with one reciprocal, of the product of the
+// denominators: the special-function unit, a power and a reciprocal each, is what
+// the epilogue waits for.  e is cut to 31, so that the product stays finite; what is
+// cut off is below 2^-31 of v.  Power and reciprocal are good to a few steps of f32.
+__device__ __forceinline__ void over_one_plus(float2& v, float2& w, float2 e, float2 f) {
+  const float2 a = f2_add(make_float2(ex2_ftz(fminf(e.x, 31.f)), ex2_ftz(fminf(e.y, 31.f))),
+                          f2_of(1.f));
+  const float2 b = f2_add(make_float2(ex2_ftz(fminf(f.x, 31.f)), ex2_ftz(fminf(f.y, 31.f))),
+                          f2_of(1.f));
+  const float2 c = f2_mul(a, b);  // (v.x's and w.x's denominators, v.y's and w.y's)
+  const float2 r = f2_mul(f2_of(rcp_ftz(c.x * c.y)), make_float2(c.y, c.x));
+  v = f2_mul(v, f2_mul(r, b));
+  w = f2_mul(w, f2_mul(r, a));
 }
 // GELU by its sigmoid: (1 + tanh a) / 2 = 1 / (1 + exp(-2 a)).
-__device__ __forceinline__ float act_gelu(float v) {
+__device__ __forceinline__ float2 gelu_power(float2 v) {
   const float k = -2.f * 0.7978845608028654f * 1.4426950408889634f;  // sqrt(2 / pi), log2 e
-  return over_one_plus(v, k * v * fmaf(0.044715f * v, v, 1.f));
+  return f2_mul(v, f2_fma(f2_mul(v, v), f2_of(0.044715f * k), f2_of(k)));
 }
-__device__ __forceinline__ float act_silu(float v) {
-  return over_one_plus(v, -1.4426950408889634f * v);
+__device__ __forceinline__ float2 silu_power(float2 v) {
+  return f2_mul(v, f2_of(-1.4426950408889634f));
+}
+template <int N, bool GELU>
+__device__ __forceinline__ void activate(float* v) {
+#pragma unroll
+  for (int j = 0; j < N; j += 4) {
+    float2 a = make_float2(v[j], v[j + 1]), b = make_float2(v[j + 2], v[j + 3]);
+    over_one_plus(a, b, GELU ? gelu_power(a) : silu_power(a), GELU ? gelu_power(b) : silu_power(b));
+    v[j] = a.x, v[j + 1] = a.y, v[j + 2] = b.x, v[j + 3] = b.y;
+  }
 }
 __device__ __forceinline__ float act_of(int act, float v) {
-  return act == RC_ACT_GELU ? act_gelu(v) : act == RC_ACT_SILU ? act_silu(v) : v;
+  float2 a = f2_of(v), b = f2_of(0.f);
+  if (act == RC_ACT_GELU) over_one_plus(a, b, gelu_power(a), b);
+  if (act == RC_ACT_SILU) over_one_plus(a, b, silu_power(a), b);
+  return a.x;
+}
+// Sums with their bias (in shared memory, 16-byte aligned).
+template <int N>
+__device__ __forceinline__ void add_bias(float* v, const float* bias) {
+#pragma unroll
+  for (int j = 0; j < N; j += 4) {
+    const float4 b = *reinterpret_cast<const float4*>(bias + j);
+    const float2 lo = f2_add(make_float2(v[j], v[j + 1]), make_float2(b.x, b.y));
+    const float2 hi = f2_add(make_float2(v[j + 2], v[j + 3]), make_float2(b.z, b.w));
+    v[j] = lo.x, v[j + 1] = lo.y, v[j + 2] = hi.x, v[j + 3] = hi.y;
+  }
 }
 
-// Barriers of the four scale warps, and of the two epilogue warps of a row.
+// A warp's 32 rows of 64 bytes to y by TMA, by way of its shared memory, in the
+// layout of a box with a swizzle as wide as its rows (which also keeps the writes free
+// of bank conflicts); what lies outside y is not written.  First `put_pieces`, N
+// pieces of 16 bytes from piece `k0` on (lane = row, `q` its bytes).
+template <int N>
+__device__ __forceinline__ void put_pieces(uint8_t* stg, int lane, int k0, const uint32_t* q) {
+  const uint32_t s0 = saddr(stg) + lane * 64;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                     s0 + 16 * ((k0 + k) ^ ((lane >> 1) & 3))),
+                 "r"(q[4 * k]), "r"(q[4 * k + 1]), "r"(q[4 * k + 2]), "r"(q[4 * k + 3])
+                 : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint8_t* stg, int lane, int r0,
+                                          int c0) {
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) tma_store_2d(map, saddr(stg), c0, r0);
+}
+// The box before has been read.
+__device__ __forceinline__ void box_free(int lane) {
+  if (lane == 0) tma_store_wait_read<0>();
+  __syncwarp();
+}
+// Sixteen columns (lane = row) of any alignment: the first `rows` rows and `cols`
+// columns at y, neighbouring lanes neighbouring columns.
+template <class T>
+__device__ __forceinline__ void write_columns(T* y, long long ldy, int rows, int cols,
+                                              uint8_t* stg, int lane, const float* v) {
+  box_free(lane);
+  float* s = reinterpret_cast<float*>(stg);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) s[lane * 16 + (j ^ (lane & 15))] = v[j];
+  __syncwarp();
+  const int c = lane & 15;
+  if (c < cols)
+    for (int r = lane >> 4; r < min(32, rows); r += 2) y[r * ldy + c] = T(s[r * 16 + (c ^ (r & 15))]);
+  __syncwarp();
+}
+
+// Barriers of the four scale warps, and of the four epilogue warps of a row.
 __device__ __forceinline__ void scale_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ void rows_sync(int sp) {
-  asm volatile("bar.sync %0, 64;" ::"r"(2 + sp) : "memory");
+  asm volatile("bar.sync %0, 128;" ::"r"(2 + sp) : "memory");
 }
 
 // How CTAs work together, as in rc_fp8_linear.  PAIRS: clusters of two share each
@@ -110,9 +192,11 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   uint8_t* stg = smem + RING_BYTES;
-  uint32_t* words = reinterpret_cast<uint32_t*>(stg + EPI_WARPS * CHUNK_STAGING);
+  uint32_t* words = reinterpret_cast<uint32_t*>(stg + EPI_WARPS * STAGING);
   uint32_t* tops = words + SCALE_BYTES / 4;
-  Tables& tab = *reinterpret_cast<Tables*>(tops + TOPS_BYTES / 4);
+  float* biases = reinterpret_cast<float*>(tops + TOPS_BYTES / 4);
+  int4* fours = reinterpret_cast<int4*>(biases + BIAS_BYTES / 4);
+  Tables& tab = *reinterpret_cast<Tables*>(fours + FOURS);
   uint64_t* bars = reinterpret_cast<uint64_t*>(&tab + 1);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 2 * SCALES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -125,7 +209,9 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   if (threadIdx.x == 0) {
     for (int s = 0; s < MAX_STAGES; ++s) {
       mbar_init(full0 + 8 * s, PAIR ? 1 : 2);  // (x's and W's loads)
-      mbar_init(empty0 + 8 * s, 1);
+      // (the MMAs, and x's warps, of which none gets a turn of the ring ahead or behind:
+      // some have nothing to load for a tile)
+      mbar_init(empty0 + 8 * s, 1 + X_WARPS);
     }
     for (int s = 0; s < SCALES; ++s) {
       mbar_init(sfull0 + 8 * s, 4 * CTAS);
@@ -133,7 +219,9 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(tfull0 + 8 * i, 1);
-      mbar_init(tempty0 + 8 * i, EPI_WARPS * CTAS);
+      // (of a pair, the second's warps are told of by its warp 1: an arrival in
+      // another CTA waits for the thread's stores)
+      mbar_init(tempty0 + 8 * i, EPI_WARPS + (PAIR && rank == 0 ? 1 : 0));
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -200,7 +288,6 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   const bool gated = a.act == RC_ACT_GATED_SILU;
   const int half_bn = BN / 2, cols_out = gated ? half_bn : BN;  // outputs of a tile
   const int e_rows = a.w.rows / a.experts, N = gated ? 2 * a.n : a.n;
-  const int tiles = m_tiles * pl.nt;
   // this CTA's (or pair's) tiles pos, pos + G .. and, of each, its blocks
   // k0 .. k0 + KB - 1
   const int parts = MODE == SPLIT ? pl.parts : 1;
@@ -209,18 +296,30 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   const int G = int(gridDim.x) / (CTAS * parts), pos = int(blockIdx.x) / (CTAS * parts);
   bool ok = true;
 
-  // tile t: its expert, first place, places left there and number among the columns
+  // The CTA's (or pair's) tiles, `step` apart: M tile (of all experts'), number among
+  // the columns and entry of the tables.
+  struct Walk { int q, n, i; };
+  const auto locate = [&](Walk& w) {
+    while (w.i + 8 < entries && tab.first[w.i + 8] <= w.q) w.i += 8;
+    while (w.i + 1 < entries && tab.first[w.i + 1] <= w.q) ++w.i;
+  };
+  const int step_q = G / pl.nt, step_n = G - step_q * pl.nt;
+  const auto first_tile = [&] {
+    Walk w{pos / pl.nt, pos % pl.nt, 0};
+    locate(w);
+    return w;
+  };
+  const auto next_tile = [&](Walk& w) {
+    w.q += step_q;
+    w.n += step_n;
+    if (w.n >= pl.nt) w.n -= pl.nt, ++w.q;
+    if (w.q < m_tiles) locate(w);
+  };
+  // a tile's expert, first place, places left there and number among the columns
   struct Tile { int expert, place, left, n; };
-  const auto tile_of = [&](int t) {
-    const int q = t / pl.nt;
-    int lo = 0, hi = entries;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (tab.first[mid] <= q) lo = mid;
-      else hi = mid;
-    }
-    const int p = tab.row[lo] + (q - tab.first[lo]) * TM;
-    return Tile{tab.expert[lo], p, tab.end[lo] - p, t - q * pl.nt};
+  const auto tile_of = [&](const Walk& w) {
+    const int p = tab.row[w.i] + (w.q - tab.first[w.i]) * TM;
+    return Tile{tab.expert[w.i], p, tab.end[w.i] - p, w.n};
   };
   // rows of a CTA of this tile (the second of a pair may have none)
   const auto rows_of = [&](const Tile& t, int r) { return max(0, min(BM, t.left - r * BM)); };
@@ -235,92 +334,127 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   // many neighbouring rows come as one box
   const auto in_box = [&](int rows) { return !a.source && rows > 32; };
 
-  if (warp == 0) {
-    // ---------------------------------------------------------------- TMA: x
-    int stage = 0;
-    uint32_t phase = 0;
-    for (int t = pos; ok && t < tiles; t += G) {
-      const Tile tl = tile_of(t);
-      const int rows = rows_of(tl, int(rank)), place = tl.place + int(rank) * BM;
-      const bool box = in_box(rows);
-      int r[4] = {0, 0, 0, 0};
-      if (!box) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (4 * lane + j < rows) r[j] = row_of(place + 4 * lane + j);
-      }
-      const auto bytes = [&](int n) { return in_box(n) ? STAGE_A : (n + 3) / 4 * 4 * BK; };
-      int expect = bytes(rows_of(tl, 0));
-      if (PAIR) expect += bytes(rows_of(tl, 1)) + BN * BK;
-      for (int kb = 0; kb < KB; ++kb) {
-        ok = __all_sync(~0u, mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag));
-        if (!ok) break;
-        const uint32_t st = saddr(smem + stage * STAGE), fb = full0 + 8 * stage;
-        const uint32_t bar = PAIR ? mapa_shared(fb, 0) : fb;
-        // (a barrier may see bytes before it is told of them: its phase still
-        // needs that arrival)
-        if (rank == 0 && lane == 0) mbar_expect_tx(fb, uint32_t(expect));
-        if (box) {
-          if (elect_one()) {
-            if (PAIR) tma_load_2d_pair(st, &tmX, bar, (k0 + kb) * BK, place);
-            else tma_load_2d(st, &tmX, bar, (k0 + kb) * BK, place);
-          }
-        } else if (4 * lane < rows) {
-          tma_gather4<PAIR>(st + lane * 4 * BK, &tmG, bar, (k0 + kb) * BK, r);
-        }
-        __syncwarp();
-        if (++stage == STAGES) { stage = 0; phase ^= 1; }
-      }
-    }
-  } else if (warp == 2) {
-    // ---------------------------------------------------------------- TMA: W
-    if (elect_one()) {
+  if (warp < SCALE_WARP || warp >= MORE_X_WARP) {
+    if (warp == 0 || warp == 3 || warp >= MORE_X_WARP) {
+      // ---------------------------------------------------------------- TMA: x
+      // The fours of rows are dealt to the warps; one thread of each issues them (a
+      // lane's own operands would be brought to uniform registers lane by lane).
+      // Lane i < MOST looks up the warp's i-th four, a tile ahead.
+      const int w = warp == 0 ? 0 : warp == 3 ? 1 : warp - MORE_X_WARP + 2;
+      constexpr int MOST = (BM / 4 + X_WARPS - 1) / X_WARPS;
+      int4* own = fours + w * MOST;
       int stage = 0;
       uint32_t phase = 0;
-      for (int t = pos; ok && t < tiles; t += G) {
-        const Tile tl = tile_of(t);
-        const int n0 = tl.expert * e_rows + tl.n * cols_out;
+      Walk wk = first_tile();
+      Tile tl = {};
+      int r[4];
+      const auto look_up = [&] {
+        tl = tile_of(wk);
+        const int rows = rows_of(tl, int(rank)), at = 4 * (w + X_WARPS * lane);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          r[j] = lane < MOST && at + j < rows ? row_of(tl.place + int(rank) * BM + at + j) : 0;
+      };
+      if (wk.q < m_tiles) look_up();
+      while (ok && wk.q < m_tiles) {
+        const int rows = rows_of(tl, int(rank)), place = tl.place + int(rank) * BM;
+        const bool box = in_box(rows);
+        const auto bytes = [&](int n) { return in_box(n) ? STAGE_A : (n + 3) / 4 * 4 * BK; };
+        int expect = bytes(rows_of(tl, 0));
+        if (PAIR) expect += bytes(rows_of(tl, 1)) + BN * BK;
+        if (lane < MOST) own[lane] = make_int4(r[0], r[1], r[2], r[3]);
+        __syncwarp();
+        int4 four[MOST];
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) four[i] = own[i];
+        __syncwarp();
+        next_tile(wk);
+        if (wk.q < m_tiles) look_up();
+#pragma unroll 1
         for (int kb = 0; kb < KB; ++kb) {
-          if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
-          const uint32_t st = saddr(smem + stage * STAGE) + STAGE_A, fb = full0 + 8 * stage;
-          const int c = (k0 + kb) * BK;
-          if (PAIR) {  // both CTAs' bytes land on rank 0's barrier (warp 0 told it of them)
-            tma_load_2d_pair(st, &tmW, mapa_shared(fb, 0), c,
-                             n0 + int(rank) * (gated ? a.n : half_bn));
-          } else {
-            mbar_expect_tx(fb, uint32_t(STAGE - STAGE_A));
-            tma_load_2d(st, &tmW, fb, c, n0);
-            if (gated) tma_load_2d(st + half_bn * BK, &tmW, fb, c, n0 + a.n);
+          ok = mbar_sleep_warp(empty0 + 8 * stage, phase ^ 1, abort_flag);
+          if (!ok) break;
+          if (elect_one()) {
+            const uint32_t st = saddr(smem + stage * STAGE), fb = full0 + 8 * stage;
+            const uint32_t bar = PAIR ? mapa_shared(fb, 0) : fb;
+            const int c = (k0 + kb) * BK;
+            // (a barrier may see bytes before it is told of them: its phase still
+            // needs that arrival)
+            if (rank == 0 && w == 0) mbar_expect_tx(fb, uint32_t(expect));
+            if (!box) {
+#pragma unroll
+              for (int i = 0; i < MOST; ++i)
+                if (4 * (w + X_WARPS * i) < rows)
+                  tma_gather4<PAIR>(st + (w + X_WARPS * i) * 4 * BK, &tmG, bar, c, four[i]);
+            } else if (w == 0) {
+              if (PAIR) tma_load_2d_pair(st, &tmX, bar, c, place);
+              else tma_load_2d(st, &tmX, bar, c, place);
+            }
+            mbar_arrive(empty0 + 8 * stage);
           }
+          __syncwarp();
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
       }
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
-    if (rank == 0 && elect_one()) {
-      const uint32_t idesc = IDESC_E4M3 | (uint32_t(BN >> 3) << 17) | (uint32_t(CTAS) << 27);
-      const uint64_t da = sw128_desc(saddr(smem)), db = sw128_desc(saddr(smem + STAGE_A));
-      int stage = 0, acc = 0, sc = 0;
-      uint32_t phase = 0, acc_phase = 0, sc_phase = 0;
-      uint64_t so = 0;     // the stage's offset in the descriptors' address field
-      bool ready = false;  // the current stage was seen full already
-      for (int t = pos; ok && t < tiles; t += G) {
-        if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
-        const uint32_t d = tmem + uint32_t(acc * ACC_BN);
-        uint32_t accumulate = 0;
-        for (int kb = 0; ok && kb < KB;) {
-          if (!mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
-          uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT);
-          const int end = min(kb + SCALE_BATCH, KB);
-          while (ok && kb < end) {
-#pragma unroll
-            for (int byte = 0; byte < WORD_KB; ++byte) {
-              if (kb >= end) break;
+    } else if (warp == 2) {
+      // ---------------------------------------------------------------- TMA: W
+      if (elect_one()) {
+        int stage = 0;
+        uint32_t phase = 0;
+        for (Walk wk = first_tile(); ok && wk.q < m_tiles; next_tile(wk)) {
+          const Tile tl = tile_of(wk);
+          const int n0 = tl.expert * e_rows + tl.n * cols_out;
+          for (int kb = 0; kb < KB; ++kb) {
+            if (!mbar_sleep(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
+            const uint32_t st = saddr(smem + stage * STAGE) + STAGE_A, fb = full0 + 8 * stage;
+            const int c = (k0 + kb) * BK;
+            if (PAIR) {  // both CTAs' bytes land on rank 0's barrier
+              tma_load_2d_pair(st, &tmW, mapa_shared(fb, 0), c,
+                               n0 + int(rank) * (gated ? a.n : half_bn));
+            } else {
+              mbar_expect_tx(fb, uint32_t(STAGE - STAGE_A));
+              tma_load_2d(st, &tmW, fb, c, n0);
+              if (gated) tma_load_2d(st + half_bn * BK, &tmW, fb, c, n0 + a.n);
+            }
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          }
+        }
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ MMA issuer
+      if (PAIR && rank == 1 && elect_one()) {
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (Walk wk = first_tile(); ok && wk.q < m_tiles; next_tile(wk)) {
+          ok = mbar_sleep(tempty0 + 8 * acc, acc_phase, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          tc_fence_before();
+          mbar_arrive_cluster(mapa_shared(tempty0 + 8 * acc, 0));
+          if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
+        }
+      }
+      if (rank == 0 && elect_one()) {
+        const uint32_t idesc = IDESC_E4M3 | (uint32_t(BN >> 3) << 17) | (uint32_t(CTAS) << 27);
+        const uint64_t da = sw128_desc(saddr(smem)), db = sw128_desc(saddr(smem + STAGE_A));
+        int stage = 0, acc = 0, sc = 0;
+        uint32_t phase = 0, acc_phase = 0, sc_phase = 0;
+        uint64_t so = 0;     // the stage's offset in the descriptors' address field
+        bool ready = false;  // the current stage was seen full already
+        for (Walk wk = first_tile(); ok && wk.q < m_tiles; next_tile(wk)) {
+          if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
+          const uint32_t d = tmem + uint32_t(acc * ACC_BN);
+          uint32_t accumulate = 0;
+          for (int kb = 0; ok && kb < KB;) {
+            if (!mbar_wait(sfull0 + 8 * sc, sc_phase, abort_flag)) { ok = false; break; }
+            uint32_t sa = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT);
+            const int end = min(kb + SCALE_BATCH, KB);
+            // (one copy of this loop: the roles' code together has to stay in the SM's
+            // instruction cache)
+            for (int byte = 0; kb < end; ++kb) {
               if (!ready && !mbar_wait(full0 + 8 * stage, phase, abort_flag)) { ok = false; break; }
               const uint64_t da_ = da + so, db_ = db + so;
               const uint32_t eb = empty0 + 8 * stage;
-              ++kb;
               so += uint64_t(STAGE >> 4);
               if (++stage == STAGES) { stage = 0; phase ^= 1; so = 0; }
               // (the next stage's test runs beside this one's MMAs)
@@ -337,21 +471,21 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
               }
               if (PAIR) umma_commit_pair(eb);
               else umma_commit(eb);
+              if (++byte == WORD_KB) byte = 0, sa += SCALE_STEP;
             }
-            sa += SCALE_STEP;
+            if (!ok) break;
+            if (PAIR) umma_commit_pair(sempty0 + 8 * sc);
+            else umma_commit(sempty0 + 8 * sc);
+            if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
           }
           if (!ok) break;
-          if (PAIR) umma_commit_pair(sempty0 + 8 * sc);
-          else umma_commit(sempty0 + 8 * sc);
-          if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
+          if (PAIR) umma_commit_pair(tfull0 + 8 * acc);
+          else umma_commit(tfull0 + 8 * acc);
+          if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
         }
-        if (!ok) break;
-        if (PAIR) umma_commit_pair(tfull0 + 8 * acc);
-        else umma_commit(tfull0 + 8 * acc);
-        if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
       }
     }
-  } else if (warp >= SCALE_WARP && warp < EPI_WARP) {
+  } else if (warp < EPI_WARP) {
     // -------------------------------------------------------- scale words
     // A thread loads a batch's bytes of one row of x, and 64 of them one byte of the
     // blocks of 128 rows of W that a tile can meet: two for each half of a gated
@@ -362,12 +496,12 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     const int slot = tid / SCALE_BATCH, u = tid % SCALE_BATCH, e_blocks = e_rows / 128;
     uint8_t bx[SCALE_BATCH], bw = 0;
     bool in = false;  // the thread's row is one of the expert's
-    int xrow = 0, t_of = -1;
+    int xrow = 0;
     Tile tl = {};
-    const auto fetch = [&](int t, int kb) {
-      if (t != t_of) {
-        t_of = t;
-        tl = tile_of(t);
+    Walk wk = first_tile();
+    const auto fetch = [&](int kb) {
+      if (kb == 0) {
+        tl = tile_of(wk);
         in = tid < rows_of(tl, int(rank));
         xrow = in ? row_of(tl.place + int(rank) * BM + tid) : 0;
       }
@@ -384,10 +518,10 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
                         tl.expert * e_blocks + block];
       }
     };
-    int sc = 0, t = pos, kb = 0;
+    int sc = 0, kb = 0;
     uint32_t sc_phase = 0;
-    if (t < tiles) fetch(t, kb);
-    while (t < tiles) {
+    if (wk.q < m_tiles) fetch(0);
+    while (wk.q < m_tiles) {
       scale_sync();  // (the batch before has been taken)
 #pragma unroll
       for (int g = 0; g < SCALE_GROUPS; ++g)
@@ -410,24 +544,24 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         of[i] = 128 + min(of[i], 3);
       }
       kb += SCALE_BATCH;
-      if (kb >= KB) { kb = 0; t += G; }
-      if (t < tiles) fetch(t, kb);
+      if (kb >= KB) kb = 0, next_tile(wk);
+      if (wk.q < m_tiles) fetch(kb);
       if (ok) ok = mbar_sleep(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
       // (after a failed wait the warp goes on to the barriers, without work)
       ok = __all_sync(0xffffffffu, ok);
       if (ok) {
         tc_fence_after();
-        uint32_t v[SCALE_SLOT];
-#pragma unroll
-        for (int g = 0; g < SCALE_GROUPS; ++g) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[g * SCALE_STEP + i] = words[g * SCALE_ROWS + 32 * i + lane];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[g * SCALE_STEP + 4 + i] = words[g * SCALE_ROWS + of[i]];
-        }
         const uint32_t ta = tmem + uint32_t(SCALE_COL + sc * SCALE_SLOT) + part;
-        tmem_st16(ta, v);
-        tmem_st32(ta + 16, v + 16);
+#pragma unroll 1
+        for (int g = 0; g < SCALE_GROUPS; ++g) {
+          uint32_t v[SCALE_STEP];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = words[g * SCALE_ROWS + 32 * i + lane];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[4 + i] = words[g * SCALE_ROWS + of[i]];
+          tmem_st4(ta + g * SCALE_STEP, v);
+          tmem_st8(ta + g * SCALE_STEP + 4, v + 4);
+        }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -438,162 +572,176 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       }
       if (++sc == SCALES) { sc = 0; sc_phase ^= 1; }
     }
-  } else if (warp >= EPI_WARP) {
+  } else {
     // ------------------------------------------------------------ epilogue
-    // A warp takes 32 rows (a quarter of the tile's) and half of the chunks of 32
-    // outputs: every second, or with codes every second pair, so that two warps
-    // hold the 128 columns of a scale between them.
-    const int sp = warp & 3, half = (warp - EPI_WARP) >> 2;
-    const uint32_t tempty_r0 = PAIR ? mapa_shared(tempty0, 0) : tempty0;
-    uint8_t* own = stg + (warp - EPI_WARP) * CHUNK_STAGING;
-    constexpr int BUFS = OUT == F32 ? 1 : 2;  // staging of this many chunks
-    constexpr int CHUNKS = MAX_BN / 64;
-    const auto chunk_of = [&](int i) {
-      return OUT == CODES ? (i >> 1) * 4 + half * 2 + (i & 1) : half + 2 * i;
-    };
+    // A warp takes 32 rows (a quarter of the tile's) and every fourth chunk of 32
+    // outputs, so that with codes four warps hold the 128 columns of a scale.  (With
+    // eight warps, two chunks' work under way for each scheduler: 16384 x 2 rows, 1152 x
+    // 4608 with GELU, 259 us.)
+    const int sp = warp & 3, part = (warp - EPI_WARP) >> 2;
+    uint8_t* own = stg + (warp - EPI_WARP) * STAGING;
+    float* own_bias = biases + (warp - EPI_WARP) * CHUNKS * 32;
     T* const y = static_cast<T*>(OUT == CODES ? a.y8.codes : a.y);
     const int ldy = OUT == CODES ? a.y8.ld : a.ldy;
-    int acc = 0, buf = 0, turn = 0;
-    uint32_t acc_phase = 0;
-    for (int t = pos; t < tiles; t += G) {
-      const Tile tl = tile_of(t);
-      const int left = rows_of(tl, int(rank)) - sp * 32;  // the warp's rows, from `r0`
-      const int r0 = tl.place + int(rank) * BM + sp * 32;
-      // (the bias before the accumulator is ready)
-      float ba[CHUNKS], bb[CHUNKS];
+    // the bias of a lane's columns (of a gated tile, a chunk's and then that of the
+    // factors), a tile ahead
+    Walk wk = first_tile();
+    Tile tl = {};
+    float bias[CHUNKS];
+    const auto fetch = [&] {
+      tl = tile_of(wk);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
-        const int ch = chunk_of(i), c = tl.n * cols_out + ch * 32 + lane;
-        const bool there = a.bias && ch * 32 < cols_out && c < a.n;
-        ba[i] = there ? __ldg(a.bias + (long long)tl.expert * N + c) : 0.f;
-        bb[i] = there && gated ? __ldg(a.bias + (long long)tl.expert * N + a.n + c) : 0.f;
+        const int ch = gated ? part : part + 4 * i, c = tl.n * cols_out + ch * 32 + lane;
+        bias[i] = 0.f;
+        if (a.bias && ch * 32 < cols_out && c < a.n)
+          bias[i] = __ldg(a.bias + (long long)tl.expert * N + c + (gated && i > 0 ? a.n : 0));
       }
+    };
+    int acc = 0, turn = 0;
+    uint32_t acc_phase = 0;
+    if (wk.q < m_tiles) fetch();
+    while (wk.q < m_tiles) {
+      const int left = rows_of(tl, int(rank)) - sp * 32;  // the warp's rows, from `r0`
+      const int r0 = tl.place + int(rank) * BM + sp * 32, n0 = tl.n * cols_out;
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) own_bias[i * 32 + lane] = bias[i];
+      __syncwarp();
+      next_tile(wk);
+      if (wk.q < m_tiles) fetch();
+      // the warp's chunks that hold outputs (with codes, all four of a scale's columns)
+      int chunks = 0;
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i)
+        if (left > 0 && (part + 4 * i) * 32 < cols_out &&
+            n0 + (OUT == CODES ? 4 * i : part + 4 * i) * 32 < a.n)
+          chunks = i + 1;
       if (ok) ok = mbar_sleep_warp(tfull0 + 8 * acc, acc_phase, abort_flag);
       // (after a failed wait the warp goes on to the barriers, without work)
       tc_fence_after();
       const uint32_t tb = tmem + uint32_t(acc * ACC_BN) + (uint32_t(sp * 32) << 16);
-      // the outputs of chunk i (all 32 rows of the warp)
-      const auto outputs = [&](int i, float* v) {
-        const int ch = chunk_of(i);
-        tmem_ld32(tb + uint32_t(ch * 32), v);
-        if (a.bias)
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, ba[i], j);
+      const auto release = [&] {  // (what the warp had to read of the accumulator is read)
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0 && ok) mbar_arrive(tempty0 + 8 * acc);
+      };
+      // sixteen outputs from column `h` of chunk i on (all 32 rows of the warp)
+      const auto outputs = [&](int i, int h, float* v) {
+        const uint32_t at = tb + uint32_t((part + 4 * i) * 32 + h);
+        const bool last = OUT != CODES && h == 16 && i == chunks - 1;
+        tmem_ld16(at, v);
         if (gated) {
-          float w[32];
-          tmem_ld32(tb + uint32_t(half_bn + ch * 32), w);
+          add_bias<16>(v, own_bias + h);
+          activate<16, false>(v);
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            v[j] = act_silu(v[j]) * (w[j] + __shfl_sync(0xffffffffu, bb[i], j));
-        } else if (a.act != RC_ACT_NONE) {
+          for (int k = 0; k < 16; k += 8) {  // (few registers at a time)
+            float w[8];
+            tmem_ld8(at + uint32_t(half_bn + k), w);
+            if (k == 8 && last) release();
+            add_bias<8>(w, own_bias + 32 + h + k);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = act_of(a.act, v[j]);
+            for (int j = 0; j < 8; j += 2) {
+              const float2 o = f2_mul(make_float2(v[k + j], v[k + j + 1]),
+                                      make_float2(w[j], w[j + 1]));
+              v[k + j] = o.x, v[k + j + 1] = o.y;
+            }
+          }
+        } else {
+          if (last) release();
+          add_bias<16>(v, own_bias + i * 32 + h);
+          if (a.act == RC_ACT_GELU) activate<16, true>(v);
+          else if (a.act == RC_ACT_SILU) activate<16, false>(v);
         }
       };
       if (MODE == SPLIT) {  // (every MMA is done: the operand ring is free)
         float* to = reinterpret_cast<float*>(smem) + sp * 32 + lane;
-        for (int ch = half; ok && left > 0 && ch < BN / 32; ch += 2) {
+        for (int ch = part; ok && left > 0 && ch < BN / 32; ch += 4) {
           float v[32];
           tmem_ld32(tb + uint32_t(ch * 32), v);
           if (lane < left)
 #pragma unroll
             for (int j = 0; j < 32; ++j) to[(ch * 32 + j) * 129] = v[j];
         }
-      } else if constexpr (OUT == CODES) {
+      } else if (chunks == 0) {
+        release();
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < chunks; ++i) {  // (with codes, the four warps of the rows alike)
+          const int c0 = n0 + (part + 4 * i) * 32;
+          if constexpr (OUT == CODES) {
+            // the outputs go back to where their sums were until the scale is known
+            const uint32_t at = tb + uint32_t((part + 4 * i) * 32);
+            uint32_t top = 0;
+#pragma unroll 1
+            for (int h = 0; ok && h < 32; h += 16) {
+              float v[16];
+              outputs(i, h, v);
 #pragma unroll
-        for (int g = 0; g < CHUNKS / 2; ++g) {
-          const int c0 = tl.n * cols_out + g * 128;
-          if (left <= 0 || g * 128 >= cols_out || c0 >= a.n) break;  // (both warps alike)
-          float v[2][32];
-          uint32_t top = 0;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (ok) outputs(2 * g + i, v[i]);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (c0 + (half * 2 + i) * 32 + j >= a.n) v[i][j] = 0.f;
-              top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+              for (int j = 0; j < 16; ++j) {
+                if (c0 + h + j >= a.n) v[j] = 0.f;
+                top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+              }
+              tmem_st16(at + uint32_t(h), reinterpret_cast<const uint32_t*>(v));
             }
-          }
-          uint32_t* to = tops + turn * EPI_WARPS * 32;
-          to[(warp - EPI_WARP) * 32 + lane] = top;
-          rows_sync(sp);
-          top = max(top, to[((warp - EPI_WARP) ^ 4) * 32 + lane]);
-          turn ^= 1;
-          if (!ok) continue;
-          const int b = scale_byte(top);
-          const uint64_t inv = both(scale_inverse(b));
-          if (half == 0 && lane < left)
-            a.y8.scales[(long long)(c0 / 128) * a.y8.lds + r0 + lane] = uint8_t(b);
-          uint4 q[4];
+            tmem_wait_st();
+            uint32_t* to = tops + turn * EPI_WARPS * 32 + sp * 32 + lane;
+            to[part * 128] = top;
+            rows_sync(sp);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t w[4];
+            for (int k = 0; k < 4; ++k) top = max(top, to[k * 128]);
+            turn ^= 1;
+            if (!ok) continue;
+            const int b = scale_byte(top);
+            const uint64_t inv = both(scale_inverse(b));
+            if (part == 0 && lane < left)
+              a.y8.scales[(long long)(c0 / 128) * a.y8.lds + r0 + lane] = uint8_t(b);
+            uint8_t* dst = y + (long long)(r0 + lane) * ldy + c0;
+#pragma unroll 1
+            for (int h = 0; h < 32; h += 16, dst += 16) {
+              float v[16];
+              tmem_ld16(at + uint32_t(h), v);
+              if (h == 16 && i == chunks - 1) release();
+              uint32_t q[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float* s = v[k >> 1] + 16 * (k & 1) + 4 * j;
-              w[j] = __byte_perm(e4m3x2(s[0], s[1], inv), e4m3x2(s[2], s[3], inv), 0x5410);
+              for (int k = 0; k < 4; ++k)
+                q[k] = __byte_perm(e4m3x2(v[4 * k], v[4 * k + 1], inv),
+                                   e4m3x2(v[4 * k + 2], v[4 * k + 3], inv), 0x5410);
+              if (lane < left && c0 + h + 16 <= a.n) {
+                *reinterpret_cast<uint4*>(dst) = make_uint4(q[0], q[1], q[2], q[3]);
+              } else if (lane < left) {
+#pragma unroll
+                for (int j = 0; j < 15; ++j)
+                  if (c0 + h + j < a.n) dst[j] = uint8_t(q[j >> 2] >> (8 * (j & 3)));
+              }
             }
-            q[k] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          const int c = c0 + half * 64;
-          // (64 codes are as wide as 32 bf16 values; a box of bytes that crosses the last
-          // column is cut off at 16 of them only)
-          if (left >= 32 && (c + 64 <= a.n || a.n % 16 == 0)) {
-            if (lane == 0) tma_store_wait_read<BUFS - 1>();  // this buffer's chunk has been read
-            __syncwarp();
-            const uint32_t s0 = saddr(own + buf * (CHUNK_STAGING / 2));
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                               s0 + lane * 64 + 16 * (k ^ ((lane >> 1) & 3))),
-                           "r"(q[k].x), "r"(q[k].y), "r"(q[k].z), "r"(q[k].w)
-                           : "memory");
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0 && c < a.n) tma_store_2d(&tmY, s0, c, r0);
-            buf ^= 1;
-          } else if (lane < left) {
-            uint8_t* dst = y + (long long)(r0 + lane) * ldy + c;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int n = a.n - c - 16 * k;
-              if (n >= 16) {
-                *reinterpret_cast<uint4*>(dst + 16 * k) = q[k];
+          } else {
+            if (!ok) break;
+            const bool box = a.tma && left >= 32;
+#pragma unroll 1
+            for (int h = 0; h < 32; h += 16) {
+              float v[16];
+              outputs(i, h, v);
+              if (!box) {
+                if (c0 + h < a.n)
+                  write_columns(y + (long long)r0 * ldy + c0 + h, ldy, left, a.n - c0 - h, own,
+                                lane, v);
+                continue;
+              }
+              if (OUT == F32 || h == 0) box_free(lane);
+              if constexpr (OUT == F32) {
+                put_pieces<4>(own, lane, 0, reinterpret_cast<const uint32_t*>(v));
+                if (c0 + h < a.n) store_box(&tmY, own, lane, r0, c0 + h);
               } else {
-                const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+                uint32_t q[8];
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                  if (j < n) dst[16 * k + j] = uint8_t(w[j >> 2] >> (8 * (j & 3)));
+                for (int k = 0; k < 8; ++k) q[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+                put_pieces<2>(own, lane, h / 8, q);
+                if (h == 16) store_box(&tmY, own, lane, r0, c0);
               }
             }
           }
         }
-      } else if (ok) {
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) {
-          const int ch = chunk_of(i), c0 = tl.n * cols_out + ch * 32;
-          if (left <= 0 || ch * 32 >= cols_out || c0 >= a.n) break;
-          float v[32];
-          outputs(i, v);
-          if (a.tma && left >= 32) {
-            if (lane == 0) tma_store_wait_read<BUFS - 1>();  // this buffer's chunk has been read
-            __syncwarp();
-            store_chunk<T>(&tmY, own + buf * (CHUNK_STAGING / 2), lane, v, r0, c0);
-            if (BUFS == 2) buf ^= 1;
-          } else {
-            // (an earlier chunk may still be read from where this one goes)
-            if (lane == 0) tma_store_wait_read<0>();
-            __syncwarp();
-            write_chunk(y + (long long)r0 * ldy + c0, ldy, left, a.n - c0, own, lane, v);
-          }
-        }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0 && ok) {
-        if (PAIR) mbar_arrive_cluster(tempty_r0 + 8 * acc);
-        else mbar_arrive(tempty0 + 8 * acc);
       }
       if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
     }
@@ -601,9 +749,10 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   }
   if (MODE == SPLIT) {
     cluster_sync();
-    if (pos < tiles) {
+    const Walk wk = first_tile();
+    if (wk.q < m_tiles) {
       // the rows' chunks of 32 outputs (128 with codes), dealt to the cluster's warps
-      const Tile tl = tile_of(pos);
+      const Tile tl = tile_of(wk);
       const int rows = rows_of(tl, 0);
       constexpr int LANES = OUT == CODES ? 4 : 1;  // columns of a lane
       const int chunks = cols_out / (32 * LANES);
@@ -630,7 +779,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
           if (c >= a.n) continue;
           const float* b = a.bias ? a.bias + (long long)tl.expert * N + c : nullptr;
           v[i] = sum(col, row) + (b ? __ldg(b) : 0.f);
-          v[i] = gated ? act_silu(v[i]) * (sum(half_bn + col, row) + (b ? __ldg(b + a.n) : 0.f))
+          v[i] = gated ? act_of(RC_ACT_SILU, v[i]) * (sum(half_bn + col, row) + (b ? __ldg(b + a.n) : 0.f))
                        : act_of(a.act, v[i]);
         }
         if constexpr (OUT == CODES) {
@@ -670,16 +819,18 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 
 constexpr int SMS = 152;
 
-// Codes [rows][n] in boxes of 64 x 32 whose rows are swizzled over their own width.
-cudaError_t tma_map_codes(const Fp8Mat& y, int rows, CUtensorMap* out) {
+// y [rows][n] in boxes of 64 bytes x 32 rows, swizzled over their own width.
+template <class T>
+cudaError_t tma_map_boxes(T* y, int rows, int n, int ld, CUtensorMap* out) {
   auto fn = tma_encode_fn();
   if (!fn) return cudaErrorNotSupported;
-  const cuuint64_t dims[2] = {cuuint64_t(y.cols), cuuint64_t(rows)};
-  const cuuint64_t strides[1] = {cuuint64_t(y.ld)};
-  const cuuint32_t box[2] = {64, 32}, es[2] = {1, 1};
-  const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y.codes, dims, strides, box, es,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
-                        CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint64_t dims[2] = {cuuint64_t(n), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {cuuint64_t(ld) * sizeof(T)};
+  const cuuint32_t box[2] = {cuuint32_t(64 / sizeof(T)), 32}, es[2] = {1, 1};
+  const CUresult r =
+      fn(out, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+         2, y, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+         CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
@@ -719,12 +870,10 @@ cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
   RC_TRY(tma_map_bytes(a.x.codes, a.x.rows, a.x.cols, a.x.ld, 1, &mg));
   RC_TRY(tma_map_bytes(a.w.codes, a.w.rows, a.w.cols, a.w.ld, PAIR || gated ? bn / 2 : bn, &mw));
   my = mx;  // (not used without tma)
-  if constexpr (OUT == CODES) {
-    RC_TRY(tma_map_codes(a.y8, a.pairs, &my));
-  } else {
+  if constexpr (OUT != CODES) {
     const uintptr_t row = uintptr_t(a.ldy) * sizeof(T);
     a.tma = ((reinterpret_cast<uintptr_t>(a.y) | row) & 15u) == 0;
-    if (a.tma) RC_TRY(tma_map_chunks(static_cast<T*>(a.y), a.pairs, a.n, a.ldy, &my));
+    if (a.tma) RC_TRY(tma_map_boxes(static_cast<T*>(a.y), a.pairs, a.n, a.ldy, &my));
   }
   count_launches(1);
   const int cluster = PAIR ? 2 : ch.parts, slots = SMS / cluster;

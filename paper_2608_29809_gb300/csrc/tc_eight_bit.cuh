@@ -15,30 +15,51 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
       : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// All but the thread's last N bulk groups have read their shared memory.
+template <int N>
+__device__ __forceinline__ void tma_store_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+
 // Four rows of a matrix (a map whose box is one row high), one below the other in
 // this CTA's shared memory; their bytes are counted by `bar`, of PAIR either CTA's.
 template <bool PAIR>
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, uint32_t bar,
-                                            int x, const int* rows) {
+                                            int x, int4 rows) {
   if (PAIR)
     asm volatile(
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
         ".mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(rows[0]), "r"(rows[1]),
-        "r"(rows[2]), "r"(rows[3])
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(rows.x), "r"(rows.y),
+        "r"(rows.z), "r"(rows.w)
         : "memory");
   else
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4"
         ".mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(rows[0]), "r"(rows[1]),
-        "r"(rows[2]), "r"(rows[3])
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(rows.x), "r"(rows.y),
+        "r"(rows.z), "r"(rows.w)
         : "memory");
 }
-// All but the thread's last N bulk groups have read their shared memory.
-template <int N>
-__device__ __forceinline__ void tma_store_wait_read() {
-  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+// Eight and sixteen f32 columns of this thread's TMEM lane, and four words to it.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
+  uint32_t r[8];
+  tmem_ld8_nowait(taddr, r);
+  tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+  uint32_t r[16];
+  tmem_ld16_nowait(taddr, r);
+  tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
 }
 
 // D (+)= A B of e4m3 tiles (K-major, 32 columns), each row's products times
