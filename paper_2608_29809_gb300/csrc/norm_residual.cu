@@ -6,15 +6,17 @@
 #include "common.cuh"
 #include "fp8.cuh"
 
+#include <type_traits>
+
 namespace rc {
 
 namespace {
 
-// A row is dealt in vectors of eight columns: thread t of the row's TPR holds
-// vectors t, t + TPR ..  (NV at most), from the first load to the last store, so
-// x and h are read once; the sums of a norm go through the registers that hold
-// the row (its variance is that of the differences from the mean, two passes
-// there).  Sixteen neighbouring threads hold the 128 columns of a scale.
+// A row is dealt in vectors of eight columns to a CTA's threads, which hold them from
+// the first load to the last store, so x and h are read once; the sums of a norm go
+// through the registers that hold the row (its variance is that of the differences
+// from the mean, two passes there).  Sixteen neighbouring threads hold the 128 columns
+// of a scale.
 __device__ __forceinline__ void unpack(const Eight<bf16>& e, float* v) {
   const uint32_t w[4] = {e.u.x, e.u.y, e.u.z, e.u.w};
 #pragma unroll
@@ -66,12 +68,11 @@ __device__ __forceinline__ void store(float* p, const float* v, int n, bool wide
   }
 }
 
-// Sum over the row's threads; `slots` of the CTA's warps (TPR > 32), used in
-// turn so that one barrier a sum is enough.
+// Sum over the row's threads; `slots` of the CTA's warps, used in turn so that one
+// barrier a sum is enough.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float (*slots)[16], int& turn) {
   v = warp_sum(v);
-  if (TPR == 32) return v;
   const int warp = threadIdx.x >> 5;
   if ((threadIdx.x & 31) == 0) slots[turn][warp] = v;
   __syncthreads();
@@ -117,11 +118,23 @@ __device__ __forceinline__ void normalise(const NormOf& o, float (*v)[8], int t,
   }
 }
 
-// The item that owns `row`, -1 for none, by the whole warp: the last offset that is
-// not above the row, a thirty-second of the list at a time.
-__device__ __forceinline__ int item_of(const int* offsets, int n_items, int rows, int row) {
+// The item that owns `row` (-1 for none) and the first row behind it that may have
+// another, by the whole warp: the last offset that is not above the row, a
+// thirty-second of the list at a time.
+__device__ __forceinline__ int item_of(const int* offsets, int n_items, int rows, int row,
+                                       int& end) {
   const int lane = threadIdx.x & 31;
   int lo = 0, len = n_items;
+  end = row + 1;
+  if (n_items < 32) {  // (all of it with one load)
+    const int v = lane <= n_items ? offsets[lane] : 0;
+    const int last = 31 - __clz(int(__ballot_sync(0xffffffffu, lane < n_items && v <= row)));
+    const int first = __shfl_sync(0xffffffffu, v, max(last, 0));
+    const int behind = __shfl_sync(0xffffffffu, v, max(last, 0) + 1);
+    if (last < 0 || first < 0 || row >= behind || behind > rows) return -1;
+    end = behind;
+    return last;
+  }
   while (len > 1) {
     const int step = (len - 1) / 32 + 1;
     const long long at = (long long)lane * step;
@@ -131,32 +144,351 @@ __device__ __forceinline__ int item_of(const int* offsets, int n_items, int rows
     lo += last * step;
     len = min(step, len - last * step);
   }
-  const int first = offsets[lo], end = offsets[lo + 1];
-  return first >= 0 && first <= row && row < end && end <= rows ? lo : -1;
+  const int first = offsets[lo], behind = offsets[lo + 1];
+  if (first < 0 || first > row || row >= behind || behind > rows) return -1;
+  end = behind;
+  return lo;
+}
+// Offsets that are not in order are reported (one CTA).
+__device__ __forceinline__ void check_offsets(const ResidualArgs& a) {
+  for (int i = threadIdx.x; i < a.n_items; i += blockDim.x)
+    if (a.row_offsets[i] < 0 || a.row_offsets[i] > a.row_offsets[i + 1] ||
+        a.row_offsets[i + 1] > a.rows)
+      atomicOr(a.err, DEVERR_COUNT);
+}
+template <class T>
+__device__ __forceinline__ bool wide_rows(const T* p, long long ld) {
+  return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld * sizeof(T))) & 15) == 0;
+}
+// Eight (n) outputs of a row as codes; sixteen neighbouring threads hold the columns
+// of a scale (n <= 0: a thread without columns).
+__device__ __forceinline__ void store_codes(const Fp8Mat& y, long long row, int c, int n,
+                                            const float* v) {
+  Eight<float> e;
+  e.a = make_float4(v[0], v[1], v[2], v[3]);
+  e.b = make_float4(v[4], v[5], v[6], v[7]);
+  if (n <= 0) e.zero();
+  uint32_t top = e.top();
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const int b = scale_byte(top);
+  const uint2 q = e.codes(scale_inverse(b));
+  uint8_t* dst = y.codes + row * y.ld + c;
+  if (n >= 8) {
+    *reinterpret_cast<uint2*>(dst) = q;
+  } else {
+    for (int k = 0; k < n; ++k) dst[k] = uint8_t((k < 4 ? q.x : q.y) >> (8 * (k & 3)));
+  }
+  if (n > 0 && (c & 127) == 0) y.scales[(long long)(c / 128) * y.lds + row] = uint8_t(b);
+}
+__device__ __forceinline__ void store_y(const ResidualArgs& a, long long row, int c, int n,
+                                        const float* v) {
+  if (a.y8.codes) {
+    store_codes(a.y8, row, c, n, v);
+  } else if (n > 0 && a.y_f32) {
+    float* y = static_cast<float*>(a.y);
+    store(y + row * a.ldy + c, v, n, wide_rows(y, a.ldy));
+  } else if (n > 0) {
+    bf16* y = static_cast<bf16*>(a.y);
+    store(y + row * a.ldy + c, v, n, wide_rows(y, a.ldy));
+  }
 }
 
+// Rows of up to 8 columns a thread of the CTA (cols <= 5120).  A CTA takes neighbouring
+// rows, two at a time: their sums share barriers and shuffles, the next four are on
+// their way into shared memory meanwhile, and what the columns' values are multiplied
+// with and added to (weights, biases and the item's modulation, folded into one factor
+// and one term for each of the two norms) stays in registers until the item changes.
+// Two columns an instruction throughout.  Bound by memory where rows are many (16384 x
+// 4608 bf16 94 us, 6.4 TB/s; two instructions in three were tests and scalar
+// arithmetic before: 219 us, and a row for each 128 threads with its parameters
+// read anew 237), and by the first rows' way where a CTA has ten (4128 x 1152
+// f32 15.1 us for 8.4 of traffic; it was 27.4).
+constexpr int ROWS = 2;
+// Sums of both rows over the CTA's threads: the lower sixteen lanes end up with the
+// first row's, the upper ones with the second's, of the warp and then of all warps.
+__device__ __forceinline__ void sums(float (&v)[2], float (*slots)[2][32], int& turn) {
+  const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15;
+  float s = half ? v[1] : v[0];
+  s += __shfl_xor_sync(0xffffffffu, half ? v[0] : v[1], 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (l == 0) slots[turn][half][threadIdx.x >> 5] = s;
+  __syncthreads();
+  // (slots of warps that there are not hold zeros)
+  s = slots[turn][half][l] + slots[turn][half][l + 16];
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const float other = __shfl_xor_sync(0xffffffffu, s, 16);
+  v[0] = half ? other : s, v[1] = half ? s : other;
+  turn ^= 1;
+}
+// v - mean of the rows' columns, and 1 / root of each row; part = 1 / cols.  n of the
+// thread's columns are in the row and the others hold zeros; they do again, but where
+// vectors are WHOLE: then a thread without columns is of no consequence.
+template <bool WHOLE>
+__device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], float (&root)[2],
+                                            int n, float cols, float part,
+                                            float (*slots)[2][32], int& turn) {
+  root[0] = root[1] = 1.f;
+  if (o.kind == RC_NORM_NONE) return;
+  float s[2];
+  if (o.kind == RC_NORM_LAYER) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float2 t = f2_add(f2_add(v[r][0], v[r][1]), f2_add(v[r][2], v[r][3]));
+      s[r] = t.x + t.y;
+    }
+    sums(s, slots, turn);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      // the quotient s / cols (exact for a constant row)
+      float m = s[r] * part;
+      m = fmaf(fmaf(-m, cols, s[r]), part, m);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 d = f2_add(v[r][k], f2_of(-m));
+        v[r][k] = WHOLE ? d : make_float2(2 * k < n ? d.x : 0.f, 2 * k + 1 < n ? d.y : 0.f);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    float2 t = f2_mul(v[r][0], v[r][0]);
+#pragma unroll
+    for (int k = 1; k < 4; ++k) t = f2_fma(v[r][k], v[r][k], t);
+    s[r] = WHOLE && n <= 0 ? 0.f : t.x + t.y;
+  }
+  sums(s, slots, turn);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) root[r] = rsqrtf(fmaf(s[r], part, o.eps));
+}
+// A thread's eight (n) columns of a row into its place in shared memory: under way,
+// or there where the row is not aligned or too short for that.
+template <class T>
+__device__ __forceinline__ void stage(Eight<T>* to, const T* p, int n, bool wide) {
+  if (wide && n >= 8) {
+#pragma unroll
+    for (int k = 0; k < int(sizeof(T)) / 2; ++k)
+      copy_16(reinterpret_cast<uint4*>(to) + k, reinterpret_cast<const uint4*>(p) + k);
+  } else {
+    Eight<T> e;
+    load(e, p, n, false);
+    *to = e;
+  }
+}
+// Batches of rows of a CTA under way or in use.
+template <class TX, class TH, int THREADS>
+constexpr int depth() {
+  return THREADS > 256 && sizeof(TX) + sizeof(TH) == 8 ? 2 : 3;
+}
+__device__ __forceinline__ void pairs_of(const float* u, float2* v) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = make_float2(u[2 * k], u[2 * k + 1]);
+}
+
+// TY: bf16 or float where x, h, x_out and y (of that type) are all there with whole,
+// aligned vectors and no places; void for everything else (the tests of what there
+// is, for each vector, took half of the instructions).
+template <class TX, class TH, class TY, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 2 : 1)
+norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
+  constexpr bool PLAIN = !std::is_void<TY>::value;
+  constexpr int DEPTH = depth<TX, TH, THREADS>();
+  extern __shared__ uint4 staged[];  // [DEPTH][ROWS][threads] of x, then of h
+  __shared__ float slots[2][2][32];
+  for (int i = threadIdx.x; i < 128; i += blockDim.x) (&slots[0][0][0])[i] = 0.f;
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  if (a.row_offsets && blockIdx.x == 0) check_offsets(a);
+  const int c = threadIdx.x * 8, n = a.cols - c;
+  const TX* x = static_cast<const TX*>(a.x);
+  const TH* h = static_cast<const TH*>(a.h);
+  TX* x_out = static_cast<TX*>(a.x_out);
+  const bool wide_x = wide_rows(x, a.ldx), wide_h = wide_rows(h, a.ldh),
+             wide_out = wide_rows(x_out, a.ldx_out);
+  const int last = int((long long)(blockIdx.x + 1) * a.rows / gridDim.x);
+  int row = int((long long)blockIdx.x * a.rows / gridDim.x), end = row, item = -1, turn = 0;
+  Eight<TX>* sx = reinterpret_cast<Eight<TX>*>(staged) + threadIdx.x;
+  Eight<TH>* sh = reinterpret_cast<Eight<TH>*>(reinterpret_cast<Eight<TX>*>(staged) +
+                                               DEPTH * ROWS * blockDim.x) + threadIdx.x;
+  const bool own_h = h && a.top_k == 0;
+  // rows are staged in order, a group of copies for each; `to` and `at` are the places
+  // of the next to be staged and to be read (in rows of the CTA's threads)
+  const int step = blockDim.x, places = DEPTH * ROWS * step;
+  int staged_to = row, to = 0, at = 0;
+  const TX* px = x + (long long)row * a.ldx + c;
+  const TH* ph = h + (long long)row * a.ldh + c;
+  const auto fetch = [&] {
+    if (staged_to < last && n > 0) {
+      if (PLAIN) {
+        stage(sx + to, px, 8, true), stage(sh + to, ph, 8, true);
+      } else {
+        if (x) stage(sx + to, px, n, wide_x);
+        if (own_h) stage(sh + to, ph, n, wide_h);
+      }
+    }
+    copy_commit();
+    ++staged_to;
+    px += a.ldx, ph += a.ldh;
+    to += step;
+    if (to == places) to = 0;
+  };
+  // (threads without columns, and those of what there is not, read zeros)
+#pragma unroll 1
+  for (int i = 0; i < DEPTH * ROWS; ++i) {
+    Eight<TX> zx;
+    Eight<TH> zh;
+    zx.zero(), zh.zero();
+    if (n <= 0 || !x) sx[i * step] = zx;
+    if (n <= 0 || !own_h) sh[i * step] = zh;
+  }
+#pragma unroll 1
+  for (int i = 0; i < DEPTH * ROWS; ++i) fetch();
+  TX* po = x_out + (long long)row * a.ldx_out + c;
+  const bool codes = a.y8.codes, y_wide = a.y_f32 ? wide_rows(static_cast<float*>(a.y), a.ldy)
+                                                  : wide_rows(static_cast<bf16*>(a.y), a.ldy);
+  const int y_size = a.y_f32 ? 4 : 2;
+  const long long y_step = (long long)a.ldy * y_size;
+  uint8_t* py = static_cast<uint8_t*>(a.y) + row * y_step + c * y_size;
+  const float cols = float(a.cols), part = 1.f / cols;
+  float2 pa[4], pb[4], qa[4], qb[4];  // of the branch and of y; zero outside the row
+  while (row < last) {
+    if (row >= end) {
+      // (what does not depend on the item is on its way while that is looked up)
+      float t[8], b[8], t2[8], b2[8], u[8], u2[8];
+      parameters(a.post.weight, c, n, 1.f, t);
+      parameters(a.post.bias, c, n, 0.f, b);
+      parameters(a.pre.weight, c, n, 1.f, t2);
+      parameters(a.pre.bias, c, n, 0.f, b2);
+      if (a.row_offsets) {
+        item = item_of(a.row_offsets, a.n_items, a.rows, row, end);
+      } else {
+        item = 0, end = a.rows;
+      }
+      const long long mod = (long long)max(item, 0) * a.ld_mod;
+      parameters(a.gate ? a.gate + mod : nullptr, c, n, 1.f, u);
+      parameters(a.scale ? a.scale + mod : nullptr, c, n, 0.f, u2);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        t[k] = k < n ? t[k] * u[k] : 0.f, b[k] *= u[k];
+        t2[k] = k < n ? fmaf(t2[k], u2[k], t2[k]) : 0.f, b2[k] = fmaf(b2[k], u2[k], b2[k]);
+      }
+      parameters(a.shift ? a.shift + mod : nullptr, c, n, 0.f, u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) b2[k] += u[k];
+      pairs_of(t, pa), pairs_of(b, pb), pairs_of(t2, qa), pairs_of(b2, qb);
+    }
+    const int rows = item < 0 ? 0 : min(ROWS, min(last, end) - row);
+    float2 v[ROWS][4], b[ROWS][4];
+    copy_wait<(DEPTH - 1) * ROWS>();
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      // (behind the last row: of no consequence)
+      const int from = at + r * step < places ? at + r * step : at + r * step - places;
+      const Eight<TX> ex = sx[from];
+      const Eight<TH> eh = sh[from];
+      float u[8];
+      unpack(ex, u), pairs_of(u, v[r]);
+      unpack(eh, u), pairs_of(u, b[r]);
+    }
+    // (the thread's own places: what it has read may be staged anew)
+    const int done = max(rows, 1);
+    if (done == ROWS) {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) fetch();
+    } else {
+      for (int i = 0; i < done; ++i) fetch();
+    }
+    at += done * step;
+    if (at >= places) at -= places;
+    if (rows == 0) {  // (a row of no item)
+      row += 1, po += a.ldx_out, py += y_step;
+      continue;
+    }
+    const float2 scale = f2_of(a.residual_scale);
+    if (PLAIN || h) {
+      for (int j = 0; !PLAIN && j < a.top_k; ++j) {
+        Eight<TH> e[ROWS];
+        float w[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          const long long pair = (long long)(row + (r < rows ? r : 0)) * a.top_k + j;
+          const int place = r < rows ? a.places[pair] : -1;
+          const bool there = place >= 0 && place < a.h_rows;
+          if (place >= a.h_rows && threadIdx.x == 0) atomicOr(a.err, DEVERR_INDEX);
+          w[r] = there ? a.weights[pair] : 0.f;
+          load(e[r], h + (long long)place * a.ldh + c, there ? n : 0, wide_h);
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          float u[8];
+          float2 t[4];
+          unpack(e[r], u), pairs_of(u, t);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) b[r][k] = f2_fma(f2_of(w[r]), t[k], b[r][k]);
+        }
+      }
+      float root[ROWS];
+      standardise<PLAIN>(a.post, b, root, n, cols, part, slots, turn);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          v[r][k] = f2_fma(v[r][k], scale,
+                           f2_fma(f2_mul(b[r][k], f2_of(root[r])), pa[k], pb[k]));
+    } else {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[r][k] = f2_mul(v[r][k], scale);
+    }
+    if (PLAIN || x_out) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+        if (r < rows && n > 0)
+          store(po + (long long)r * a.ldx_out, &v[r][0].x, PLAIN ? 8 : n, PLAIN || wide_out);
+    }
+    if (PLAIN || a.y || codes) {
+      float root[ROWS];
+      standardise<PLAIN>(a.pre, v, root, n, cols, part, slots, turn);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        if (r >= rows) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          v[r][k] = f2_fma(f2_mul(v[r][k], f2_of(root[r])), qa[k], qb[k]);
+        if constexpr (PLAIN) {
+          if (n > 0) store(reinterpret_cast<TY*>(py + r * y_step), &v[r][0].x, 8, true);
+          continue;
+        }
+        if (codes) store_codes(a.y8, row + r, c, n, &v[r][0].x);
+        else if (n > 0 && a.y_f32)
+          store(reinterpret_cast<float*>(py + r * y_step), &v[r][0].x, n, y_wide);
+        else if (n > 0)
+          store(reinterpret_cast<bf16*>(py + r * y_step), &v[r][0].x, n, y_wide);
+      }
+    }
+    row += done, po += done * (long long)a.ldx_out, py += done * y_step;
+  }
+  copy_wait<0>();
+}
+
+// Wider rows, one for each CTA: thread t of TPR holds vectors t, t + TPR ..  (NV at
+// most).
 template <class TX, class TH, int TPR, int NV>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
+__global__ void __launch_bounds__(TPR)
 norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
   __shared__ float slots[2][16];
   pdl_wait();
   pdl_trigger();
-  constexpr int ROWS = TPR == 32 ? 4 : 1;
-  const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
-  if (a.row_offsets && blockIdx.x == 0)
-    for (int i = threadIdx.x; i < a.n_items; i += blockDim.x)
-      if (a.row_offsets[i] < 0 || a.row_offsets[i] > a.row_offsets[i + 1] ||
-          a.row_offsets[i + 1] > a.rows)
-        atomicOr(a.err, DEVERR_COUNT);
-  const long long row = (long long)blockIdx.x * ROWS + (TPR == 32 ? threadIdx.x >> 5 : 0);
-  if (row >= a.rows) return;
-
-  const auto wide = [](const void* p, long long ld, int size) {
-    return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld * size)) & 15) == 0;
-  };
+  const int t = threadIdx.x;
+  if (a.row_offsets && blockIdx.x == 0) check_offsets(a);
+  const long long row = blockIdx.x;
   const TX* x = static_cast<const TX*>(a.x);
   const TH* h = static_cast<const TH*>(a.h);
-  const bool wide_x = wide(x, a.ldx, sizeof(TX)), wide_h = wide(h, a.ldh, sizeof(TH));
+  const bool wide_x = wide_rows(x, a.ldx), wide_h = wide_rows(h, a.ldh);
   float v[NV][8], r[NV][8];
   {
     Eight<TX> ex[NV];
@@ -170,7 +502,8 @@ norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) unpack(ex[i], v[i]), unpack(eh[i], r[i]);
   }
-  const int item = a.row_offsets ? item_of(a.row_offsets, a.n_items, a.rows, int(row)) : 0;
+  int end;
+  const int item = a.row_offsets ? item_of(a.row_offsets, a.n_items, a.rows, int(row), end) : 0;
   if (item < 0) return;  // (the row's threads alike)
   const long long mod = (long long)item * a.ld_mod;
 
@@ -218,7 +551,7 @@ norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
   }
   if (a.x_out) {
     TX* out = static_cast<TX*>(a.x_out);
-    const bool wide_out = wide(out, a.ldx_out, sizeof(TX));
+    const bool wide_out = wide_rows(out, a.ldx_out);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * TPR) * 8;
@@ -238,46 +571,45 @@ norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[i][k] = k < n ? fmaf(v[i][k], 1.f + s[k], b[k]) : 0.f;
     }
-    if (a.y8.codes) {
-      Eight<float> e;
-      e.a = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
-      e.b = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
-      if (n <= 0) e.zero();
-      uint32_t top = e.top();
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const int b = scale_byte(top);
-      const uint2 q = e.codes(scale_inverse(b));
-      uint8_t* dst = a.y8.codes + row * a.y8.ld + c;
-      if (n >= 8) {
-        *reinterpret_cast<uint2*>(dst) = q;
-      } else {
-        for (int k = 0; k < n; ++k) dst[k] = uint8_t((k < 4 ? q.x : q.y) >> (8 * (k & 3)));
-      }
-      if (n > 0 && (t & 15) == 0) a.y8.scales[(long long)(c / 128) * a.y8.lds + row] = uint8_t(b);
-    } else if (n > 0) {
-      if (a.y_f32) {
-        float* y = static_cast<float*>(a.y);
-        store(y + row * a.ldy + c, v[i], n, wide(y, a.ldy, 4));
-      } else {
-        bf16* y = static_cast<bf16*>(a.y);
-        store(y + row * a.ldy + c, v[i], n, wide(y, a.ldy, 2));
-      }
-    }
+    store_y(a, row, c, n, v[i]);
   }
+}
+
+constexpr int SMS = 152;
+
+template <class TX, class TH, class TY, int THREADS>
+cudaError_t rows(const ResidualArgs& a, int threads, int ctas, cudaStream_t st) {
+  const size_t smem = size_t(depth<TX, TH, THREADS>()) * ROWS * threads * 8 *
+                      (sizeof(TX) + sizeof(TH));
+  // (an attribute of the current device, so set for each call)
+  RC_TRY(cudaFuncSetAttribute(norm_rows_kernel<TX, TH, TY, THREADS>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+  return launch_k(norm_rows_kernel<TX, TH, TY, THREADS>,
+                  dim3(unsigned(a.rows < SMS * ctas ? a.rows : SMS * ctas)),
+                  dim3(unsigned(threads)), smem, st, a);
+}
+template <class TX, class TH, class TY>
+cudaError_t of_type(const ResidualArgs& a, int threads, cudaStream_t st) {
+  // (CTAs that an SM holds at once, by their registers)
+  if (threads <= 256) return rows<TX, TH, TY, 256>(a, threads, threads <= 160 ? 3 : 2, st);
+  return rows<TX, TH, TY, 640>(a, threads, 1, st);
 }
 
 template <class TX, class TH>
 cudaError_t go(const ResidualArgs& a, cudaStream_t st) {
   count_launches(1);
-  const auto one = [&](void (*kernel)(ResidualArgs), int threads, int rows) {
-    return launch_k(kernel, dim3(unsigned((a.rows + (long long)rows - 1) / rows)), dim3(threads),
-                    0, st, a);
+  const int threads = (a.cols + 255) / 256 * 32;
+  if (threads > 640)
+    return launch_k(norm_residual_kernel<TX, TH, 512, 4>, dim3(unsigned(a.rows)), dim3(512), 0, st,
+                    a);
+  const auto wide = [](const void* p, long long ld, int size) {
+    return p && ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld * size)) & 15) == 0;
   };
-  if (a.cols <= 1280 && a.rows > 1024) return one(norm_residual_kernel<TX, TH, 32, 5>, 128, 4);
-  if (a.cols <= 2048) return one(norm_residual_kernel<TX, TH, 128, 2>, 128, 1);
-  if (a.cols <= 5120) return one(norm_residual_kernel<TX, TH, 128, 5>, 128, 1);
-  return one(norm_residual_kernel<TX, TH, 512, 4>, 512, 1);
+  const bool plain = a.cols % 8 == 0 && a.top_k == 0 && wide(a.x, a.ldx, sizeof(TX)) &&
+                     wide(a.h, a.ldh, sizeof(TH)) && wide(a.x_out, a.ldx_out, sizeof(TX)) &&
+                     wide(a.y, a.ldy, a.y_f32 ? 4 : 2);
+  if (!plain) return of_type<TX, TH, void>(a, threads, st);
+  return a.y_f32 ? of_type<TX, TH, float>(a, threads, st) : of_type<TX, TH, bf16>(a, threads, st);
 }
 
 }  // namespace
