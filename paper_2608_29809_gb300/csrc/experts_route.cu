@@ -5,6 +5,7 @@
 #include "../../include/regioncache.h"
 #include "block.h"
 #include "common.cuh"
+#include "per_device.h"
 #include "tc_common.cuh"
 
 namespace rc {
@@ -43,7 +44,7 @@ __device__ __forceinline__ float warp_maxf(float v) { return of_key(warp_max(key
 // with |z - m| roundings in each exponential, whose mean is at most log(experts)
 // = 7, and 37 additions.  A score plus a bias is off by half a step more.
 __device__ __forceinline__ float score_error(int score, float s) {
-  return score == RC_SCORE_SIGMOID ? 0x1p-21f : 0x1p-18f * s + 0x1p-23f;
+  return score == RC_SCORE_SIGMOID ? 0x1p-21f : 0x1p-17f * s + 0x1p-22f;
 }
 
 // Keys of the groups that are not among the best `top_groups` become 0.  `scratch`:
@@ -152,28 +153,57 @@ __device__ __noinline__ int choose_f64(const float (&z)[PER], const RoutingArgs&
   return id;
 }
 
+// The score of a logit, m the row's largest (a softmax's without its sum).
+__device__ __forceinline__ float score_of(bool softmax, float z, float m) {
+  const float l = 1.4426950408889634f;  // log2 e
+  return softmax ? ex2_ftz((z - m) * l) : rcp_ftz(1.f + ex2_ftz(-z * l));
+}
 __device__ __forceinline__ float logit(const void* p, bool f32, long long i) {
   const float z = f32 ? static_cast<const float*>(p)[i] : bf2f(static_cast<const bf16*>(p)[i]);
   return z != z ? -INFINITY : fminf(z, FLT_MAX);
 }
 
-constexpr int ROUTE_WARPS = 4;
-
+// Lane j: the expert `id` of the row's j-th choice (-1: none) and its weight, with the
+// row's logits z (a lane's) and their largest m (where `with_m`).  With their sum
+// divided out, exponentials are taken from the largest of the chosen, so that no range
+// of scores is lost.
 template <class T, int PER>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS)
-route_kernel(const __grid_constant__ RoutingArgs a) {
-  __shared__ uint64_t s_scratch[ROUTE_WARPS][PER * 32];
-  pdl_wait();
-  pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
-  if (row >= a.rows) return;
-  const int rows = live_count(a.count, a.rows, row == 0 && lane == 0 ? a.err : nullptr);
-  if (row >= rows) {
-    if (lane < a.top_k) a.ids[row * a.top_k + lane] = -1, a.weights[row * a.top_k + lane] = 0.f;
-    return;
+__device__ __forceinline__ void write_choice(const RoutingArgs& a, long long row, int lane, int id,
+                                             const float (&z)[PER], float m, bool with_m) {
+  const bool softmax = a.score == RC_SCORE_SOFTMAX;
+  if (lane >= a.top_k) id = -1;
+  const float zi = id < 0 ? -INFINITY : logit(a.logits, sizeof(T) == 4, row * a.ld + id);
+  const float mc = warp_maxf(zi);
+  float w = 0.f;
+  if (softmax) {
+    if (a.renormalise) {
+      w = id < 0 || (with_m && mc - m < -745.f) ? 0.f : expf(zi - mc);
+    } else {
+      float all = 0.f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) all += z[i] == -INFINITY ? 0.f : expf(z[i] - m);
+      all = warp_sum(all);
+      w = id < 0 ? 0.f : expf(zi - m) / all;
+    }
+  } else if (id >= 0) {
+    const float from = a.renormalise ? fminf(mc, 0.f) : 0.f;
+    w = zi > 0.f ? 1.f / (1.f + expf(-zi)) : expf(zi - from) / (1.f + expf(zi));
+    if (from < -745.f) w = 0.f;
   }
-  uint64_t* scratch = s_scratch[threadIdx.x >> 5];
+  if (a.renormalise) {
+    const float all = warp_sum(w);
+    w = all > 0.f ? w / all : 0.f;
+  }
+  if (lane < a.top_k) {
+    a.ids[row * a.top_k + lane] = id;
+    a.weights[row * a.top_k + lane] = w * a.scale;
+  }
+}
+
+// A row with all that can be asked for.
+template <class T, int PER>
+__device__ __noinline__ void route_row(const RoutingArgs& a, long long row, int lane,
+                                       uint64_t* scratch) {
   const long long base = row * a.ld;
   float z[PER], m = -INFINITY;
 #pragma unroll
@@ -187,7 +217,7 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
   // (without a bias larger logits have larger scores)
   const bool by_logits = !a.bias && (!grouped || a.group_best == 1);
   float sum = 0.f;
-  if (!by_logits || (softmax && !a.renormalise)) m = warp_maxf(m);
+  m = warp_maxf(m);
   uint32_t key[PER];
   if (by_logits) {
 #pragma unroll
@@ -196,8 +226,7 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
     float s[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      s[i] = softmax ? __expf(z[i] - m) : __fdividef(1.f, 1.f + __expf(-z[i]));
-      if (z[i] == -INFINITY) s[i] = 0.f;
+      s[i] = z[i] == -INFINITY ? 0.f : score_of(softmax, z[i], m);
       sum += s[i];
     }
     const float r = softmax ? 1.f / warp_sum(sum) : 1.f;
@@ -235,105 +264,373 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
     }
     if (__any_sync(~0u, close)) id = choose_f64(z, a, lane, m, scratch);
   }
-  // lane j: the weight of the j-th.  (With their sum divided out, exponentials are
-  // taken from the largest of the chosen, so that no range of scores is lost.)
-  if (lane >= a.top_k) id = -1;
-  const float zi = id < 0 ? -INFINITY : logit(a.logits, sizeof(T) == 4, base + id);
-  const float mc = warp_maxf(zi);
-  float w = 0.f;
-  if (softmax) {
-    if (a.renormalise) {
-      w = id < 0 || (!by_logits && mc - m < -745.f) ? 0.f : expf(zi - mc);
-    } else {
-      float all = 0.f;
+  write_choice<T>(a, row, lane, id, z, m, true);
+}
+
+// Keys of a lane in descending order (Batcher's merges of sorted halves).
+template <int N, int STRIDE, int AT, int PER>
+__device__ __forceinline__ void merge_halves(uint32_t (&k)[PER]) {
+  const auto order = [&](int i, int j) {
+    const uint32_t hi = max(k[i], k[j]), lo = min(k[i], k[j]);
+    k[i] = hi, k[j] = lo;
+  };
+  if constexpr (2 * STRIDE < N) {
+    merge_halves<N, 2 * STRIDE, AT>(k);
+    merge_halves<N, 2 * STRIDE, AT + STRIDE>(k);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) all += z[i] == -INFINITY ? 0.f : expf(z[i] - m);
-      all = warp_sum(all);
-      w = id < 0 ? 0.f : expf(zi - m) / all;
+    for (int i = AT + STRIDE; i + STRIDE < AT + N; i += 2 * STRIDE) order(i, i + STRIDE);
+  } else {
+    order(AT, AT + STRIDE);
+  }
+}
+template <int N, int AT, int PER>
+__device__ __forceinline__ void sort_keys(uint32_t (&k)[PER]) {
+  if constexpr (N > 1) {
+    sort_keys<N / 2, AT>(k);
+    sort_keys<N / 2, AT + N / 2>(k);
+    merge_halves<N, 1, AT>(k);
+  }
+}
+
+constexpr int ROUTE_WARPS = 4;
+// Choices that are looked at behind the last one where the order is not clear.
+constexpr int MORE = 4;
+
+// The experts `id` of the lanes (-1: none) in the order of their logits or sigmoid
+// scores with bias, as of f64: lane j gets the j-th.
+__device__ __noinline__ int in_order(const RoutingArgs& a, bool f32, long long row, int lane,
+                                     int id) {
+  uint64_t mine = 0;
+  if (id >= 0) {
+    const double z = logit(a.logits, f32, row * a.ld + id);
+    const double v = a.bias ? 1 / (1 + exp(-z)) + double(fminf(a.bias[id], FLT_MAX))
+                            : a.top_groups < a.groups && a.group_best > 1 ? 1 / (1 + exp(-z)) : z;
+    mine = key_of(v);
+  }
+  int rank = 0;
+  for (int j = 0; j < RC_EXPERTS_MAX_TOP_K + 1 + MORE; ++j) {
+    const uint64_t k = __shfl_sync(~0u, mine, j);
+    const int other = __shfl_sync(~0u, id, j);
+    rank += other >= 0 && (k > mine || (k == mine && other < id));
+  }
+  int out = -1;
+  for (int j = 0; j < RC_EXPERTS_MAX_TOP_K + 1 + MORE; ++j) {
+    const int r = __shfl_sync(~0u, id >= 0 ? rank : -1, j), other = __shfl_sync(~0u, id, j);
+    if (r == lane) out = other;
+  }
+  return out;
+}
+
+// Any routing, a row for each warp.
+template <class T, int PER>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS)
+route_any_kernel(const __grid_constant__ RoutingArgs a) {
+  __shared__ uint64_t scratch[ROUTE_WARPS][PER * 32];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
+  if (row >= a.rows) return;
+  const int rows = live_count(a.count, a.rows, row == 0 && lane == 0 ? a.err : nullptr);
+  if (row < rows) {
+    route_row<T, PER>(a, row, lane, scratch[threadIdx.x >> 5]);
+  } else if (lane < a.top_k) {
+    a.ids[row * a.top_k + lane] = -1, a.weights[row * a.top_k + lane] = 0.f;
+  }
+}
+
+// The same where a lane's experts are of one group (a group then is 1, 2, 4 .. lanes),
+// for the rows whose choice can be told from shortened keys: the value's upper bits,
+// and below them the expert's number, lower numbers larger.  Keys are sorted in their
+// lanes once, and a choice is then the largest head.  Neighbours closer than what a
+// shortened key may be off are put in order by f64 (a softmax's with a bias, and groups
+// that close, by route_row).  A warp keeps the bias and takes
+// several rows, the next one's logits under way.  (All rows as route_row does them:
+// 16384 rows of 256, sigmoid, groups, 8 each, 48 us, 1700 instructions a row.)
+template <class T, int PER>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, PER <= 8 ? 5 : 2)
+route_kernel(const __grid_constant__ RoutingArgs a) {
+  __shared__ uint64_t scratch[ROUTE_WARPS][PER * 32];
+  const int lane = threadIdx.x & 31, e0 = lane * PER;
+  const bool softmax = a.score == RC_SCORE_SOFTMAX, grouped = a.top_groups < a.groups;
+  const bool by_logits = !a.bias && (!grouped || a.group_best == 1);
+  constexpr uint32_t LOW = 32 * PER - 1;  // where a key has the expert
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.logits) | uintptr_t(a.ld * sizeof(T))) &
+                     (PER * sizeof(T) < 16 ? PER * sizeof(T) - 1 : 15)) == 0 &&
+                    e0 + PER <= a.experts;
+  const int size = a.experts / a.groups, lanes = size / PER, group = grouped ? lane / lanes : 0;
+  pdl_wait();
+  pdl_trigger();
+  const int rows = live_count(a.count, a.rows, blockIdx.x == 0 && threadIdx.x == 0 ? a.err : nullptr);
+  float b[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    b[i] = a.bias && e0 + i < a.experts ? a.bias[e0 + i] : 0.f;
+    b[i] = b[i] > -INFINITY ? fminf(b[i], FLT_MAX) : -INFINITY;  // (NaN: none)
+  }
+  constexpr int BYTES = PER * int(sizeof(T)), WORDS = BYTES < 4 ? 1 : BYTES / 4;
+  uint32_t raw[WORDS];  // the lane's logits as they are
+  const auto fetch = [&](long long row) {
+    const T* p = static_cast<const T*>(a.logits) + row * a.ld + e0;
+    if (wide) {
+      if constexpr (BYTES >= 16) {
+#pragma unroll
+        for (int k = 0; k < WORDS; k += 4) {
+          const uint4 u = reinterpret_cast<const uint4*>(p)[k / 4];
+          raw[k] = u.x, raw[k + 1] = u.y, raw[k + 2] = u.z, raw[k + 3] = u.w;
+        }
+      } else if constexpr (BYTES == 8) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        raw[0] = u.x, raw[1] = u.y;
+      } else if constexpr (BYTES == 4) {
+        raw[0] = *reinterpret_cast<const uint32_t*>(p);
+      } else {
+        raw[0] = *reinterpret_cast<const uint16_t*>(p);
+      }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        raw[i] = e0 + i < a.experts ? reinterpret_cast<const uint32_t*>(p)[i] : 0xff800000u;  // -inf
+    } else {
+#pragma unroll
+      for (int k = 0; k < WORDS; ++k) raw[k] = 0xff80ff80u;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (e0 + i < a.experts) {
+          const uint32_t u = reinterpret_cast<const uint16_t*>(p)[i];
+          raw[i / 2] = i & 1 ? (raw[i / 2] & 0xffffu) | u << 16 : (raw[i / 2] & 0xffff0000u) | u;
+        }
     }
-  } else if (id >= 0) {
-    const float from = a.renormalise ? fminf(mc, 0.f) : 0.f;
-    w = zi > 0.f ? 1.f / (1.f + expf(-zi)) : expf(zi - from) / (1.f + expf(zi));
-    if (from < -745.f) w = 0.f;
+  };
+  const int step = gridDim.x * ROUTE_WARPS;
+  uint32_t again = 0;  // of the last `turn` rows, those for route_row
+  int turn = 0;
+  long long row = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
+  if (row < rows) fetch(row);
+  for (; row < rows; row += step) {
+    float z[PER], m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t u = sizeof(T) == 4 ? raw[i % WORDS]
+                         : i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16;
+      z[i] = fminf(fmaxf(__uint_as_float(u), -INFINITY), FLT_MAX);  // (NaN: none)
+      if (a.bias && b[i] == -INFINITY) z[i] = -INFINITY;
+    }
+    if (row + step < rows) fetch(row + step);
+    const bool with_m = softmax && (!by_logits || !a.renormalise);
+    if (with_m) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) m = fmaxf(m, z[i]);
+      m = warp_maxf(m);
+    }
+    float c[PER];  // what experts are chosen by
+    if (by_logits) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) c[i] = z[i];
+    } else {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        c[i] = z[i] == -INFINITY ? 0.f : score_of(softmax, z[i], m);
+        sum += c[i];
+      }
+      const float r = softmax ? 1.f / warp_sum(sum) : 1.f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) c[i] = z[i] == -INFINITY ? -INFINITY : fmaf(c[i], r, b[i]);
+    }
+    bool close = false;
+    if (grouped) {
+      float one = -INFINITY, two = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        two = fmaxf(two, fminf(one, c[i]));
+        one = fmaxf(one, c[i]);
+      }
+      for (int o = 1; o < lanes; o <<= 1) {
+        const float k = __shfl_xor_sync(~0u, one, o), l = __shfl_xor_sync(~0u, two, o);
+        two = fmaxf(fminf(one, k), fmaxf(two, l));
+        one = fmaxf(one, k);
+      }
+      const float mine = a.group_best == 2 && two > -INFINITY ? one + two : one;
+      int rank = 0;
+      for (int h = 0; h < a.groups; ++h) {
+        const float v = __shfl_sync(~0u, mine, h * lanes);
+        rank += v > mine || (v == mine && h < group);
+      }
+      const bool kept = group < a.groups && mine > -INFINITY && rank < a.top_groups;
+      if (!by_logits) {
+        const uint32_t k = group < a.groups ? key_of(mine) : 0u;
+        const float most = of_key(max(warp_max(kept ? 0u : k), key_of(-FLT_MAX)));
+        const float least = of_key(~warp_max(kept ? ~k : 0u));
+        // (sums of two values: at most twice their errors)
+        close = __any_sync(~0u, kept) &&
+                !(least - most > 4.f * score_error(a.score, 1.f) +
+                                     0x1p-20f * fmaxf(fabsf(least), fabsf(most)) + 0x1p-20f *
+                                     fmaxf(fabsf(one), fabsf(two > -INFINITY ? two : 0.f)));
+      }
+      if (!kept)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = -INFINITY;
+    }
+    uint32_t k[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) k[i] = (key_of(c[i]) & ~LOW) | (LOW - uint32_t(e0 + i));
+    sort_keys<PER, 0>(k);
+    uint32_t value = 0;  // lane j: the j-th largest
+    const auto pick_more = [&](int from, int to) {
+#pragma unroll 1
+      for (int j = from; j < to; ++j) {
+        const uint32_t top = warp_max(k[0]);
+        if (k[0] == top) {
+#pragma unroll
+          for (int i = 0; i + 1 < PER; ++i) k[i] = k[i + 1];
+          k[PER - 1] = 0;
+        }
+        if (lane == j && top >= (key_of(-FLT_MAX) & ~LOW)) value = top;  // (others: -inf)
+      }
+    };
+    // whether lane j's choice may not come before lane j + 1's (asked by all lanes)
+    const auto near = [&] {
+      const uint32_t next = __shfl_down_sync(~0u, value, 1);
+      // (of bf16 the lower half of a key is free: equal logits are in order)
+      if (by_logits) return next && sizeof(T) == 4 && ((value ^ next) & ~LOW) == 0;
+      const float v = of_key(value & ~LOW), w = of_key(next & ~LOW);
+      return next && !(v - w > 2.f * score_error(a.score, 1.f) +
+                                   (LOW + 5) * 0x1p-23f * fmaxf(fabsf(v), fabsf(w)) + 0x1p-100f);
+    };
+    pick_more(0, a.top_k + 1);
+    int id = value ? int(LOW - (value & LOW)) : -1;
+    const bool unclear = near();
+    if (__any_sync(~0u, lane < a.top_k && unclear)) {
+      // a few more, up to the first behind the last choice that is clear of the next
+      pick_more(a.top_k + 1, a.top_k + 1 + MORE);
+      id = value ? int(LOW - (value & LOW)) : -1;
+      const bool apart = !near();
+      const uint32_t ends = __ballot_sync(~0u, apart && lane >= a.top_k - 1 &&
+                                                   lane < a.top_k + MORE);
+      if (!ends || (softmax && !by_logits)) close = true;
+      else id = in_order(a, sizeof(T) == 4, row, lane, lane < __ffs(int(ends)) ? id : -1);
+    }
+    if (__any_sync(~0u, close))
+      again |= 1u << turn;
+    else
+      write_choice<T>(a, row, lane, id, z, m, with_m);
+    if (++turn == 32 || row + step >= rows) {
+      // (here, where little else is alive)
+      for (; again; again &= again - 1)
+        route_row<T, PER>(a, row - (turn - __ffs(int(again))) * (long long)step, lane,
+                          scratch[threadIdx.x >> 5]);
+      turn = 0;
+    }
   }
-  if (a.renormalise) {
-    const float all = warp_sum(w);
-    w = all > 0.f ? w / all : 0.f;
-  }
-  if (lane < a.top_k) {
-    a.ids[row * a.top_k + lane] = id;
-    a.weights[row * a.top_k + lane] = w * a.scale;
-  }
+  for (row = rows + blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); row < a.rows; row += step)
+    if (lane < a.top_k) a.ids[row * a.top_k + lane] = -1, a.weights[row * a.top_k + lane] = 0.f;
+}
+
+template <class T, int PER>
+cudaError_t route_of(const RoutingArgs& a, cudaStream_t st) {
+  const int size = a.experts / a.groups, lanes = size / PER;
+  const bool whole = a.top_groups == a.groups ||
+                     (size % PER == 0 && (lanes & (lanes - 1)) == 0);
+  const long long ctas = (a.rows + ROUTE_WARPS - 1LL) / ROUTE_WARPS;
+  const dim3 block(32 * ROUTE_WARPS);
+  if (!whole) return launch_k(route_any_kernel<T, PER>, dim3(unsigned(ctas)), block, 0, st, a);
+  // (as many CTAs as the SMs hold at once)
+  return launch_k(route_kernel<T, PER>, dim3(unsigned(ctas < 152 * 5 ? ctas : 152 * 5)), block, 0,
+                  st, a);
 }
 
 template <class T>
 cudaError_t route(const RoutingArgs& a, cudaStream_t st) {
-  const dim3 grid(unsigned((a.rows + ROUTE_WARPS - 1LL) / ROUTE_WARPS)), block(32 * ROUTE_WARPS);
   count_launches(1);
-  if (a.experts <= 32) return launch_k(route_kernel<T, 1>, grid, block, 0, st, a);
-  if (a.experts <= 64) return launch_k(route_kernel<T, 2>, grid, block, 0, st, a);
-  if (a.experts <= 128) return launch_k(route_kernel<T, 4>, grid, block, 0, st, a);
-  if (a.experts <= 256) return launch_k(route_kernel<T, 8>, grid, block, 0, st, a);
-  if (a.experts <= 512) return launch_k(route_kernel<T, 16>, grid, block, 0, st, a);
-  return launch_k(route_kernel<T, 32>, grid, block, 0, st, a);
+  if (a.experts <= 32) return route_of<T, 1>(a, st);
+  if (a.experts <= 64) return route_of<T, 2>(a, st);
+  if (a.experts <= 128) return route_of<T, 4>(a, st);
+  if (a.experts <= 256) return route_of<T, 8>(a, st);
+  if (a.experts <= 512) return route_of<T, 16>(a, st);
+  return route_of<T, 32>(a, st);
 }
 
 // ------------------------------------------------------------------- sorting
-// A stable counting sort by one cluster.  Each warp owns a run of consecutive
-// pairs and counts its experts in a row of its own; the counts become first places
-// by a scan over warps, CTAs (through their shared memory) and experts; then the
-// warp deals its run out, 32 pairs at a time, equal experts of the 32 in order.
-constexpr int SORT_WARPS = 32, SORT_CTAS = 8;
+// A stable counting sort by one cluster.  Each warp owns a run of consecutive pairs and
+// counts its experts in a row of its own, 32 pairs at a time; a pair's place among its
+// warp's is what the count was, and its number among equal ones of the 32.  The counts
+// become first places by a scan over warps, CTAs (through their shared memory) and
+// experts.  The pairs and their places in the run stay in registers in between where a
+// run has KEEP or fewer of the 32s.
+constexpr int SORT_WARPS = 32, KEEP = 8;
 
 __global__ void __launch_bounds__(32 * SORT_WARPS, 1)
 sort_kernel(const __grid_constant__ SortArgs a) {
-  extern __shared__ int counts[];  // [SORT_WARPS][experts], then sums and bases [experts]
+  extern __shared__ int counts[];  // [warps][experts], then sums and bases [experts]
   __shared__ int parts[32];
   const int E = a.experts, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int* sums = counts + SORT_WARPS * E;
-  int* bases = sums + E;
   const int ctas = int(gridDim.x), cta = int(tc::cluster_ctarank());
-  for (int i = tid; i < SORT_WARPS * E; i += blockDim.x) counts[i] = 0;
   pdl_wait();
   pdl_trigger();
   const int all = a.rows * a.top_k;
   const int n = live_count(a.count, a.rows, cta == 0 && tid == 0 ? a.err : nullptr) * a.top_k;
-  // (a run is a multiple of 32)
+  // (a run is a multiple of 32; where there is one CTA, a warp each 32)
   const int warps = ctas * SORT_WARPS, run = ((n + 31) / 32 + warps - 1) / warps * 32;
+  const int used = ctas > 1 ? SORT_WARPS : min(SORT_WARPS, (n + 31) / 32);  // warps with pairs
+  int* sums = counts + SORT_WARPS * E;
+  int* bases = sums + E;
   const int from = int(min((long long)(cta * SORT_WARPS + warp) * run, (long long)n));
   const int to = int(min((long long)from + run, (long long)n));
   int* own = counts + warp * E;
+  int e[KEEP], at[KEEP];
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k) {
+    const int i = from + 32 * k + lane;
+    e[k] = i < to ? a.ids[i] : -1;
+  }
+  for (int i = tid; i < used * E; i += blockDim.x) counts[i] = 0;
   __syncthreads();
   bool bad = false;
-  for (int i = from + lane; i < to; i += 32) {
-    const int e = a.ids[i];
-    bad |= e >= E;
-    if (e >= 0 && e < E) atomicAdd(own + e, 1);
+  const auto count = [&](int& id) {
+    bad |= id >= E;
+    if (id < 0 || id >= E) id = -1;
+    const uint32_t same = __match_any_sync(~0u, id);
+    int place = 0;
+    if (id >= 0) place = own[id] + __popc(same & ((1u << lane) - 1));
+    __syncwarp();
+    if (id >= 0 && lane == 31 - __clz(int(same))) own[id] = place + 1;
+    __syncwarp();
+    return place;
+  };
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k)
+    if (from + 32 * k < to) at[k] = count(e[k]);
+  for (int i0 = from + 32 * KEEP; i0 < to; i0 += 32) {
+    int id = i0 + lane < to ? a.ids[i0 + lane] : -1;
+    const int place = count(id);
+    if (i0 + lane < to) a.places[i0 + lane] = place;  // (for now)
   }
   if (bad) atomicOr(a.err, DEVERR_INDEX);
   __syncthreads();
-  for (int e = tid; e < E; e += blockDim.x) {
-    int c[SORT_WARPS], sum = 0;
-#pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) c[w] = counts[w * E + e];
-#pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) {
-      counts[w * E + e] = sum;
-      sum += c[w];
-    }
-    sums[e] = sum;
-  }
-  tc::cluster_sync();
-  // thread e: its expert's first place, and this CTA's (experts <= the block's threads)
-  int total = 0, before = 0;
+  int total = 0, before = 0;  // of expert `tid` (experts <= the block's threads)
   if (tid < E) {
-    const uint32_t at = tc::saddr(sums + tid);
-    for (int c = 0; c < ctas; ++c) {
-      int v;
-      asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v)
-                   : "r"(tc::mapa_shared(at, uint32_t(c))));
-      if (c < cta) before += v;
-      total += v;
+    int sum = 0;
+#pragma unroll 8
+    for (int w = 0; w < used; ++w) {
+      const int c = counts[w * E + tid];
+      counts[w * E + tid] = sum;
+      sum += c;
+    }
+    sums[tid] = total = sum;
+  }
+  if (ctas > 1) {
+    tc::cluster_sync();
+    if (tid < E) {
+      const uint32_t mine = tc::saddr(sums + tid);
+      total = 0;
+      for (int c = 0; c < ctas; ++c) {
+        int v;
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v)
+                     : "r"(tc::mapa_shared(mine, uint32_t(c))));
+        if (c < cta) before += v;
+        total += v;
+      }
     }
   }
   int scan = total;
@@ -344,41 +641,34 @@ sort_kernel(const __grid_constant__ SortArgs a) {
   }
   if (lane == 31) parts[warp] = scan;
   __syncthreads();
-  if (warp == 0) {
-    int p = parts[lane];
+  // (every warp sums up the parts before it)
+  int p = lane < warp ? parts[lane] : 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(~0u, p, o);
-      if (lane >= o) p += v;
-    }
-    parts[lane] = p;
-  }
-  __syncthreads();
-  if (warp > 0) scan += parts[warp - 1];
+  for (int o = 16; o > 0; o >>= 1) p += __shfl_xor_sync(~0u, p, o);
+  scan += p;
   if (tid < E) {
     bases[tid] = scan - total + before;
     if (cta == 0) a.offsets[tid] = scan - total;
     if (cta == 0 && tid == E - 1) a.offsets[E] = scan;
   }
   __syncthreads();
-  for (int i0 = from; i0 < to; i0 += 32) {
-    const int i = i0 + lane;
-    int e = i < to ? a.ids[i] : -1;
-    if (e < 0 || e >= E) e = -1;
-    const uint32_t same = __match_any_sync(~0u, e);
-    int place = -1;
-    if (e >= 0) place = bases[e] + own[e] + __popc(same & ((1u << lane) - 1));
-    __syncwarp();
-    if (e >= 0 && lane == __ffs(int(same)) - 1) own[e] += __popc(same);
-    __syncwarp();
-    if (i < to) {
-      a.places[i] = place;
-      if (place >= 0) a.source[place] = i / a.top_k;
+  const auto write = [&](int i, int id, int place) {
+    if (id >= 0) {
+      place += bases[id] + own[id];
+      a.source[place] = i / a.top_k;
     }
+    a.places[i] = id >= 0 ? place : -1;
+  };
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k)
+    if (from + 32 * k + lane < to) write(from + 32 * k + lane, e[k], at[k]);
+  for (int i = from + 32 * KEEP + lane; i < to; i += 32) {
+    const int id = a.ids[i];
+    write(i, id >= E ? -1 : id, a.places[i]);
   }
   for (int i = n + cta * int(blockDim.x) + tid; i < all; i += ctas * int(blockDim.x))
     a.places[i] = -1;
-  tc::cluster_sync();  // (no CTA leaves while another may read its sums)
+  if (ctas > 1) tc::cluster_sync();  // (no CTA leaves while another may read its sums)
 }
 
 }  // namespace
@@ -387,13 +677,41 @@ cudaError_t launch_experts_route(const RoutingArgs& a, cudaStream_t st) {
   return a.f32 ? route<float>(a, st) : route<bf16>(a, st);
 }
 
+// Whether the device places a cluster of sixteen CTAs (more than any device has to).
+bool sixteen_fit(size_t smem) {
+  static PerDevice<1> known;
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) return false;
+  return known.get(device, 0, [&] {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(32 * SORT_WARPS);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 16, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, sort_kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    return clusters > 0 ? 1 : 0;
+  }) > 0;
+}
+
 cudaError_t launch_experts_sort(const SortArgs& a, cudaStream_t st) {
   const size_t smem = size_t(SORT_WARPS + 2) * a.experts * sizeof(int);
-  // (an attribute of the current device, so set for each call)
-  RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              int(size_t(SORT_WARPS + 2) * RC_EXPERTS_MAX * sizeof(int))));
+  constexpr size_t most = size_t(SORT_WARPS + 2) * RC_EXPERTS_MAX * sizeof(int);
+  // (attributes of the current device, so set for each call)
+  RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)));
+  RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   count_launches(1);
-  const int ctas = (long long)a.rows * a.top_k > 32 * SORT_WARPS ? SORT_CTAS : 1;
+  // One CTA where it has a warp for each 32 pairs; sixteen where the places' writes are
+  // what counts (131072 pairs: a CTA's 32 scattered writes take an SM as many cycles).
+  const long long pairs = (long long)a.rows * a.top_k;
+  const int ctas = pairs <= 32 * SORT_WARPS ? 1 : pairs > 16384 && sixteen_fit(most) ? 16 : 8;
   return launch_k_cluster(sort_kernel, dim3(unsigned(ctas)), dim3(32 * SORT_WARPS), smem, ctas,
                           st, a);
 }
