@@ -17,10 +17,11 @@ namespace {
 // are compared as unsigned keys of the same order (0: no such expert), so that a
 // warp's largest is one reduction and the lowest lane and slot that hold it are
 // the lowest index.
-__device__ __forceinline__ uint32_t key_of(float v) {
-  const uint32_t u = __float_as_uint(v + 0.f);  // (-0 as 0)
-  return u >> 31 ? ~u : u | 0x80000000u;
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u ^ (uint32_t(int(u) >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ uint32_t key_of(float v) { return order_of(v + 0.f); }  // (-0 as 0)
 __device__ __forceinline__ uint64_t key_of(double v) {
   const uint64_t u = uint64_t(__double_as_longlong(v + 0.0));
   return u >> 63 ? ~u : u | (uint64_t(1) << 63);
@@ -125,7 +126,7 @@ __device__ __forceinline__ void pick(K (&key)[PER], int lane, int n, int& id, K&
 
 // The choice with scores in f64 (rows whose f32 values are too close).
 template <int PER>
-__device__ __noinline__ int choose_f64(const float (&z)[PER], const RoutingArgs& a, int lane,
+__device__ __forceinline__ int choose_f64(const float (&z)[PER], const RoutingArgs& a, int lane,
                                        float m, uint64_t* scratch) {
   double s[PER], sum = 0;
 #pragma unroll
@@ -202,7 +203,7 @@ __device__ __forceinline__ void write_choice(const RoutingArgs& a, long long row
 
 // A row with all that can be asked for.
 template <class T, int PER>
-__device__ __noinline__ void route_row(const RoutingArgs& a, long long row, int lane,
+__device__ __forceinline__ void route_row(const RoutingArgs& a, long long row, int lane,
                                        uint64_t* scratch) {
   const long long base = row * a.ld;
   float z[PER], m = -INFINITY;
@@ -298,7 +299,7 @@ constexpr int MORE = 4;
 
 // The experts `id` of the lanes (-1: none) in the order of their logits or sigmoid
 // scores with bias, as of f64: lane j gets the j-th.
-__device__ __noinline__ int in_order(const RoutingArgs& a, bool f32, long long row, int lane,
+__device__ __forceinline__ int in_order(const RoutingArgs& a, bool f32, long long row, int lane,
                                      int id) {
   uint64_t mine = 0;
   if (id >= 0) {
@@ -347,8 +348,10 @@ route_any_kernel(const __grid_constant__ RoutingArgs a) {
 // that close, by route_row).  A warp keeps the bias and takes
 // several rows, the next one's logits under way.  (All rows as route_row does them:
 // 16384 rows of 256, sigmoid, groups, 8 each, 48 us, 1700 instructions a row.)
+template <int PER>
+constexpr int ROUTE_CTAS = PER <= 4 ? 8 : PER == 8 ? 6 : PER == 16 ? 4 : 2;  // of an SM
 template <class T, int PER>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS, PER <= 8 ? 5 : 2)
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, ROUTE_CTAS<PER>)
 route_kernel(const __grid_constant__ RoutingArgs a) {
   __shared__ uint64_t scratch[ROUTE_WARPS][PER * 32];
   const int lane = threadIdx.x & 31, e0 = lane * PER;
@@ -403,9 +406,10 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
     }
   };
   const int step = gridDim.x * ROUTE_WARPS;
-  uint32_t again = 0;  // of the last `turn` rows, those for route_row
+  uint32_t again = 0;  // of the warp's rows (32 at most), those for route_row
   int turn = 0;
-  long long row = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
+  const long long first = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
+  long long row = first;
   if (row < rows) fetch(row);
   for (; row < rows; row += step) {
     float z[PER], m = -INFINITY;
@@ -414,7 +418,11 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
       const uint32_t u = sizeof(T) == 4 ? raw[i % WORDS]
                          : i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16;
       z[i] = fminf(fmaxf(__uint_as_float(u), -INFINITY), FLT_MAX);  // (NaN: none)
-      if (a.bias && b[i] == -INFINITY) z[i] = -INFINITY;
+    }
+    if (softmax && a.bias) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (b[i] == -INFINITY) z[i] = -INFINITY;
     }
     if (row + step < rows) fetch(row + step);
     const bool with_m = softmax && (!by_logits || !a.renormalise);
@@ -426,17 +434,19 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
     float c[PER];  // what experts are chosen by
     if (by_logits) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) c[i] = z[i];
-    } else {
+      for (int i = 0; i < PER; ++i) c[i] = z[i] + 0.f;  // (-0 as 0)
+    } else if (softmax) {
       float sum = 0.f;
+      m = fmaxf(m, -FLT_MAX);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        c[i] = z[i] == -INFINITY ? 0.f : score_of(softmax, z[i], m);
-        sum += c[i];
-      }
-      const float r = softmax ? 1.f / warp_sum(sum) : 1.f;
+      for (int i = 0; i < PER; ++i) sum += c[i] = score_of(true, z[i], m);
+      const float r = 1.f / warp_sum(sum);
 #pragma unroll
       for (int i = 0; i < PER; ++i) c[i] = z[i] == -INFINITY ? -INFINITY : fmaf(c[i], r, b[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        c[i] = z[i] == -INFINITY ? -INFINITY : score_of(false, z[i], 0.f) + b[i];
     }
     bool close = false;
     if (grouped) {
@@ -474,7 +484,7 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
     }
     uint32_t k[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) k[i] = (key_of(c[i]) & ~LOW) | (LOW - uint32_t(e0 + i));
+    for (int i = 0; i < PER; ++i) k[i] = (order_of(c[i]) & ~LOW) | (LOW - uint32_t(e0 + i));
     sort_keys<PER, 0>(k);
     uint32_t value = 0;  // lane j: the j-th largest
     const auto pick_more = [&](int from, int to) {
@@ -515,14 +525,12 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
       again |= 1u << turn;
     else
       write_choice<T>(a, row, lane, id, z, m, with_m);
-    if (++turn == 32 || row + step >= rows) {
-      // (here, where little else is alive)
-      for (; again; again &= again - 1)
-        route_row<T, PER>(a, row - (turn - __ffs(int(again))) * (long long)step, lane,
-                          scratch[threadIdx.x >> 5]);
-      turn = 0;
-    }
+    ++turn;
   }
+  // (here, where nothing else is alive)
+  for (; again; again &= again - 1)
+    route_row<T, PER>(a, first + (__ffs(int(again)) - 1) * (long long)step, lane,
+                      scratch[threadIdx.x >> 5]);
   for (row = rows + blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5); row < a.rows; row += step)
     if (lane < a.top_k) a.ids[row * a.top_k + lane] = -1, a.weights[row * a.top_k + lane] = 0.f;
 }
@@ -535,9 +543,10 @@ cudaError_t route_of(const RoutingArgs& a, cudaStream_t st) {
   const long long ctas = (a.rows + ROUTE_WARPS - 1LL) / ROUTE_WARPS;
   const dim3 block(32 * ROUTE_WARPS);
   if (!whole) return launch_k(route_any_kernel<T, PER>, dim3(unsigned(ctas)), block, 0, st, a);
-  // (as many CTAs as the SMs hold at once)
-  return launch_k(route_kernel<T, PER>, dim3(unsigned(ctas < 152 * 5 ? ctas : 152 * 5)), block, 0,
-                  st, a);
+  // (as many CTAs as the SMs hold at once, or more: a warp takes 32 rows at most)
+  const long long held = 152 * ROUTE_CTAS<PER>, least = (ctas + 31) / 32;
+  const long long grid = ctas < held ? ctas : least > held ? least : held;
+  return launch_k(route_kernel<T, PER>, dim3(unsigned(grid)), block, 0, st, a);
 }
 
 template <class T>
@@ -590,7 +599,13 @@ sort_kernel(const __grid_constant__ SortArgs a) {
   const auto count = [&](int& id) {
     bad |= id >= E;
     if (id < 0 || id >= E) id = -1;
-    const uint32_t same = __match_any_sync(~0u, id);
+    // the lanes of the same expert, by its bits
+    uint32_t same = __ballot_sync(~0u, id >= 0);
+    if (id < 0) same = ~same;
+    for (int b = 1; b < E; b <<= 1) {
+      const uint32_t set = __ballot_sync(~0u, id & b);
+      same &= id & b ? set : ~set;
+    }
     int place = 0;
     if (id >= 0) place = own[id] + __popc(same & ((1u << lane) - 1));
     __syncwarp();
