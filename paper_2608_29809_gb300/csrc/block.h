@@ -77,5 +77,8 @@ struct ExpertsArgs {
   unsigned* err;
 };
 cudaError_t launch_experts_linear(const ExpertsArgs& a, cudaStream_t st);
+// The same for few experts of a few rows each, and whether a call is of those.
+bool experts_few(const ExpertsArgs& a);
+cudaError_t launch_experts_few(const ExpertsArgs& a, cudaStream_t st);
 
 }  // namespace rc

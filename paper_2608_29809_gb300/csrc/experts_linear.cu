@@ -20,6 +20,7 @@
 #include "../../include/regioncache.h"
 #include "block.h"
 #include "common.cuh"
+#include "experts_act.cuh"
 #include "fp8.cuh"
 #include "tc_chunks.cuh"
 
@@ -69,36 +70,13 @@ __host__ __device__ constexpr int stage_bytes(int bn) {
   return STAGE_A + (PAIR ? bn / 2 : bn) * BK;
 }
 
-enum Kind { BF16, F32, CODES };
-template <Kind>
+template <ExpertsOut>
 struct TypeOf { typedef bf16 T; };
 template <>
-struct TypeOf<F32> { typedef float T; };
+struct TypeOf<OUT_F32> { typedef float T; };
 template <>
-struct TypeOf<CODES> { typedef uint8_t T; };
+struct TypeOf<OUT_CODES> { typedef uint8_t T; };
 
-// v / (1 + 2^e) of four values with one reciprocal, of the product of the
-// denominators: the special-function unit, a power and a reciprocal each, is what
-// the epilogue waits for.  e is cut to 31, so that the product stays finite; what is
-// cut off is below 2^-31 of v.  Power and reciprocal are good to a few steps of f32.
-__device__ __forceinline__ void over_one_plus(float2& v, float2& w, float2 e, float2 f) {
-  const float2 a = f2_add(make_float2(ex2_ftz(fminf(e.x, 31.f)), ex2_ftz(fminf(e.y, 31.f))),
-                          f2_of(1.f));
-  const float2 b = f2_add(make_float2(ex2_ftz(fminf(f.x, 31.f)), ex2_ftz(fminf(f.y, 31.f))),
-                          f2_of(1.f));
-  const float2 c = f2_mul(a, b);  // (v.x's and w.x's denominators, v.y's and w.y's)
-  const float2 r = f2_mul(f2_of(rcp_ftz(c.x * c.y)), make_float2(c.y, c.x));
-  v = f2_mul(v, f2_mul(r, b));
-  w = f2_mul(w, f2_mul(r, a));
-}
-// GELU by its sigmoid: (1 + tanh a) / 2 = 1 / (1 + exp(-2 a)).
-__device__ __forceinline__ float2 gelu_power(float2 v) {
-  const float k = -2.f * 0.7978845608028654f * 1.4426950408889634f;  // sqrt(2 / pi), log2 e
-  return f2_mul(v, f2_fma(f2_mul(v, v), f2_of(0.044715f * k), f2_of(k)));
-}
-__device__ __forceinline__ float2 silu_power(float2 v) {
-  return f2_mul(v, f2_of(-1.4426950408889634f));
-}
 template <int N, bool GELU>
 __device__ __forceinline__ void activate(float* v) {
 #pragma unroll
@@ -107,12 +85,6 @@ __device__ __forceinline__ void activate(float* v) {
     over_one_plus(a, b, GELU ? gelu_power(a) : silu_power(a), GELU ? gelu_power(b) : silu_power(b));
     v[j] = a.x, v[j + 1] = a.y, v[j + 2] = b.x, v[j + 3] = b.y;
   }
-}
-__device__ __forceinline__ float act_of(int act, float v) {
-  float2 a = f2_of(v), b = f2_of(0.f);
-  if (act == RC_ACT_GELU) over_one_plus(a, b, gelu_power(a), b);
-  if (act == RC_ACT_SILU) over_one_plus(a, b, silu_power(a), b);
-  return a.x;
 }
 // Sums with their bias (in shared memory, 16-byte aligned).
 template <int N>
@@ -178,7 +150,7 @@ __device__ __forceinline__ void rows_sync(int sp) {
 // leaves its part in shared memory, and the parts are added there in order.
 enum Mode { ALONE, PAIRS, SPLIT };
 
-template <Kind OUT, Mode MODE>
+template <ExpertsOut OUT, Mode MODE>
 __global__ void __launch_bounds__(THREADS, 1)
 experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
                       const __grid_constant__ CUtensorMap tmG,
@@ -581,8 +553,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     const int sp = warp & 3, part = (warp - EPI_WARP) >> 2;
     uint8_t* own = stg + (warp - EPI_WARP) * STAGING;
     float* own_bias = biases + (warp - EPI_WARP) * CHUNKS * 32;
-    T* const y = static_cast<T*>(OUT == CODES ? a.y8.codes : a.y);
-    const int ldy = OUT == CODES ? a.y8.ld : a.ldy;
+    T* const y = static_cast<T*>(OUT == OUT_CODES ? a.y8.codes : a.y);
+    const int ldy = OUT == OUT_CODES ? a.y8.ld : a.ldy;
     // the bias of a lane's columns (of a gated tile, a chunk's and then that of the
     // factors), a tile ahead
     Walk wk = first_tile();
@@ -615,7 +587,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i)
         if (left > 0 && (part + 4 * i) * 32 < cols_out &&
-            n0 + (OUT == CODES ? 4 * i : part + 4 * i) * 32 < a.n)
+            n0 + (OUT == OUT_CODES ? 4 * i : part + 4 * i) * 32 < a.n)
           chunks = i + 1;
       if (ok) ok = mbar_sleep_warp(tfull0 + 8 * acc, acc_phase, abort_flag);
       // (after a failed wait the warp goes on to the barriers, without work)
@@ -629,7 +601,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       // sixteen outputs from column `h` of chunk i on (all 32 rows of the warp)
       const auto outputs = [&](int i, int h, float* v) {
         const uint32_t at = tb + uint32_t((part + 4 * i) * 32 + h);
-        const bool last = OUT != CODES && h == 16 && i == chunks - 1;
+        const bool last = OUT != OUT_CODES && h == 16 && i == chunks - 1;
         tmem_ld16(at, v);
         if (gated) {
           add_bias<16>(v, own_bias + h);
@@ -669,7 +641,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 #pragma unroll 1
         for (int i = 0; i < chunks; ++i) {  // (with codes, the four warps of the rows alike)
           const int c0 = n0 + (part + 4 * i) * 32;
-          if constexpr (OUT == CODES) {
+          if constexpr (OUT == OUT_CODES) {
             // the outputs go back to where their sums were until the scale is known
             const uint32_t at = tb + uint32_t((part + 4 * i) * 32);
             uint32_t top = 0;
@@ -728,8 +700,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
                                 lane, v);
                 continue;
               }
-              if (OUT == F32 || h == 0) box_free(lane);
-              if constexpr (OUT == F32) {
+              if (OUT == OUT_F32 || h == 0) box_free(lane);
+              if constexpr (OUT == OUT_F32) {
                 put_pieces<4>(own, lane, 0, reinterpret_cast<const uint32_t*>(v));
                 if (c0 + h < a.n) store_box(&tmY, own, lane, r0, c0 + h);
               } else {
@@ -754,7 +726,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       // the rows' chunks of 32 outputs (128 with codes), dealt to the cluster's warps
       const Tile tl = tile_of(wk);
       const int rows = rows_of(tl, 0);
-      constexpr int LANES = OUT == CODES ? 4 : 1;  // columns of a lane
+      constexpr int LANES = OUT == OUT_CODES ? 4 : 1;  // columns of a lane
       const int chunks = cols_out / (32 * LANES);
       const auto sum = [&](int col, int row) {
         float v = 0.f;
@@ -782,7 +754,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
           v[i] = gated ? act_of(RC_ACT_SILU, v[i]) * (sum(half_bn + col, row) + (b ? __ldg(b + a.n) : 0.f))
                        : act_of(a.act, v[i]);
         }
-        if constexpr (OUT == CODES) {
+        if constexpr (OUT == OUT_CODES) {
           uint32_t top = 0;
 #pragma unroll
           for (int i = 0; i < LANES; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
@@ -845,7 +817,7 @@ struct Choice {
   int bn, parts;
 };
 
-template <Kind OUT, Mode MODE>
+template <ExpertsOut OUT, Mode MODE>
 cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
   constexpr bool PAIR = MODE == PAIRS;
   using T = typename TypeOf<OUT>::T;
@@ -870,7 +842,7 @@ cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
   RC_TRY(tma_map_bytes(a.x.codes, a.x.rows, a.x.cols, a.x.ld, 1, &mg));
   RC_TRY(tma_map_bytes(a.w.codes, a.w.rows, a.w.cols, a.w.ld, PAIR || gated ? bn / 2 : bn, &mw));
   my = mx;  // (not used without tma)
-  if constexpr (OUT != CODES) {
+  if constexpr (OUT != OUT_CODES) {
     const uintptr_t row = uintptr_t(a.ldy) * sizeof(T);
     a.tma = ((reinterpret_cast<uintptr_t>(a.y) | row) & 15u) == 0;
     if (a.tma) RC_TRY(tma_map_boxes(static_cast<T*>(a.y), a.pairs, a.n, a.ldy, &my));
@@ -928,9 +900,9 @@ Choice choose(const ExpertsArgs& a, bool codes) {
   return best;
 }
 
-template <Kind OUT>
+template <ExpertsOut OUT>
 cudaError_t linear(const ExpertsArgs& a, cudaStream_t st) {
-  const Choice c = choose(a, OUT == CODES);
+  const Choice c = choose(a, OUT == OUT_CODES);
   if (c.mode == PAIRS) return go<OUT, PAIRS>(a, c, st);
   if (c.mode == SPLIT) return go<OUT, SPLIT>(a, c, st);
   return go<OUT, ALONE>(a, c, st);
@@ -939,8 +911,9 @@ cudaError_t linear(const ExpertsArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_experts_linear(const ExpertsArgs& a, cudaStream_t st) {
-  if (a.y8.codes) return linear<CODES>(a, st);
-  return a.f32 ? linear<F32>(a, st) : linear<BF16>(a, st);
+  if (experts_few(a)) return launch_experts_few(a, st);
+  if (a.y8.codes) return linear<OUT_CODES>(a, st);
+  return a.f32 ? linear<OUT_F32>(a, st) : linear<OUT_BF16>(a, st);
 }
 
 }  // namespace rc
