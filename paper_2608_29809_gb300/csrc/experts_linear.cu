@@ -34,7 +34,7 @@ constexpr int BM = 128, BK = 128;
 constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 16, MORE_X_WARP = 24;
 constexpr int X_WARPS = 6, THREADS = 32 * (MORE_X_WARP + X_WARPS - 2);
 constexpr int STAGE_A = BM * BK;
-constexpr int RING_BYTES = 168 * 1024, MAX_STAGES = 7;
+constexpr int RING_BYTES = 168 * 1024, MAX_STAGES = 6;
 // tensor memory: accumulators at 0 and ACC_BN (one, where a tile is wider), then a
 // ring of scale words: a batch holds, for each WORD_KB blocks, 4 columns for x and
 // 8 for W
@@ -54,16 +54,16 @@ struct Tables {
 constexpr int TOPS_BYTES = 2 * EPI_WARPS * 32 * 4;
 constexpr int CHUNKS = MAX_BN / 128;  // of an epilogue warp, at most
 constexpr int BIAS_BYTES = EPI_WARPS * CHUNKS * 32 * 4;
-constexpr int FOURS = X_WARPS * ((BM / 4 + X_WARPS - 1) / X_WARPS);  // of rows of x
+constexpr int MOST_FOURS = 16, FOURS = X_WARPS * MOST_FOURS;  // of rows of x, of a warp
 constexpr int STAGING = 32 * 64;  // of an epilogue warp: 32 rows of 64 bytes
 constexpr size_t SMEM_BYTES = size_t(RING_BYTES) + EPI_WARPS * STAGING + SCALE_BYTES +
                               TOPS_BYTES + BIAS_BYTES + FOURS * 16 +
-                              sizeof(Tables) + 1024 + 256;
+                              sizeof(Tables) + 1024 + 192;
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 static_assert(MAX_BN * 129 * 4 <= RING_BYTES, "a split tile's part");
 
 struct Plan {
-  int bn, stages, nt, kb, parts, accs, most;  // most: tiles of TM rows there can be
+  int bn, stages, groups, nt, kb, parts, accs, most;  // most: tiles of TM rows there can be
 };
 template <bool PAIR>
 __host__ __device__ constexpr int stage_bytes(int bn) {
@@ -181,9 +181,9 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   if (threadIdx.x == 0) {
     for (int s = 0; s < MAX_STAGES; ++s) {
       mbar_init(full0 + 8 * s, PAIR ? 1 : 2);  // (x's and W's loads)
-      // (the MMAs, and x's warps, of which none gets a turn of the ring ahead or behind:
-      // some have nothing to load for a tile)
-      mbar_init(empty0 + 8 * s, 1 + X_WARPS);
+      // (the MMAs, and the stage's warps of x, of which none gets a turn of the ring
+      // behind: some have nothing to load for a tile)
+      mbar_init(empty0 + 8 * s, 1 + X_WARPS / pl.groups);
     }
     for (int s = 0; s < SCALES; ++s) {
       mbar_init(sfull0 + 8 * s, 4 * CTAS);
@@ -309,23 +309,26 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   if (warp < SCALE_WARP || warp >= MORE_X_WARP) {
     if (warp == 0 || warp == 3 || warp >= MORE_X_WARP) {
       // ---------------------------------------------------------------- TMA: x
-      // The fours of rows are dealt to the warps; one thread of each issues them (a
-      // lane's own operands would be brought to uniform registers lane by lane).
-      // Lane i < MOST looks up the warp's i-th four, a tile ahead.
+      // Groups of its warps take the ring's stages in turn (a stage is always the same
+      // group's, so that it waits for its own last use), a block's fours of rows dealt
+      // to a group's warps; one thread of each issues them (a lane's own operands
+      // would be brought to uniform registers lane by lane).  Lane i < MOST looks up
+      // the warp's i-th four, a tile ahead.
       const int w = warp == 0 ? 0 : warp == 3 ? 1 : warp - MORE_X_WARP + 2;
-      constexpr int MOST = (BM / 4 + X_WARPS - 1) / X_WARPS;
-      int4* own = fours + w * MOST;
-      int stage = 0;
+      const int groups = pl.groups, of = X_WARPS / groups, group = w / of, wi = w - group * of;
+      int4* own = fours + w * MOST_FOURS;
+      int stage = group, next = group;  // the warp's next block, from the tile's first
       uint32_t phase = 0;
       Walk wk = first_tile();
       Tile tl = {};
       int r[4];
       const auto look_up = [&] {
         tl = tile_of(wk);
-        const int rows = rows_of(tl, int(rank)), at = 4 * (w + X_WARPS * lane);
+        const int rows = rows_of(tl, int(rank)), at = 4 * (wi + of * lane);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          r[j] = lane < MOST && at + j < rows ? row_of(tl.place + int(rank) * BM + at + j) : 0;
+          r[j] = lane < MOST_FOURS && at + j < rows
+                     ? row_of(tl.place + int(rank) * BM + at + j) : 0;
       };
       if (wk.q < m_tiles) look_up();
       while (ok && wk.q < m_tiles) {
@@ -334,39 +337,37 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         const auto bytes = [&](int n) { return in_box(n) ? STAGE_A : (n + 3) / 4 * 4 * BK; };
         int expect = bytes(rows_of(tl, 0));
         if (PAIR) expect += bytes(rows_of(tl, 1)) + BN * BK;
-        if (lane < MOST) own[lane] = make_int4(r[0], r[1], r[2], r[3]);
-        __syncwarp();
-        int4 four[MOST];
-#pragma unroll
-        for (int i = 0; i < MOST; ++i) four[i] = own[i];
+        if (lane < MOST_FOURS) own[lane] = make_int4(r[0], r[1], r[2], r[3]);
         __syncwarp();
         next_tile(wk);
         if (wk.q < m_tiles) look_up();
+        // (fours of this warp, of those that hold rows)
+        const int count = box ? 0 : max(0, ((rows + 3) / 4 - wi + of - 1) / of);
 #pragma unroll 1
-        for (int kb = 0; kb < KB; ++kb) {
+        for (; next < KB; next += groups) {
           ok = mbar_sleep_warp(empty0 + 8 * stage, phase ^ 1, abort_flag);
           if (!ok) break;
           if (elect_one()) {
             const uint32_t st = saddr(smem + stage * STAGE), fb = full0 + 8 * stage;
             const uint32_t bar = PAIR ? mapa_shared(fb, 0) : fb;
-            const int c = (k0 + kb) * BK;
+            const int c = (k0 + next) * BK;
             // (a barrier may see bytes before it is told of them: its phase still
             // needs that arrival)
-            if (rank == 0 && w == 0) mbar_expect_tx(fb, uint32_t(expect));
-            if (!box) {
-#pragma unroll
-              for (int i = 0; i < MOST; ++i)
-                if (4 * (w + X_WARPS * i) < rows)
-                  tma_gather4<PAIR>(st + (w + X_WARPS * i) * 4 * BK, &tmG, bar, c, four[i]);
-            } else if (w == 0) {
+            if (rank == 0 && wi == 0) mbar_expect_tx(fb, uint32_t(expect));
+#pragma unroll 4
+            for (int i = 0; i < count; ++i)
+              tma_gather4<PAIR>(st + (wi + of * i) * 4 * BK, &tmG, bar, c, own[i]);
+            if (box && wi == 0) {
               if (PAIR) tma_load_2d_pair(st, &tmX, bar, c, place);
               else tma_load_2d(st, &tmX, bar, c, place);
             }
             mbar_arrive(empty0 + 8 * stage);
           }
           __syncwarp();
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          stage += groups;
+          if (stage >= STAGES) { stage -= STAGES; phase ^= 1; }
         }
+        next -= KB;
       }
     } else if (warp == 2) {
       // ---------------------------------------------------------------- TMA: W
@@ -829,7 +830,10 @@ cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
   Plan pl;
   pl.bn = bn;
   const int fit = RING_BYTES / stage_bytes<PAIR>(bn);
-  pl.stages = fit < MAX_STAGES ? fit : MAX_STAGES;
+  // (stages are dealt to groups of x's six warps: a multiple of the groups, which are
+  // of two or three)
+  pl.stages = fit >= 6 ? 6 : fit >= 4 ? 4 : 3;
+  pl.groups = pl.stages == 4 ? 2 : 3;
   pl.nt = (a.n - 1) / cols_out + 1;
   pl.kb = (a.x.cols - 1) / BK + 1;
   pl.parts = ch.parts;
