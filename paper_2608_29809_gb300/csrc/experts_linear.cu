@@ -41,7 +41,8 @@ constexpr int RING_BYTES = 168 * 1024, MAX_STAGES = 6;
 constexpr int ACC_BN = 192, MAX_BN = 256, SCALE_COL = 2 * ACC_BN, TMEM_COLS = 512;
 constexpr int WORD_KB = 4, SCALE_BATCH = 16, SCALE_GROUPS = SCALE_BATCH / WORD_KB;
 constexpr int SCALE_STEP = 12, SCALE_SLOT = SCALE_GROUPS * SCALE_STEP, SCALES = 2;
-static_assert(SCALE_COL + SCALES * SCALE_SLOT <= TMEM_COLS, "tensor memory");
+static_assert(SCALE_COL + SCALES * SCALE_SLOT <= TMEM_COLS && MAX_BN + 128 <= SCALE_COL,
+              "tensor memory");
 // the batch's words in shared memory: 128 rows of x, four shared rows of W
 constexpr int SCALE_ROWS = 128 + 4, SCALE_BYTES = SCALE_GROUPS * SCALE_ROWS * 4;
 // the experts that have rows: tiles before, first row, end, number
@@ -571,6 +572,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
           bias[i] = __ldg(a.bias + (long long)tl.expert * N + c + (gated && i > 0 ? a.n : 0));
       }
     };
+    const bool in_place = OUT == OUT_CODES && ACCS > 1;
     int acc = 0, turn = 0;
     uint32_t acc_phase = 0;
     if (wk.q < m_tiles) fetch();
@@ -602,7 +604,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       // sixteen outputs from column `h` of chunk i on (all 32 rows of the warp)
       const auto outputs = [&](int i, int h, float* v) {
         const uint32_t at = tb + uint32_t((part + 4 * i) * 32 + h);
-        const bool last = OUT != OUT_CODES && h == 16 && i == chunks - 1;
+        const bool last = !in_place && h == 16 && i == chunks - 1;
         tmem_ld16(at, v);
         if (gated) {
           add_bias<16>(v, own_bias + h);
@@ -643,8 +645,11 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         for (int i = 0; i < chunks; ++i) {  // (with codes, the four warps of the rows alike)
           const int c0 = n0 + (part + 4 * i) * 32;
           if constexpr (OUT == OUT_CODES) {
-            // the outputs go back to where their sums were until the scale is known
-            const uint32_t at = tb + uint32_t((part + 4 * i) * 32);
+            // the outputs wait in tensor memory until the scale is known: where their
+            // sums were, or beside an only accumulator, which is free again the sooner
+            const uint32_t at = in_place ? tb + uint32_t((part + 4 * i) * 32)
+                                         : tmem + uint32_t(MAX_BN + part * 32) +
+                                               (uint32_t(sp * 32) << 16);
             uint32_t top = 0;
 #pragma unroll 1
             for (int h = 0; ok && h < 32; h += 16) {
@@ -674,7 +679,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
             for (int h = 0; h < 32; h += 16, dst += 16) {
               float v[16];
               tmem_ld16(at + uint32_t(h), v);
-              if (h == 16 && i == chunks - 1) release();
+              if (in_place && h == 16 && i == chunks - 1) release();
               uint32_t q[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k)
@@ -817,6 +822,12 @@ struct Choice {
   Mode mode;
   int bn, parts;
 };
+// Stages of the ring: dealt to groups of x's six warps, of two or three, and so a
+// multiple of the groups.
+int stages_of(bool pair, int bn) {
+  const int fit = RING_BYTES / (pair ? stage_bytes<true>(bn) : stage_bytes<false>(bn));
+  return fit >= 6 ? 6 : fit >= 4 ? 4 : 3;
+}
 
 template <ExpertsOut OUT, Mode MODE>
 cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
@@ -829,10 +840,7 @@ cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
   const int bn = ch.bn, cols_out = gated ? bn / 2 : bn;
   Plan pl;
   pl.bn = bn;
-  const int fit = RING_BYTES / stage_bytes<PAIR>(bn);
-  // (stages are dealt to groups of x's six warps: a multiple of the groups, which are
-  // of two or three)
-  pl.stages = fit >= 6 ? 6 : fit >= 4 ? 4 : 3;
+  pl.stages = stages_of(PAIR, bn);
   pl.groups = pl.stages == 4 ? 2 : 3;
   pl.nt = (a.n - 1) / cols_out + 1;
   pl.kb = (a.x.cols - 1) / BK + 1;
@@ -863,31 +871,37 @@ cudaError_t go(ExpertsArgs a, const Choice& ch, cudaStream_t st) {
 }
 
 // The tile width, and how CTAs share a tile, of least estimated duration (SM
-// cycles; rates as rc_fp8_linear's), for experts with even shares of the places.
+// cycles), for experts with even shares of the places.  A block of columns takes what
+// rc_fp8_linear's does, or a stage's way round by the number of stages: 1000 of
+// latencies, the MMAs, and 900 for 128 gathered rows (alone at 256 columns, three
+// stages, the gated 4128 x 2 rows of 16 experts to codes took 67 us).
 Choice choose(const ExpertsArgs& a, bool codes) {
   const bool gated = a.act == RC_ACT_GATED_SILU;
   const int kb = (a.x.cols - 1) / BK + 1;
   const long long used = a.pairs < a.experts ? a.pairs : a.experts;
   const double rows = double(a.pairs) / double(used);  // of an expert
   // (uneven shares: half a tile more for each expert)
-  const auto m_tiles = [&](int high) { return rows <= high / 2 ? double(used)
-                                                               : a.pairs / double(high) + 0.5 * used; };
+  const auto m_tiles = [&](int high) {
+    return rows <= high / 2 ? double(used) : a.pairs / double(high) + 0.5 * used;
+  };
   Choice best{ALONE, gated ? 256 : 128, 1};
   double least = 1e30;
   const auto look = [&](Mode mode, int bn, int parts) {
     const long long nt = (a.n - 1) / (gated ? bn / 2 : bn) + 1;
     const double tiles = m_tiles(mode == PAIRS ? 2 * BM : BM) * nt;
     const double x = rows < BM ? rows / BM : 1;  // of a full tile's rows
+    const double round = 1000 + 2.0 * bn + (a.source ? 900 * x : 100);
+    double block = mode == PAIRS ? 405 + 0.42 * bn : 60 + 160 * x + 1.83 * bn;
+    if (block < round / stages_of(mode == PAIRS, bn)) block = round / stages_of(mode == PAIRS, bn);
     double cost;
     if (mode == SPLIT) {
       if (most_tiles(a, BM) * nt * parts > SMS - 8) return;
-      cost = (kb + parts - 1) / parts * (60 + 160 * x + 1.83 * bn) + 4.0 * bn + 600 + 800 * parts;
+      cost = (kb + parts - 1) / parts * block + 4.0 * bn + 600 + 800 * parts;
     } else {
       const double slots = mode == PAIRS ? SMS / 2 : SMS;
       const double waves = tiles <= slots ? 1 : ceil(tiles / slots - 0.05);
-      cost = waves * (mode == PAIRS ? kb * (405 + 0.42 * bn) + 9.5 * bn
-                                    : kb * (60 + 160 * x + 1.83 * bn) + 7.0 * bn);
-      if (bn > ACC_BN) cost += (waves - 1) * 12.0 * bn;  // (the only accumulator is drained)
+      cost = waves * kb * block + (mode == PAIRS ? 9.5 : 7.0) * bn;
+      if (bn > ACC_BN) cost += (waves - 1) * 6.0 * bn;  // (the only accumulator is drained)
       if (mode == PAIRS) cost += 3000;
     }
     if (cost < least) {
