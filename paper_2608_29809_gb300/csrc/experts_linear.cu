@@ -52,13 +52,13 @@ struct Tables {
   uint16_t expert[MAX_E];
   unsigned long long parts[THREADS / 32];
 };
-constexpr int TOPS_BYTES = 2 * EPI_WARPS * 32 * 4;
+constexpr int LIST = 256;  // tiles of a CTA that are looked up once
 constexpr int CHUNKS = MAX_BN / 128;  // of an epilogue warp, at most
 constexpr int BIAS_BYTES = EPI_WARPS * CHUNKS * 32 * 4;
 constexpr int MOST_FOURS = 16, FOURS = X_WARPS * MOST_FOURS;  // of rows of x, of a warp
 constexpr int STAGING = 32 * 64;  // of an epilogue warp: 32 rows of 64 bytes
 constexpr size_t SMEM_BYTES = size_t(RING_BYTES) + EPI_WARPS * STAGING + SCALE_BYTES +
-                              TOPS_BYTES + BIAS_BYTES + FOURS * 16 +
+                              LIST * 16 + BIAS_BYTES + FOURS * 16 +
                               sizeof(Tables) + 1024 + 192;
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
 static_assert(MAX_BN * 129 * 4 <= RING_BYTES, "a split tile's part");
@@ -166,8 +166,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
                                              ~uintptr_t(1023));
   uint8_t* stg = smem + RING_BYTES;
   uint32_t* words = reinterpret_cast<uint32_t*>(stg + EPI_WARPS * STAGING);
-  uint32_t* tops = words + SCALE_BYTES / 4;
-  float* biases = reinterpret_cast<float*>(tops + TOPS_BYTES / 4);
+  int4* list = reinterpret_cast<int4*>(words + SCALE_BYTES / 4);
+  float* biases = reinterpret_cast<float*>(list + LIST);
   int4* fours = reinterpret_cast<int4*>(biases + BIAS_BYTES / 4);
   Tables& tab = *reinterpret_cast<Tables*>(fours + FOURS);
   uint64_t* bars = reinterpret_cast<uint64_t*>(&tab + 1);
@@ -250,50 +250,51 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     // (offsets that descend can name rows twice)
     entries = int(all >> 32), m_tiles = int(min(all & 0xffffffffull, (unsigned long long)pl.most));
   }
+  // this CTA's (or pair's) tiles pos, pos + G ..: expert, first place, places left there
+  // and number among the columns.  The first LIST of them are found here, once for all
+  // warps.
+  const int parts = MODE == SPLIT ? pl.parts : 1;
+  const int G = int(gridDim.x) / (CTAS * parts), pos = int(blockIdx.x) / (CTAS * parts);
+  struct Tile { int expert, place, left, n; };
+  const auto search = [&](int t) {
+    const int q = t / pl.nt;
+    int lo = 0, hi = entries;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (tab.first[mid] <= q) lo = mid;
+      else hi = mid;
+    }
+    const int p = tab.row[lo] + (q - tab.first[lo]) * TM;
+    return Tile{tab.expert[lo], p, tab.end[lo] - p, t - q * pl.nt};
+  };
+  const int own_tiles = m_tiles * pl.nt > pos ? (m_tiles * pl.nt - pos - 1) / G + 1 : 0;
+  __syncthreads();
+  if (threadIdx.x < min(LIST, own_tiles)) {
+    const Tile t = search(pos + int(threadIdx.x) * G);
+    list[threadIdx.x] = make_int4(t.expert, t.place, t.left, t.n);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   if (PAIR) cluster_sync();  // (the peer's barriers are ready)
 
+  const auto tile_of = [&](int i) {
+    if (i >= LIST) return search(pos + i * G);
+    const int4 t = list[i];
+    return Tile{t.x, t.y, t.z, t.w};
+  };
+
   const int BN = pl.bn, STAGES = pl.stages, ACCS = pl.accs;
   const int STAGE = stage_bytes<PAIR>(BN);
   const bool gated = a.act == RC_ACT_GATED_SILU;
   const int half_bn = BN / 2, cols_out = gated ? half_bn : BN;  // outputs of a tile
   const int e_rows = a.w.rows / a.experts, N = gated ? 2 * a.n : a.n;
-  // this CTA's (or pair's) tiles pos, pos + G .. and, of each, its blocks
-  // k0 .. k0 + KB - 1
-  const int parts = MODE == SPLIT ? pl.parts : 1;
+  // of each tile, this CTA's blocks k0 .. k0 + KB - 1
   const int part_of = MODE == SPLIT ? int(cluster_ctarank()) : 0;
   const int k0 = part_of * pl.kb / parts, KB = (part_of + 1) * pl.kb / parts - k0;
-  const int G = int(gridDim.x) / (CTAS * parts), pos = int(blockIdx.x) / (CTAS * parts);
   bool ok = true;
 
-  // The CTA's (or pair's) tiles, `step` apart: M tile (of all experts'), number among
-  // the columns and entry of the tables.
-  struct Walk { int q, n, i; };
-  const auto locate = [&](Walk& w) {
-    while (w.i + 8 < entries && tab.first[w.i + 8] <= w.q) w.i += 8;
-    while (w.i + 1 < entries && tab.first[w.i + 1] <= w.q) ++w.i;
-  };
-  const int step_q = G / pl.nt, step_n = G - step_q * pl.nt;
-  const auto first_tile = [&] {
-    Walk w{pos / pl.nt, pos % pl.nt, 0};
-    locate(w);
-    return w;
-  };
-  const auto next_tile = [&](Walk& w) {
-    w.q += step_q;
-    w.n += step_n;
-    if (w.n >= pl.nt) w.n -= pl.nt, ++w.q;
-    if (w.q < m_tiles) locate(w);
-  };
-  // a tile's expert, first place, places left there and number among the columns
-  struct Tile { int expert, place, left, n; };
-  const auto tile_of = [&](const Walk& w) {
-    const int p = tab.row[w.i] + (w.q - tab.first[w.i]) * TM;
-    return Tile{tab.expert[w.i], p, tab.end[w.i] - p, w.n};
-  };
   // rows of a CTA of this tile (the second of a pair may have none)
   const auto rows_of = [&](const Tile& t, int r) { return max(0, min(BM, t.left - r * BM)); };
   // the row of x of a place (row 0 for one outside, which is reported)
@@ -320,19 +321,19 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       int4* own = fours + w * MOST_FOURS;
       int stage = group, next = group;  // the warp's next block, from the tile's first
       uint32_t phase = 0;
-      Walk wk = first_tile();
+      int tile = 0;
       Tile tl = {};
       int r[4];
       const auto look_up = [&] {
-        tl = tile_of(wk);
+        tl = tile_of(tile);
         const int rows = rows_of(tl, int(rank)), at = 4 * (wi + of * lane);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           r[j] = lane < MOST_FOURS && at + j < rows
                      ? row_of(tl.place + int(rank) * BM + at + j) : 0;
       };
-      if (wk.q < m_tiles) look_up();
-      while (ok && wk.q < m_tiles) {
+      if (tile < own_tiles) look_up();
+      while (ok && tile < own_tiles) {
         const int rows = rows_of(tl, int(rank)), place = tl.place + int(rank) * BM;
         const bool box = in_box(rows);
         const auto bytes = [&](int n) { return in_box(n) ? STAGE_A : (n + 3) / 4 * 4 * BK; };
@@ -340,8 +341,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         if (PAIR) expect += bytes(rows_of(tl, 1)) + BN * BK;
         if (lane < MOST_FOURS) own[lane] = make_int4(r[0], r[1], r[2], r[3]);
         __syncwarp();
-        next_tile(wk);
-        if (wk.q < m_tiles) look_up();
+        ++tile;
+        if (tile < own_tiles) look_up();
         // (fours of this warp, of those that hold rows)
         const int count = box ? 0 : max(0, ((rows + 3) / 4 - wi + of - 1) / of);
 #pragma unroll 1
@@ -375,8 +376,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       if (elect_one()) {
         int stage = 0;
         uint32_t phase = 0;
-        for (Walk wk = first_tile(); ok && wk.q < m_tiles; next_tile(wk)) {
-          const Tile tl = tile_of(wk);
+        for (int tile = 0; ok && tile < own_tiles; ++tile) {
+          const Tile tl = tile_of(tile);
           const int n0 = tl.expert * e_rows + tl.n * cols_out;
           for (int kb = 0; kb < KB; ++kb) {
             if (!mbar_sleep(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
@@ -399,7 +400,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       if (PAIR && rank == 1 && elect_one()) {
         int acc = 0;
         uint32_t acc_phase = 0;
-        for (Walk wk = first_tile(); ok && wk.q < m_tiles; next_tile(wk)) {
+        for (int tile = 0; ok && tile < own_tiles; ++tile) {
           ok = mbar_sleep(tempty0 + 8 * acc, acc_phase, abort_flag);
           if (!ok) break;
           tc_fence_after();
@@ -415,7 +416,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         uint32_t phase = 0, acc_phase = 0, sc_phase = 0;
         uint64_t so = 0;     // the stage's offset in the descriptors' address field
         bool ready = false;  // the current stage was seen full already
-        for (Walk wk = first_tile(); ok && wk.q < m_tiles; next_tile(wk)) {
+        for (int tile = 0; ok && tile < own_tiles; ++tile) {
           if (!mbar_wait(tempty0 + 8 * acc, acc_phase ^ 1, abort_flag)) { ok = false; break; }
           const uint32_t d = tmem + uint32_t(acc * ACC_BN);
           uint32_t accumulate = 0;
@@ -472,10 +473,10 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     bool in = false;  // the thread's row is one of the expert's
     int xrow = 0;
     Tile tl = {};
-    Walk wk = first_tile();
+    int tile = 0;
     const auto fetch = [&](int kb) {
       if (kb == 0) {
-        tl = tile_of(wk);
+        tl = tile_of(tile);
         in = tid < rows_of(tl, int(rank));
         xrow = in ? row_of(tl.place + int(rank) * BM + tid) : 0;
       }
@@ -494,8 +495,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     };
     int sc = 0, kb = 0;
     uint32_t sc_phase = 0;
-    if (wk.q < m_tiles) fetch(0);
-    while (wk.q < m_tiles) {
+    if (tile < own_tiles) fetch(0);
+    while (tile < own_tiles) {
       scale_sync();  // (the batch before has been taken)
 #pragma unroll
       for (int g = 0; g < SCALE_GROUPS; ++g)
@@ -518,8 +519,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         of[i] = 128 + min(of[i], 3);
       }
       kb += SCALE_BATCH;
-      if (kb >= KB) kb = 0, next_tile(wk);
-      if (wk.q < m_tiles) fetch(kb);
+      if (kb >= KB) kb = 0, ++tile;
+      if (tile < own_tiles) fetch(kb);
       if (ok) ok = mbar_sleep(sempty0 + 8 * sc, sc_phase ^ 1, abort_flag);
       // (after a failed wait the warp goes on to the barriers, without work)
       ok = __all_sync(0xffffffffu, ok);
@@ -559,11 +560,11 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     const int ldy = OUT == OUT_CODES ? a.y8.ld : a.ldy;
     // the bias of a lane's columns (of a gated tile, a chunk's and then that of the
     // factors), a tile ahead
-    Walk wk = first_tile();
+    int tile = 0;
     Tile tl = {};
     float bias[CHUNKS];
     const auto fetch = [&] {
-      tl = tile_of(wk);
+      tl = tile_of(tile);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
         const int ch = gated ? part : part + 4 * i, c = tl.n * cols_out + ch * 32 + lane;
@@ -575,16 +576,16 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
     const bool in_place = OUT == OUT_CODES && ACCS > 1;
     int acc = 0, turn = 0;
     uint32_t acc_phase = 0;
-    if (wk.q < m_tiles) fetch();
-    while (wk.q < m_tiles) {
+    if (tile < own_tiles) fetch();
+    while (tile < own_tiles) {
       const int left = rows_of(tl, int(rank)) - sp * 32;  // the warp's rows, from `r0`
       const int r0 = tl.place + int(rank) * BM + sp * 32, n0 = tl.n * cols_out;
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) own_bias[i * 32 + lane] = bias[i];
       __syncwarp();
-      next_tile(wk);
-      if (wk.q < m_tiles) fetch();
+      ++tile;
+      if (tile < own_tiles) fetch();
       // the warp's chunks that hold outputs (with codes, all four of a scale's columns)
       int chunks = 0;
 #pragma unroll
@@ -663,7 +664,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
               tmem_st16(at + uint32_t(h), reinterpret_cast<const uint32_t*>(v));
             }
             tmem_wait_st();
-            uint32_t* to = tops + turn * EPI_WARPS * 32 + sp * 32 + lane;
+            uint32_t* to = reinterpret_cast<uint32_t*>(stg) + turn * EPI_WARPS * 32 + sp * 32 + lane;
             to[part * 128] = top;
             rows_sync(sp);
 #pragma unroll
@@ -727,10 +728,10 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   }
   if (MODE == SPLIT) {
     cluster_sync();
-    const Walk wk = first_tile();
-    if (wk.q < m_tiles) {
+    const int tile = 0;
+    if (tile < own_tiles) {
       // the rows' chunks of 32 outputs (128 with codes), dealt to the cluster's warps
-      const Tile tl = tile_of(wk);
+      const Tile tl = tile_of(tile);
       const int rows = rows_of(tl, 0);
       constexpr int LANES = OUT == OUT_CODES ? 4 : 1;  // columns of a lane
       const int chunks = cols_out / (32 * LANES);
