@@ -287,16 +287,26 @@ __device__ __forceinline__ void pairs_of(const float* u, float2* v) {
   for (int k = 0; k < 4; ++k) v[k] = make_float2(u[2 * k], u[2 * k + 1]);
 }
 
-// TY: bf16 or float where x, h, x_out and y (of that type) are all there with whole,
-// aligned vectors and no places; void for everything else (the tests of what there
-// is, for each vector, took half of the instructions).
-template <class TX, class TH, class TY, int THREADS>
+// FORM says what there is, with whole, aligned vectors: NEXT_BF16, NEXT_F32 x, h (without
+// places), x_out and y of that type; CODES x and y8 alone; JOIN x, h by places and x_out.
+// ANY is everything else (the tests of what there is, for each vector, took half of the
+// instructions: 4128 x 1152 f32 to codes 8.4 us for 10.6, joined with two bf16 rows of
+// each by places, looked up once, 7.9 for 12.6).
+enum Form { ANY, NEXT_BF16, NEXT_F32, CODES, JOIN };
+// Places and weights that a CTA has in shared memory at once; RC_EXPERTS_MAX_TOP_K of a
+// row at most.
+constexpr int PAIRS = 512;
+template <class TX, class TH, Form FORM, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 2 : 1)
 norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
-  constexpr bool PLAIN = !std::is_void<TY>::value;
+  constexpr bool PLAIN = FORM != ANY, NEXT = FORM == NEXT_BF16 || FORM == NEXT_F32,
+                 MAY_JOIN = FORM == ANY || FORM == JOIN;
+  using TY = std::conditional_t<FORM == NEXT_F32, float, bf16>;
   constexpr int DEPTH = depth<TX, TH, THREADS>();
   extern __shared__ uint4 staged[];  // [DEPTH][ROWS][threads] of x, then of h
   __shared__ float slots[2][2][32];
+  __shared__ int place_of[MAY_JOIN ? PAIRS : 1];
+  __shared__ float weight_of[MAY_JOIN ? PAIRS : 1];
   for (int i = threadIdx.x; i < 128; i += blockDim.x) (&slots[0][0][0])[i] = 0.f;
   __syncthreads();
   pdl_wait();
@@ -313,7 +323,8 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
   Eight<TX>* sx = reinterpret_cast<Eight<TX>*>(staged) + threadIdx.x;
   Eight<TH>* sh = reinterpret_cast<Eight<TH>*>(reinterpret_cast<Eight<TX>*>(staged) +
                                                DEPTH * ROWS * blockDim.x) + threadIdx.x;
-  const bool own_h = h && a.top_k == 0;
+  const int top_k = MAY_JOIN ? a.top_k : 0;
+  const bool own_h = FORM == ANY ? h && top_k == 0 : NEXT;
   // rows are staged in order, a group of copies for each; `to` and `at` are the places
   // of the next to be staged and to be read (in rows of the CTA's threads)
   const int step = blockDim.x, places = DEPTH * ROWS * step;
@@ -323,7 +334,8 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
   const auto fetch = [&] {
     if (staged_to < last && n > 0) {
       if (PLAIN) {
-        stage(sx + to, px, 8, true), stage(sh + to, ph, 8, true);
+        stage(sx + to, px, 8, true);
+        if (NEXT) stage(sh + to, ph, 8, true);
       } else {
         if (x) stage(sx + to, px, n, wide_x);
         if (own_h) stage(sh + to, ph, n, wide_h);
@@ -342,19 +354,34 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
     Eight<TH> zh;
     zx.zero(), zh.zero();
     if (n <= 0 || !x) sx[i * step] = zx;
-    if (n <= 0 || !own_h) sh[i * step] = zh;
+    if (n <= 0 && own_h) sh[i * step] = zh;
   }
 #pragma unroll 1
   for (int i = 0; i < DEPTH * ROWS; ++i) fetch();
   TX* po = x_out + (long long)row * a.ldx_out + c;
-  const bool codes = a.y8.codes, y_wide = a.y_f32 ? wide_rows(static_cast<float*>(a.y), a.ldy)
+  const bool codes = FORM == ANY ? a.y8.codes != nullptr : FORM == CODES,
+             y_wide = a.y_f32 ? wide_rows(static_cast<float*>(a.y), a.ldy)
                                                   : wide_rows(static_cast<bf16*>(a.y), a.ldy);
   const int y_size = a.y_f32 ? 4 : 2;
   const long long y_step = (long long)a.ldy * y_size;
   uint8_t* py = static_cast<uint8_t*>(a.y) + row * y_step + c * y_size;
   const float cols = float(a.cols), part = 1.f / cols;
   float2 pa[4], pb[4], qa[4], qb[4];  // of the branch and of y; zero outside the row
+  int paired = row, pairs_from = row;  // rows whose places are in shared memory (-2: one
+                                       // that there is not, of no consequence elsewhere)
   while (row < last) {
+    if (MAY_JOIN && top_k > 0 && row + ROWS > paired && paired < last) {
+      __syncthreads();
+      pairs_from = row, paired = min(last, row + PAIRS / top_k);
+      for (int i = threadIdx.x; i < (paired - row) * top_k; i += step) {
+        const long long pair = (long long)row * top_k + i;
+        const int place = a.places[pair];
+        const bool there = place >= 0 && place < a.h_rows;
+        place_of[i] = there ? place : place < 0 ? -1 : -2;
+        weight_of[i] = there ? a.weights[pair] : 0.f;
+      }
+      __syncthreads();
+    }
     if (row >= end) {
       // (what does not depend on the item is on its way while that is looked up)
       float t[8], b[8], t2[8], b2[8], u[8], u2[8];
@@ -388,7 +415,9 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
       // (behind the last row: of no consequence)
       const int from = at + r * step < places ? at + r * step : at + r * step - places;
       const Eight<TX> ex = sx[from];
-      const Eight<TH> eh = sh[from];
+      Eight<TH> eh;
+      if (own_h) eh = sh[from];
+      else eh.zero();
       float u[8];
       unpack(ex, u), pairs_of(u, v[r]);
       unpack(eh, u), pairs_of(u, b[r]);
@@ -408,18 +437,19 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
       continue;
     }
     const float2 scale = f2_of(a.residual_scale);
-    if (PLAIN || h) {
-      for (int j = 0; !PLAIN && j < a.top_k; ++j) {
+    if (PLAIN ? FORM != CODES : h != nullptr) {
+#pragma unroll 2
+      for (int j = 0; j < top_k; ++j) {
         Eight<TH> e[ROWS];
         float w[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-          const long long pair = (long long)(row + (r < rows ? r : 0)) * a.top_k + j;
-          const int place = r < rows ? a.places[pair] : -1;
-          const bool there = place >= 0 && place < a.h_rows;
-          if (place >= a.h_rows && threadIdx.x == 0) atomicOr(a.err, DEVERR_INDEX);
-          w[r] = there ? a.weights[pair] : 0.f;
-          load(e[r], h + (long long)place * a.ldh + c, there ? n : 0, wide_h);
+          const int pair = (row - pairs_from + (r < rows ? r : 0)) * top_k + j;
+          const int place = place_of[pair];
+          w[r] = weight_of[pair];
+          if (place == -2 && threadIdx.x == 0) atomicOr(a.err, DEVERR_INDEX);
+          load(e[r], h + (long long)place * a.ldh + c, place < 0 || n <= 0 ? 0 : PLAIN ? 8 : n,
+               PLAIN || wide_h);
         }
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -444,13 +474,13 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[r][k] = f2_mul(v[r][k], scale);
     }
-    if (PLAIN || x_out) {
+    if (PLAIN ? FORM != CODES : x_out != nullptr) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
         if (r < rows && n > 0)
           store(po + (long long)r * a.ldx_out, &v[r][0].x, PLAIN ? 8 : n, PLAIN || wide_out);
     }
-    if (PLAIN || a.y || codes) {
+    if (PLAIN ? FORM != JOIN : a.y || codes) {
       float root[ROWS];
       standardise<PLAIN>(a.pre, v, root, n, cols, part, slots, turn);
 #pragma unroll
@@ -459,7 +489,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           v[r][k] = f2_fma(f2_mul(v[r][k], f2_of(root[r])), qa[k], qb[k]);
-        if constexpr (PLAIN) {
+        if constexpr (NEXT) {
           if (n > 0) store(reinterpret_cast<TY*>(py + r * y_step), &v[r][0].x, 8, true);
           continue;
         }
@@ -577,22 +607,23 @@ norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
 
 constexpr int SMS = 152;
 
-template <class TX, class TH, class TY, int THREADS>
+template <class TX, class TH, Form FORM, int THREADS>
 cudaError_t rows(const ResidualArgs& a, int threads, int ctas, cudaStream_t st) {
+  const bool own_h = a.h && a.top_k == 0;
   const size_t smem = size_t(depth<TX, TH, THREADS>()) * ROWS * threads * 8 *
-                      (sizeof(TX) + sizeof(TH));
+                      (sizeof(TX) + (own_h ? sizeof(TH) : 0));
   // (an attribute of the current device, so set for each call)
-  RC_TRY(cudaFuncSetAttribute(norm_rows_kernel<TX, TH, TY, THREADS>,
+  RC_TRY(cudaFuncSetAttribute(norm_rows_kernel<TX, TH, FORM, THREADS>,
                               cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
-  return launch_k(norm_rows_kernel<TX, TH, TY, THREADS>,
+  return launch_k(norm_rows_kernel<TX, TH, FORM, THREADS>,
                   dim3(unsigned(a.rows < SMS * ctas ? a.rows : SMS * ctas)),
                   dim3(unsigned(threads)), smem, st, a);
 }
-template <class TX, class TH, class TY>
-cudaError_t of_type(const ResidualArgs& a, int threads, cudaStream_t st) {
+template <class TX, class TH, Form FORM>
+cudaError_t of_form(const ResidualArgs& a, int threads, cudaStream_t st) {
   // (CTAs that an SM holds at once, by their registers)
-  if (threads <= 256) return rows<TX, TH, TY, 256>(a, threads, threads <= 160 ? 3 : 2, st);
-  return rows<TX, TH, TY, 640>(a, threads, 1, st);
+  if (threads <= 256) return rows<TX, TH, FORM, 256>(a, threads, threads <= 160 ? 3 : 2, st);
+  return rows<TX, TH, FORM, 640>(a, threads, 1, st);
 }
 
 template <class TX, class TH>
@@ -605,11 +636,16 @@ cudaError_t go(const ResidualArgs& a, cudaStream_t st) {
   const auto wide = [](const void* p, long long ld, int size) {
     return p && ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld * size)) & 15) == 0;
   };
-  const bool plain = a.cols % 8 == 0 && a.top_k == 0 && wide(a.x, a.ldx, sizeof(TX)) &&
-                     wide(a.h, a.ldh, sizeof(TH)) && wide(a.x_out, a.ldx_out, sizeof(TX)) &&
-                     wide(a.y, a.ldy, a.y_f32 ? 4 : 2);
-  if (!plain) return of_type<TX, TH, void>(a, threads, st);
-  return a.y_f32 ? of_type<TX, TH, float>(a, threads, st) : of_type<TX, TH, bf16>(a, threads, st);
+  const bool x = a.cols % 8 == 0 && wide(a.x, a.ldx, sizeof(TX)),
+             h = wide(a.h, a.ldh, sizeof(TH)), out = wide(a.x_out, a.ldx_out, sizeof(TX)),
+             y = wide(a.y, a.ldy, a.y_f32 ? 4 : 2);
+  if (x && !a.h && !a.x_out && a.y8.codes) return of_form<TX, bf16, CODES>(a, threads, st);
+  if (x && h && out && a.top_k > 0 && !a.y && !a.y8.codes)
+    return of_form<TX, TH, JOIN>(a, threads, st);
+  if (x && h && out && a.top_k == 0 && y)
+    return a.y_f32 ? of_form<TX, TH, NEXT_F32>(a, threads, st)
+                   : of_form<TX, TH, NEXT_BF16>(a, threads, st);
+  return of_form<TX, TH, ANY>(a, threads, st);
 }
 
 }  // namespace

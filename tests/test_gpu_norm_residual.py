@@ -170,6 +170,35 @@ def test_sums_of_expert_rows(lib, rows, cols, k, th):
     B.close(x_out, x1, dx, F32)
 
 
+@pytest.mark.parametrize("rows,cols,k", [(40000, 8, 16), (30001, 20, 11)])
+def test_sums_where_many_rows_have_many_places(lib, rows, cols, k):
+    """More of them than a CTA holds at once; whole sums of small numbers, so exact."""
+    R, ctx = lib
+    pairs = rows * k // 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    h = torch.randint(-8, 9, (pairs, cols), generator=g, device="cuda").float()
+    x = torch.randint(-8, 9, (rows, cols), generator=g, device="cuda").float()
+    places = torch.randint(-pairs // 8, pairs, (rows, k), generator=g, device="cuda").int()
+    w = torch.randint(-4, 5, (rows, k), generator=g, device="cuda").float()
+    want = x + torch.where((places >= 0)[:, :, None],
+                           h[places.long().clamp(min=0)] * w[:, :, None], 0.0).sum(1)
+    R.rc_norm_residual(ctx, R.ResidualNorm(cols, x=x, h=h, x_out=x, places=places, weights=w))
+    R.rc_sync(ctx)
+    assert torch.equal(x, want)
+
+
+def test_places_of_rows_without_an_item_are_not_read_as_such(lib):
+    R, ctx = lib
+    h, x, out = _rand(4, 64, seed=1), _rand(5, 64, seed=2), torch.full((5, 64), 7.0, device="cuda")
+    places = torch.tensor([[9], [2], [0], [2 ** 31 - 1], [4]], dtype=torch.int32, device="cuda")
+    R.rc_norm_residual(ctx, R.ResidualNorm(
+        64, x=x, h=h, x_out=out, places=places, weights=torch.ones(5, 1, device="cuda"),
+        row_offsets=torch.tensor([1, 3], dtype=torch.int32, device="cuda")))
+    R.rc_sync(ctx)
+    assert torch.equal(out[1:3], x[1:3] + h[[2, 0]])
+    assert bool((out[[0, 3, 4]] == 7).all())
+
+
 def test_bad_places_are_passed_over_and_reported(lib):
     R, ctx = lib
     h, x = _rand(4, 64, seed=1), _rand(2, 64, seed=2)
