@@ -192,6 +192,7 @@ rc_status rc_rotary_apply(rc_ctx* c, const rc_rotary* plan, const void* x, int l
   RC_CHECK(check_device(c, fn));
   rc::RotaryArgs a = {};
   a.plan = *plan;
+  for (int i = plan->axes; i < 3; ++i) a.plan.pairs[i] = 0;  // (whatever a caller left there)
   a.x = x, a.y = y, a.ldx = ldx, a.ldy = ldy;
   a.rows = rows, a.heads = heads, a.head_dim = head_dim, a.f32 = type == RC_F32;
   a.positions = positions, a.count = count, a.inverse = inverse != 0;

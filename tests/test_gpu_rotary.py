@@ -149,6 +149,23 @@ def test_bad_counts_are_reported(lib, count):
     assert bool((y == 7).all())
 
 
+@pytest.mark.parametrize("axes", [1, 2])
+def test_a_callers_own_plan(lib, axes):
+    """What stands behind the plan's axes is of no consequence."""
+    R, ctx = lib
+    pairs = [16, 16][:axes] if axes == 2 else [32]
+    plan, x = R.Rotary(64, pairs=pairs), _rand(9, 64, seed=4)
+    at = torch.randint(0, 5000, (9, axes), dtype=torch.int32,
+                       generator=torch.Generator().manual_seed(2)).cuda()
+    ys = [torch.zeros_like(x) for _ in range(2)]
+    for i in range(2):
+        R.rc_rotary_apply(ctx, plan, x, 64, R.RC_F32, 9, 1, 64, at, None, False, ys[i], 64)
+        for a in range(axes, 3):
+            plan.c.pairs[a] = -20 + a
+    R.rc_sync(ctx)
+    assert torch.equal(ys[0], ys[1])
+
+
 def test_captured(lib):
     R, ctx = lib
     x, y = _rand(500, 16 * 72, seed=1).to(BF), torch.zeros(500, 16 * 72, dtype=BF, device="cuda")
