@@ -209,6 +209,11 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
   // tiles are summed in one word)
   int entries, m_tiles;
   {
+    // (offsets that descend can name rows twice: any sum of tiles fits below)
+    constexpr unsigned long long ONE = 1ull << 48, TILES = ONE - 1;
+    const auto most = [&](unsigned long long v) {
+      return int(min(v & TILES, (unsigned long long)pl.most));
+    };
     int lo[2], hi[2];
     unsigned long long mine = 0;
 #pragma unroll
@@ -222,7 +227,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
           lo[j] = hi[j] = 0;
         }
       }
-      if (hi[j] > lo[j]) mine += (1ull << 32) + unsigned((hi[j] - lo[j] - 1) / TM + 1);
+      if (hi[j] > lo[j]) mine += ONE + unsigned((hi[j] - lo[j] - 1) / TM + 1);
     }
     unsigned long long sum = mine;
 #pragma unroll
@@ -241,14 +246,13 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (hi[j] > lo[j]) {
-        const int i = int(before >> 32);
-        tab.first[i] = int(before & 0xffffffffu);
+        const int i = int(before >> 48);
+        tab.first[i] = most(before);
         tab.row[i] = lo[j], tab.end[i] = hi[j];
         tab.expert[i] = uint16_t(2 * threadIdx.x + j);
-        before += (1ull << 32) + unsigned((hi[j] - lo[j] - 1) / TM + 1);
+        before += ONE + unsigned((hi[j] - lo[j] - 1) / TM + 1);
       }
-    // (offsets that descend can name rows twice)
-    entries = int(all >> 32), m_tiles = int(min(all & 0xffffffffull, (unsigned long long)pl.most));
+    entries = int(all >> 48), m_tiles = most(all);
   }
   // this CTA's (or pair's) tiles pos, pos + G ..: expert, first place, places left there
   // and number among the columns.  The first LIST of them are found here, once for all

@@ -686,12 +686,6 @@ sort_kernel(const __grid_constant__ SortArgs a) {
   if (ctas > 1) tc::cluster_sync();  // (no CTA leaves while another may read its sums)
 }
 
-}  // namespace
-
-cudaError_t launch_experts_route(const RoutingArgs& a, cudaStream_t st) {
-  return a.f32 ? route<float>(a, st) : route<bf16>(a, st);
-}
-
 // Whether the device places a cluster of sixteen CTAs (more than any device has to).
 bool sixteen_fit(size_t smem) {
   static PerDevice<1> known;
@@ -714,6 +708,12 @@ bool sixteen_fit(size_t smem) {
     }
     return clusters > 0 ? 1 : 0;
   }) > 0;
+}
+
+}  // namespace
+
+cudaError_t launch_experts_route(const RoutingArgs& a, cudaStream_t st) {
+  return a.f32 ? route<float>(a, st) : route<bf16>(a, st);
 }
 
 cudaError_t launch_experts_sort(const SortArgs& a, cudaStream_t st) {

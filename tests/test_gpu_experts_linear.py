@@ -276,6 +276,60 @@ def test_what_is_not_finite_stays_in_its_row(lib):
     assert bool((m.scales[:, rest] != 255).all())
 
 
+@pytest.mark.parametrize("pairs", [5, 300])
+@pytest.mark.parametrize("act", ACTS)
+def test_sums_of_any_size(lib, pairs, act):
+    """Activations far out, where they end, and beside columns that are not finite."""
+    R, ctx = lib
+    v = torch.tensor([math.nan, 1.0, -1.0, 0.5, math.inf, -2.0, 3.0, -math.inf, -1e30, 1e30, -1e4,
+                      1e4, -100.0, -22.0, -21.0, -6.0, -5.5, -5.0, -0.0, 20.0, 0.0, 1e-20, -1e-20,
+                      6.0, math.nan, math.nan, math.inf, 2.0, -math.inf, 4.0, -1e38, -3.0])
+    v = torch.cat([v, v.flip(0), v[:5]])
+    n = len(v)
+    gated = act == "gated_silu"
+    b = torch.cat([v, torch.linspace(0.5, 2.0, n)]) if gated else v
+    x, W = R.Fp8Matrix(pairs, 128, 1), R.Fp8Matrix(256, 128, 128)
+    R.rc_fp8_quantize(ctx, _rand(pairs, 128, seed=1), 128, R.RC_F32, x)
+    R.rc_fp8_quantize(ctx, torch.zeros(256, 128, device="cuda"), 128, R.RC_F32, W)
+    y = torch.zeros(pairs, n, device="cuda")
+    R.rc_experts_linear(ctx, x, W, b.cuda()[None].contiguous(), 1, n,
+                        torch.tensor([0, pairs], dtype=torch.int32, device="cuda"), None, pairs,
+                        ACTS.index(act), y, n, R.RC_F32)
+    R.rc_sync(ctx)
+    u = v.double()
+    want = u if act == "none" else _gelu(u) if act == "gelu" else u * torch.sigmoid(u)
+    want = want * b[n:].double() if gated else want
+    got = y.cpu().double()
+    plain = want.isfinite()
+    assert torch.equal(got.isnan(), want.isnan().expand_as(got))
+    assert bool((got[:, want == math.inf] == math.inf).all())
+    assert bool((got[:, want == -math.inf] == -math.inf).all())
+    # the powers as in the sums' tolerance; 2^-25 for the 2^-31 that quotients are cut by, times
+    # sums of 22 where they are not 0 and a factor of 2
+    off = (got - want)[:, plain].abs()
+    assert bool((off <= 2.0 ** -16 * want[plain].abs() + 2.0 ** -25).all())
+
+
+def test_offsets_that_name_many_rows_again_and_again(lib):
+    """2^32 tiles and more, were they counted as they stand: reported, and nothing else touched."""
+    R, ctx = lib
+    pairs, experts, guard = R.RC_EXPERTS_MAX_PAIRS, 1024, 4096
+    x, W = R.Fp8Matrix(4, 16, 1), R.Fp8Matrix(experts * 128, 16, 128)
+    R.rc_fp8_quantize(ctx, _rand(4, 16, seed=1), 16, R.RC_F32, x)
+    R.rc_fp8_quantize(ctx, _rand(experts * 128, 16, seed=2), 16, R.RC_F32, W)
+    off = torch.tensor([0, pairs] * (experts // 2) + [0], dtype=torch.int32, device="cuda")
+    buf = torch.full((pairs + 2 * guard,), 7.0, dtype=BF, device="cuda")
+    y = buf[guard:guard + pairs].view(pairs, 1)
+    source = torch.zeros(pairs, dtype=torch.int32, device="cuda")
+    R.rc_experts_linear(ctx, x, W, None, experts, 1, off, source, pairs, R.RC_ACT_NONE, y, 1,
+                        R.RC_BF16)
+    with pytest.raises(R.RCError) as e:
+        R.rc_sync(ctx)
+    assert e.value.status == 6
+    R.rc_sync(ctx)
+    assert bool((buf[:guard] == 7).all()) and bool((buf[guard + pairs:] == 7).all())
+
+
 def test_captured_with_other_offsets(lib):
     """A graph follows the rows that its experts get later; two streams at once."""
     R, ctx = lib
