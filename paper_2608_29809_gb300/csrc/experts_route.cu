@@ -130,11 +130,10 @@ __device__ __forceinline__ int choose_f64(const float (&z)[PER], const RoutingAr
                                        float m, uint64_t* scratch) {
   double s[PER], sum = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    s[i] = 0;
-    if (z[i] == -INFINITY) continue;
-    s[i] = a.score == RC_SCORE_SOFTMAX ? exp(double(z[i]) - double(m))
-                                       : 1 / (1 + exp(-double(z[i])));
+  for (int i = 0; i < PER; ++i) {  // (no branches: the exponentials run side by side)
+    const bool softmax = a.score == RC_SCORE_SOFTMAX;
+    const double p = exp(softmax ? double(z[i]) - double(fmaxf(m, -FLT_MAX)) : -double(z[i]));
+    s[i] = softmax ? p : 1 / (1 + p);  // (0 for -inf)
     sum += s[i];
   }
 #pragma unroll
@@ -322,6 +321,41 @@ __device__ __forceinline__ int in_order(const RoutingArgs& a, bool f32, long lon
   return out;
 }
 
+// Whether the lane's group (of `lanes` lanes) is among the best by sigmoid scores with bias
+// as of f64.  c: the scores in f32, two: the second best of the group, of which what may be
+// among the best two in f64 is no farther than both scores may be off.
+template <int PER>
+__device__ __forceinline__ bool keep_group_f64(const RoutingArgs& a, bool f32, long long row,
+                                               int lane, int lanes, int group,
+                                               const float (&c)[PER], float two32) {
+  const float least = two32 - (0x1p-19f + 0x1p-21f * fabsf(two32));
+  uint32_t left = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) left |= uint32_t(c[i] > -INFINITY && !(c[i] < least)) << i;
+  double one = -INFINITY, two = -INFINITY;
+  while (__any_sync(~0u, left)) {
+    if (!left) continue;
+    const int e = lane * PER + __ffs(int(left)) - 1;
+    left &= left - 1;
+    const double z = logit(a.logits, f32, row * a.ld + e);
+    const double v = 1 / (1 + exp(-z)) + (a.bias ? double(fminf(a.bias[e], FLT_MAX)) : 0);
+    two = fmax(two, fmin(one, v));
+    one = fmax(one, v);
+  }
+  for (int o = 1; o < lanes; o <<= 1) {
+    const double k = __shfl_xor_sync(~0u, one, o), l = __shfl_xor_sync(~0u, two, o);
+    two = fmax(fmin(one, k), fmax(two, l));
+    one = fmax(one, k);
+  }
+  const double mine = a.group_best == 2 && two > -INFINITY ? one + two : one;
+  int rank = 0;
+  for (int h = 0; h < a.groups; ++h) {
+    const double v = __shfl_sync(~0u, mine, h * lanes);
+    rank += v > mine || (v == mine && h < group);
+  }
+  return group < a.groups && mine > -INFINITY && rank < a.top_groups;
+}
+
 // Any routing, a row for each warp.
 template <class T, int PER>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS)
@@ -344,10 +378,12 @@ route_any_kernel(const __grid_constant__ RoutingArgs a) {
 // for the rows whose choice can be told from shortened keys: the value's upper bits,
 // and below them the expert's number, lower numbers larger.  Keys are sorted in their
 // lanes once, and a choice is then the largest head.  Neighbours closer than what a
-// shortened key may be off are put in order by f64 (a softmax's with a bias, and groups
-// that close, by route_row).  A warp keeps the bias and takes
-// several rows, the next one's logits under way.  (All rows as route_row does them:
-// 16384 rows of 256, sigmoid, groups, 8 each, 48 us, 1700 instructions a row.)
+// shortened key may be off are put in order by f64, and so are a sigmoid's groups; a
+// softmax's that are that close, and rows where more values than MORE behind the last
+// choice are, are left to route_row when the others are done (f64 of all experts: 12 us
+// for one row).  A warp keeps the bias and takes several rows, the next one's logits
+// under way.  (All rows as route_row does them: 16384 rows of 256, sigmoid, groups, 8
+// each, 48 us, 1700 instructions a row; now 21.7, 970.)
 template <int PER>
 constexpr int ROUTE_CTAS = PER <= 4 ? 8 : PER == 8 ? 6 : PER == 16 ? 4 : 2;  // of an SM
 template <class T, int PER>
@@ -432,6 +468,7 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
       m = warp_maxf(m);
     }
     float c[PER];  // what experts are chosen by
+    float most = 1.f;  // of a score
     if (by_logits) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) c[i] = z[i] + 0.f;  // (-0 as 0)
@@ -441,6 +478,7 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) sum += c[i] = score_of(true, z[i], m);
       const float r = 1.f / warp_sum(sum);
+      most = fminf(most, r);
 #pragma unroll
       for (int i = 0; i < PER; ++i) c[i] = z[i] == -INFINITY ? -INFINITY : fmaf(c[i], r, b[i]);
     } else {
@@ -467,16 +505,20 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
         const float v = __shfl_sync(~0u, mine, h * lanes);
         rank += v > mine || (v == mine && h < group);
       }
-      const bool kept = group < a.groups && mine > -INFINITY && rank < a.top_groups;
+      bool kept = group < a.groups && mine > -INFINITY && rank < a.top_groups;
       if (!by_logits) {
         const uint32_t k = group < a.groups ? key_of(mine) : 0u;
-        const float most = of_key(max(warp_max(kept ? 0u : k), key_of(-FLT_MAX)));
+        const float other = of_key(max(warp_max(kept ? 0u : k), key_of(-FLT_MAX)));
         const float least = of_key(~warp_max(kept ? ~k : 0u));
         // (sums of two values: at most twice their errors)
         close = __any_sync(~0u, kept) &&
-                !(least - most > 4.f * score_error(a.score, 1.f) +
-                                     0x1p-20f * fmaxf(fabsf(least), fabsf(most)) + 0x1p-20f *
-                                     fmaxf(fabsf(one), fabsf(two > -INFINITY ? two : 0.f)));
+                !(least - other > 4.f * score_error(a.score, most) +
+                                      0x1p-20f * fmaxf(fabsf(least), fabsf(other)) + 0x1p-20f *
+                                      fmaxf(fabsf(one), fabsf(two > -INFINITY ? two : 0.f)));
+        if (!softmax && __any_sync(~0u, close)) {
+          kept = keep_group_f64(a, sizeof(T) == 4, row, lane, lanes, group, c, two);
+          close = false;
+        }
       }
       if (!kept)
 #pragma unroll
@@ -505,7 +547,7 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
       // (of bf16 the lower half of a key is free: equal logits are in order)
       if (by_logits) return next && sizeof(T) == 4 && ((value ^ next) & ~LOW) == 0;
       const float v = of_key(value & ~LOW), w = of_key(next & ~LOW);
-      return next && !(v - w > 2.f * score_error(a.score, 1.f) +
+      return next && !(v - w > 2.f * score_error(a.score, most) +
                                    (LOW + 5) * 0x1p-23f * fmaxf(fabsf(v), fabsf(w)) + 0x1p-100f);
     };
     pick_more(0, a.top_k + 1);
