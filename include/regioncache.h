@@ -736,8 +736,8 @@ rc_status rc_norm_residual(rc_ctx* ctx, const rc_residual* op, rc_stream stream)
  *                       stay, slow ones are stretched;
  *     RC_ROTARY_RAMP    the same with k = 1 - (i - lo) / (hi - lo), cut to 0 .. 1,
  *                       where lo (rounded down, at least 0) and hi (up, at most
- *                       p - 1) are the indexes of pairs that turn fast and slow times, and hi - lo
- *                       counts as 0.001 at least; theta > 1.
+ *                       p - 1) are the indexes of pairs that turn fast and slow
+ *                       times, and hi - lo counts as 0.001 at least; theta > 1.
  *              fast > slow > 0 (in turns over native_length > 0) for the last two.
  *   amplitude  finite.
  * A plan holds a pair's turns a position as a fraction of 2^64: a position
@@ -795,8 +795,8 @@ rc_status rc_rotary_apply(rc_ctx* ctx, const rc_rotary* plan, const void* x, int
  * scores closer than they are exact are computed again.  Without bias, and with
  * groups valued by one expert, it is decided by the logits themselves.
  * An expert whose logit or bias is NaN or -inf (a mask) is never chosen and
- * adds nothing to a softmax; a logit or bias of +inf counts as the largest f32.  Where fewer than
- * top_k are left, the rest of ids is -1 with weight 0.
+ * adds nothing to a softmax; a logit or bias of +inf counts as the largest f32.
+ * Where fewer than top_k are left, the rest of ids is -1 with weight 0.
  *   experts 1 .. RC_EXPERTS_MAX, a multiple of groups; top_k 1 ..
  *   RC_EXPERTS_MAX_TOP_K; groups 1 .. 32, top_groups 1 .. groups, group_best 1
  *   or 2; scale finite.
@@ -853,9 +853,12 @@ rc_status rc_experts_sort(rc_ctx* ctx, const int32_t* ids, int rows, int top_k, 
  *   y8       codes instead: pairs rows at least, n columns, group 1, as
  *            rc_fp8_quantize gives them for the f32 values.
  * Places outside offsets are left as they were.  experts 1 .. RC_EXPERTS_MAX,
- * pairs 0 .. RC_EXPERTS_MAX_PAIRS, (pairs / 128 + experts) * (n / 32 + 1) < 2^31 - 152.
- * Results are bit-identical from call to call.  One expert without source is a plain quantised
- * layer with its activation: offsets {0, rows}.
+ * pairs 0 .. RC_EXPERTS_MAX_PAIRS,
+ * (pairs / 128 + experts) * (n / 32 + 1) < 2^31 - 152.
+ * The work is shared out on the host for even shares of the pairs; uneven ones
+ * cost time, not results.  Activations are good to 2^-16 of themselves and 2^-31
+ * of the sum.  Results are bit-identical from call to call.  One expert without
+ * source is a plain quantised layer with its activation: offsets {0, rows}.
  * Device checks: offsets that descend or leave 0 .. pairs (the expert is left
  * out) and a source outside x (taken as row 0) are reported.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */

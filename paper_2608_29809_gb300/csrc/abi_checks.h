@@ -20,7 +20,9 @@ inline rc_status fail(rc_status s, const char* fmt, ...) {
   return s;
 }
 
-inline bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+inline bool aligned(const void* p, unsigned n) {
+  return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0;
+}
 
 // RC_OK, or the failure of a launch.
 inline rc_status launched(cudaError_t e, const char* what) {

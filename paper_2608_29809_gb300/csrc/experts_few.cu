@@ -2,7 +2,8 @@
 // experts have a few rows each and there are few of them: latency is all that counts,
 // to which the tensor core of experts_linear.cu, fed by way of shared and tensor
 // memory, adds (a block of one token: 9.5 and 10.5 us for its two products of 5 MB
-// each).
+// each; here 8.1 and 6.5, most of them a chain of round trips: offsets, source, x and
+// scales, blocks of W, the join).
 //
 // A CTA's warps take up to ROWS rows of an expert and CW tiles of 16 of its outputs, the
 // columns in runs for the rest of its warps.  A warp copies its tile's codes, 16 bytes a
@@ -230,7 +231,8 @@ experts_few_kernel(const __grid_constant__ ExpertsArgs a, const __grid_constant_
       if (o >= out_cols || c >= a.n) continue;
       float s[2] = {0.f, 0.f};
       for (int part = 0; part < parts; ++part) {
-        for (int k = 0; k < pl.kw; ++k) s[part] += sums[((part * pl.kw + k) * ROWS + row) * out_cols + o];
+        for (int k = 0; k < pl.kw; ++k)
+          s[part] += sums[((part * pl.kw + k) * ROWS + row) * out_cols + o];
         if (a.bias) s[part] += __ldg(a.bias + (long long)expert * N + part * a.n + c);
       }
       v[i] = gated ? act_of(RC_ACT_SILU, s[0]) * s[1] : act_of(a.act, s[0]);
@@ -315,7 +317,7 @@ cudaError_t few(const ExpertsArgs& a, cudaStream_t st) {
 bool experts_few(const ExpertsArgs& a) {
   // few rows of each expert that can have one, a CTA or less for each SM, rows of x that
   // shared memory holds (48 rows by 6 of 64 experts, 1152 x 1152, 576 CTAs: 28 us,
-  // where experts_linear.cu takes 20)
+  // where experts_linear.cu takes 18)
   const long long used = a.pairs < a.experts ? a.pairs : a.experts;
   return a.pairs <= 8 * used && chunks_of(a, rows_of(a)) * ((a.n - 1) / 128 + 1) <= SMS &&
          smem_of(a, rows_of(a), warps_of(a)) <= 227 * 1024;

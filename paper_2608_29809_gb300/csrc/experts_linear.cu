@@ -7,22 +7,23 @@
 // rows of x, warp 2 W, warp 1 issues the MMAs, warps 4..7 put the scale bytes into
 // tensor memory, warps 8..23 drain the accumulator.  Rows are gathered by TMA, four an
 // instruction, of which a warp issues one in 60 to 130 cycles: 16384 x 2 rows, 1152 x
-// 4608, took 508 us with one warp, 290 with two; now 214 (neighbouring rows, in one
-// box: 155).  Two things bound the rest more than the tensor core (90 us): the roles'
-// code has to stay in the SM's instruction cache (at 96 KB it did not: 180 us for
-// neighbouring rows), and nothing may be spilled (registers for 28 warps: 72).
+// 4608, GELU, took 508 us with one warp, 290 with two; now 195 (neighbouring rows, in
+// one box, without the activation: 144).  What bounds it more than the tensor core (90
+// us; its pipe is busy 40 % of the time) is the epilogue's instructions (59 % of all issue
+// slots) beside the gathers; the roles' code has to stay in the SM's instruction cache
+// (at 96 KB it did not: 180 us for neighbouring rows), and nothing may be spilled
+// (registers for 28 warps: 72).
 // Each CTA first lists the experts that have rows, with the tiles of BM rows before
 // each; a tile's number names its rows by a search there, and its columns.  Rows of
 // an accumulator do not mix, so what a tile holds beyond its expert's rows (stale
 // shared memory, the next expert's rows) is only never written.
-#include <float.h>
-
 #include "../../include/regioncache.h"
 #include "block.h"
 #include "common.cuh"
 #include "experts_act.cuh"
 #include "fp8.cuh"
-#include "tc_chunks.cuh"
+#include "tc_eight_bit.cuh"
+#include "tma_host.h"
 
 namespace rc {
 
@@ -136,7 +137,8 @@ __device__ __forceinline__ void write_columns(T* y, long long ldy, int rows, int
   __syncwarp();
   const int c = lane & 15;
   if (c < cols)
-    for (int r = lane >> 4; r < min(32, rows); r += 2) y[r * ldy + c] = T(s[r * 16 + (c ^ (r & 15))]);
+    for (int r = lane >> 4; r < min(32, rows); r += 2)
+      y[r * ldy + c] = T(s[r * 16 + (c ^ (r & 15))]);
   __syncwarp();
 }
 
@@ -668,7 +670,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
               tmem_st16(at + uint32_t(h), reinterpret_cast<const uint32_t*>(v));
             }
             tmem_wait_st();
-            uint32_t* to = reinterpret_cast<uint32_t*>(stg) + turn * EPI_WARPS * 32 + sp * 32 + lane;
+            uint32_t* to =
+                reinterpret_cast<uint32_t*>(stg) + turn * EPI_WARPS * 32 + sp * 32 + lane;
             to[part * 128] = top;
             rows_sync(sp);
 #pragma unroll
@@ -762,8 +765,12 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
           if (c >= a.n) continue;
           const float* b = a.bias ? a.bias + (long long)tl.expert * N + c : nullptr;
           v[i] = sum(col, row) + (b ? __ldg(b) : 0.f);
-          v[i] = gated ? act_of(RC_ACT_SILU, v[i]) * (sum(half_bn + col, row) + (b ? __ldg(b + a.n) : 0.f))
-                       : act_of(a.act, v[i]);
+          if (gated) {
+            const float w = sum(half_bn + col, row) + (b ? __ldg(b + a.n) : 0.f);
+            v[i] = act_of(RC_ACT_SILU, v[i]) * w;
+          } else {
+            v[i] = act_of(a.act, v[i]);
+          }
         }
         if constexpr (OUT == OUT_CODES) {
           uint32_t top = 0;

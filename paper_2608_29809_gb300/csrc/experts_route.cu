@@ -400,7 +400,8 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
   const int size = a.experts / a.groups, lanes = size / PER, group = grouped ? lane / lanes : 0;
   pdl_wait();
   pdl_trigger();
-  const int rows = live_count(a.count, a.rows, blockIdx.x == 0 && threadIdx.x == 0 ? a.err : nullptr);
+  const int rows =
+      live_count(a.count, a.rows, blockIdx.x == 0 && threadIdx.x == 0 ? a.err : nullptr);
   float b[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -429,7 +430,8 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        raw[i] = e0 + i < a.experts ? reinterpret_cast<const uint32_t*>(p)[i] : 0xff800000u;  // -inf
+        raw[i] = e0 + i < a.experts ? reinterpret_cast<const uint32_t*>(p)[i]
+                                    : 0xff800000u;  // -inf
     } else {
 #pragma unroll
       for (int k = 0; k < WORDS; ++k) raw[k] = 0xff80ff80u;

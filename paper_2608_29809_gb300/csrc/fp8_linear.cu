@@ -20,7 +20,8 @@
 #include "common.cuh"
 #include "eight_bit.h"
 #include "fp8.cuh"
-#include "tc_chunks.cuh"
+#include "tc_eight_bit.cuh"
+#include "tma_host.h"
 
 namespace rc {
 
@@ -33,7 +34,7 @@ constexpr int THREADS = 512;
 constexpr int SCALE_WARP = 4, EPI_WARP = 8, EPI_WARPS = 8;
 constexpr int STAGE_A = BM * BK;
 constexpr int RING_BYTES = 187 * 1024, MAX_STAGES = 7;
-constexpr int STAGING_WARP = CHUNK_STAGING;  // per epilogue warp
+constexpr int STAGING_WARP = 32 * 128;  // 32 rows of 32 columns per epilogue warp
 // tensor memory: accumulators at 0 and PAIR_BN, then a ring of scale words: a
 // batch holds, for each WORD_KB blocks, 4 columns for x and 8 for W
 constexpr int PAIR_BN = 192, MAX_BN = 256, SCALE_COL = 2 * PAIR_BN, TMEM_COLS = 512;
@@ -63,6 +64,54 @@ struct Out {
   bool tma;  // y's rows are 16-byte aligned: chunks leave by TMA
   unsigned* err;
 };
+
+// One warp's 32 x 32 chunk of the accumulator (lane = row r0 + lane, v = its
+// columns c0 .., `bias` that of column c0 + lane), by way of the warp's own
+// shared memory.
+// TMA: in the layout of a box of 32 columns with a swizzle as wide as its rows
+// (which also keeps the row-per-lane writes free of bank conflicts); what lies
+// outside y is not written.
+template <class T>
+__device__ __forceinline__ void store_chunk(const CUtensorMap* map, uint8_t* stg, int lane,
+                                            const float* v, int r0, int c0) {
+  const uint32_t s0 = saddr(stg);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       s0 + lane * 128 + 16 * (j ^ (lane & 7))),
+                   "f"(v[4 * j]), "f"(v[4 * j + 1]), "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       s0 + lane * 64 + 16 * (j ^ ((lane >> 1) & 3))),
+                   "r"(pack_bf16x2(v[8 * j], v[8 * j + 1])),
+                   "r"(pack_bf16x2(v[8 * j + 2], v[8 * j + 3])),
+                   "r"(pack_bf16x2(v[8 * j + 4], v[8 * j + 5])),
+                   "r"(pack_bf16x2(v[8 * j + 6], v[8 * j + 7]))
+                   : "memory");
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) tma_store_2d(map, s0, c0, r0);
+}
+// Any alignment: neighbouring lanes write neighbouring columns.
+template <class T>
+__device__ __forceinline__ void write_chunk(const Out<T>& o, uint8_t* stg, int lane,
+                                            const float* v, int r0, int c0) {
+  float* s = reinterpret_cast<float*>(stg);
+#pragma unroll
+  for (int j = 0; j < 32; ++j) s[lane * 32 + (j ^ lane)] = v[j];
+  __syncwarp();
+  const int rows = min(32, o.rows - r0);
+  if (lane < o.n - c0) {
+    T* y = o.y + (long long)r0 * o.ldy + c0 + lane;
+    for (int row = 0; row < rows; ++row, y += o.ldy) *y = T(s[row * 32 + (lane ^ row)]);
+  }
+  __syncwarp();  // the staging area is rewritten by the next chunk
+}
 
 // Named barrier of the four scale warps.
 __device__ __forceinline__ void scale_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
@@ -355,8 +404,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
           store_chunk<T>(&tmY, own + buf * (STAGING_WARP / 2), lane, v, r0, c0);
           if (BUFS == 2) buf ^= 1;
         } else {
-          write_chunk(out.y + (long long)r0 * out.ldy + c0, out.ldy, out.rows - r0, out.n - c0, own,
-                      lane, v);
+          write_chunk(out, own, lane, v, r0, c0);
         }
       }
       tc_fence_before();
@@ -397,8 +445,7 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
           __syncwarp();
           store_chunk<T>(&tmY, own, lane, v, r0, c0);
         } else {
-          write_chunk(out.y + (long long)r0 * out.ldy + c0, out.ldy, out.rows - r0, out.n - c0, own,
-                      lane, v);
+          write_chunk(out, own, lane, v, r0, c0);
         }
       }
       if (lane == 0) tma_store_wait_read<0>();
@@ -421,6 +468,23 @@ fp8_linear_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant
 }
 
 constexpr int SMS = 152;
+
+// y [rows][n] in boxes of 32 x 32 whose rows are swizzled over their own width.
+template <class T>
+cudaError_t tma_map_chunks(T* y, int rows, int n, int ld, CUtensorMap* out) {
+  auto fn = tma_encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  constexpr bool F32 = sizeof(T) == 4;
+  const cuuint64_t dims[2] = {cuuint64_t(n), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {cuuint64_t(ld) * sizeof(T)};
+  const cuuint32_t box[2] = {32, 32}, es[2] = {1, 1};
+  const CUresult r =
+      fn(out, F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, y, dims,
+         strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+         F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+         CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
 
 template <class T, Mode MODE>
 cudaError_t go(const Fp8Mat& x, const Fp8Mat& w, const Out<T>& o, int bn, int parts,

@@ -62,6 +62,10 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
                : "memory");
 }
 
+// The instruction descriptor of kind::mxf8f6f4 without its sizes: e4m3 x e4m3
+// into f32, both K-major, power-of-two scale bytes; N >> 3 at bit 17, M >> 7 at
+// bit 27, the byte of each scale word that the MMA takes at bits 4 (W) and 29 (x).
+constexpr uint32_t IDESC_E4M3 = 1u << 23;
 // D (+)= A B of e4m3 tiles (K-major, 32 columns), each row's products times
 // 2^(scale byte - 127) of A's and of B's row: scale words in tensor memory,
 // row i in lane i % 32 (of every 32-lane partition), column i / 32; the

@@ -58,8 +58,9 @@ def close(got, want, tol, dtype, what=""):
     got = got.cpu().double()
     limit = tol + rounding(dtype) * (want.abs() + tol) + 1e-37
     bad = ~((got - want).abs() <= limit)
+    most = float(((got - want).abs() / limit).max()) if got.numel() else 0.0
     assert not bool(bad.any()), \
-        f"{what}: {int(bad.sum())} of {bad.numel()} off, at most {float(((got - want).abs() / limit).max()):.2f} of the limit"
+        f"{what}: {int(bad.sum())} of {bad.numel()} off, at most {most:.2f} of the limit"
 
 
 def frequencies(pairs, theta, scaling="plain", factor=1.0, native=0.0, fast=0.0, slow=0.0):

@@ -3,6 +3,8 @@ key and value products, rotary positions, the eight-bit cache and its attention,
 product, the norm between, routing, experts and their sum; eagerly, captured and replayed with
 another step's values, and on two streams at once."""
 import math
+import os
+import re
 
 import pytest
 import torch
@@ -263,3 +265,46 @@ def test_two_streams_at_once(lib):
     other.feed(40, *FILL)
     other.step()
     _same(blocks[1].results()[:9], other.results()[:9])
+
+
+def test_the_readmes_block_of_experts_runs(lib):
+    R, ctx = lib
+    readme = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")
+    code = re.findall(r"```python\n(.*?)```", open(readme).read(), re.S)[1]
+    rows = 7
+
+    def weight(n, cols, seed):
+        m = R.Fp8Matrix(n, cols, 128)
+        R.rc_fp8_quantize(ctx, _rand(n, cols, seed=seed, scale=1 / math.sqrt(cols)), cols, R.RC_F32,
+                          m)
+        return m
+
+    def ints(*shape):
+        return torch.zeros(shape, dtype=torch.int32, device="cuda")
+
+    x = _rand(rows, 1152, seed=1)
+    x0 = x.cpu().double()
+    names = dict(R=R, ctx=ctx, rows=rows, x=x, norm_weight=1 + _rand(1152, seed=2, scale=0.1),
+                 w_router=weight(16, 1152, 3), w_up=weight(16 * 4608, 1152, 4),
+                 w_down=weight(16 * 1152, 2304, 5), logits=torch.zeros(rows, 16, device="cuda"),
+                 ids=ints(rows, 2), weights=torch.zeros(rows, 2, device="cuda"), first=ints(17),
+                 source=ints(2 * rows), places=ints(rows, 2),
+                 d=torch.zeros(2 * rows, 1152, dtype=BF, device="cuda"))
+    exec(code, names)
+    R.rc_sync(ctx)
+    ids, weights = B.route(names["logits"], "softmax", 2)
+    assert torch.equal(names["ids"].cpu(), ids)
+    first, source, places = B.sort(ids, 16)
+    assert torch.equal(names["first"].cpu(), first) and torch.equal(names["places"].cpu(), places)
+    u8, w = names["u8"], names["w_down"]
+    uv = E.values(u8.codes, u8.scales, 1, 2304)
+    wv = E.values(w.codes, w.scales, 128, 2304).view(16, 1152, 2304)
+    of = torch.repeat_interleave(torch.arange(16), (first[1:] - first[:-1]).long())
+    d = torch.stack([wv[e] @ v for e, v in zip(of, uv)])
+    mag = torch.stack([wv[e].abs() @ v.abs() for e, v in zip(of, uv)])
+    B.close(names["d"], d, 2304 * 2.0 ** -23 * mag, BF, "down")
+    part = names["d"].cpu().double()[places.long()] * names["weights"].cpu().double()[:, :, None]
+    none = ("none", 0, None, None)
+    want, tol, _, _ = B.residual(x0, part.sum(1), 2 * B.F32_HALF * part.abs().sum(1), None, 1.0,
+                                 none, none, None, None)
+    B.close(x, want, tol, F32, "joined")

@@ -73,7 +73,8 @@ class Problem:
         self.offsets = torch.cat([torch.zeros(1).long(), shares.cumsum(0)]).int()
         self.source = torch.randint(0, rows, (self.pairs,), generator=g).int() if gather else None
         xv = E.values(self.x.codes, self.x.scales, 1, cols)
-        wv = E.values(self.W.codes, self.W.scales, 128, cols).view(self.experts, per, cols)[:, :wide]
+        wv = E.values(self.W.codes, self.W.scales, 128, cols)
+        wv = wv.view(self.experts, per, cols)[:, :wide]
         xv = xv[self.source.long()] if gather else xv
         y, mag = torch.zeros(self.pairs, wide).double(), torch.zeros(self.pairs, wide).double()
         for e in range(self.experts):

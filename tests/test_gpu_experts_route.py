@@ -77,7 +77,8 @@ def test_sizes(lib, rows, e, k, score, dtype, bias):
 
 
 @pytest.mark.parametrize("e,groups,top,k", [
-    (256, 8, 4, 8), (64, 4, 1, 5), (60, 4, 2, 10), (60, 20, 7, 9), (1024, 32, 3, 16), (32, 32, 5, 5),
+    (256, 8, 4, 8), (64, 4, 1, 5), (60, 4, 2, 10), (60, 20, 7, 9), (1024, 32, 3, 16),
+    (32, 32, 5, 5),
     (160, 2, 1, 6), (96, 3, 2, 8), (6, 2, 1, 3), (512, 1, 1, 10), (62, 31, 30, 4), (8, 4, 4, 8)])
 @pytest.mark.parametrize("of_best", [1, 2])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])

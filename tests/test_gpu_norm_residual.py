@@ -253,7 +253,8 @@ def test_constant_and_zero_rows(lib):
     R, ctx = lib
     x = torch.full((2, 1000), 3.0, device="cuda")
     b, y = _rand(1000, seed=2), torch.zeros(2, 1000, device="cuda")
-    R.rc_norm_residual(ctx, R.ResidualNorm(1000, x=x, y=y, pre=R.Norm(R.RC_NORM_LAYER, 1e-5, None, b)))
+    R.rc_norm_residual(ctx, R.ResidualNorm(1000, x=x, y=y,
+                                           pre=R.Norm(R.RC_NORM_LAYER, 1e-5, None, b)))
     R.rc_sync(ctx)
     assert torch.equal(y, b.expand(2, -1))
     x.zero_()
