@@ -7,12 +7,12 @@
 // rows of x, warp 2 W, warp 1 issues the MMAs, warps 4..7 put the scale bytes into
 // tensor memory, warps 8..23 drain the accumulator.  Rows are gathered by TMA, four an
 // instruction, of which a warp issues one in 60 to 130 cycles: 16384 x 2 rows, 1152 x
-// 4608, GELU, took 508 us with one warp, 290 with two; now 195 (neighbouring rows, in
+// 4608, GELU, took 508 us with one warp, 290 with two; now 186 (neighbouring rows, in
 // one box, without the activation: 144).  What bounds it more than the tensor core (90
-// us; its pipe is busy 40 % of the time) is the epilogue's instructions (59 % of all issue
-// slots) beside the gathers; the roles' code has to stay in the SM's instruction cache
-// (at 96 KB it did not: 180 us for neighbouring rows), and nothing may be spilled
-// (registers for 28 warps: 72).
+// us; its pipe is busy 40 % of the time) are the gathers, 110 cycles each where the epilogue
+// takes the issue slots (59 % of all) beside them, 60 alone; the roles' code has to stay in
+// the SM's instruction cache (at 96 KB it did not: 180 us for neighbouring rows), and
+// nothing may be spilled (registers for 28 warps: 72).
 // Each CTA first lists the experts that have rows, with the tiles of BM rows before
 // each; a tile's number names its rows by a search there, and its columns.  Rows of
 // an accumulator do not mix, so what a tile holds beyond its expert's rows (stale
@@ -303,10 +303,10 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 
   // rows of a CTA of this tile (the second of a pair may have none)
   const auto rows_of = [&](const Tile& t, int r) { return max(0, min(BM, t.left - r * BM)); };
-  // the row of x of a place (row 0 for one outside, which is reported)
-  const auto row_of = [&](int place) {
-    if (!a.source) return place;
-    const int r = a.source[place];
+  // the row of x of a place as it stands in `source`, and then (row 0 for one outside,
+  // which is reported)
+  const auto source_of = [&](int place) { return a.source ? a.source[place] : place; };
+  const auto row_of = [&](int r) {
     if (r >= 0 && r < a.x.rows) return r;
     atomicOr(a.err, DEVERR_INDEX);
     return 0;
@@ -321,7 +321,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       // group's, so that it waits for its own last use), a block's fours of rows dealt
       // to a group's warps; one thread of each issues them (a lane's own operands
       // would be brought to uniform registers lane by lane).  Lane i < MOST looks up
-      // the warp's i-th four, a tile ahead.
+      // the warp's i-th four, a tile ahead (and at their bounds only when they are
+      // needed: the wait for them took a quarter of the warp's time).
       const int w = warp == 0 ? 0 : warp == 3 ? 1 : warp - MORE_X_WARP + 2;
       const int groups = pl.groups, of = X_WARPS / groups, group = w / of, wi = w - group * of;
       int4* own = fours + w * MOST_FOURS;
@@ -336,7 +337,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           r[j] = lane < MOST_FOURS && at + j < rows
-                     ? row_of(tl.place + int(rank) * BM + at + j) : 0;
+                     ? source_of(tl.place + int(rank) * BM + at + j) : 0;
       };
       if (tile < own_tiles) look_up();
       while (ok && tile < own_tiles) {
@@ -345,12 +346,12 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         const auto bytes = [&](int n) { return in_box(n) ? STAGE_A : (n + 3) / 4 * 4 * BK; };
         int expect = bytes(rows_of(tl, 0));
         if (PAIR) expect += bytes(rows_of(tl, 1)) + BN * BK;
-        if (lane < MOST_FOURS) own[lane] = make_int4(r[0], r[1], r[2], r[3]);
+        if (lane < MOST_FOURS)
+          own[lane] = make_int4(row_of(r[0]), row_of(r[1]), row_of(r[2]), row_of(r[3]));
         __syncwarp();
         ++tile;
         if (tile < own_tiles) look_up();
-        // (fours of this warp, of those that hold rows)
-        const int count = box ? 0 : max(0, ((rows + 3) / 4 - wi + of - 1) / of);
+        const int fours_here = box ? 0 : (rows + 3) / 4;  // (of which this warp has every of-th)
 #pragma unroll 1
         for (; next < KB; next += groups) {
           ok = mbar_sleep_warp(empty0 + 8 * stage, phase ^ 1, abort_flag);
@@ -362,9 +363,11 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
             // (a barrier may see bytes before it is told of them: its phase still
             // needs that arrival)
             if (rank == 0 && wi == 0) mbar_expect_tx(fb, uint32_t(expect));
-#pragma unroll 4
-            for (int i = 0; i < count; ++i)
-              tma_gather4<PAIR>(st + (wi + of * i) * 4 * BK, &tmG, bar, c, own[i]);
+            const int4* rows4 = own;
+            uint32_t to = st + wi * 4 * BK;
+#pragma unroll 8
+            for (int i = wi; i < fours_here; i += of, to += of * 4 * BK)
+              tma_gather4<PAIR>(to, &tmG, bar, c, *rows4++);
             if (box && wi == 0) {
               if (PAIR) tma_load_2d_pair(st, &tmX, bar, c, place);
               else tma_load_2d(st, &tmX, bar, c, place);
@@ -484,7 +487,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
       if (kb == 0) {
         tl = tile_of(tile);
         in = tid < rows_of(tl, int(rank));
-        xrow = in ? row_of(tl.place + int(rank) * BM + tid) : 0;
+        xrow = in ? row_of(source_of(tl.place + int(rank) * BM + tid)) : 0;
       }
       const uint8_t* p = a.x.scales + xrow;
       if (in) {
