@@ -114,6 +114,16 @@ __device__ __forceinline__ void put_pieces(uint8_t* stg, int lane, int k0, const
                  "r"(q[4 * k]), "r"(q[4 * k + 1]), "r"(q[4 * k + 2]), "r"(q[4 * k + 3])
                  : "memory");
 }
+// The lane's four, read back.
+__device__ __forceinline__ void get_pieces(const uint8_t* stg, int lane, float* q) {
+  const uint32_t s0 = saddr(stg) + lane * 64;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(q[4 * k]), "=f"(q[4 * k + 1]), "=f"(q[4 * k + 2]), "=f"(q[4 * k + 3])
+                 : "r"(s0 + 16 * (k ^ ((lane >> 1) & 3)))
+                 : "memory");
+}
 __device__ __forceinline__ void store_box(const CUtensorMap* map, uint8_t* stg, int lane, int r0,
                                           int c0) {
   fence_proxy_async_smem();
@@ -365,7 +375,7 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
             if (rank == 0 && wi == 0) mbar_expect_tx(fb, uint32_t(expect));
             const int4* rows4 = own;
             uint32_t to = st + wi * 4 * BK;
-#pragma unroll 8
+#pragma unroll 4
             for (int i = wi; i < fours_here; i += of, to += of * 4 * BK)
               tma_gather4<PAIR>(to, &tmG, bar, c, *rows4++);
             if (box && wi == 0) {
@@ -611,12 +621,23 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
         __syncwarp();
         if (lane == 0 && ok) mbar_arrive(tempty0 + 8 * acc);
       };
+      // the gated sums of sixteen columns and of their factors
+      const auto gate = [&](const float* bias, float* v, float* w) {
+        add_bias<16>(v, bias);
+        add_bias<16>(w, bias + 32);
+        activate<16, false>(v);
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+          const float2 o = f2_mul(make_float2(v[j], v[j + 1]), make_float2(w[j], w[j + 1]));
+          v[j] = o.x, v[j + 1] = o.y;
+        }
+      };
       // sixteen outputs from column `h` of chunk i on (all 32 rows of the warp)
       const auto outputs = [&](int i, int h, float* v) {
         const uint32_t at = tb + uint32_t((part + 4 * i) * 32 + h);
         const bool last = !in_place && h == 16 && i == chunks - 1;
         tmem_ld16(at, v);
-        if (gated) {
+        if (OUT != OUT_CODES && gated) {
           add_bias<16>(v, own_bias + h);
           activate<16, false>(v);
 #pragma unroll
@@ -661,20 +682,51 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
                                          : tmem + uint32_t(MAX_BN + part * 32) +
                                                (uint32_t(sp * 32) << 16);
             uint32_t top = 0;
-#pragma unroll 1
-            for (int h = 0; ok && h < 32; h += 16) {
-              float v[16];
-              outputs(i, h, v);
+            const auto largest = [&](int h, float* v) {  // (outputs behind the last are 0)
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
                 if (c0 + h + j >= a.n) v[j] = 0.f;
                 top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
               }
+            };
+            if (gated && ok) {
+              // Half of the sums go beside the accumulator as they are, the others into
+              // registers: it is free again before anything is computed (4128 x 2 rows of
+              // 16 experts, 1152 x 2 x 2304: 62.7 us, with activations first 65.7).
+              float v[16], w[16];
+              const uint32_t from = tb + uint32_t(part * 32);
+              tmem_ld16(from + 16, v);
+              tmem_st16(at, reinterpret_cast<const uint32_t*>(v));
+              tmem_ld16(from + uint32_t(half_bn) + 16, w);
+              tmem_st16(at + 16, reinterpret_cast<const uint32_t*>(w));
+#pragma unroll 1
+              for (int h = 0; h < 32; h += 16) {
+                tmem_ld16(h ? at : from, v);
+                tmem_ld16(h ? at + 16 : from + uint32_t(half_bn), w);
+                if (h == 0) {
+                  release();
+                  tmem_wait_st();
+                }
+                gate(own_bias + h, v, w);
+                largest(h, v);
+                if (h == 0) put_pieces<4>(own, lane, 0, reinterpret_cast<const uint32_t*>(v));
+                else tmem_st16(at + 16, reinterpret_cast<const uint32_t*>(v));
+              }
+            }
+#pragma unroll 1
+            for (int h = 0; !gated && ok && h < 32; h += 16) {
+              float v[16];
+              outputs(i, h, v);
+              largest(h, v);
               tmem_st16(at + uint32_t(h), reinterpret_cast<const uint32_t*>(v));
             }
             tmem_wait_st();
+            // (behind the ring's stages, which with codes' tiles, of 128 columns or 256, take
+            // 144 KB at most)
+            static_assert(RING_BYTES - 144 * 1024 >= 2 * EPI_WARPS * 32 * 4, "the largest");
             uint32_t* to =
-                reinterpret_cast<uint32_t*>(stg) + turn * EPI_WARPS * 32 + sp * 32 + lane;
+                reinterpret_cast<uint32_t*>(smem + STAGES * STAGE) + turn * EPI_WARPS * 32 +
+                sp * 32 + lane;
             to[part * 128] = top;
             rows_sync(sp);
 #pragma unroll
@@ -689,7 +741,8 @@ experts_linear_kernel(const __grid_constant__ CUtensorMap tmX,
 #pragma unroll 1
             for (int h = 0; h < 32; h += 16, dst += 16) {
               float v[16];
-              tmem_ld16(at + uint32_t(h), v);
+              if (gated && h == 0) get_pieces(own, lane, v);
+              else tmem_ld16(at + uint32_t(h), v);
               if (in_place && h == 16 && i == chunks - 1) release();
               uint32_t q[4];
 #pragma unroll
