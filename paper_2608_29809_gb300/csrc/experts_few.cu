@@ -262,6 +262,7 @@ experts_few_kernel(const __grid_constant__ ExpertsArgs a, const __grid_constant_
 }
 
 constexpr int SMS = 152;
+constexpr size_t MOST_SMEM = 227 * 1024;
 
 size_t smem_of(const ExpertsArgs& a, int rows, int warps) {
   const size_t kb = size_t(a.x.cols - 1) / 128 + 1, parts = a.act == RC_ACT_GATED_SILU ? 2 : 1;
@@ -290,9 +291,10 @@ cudaError_t go(const ExpertsArgs& a, cudaStream_t st) {
   pl.kw = WARPS / pl.cw;
   pl.nt = (a.n - 1) / (16 * pl.cw) + 1;
   const size_t smem = smem_of(a, ROWS, WARPS);
-  // (an attribute of the current device, so set for each call)
+  // (an attribute of the current device, so set for each call; always to the same, for
+  // calls of several threads)
   RC_TRY(cudaFuncSetAttribute(experts_few_kernel<OUT, NT, WARPS>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(MOST_SMEM)));
   count_launches(1);
   return launch_k(experts_few_kernel<OUT, NT, WARPS>, dim3(unsigned(chunks * pl.nt)),
                   dim3(32 * WARPS), smem, st, a, pl);
@@ -320,7 +322,7 @@ bool experts_few(const ExpertsArgs& a) {
   // where experts_linear.cu takes 18)
   const long long used = a.pairs < a.experts ? a.pairs : a.experts;
   return a.pairs <= 8 * used && chunks_of(a, rows_of(a)) * ((a.n - 1) / 128 + 1) <= SMS &&
-         smem_of(a, rows_of(a), warps_of(a)) <= 227 * 1024;
+         smem_of(a, rows_of(a), warps_of(a)) <= MOST_SMEM;
 }
 
 cudaError_t launch_experts_few(const ExpertsArgs& a, cudaStream_t st) {

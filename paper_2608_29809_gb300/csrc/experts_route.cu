@@ -763,13 +763,16 @@ cudaError_t launch_experts_route(const RoutingArgs& a, cudaStream_t st) {
 cudaError_t launch_experts_sort(const SortArgs& a, cudaStream_t st) {
   const size_t smem = size_t(SORT_WARPS + 2) * a.experts * sizeof(int);
   constexpr size_t most = size_t(SORT_WARPS + 2) * RC_EXPERTS_MAX * sizeof(int);
-  // (attributes of the current device, so set for each call)
-  RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)));
-  RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-  count_launches(1);
   // One CTA where it has a warp for each 32 pairs; sixteen where the places' writes are
   // what counts (131072 pairs: a CTA's 32 scattered writes take an SM as many cycles).
   const long long pairs = (long long)a.rows * a.top_k;
+  // (attributes of the current device, so set for each call that needs them)
+  if (pairs > 16384)
+    RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  if (pairs > 16384 || smem > 40 * 1024)  // (up to 48 KB a launch has without asking)
+    RC_TRY(cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                int(most)));
+  count_launches(1);
   const int ctas = pairs <= 32 * SORT_WARPS ? 1 : pairs > 16384 && sixteen_fit(most) ? 16 : 8;
   return launch_k_cluster(sort_kernel, dim3(unsigned(ctas)), dim3(32 * SORT_WARPS), smem, ctas,
                           st, a);

@@ -606,15 +606,19 @@ norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
 }
 
 constexpr int SMS = 152;
+constexpr size_t ANY_SMEM = 40 * 1024;  // that a launch has without asking, beside the slots
 
 template <class TX, class TH, Form FORM, int THREADS>
 cudaError_t rows(const ResidualArgs& a, int threads, int ctas, cudaStream_t st) {
   const bool own_h = a.h && a.top_k == 0;
   const size_t smem = size_t(depth<TX, TH, THREADS>()) * ROWS * threads * 8 *
                       (sizeof(TX) + (own_h ? sizeof(TH) : 0));
-  // (an attribute of the current device, so set for each call)
-  RC_TRY(cudaFuncSetAttribute(norm_rows_kernel<TX, TH, FORM, THREADS>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+  // (an attribute of the current device, so set for each call that needs it; always to the
+  // same, for calls of several threads)
+  constexpr int most = depth<TX, TH, THREADS>() * ROWS * THREADS * 8 * (sizeof(TX) + sizeof(TH));
+  if (smem > ANY_SMEM)
+    RC_TRY(cudaFuncSetAttribute(norm_rows_kernel<TX, TH, FORM, THREADS>,
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, most));
   return launch_k(norm_rows_kernel<TX, TH, FORM, THREADS>,
                   dim3(unsigned(a.rows < SMS * ctas ? a.rows : SMS * ctas)),
                   dim3(unsigned(threads)), smem, st, a);

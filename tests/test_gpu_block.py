@@ -308,3 +308,47 @@ def test_the_readmes_block_of_experts_runs(lib):
     want, tol, _, _ = B.residual(x0, part.sum(1), 2 * B.F32_HALF * part.abs().sum(1), None, 1.0,
                                  none, none, None, None)
     B.close(x, want, tol, F32, "joined")
+
+
+def test_calls_of_several_threads(lib):
+    """Two host threads at once, each with its stream and its sizes of shared memory."""
+    import threading
+    R, ctx = lib
+    jobs = []
+    for cols, cols8 in ((1152, 256), (2304, 4608)):
+        x, h, y = (_rand(64, cols, seed=i) for i in range(3))
+        x8, W = R.Fp8Matrix(4, cols8), R.Fp8Matrix(2 * 128, cols8, 128)
+        R.rc_fp8_quantize(ctx, _rand(4, cols8, seed=4), cols8, R.RC_F32, x8)
+        R.rc_fp8_quantize(ctx, _rand(256, cols8, seed=5), cols8, R.RC_F32, W)
+        jobs.append(dict(op=R.ResidualNorm(cols, x=x, h=h, x_out=torch.empty_like(x), y=y,
+                                           pre=R.Norm(R.RC_NORM_RMS, 1e-6)), y=y, x8=x8, W=W,
+                         first=torch.tensor([0, 1, 4], dtype=torch.int32, device="cuda"),
+                         z=torch.zeros(4, 128, device="cuda"), stream=torch.cuda.Stream(),
+                         errors=[]))
+
+    def work(j, n):
+        try:
+            for _ in range(n):
+                R.rc_norm_residual(ctx, j["op"], j["stream"].cuda_stream)
+                R.rc_experts_linear(ctx, j["x8"], j["W"], None, 2, 128, j["first"], None, 4,
+                                    R.RC_ACT_GELU, j["z"], 128, R.RC_F32, None,
+                                    j["stream"].cuda_stream)
+        except Exception as e:  # noqa: BLE001
+            j["errors"].append(e)
+
+    torch.cuda.synchronize()
+    want = []
+    for j in jobs:
+        work(j, 1)
+        R.rc_sync(ctx)
+        want.append((j["y"].clone(), j["z"].clone()))
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(j, 300)) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    R.rc_sync(ctx)
+    for j, (y, z) in zip(jobs, want):
+        assert not j["errors"]
+        assert torch.equal(j["y"], y) and torch.equal(j["z"], z)
