@@ -287,21 +287,23 @@ __device__ __forceinline__ void pairs_of(const float* u, float2* v) {
   for (int k = 0; k < 4; ++k) v[k] = make_float2(u[2 * k], u[2 * k + 1]);
 }
 
-// FORM says what there is, with whole, aligned vectors: NEXT_BF16, NEXT_F32 x, h (without
-// places), x_out and y of that type; CODES x and y8 alone; JOIN x, h by places and x_out.
+// FORM says what there is, with whole, aligned vectors: NEXT x, h (without places), x_out
+// and y (of that type, or as codes); ONLY x and y alone; JOIN x, h by places and x_out.
 // ANY is everything else (the tests of what there is, for each vector, took half of the
-// instructions: 4128 x 1152 f32 to codes 8.4 us for 10.6, joined with two bf16 rows of
-// each by places, looked up once, 7.9 for 12.6).
-enum Form { ANY, NEXT_BF16, NEXT_F32, CODES, JOIN };
+// instructions: 4128 x 1152 bf16 to codes 8.4 us for 10.6, joined with two bf16 rows of
+// each by places, looked up once, 7.9 for 12.6; one row to bf16 3.3 for 4.1).
+enum Form { ANY, NEXT_BF16, NEXT_F32, NEXT_CODES, ONLY_BF16, ONLY_F32, ONLY_CODES, JOIN };
 // Places and weights that a CTA has in shared memory at once; RC_EXPERTS_MAX_TOP_K of a
 // row at most.
 constexpr int PAIRS = 512;
 template <class TX, class TH, Form FORM, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 2 : 1)
 norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
-  constexpr bool PLAIN = FORM != ANY, NEXT = FORM == NEXT_BF16 || FORM == NEXT_F32,
-                 MAY_JOIN = FORM == ANY || FORM == JOIN;
-  using TY = std::conditional_t<FORM == NEXT_F32, float, bf16>;
+  constexpr bool PLAIN = FORM != ANY, MAY_JOIN = FORM == ANY || FORM == JOIN,
+                 NEXT = FORM == NEXT_BF16 || FORM == NEXT_F32 || FORM == NEXT_CODES,
+                 ONLY = FORM == ONLY_BF16 || FORM == ONLY_F32 || FORM == ONLY_CODES,
+                 CODES = FORM == NEXT_CODES || FORM == ONLY_CODES;
+  using TY = std::conditional_t<FORM == NEXT_F32 || FORM == ONLY_F32, float, bf16>;
   constexpr int DEPTH = depth<TX, TH, THREADS>();
   extern __shared__ uint4 staged[];  // [DEPTH][ROWS][threads] of x, then of h
   __shared__ float slots[2][2][32];
@@ -359,7 +361,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll 1
   for (int i = 0; i < DEPTH * ROWS; ++i) fetch();
   TX* po = x_out + (long long)row * a.ldx_out + c;
-  const bool codes = FORM == ANY ? a.y8.codes != nullptr : FORM == CODES,
+  const bool codes = FORM == ANY ? a.y8.codes != nullptr : CODES,
              y_wide = a.y_f32 ? wide_rows(static_cast<float*>(a.y), a.ldy)
                                                   : wide_rows(static_cast<bf16*>(a.y), a.ldy);
   const int y_size = a.y_f32 ? 4 : 2;
@@ -372,7 +374,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
   while (row < last) {
     if (MAY_JOIN && top_k > 0 && row + ROWS > paired && paired < last) {
       __syncthreads();
-      pairs_from = row, paired = min(last, row + PAIRS / top_k);
+      pairs_from = row, paired = min(last, row + PAIRS / max(top_k, 1));
       for (int i = threadIdx.x; i < (paired - row) * top_k; i += step) {
         const long long pair = (long long)row * top_k + i;
         const int place = a.places[pair];
@@ -437,7 +439,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
       continue;
     }
     const float2 scale = f2_of(a.residual_scale);
-    if (PLAIN ? FORM != CODES : h != nullptr) {
+    if (PLAIN ? !ONLY : h != nullptr) {
 #pragma unroll 2
       for (int j = 0; j < top_k; ++j) {
         Eight<TH> e[ROWS];
@@ -474,7 +476,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[r][k] = f2_mul(v[r][k], scale);
     }
-    if (PLAIN ? FORM != CODES : x_out != nullptr) {
+    if (PLAIN ? !ONLY : x_out != nullptr) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
         if (r < rows && n > 0)
@@ -489,7 +491,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           v[r][k] = f2_fma(f2_mul(v[r][k], f2_of(root[r])), qa[k], qb[k]);
-        if constexpr (NEXT) {
+        if constexpr (PLAIN && !CODES) {
           if (n > 0) store(reinterpret_cast<TY*>(py + r * y_step), &v[r][0].x, 8, true);
           continue;
         }
@@ -643,12 +645,16 @@ cudaError_t go(const ResidualArgs& a, cudaStream_t st) {
   const bool x = a.cols % 8 == 0 && wide(a.x, a.ldx, sizeof(TX)),
              h = wide(a.h, a.ldh, sizeof(TH)), out = wide(a.x_out, a.ldx_out, sizeof(TX)),
              y = wide(a.y, a.ldy, a.y_f32 ? 4 : 2);
-  if (x && !a.h && !a.x_out && a.y8.codes) return of_form<TX, bf16, CODES>(a, threads, st);
+  if (x && !a.h && !a.x_out && (a.y8.codes || y))  // (h's type is of no consequence)
+    return a.y8.codes ? of_form<TX, bf16, ONLY_CODES>(a, threads, st)
+           : a.y_f32  ? of_form<TX, bf16, ONLY_F32>(a, threads, st)
+                      : of_form<TX, bf16, ONLY_BF16>(a, threads, st);
   if (x && h && out && a.top_k > 0 && !a.y && !a.y8.codes)
     return of_form<TX, TH, JOIN>(a, threads, st);
-  if (x && h && out && a.top_k == 0 && y)
-    return a.y_f32 ? of_form<TX, TH, NEXT_F32>(a, threads, st)
-                   : of_form<TX, TH, NEXT_BF16>(a, threads, st);
+  if (x && h && out && a.top_k == 0 && (a.y8.codes || y))
+    return a.y8.codes ? of_form<TX, TH, NEXT_CODES>(a, threads, st)
+           : a.y_f32  ? of_form<TX, TH, NEXT_F32>(a, threads, st)
+                      : of_form<TX, TH, NEXT_BF16>(a, threads, st);
   return of_form<TX, TH, ANY>(a, threads, st);
 }
 

@@ -232,6 +232,32 @@ def test_codes_are_those_of_the_f32_values(lib, rows, cols):
     assert bool((m.codes[rows:] == 0x55).all()) and bool((m.codes[:, cols:] == 0x55).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 1152), (3, 130), (2, 4608), (1030, 1152), (900, 2056),
+                                       (2, 9000)])
+@pytest.mark.parametrize("tx,th", [(BF, BF), (F32, BF), (BF, F32), (F32, F32)])
+def test_codes_beside_the_residual(lib, rows, cols, tx, th):
+    """The same x' and, of the same f32 values, codes as with another kind of y."""
+    R, ctx = lib
+    x, h = _rand(rows, cols, seed=3, scale=3.0).to(tx), _rand(rows, cols, seed=5).to(th)
+    off = torch.tensor([0, rows // 2, rows], dtype=torch.int32, device="cuda")
+    mod = _rand(2, 3 * cols, seed=6)
+    kw = dict(x=x, h=h, pre=R.Norm(R.RC_NORM_LAYER, 1e-6, _rand(cols, seed=4)), row_offsets=off,
+              post=R.Norm(R.RC_NORM_RMS, 1e-6), gate=mod[:, :cols],
+              scale=mod[:, cols:2 * cols], shift=mod[:, 2 * cols:])
+    y, m = torch.zeros(rows, cols, device="cuda"), R.Fp8Matrix(rows + 2, cols)
+    m.codes.fill_(0x55)
+    outs = [torch.zeros_like(x) for _ in range(2)]
+    R.rc_norm_residual(ctx, R.ResidualNorm(cols, x_out=outs[0], y=y, **kw))
+    R.rc_norm_residual(ctx, R.ResidualNorm(cols, x_out=outs[1], y=m, **kw))
+    want = R.Fp8Matrix(rows, cols)
+    R.rc_fp8_quantize(ctx, y, cols, R.RC_F32, want)
+    R.rc_sync(ctx)
+    assert torch.equal(outs[0], outs[1])
+    assert torch.equal(m.codes[:rows, :cols], want.codes[:, :cols])
+    assert torch.equal(m.scales[:, :rows], want.scales)
+    assert bool((m.codes[rows:] == 0x55).all()) and bool((m.codes[:, cols:] == 0x55).all())
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_what_is_not_finite_stays_in_its_row(lib, bad):
     R, ctx = lib
