@@ -352,3 +352,49 @@ def test_calls_of_several_threads(lib):
     for j, (y, z) in zip(jobs, want):
         assert not j["errors"]
         assert torch.equal(j["y"], y) and torch.equal(j["z"], z)
+
+
+def _far(rows, cols, ld, dtype):
+    """A matrix whose last rows lie beyond 2^31 elements."""
+    assert (rows - 1) * ld > 2 ** 31
+    buf = torch.empty((rows - 1) * ld + cols, dtype=dtype, device="cuda")
+    return buf.as_strided((rows, cols), (ld, 1))
+
+
+def test_offsets_beyond_32_bits(lib):
+    R, ctx = lib
+    ld, cols = 1_200_000_008, 128
+    near = _rand(3, cols, seed=1).to(BF)
+    for align in (0, 1):  # (whole vectors, and the general way)
+        x = _far(3, cols, ld - align, BF)
+        x.copy_(near)
+        outs = []
+        for t in (x, near.clone()):
+            y = torch.zeros(3, cols, device="cuda")
+            R.rc_norm_residual(ctx, R.ResidualNorm(cols, x=t, x_out=t, h=near, y=y,
+                                                   pre=R.Norm(R.RC_NORM_RMS, 1e-6)))
+            R.rc_rotary_apply(ctx, R.Rotary(64), t, t.stride(0), R.RC_BF16, 3, 2, 64, None, None,
+                              False, t, t.stride(0))
+            ids = torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+            w = torch.zeros(3, 4, device="cuda")
+            R.rc_experts_route(ctx, R.Routing(cols, 4), t, t.stride(0), R.RC_BF16, 3, None, ids, w)
+            R.rc_sync(ctx)
+            outs.append((t.clone(), y, ids, w))
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+        del x, outs, t, y
+
+
+@pytest.mark.parametrize("rows,ld", [(3, 1_200_000_008), (40, 60_000_000), (40, 60_000_001)])
+def test_experts_results_beyond_32_bits(lib, rows, ld):
+    R, ctx = lib
+    x, W = R.Fp8Matrix(rows, 200), R.Fp8Matrix(128, 200, 128)
+    R.rc_fp8_quantize(ctx, _rand(rows, 200, seed=1), 200, R.RC_F32, x)
+    R.rc_fp8_quantize(ctx, _rand(128, 200, seed=2), 200, R.RC_F32, W)
+    first = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    far, near = _far(rows, 100, ld, BF), torch.zeros(rows, 100, dtype=BF, device="cuda")
+    for y in (far, near):
+        R.rc_experts_linear(ctx, x, W, None, 1, 100, first, None, rows, R.RC_ACT_SILU, y,
+                            y.stride(0), R.RC_BF16)
+    R.rc_sync(ctx)
+    assert torch.equal(far, near)
