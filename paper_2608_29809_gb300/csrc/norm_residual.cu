@@ -290,7 +290,7 @@ __device__ __forceinline__ void pairs_of(const float* u, float2* v) {
 // FORM says what there is, with whole, aligned vectors: NEXT x, h (without places), x_out
 // and y (of that type, or as codes); ONLY x and y alone; JOIN x, h by places and x_out.
 // ANY is everything else (the tests of what there is, for each vector, took half of the
-// instructions: 4128 x 1152 bf16 to codes 8.4 us for 10.6, joined with two bf16 rows of
+// instructions: 4128 x 1152 bf16 to codes 7.1 us for 10.6, joined with two bf16 rows of
 // each by places, looked up once, 7.9 for 12.6; one row to bf16 3.3 for 4.1).
 enum Form { ANY, NEXT_BF16, NEXT_F32, NEXT_CODES, ONLY_BF16, ONLY_F32, ONLY_CODES, JOIN };
 // Places and weights that a CTA has in shared memory at once; RC_EXPERTS_MAX_TOP_K of a
@@ -628,7 +628,9 @@ cudaError_t rows(const ResidualArgs& a, int threads, int ctas, cudaStream_t st) 
 template <class TX, class TH, Form FORM>
 cudaError_t of_form(const ResidualArgs& a, int threads, cudaStream_t st) {
   // (CTAs that an SM holds at once, by their registers)
-  if (threads <= 256) return rows<TX, TH, FORM, 256>(a, threads, threads <= 160 ? 3 : 2, st);
+  constexpr bool ONLY = FORM == ONLY_BF16 || FORM == ONLY_F32 || FORM == ONLY_CODES;
+  if (threads <= 256)
+    return rows<TX, TH, FORM, 256>(a, threads, threads > 160 ? 2 : ONLY ? 4 : 3, st);
   return rows<TX, TH, FORM, 640>(a, threads, 1, st);
 }
 
