@@ -195,7 +195,7 @@ __device__ __forceinline__ void store_y(const ResidualArgs& a, long long row, in
 }
 
 // Rows of up to 8 columns a thread of the CTA (cols <= 5120).  A CTA takes neighbouring
-// rows, two at a time: their sums share barriers and shuffles, the next four are on
+// rows, two at a time: their sums share barriers and shuffles, the next two are on
 // their way into shared memory meanwhile, and what the columns' values are multiplied
 // with and added to (weights, biases and the item's modulation, folded into one factor
 // and one term for each of the two norms) stays in registers until the item changes.
@@ -203,7 +203,7 @@ __device__ __forceinline__ void store_y(const ResidualArgs& a, long long row, in
 // 4608 bf16 94 us, 6.4 TB/s; two instructions in three were tests and scalar
 // arithmetic before: 219 us, and a row for each 128 threads with its parameters
 // read anew 237), and by the first rows' way where a CTA has ten (4128 x 1152
-// f32 15.1 us for 8.4 of traffic; it was 27.4).
+// f32 14.1 us for 8.4 of traffic; it was 27.4).
 constexpr int ROWS = 2;
 // Sums of both rows over the CTA's threads: the lower sixteen lanes end up with the
 // first row's, the upper ones with the second's, of the warp and then of all warps.
@@ -277,11 +277,9 @@ __device__ __forceinline__ void stage(Eight<T>* to, const T* p, int n, bool wide
     *to = e;
   }
 }
-// Batches of rows of a CTA under way or in use.
-template <class TX, class TH, int THREADS>
-constexpr int depth() {
-  return THREADS > 256 && sizeof(TX) + sizeof(TH) == 8 ? 2 : 3;
-}
+// Batches of rows of a CTA under way or in use (4128 x 1152 f32 14.1 us; with three 15.2,
+// with four 16.1, as many CTAs on an SM: the first batch waits for all that is asked for).
+constexpr int DEPTH = 2;
 __device__ __forceinline__ void pairs_of(const float* u, float2* v) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) v[k] = make_float2(u[2 * k], u[2 * k + 1]);
@@ -290,8 +288,8 @@ __device__ __forceinline__ void pairs_of(const float* u, float2* v) {
 // FORM says what there is, with whole, aligned vectors: NEXT x, h (without places), x_out
 // and y (of that type, or as codes); ONLY x and y alone; JOIN x, h by places and x_out.
 // ANY is everything else (the tests of what there is, for each vector, took half of the
-// instructions: 4128 x 1152 bf16 to codes 7.1 us for 10.6, joined with two bf16 rows of
-// each by places, looked up once, 7.9 for 12.6; one row to bf16 3.3 for 4.1).
+// instructions: 4128 x 1152 bf16 to codes 7.0 us for 10.6, joined with two bf16 rows of
+// each by places, looked up once, 7.8 for 12.6; one row to bf16 3.3 for 4.1).
 enum Form { ANY, NEXT_BF16, NEXT_F32, NEXT_CODES, ONLY_BF16, ONLY_F32, ONLY_CODES, JOIN };
 // Places and weights that a CTA has in shared memory at once; RC_EXPERTS_MAX_TOP_K of a
 // row at most.
@@ -304,7 +302,6 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
                  ONLY = FORM == ONLY_BF16 || FORM == ONLY_F32 || FORM == ONLY_CODES,
                  CODES = FORM == NEXT_CODES || FORM == ONLY_CODES;
   using TY = std::conditional_t<FORM == NEXT_F32 || FORM == ONLY_F32, float, bf16>;
-  constexpr int DEPTH = depth<TX, TH, THREADS>();
   extern __shared__ uint4 staged[];  // [DEPTH][ROWS][threads] of x, then of h
   __shared__ float slots[2][2][32];
   __shared__ int place_of[MAY_JOIN ? PAIRS : 1];
@@ -613,11 +610,11 @@ constexpr size_t ANY_SMEM = 40 * 1024;  // that a launch has without asking, bes
 template <class TX, class TH, Form FORM, int THREADS>
 cudaError_t rows(const ResidualArgs& a, int threads, int ctas, cudaStream_t st) {
   const bool own_h = a.h && a.top_k == 0;
-  const size_t smem = size_t(depth<TX, TH, THREADS>()) * ROWS * threads * 8 *
+  const size_t smem = size_t(DEPTH) * ROWS * threads * 8 *
                       (sizeof(TX) + (own_h ? sizeof(TH) : 0));
   // (an attribute of the current device, so set for each call that needs it; always to the
   // same, for calls of several threads)
-  constexpr int most = depth<TX, TH, THREADS>() * ROWS * THREADS * 8 * (sizeof(TX) + sizeof(TH));
+  constexpr int most = DEPTH * ROWS * THREADS * 8 * (sizeof(TX) + sizeof(TH));
   if (smem > ANY_SMEM)
     RC_TRY(cudaFuncSetAttribute(norm_rows_kernel<TX, TH, FORM, THREADS>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, most));
