@@ -501,7 +501,10 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
         two = fmaxf(fminf(one, k), fmaxf(two, l));
         one = fmaxf(one, k);
       }
-      const float mine = a.group_best == 2 && two > -INFINITY ? one + two : one;
+      // (a sum of two of the lowest biases is beyond f32: the group is there all the same, and
+      // as close to another such as can be)
+      const float mine = one == -INFINITY ? one
+                         : fmaxf(a.group_best == 2 && two > -INFINITY ? one + two : one, -FLT_MAX);
       int rank = 0;
       for (int h = 0; h < a.groups; ++h) {
         const float v = __shfl_sync(~0u, mine, h * lanes);

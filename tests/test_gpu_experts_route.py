@@ -273,3 +273,22 @@ def test_captured(lib):
         assert all(torch.equal(a, b) for a, b in zip(got, (ids, w, off, src, at)))
         want = B.sort(ids.cpu(), 64)
         assert torch.equal(off.cpu(), want[0]) and torch.equal(src.cpu(), want[1])
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups", [(8, 4), (64, 8), (12, 4), (256, 32)])
+@pytest.mark.parametrize("value", [LOWEST, -LOWEST])
+def test_biases_at_the_ends_of_f32_mask_nothing(lib, score, experts, groups, value):
+    """Two of them add up to more than f32 holds; beside them groups that are masked."""
+    size = experts // groups
+    z = _rand(30, experts, seed=11)
+    z[3, :size] = -math.inf
+    z[4, size:2 * size] = -math.inf
+    z[5] = -math.inf
+    z[6, 1::size] = -math.inf
+    b = torch.full((experts,), value, device="cuda")
+    b[:size] = 0.25
+    for top in (1, 2, groups - 1):
+        for of_best in (1, 2):
+            _check(lib, z, score, min(16, 2 * size), bias=b, groups=groups, top=top,
+                   of_best=of_best)
