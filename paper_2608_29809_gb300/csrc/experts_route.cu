@@ -255,12 +255,29 @@ __device__ __forceinline__ void route_row(const RoutingArgs& a, long long row, i
     // neighbours in the order that f32 does not tell apart (but for equal ones)
     const float zi = id < 0 ? 0.f : logit(a.logits, sizeof(T) == 4, base + id);
     const float bi = a.bias && id >= 0 ? a.bias[id] : 0.f, v = id < 0 ? 0.f : of_key(value);
+    const auto near = [&](float vn, float bn) {
+      const float s = fminf(1.f, fmaxf(fabsf(v - bi), fabsf(vn - bn)) + 0x1p-22f);
+      return v - vn <= 2.f * score_error(a.score, s) + 0x1p-22f * fmaxf(fabsf(v), fabsf(vn));
+    };
     const int next = __shfl_down_sync(~0u, id, 1);
     const float zn = __shfl_down_sync(~0u, zi, 1), bn = __shfl_down_sync(~0u, bi, 1);
     const float vn = __shfl_down_sync(~0u, v, 1);
-    if (lane < a.top_k && id >= 0 && next >= 0 && !(zi == zn && bi == bn)) {
-      const float s = fminf(1.f, fmaxf(fabsf(v - bi), fabsf(vn - bn)) + 0x1p-22f);
-      close |= v - vn <= 2.f * score_error(a.score, s) + 0x1p-22f * fmaxf(fabsf(v), fabsf(vn));
+    const bool asked = lane < a.top_k && id >= 0 && next >= 0, equal = zi == zn && bi == bn;
+    close |= asked && !equal && near(vn, bn);
+    // where the last choice's neighbour is its equal, the first one behind that is not
+    bool tied = asked && equal && lane == a.top_k - 1;
+    while (__any_sync(~0u, tied && !close)) {
+      int other;
+      uint32_t v0;
+      pick(key, lane, 1, other, v0);
+      other = __shfl_sync(~0u, other, 0), v0 = __shfl_sync(~0u, v0, 0);
+      if (other < 0) break;
+      const float zo = logit(a.logits, sizeof(T) == 4, base + other);
+      const float bo = a.bias ? a.bias[other] : 0.f;
+      if (tied && !(zi == zo && bi == bo)) {
+        close |= near(of_key(v0), bo);
+        tied = false;
+      }
     }
     if (__any_sync(~0u, close)) id = choose_f64(z, a, lane, m, scratch);
   }

@@ -292,3 +292,21 @@ def test_biases_at_the_ends_of_f32_mask_nothing(lib, score, experts, groups, val
         for of_best in (1, 2):
             _check(lib, z, score, min(16, 2 * size), bias=b, groups=groups, top=top,
                    of_best=of_best)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("grouped", [False, True])
+@pytest.mark.parametrize("equal", [2, 3])
+@pytest.mark.parametrize("steps", [1, 2])
+def test_equal_experts_at_the_last_choice_hide_no_better_one(lib, score, grouped, equal, steps):
+    """Experts of one logit for the last place, and one a step of f32 above them behind."""
+    a = -0.5 - 6 * torch.rand(500, generator=torch.Generator().manual_seed(3))
+    z = torch.full((500, 12), -20.0)
+    z[:, 0] = 0.0
+    z[:, 1:1 + equal] = a[:, None]
+    z[:, 4] = (a.view(torch.int32) - steps).view(torch.float32)  # (towards zero)
+    kw = dict(groups=3, top=2, of_best=1) if grouped else {}
+    if grouped:  # (groups of three lanes: the general way)
+        z = z[:, :9]
+    assert bool((z[:, 4] > a).all())
+    _check(lib, z.contiguous().cuda(), score, 2, bias=torch.zeros(z.shape[1], device="cuda"), **kw)
