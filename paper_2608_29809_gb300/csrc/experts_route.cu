@@ -532,11 +532,13 @@ route_kernel(const __grid_constant__ RoutingArgs a) {
         const uint32_t k = group < a.groups ? key_of(mine) : 0u;
         const float other = of_key(max(warp_max(kept ? 0u : k), key_of(-FLT_MAX)));
         const float least = of_key(~warp_max(kept ? ~k : 0u));
-        // (sums of two values: at most twice their errors)
+        // (sums of two values: at most twice their errors; a lane without a group, or of a masked
+        // one, has nothing to add)
+        const float largest = fmaxf(one > -INFINITY ? fabsf(one) : 0.f,
+                                    two > -INFINITY ? fabsf(two) : 0.f);
         close = __any_sync(~0u, kept) &&
-                !(least - other > 4.f * score_error(a.score, most) +
-                                      0x1p-20f * fmaxf(fabsf(least), fabsf(other)) + 0x1p-20f *
-                                      fmaxf(fabsf(one), fabsf(two > -INFINITY ? two : 0.f)));
+                !(least - other > 4.f * score_error(a.score, most) + 0x1p-20f * largest +
+                                      0x1p-20f * fmaxf(fabsf(least), fabsf(other)));
         if (!softmax && __any_sync(~0u, close)) {
           kept = keep_group_f64(a, sizeof(T) == 4, row, lane, lanes, group, c, two);
           close = false;
