@@ -12,7 +12,9 @@
 // there once for the CTA.  Codes become f16 (exact) and go through the m16n8k16 MMA: a
 // product's order of columns is free, so each lane's 16 bytes are four such steps of
 // its own.  A block's sums, f32, are scaled and added up; runs and the activation are
-// joined in shared memory.
+// joined in shared memory.  A scale is kept as two powers of 2 of half the exponent: sums
+// times one of x's and of W's, and then times the others, pass the largest f32 on the way
+// only where the result does (x of 1e36 and W of 1e-36: either scale alone is too much).
 #include "../../include/regioncache.h"
 #include "block.h"
 #include "common.cuh"
@@ -35,6 +37,14 @@ __device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint
       "{%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The two powers of 2 whose product is a scale (NaN for 255), the larger one first for
+// x's and last for W's.
+__device__ __forceinline__ float2 scale_halves(int b, bool larger_first) {
+  if (b == 255) return make_float2(__uint_as_float(0x7fffffffu), 1.f);
+  const int lo = (b - 127) >> 1, hi = b - 127 - lo;
+  return make_float2(__uint_as_float(uint32_t(127 + (larger_first ? hi : lo)) << 23),
+                     __uint_as_float(uint32_t(127 + (larger_first ? lo : hi)) << 23));
 }
 // Sixteen codes of which the first `left` are columns into shared memory, zeros behind.
 __device__ __forceinline__ void copy_some(uint4* to, const uint8_t* from, int left) {
@@ -94,9 +104,9 @@ experts_few_kernel(const __grid_constant__ ExpertsArgs a, const __grid_constant_
   // another), their scales [block][row], W's [part][first, second 128 rows][block], sums
   uint4* ring = smem + warp * (DEPTH * BLOCK / 16) + lane;
   uint8_t* xs = reinterpret_cast<uint8_t*>(smem + WARPS * (DEPTH * BLOCK / 16));
-  float* sx = reinterpret_cast<float*>(xs + pl.kb * ROWS * 128);
-  float* sw = sx + pl.kb * ROWS;
-  float* sums = sw + 4 * pl.kb;
+  float2* sx = reinterpret_cast<float2*>(xs + pl.kb * ROWS * 128);
+  float2* sw = sx + pl.kb * ROWS;
+  float* sums = reinterpret_cast<float*>(sw + 4 * pl.kb);
 
   // (outputs behind the last read rows of the expert that are never written; its
   // matrix has them up to a multiple of 128)
@@ -152,17 +162,18 @@ experts_few_kernel(const __grid_constant__ ExpertsArgs a, const __grid_constant_
           else copy_some(at, from + c, cols - c);
         }
         for (int k = lane; k < pl.kb; k += 32)
-          sx[k * ROWS + r] = scale_value(a.x.scales[(long long)k * a.x.lds + row]);
+          sx[k * ROWS + r] = scale_halves(a.x.scales[(long long)k * a.x.lds + row], true);
       }
       for (int i = threadIdx.x; i < 2 * parts * pl.kb; i += THREADS) {
         const int k = i % pl.kb, which = i / pl.kb;  // [part][first, second]
-        sw[i] = scale_value(a.w.scales[(long long)k * a.w.lds +
-                                       w_row(which >> 1, which & 1 ? out_cols - 1 : 0) / 128]);
+        sw[i] = scale_halves(a.w.scales[(long long)k * a.w.lds +
+                                        w_row(which >> 1, which & 1 ? out_cols - 1 : 0) / 128],
+                             false);
       }
       __syncthreads();
     }
     const long long block0 = w_row(part, 0) / 128;
-    const float* f_of[2];
+    const float2* f_of[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       f_of[i] = sw + (2 * part + (w_row(part, r0 + 8 * i) / 128 != block0 ? 1 : 0)) * pl.kb;
@@ -198,14 +209,17 @@ experts_few_kernel(const __grid_constant__ ExpertsArgs a, const __grid_constant_
       }
       fetch();
       if (++slot == DEPTH) slot = 0;
-      const float f0 = f_of[0][kb], f1 = f_of[1][kb];
+      const float2 f[2] = {f_of[0][kb], f_of[1][kb]};
 #pragma unroll
       for (int j = 0; j < NT; ++j) {  // (the lane's rows 2 t, 2 t + 1 of each eight)
-        const float2 x = *reinterpret_cast<const float2*>(sx + kb * ROWS + 8 * j + 2 * t);
-        total[j][0] = fmaf((block[j][0][0] + block[j][1][0]) * x.x, f0, total[j][0]);
-        total[j][1] = fmaf((block[j][0][1] + block[j][1][1]) * x.y, f0, total[j][1]);
-        total[j][2] = fmaf((block[j][0][2] + block[j][1][2]) * x.x, f1, total[j][2]);
-        total[j][3] = fmaf((block[j][0][3] + block[j][1][3]) * x.y, f1, total[j][3]);
+        const float4 two = *reinterpret_cast<const float4*>(sx + kb * ROWS + 8 * j + 2 * t);
+        const float2 x[2] = {make_float2(two.x, two.y), make_float2(two.z, two.w)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float sum = block[j][0][i] + block[j][1][i];
+          total[j][i] = fmaf(sum * (x[i & 1].x * f[i >> 1].x), x[i & 1].y * f[i >> 1].y,
+                             total[j][i]);
+        }
       }
     }
     copy_wait<0>();
@@ -266,7 +280,7 @@ constexpr size_t MOST_SMEM = 227 * 1024;
 
 size_t smem_of(const ExpertsArgs& a, int rows, int warps) {
   const size_t kb = size_t(a.x.cols - 1) / 128 + 1, parts = a.act == RC_ACT_GATED_SILU ? 2 : 1;
-  return size_t(warps) * DEPTH * BLOCK + kb * (rows * 132 + 16) +
+  return size_t(warps) * DEPTH * BLOCK + kb * (rows * 136 + 32) +
          parts * warps * 16 * rows * sizeof(float);
 }
 // (codes are made 128 outputs at a time: the CTAs are fewer, and have more warps)

@@ -368,3 +368,21 @@ def test_captured_with_other_offsets(lib):
     limit = 1.13 * 513 * 2.0 ** -23 * mag + 2.0 ** -16 * _gelu(z).abs()
     limit = limit + 2.0 ** -8 * (_gelu(z).abs() + limit) + 1e-37
     assert bool(((got.cpu().double() - _gelu(z)).abs() <= limit).all())
+
+
+@pytest.mark.parametrize("shares", [[3, 0, 2], [20, 11], [200, 0, 300]])
+@pytest.mark.parametrize("up", [True, False])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_scales_far_from_one(lib, shares, up, act):
+    """x at one end of f32 and W as far towards the other: the same results."""
+    p = Problem(lib, torch.tensor(shares), 300, 90, act, scale=64.0)
+    xs, ws = p.x.scales.int(), p.W.scales.int()
+    assert int(xs.min()) > 0 and int(ws.min()) > 0
+    by = min(247 - int(xs.max()), int(ws.min()) - 1) if up else \
+        -min(int(xs.min()) - 1, 247 - int(ws.max()))
+    assert abs(by) > 105
+    p.x.scales.copy_((xs + by).to(torch.uint8))
+    p.W.scales.copy_((ws - by).to(torch.uint8))
+    p.check(F32)
+    p.check(BF)
+    p.check_codes()
