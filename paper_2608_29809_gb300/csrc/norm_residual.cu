@@ -224,8 +224,8 @@ __device__ __forceinline__ void sums(float (&v)[2], float (*slots)[2][32], int& 
   turn ^= 1;
 }
 // v - mean of the rows' columns, and 1 / root of each row; part = 1 / cols.  n of the
-// thread's columns are in the row and the others hold zeros; they do again, but where
-// vectors are WHOLE: then a thread without columns is of no consequence.
+// thread's columns are in the row and the others hold zeros; they do again (where vectors
+// are WHOLE, all or none are in the row).
 template <bool WHOLE>
 __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], float (&root)[2],
                                             int n, float cols, float part,
@@ -245,6 +245,7 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
       // the quotient s / cols (exact for a constant row)
       float m = s[r] * part;
       m = fmaf(fmaf(-m, cols, s[r]), part, m);
+      if (WHOLE && n <= 0) m = 0.f;  // (a large mean times a large root is no finite number)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float2 d = f2_add(v[r][k], f2_of(-m));
@@ -257,7 +258,7 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
     float2 t = f2_mul(v[r][0], v[r][0]);
 #pragma unroll
     for (int k = 1; k < 4; ++k) t = f2_fma(v[r][k], v[r][k], t);
-    s[r] = WHOLE && n <= 0 ? 0.f : t.x + t.y;
+    s[r] = t.x + t.y;
   }
   sums(s, slots, turn);
 #pragma unroll

@@ -322,3 +322,26 @@ def test_captured_and_on_another_stream(lib):
         R.rc_norm_residual(ctx, op)
     R.rc_sync(ctx, s)
     assert torch.equal(y, want) and torch.equal(x, want_x)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1000), (5, 1000), (3, 520), (2, 72), (2, 4616), (2, 77)])
+@pytest.mark.parametrize("out", ["f32", "bf16", "codes"])
+def test_large_constant_rows_beside_threads_without_columns(lib, rows, cols, out):
+    """The branch's layer norm is its bias; its differences from the mean are nothing, whatever the
+    mean times the root is.  (Sums of 2^115 are exact, and f32 holds 8191 of them.)"""
+    R, ctx = lib
+    x, h = _rand(rows, cols, seed=1), torch.full((rows, cols), 2.0 ** 115, device="cuda")
+    b = _rand(cols, seed=2)
+    x_out, m = torch.zeros_like(x), R.Fp8Matrix(rows, cols)
+    y = torch.zeros(rows, cols, dtype=BF if out == "bf16" else F32, device="cuda")
+    R.rc_norm_residual(ctx, R.ResidualNorm(
+        cols, x=x, h=h, x_out=x_out, y=m if out == "codes" else y,
+        post=R.Norm(R.RC_NORM_LAYER, 1e-12, None, b), pre=R.Norm(R.RC_NORM_LAYER, 1e-6)))
+    R.rc_sync(ctx)
+    assert torch.equal(x_out, x + b)
+    x1 = x.cpu().double() + b.cpu().double()
+    want, tol = B.norm("layer", 1e-6, None, None, x1, B.F32_HALF * x1.abs())
+    if out == "codes":
+        assert bool((m.scales != 255).all()) and bool(((m.codes[:, :cols] & 0x7f) != 0x7f).all())
+    else:
+        B.close(y, want, tol, y.dtype)
