@@ -151,7 +151,7 @@ __device__ __forceinline__ int item_of(const int* offsets, int n_items, int rows
 }
 // Offsets that are not in order are reported (one CTA).
 __device__ __forceinline__ void check_offsets(const ResidualArgs& a) {
-  for (int i = threadIdx.x; i < a.n_items; i += blockDim.x)
+  for (long long i = threadIdx.x; i < a.n_items; i += blockDim.x)
     if (a.row_offsets[i] < 0 || a.row_offsets[i] > a.row_offsets[i + 1] ||
         a.row_offsets[i + 1] > a.rows)
       atomicOr(a.err, DEVERR_COUNT);
@@ -325,14 +325,15 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
                                                DEPTH * ROWS * blockDim.x) + threadIdx.x;
   const int top_k = MAY_JOIN ? a.top_k : 0;
   const bool own_h = FORM == ANY ? h && top_k == 0 : NEXT;
-  // rows are staged in order, a group of copies for each; `to` and `at` are the places
+  // rows are staged in order, a group of copies for each (`left` of them are still to come;
+  // below 0: asked for behind the last, where there are none); `to` and `at` are the places
   // of the next to be staged and to be read (in rows of the CTA's threads)
   const int step = blockDim.x, places = DEPTH * ROWS * step;
-  int staged_to = row, to = 0, at = 0;
+  int left = last - row, to = 0, at = 0;
   const TX* px = x + (long long)row * a.ldx + c;
   const TH* ph = h + (long long)row * a.ldh + c;
   const auto fetch = [&] {
-    if (staged_to < last && n > 0) {
+    if (left > 0 && n > 0) {
       if (PLAIN) {
         stage(sx + to, px, 8, true);
         if (NEXT) stage(sh + to, ph, 8, true);
@@ -342,7 +343,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
       }
     }
     copy_commit();
-    ++staged_to;
+    --left;
     px += a.ldx, ph += a.ldh;
     to += step;
     if (to == places) to = 0;
@@ -370,9 +371,9 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
   int paired = row, pairs_from = row;  // rows whose places are in shared memory (-2: one
                                        // that there is not, of no consequence elsewhere)
   while (row < last) {
-    if (MAY_JOIN && top_k > 0 && row + ROWS > paired && paired < last) {
+    if (MAY_JOIN && top_k > 0 && paired - row < ROWS && paired < last) {
       __syncthreads();
-      pairs_from = row, paired = min(last, row + PAIRS / max(top_k, 1));
+      pairs_from = row, paired = row + min(last - row, PAIRS / max(top_k, 1));
       for (int i = threadIdx.x; i < (paired - row) * top_k; i += step) {
         const long long pair = (long long)row * top_k + i;
         const int place = a.places[pair];

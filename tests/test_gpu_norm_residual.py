@@ -345,3 +345,19 @@ def test_large_constant_rows_beside_threads_without_columns(lib, rows, cols, out
         assert bool((m.scales != 255).all()) and bool(((m.codes[:, :cols] & 0x7f) != 0x7f).all())
     else:
         B.close(y, want, tol, y.dtype)
+
+
+@pytest.mark.parametrize("top_k", [0, 1])
+def test_as_many_rows_as_there_can_be(lib, top_k):
+    """What is asked for ahead ends with the last row, where counting on would wrap."""
+    R, ctx = lib
+    rows = 2 ** 31 - 1
+    buf = torch.ones(rows + 64, dtype=BF, device="cuda")
+    buf[rows:] = 7.0
+    x = buf[:rows].view(rows, 1)
+    h = torch.full((1, 1) if top_k else (rows, 1), 3.0, dtype=BF, device="cuda")
+    kw = dict(places=torch.zeros(rows, 1, dtype=torch.int32, device="cuda"),
+              weights=torch.ones(rows, 1, device="cuda")) if top_k else {}
+    R.rc_norm_residual(ctx, R.ResidualNorm(1, x=x, h=h, x_out=x, residual_scale=2.0, **kw))
+    R.rc_sync(ctx)
+    assert bool((buf[:rows] == 5).all()) and bool((buf[rows:] == 7).all())
