@@ -361,3 +361,43 @@ def test_as_many_rows_as_there_can_be(lib, top_k):
     R.rc_norm_residual(ctx, R.ResidualNorm(1, x=x, h=h, x_out=x, residual_scale=2.0, **kw))
     R.rc_sync(ctx)
     assert bool((buf[:rows] == 5).all()) and bool((buf[rows:] == 7).all())
+
+
+@pytest.mark.parametrize("cols", [40, 129, 1000, 1152, 4608, 6000, 16384])
+def test_constant_rows_of_any_value(lib, cols):
+    """A layer norm of a constant row is its bias, whatever the sums' roundings."""
+    R, ctx = lib
+    c = torch.cat([torch.tensor([321.55563, 0.1, 1000.1, -77.77, 1e-3, 0.0, 16777215.0]),
+                   1000 * torch.rand(60, generator=torch.Generator().manual_seed(1))])
+    x = c[:, None].expand(-1, cols).contiguous().cuda()
+    b, y = _rand(cols, seed=2), torch.zeros(len(c), cols, device="cuda")
+    eps = 1e-6
+    R.rc_norm_residual(ctx, R.ResidualNorm(cols, x=x, y=y,
+                                           pre=R.Norm(R.RC_NORM_LAYER, eps, None, b)))
+    R.rc_sync(ctx)
+    # the mean is off by n / 32 + 16 roundings of c at most, its differences' mean by as many of
+    # that and four more; the root is 1 / sqrt(eps) at most
+    steps = (cols / 32 + 20) * B.F32_HALF
+    tol = c.double().abs()[:, None] * steps ** 2 / eps ** 0.5 + B.F32_HALF * b.cpu().double().abs()
+    off = (y.cpu().double() - b.cpu().double()).abs()
+    assert bool((off <= tol + 1e-30).all()), (off.amax(1) / tol.amax(1)).max()
+
+
+@pytest.mark.parametrize("cols", [40, 1000, 1152, 4608, 9000])
+@pytest.mark.parametrize("far", [300.0, -4096.0])
+def test_rows_far_from_zero(lib, cols, far):
+    """Differences from the mean of rows whose mean is large against them."""
+    R, ctx = lib
+    x = _rand(40, cols, seed=3) + far
+    y = torch.zeros_like(x)
+    R.rc_norm_residual(ctx, R.ResidualNorm(cols, x=x, y=y, pre=R.Norm(R.RC_NORM_LAYER, 1e-6)))
+    R.rc_sync(ctx)
+    v = x.cpu().double()
+    d = v - v.mean(1, keepdim=True)
+    r = 1 / torch.sqrt((d * d).mean(1, keepdim=True) + 1e-6)
+    # differences from a first mean, of numbers so close, are exact; their sums' and squares' sums
+    # are off by n / 32 + 16 roundings, and some more of the statistics and the result (the first
+    # mean's own error, below a fiftieth of the differences, in them)
+    tol = 1.1 * (cols / 32 + 32) * B.F32_HALF * ((d * r).abs() + d.abs().mean(1, keepdim=True) * r)
+    off = (y.cpu().double() - d * r).abs()
+    assert bool((off <= tol).all()), (off / tol).max()
