@@ -735,9 +735,11 @@ rc_status rc_norm_residual(rc_ctx* ctx, const rc_residual* op, rc_stream stream)
  *                       slow) / (fast - slow), cut to 0 .. 1: pairs that turn often
  *                       stay, slow ones are stretched;
  *     RC_ROTARY_RAMP    the same with k = 1 - (i - lo) / (hi - lo), cut to 0 .. 1,
- *                       where lo (rounded down, at least 0) and hi (up, at most
- *                       p - 1) are the indexes of pairs that turn fast and slow
- *                       times, and hi - lo counts as 0.001 at least; theta > 1.
+ *                       where lo (rounded down, at least 0) and hi (up) are the
+ *                       indexes of pairs that turn fast and slow times, and
+ *                       hi - lo counts as 0.001 at least; theta > 1.  With one
+ *                       axis, as YaRN has it, hi is at most rot - 1, so the ramp
+ *                       may end behind the last pair; with several, p - 1.
  *              fast > slow > 0 (in turns over native_length > 0) for the last two.
  *   amplitude  finite.
  * A plan holds a pair's turns a position as a fraction of 2^64: a position

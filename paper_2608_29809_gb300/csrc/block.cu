@@ -152,7 +152,9 @@ rc_status rc_rotary_plan(const rc_rotary_spec* s, rc_rotary* out) {
       lo = floor(n * log(s->native_length / (s->fast * two_pi)) / log(theta));
       hi = ceil(n * log(s->native_length / (s->slow * two_pi)) / log(theta));
       lo = fmax(lo, 0);
-      hi = fmin(hi, n - 1);
+      // (of one axis as YaRN's ramp, which may run out behind the last pair; an axis of several,
+      // for which there is no published ramp, ends with its own last pair)
+      hi = fmin(hi, p.axes == 1 ? p.rot - 1 : n - 1);
     }
     for (int i = 0; i < n; ++i) {
       double f = pow(theta, -double(i) / n), k = 1;

@@ -267,3 +267,26 @@ def test_wrappers_refuse_tensors_that_do_not_fit(R):
         R.Rotary(63)
     with pytest.raises(ValueError):
         R.Rotary(64, pairs=[8, 8, 8, 8])
+
+
+@pytest.mark.parametrize("rot,theta,native,fast", [
+    (128, 1e4, 4096.0, 32.0), (128, 1e4, 131072.0, 32.0), (36, 100.0, 4096.0, 64.0),
+    (64, 10.0, 65536.0, 4096.0), (2, 1e4, 4096.0, 8.0), (2, 2.0, 4096.0, 8.0),
+    (128, 5e5, 8192.0, 4.0)])
+def test_ramp_of_one_axis_is_the_published_one(R, rot, theta, native, fast):
+    """YaRN's: from the channel pair that turns `fast` times over the native length, rounded down,
+    to the one that turns once, rounded up, between 0 and the turned channels less one, which may
+    lie behind the last pair."""
+    p = R.Rotary(rot, theta, scaling=R.RC_ROTARY_RAMP, factor=8.0, native_length=native, fast=fast,
+                 slow=1.0)
+
+    def dim(turns):
+        return rot * math.log(native / (turns * 2 * math.pi)) / (2 * math.log(theta))
+
+    lo, hi = max(math.floor(dim(fast)), 0), min(math.ceil(dim(1.0)), rot - 1)
+    for i in range(rot // 2):
+        f = theta ** (-2 * i / rot)
+        stretched = min(max((i - lo) / (hi - lo if hi > lo else 0.001), 0.0), 1.0)
+        want = (f / 8.0 * stretched + f * (1 - stretched)) / (2 * math.pi)
+        # a few roundings of f64 (powers and quotients) and the last place of 2^-64
+        assert abs(p.c.turns[i] / 2.0 ** 64 - want) <= 32 * 2.0 ** -53 * want + 2.0 ** -63
