@@ -858,9 +858,10 @@ rc_status rc_experts_sort(rc_ctx* ctx, const int32_t* ids, int rows, int top_k, 
  * pairs 0 .. RC_EXPERTS_MAX_PAIRS,
  * (pairs / 128 + experts) * (n / 32 + 1) < 2^31 - 152.
  * The work is shared out on the host for even shares of the pairs; uneven ones
- * cost time, not results.  Activations are good to 2^-16 of themselves and 2^-31
- * of the sum.  Results are bit-identical from call to call.  One expert without
- * source is a plain quantised layer with its activation: offsets {0, rows}.
+ * cost time, not results.  Activations are good to 2^-15 of themselves, however
+ * small they are against the sum (below 2^-126 of it: 0).  Results are
+ * bit-identical from call to call.  One expert without source is a plain
+ * quantised layer with its activation: offsets {0, rows}.
  * Device checks: offsets that descend or leave 0 .. pairs (the expert is left
  * out) and a source outside x (taken as row 0) are reported.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_SHAPE. */

@@ -79,15 +79,6 @@ struct TypeOf<OUT_F32> { typedef float T; };
 template <>
 struct TypeOf<OUT_CODES> { typedef uint8_t T; };
 
-template <int N, bool GELU>
-__device__ __forceinline__ void activate(float* v) {
-#pragma unroll
-  for (int j = 0; j < N; j += 4) {
-    float2 a = make_float2(v[j], v[j + 1]), b = make_float2(v[j + 2], v[j + 3]);
-    over_one_plus(a, b, GELU ? gelu_power(a) : silu_power(a), GELU ? gelu_power(b) : silu_power(b));
-    v[j] = a.x, v[j + 1] = a.y, v[j + 2] = b.x, v[j + 3] = b.y;
-  }
-}
 // Sums with their bias (in shared memory, 16-byte aligned).
 template <int N>
 __device__ __forceinline__ void add_bias(float* v, const float* bias) {

@@ -386,3 +386,46 @@ def test_scales_far_from_one(lib, shares, up, act):
     p.check(F32)
     p.check(BF)
     p.check_codes()
+
+
+@pytest.mark.parametrize("pairs", [5, 300])
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_activations_far_below_zero(lib, pairs, act):
+    """Small results keep their bits, in each type."""
+    R, ctx = lib
+    n = 300
+    v = torch.linspace(-7.5, 2.0, n) if act == "gelu" else torch.linspace(-80.0, 2.0, n)
+    gated = act == "gated_silu"
+    b = torch.cat([v, torch.linspace(0.5, 2.0, n)]) if gated else v
+    x, W = R.Fp8Matrix(pairs, 128, 1), R.Fp8Matrix(640, 128, 128)
+    R.rc_fp8_quantize(ctx, _rand(pairs, 128, seed=1), 128, R.RC_F32, x)
+    R.rc_fp8_quantize(ctx, torch.zeros(640, 128, device="cuda"), 128, R.RC_F32, W)
+    m = R.Fp8Matrix(pairs, n)
+    outs = {t: torch.zeros(pairs, n, dtype=t, device="cuda") for t in (F32, BF)}
+    for t, y in list(outs.items()) + [(None, None)]:
+        R.rc_experts_linear(ctx, x, W, b.cuda()[None].contiguous(), 1, n,
+                            torch.tensor([0, pairs], dtype=torch.int32, device="cuda"), None,
+                            pairs, ACTS.index(act), y, n, R.RC_F32 if t is None else R.DTYPES[t],
+                            None if y is not None else m)
+    R.rc_sync(ctx)
+    u = v.double()
+    want = _gelu(u) if act == "gelu" else u * torch.sigmoid(u)
+    want = want * b[n:].double() if gated else want
+    # the power of 2 that is taken, at most 116 (61 with GELU), is off by two roundings of f32
+    # (five), and so is the result by 61 * 5 * 2^-24 of itself times log 2 at most; the powers'
+    # and reciprocals' few steps
+    tol = 2.0 ** -16 * want.abs()
+    for t, y in outs.items():
+        limit = tol + torch.finfo(t).eps / 2 * (want.abs() + tol) + 1e-37
+        bad = ~((y.cpu().double() - want).abs() <= limit)
+        assert not bool(bad.any()), (t, bad.nonzero()[:4].tolist(), y[bad.cuda()][:4])
+    for g in range(-(-n // 128)):
+        at = slice(128 * g, min(n, 128 * g + 128))
+        w = want[at]
+        scale = torch.exp2(m.scales[g].cpu().double() - 127)[:, None]
+        e = E.scale_exponent((w.abs().max() * torch.tensor([1 - 2.0 ** -16, 1 + 2.0 ** -16])))
+        assert bool(((scale >= 2.0 ** e[0]) & (scale <= 2.0 ** e[1])).all())
+        got = m.codes[:, at].cpu().view(E.F8).double() * scale
+        # half a step of e4m3: 2^-4 of the value, and of the least normal (2^-6) below it
+        limit = tol[at] + 2.0 ** -4 * (w.abs() + tol[at]) + 2.0 ** -10 * scale
+        assert bool(((got - w).abs() <= limit).all())
