@@ -429,3 +429,48 @@ def test_activations_far_below_zero(lib, pairs, act):
         # half a step of e4m3: 2^-4 of the value, and of the least normal (2^-6) below it
         limit = tol[at] + 2.0 ** -4 * (w.abs() + tol[at]) + 2.0 ** -10 * scale
         assert bool(((got - w).abs() <= limit).all())
+
+
+@pytest.mark.parametrize("shares,off", [
+    ([40, 0, 30], [0, 50, 30, 60]), ([40, 0, 30], [-1, 40, 40, 70]), ([40, 0, 30], [0, 40, 71, 71]),
+    ([40, 0, 30], [0, 2 ** 31 - 1, -2 ** 31, 70]), ([40, 0, 30], [70, 3, 2, 1]),
+    ([400, 0, 300], [10, 400, 701, 700]), ([400, 0, 300], [700, 20, 0, 500]),
+    ([3, 0, 2], [0, 4, 2, 3]), ([3, 0, 2], [-1, 3, 3, 5]), ([3, 0, 2], [0, 3, 6, 6]),
+    ([3, 0, 2], [1, 2, 2 ** 31 - 1, -2 ** 31]), ([3, 0, 2], [5, 1, 0, 4])])
+@pytest.mark.parametrize("gather", [True, False])
+def test_what_bad_offsets_leave(lib, shares, off, gather):
+    """Experts whose offsets are in order get their rows' results; the others' places, and those
+    of no expert, are left as they were."""
+    R, ctx = lib
+    p = Problem(lib, torch.tensor(shares), 200, 96, gather=gather)
+    off_t = torch.tensor(off, dtype=torch.int32)
+    y = torch.full((p.pairs, 96), 7.0, device="cuda")
+    m = R.Fp8Matrix(p.pairs, 96)
+    m.codes.fill_(0x55)
+    m.scales.fill_(0x33)
+    for call in ((y, 96, R.RC_F32, None), (None, 0, 0, m)):
+        p.call(*call, offsets=off_t)
+        with pytest.raises(R.RCError) as e:
+            R.rc_sync(ctx)
+        assert e.value.status == 6
+    xv = E.values(p.x.codes, p.x.scales, 1, 200)
+    wv = E.values(p.W.codes, p.W.scales, 128, 200).view(3, -1, 200)[:, :96]
+    of = [[] for _ in range(p.pairs)]
+    for e, (lo, hi) in enumerate(zip(off, off[1:])):
+        if 0 <= lo <= hi <= p.pairs:
+            for r in range(lo, hi):
+                of[r].append(e)
+    codes = E.values(m.codes, m.scales, 1, 96)
+    for r, experts in enumerate(of):
+        if not experts:
+            assert bool((y[r] == 7).all()) and bool((m.codes[r] == 0x55).all())
+            assert bool((m.scales[:, r] == 0x33).all())
+        elif len(experts) == 1:  # (a place of two experts: either's)
+            x, w, b = xv[p.source[r] if gather else r], wv[experts[0]], p.b[experts[0]].cpu()
+            want = w @ x + b.double()
+            # as of Problem: 201 additions
+            tol = 201 * 2.0 ** -23 * (w.abs() @ x.abs() + b.double().abs())
+            assert bool(((y[r].cpu().double() - want).abs() <= tol + 2.0 ** -24 * want.abs()).all())
+            # half a step of e4m3, of its least value with the scale a quarter of the largest's
+            limit = tol + 2.0 ** -4 * (want.abs() + tol) + 2.0 ** -10 * want.abs().max() / 112
+            assert bool(((codes[r] - want).abs() <= limit).all())
