@@ -412,7 +412,7 @@ def _handles(st):
         st["W18"] = R.Fp8Matrix.of(st["W1"], st["W1s"], cols, GROUP)
         st["W28"] = R.Fp8Matrix.of(st["W2"], st["W2s"], mlp, GROUP)
         st["n8"], st["u8"] = R.Fp8Matrix(rows, cols), R.Fp8Matrix(rows * k, mlp)
-        st["d"] = torch.zeros(rows * k, cols, dtype=torch.bfloat16, device=DEV)
+        st["d"] = torch.zeros(rows * k, cols, device=DEV)
         st["before"] = R.ResidualNorm(cols, x=st["xin"], y=st["n8"],
                                       pre=R.Norm(R.RC_NORM_RMS, EPS, st["nw"], None))
         st["after"] = R.ResidualNorm(cols, x=st["xin"], h=st["d"], places=st["places"],
@@ -453,7 +453,7 @@ def _run_own(st):
         R.rc_experts_linear(ctx, st["n8"], st["W18"], st["b1"], e, st["mlp"], st["first"],
                             st["source"], rows * k, st["act_"], None, 0, 0, st["u8"])
         R.rc_experts_linear(ctx, st["u8"], st["W28"], None, e, st["cols"], st["first"], None,
-                            rows * k, R.RC_ACT_NONE, st["d"], st["cols"], R.RC_BF16)
+                            rows * k, R.RC_ACT_NONE, st["d"], st["cols"], R.RC_F32)
         R.rc_norm_residual(ctx, st["after"])
         return st["xout"]
     R.rc_experts_linear(ctx, st["x8"], st["W8"], st["b"], st["experts"], st["n"], st["first"],
