@@ -6,8 +6,6 @@
 #include "common.cuh"
 #include "fp8.cuh"
 
-#include <float.h>
-
 #include <type_traits>
 
 namespace rc {
@@ -16,12 +14,12 @@ namespace {
 
 // A row is dealt in vectors of eight columns to a CTA's threads, which hold them from
 // the first load to the last store, so x and h are read once; the sums of a norm go
-// through the registers that hold the row.  Its variance is that of the differences d from
-// the mean, two passes there; the first pass' sum is rounded, so the second takes the sum
-// of d beside that of their squares, and their own mean e comes off both: (d - e) and
-// mean(d^2) - e^2.  What is left of a mean's error is its error's rounding (a constant row
-// of 321.55563 gave 0.03 of a root of 1e-3 without).  Sixteen neighbouring threads hold the
-// 128 columns of a scale.
+// through the registers that hold the row (its variance is that of the differences
+// from the mean, two passes there).  A mean m is as good as its sum, so the differences d
+// may be off by some 2^-24 m, which is nothing to them while |m| is at most their root mean
+// square.  Rows with a larger mean go through both passes once more (a constant row of
+// 321.55563 gave 0.03 of a root of 1e-3 without).  The mean of d taken off every row, beside
+// the squares, cost 16 % (16384 x 4608 bf16, layer norm alone, 74 us; now 66).  Sixteen neighbouring threads hold the 128 columns of a scale.
 __device__ __forceinline__ void unpack(const Eight<bf16>& e, float* v) {
   const uint32_t w[4] = {e.u.x, e.u.y, e.u.z, e.u.w};
 #pragma unroll
@@ -76,7 +74,7 @@ __device__ __forceinline__ void store(float* p, const float* v, int n, bool wide
 // Sum over the row's threads; `slots` of the CTA's warps, used in turn so that one
 // barrier a sum is enough.
 template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float (*slots)[32], int& turn) {
+__device__ __forceinline__ float row_sum(float v, float (*slots)[16], int& turn) {
   v = warp_sum(v);
   const int warp = threadIdx.x >> 5;
   if ((threadIdx.x & 31) == 0) slots[turn][warp] = v;
@@ -88,64 +86,40 @@ __device__ __forceinline__ float row_sum(float v, float (*slots)[32], int& turn)
   return v;
 }
 
-// Two sums behind one barrier.
-template <int TPR>
-__device__ __forceinline__ float2 row_sums(float v, float w, float (*slots)[32], int& turn) {
-  v = warp_sum(v), w = warp_sum(w);
-  float* own = slots[turn];
-  const int warp = threadIdx.x >> 5;
-  if ((threadIdx.x & 31) == 0) own[warp] = v, own[16 + warp] = w;
-  __syncthreads();
-  v = w = 0.f;
-#pragma unroll
-  for (int i = 0; i < TPR / 32; ++i) v += own[i], w += own[16 + i];
-  turn ^= 1;
-  return make_float2(v, w);
-}
-// The mean e of differences from nearly the mean (of those whose sum passes f32: none), and
-// their variance by that and the mean of their squares (beyond f32 it stays infinite).
-__device__ __forceinline__ float variance(float square, float& e) {
-  if (!(fabsf(e) <= FLT_MAX)) e = 0.f;
-  return square <= FLT_MAX ? fmaxf(fmaf(-e, e, square), 0.f) : square;
+// Whether the row's mean is large against what is left of it (the same for all threads).
+__device__ __forceinline__ bool far_from_zero(float mean, float root) {
+  return fabsf(mean) * root > 1.f;
 }
 
 template <int TPR, int NV>
 __device__ __forceinline__ void normalise(const NormOf& o, float (*v)[8], int t, int cols,
-                                          float (*slots)[32], int& turn) {
+                                          float (*slots)[16], int& turn) {
   if (o.kind == RC_NORM_NONE) return;
-  const bool layer = o.kind == RC_NORM_LAYER;
-  float mean = 0.f, sum = 0.f, rest = 0.f, var;
-  if (layer) {
+  float r;
+#pragma unroll 1
+  for (bool again = o.kind == RC_NORM_LAYER, first = true;; first = false) {
+    float mean = 0.f, sum = 0.f;
+    if (again) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum += v[i][k];
-    mean = row_sum<TPR>(sum, slots, turn) / float(cols);
-    sum = 0.f;
-  }
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int n = cols - (t + i * TPR) * 8;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      v[i][k] = k < n ? v[i][k] - mean : 0.f;
-      rest += v[i][k];
-      sum = fmaf(v[i][k], v[i][k], sum);
+        for (int k = 0; k < 8; ++k) sum += v[i][k];
+      mean = row_sum<TPR>(sum, slots, turn) / float(cols);
+      sum = 0.f;
     }
-  }
-  if (layer) {
-    const float2 both = row_sums<TPR>(rest, sum, slots, turn);
-    rest = both.x / float(cols);
-    var = variance(both.y / float(cols), rest);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      const int n = cols - (t + i * TPR) * 8;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)  // (columns outside the row are not written)
-        v[i][k] -= k < cols - (t + i * TPR) * 8 ? rest : 0.f;
-  } else {
-    var = row_sum<TPR>(sum, slots, turn) / float(cols);
+      for (int k = 0; k < 8; ++k) {
+        v[i][k] = k < n ? v[i][k] - mean : 0.f;
+        sum = fmaf(v[i][k], v[i][k], sum);
+      }
+    }
+    r = 1.f / sqrtf(row_sum<TPR>(sum, slots, turn) / float(cols) + o.eps);
+    again = again && first && far_from_zero(mean, r);
+    if (!again) break;
   }
-  const float r = 1.f / sqrtf(var + o.eps);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (t + i * TPR) * 8, n = cols - c;
@@ -247,7 +221,7 @@ __device__ __forceinline__ void store_y(const ResidualArgs& a, long long row, in
 constexpr int ROWS = 2;
 // Sums of both rows over the CTA's threads: the lower sixteen lanes end up with the
 // first row's, the upper ones with the second's, of the warp and then of all warps.
-__device__ __forceinline__ void sums(float (&v)[2], float (*slots)[4][32], int& turn) {
+__device__ __forceinline__ void sums(float (&v)[2], float (*slots)[2][32], int& turn) {
   const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15;
   float s = half ? v[1] : v[0];
   s += __shfl_xor_sync(0xffffffffu, half ? v[0] : v[1], 16);
@@ -263,76 +237,52 @@ __device__ __forceinline__ void sums(float (&v)[2], float (*slots)[4][32], int& 
   v[0] = half ? other : s, v[1] = half ? s : other;
   turn ^= 1;
 }
-// The same of four values, a quarter of the lanes for each.
-__device__ __forceinline__ void sums(float (&v)[4], float (*slots)[4][32], int& turn) {
-  const int lane = threadIdx.x & 31, quarter = lane >> 3, l = lane & 7;
-  const bool upper = lane & 16, odd = lane & 8;
-  float s = upper ? v[2] : v[0], t = upper ? v[3] : v[1];
-  s += __shfl_xor_sync(0xffffffffu, upper ? v[0] : v[2], 16);
-  t += __shfl_xor_sync(0xffffffffu, upper ? v[1] : v[3], 16);
-  const float mine = odd ? t : s;
-  s = mine + __shfl_xor_sync(0xffffffffu, odd ? s : t, 8);
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (l == 0) slots[turn][quarter][threadIdx.x >> 5] = s;
-  __syncthreads();
-  const float* of = slots[turn][quarter] + l;
-  s = (of[0] + of[8]) + (of[16] + of[24]);
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(0xffffffffu, s, 8 * i);
-  turn ^= 1;
-}
 // v - mean of the rows' columns, and 1 / root of each row; part = 1 / cols.  n of the
 // thread's columns are in the row and the others hold zeros; they do again (where vectors
 // are WHOLE, all or none are in the row).
 template <bool WHOLE>
 __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], float (&root)[2],
                                             int n, float cols, float part,
-                                            float (*slots)[4][32], int& turn) {
+                                            float (*slots)[2][32], int& turn) {
   root[0] = root[1] = 1.f;
   if (o.kind == RC_NORM_NONE) return;
-  const auto sum = [](const float2 (&u)[4]) {
-    const float2 t = f2_add(f2_add(u[0], u[1]), f2_add(u[2], u[3]));
-    return t.x + t.y;
-  };
-  const auto squares = [](const float2 (&u)[4]) {
-    float2 t = f2_mul(u[0], u[0]);
+  float s[2];
+#pragma unroll 1
+  for (bool again = o.kind == RC_NORM_LAYER, first = true;; first = false) {
+    float m[2] = {0.f, 0.f};
+    if (again) {
 #pragma unroll
-    for (int k = 1; k < 4; ++k) t = f2_fma(u[k], u[k], t);
-    return t.x + t.y;
-  };
-  if (o.kind == RC_NORM_RMS) {
-    float s[2] = {squares(v[0]), squares(v[1])};
+      for (int r = 0; r < 2; ++r) {
+        const float2 t = f2_add(f2_add(v[r][0], v[r][1]), f2_add(v[r][2], v[r][3]));
+        s[r] = t.x + t.y;
+      }
+      sums(s, slots, turn);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        m[r] = s[r] * part;
+        m[r] = fmaf(fmaf(-m[r], cols, s[r]), part, m[r]);  // (the quotient s / cols)
+        // (a large mean times a large root is no finite number)
+        const float of = WHOLE && n <= 0 ? 0.f : m[r];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 d = f2_add(v[r][k], f2_of(-of));
+          v[r][k] = WHOLE ? d : make_float2(2 * k < n ? d.x : 0.f, 2 * k + 1 < n ? d.y : 0.f);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float2 t = f2_mul(v[r][0], v[r][0]);
+#pragma unroll
+      for (int k = 1; k < 4; ++k) t = f2_fma(v[r][k], v[r][k], t);
+      s[r] = t.x + t.y;
+    }
     sums(s, slots, turn);
 #pragma unroll
     for (int r = 0; r < 2; ++r) root[r] = rsqrtf(fmaf(s[r], part, o.eps));
-    return;
-  }
-  const auto less = [&](float2 (&u)[4], float m) {
-    if (WHOLE && n <= 0) m = 0.f;  // (a large mean times a large root is no finite number)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 d = f2_add(u[k], f2_of(-m));
-      u[k] = WHOLE ? d : make_float2(2 * k < n ? d.x : 0.f, 2 * k + 1 < n ? d.y : 0.f);
-    }
-  };
-  float s[2] = {sum(v[0]), sum(v[1])}, t[4];
-  sums(s, slots, turn);
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    float m = s[r] * part;
-    m = fmaf(fmaf(-m, cols, s[r]), part, m);  // (the quotient s / cols)
-    less(v[r], m);
-    t[r] = sum(v[r]), t[2 + r] = squares(v[r]);
-  }
-  sums(t, slots, turn);
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    float e = t[r] * part;
-    root[r] = rsqrtf(variance(t[2 + r] * part, e) + o.eps);
-    less(v[r], e);
+    again = again && first &&
+            (far_from_zero(m[0], root[0]) || far_from_zero(m[1], root[1]));
+    if (!again) break;
   }
 }
 // A thread's eight (n) columns of a row into its place in shared memory: under way,
@@ -375,10 +325,10 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
                  CODES = FORM == NEXT_CODES || FORM == ONLY_CODES;
   using TY = std::conditional_t<FORM == NEXT_F32 || FORM == ONLY_F32, float, bf16>;
   extern __shared__ uint4 staged[];  // [DEPTH][ROWS][threads] of x, then of h
-  __shared__ float slots[2][4][32];
+  __shared__ float slots[2][2][32];
   __shared__ int place_of[MAY_JOIN ? PAIRS : 1];
   __shared__ float weight_of[MAY_JOIN ? PAIRS : 1];
-  for (int i = threadIdx.x; i < 256; i += blockDim.x) (&slots[0][0][0])[i] = 0.f;
+  for (int i = threadIdx.x; i < 128; i += blockDim.x) (&slots[0][0][0])[i] = 0.f;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
@@ -582,7 +532,7 @@ norm_rows_kernel(const __grid_constant__ ResidualArgs a) {
 template <class TX, class TH, int TPR, int NV>
 __global__ void __launch_bounds__(TPR)
 norm_residual_kernel(const __grid_constant__ ResidualArgs a) {
-  __shared__ float slots[2][32];
+  __shared__ float slots[2][16];
   pdl_wait();
   pdl_trigger();
   const int t = threadIdx.x;
