@@ -246,11 +246,13 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
                                             float (*slots)[2][32], int& turn) {
   root[0] = root[1] = 1.f;
   if (o.kind == RC_NORM_NONE) return;
+  const bool layer = o.kind == RC_NORM_LAYER;
+  bool far[2] = {layer, layer};
   float s[2];
 #pragma unroll 1
-  for (bool again = o.kind == RC_NORM_LAYER, first = true;; first = false) {
+  for (bool first = true;; first = false) {
     float m[2] = {0.f, 0.f};
-    if (again) {
+    if (layer) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float2 t = f2_add(f2_add(v[r][0], v[r][1]), f2_add(v[r][2], v[r][3]));
@@ -261,8 +263,9 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
       for (int r = 0; r < 2; ++r) {
         m[r] = s[r] * part;
         m[r] = fmaf(fmaf(-m[r], cols, s[r]), part, m[r]);  // (the quotient s / cols)
-        // (a large mean times a large root is no finite number)
-        const float of = WHOLE && n <= 0 ? 0.f : m[r];
+        // (a large mean times a large root is no finite number; a row does not hang on its
+        // neighbour, which may be none)
+        const float of = (WHOLE && n <= 0) || !far[r] ? 0.f : m[r];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float2 d = f2_add(v[r][k], f2_of(-of));
@@ -280,9 +283,9 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
     sums(s, slots, turn);
 #pragma unroll
     for (int r = 0; r < 2; ++r) root[r] = rsqrtf(fmaf(s[r], part, o.eps));
-    again = again && first &&
-            (far_from_zero(m[0], root[0]) || far_from_zero(m[1], root[1]));
-    if (!again) break;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) far[r] = first && far_from_zero(m[r], root[r]);
+    if (!far[0] && !far[1]) break;
   }
 }
 // A thread's eight (n) columns of a row into its place in shared memory: under way,

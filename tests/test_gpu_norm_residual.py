@@ -405,3 +405,25 @@ def test_rows_far_from_zero(lib, cols, far):
     tol = 1.1 * (cols / 32 + 32) * B.F32_HALF * ((d * r).abs() + d.abs().mean(1, keepdim=True) * r)
     off = (y.cpu().double() - d * r).abs()
     assert bool((off <= tol).all()), (off / tol).max()
+
+
+@pytest.mark.parametrize("cols", [72, 77, 1152, 4616])
+@pytest.mark.parametrize("far", [1e4, math.nan, math.inf])
+def test_rows_do_not_hang_on_their_neighbours(lib, cols, far):
+    """A row gets the same bits alone, beside another, and beside one whose mean is far off."""
+    R, ctx = lib
+    n = R.Norm(R.RC_NORM_LAYER, 1e-6)
+    rows = _rand(6, cols, seed=4) * torch.tensor([1, 1, 3, 0.01, 1, 1], device="cuda")[:, None]
+    rows[4] += 2.0  # (itself one of a large mean)
+    want = torch.zeros_like(rows)
+    for i in range(6):
+        R.rc_norm_residual(ctx, R.ResidualNorm(cols, x=rows[i:i + 1], y=want[i:i + 1], pre=n))
+    for before in (0, 1):
+        x = torch.cat([rows.new_full((before, cols), far), rows.repeat_interleave(2, 0)])
+        x[before + 1::2] = x[before + 1::2] + far
+        x = x.repeat(300, 1)  # (of which a CTA takes several)
+        y = torch.zeros_like(x)
+        R.rc_norm_residual(ctx, R.ResidualNorm(cols, x=x, y=y, pre=n))
+        R.rc_sync(ctx)
+        got = y.view(300, 12 + before, cols)[:, before::2]
+        assert torch.equal(got, want.expand_as(got))
