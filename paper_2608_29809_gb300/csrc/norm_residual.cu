@@ -246,33 +246,8 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
                                             float (*slots)[2][32], int& turn) {
   root[0] = root[1] = 1.f;
   if (o.kind == RC_NORM_NONE) return;
-  const bool layer = o.kind == RC_NORM_LAYER;
-  bool far[2] = {layer, layer};
   float s[2];
-#pragma unroll 1
-  for (bool first = true;; first = false) {
-    float m[2] = {0.f, 0.f};
-    if (layer) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float2 t = f2_add(f2_add(v[r][0], v[r][1]), f2_add(v[r][2], v[r][3]));
-        s[r] = t.x + t.y;
-      }
-      sums(s, slots, turn);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        m[r] = s[r] * part;
-        m[r] = fmaf(fmaf(-m[r], cols, s[r]), part, m[r]);  // (the quotient s / cols)
-        // (a large mean times a large root is no finite number; a row does not hang on its
-        // neighbour, which may be none)
-        const float of = (WHOLE && n <= 0) || !far[r] ? 0.f : m[r];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 d = f2_add(v[r][k], f2_of(-of));
-          v[r][k] = WHOLE ? d : make_float2(2 * k < n ? d.x : 0.f, 2 * k + 1 < n ? d.y : 0.f);
-        }
-      }
-    }
+  const auto roots = [&] {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       float2 t = f2_mul(v[r][0], v[r][0]);
@@ -283,9 +258,38 @@ __device__ __forceinline__ void standardise(const NormOf& o, float2 (&v)[2][4], 
     sums(s, slots, turn);
 #pragma unroll
     for (int r = 0; r < 2; ++r) root[r] = rsqrtf(fmaf(s[r], part, o.eps));
+  };
+  if (o.kind == RC_NORM_RMS) {
+    roots();
+    return;
+  }
+  bool far[2] = {true, true};
+#pragma unroll 1
+  for (bool first = true;; first = false) {
+    float m[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float2 t = f2_add(f2_add(v[r][0], v[r][1]), f2_add(v[r][2], v[r][3]));
+      s[r] = t.x + t.y;
+    }
+    sums(s, slots, turn);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      m[r] = s[r] * part;
+      m[r] = fmaf(fmaf(-m[r], cols, s[r]), part, m[r]);  // (the quotient s / cols)
+      // (a large mean times a large root is no finite number; a row does not hang on its
+      // neighbour, which may be none)
+      const float of = (WHOLE && n <= 0) || !far[r] ? 0.f : m[r];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 d = f2_add(v[r][k], f2_of(-of));
+        v[r][k] = WHOLE ? d : make_float2(2 * k < n ? d.x : 0.f, 2 * k + 1 < n ? d.y : 0.f);
+      }
+    }
+    roots();
 #pragma unroll
     for (int r = 0; r < 2; ++r) far[r] = first && far_from_zero(m[r], root[r]);
-    if (!far[0] && !far[1]) break;
+    if (!far[0] && !far[1]) return;
   }
 }
 // A thread's eight (n) columns of a row into its place in shared memory: under way,
