@@ -2,7 +2,7 @@
 // experts have a few rows each and there are few of them: latency is all that counts,
 // to which the tensor core of experts_linear.cu, fed by way of shared and tensor
 // memory, adds (a block of one token: 9.5 and 10.5 us for its two products of 5 MB
-// each; here 8.1 and 6.5, most of them a chain of round trips: offsets, source, x and
+// each; here 8.1 and 6.6, most of them a chain of round trips: offsets, source, x and
 // scales, blocks of W, the join).
 //
 // A CTA's warps take up to ROWS rows of an expert and CW tiles of 16 of its outputs, the

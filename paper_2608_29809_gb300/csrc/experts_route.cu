@@ -400,7 +400,7 @@ route_any_kernel(const __grid_constant__ RoutingArgs a) {
 // choice are, are left to route_row when the others are done (f64 of all experts: 12 us
 // for one row).  A warp keeps the bias and takes several rows, the next one's logits
 // under way.  (All rows as route_row does them: 16384 rows of 256, sigmoid, groups, 8
-// each, 48 us, 1700 instructions a row; now 21.7, 970.)
+// each, 48 us, 1700 instructions a row; now 22.1, 970.)
 template <int PER>
 constexpr int ROUTE_CTAS = PER <= 4 ? 8 : PER == 8 ? 6 : PER == 16 ? 4 : 2;  // of an SM
 template <class T, int PER>

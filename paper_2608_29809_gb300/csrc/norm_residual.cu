@@ -217,7 +217,7 @@ __device__ __forceinline__ void store_y(const ResidualArgs& a, long long row, in
 // 4608 bf16 94 us, 6.4 TB/s; two instructions in three were tests and scalar
 // arithmetic before: 219 us, and a row for each 128 threads with its parameters
 // read anew 237), and by the first rows' way where a CTA has ten (4128 x 1152
-// f32 14.1 us for 8.4 of traffic; it was 27.4).
+// f32 14.3 us for 8.4 of traffic; it was 27.4).
 constexpr int ROWS = 2;
 // Sums of both rows over the CTA's threads: the lower sixteen lanes end up with the
 // first row's, the upper ones with the second's, of the warp and then of all warps.
@@ -306,7 +306,7 @@ __device__ __forceinline__ void stage(Eight<T>* to, const T* p, int n, bool wide
     *to = e;
   }
 }
-// Batches of rows of a CTA under way or in use (4128 x 1152 f32 14.1 us; with three 15.2,
+// Batches of rows of a CTA under way or in use (4128 x 1152 f32 14.3 us; with three 15.2,
 // with four 16.1, as many CTAs on an SM: the first batch waits for all that is asked for).
 constexpr int DEPTH = 2;
 __device__ __forceinline__ void pairs_of(const float* u, float2* v) {
@@ -654,7 +654,9 @@ cudaError_t rows(const ResidualArgs& a, int threads, int ctas, cudaStream_t st) 
 }
 template <class TX, class TH, Form FORM>
 cudaError_t of_form(const ResidualArgs& a, int threads, cudaStream_t st) {
-  // (CTAs that an SM holds at once, by their registers)
+  // (CTAs of an SM: what it holds at once, by their registers, of 160 threads, for 1152
+  // columns.  Narrower rows, of a warp or two, could have more and run as few: 524288 x 128
+  // bf16, alone, 190 us where 268 MB take 40.)
   constexpr bool ONLY = FORM == ONLY_BF16 || FORM == ONLY_F32 || FORM == ONLY_CODES;
   if (threads <= 256)
     return rows<TX, TH, FORM, 256>(a, threads, threads > 160 ? 2 : ONLY ? 4 : 3, st);

@@ -12,7 +12,7 @@ namespace {
 // cos and sin of a place within the turn (a fraction of 2^64).  The nearest
 // quarter turn comes off in integers, so nothing is lost; on what is left, at
 // most an eighth of a turn, the Taylor series up to the 10th (cos) and 9th
-// degree (sin): the next terms are below 2^-33 and 2^-29 of the result.
+// degree (sin): the next terms are below 2^-32 and 2^-28 of the result.
 __device__ __forceinline__ float2 cos_sin(uint64_t place) {
   const uint32_t quarter = uint32_t((place + (uint64_t(1) << 61)) >> 62) & 3u;
   const long long rest = (long long)(place - (uint64_t(quarter) << 62));
@@ -44,9 +44,10 @@ __device__ __forceinline__ void put(bf16& to, float v) { to = f2bf(v); }
 // heads) go to shared memory, then a thread takes the same unit of one head after
 // another.  In a head, units 0 .. pair_units - 1 are turned: with HALF W channels
 // and the W that are rot / 2 further, with PAIRS W neighbours (W = 1: a pair); the
-// others are W channels that are only copied.  Bound by memory: 16384 rows of 32 x 72,
-// pairs, two axes, 30.7 us where 151 MB take 22 (a unit of eight bytes found by two
-// divisions: 33; the next unit loaded before this one is turned: 36).
+// others are W channels that are only copied.  Bound by memory,
+// and by a CTA's start, whose first loads wait for the cosines: 16384 rows of 32 x 72, pairs,
+// two axes, 31.0 us where 151 MB take 22, 4096 CTAs, 1216 at once (a unit of eight bytes
+// found by two divisions: 33; the next unit loaded before this one is turned: 36).
 template <class T, int W, bool HALF>
 __global__ void __launch_bounds__(256)
 rotary_kernel(const __grid_constant__ RotaryArgs a) {
